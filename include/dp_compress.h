@@ -677,6 +677,190 @@ int dp_tensor_head_grad_f64(const double *T, const double *a, const double *dA, 
 int dp_tensor_head_grad_f32(const float *T, const float *a, const float *dA, int64_t nloc, int M1, float *dT,
                             float *da, int accumulate, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Several nets ("experts") over the same atoms: rows of features are sorted
+ * by the net they go to and brought back with weights, the nets' layers may
+ * run in 8-bit integers where only values are wanted (screening), and the
+ * norms around a block are one pass with its gate and residual scale.  The
+ * paper's fitting nets are the case of one expert per atom, its type; the
+ * dp_fitting_* calls then take the sorted rows and type_start = start.
+ *
+ * Suffixes: rows of f64, f32, bf16 or f16 (the last two as uint16_t bit
+ * patterns); weights, scales and sums are f32 (f64 for f64 rows).  Unlike the
+ * calls above, rows may start at any multiple of their element's size:
+ * pointers and row lengths that allow 16-byte accesses are faster.
+ * ---------------------------------------------------------------------- */
+
+/*
+ * Plan: ntok tokens (atoms) with topk experts each.  Pair q = t topk + j goes
+ * to expert[q]; an id outside [0, nexp) drops the pair.  Pairs are sorted by
+ * expert, in order of q within one (a stable sort: the plan is unique).
+ *   expert [ntok][topk] int32
+ *   start  [nexp + 1] output: expert e has sorted rows start[e] .. start[e+1] - 1;
+ *          start[nexp] rows are kept
+ *   src    [ntok topk] output: the pair at each sorted row, -1 past the kept ones
+ *   pos    [ntok][topk] output: the sorted row of each pair, -1 for a dropped one
+ *   work, work_bytes  device scratch, 16-byte aligned, at least
+ *          dp_route_work_bytes(ntok, topk, nexp) bytes (0: bad arguments)
+ * Errors: DP_ERR_NULL, DP_ERR_SHAPE (ntok < 0, topk outside [1, 64], 2^31 or
+ * more pairs, nexp < 1, a short or misaligned work buffer),
+ * DP_ERR_UNSUPPORTED (nexp above 1024), DP_ERR_CUDA.
+ */
+size_t dp_route_work_bytes(int64_t ntok, int topk, int nexp);
+int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64_t *start, int32_t *src, int32_t *pos,
+                  void *work, size_t work_bytes, void *stream);
+
+/*
+ * Rows to their sorted places and back, H elements a row, with a plan's src and pos.
+ *   gather   xs[p] = x[src[p] / topk]; rows past the kept ones are zero
+ *            (its backward is combine of the rows' gradients with w NULL)
+ *   combine  y[t] = sum_j w[t][j] z[pos[t][j]], j in order, dropped pairs left
+ *            out (their rows are not read; a token without pairs gets zeros);
+ *            w [ntok][topk], or NULL for ones
+ *   combine_grad  from dy: dz[p] = w_q dy[t] (rows past the kept ones zero) and
+ *            dw_q = <dy[t], z[p]> (0 for a dropped pair); dw NULL: not
+ *            computed, z is not read
+ *   x, y, dy [ntok][H]; xs, z, dz [ntok topk][H]; dw [ntok][topk]
+ * Every sum has a fixed order; entries of src and pos outside their range count
+ * as dropped.  ntok == 0 reads no device pointer.  Errors: DP_ERR_NULL,
+ * DP_ERR_SHAPE (as the plan; H outside [1, 2^20]; an array not aligned to its
+ * elements), DP_ERR_CUDA.
+ */
+int dp_route_gather_f64(const double *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int H,
+                        double *xs, void *stream);
+int dp_route_gather_f32(const float *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int H,
+                        float *xs, void *stream);
+int dp_route_gather_bf16(const uint16_t *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int H,
+                         uint16_t *xs, void *stream);
+int dp_route_gather_f16(const uint16_t *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int H,
+                        uint16_t *xs, void *stream);
+int dp_route_combine_f64(const double *z, const int32_t *pos, const double *w, int64_t ntok, int topk, int H,
+                         double *y, void *stream);
+int dp_route_combine_f32(const float *z, const int32_t *pos, const float *w, int64_t ntok, int topk, int H, float *y,
+                         void *stream);
+int dp_route_combine_bf16(const uint16_t *z, const int32_t *pos, const float *w, int64_t ntok, int topk, int H,
+                          uint16_t *y, void *stream);
+int dp_route_combine_f16(const uint16_t *z, const int32_t *pos, const float *w, int64_t ntok, int topk, int H,
+                         uint16_t *y, void *stream);
+int dp_route_combine_grad_f64(const double *z, const int32_t *src, const int32_t *pos, const double *w,
+                              const double *dy, int64_t ntok, int topk, int H, double *dz, double *dw, void *stream);
+int dp_route_combine_grad_f32(const float *z, const int32_t *src, const int32_t *pos, const float *w, const float *dy,
+                              int64_t ntok, int topk, int H, float *dz, float *dw, void *stream);
+int dp_route_combine_grad_bf16(const uint16_t *z, const int32_t *src, const int32_t *pos, const float *w,
+                               const uint16_t *dy, int64_t ntok, int topk, int H, uint16_t *dz, float *dw,
+                               void *stream);
+int dp_route_combine_grad_f16(const uint16_t *z, const int32_t *src, const int32_t *pos, const float *w,
+                              const uint16_t *dy, int64_t ntok, int topk, int H, uint16_t *dz, float *dw,
+                              void *stream);
+
+/*
+ * Rows to 8-bit integers with a scale each.  x is rounded to f32; then, in f32,
+ *   amax = max_k |x_k|,  r = 127 / amax,  q_k = rint(x_k r) (ties to even),  sx = amax / 127,
+ * so x_k ~ sx q_k with q in [-127, 127].  A row with amax < 2^-100 gives zeros
+ * and sx = 0; a row that holds an infinity or NaN gives zeros and sx = NaN (its
+ * outputs become NaN).  Weights are rows too: W [nexp][N][K] by its nexp N rows.
+ *   xq  [rows][ldq] output, ldq = K rounded up to a multiple of 16, the columns
+ *       past K zero; 16-byte aligned.    sx  [rows] output
+ * src and pos NULL: rows = ntok, topk = 1.  With a plan's src and pos the rows go
+ * to their sorted places in the same pass (dp_route_gather_* of them: rows =
+ * ntok topk, those past the kept ones zero with sx = 0).
+ * Errors: DP_ERR_NULL, DP_ERR_SHAPE, DP_ERR_UNSUPPORTED (K above 65536), DP_ERR_CUDA.
+ */
+int dp_quant_rows_i8_f64(const double *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int K,
+                         int8_t *xq, float *sx, void *stream);
+int dp_quant_rows_i8_f32(const float *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int K,
+                         int8_t *xq, float *sx, void *stream);
+int dp_quant_rows_i8_bf16(const uint16_t *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int K,
+                          int8_t *xq, float *sx, void *stream);
+int dp_quant_rows_i8_f16(const uint16_t *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int K,
+                         int8_t *xq, float *sx, void *stream);
+
+/*
+ * Product of 8-bit rows with 8-bit weights:
+ *   y_in = act(float(sum_k xq_ik wq_enk) sx_i sw_en + bias_en),  e the expert of row i
+ * The integer sum is exact (any int8 values); the rest is f32, rounded to the
+ * rows' type (f64 rows hold f32 values: 8-bit inputs leave no more).
+ * The result has no gradient: with quantised rows y is piecewise constant in
+ * x, so forces come from the dp_fitting_* calls.
+ *   xq    [rows][K], K a multiple of 16 (dp_quant_rows_i8_*: ldq)
+ *   wq    [nexp][N][K];  sw, bias [nexp][N] (bias NULL: none)
+ *   start [nexp + 1] device, a plan's, increasing; rows past start[nexp] become
+ *         zero rows.  NULL with nexp = 1: all rows
+ *   act   DP_ACT_NONE or DP_ACT_TANH
+ *   y     [rows][N]
+ * xq and wq are 16-byte aligned.  rows == 0 reads no device pointer.  Errors:
+ * DP_ERR_NULL, DP_ERR_SHAPE, DP_ERR_UNSUPPORTED (K above 65536), DP_ERR_CUDA.
+ */
+#define DP_ACT_NONE 0
+#define DP_ACT_TANH 1
+int dp_linear_i8_f64(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t *wq, const float *sw,
+                     const float *bias, int nexp, int N, const int64_t *start, int act, double *y, void *stream);
+int dp_linear_i8_f32(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t *wq, const float *sw,
+                     const float *bias, int nexp, int N, const int64_t *start, int act, float *y, void *stream);
+int dp_linear_i8_bf16(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t *wq, const float *sw,
+                      const float *bias, int nexp, int N, const int64_t *start, int act, uint16_t *y, void *stream);
+int dp_linear_i8_f16(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t *wq, const float *sw,
+                     const float *bias, int nexp, int N, const int64_t *start, int act, uint16_t *y, void *stream);
+
+/*
+ * The norms around a block with its gate and residual scale.  For each token,
+ * with v^ = (v - m) s, m = 0 and s = (mean v^2 + eps)^-1/2 (DP_NORM_RMS) or
+ * m = mean v and s = (mean (v - m)^2 + eps)^-1/2 (DP_NORM_LAYER):
+ *   p  = f^ w1 (+ b1)        after the block (f its output)
+ *   r2 = r + a G p           the residual stream
+ *   u  = r2^ w2 (+ b2)       before the next block, from r2 unrounded
+ *   r, f, r2, u [ntok][H];  a, w1, w2, b1, b2 [H] (b1, b2 for DP_NORM_LAYER only)
+ *   gate  DP_GATE_FULL [ntok][H], DP_GATE_TOKEN [ntok], DP_GATE_NONE (G = 1)
+ *   stats [ntok][4] output: m1, s1, m2, s2
+ * Backward, from dr2 = dE/dr2 and du = dE/du and the forward's r2 and stats:
+ *   dr, df [ntok][H], dgate (the gate's shape), and the sums over the tokens
+ *   da, dw1, dw2 [H], for DP_NORM_LAYER also db1, db2 [H]
+ *   work, work_bytes  device scratch, 16-byte aligned, at least
+ *         dp_norm_gate_work_bytes(H, sizeof(element)) bytes
+ * The sums over the tokens have a fixed order.  ntok == 0: the backward's sums
+ * are zero.  Errors: DP_ERR_NULL, DP_ERR_SHAPE (eps not positive, an unknown
+ * kind or gate kind, alignment, a short work buffer), DP_ERR_UNSUPPORTED
+ * (H above 16384), DP_ERR_CUDA.
+ */
+#define DP_NORM_RMS 0
+#define DP_NORM_LAYER 1
+#define DP_GATE_NONE 0
+#define DP_GATE_TOKEN 1
+#define DP_GATE_FULL 2
+size_t dp_norm_gate_work_bytes(int H, int elem_bytes); /* 0 on bad arguments */
+int dp_norm_gate_fwd_f64(const double *r, const double *f, const double *gate, int gate_kind, const double *a,
+                         const double *w1, const double *b1, const double *w2, const double *b2, int64_t ntok, int H,
+                         int kind, double eps, double *r2, double *u, double *stats, void *stream);
+int dp_norm_gate_fwd_f32(const float *r, const float *f, const float *gate, int gate_kind, const float *a,
+                         const float *w1, const float *b1, const float *w2, const float *b2, int64_t ntok, int H,
+                         int kind, double eps, float *r2, float *u, float *stats, void *stream);
+int dp_norm_gate_fwd_bf16(const uint16_t *r, const uint16_t *f, const uint16_t *gate, int gate_kind, const float *a,
+                          const float *w1, const float *b1, const float *w2, const float *b2, int64_t ntok, int H,
+                          int kind, double eps, uint16_t *r2, uint16_t *u, float *stats, void *stream);
+int dp_norm_gate_fwd_f16(const uint16_t *r, const uint16_t *f, const uint16_t *gate, int gate_kind, const float *a,
+                         const float *w1, const float *b1, const float *w2, const float *b2, int64_t ntok, int H,
+                         int kind, double eps, uint16_t *r2, uint16_t *u, float *stats, void *stream);
+int dp_norm_gate_grad_f64(const double *r2, const double *f, const double *gate, int gate_kind, const double *a,
+                          const double *w1, const double *b1, const double *w2, const double *stats,
+                          const double *dr2, const double *du, int64_t ntok, int H, int kind, double *dr, double *df,
+                          double *dgate, double *da, double *dw1, double *dw2, double *db1, double *db2, void *work,
+                          size_t work_bytes, void *stream);
+int dp_norm_gate_grad_f32(const float *r2, const float *f, const float *gate, int gate_kind, const float *a,
+                          const float *w1, const float *b1, const float *w2, const float *stats, const float *dr2,
+                          const float *du, int64_t ntok, int H, int kind, float *dr, float *df, float *dgate,
+                          float *da, float *dw1, float *dw2, float *db1, float *db2, void *work, size_t work_bytes,
+                          void *stream);
+int dp_norm_gate_grad_bf16(const uint16_t *r2, const uint16_t *f, const uint16_t *gate, int gate_kind, const float *a,
+                           const float *w1, const float *b1, const float *w2, const float *stats, const uint16_t *dr2,
+                           const uint16_t *du, int64_t ntok, int H, int kind, uint16_t *dr, uint16_t *df,
+                           uint16_t *dgate, float *da, float *dw1, float *dw2, float *db1, float *db2, void *work,
+                           size_t work_bytes, void *stream);
+int dp_norm_gate_grad_f16(const uint16_t *r2, const uint16_t *f, const uint16_t *gate, int gate_kind, const float *a,
+                          const float *w1, const float *b1, const float *w2, const float *stats, const uint16_t *dr2,
+                          const uint16_t *du, int64_t ntok, int H, int kind, uint16_t *dr, uint16_t *df,
+                          uint16_t *dgate, float *da, float *dw1, float *dw2, float *db1, float *db2, void *work,
+                          size_t work_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -154,6 +154,20 @@ _SIGS = {
                               ctypes.c_int),
     "dp_fitting_grad_tc_f64": ([_P, _P, ctypes.c_int, ctypes.c_int, _P, _P, _P, _P, _P, ctypes.c_size_t, _P],
                                ctypes.c_int),
+    "dp_route_work_bytes": ([_I64, ctypes.c_int, ctypes.c_int], ctypes.c_size_t),
+    "dp_route_plan": ([_P, _I64, ctypes.c_int, ctypes.c_int, _P, _P, _P, _P, ctypes.c_size_t, _P], ctypes.c_int),
+    "dp_norm_gate_work_bytes": ([ctypes.c_int, ctypes.c_int], ctypes.c_size_t),
+    **{f"{name}_{x}": (args, ctypes.c_int) for x in ("f64", "f32", "bf16", "f16") for name, args in (
+        ("dp_route_gather", [_P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _P]),
+        ("dp_route_combine", [_P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _P]),
+        ("dp_route_combine_grad", [_P, _P, _P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _P, _P]),
+        ("dp_quant_rows_i8", [_P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _P, _P]),
+        ("dp_linear_i8", [_P, _P, _I64, ctypes.c_int, _P, _P, _P, ctypes.c_int, ctypes.c_int, _P, ctypes.c_int, _P,
+                          _P]),
+        ("dp_norm_gate_fwd", [_P, _P, _P, ctypes.c_int, _P, _P, _P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _D, _P,
+                              _P, _P, _P]),
+        ("dp_norm_gate_grad", [_P, _P, _P, ctypes.c_int, _P, _P, _P, _P, _P, _P, _P, _I64, ctypes.c_int, ctypes.c_int,
+                               _P, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]))},
     "dp_env_mat_df64": ([_P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _ENV, _P, _P, _P, _P], ctypes.c_int),
     "dp_force_virial_df64": ([_P, _P, _I64, _I64, ctypes.c_int, _ENV, _P, _P, _P, _P, _P], ctypes.c_int),
 }
@@ -907,3 +921,251 @@ def dp_tensor_head_grad(T, a, dA, dT=None, da=None, accumulate=False, want=("dT"
     """(dT [nloc][4][M1], da [nloc][M1]) from dE/dA [nloc][3][3]; accumulate adds the head's dT to dT;
     want: the outputs to compute (the other is returned as None)."""
     return _head_grad("tensor", T, a, dA, (3, 3), dT, da, accumulate, want)
+
+
+# ---------------------------------------------------------------- several nets over the same atoms
+_ROW_SUFFIX = {torch.float64: "f64", torch.float32: "f32", torch.bfloat16: "bf16", torch.float16: "f16"}
+
+
+def _rows(t, name, dtype=None, shape=None, dim=2):
+    t = _dev(t, name, dtype, shape)
+    if t.dtype not in _ROW_SUFFIX:
+        raise TypeError(f"{name} must be f64, f32, bf16 or f16, got {t.dtype}")
+    if t.dim() != dim:
+        raise ValueError(f"{name} must have {dim} dimensions, got {tuple(t.shape)}")
+    return t
+
+
+def _wdtype(dtype):
+    """The type of weights and sums beside rows of dtype."""
+    return torch.float64 if dtype == torch.float64 else torch.float32
+
+
+def _same_device(first, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on different devices: {first.device} and {t.device}")
+
+
+def _out(out, name, dtype, shape, like):
+    return torch.empty(shape, dtype=dtype, device=like.device) if out is None else _dev(out, name, dtype, shape)
+
+
+def dp_route_work_bytes(ntok, topk, nexp) -> int:
+    """Bytes of device scratch dp_route_plan needs."""
+    n = int(_lib.dp_route_work_bytes(int(ntok), int(topk), int(nexp)))
+    if n == 0:
+        raise ValueError(f"bad plan: {ntok} tokens, {topk} experts each of {nexp}")
+    return n
+
+
+def dp_route_plan(expert, nexp, out=None, work=None):
+    """(start [nexp+1] int64, src [ntok*topk] int32, pos [ntok][topk] int32): the pairs of expert
+    [ntok][topk] (int32; ids outside [0, nexp) drop the pair) sorted by expert, stably."""
+    expert = _dev(expert, "expert", torch.int32)
+    if expert.dim() != 2:
+        raise ValueError(f"expert must be [ntok][topk], got {tuple(expert.shape)}")
+    ntok, topk = (int(x) for x in expert.shape)
+    start, src, pos = (None, None, None) if out is None else out
+    start = _out(start, "start", torch.int64, (int(nexp) + 1,), expert)
+    src = _out(src, "src", torch.int32, (ntok * topk,), expert)
+    pos = _out(pos, "pos", torch.int32, (ntok, topk), expert)
+    if work is None:
+        work = torch.empty((dp_route_work_bytes(ntok, topk, nexp),), dtype=torch.uint8, device=expert.device)
+    else:
+        work = _dev(work, "work", torch.uint8)
+    _same_device(expert, start, src, pos, work)
+    _check(_lib.dp_route_plan(_ptr(expert), ntok, topk, int(nexp), _ptr(start), _ptr(src), _ptr(pos), _ptr(work),
+                              work.numel(), _stream(expert)))
+    return start, src, pos
+
+
+def _plan_arrays(src, pos):
+    pos = _dev(pos, "pos", torch.int32)
+    if pos.dim() != 2:
+        raise ValueError(f"pos must be [ntok][topk], got {tuple(pos.shape)}")
+    if src is not None:
+        _dev(src, "src", torch.int32, (pos.numel(),))
+        _same_device(pos, src)
+    return int(pos.shape[0]), int(pos.shape[1])
+
+
+def dp_route_gather(x, src, pos, out=None):
+    """xs [ntok*topk][H]: each token's row of x [ntok][H] at its pairs' sorted places; rows past the kept
+    ones are zero."""
+    x = _rows(x, "x")
+    ntok, topk = _plan_arrays(_dev(src, "src", torch.int32), pos)
+    H = int(x.shape[1])
+    _dev(x, "x", None, (ntok, H))
+    xs = _out(out, "out", x.dtype, (ntok * topk, H), x)
+    _same_device(x, pos, xs)
+    _check(getattr(_lib, f"dp_route_gather_{_ROW_SUFFIX[x.dtype]}")(_ptr(x), _ptr(src), _ptr(pos), ntok, topk, H,
+                                                                   _ptr(xs), _stream(x)))
+    return xs
+
+
+def dp_route_combine(z, pos, w=None, out=None):
+    """y [ntok][H] = sum_j w[t][j] z[pos[t][j]] over the kept pairs (w None: ones; then also the backward of
+    dp_route_gather)."""
+    z = _rows(z, "z")
+    ntok, topk = _plan_arrays(None, pos)
+    H = int(z.shape[1])
+    _dev(z, "z", None, (ntok * topk, H))
+    if w is not None:
+        _dev(w, "w", _wdtype(z.dtype), (ntok, topk))
+    y = _out(out, "out", z.dtype, (ntok, H), z)
+    _same_device(z, pos, w, y)
+    _check(getattr(_lib, f"dp_route_combine_{_ROW_SUFFIX[z.dtype]}")(_ptr(z), _ptr(pos), _ptr(w), ntok, topk, H,
+                                                                    _ptr(y), _stream(z)))
+    return y
+
+
+def dp_route_combine_grad(z, src, pos, w, dy, out=None, want=("dz", "dw")):
+    """(dz [ntok*topk][H], dw [ntok][topk]) of dp_route_combine from dy [ntok][H]; w None: ones.  want without
+    "dw": dw is returned as None and z is not read (may be None)."""
+    dy = _rows(dy, "dy")
+    ntok, topk = _plan_arrays(_dev(src, "src", torch.int32), pos)
+    H, dtype = int(dy.shape[1]), dy.dtype
+    _dev(dy, "dy", None, (ntok, H))
+    if "dz" not in want or set(want) - {"dz", "dw"}:
+        raise ValueError("want is (dz,) or (dz, dw)")
+    if w is not None:
+        _dev(w, "w", _wdtype(dtype), (ntok, topk))
+    dz, dw = (None, None) if out is None else out
+    dz = _out(dz, "dz", dtype, (ntok * topk, H), dy)
+    if "dw" in want:
+        _rows(z, "z", dtype, (ntok * topk, H))
+        dw = _out(dw, "dw", _wdtype(dtype), (ntok, topk), dy)
+    else:
+        z = dw = None
+    _same_device(dy, z, src, pos, w, dz, dw)
+    _check(getattr(_lib, f"dp_route_combine_grad_{_ROW_SUFFIX[dtype]}")(
+        _ptr(z), _ptr(src), _ptr(pos), _ptr(w), _ptr(dy), ntok, topk, H, _ptr(dz), _ptr(dw), _stream(dy)))
+    return dz, dw
+
+
+def dp_quant_rows_i8(x, src=None, pos=None, out=None):
+    """(xq int8 [rows][ldq], sx f32 [rows]): each row of x [ntok][K] as 8-bit integers and a scale, ldq = K
+    rounded up to a multiple of 16 (zeros past K).  With a plan's src and pos the rows also go to their sorted
+    places (rows = ntok*topk).  Weights [nexp][N][K] are quantised by their rows, x = W.view(nexp*N, K)."""
+    x = _rows(x, "x")
+    ntok, K = (int(v) for v in x.shape)
+    topk = 1
+    if (src is None) != (pos is None):
+        raise ValueError("src and pos come together")
+    if pos is not None:
+        n, topk = _plan_arrays(src, pos)
+        _dev(x, "x", None, (n, K))
+    xq, sx = (None, None) if out is None else out
+    xq = _out(xq, "xq", torch.int8, (ntok * topk, -(-K // 16) * 16), x)
+    sx = _out(sx, "sx", torch.float32, (ntok * topk,), x)
+    _same_device(x, src, pos, xq, sx)
+    _check(getattr(_lib, f"dp_quant_rows_i8_{_ROW_SUFFIX[x.dtype]}")(_ptr(x), _ptr(src), _ptr(pos), ntok, topk, K,
+                                                                    _ptr(xq), _ptr(sx), _stream(x)))
+    return xq, sx
+
+
+_ACTS = {None: 0, "tanh": 1}
+
+
+def dp_linear_i8(xq, sx, wq, sw, bias=None, start=None, act=None, dtype=torch.float32, out=None):
+    """y [rows][N] of dtype: act(float(xq wq^T) sx sw + bias), the integer product exact; xq [rows][K] and sx
+    from dp_quant_rows_i8, wq int8 [nexp][N][K] with sw, bias f32 [nexp][N]; start [nexp+1] a plan's (rows past
+    start[nexp] become zeros), None with one expert for all rows; act None or "tanh"."""
+    xq = _dev(xq, "xq", torch.int8)
+    wq = _dev(wq, "wq", torch.int8)
+    if xq.dim() != 2 or wq.dim() != 3 or xq.shape[1] != wq.shape[2]:
+        raise ValueError(f"xq [rows][K] and wq [nexp][N][K] expected, got {tuple(xq.shape)} and {tuple(wq.shape)}")
+    if act not in _ACTS:
+        raise ValueError(f"act must be None or 'tanh', got {act!r}")
+    if dtype not in _ROW_SUFFIX:
+        raise TypeError(f"unsupported dtype {dtype}")
+    rows, K = (int(v) for v in xq.shape)
+    nexp, N = int(wq.shape[0]), int(wq.shape[1])
+    _dev(sx, "sx", torch.float32, (rows,))
+    _dev(sw, "sw", torch.float32, (nexp, N))
+    if bias is not None:
+        _dev(bias, "bias", torch.float32, (nexp, N))
+    if start is not None:
+        _dev(start, "start", torch.int64, (nexp + 1,))
+    y = _out(out, "out", dtype, (rows, N), xq)
+    _same_device(xq, sx, wq, sw, bias, start, y)
+    _check(getattr(_lib, f"dp_linear_i8_{_ROW_SUFFIX[dtype]}")(_ptr(xq), _ptr(sx), rows, K, _ptr(wq), _ptr(sw),
+                                                              _ptr(bias), nexp, N, _ptr(start), _ACTS[act], _ptr(y),
+                                                              _stream(xq)))
+    return y
+
+
+_NORMS = {"rms": 0, "layer": 1}
+
+
+def _norm_inputs(r, f, a, w1, w2, b1, b2, gate, kind, grad):
+    f = _rows(f, "f")
+    if kind not in _NORMS:
+        raise ValueError(f"kind must be 'rms' or 'layer', got {kind!r}")
+    ntok, H = (int(v) for v in f.shape)
+    wd = _wdtype(f.dtype)
+    _rows(r, "r2" if grad else "r", f.dtype, (ntok, H))
+    for t, name in ((a, "a"), (w1, "w1"), (w2, "w2")):
+        _dev(t, name, wd, (H,))
+    for t, name in ((b1, "b1"), (b2, "b2")):
+        if kind == "layer":
+            _dev(t, name, wd, (H,))
+        elif t is not None:
+            raise ValueError(f"{name} goes with kind='layer'")
+    gate_kind = 0
+    if gate is not None:
+        _dev(gate, "gate", f.dtype)
+        gate_kind = 2 if gate.dim() == 2 else 1
+        _dev(gate, "gate", f.dtype, (ntok, H) if gate_kind == 2 else (ntok,))
+    _same_device(f, r, a, w1, w2, b1, b2, gate)
+    return ntok, H, wd, gate_kind
+
+
+def dp_norm_gate_fwd(r, f, a, w1, w2, b1=None, b2=None, gate=None, kind="rms", eps=1e-6, out=None):
+    """(r2, u, stats): r2 = r + a G norm(f; w1, b1), u = norm(r2; w2, b2), stats [ntok][4] for the backward.
+    r, f [ntok][H]; a, w1, w2 (and b1, b2 for kind="layer") [H]; gate None, [ntok] or [ntok][H]."""
+    ntok, H, wd, gk = _norm_inputs(r, f, a, w1, w2, b1, b2, gate, kind, False)
+    r2, u, stats = (None, None, None) if out is None else out
+    r2 = _out(r2, "r2", f.dtype, (ntok, H), f)
+    u = _out(u, "u", f.dtype, (ntok, H), f)
+    stats = _out(stats, "stats", wd, (ntok, 4), f)
+    _same_device(f, r2, u, stats)
+    _check(getattr(_lib, f"dp_norm_gate_fwd_{_ROW_SUFFIX[f.dtype]}")(
+        _ptr(r), _ptr(f), _ptr(gate), gk, _ptr(a), _ptr(w1), _ptr(b1), _ptr(w2), _ptr(b2), ntok, H, _NORMS[kind],
+        float(eps), _ptr(r2), _ptr(u), _ptr(stats), _stream(f)))
+    return r2, u, stats
+
+
+def dp_norm_gate_work_bytes(H, dtype) -> int:
+    """Bytes of device scratch dp_norm_gate_grad needs for rows of H elements of dtype."""
+    n = int(_lib.dp_norm_gate_work_bytes(int(H), torch.empty((), dtype=dtype).element_size()))
+    if n == 0:
+        raise ValueError(f"unsupported row length {H}")
+    return n
+
+
+def dp_norm_gate_grad(r2, f, a, w1, w2, stats, dr2, du, b1=None, b2=None, gate=None, kind="rms", out=None, work=None):
+    """Backward of dp_norm_gate_fwd from dr2, du and the forward's r2 and stats: a dict of dr, df, dgate (None
+    without a gate), da, dw1, dw2, and for kind="layer" db1, db2 (else None).  b2 is accepted and not read.
+    out: such a dict of tensors to fill (missing ones are allocated)."""
+    ntok, H, wd, gk = _norm_inputs(r2, f, a, w1, w2, b1, b1 if b2 is None else b2, gate, kind, True)
+    _dev(stats, "stats", wd, (ntok, 4))
+    _rows(dr2, "dr2", f.dtype, (ntok, H))
+    _rows(du, "du", f.dtype, (ntok, H))
+    o = dict(out or {})
+    res = {"dr": _out(o.get("dr"), "dr", f.dtype, (ntok, H), f), "df": _out(o.get("df"), "df", f.dtype, (ntok, H), f),
+           "dgate": None if gate is None else _out(o.get("dgate"), "dgate", f.dtype, tuple(gate.shape), f)}
+    for name in ("da", "dw1", "dw2", "db1", "db2"):
+        res[name] = _out(o.get(name), name, wd, (H,), f) if kind == "layer" or name[1] != "b" else None
+    need = dp_norm_gate_work_bytes(H, f.dtype)
+    if work is None:
+        work = torch.empty((need,), dtype=torch.uint8, device=f.device)
+    else:
+        work = _dev(work, "work", torch.uint8)
+    _same_device(f, stats, dr2, du, work, *res.values())
+    _check(getattr(_lib, f"dp_norm_gate_grad_{_ROW_SUFFIX[f.dtype]}")(
+        _ptr(r2), _ptr(f), _ptr(gate), gk, _ptr(a), _ptr(w1), _ptr(b1), _ptr(w2), _ptr(stats), _ptr(dr2), _ptr(du),
+        ntok, H, _NORMS[kind], *(_ptr(res[n]) for n in ("dr", "df", "dgate", "da", "dw1", "dw2", "db1", "db2")),
+        _ptr(work), work.numel(), _stream(f)))
+    return res

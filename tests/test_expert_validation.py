@@ -1,0 +1,88 @@
+"""The expert-block calls refuse bad arguments on the host, before any CUDA call (CPU only: the fake pointers are
+never dereferenced)."""
+import ctypes
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def dpc():
+    import __graft_entry__
+    __graft_entry__._load_builder().build()
+    import paper_2107_02103_gb300 as m
+    return m
+
+
+FAKE = ctypes.c_void_p(0x1000)
+
+
+def test_route(dpc):
+    lib = dpc._lib
+    wb = dpc.dp_route_work_bytes(10000, 2, 8)
+    assert wb >= 16 and lib.dp_route_work_bytes(-1, 2, 8) == 0 and lib.dp_route_work_bytes(5, 65, 8) == 0
+    assert lib.dp_route_work_bytes(2 ** 30, 2, 8) == 0 and lib.dp_route_work_bytes(5, 1, 1025) == 0
+
+    def plan(expert=FAKE, ntok=10000, topk=2, nexp=8, start=FAKE, src=FAKE, pos=FAKE, work=FAKE, nbytes=wb):
+        return lib.dp_route_plan(expert, ntok, topk, nexp, start, src, pos, work, nbytes, None)
+
+    assert plan(expert=None) == plan(start=None) == plan(src=None) == plan(pos=None) == plan(work=None) == dpc.DP_ERR_NULL
+    assert plan(ntok=-1) == plan(topk=0) == plan(topk=65) == plan(nexp=0) == plan(ntok=2 ** 30) == dpc.DP_ERR_SHAPE
+    assert plan(nbytes=wb - 1) == plan(work=ctypes.c_void_p(0x1008)) == dpc.DP_ERR_SHAPE
+    assert plan(nexp=1025) == dpc.DP_ERR_UNSUPPORTED
+    for x in ("f64", "f32", "bf16", "f16"):
+        gather, combine, grad = (getattr(lib, f"dp_route_{n}_{x}") for n in ("gather", "combine", "combine_grad"))
+        assert gather(None, FAKE, FAKE, 4, 2, 8, FAKE, None) == dpc.DP_ERR_NULL
+        assert gather(FAKE, FAKE, FAKE, 4, 2, 0, FAKE, None) == dpc.DP_ERR_SHAPE
+        assert gather(ctypes.c_void_p(0x1001), FAKE, FAKE, 4, 2, 8, FAKE, None) == dpc.DP_ERR_SHAPE
+        assert gather(None, None, None, 0, 2, 8, None, None) == dpc.DP_OK
+        assert combine(FAKE, None, FAKE, 4, 2, 8, FAKE, None) == dpc.DP_ERR_NULL
+        assert combine(FAKE, FAKE, FAKE, 4, 65, 8, FAKE, None) == dpc.DP_ERR_SHAPE
+        assert grad(None, FAKE, FAKE, FAKE, FAKE, 4, 2, 8, FAKE, FAKE, None) == dpc.DP_ERR_NULL
+        assert grad(FAKE, FAKE, FAKE, FAKE, FAKE, -4, 2, 8, FAKE, FAKE, None) == dpc.DP_ERR_SHAPE
+        assert grad(None, None, None, None, None, 0, 2, 8, None, None, None) == dpc.DP_OK
+
+
+def test_linear_i8(dpc):
+    lib = dpc._lib
+    odd = ctypes.c_void_p(0x1008)
+    for x in ("f64", "f32", "bf16", "f16"):
+        q = getattr(lib, f"dp_quant_rows_i8_{x}")
+        assert q(FAKE, None, None, 4, 1, 0, FAKE, FAKE, None) == dpc.DP_ERR_SHAPE
+        assert q(FAKE, None, None, 4, 2, 8, FAKE, FAKE, None) == dpc.DP_ERR_SHAPE  # topk without a plan
+        assert q(FAKE, FAKE, None, 4, 2, 8, FAKE, FAKE, None) == dpc.DP_ERR_NULL
+        assert q(FAKE, None, None, 4, 1, 8, odd, FAKE, None) == dpc.DP_ERR_SHAPE
+        assert q(FAKE, None, None, 4, 1, 65537, FAKE, FAKE, None) == dpc.DP_ERR_UNSUPPORTED
+        assert q(None, None, None, 4, 1, 8, FAKE, FAKE, None) == dpc.DP_ERR_NULL
+        assert q(None, None, None, 0, 1, 8, None, None, None) == dpc.DP_OK
+
+        def lin(xq=FAKE, rows=4, K=32, wq=FAKE, nexp=2, N=8, start=FAKE, act=0, y=FAKE, f=getattr(lib, f"dp_linear_i8_{x}")):
+            return f(xq, FAKE, rows, K, wq, FAKE, None, nexp, N, start, act, y, None)
+
+        assert lin(xq=None) == lin(wq=None) == lin(y=None) == lin(start=None) == dpc.DP_ERR_NULL
+        assert lin(rows=-1) == lin(K=24) == lin(K=0) == lin(N=0) == lin(nexp=0) == lin(act=2) == dpc.DP_ERR_SHAPE
+        assert lin(xq=odd) == lin(wq=odd) == dpc.DP_ERR_SHAPE
+        assert lin(K=65552) == dpc.DP_ERR_UNSUPPORTED
+        assert lin(rows=0, xq=None, wq=None, y=None) == dpc.DP_OK
+
+
+def test_norm_gate(dpc):
+    lib = dpc._lib
+    wb = lib.dp_norm_gate_work_bytes(32, 4)
+    assert wb > 0 and lib.dp_norm_gate_work_bytes(0, 4) == lib.dp_norm_gate_work_bytes(16385, 4) == 0
+    assert lib.dp_norm_gate_work_bytes(32, 3) == 0
+    for x in ("f64", "f32", "bf16", "f16"):
+        def fwd(r=FAKE, gate=FAKE, gk=2, b1=FAKE, ntok=4, H=32, kind=1, eps=1e-6, u=FAKE, f=getattr(lib, f"dp_norm_gate_fwd_{x}")):
+            return f(r, FAKE, gate, gk, FAKE, FAKE, b1, FAKE, FAKE, ntok, H, kind, eps, FAKE, u, FAKE, None)
+
+        assert fwd(r=None) == fwd(gate=None) == fwd(b1=None) == fwd(u=None) == dpc.DP_ERR_NULL
+        assert fwd(gk=3) == fwd(kind=2) == fwd(ntok=-1) == fwd(H=0) == fwd(eps=0.0) == dpc.DP_ERR_SHAPE
+        assert fwd(H=16385) == dpc.DP_ERR_UNSUPPORTED
+        assert fwd(r=ctypes.c_void_p(0x1001)) == dpc.DP_ERR_SHAPE
+        assert fwd(ntok=0, r=None, gate=None, u=None) == dpc.DP_OK
+
+        def grad(dr=FAKE, dgate=FAKE, db1=FAKE, work=FAKE, nbytes=2 * wb, kind=1, f=getattr(lib, f"dp_norm_gate_grad_{x}")):
+            return f(FAKE, FAKE, FAKE, 2, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 4, 32, kind, dr, FAKE, dgate, FAKE, FAKE,
+                     FAKE, db1, FAKE, work, nbytes, None)
+
+        assert grad(dr=None) == grad(dgate=None) == grad(db1=None) == grad(work=None) == dpc.DP_ERR_NULL
+        assert grad(nbytes=16) == grad(kind=-1) == grad(work=ctypes.c_void_p(0x1008)) == dpc.DP_ERR_SHAPE
