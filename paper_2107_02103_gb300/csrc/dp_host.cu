@@ -149,6 +149,7 @@ int dp_tc_wait_timeouts(unsigned int *count) {
   *count = 0;
   int rc = dpc::take_wait_timeouts_tabulate(count);
   if (!rc) rc = dpc::take_wait_timeouts_fitting(count);
+  if (!rc) rc = dpc::take_wait_timeouts_linear_i8(count);
   return rc;
 }
 

@@ -179,6 +179,350 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_i8_few_kernel(const I8A
   }
 }
 
+// ------------------------------------------------------------------ the product on the tensor cores
+// A tile is 128 output channels (the MMA's rows) by up to TN sorted rows of one expert (its columns), so that an
+// epilogue warp holds 32 neighbouring channels of a row and stores them side by side.  sm_103a multiplies 8-bit
+// integers slowly; fp16 holds them exactly, and fp32 sums of their products are exact while K <= 1024
+// (1024 * 2^14 = 2^24): longer K is cut into chunks of 1024 whose sums are added as int32.
+//   Loader warps read the 8-bit rows from global memory into registers two stages ahead, turn them into fp16
+//   (byte q + 128 under the exponent of 1024, less 1152) and write the stage's operands, K-major core matrices of
+//   8 rows x 16 bytes without swizzle; lanes lie along the rows, so that a store's eight lanes fill one core matrix.
+//   Lane 0 of the first loader warp issues a stage's MMAs (M 128, K 16 each) one stage behind.
+//   Epilogue warps (two per TMEM lane quadrant, half the columns each) keep the chunks' int32 sums in registers and
+//   finish a tile while the next one runs in the other TMEM buffer.
+// A block per SM walks the tiles; every wait is bounded, a block that gives up writes NaN and is counted.
+namespace i8 {
+constexpr int kTM = 128, kKB = 64, kChunkK = 1024;
+constexpr int kEpiWarps = 8, kLoadWarps = 8, kThreads = (kEpiWarps + kLoadWarps) * 32;
+constexpr int kEpiRegs = 168, kLoadRegs = 88;  // of the 128 a thread is launched with
+static_assert(kEpiWarps * kEpiRegs + kLoadWarps * kLoadRegs <= (kEpiWarps + kLoadWarps) * 128, "register split");
+constexpr uint32_t kLBO = 128, kSBO = 1024;  // next core matrix along K, next 8 rows
+
+__device__ unsigned int g_timeouts;
+
+template <int TN>
+struct Shape {
+  static constexpr int kStageBytes = (kTM + TN) * kKB * 2;
+  static constexpr int kStages = TN == 256 ? 4 : 6;
+  static constexpr int kAhead = TN == 256 ? 2 : TN == 128 ? 3 : 4;  // stages held in a loader's registers
+  static constexpr uint32_t kTmemCols = 2 * TN;
+  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + (2 * kStages + 5) * 8 + 16;
+  static_assert(kSmem <= 227 * 1024 && TN % 32 == 0 && 2 * TN <= 512 && 2 * TN >= 32, "tile");
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, const volatile int *stop) {
+  uint32_t done = 0;
+  for (int it = 0; it < (1 << 22) && !done; ++it) {
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(done)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    if (!done && (it & 63) == 63 && stop && *stop) return false;
+  }
+  return done != 0;
+}
+__device__ __forceinline__ void arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ uint64_t smem_desc(uint32_t saddr) {  // K-major, no swizzle, version 1
+  return (uint64_t)((saddr & 0x3FFFF) >> 4) | ((uint64_t)(kLBO >> 4) << 16) | ((uint64_t)(kSBO >> 4) << 32) | (1ull << 46);
+}
+
+// Four int8 as two fp16 pairs.
+__device__ __forceinline__ void widen(uint32_t q, uint32_t &lo, uint32_t &hi) {
+  const uint32_t u = q ^ 0x80808080u;  // q + 128
+  lo = __byte_perm(u, 0x64646464u, 0x4140);
+  hi = __byte_perm(u, 0x64646464u, 0x4342);  // 1024 + q + 128
+  asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(lo) : "r"(0x64806480u));
+  asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(hi) : "r"(0x64806480u));
+}
+
+// Where a role stands: the tile, and the expert, rows and channels it means.
+struct Tile {
+  int64_t tile, r0, r1;
+  int e, n0;
+  bool have;
+};
+__device__ __forceinline__ void seek(const I8Args &p, int TN, int nct, Tile &t) {
+  const int64_t rt = t.tile / nct;
+  t.n0 = (int)(t.tile - rt * nct) * kTM;
+  t.have = find_tile(p, rt, TN, t.e, t.r0, t.r1);
+}
+
+template <int W>
+__device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[W]) {
+  static_assert(W == 16, "width");
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+        "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(addr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_st(uint32_t addr, const float (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
+      "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
+      "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]));
+}
+
+template <typename T, int TN>
+__global__ void __launch_bounds__(kThreads, 1) linear_i8_tc_kernel(const I8Args p) {
+  using S = Shape<TN>;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  uint64_t *full = reinterpret_cast<uint64_t *>(smem + S::kStages * S::kStageBytes), *empty = full + S::kStages;
+  uint64_t *acc_full = empty + S::kStages, *acc_empty = acc_full + 2, *done = acc_empty + 2;
+  uint32_t *holder = reinterpret_cast<uint32_t *>(done + 1);
+  volatile int *stop = reinterpret_cast<int *>(holder + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int nct = (p.N + kTM - 1) / kTM, nkb = (p.K + kKB - 1) / kKB;
+
+  if (threadIdx.x == 0) {
+    auto init = [](uint64_t *b, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(n)); };
+    for (int s = 0; s < S::kStages; ++s) {
+      init(full + s, kLoadWarps);
+      init(empty + s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      init(acc_full + b, 1);
+      init(acc_empty + b, kEpiWarps);
+    }
+    init(done, 1);
+    *stop = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(holder)),
+                 "r"(S::kTmemCols));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;");
+  const uint32_t tmem = *holder;
+  bool ok = true;
+
+  if (warp >= kEpiWarps) {
+    // ---------------------------------------------------------------- loaders, and the MMAs
+    if constexpr (TN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
+    constexpr int kA = kTM / 64, kB = TN / 64 ? TN / 64 : 1, kU = kA + kB;
+    const int lw = warp - kEpiWarps, r8 = lane & 7, kp = lane >> 3, row = lw * 8 + r8;
+    const uint32_t put = smem_u32(smem) + lw * kSBO + kp * 2 * kLBO + r8 * 16;
+    Tile at{(int64_t)blockIdx.x, 0, 0, 0, 0, false};  // the tile the loads stand at
+    int kb = 0;                                       // and its slice
+    auto next_tile = [&] {  // to the next tile with work
+      do {
+        seek(p, TN, nct, at);
+        if (at.have && at.e < p.nexp) return;
+        at.tile += gridDim.x;
+      } while (at.have);
+    };
+    next_tile();
+    uint4 raw[S::kAhead][kU];
+    int cols[S::kAhead];  // columns (rows of x) of the stage, 0 past the last tile; the tile's last slice: + 1 << 16
+    auto load = [&](uint4 (&r)[kU], int &c) {
+      c = 0;
+      if (!at.have) return;
+      const int k = kb * kKB + kp * 16, nr = (int)(at.r1 - at.r0);
+      const uint4 zero = make_uint4(0, 0, 0, 0);
+      const int8_t *w = p.wq + ((int64_t)at.e * p.N + at.n0 + row) * p.K + k, *x = p.xq + (at.r0 + row) * p.K + k;
+#pragma unroll
+      for (int i = 0; i < kA; ++i)
+        r[i] = k < p.K && at.n0 + row + 64 * i < p.N ? __ldg(reinterpret_cast<const uint4 *>(w + (int64_t)64 * i * p.K)) : zero;
+#pragma unroll
+      for (int i = 0; i < kB; ++i)
+        r[kA + i] = k < p.K && row + 64 * i < nr ? __ldg(reinterpret_cast<const uint4 *>(x + (int64_t)64 * i * p.K)) : zero;
+      c = (nr + 15) / 16 * 16;
+      if (++kb == nkb) {
+        kb = 0;
+        c |= 1 << 16;
+        at.tile += gridDim.x;
+        next_tile();
+      }
+    };
+#pragma unroll
+    for (int a = 0; a < S::kAhead; ++a) load(raw[a], cols[a]);
+    // the MMA issuer's position: one stage behind the loader's
+    int issued = 0, unit = 0, slice = 0, pending = 0;  // stages issued; accumulator uses; slice in the chunk
+    auto issue = [&](int c) {  // stage `issued`, c as cols[]
+      const int st = issued % S::kStages, buf = unit & 1;
+      if (slice == 0 && unit >= 2) ok = ok && wait(smem_u32(acc_empty + buf), ((unit >> 1) - 1) & 1, stop);
+      ok = ok && wait(smem_u32(full + st), (issued / S::kStages) & 1, stop);
+      if (!ok) return;
+      asm volatile("tcgen05.fence::after_thread_sync;");
+      const uint32_t base = smem_u32(smem) + st * S::kStageBytes;
+      const uint64_t a0 = smem_desc(base), b0 = smem_desc(base + kTM * kKB * 2);
+      const uint32_t idesc = (1u << 4) | ((uint32_t)(kTM >> 4) << 24) | ((uint32_t)((c & 0xffff) >> 3) << 17);
+#pragma unroll
+      for (int k = 0; k < kKB / 16; ++k) {
+        const uint32_t acc = slice > 0 || k > 0 ? 1u : 0u;
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(tmem + (uint32_t)(buf * TN)),
+            "l"(a0 + (uint64_t)(k * 2 * kLBO >> 4)), "l"(b0 + (uint64_t)(k * 2 * kLBO >> 4)), "r"(idesc), "r"(acc));
+      }
+      commit(smem_u32(empty + st));
+      ++issued;
+      if (++slice == kChunkK / kKB || (c >> 16)) {
+        commit(smem_u32(acc_full + buf));
+        ++unit;
+        slice = 0;
+      }
+    };
+    int j = 0;
+    for (bool more = true; more;) {
+#pragma unroll
+      for (int a = 0; a < S::kAhead; ++a) {
+        const int c = cols[a], st = j % S::kStages;
+        if (!c || !ok) {
+          more = false;
+          break;
+        }
+        if (j >= S::kStages) ok = __all_sync(0xffffffffu, wait(smem_u32(empty + st), (j / S::kStages - 1) & 1, stop));
+        if (ok) {
+          const uint32_t dst = put + st * S::kStageBytes;
+#pragma unroll
+          for (int i = 0; i < kU; ++i) {
+            const int bi = i - kA;
+            if (i >= kA && row + 64 * bi >= (c & 0xffff)) continue;
+            uint32_t h[8];
+            widen(raw[a][i].x, h[0], h[1]);
+            widen(raw[a][i].y, h[2], h[3]);
+            widen(raw[a][i].z, h[4], h[5]);
+            widen(raw[a][i].w, h[6], h[7]);
+            const uint32_t d = dst + (i < kA ? i * 8 * kSBO : kTM * kKB * 2 + bi * 8 * kSBO);
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d + kLBO), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          load(raw[a], cols[a]);
+        }
+        __syncwarp();
+        if (lane == 0) {
+          if (ok) arrive(smem_u32(full + st));
+          if (lw == 0) {
+            if (j > 0 && ok) issue(pending);
+            pending = c;
+          }
+        }
+        ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+        ++j;
+      }
+    }
+    if (lw == 0 && lane == 0) {
+      if (ok && j > 0) issue(pending);
+      commit(smem_u32(done));  // completes when every MMA issued above has
+    }
+    if (!ok) *stop = 1;
+  } else {
+    // ---------------------------------------------------------------- epilogue
+    if constexpr (TN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpiRegs));
+    constexpr int CW = TN / 2;  // columns of this warp
+    const int quad = warp & 3, c0 = (warp >> 2) * CW;
+    const uint32_t trow = tmem + ((uint32_t)(32 * quad) << 16) + c0;
+    T *y = (T *)p.y;
+    int unit = 0;
+    Tile t{(int64_t)blockIdx.x, 0, 0, 0, 0, false};
+    for (;; t.tile += gridDim.x) {
+      seek(p, TN, nct, t);
+      if (!t.have) break;
+      const int n = t.n0 + 32 * quad + lane, nr = (int)(t.r1 - t.r0);
+      const bool mine = n < p.N;
+      if (t.e == p.nexp) {
+        if (mine)
+          for (int c = c0; c < min(nr, c0 + CW); ++c) put_out(y + (t.r0 + c) * p.N + n, 0.0f);
+        continue;
+      }
+      const float sw = mine ? __ldg(p.sw + (int64_t)t.e * p.N + n) : 0.0f;
+      const float bias = mine && p.bias ? __ldg(p.bias + (int64_t)t.e * p.N + n) : 0.0f;
+      const int chunks = (nkb * kKB + kChunkK - 1) / kChunkK;
+      if (chunks > 1) {
+        int sum[CW];
+#pragma unroll
+        for (int i = 0; i < CW; ++i) sum[i] = 0;
+#pragma unroll 1
+        for (int c = 0; c < chunks; ++c, ++unit) {
+          ok = __all_sync(0xffffffffu, ok && wait(smem_u32(acc_full + (unit & 1)), (unit >> 1) & 1, stop));
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;");
+          const uint32_t col = trow + (unit & 1) * TN;
+#pragma unroll
+          for (int g = 0; g < CW; g += 16) {
+            float v[16];
+            tmem_ld(col + g, v);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[g + i] += __float2int_rn(v[i]);
+          }
+          if (c == chunks - 1) {
+#pragma unroll
+            for (int g = 0; g < CW; g += 16) {
+              float v[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) v[i] = __int2float_rn(sum[g + i]);
+              tmem_st(col + g, v);
+            }
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            break;  // the buffer is released below
+          }
+          asm volatile("tcgen05.fence::before_thread_sync;");
+          __syncwarp();
+          if (lane == 0) arrive(smem_u32(acc_empty + (unit & 1)));
+        }
+      } else {
+        ok = __all_sync(0xffffffffu, ok && wait(smem_u32(acc_full + (unit & 1)), (unit >> 1) & 1, stop));
+        asm volatile("tcgen05.fence::after_thread_sync;");
+      }
+#pragma unroll 1
+      for (int g = 0; g < CW && c0 + g < nr; g += 16) {
+        float v[16];
+        if (ok) tmem_ld(trow + (unit & 1) * TN + g, v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int c = c0 + g + i;
+          if (c < nr && mine) {
+            float o = fmaf(v[i] * __ldg(p.sx + t.r0 + c), sw, bias);
+            if (p.act == DP_ACT_TANH) o = tanhf(o);
+            put_out(y + (t.r0 + c) * p.N + n, ok ? o : __uint_as_float(0x7fc00000u));
+          }
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;");
+      __syncwarp();
+      if (lane == 0) arrive(smem_u32(acc_empty + (unit & 1)));
+      ++unit;
+    }
+    if (!ok) *stop = 1;
+  }
+  __syncwarp();
+  __syncthreads();
+  ok = wait(smem_u32(done), 0, nullptr) && !*stop;  // no MMA is in flight when the accumulators go
+  if (__syncthreads_and(ok) == 0 && threadIdx.x == 0) atomicAdd(&g_timeouts, 1u);
+  asm volatile("tcgen05.fence::after_thread_sync;");
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmemCols));
+}
+
+template <typename T, int TN>
+int launch_tc(const I8Args &p, int64_t row_tiles, cudaStream_t st, const char *who) {
+  auto k = linear_i8_tc_kernel<T, TN>;
+  cudaFuncAttributes a{};
+  cudaError_t e = cudaFuncGetAttributes(&a, k);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<TN>::kSmem);
+  if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+  const int regs = a.numRegs;
+  // the epilogue's registers come out of what the block is launched with
+  if (TN == 256 && regs * (kEpiWarps + kLoadWarps) < kEpiWarps * kEpiRegs + kLoadWarps * kLoadRegs)
+    return set_error(DP_ERR_CUDA, "%s: kernel of %d registers", who, regs);
+  const int64_t tiles = row_tiles * ((p.N + kTM - 1) / kTM);
+  k<<<(unsigned)(tiles < 152 ? tiles : 152), kThreads, Shape<TN>::kSmem, st>>>(p);
+  return DP_OK;
+}
+}  // namespace i8
+
 template <typename T>
 int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int K, int8_t *xq, float *sx,
                void *stream, const char *who) {
@@ -221,13 +565,34 @@ int linear(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t 
   if (!xq || !sx || !wq || !sw || !y) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (((uintptr_t)xq | (uintptr_t)wq) & 15) return set_error(DP_ERR_SHAPE, "%s: xq or wq is not 16-byte aligned", who);
   const I8Args p{xq, wq, sx, sw, bias, start, rows, K, N, nexp, act, y};
-  const int64_t tiles = (rows + kFewRows - 1) / kFewRows + (start ? (nexp + 1 < rows ? nexp + 1 : rows) : 0);
-  const dim3 grid((unsigned)tiles, (N + kFewWarps - 1) / kFewWarps);
-  linear_i8_few_kernel<T><<<grid, kFewWarps * 32, 0, (cudaStream_t)stream>>>(p);
+  const cudaStream_t st = (cudaStream_t)stream;
+  const int64_t pieces = start ? (nexp + 1 < rows ? nexp + 1 : rows) : 0;  // a tile more for each expert's remainder
+  auto tiles = [&](int R) { return (rows + R - 1) / R + pieces; };
+  if (rows <= 16) {
+    const dim3 grid((unsigned)tiles(kFewRows), (N + kFewWarps - 1) / kFewWarps);
+    linear_i8_few_kernel<T><<<grid, kFewWarps * 32, 0, st>>>(p);
+  } else {
+    const int64_t each = rows / nexp;
+    int rc = each > 128 ? i8::launch_tc<T, 256>(p, tiles(256), st, who)
+             : each > 64 ? i8::launch_tc<T, 128>(p, tiles(128), st, who)
+                         : i8::launch_tc<T, 64>(p, tiles(64), st, who);
+    if (rc) return rc;
+  }
   return launch_status(who);
 }
 
 }  // namespace
+
+int take_wait_timeouts_linear_i8(unsigned int *count) {
+  unsigned int v = 0, zero = 0;
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&v, i8::g_timeouts, sizeof v);
+  if (e == cudaSuccess) e = cudaMemcpyToSymbol(i8::g_timeouts, &zero, sizeof zero);
+  if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "dp_tc_wait_timeouts: %s", cudaGetErrorString(e));
+  *count += v;
+  return DP_OK;
+}
+
 }  // namespace dpc
 
 extern "C" {
