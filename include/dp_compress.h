@@ -788,19 +788,28 @@ int dp_quant_rows_i8_f16(const uint16_t *x, const int32_t *src, const int32_t *p
  *         zero rows.  NULL with nexp = 1: all rows
  *   act   DP_ACT_NONE or DP_ACT_TANH
  *   y     [rows][N]
+ *   work, work_bytes  device scratch, 16-byte aligned, at least
+ *         dp_linear_i8_work_bytes(rows, K, N, nexp) bytes; that is 0, and work may
+ *         be NULL, unless there are many rows an expert (then the weights are
+ *         widened to fp16 once a call)
  * xq and wq are 16-byte aligned.  rows == 0 reads no device pointer.  Errors:
  * DP_ERR_NULL, DP_ERR_SHAPE, DP_ERR_UNSUPPORTED (K above 65536), DP_ERR_CUDA.
  */
 #define DP_ACT_NONE 0
 #define DP_ACT_TANH 1
+size_t dp_linear_i8_work_bytes(int64_t rows, int K, int N, int nexp);
 int dp_linear_i8_f64(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t *wq, const float *sw,
-                     const float *bias, int nexp, int N, const int64_t *start, int act, double *y, void *stream);
+                     const float *bias, int nexp, int N, const int64_t *start, int act, double *y, void *work,
+                     size_t work_bytes, void *stream);
 int dp_linear_i8_f32(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t *wq, const float *sw,
-                     const float *bias, int nexp, int N, const int64_t *start, int act, float *y, void *stream);
+                     const float *bias, int nexp, int N, const int64_t *start, int act, float *y, void *work,
+                     size_t work_bytes, void *stream);
 int dp_linear_i8_bf16(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t *wq, const float *sw,
-                      const float *bias, int nexp, int N, const int64_t *start, int act, uint16_t *y, void *stream);
+                     const float *bias, int nexp, int N, const int64_t *start, int act, uint16_t *y, void *work,
+                     size_t work_bytes, void *stream);
 int dp_linear_i8_f16(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t *wq, const float *sw,
-                     const float *bias, int nexp, int N, const int64_t *start, int act, uint16_t *y, void *stream);
+                     const float *bias, int nexp, int N, const int64_t *start, int act, uint16_t *y, void *work,
+                     size_t work_bytes, void *stream);
 
 /*
  * The norms around a block with its gate and residual scale.  For each token,

@@ -156,6 +156,7 @@ _SIGS = {
                                ctypes.c_int),
     "dp_route_work_bytes": ([_I64, ctypes.c_int, ctypes.c_int], ctypes.c_size_t),
     "dp_route_plan": ([_P, _I64, ctypes.c_int, ctypes.c_int, _P, _P, _P, _P, ctypes.c_size_t, _P], ctypes.c_int),
+    "dp_linear_i8_work_bytes": ([_I64, ctypes.c_int, ctypes.c_int, ctypes.c_int], ctypes.c_size_t),
     "dp_norm_gate_work_bytes": ([ctypes.c_int, ctypes.c_int], ctypes.c_size_t),
     **{f"{name}_{x}": (args, ctypes.c_int) for x in ("f64", "f32", "bf16", "f16") for name, args in (
         ("dp_route_gather", [_P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _P]),
@@ -163,7 +164,7 @@ _SIGS = {
         ("dp_route_combine_grad", [_P, _P, _P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _P, _P]),
         ("dp_quant_rows_i8", [_P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _P, _P]),
         ("dp_linear_i8", [_P, _P, _I64, ctypes.c_int, _P, _P, _P, ctypes.c_int, ctypes.c_int, _P, ctypes.c_int, _P,
-                          _P]),
+                          _P, ctypes.c_size_t, _P]),
         ("dp_norm_gate_fwd", [_P, _P, _P, ctypes.c_int, _P, _P, _P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _D, _P,
                               _P, _P, _P]),
         ("dp_norm_gate_grad", [_P, _P, _P, ctypes.c_int, _P, _P, _P, _P, _P, _P, _P, _I64, ctypes.c_int, ctypes.c_int,
@@ -1068,10 +1069,16 @@ def dp_quant_rows_i8(x, src=None, pos=None, out=None):
 _ACTS = {None: 0, "tanh": 1}
 
 
-def dp_linear_i8(xq, sx, wq, sw, bias=None, start=None, act=None, dtype=torch.float32, out=None):
+def dp_linear_i8_work_bytes(rows, K, N, nexp) -> int:
+    """Bytes of device scratch dp_linear_i8 needs (0 for few rows)."""
+    return int(_lib.dp_linear_i8_work_bytes(int(rows), int(K), int(N), int(nexp)))
+
+
+def dp_linear_i8(xq, sx, wq, sw, bias=None, start=None, act=None, dtype=torch.float32, out=None, work=None):
     """y [rows][N] of dtype: act(float(xq wq^T) sx sw + bias), the integer product exact; xq [rows][K] and sx
     from dp_quant_rows_i8, wq int8 [nexp][N][K] with sw, bias f32 [nexp][N]; start [nexp+1] a plan's (rows past
-    start[nexp] become zeros), None with one expert for all rows; act None or "tanh"."""
+    start[nexp] become zeros), None with one expert for all rows; act None or "tanh"; work: a uint8 CUDA tensor of
+    dp_linear_i8_work_bytes(rows, K, N, nexp) bytes, or None to allocate what is needed."""
     xq = _dev(xq, "xq", torch.int8)
     wq = _dev(wq, "wq", torch.int8)
     if xq.dim() != 2 or wq.dim() != 3 or xq.shape[1] != wq.shape[2]:
@@ -1089,10 +1096,15 @@ def dp_linear_i8(xq, sx, wq, sw, bias=None, start=None, act=None, dtype=torch.fl
     if start is not None:
         _dev(start, "start", torch.int64, (nexp + 1,))
     y = _out(out, "out", dtype, (rows, N), xq)
-    _same_device(xq, sx, wq, sw, bias, start, y)
-    _check(getattr(_lib, f"dp_linear_i8_{_ROW_SUFFIX[dtype]}")(_ptr(xq), _ptr(sx), rows, K, _ptr(wq), _ptr(sw),
-                                                              _ptr(bias), nexp, N, _ptr(start), _ACTS[act], _ptr(y),
-                                                              _stream(xq)))
+    if work is None:
+        need = dp_linear_i8_work_bytes(rows, K, N, nexp)
+        work = torch.empty((need,), dtype=torch.uint8, device=xq.device) if need else None
+    else:
+        work = _dev(work, "work", torch.uint8)
+    _same_device(xq, sx, wq, sw, bias, start, y, work)
+    _check(getattr(_lib, f"dp_linear_i8_{_ROW_SUFFIX[dtype]}")(
+        _ptr(xq), _ptr(sx), rows, K, _ptr(wq), _ptr(sw), _ptr(bias), nexp, N, _ptr(start), _ACTS[act], _ptr(y),
+        _ptr(work), 0 if work is None else work.numel(), _stream(xq)))
     return y
 
 

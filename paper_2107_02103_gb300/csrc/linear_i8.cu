@@ -89,9 +89,9 @@ struct I8Args {
   const int8_t *xq, *wq;
   const float *sx, *sw, *bias;
   const int64_t *start;  // [nexp + 1], or NULL: one expert for all rows
-  int64_t rows;
-  int K, N, nexp, act;
+  int rows, K, N, nexp, act;
   void *y;
+  unsigned char *image;  // the wide form's weights (linear_i8_tc_kernel)
 };
 
 template <typename T>
@@ -102,35 +102,37 @@ __device__ __forceinline__ void put_out(T *y, float v) {
 
 // Row tile `tile` of the sorted rows cut into tiles of at most R rows that lie in one expert: the expert (nexp for
 // the rows past start[nexp]) and its rows [r0, r1).  A warp looks at 32 experts at a time.
-__device__ __forceinline__ bool find_tile(const I8Args &p, int64_t tile, int R, int &e, int64_t &r0, int64_t &r1) {
+__device__ __forceinline__ bool find_tile(const I8Args &p, int tile, int R, int &e, int &r0, int &r1) {
+  const int rows = p.rows;
   if (!p.start) {
+    if (tile >= (rows + R - 1) / R) return false;
     e = 0;
     r0 = tile * R;
-    r1 = min(r0 + R, p.rows);
-    return r0 < p.rows;
+    r1 = min(R, rows - r0) + r0;
+    return true;
   }
   const int lane = threadIdx.x & 31;
-  int64_t before = 0;
+  int before = 0;
   for (int e0 = 0; e0 <= p.nexp; e0 += 32) {
     const int k = e0 + lane;
-    int64_t lo = 0, hi = 0;
+    int lo = 0, hi = 0;
     if (k <= p.nexp) {
-      lo = k ? min(max(__ldg(p.start + k), (int64_t)0), p.rows) : 0;
-      hi = k < p.nexp ? min(max(__ldg(p.start + k + 1), lo), p.rows) : p.rows;
+      lo = k ? (int)min(max(__ldg(p.start + k), (int64_t)0), (int64_t)rows) : 0;
+      hi = k < p.nexp ? (int)min(max(__ldg(p.start + k + 1), (int64_t)lo), (int64_t)rows) : rows;
     }
-    const int64_t mine = (hi - lo + R - 1) / R;
-    int64_t inc = mine;
+    const int mine = (hi - lo + R - 1) / R;
+    int inc = mine;
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
+      const int up = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += up;
     }
     const unsigned hit = __ballot_sync(0xffffffffu, before + inc > tile);
     if (hit) {
       const int who = __ffs(hit) - 1;
-      const int64_t first = lo + (tile - (before + inc - mine)) * R;
+      const int first = lo + (tile - (before + inc - mine)) * R;
       e = e0 + who;
       r0 = __shfl_sync(0xffffffffu, first, who);
-      r1 = min(r0 + R, __shfl_sync(0xffffffffu, hi, who));
+      r1 = min(R, __shfl_sync(0xffffffffu, hi, who) - r0) + r0;
       return true;
     }
     before += __shfl_sync(0xffffffffu, inc, 31);
@@ -144,17 +146,16 @@ constexpr int kFewWarps = 8, kFewRows = 8;
 // products an instruction.
 template <typename T>
 __global__ void __launch_bounds__(kFewWarps * 32) linear_i8_few_kernel(const I8Args p) {
-  int e;
-  int64_t r0, r1;
+  int e, r0, r1;
   if (!find_tile(p, blockIdx.x, kFewRows, e, r0, r1)) return;
-  const int lane = threadIdx.x & 31, n = blockIdx.y * kFewWarps + (threadIdx.x >> 5), nr = (int)(r1 - r0);
+  const int lane = threadIdx.x & 31, n = blockIdx.y * kFewWarps + (threadIdx.x >> 5), nr = r1 - r0;
   if (n >= p.N) return;
   T *y = (T *)p.y;
   if (e == p.nexp) {
-    if (lane < nr) put_out(y + (r0 + lane) * p.N + n, 0.0f);
+    if (lane < nr) put_out(y + (int64_t)(r0 + lane) * p.N + n, 0.0f);
     return;
   }
-  const int8_t *w = p.wq + ((int64_t)e * p.N + n) * p.K, *x = p.xq + r0 * p.K;
+  const int8_t *w = p.wq + ((int64_t)e * p.N + n) * p.K, *x = p.xq + (int64_t)r0 * p.K;
   int acc[kFewRows] = {};
   for (int k = lane * 16; k < p.K; k += 512) {
     const int4 a = __ldg(reinterpret_cast<const int4 *>(w + k));
@@ -175,7 +176,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_i8_few_kernel(const I8A
     const int64_t c = (int64_t)e * p.N + n;
     float v = fmaf((float)mine * __ldg(p.sx + r0 + lane), __ldg(p.sw + c), p.bias ? __ldg(p.bias + c) : 0.0f);
     if (p.act == DP_ACT_TANH) v = tanhf(v);
-    put_out(y + (r0 + lane) * p.N + n, v);
+    put_out(y + (int64_t)(r0 + lane) * p.N + n, v);
   }
 }
 
@@ -185,29 +186,36 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_i8_few_kernel(const I8A
 // integers slowly; fp16 holds them exactly, and fp32 sums of their products are exact while K <= 1024
 // (1024 * 2^14 = 2^24): longer K is cut into chunks of 1024 whose sums are added as int32.
 //   Loader warps read the 8-bit rows from global memory into registers two stages ahead, turn them into fp16
-//   (byte q + 128 under the exponent of 1024, less 1152) and write the stage's operands, K-major core matrices of
-//   8 rows x 16 bytes without swizzle; lanes lie along the rows, so that a store's eight lanes fill one core matrix.
-//   Lane 0 of the first loader warp issues a stage's MMAs (M 128, K 16 each) one stage behind.
+//   (byte q + 128 under the exponent of 1024, less 1152) and write the stage's operands, K-major rows of 128 bytes in
+//   the 128-byte swizzle: four neighbouring lanes read 64 bytes of a row (lanes along rows instead would cost an L1
+//   access each: 2.6 times the time of a stage), and the swizzle spreads their stores over all banks.
+//   One lane of a warp of its own issues a stage's MMAs (M 128, K 16 each).
 //   Epilogue warps (two per TMEM lane quadrant, half the columns each) keep the chunks' int32 sums in registers and
 //   finish a tile while the next one runs in the other TMEM buffer.
 // A block per SM walks the tiles; every wait is bounded, a block that gives up writes NaN and is counted.
 namespace i8 {
 constexpr int kTM = 128, kKB = 64, kChunkK = 1024;
-constexpr int kEpiWarps = 8, kLoadWarps = 8, kThreads = (kEpiWarps + kLoadWarps) * 32;
-constexpr int kEpiRegs = 168, kLoadRegs = 88;  // of the 128 a thread is launched with
-static_assert(kEpiWarps * kEpiRegs + kLoadWarps * kLoadRegs <= (kEpiWarps + kLoadWarps) * 128, "register split");
-constexpr uint32_t kLBO = 128, kSBO = 1024;  // next core matrix along K, next 8 rows
+constexpr int kEpiWarps = 8;
+// The wide form's warpgroups move registers from the loaders and the last group to the epilogue's 128 sums; the
+// shares of a scheduler's five warps come to what they were launched with.
+constexpr int kRegs = 96, kEpiRegs = 152, kLoadRegs = 72, kMmaRegs = 32;
+static_assert(2 * kEpiRegs + 2 * kLoadRegs + kMmaRegs <= 5 * kRegs, "register split");
+constexpr uint32_t kRowBytes = kKB * 2, kSBO = 8 * kRowBytes;  // a slice's row; the next 8 rows
 
 __device__ unsigned int g_timeouts;
 
 template <int TN>
 struct Shape {
-  static constexpr int kStageBytes = (kTM + TN) * kKB * 2;
-  static constexpr int kStages = TN == 256 ? 4 : 6;
-  static constexpr int kAhead = TN == 256 ? 2 : TN == 128 ? 3 : 4;  // stages held in a loader's registers
+  static constexpr bool kWide = TN == 256;  // weights come widened, by bulk copies
+  // the narrow forms' 13 warps leave 128 registers a thread
+  static constexpr int kLoadWarps = kWide ? 8 : 4, kMmaWarp = kEpiWarps + kLoadWarps;
+  static constexpr int kThreads = (kMmaWarp + (kWide ? 4 : 1)) * 32;
+  static constexpr int kStageA = kTM * kKB * 2, kStageBytes = kStageA + TN * kKB * 2;
+  static constexpr int kStages = kWide ? 4 : 6;
+  static constexpr int kAhead = TN == 64 ? 3 : 2;  // stages held in a loader's registers
   static constexpr uint32_t kTmemCols = 2 * TN;
-  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + (2 * kStages + 5) * 8 + 16;
-  static_assert(kSmem <= 227 * 1024 && TN % 32 == 0 && 2 * TN <= 512 && 2 * TN >= 32, "tile");
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (2 * kStages + 5) * 8 + 16;  // aligned within
+  static_assert(kSmem <= 227 * 1024 && TN % 64 == 0 && TN <= 256, "tile");
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -229,9 +237,11 @@ __device__ __forceinline__ void arrive(uint32_t bar) {
 __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ uint64_t smem_desc(uint32_t saddr) {  // K-major, no swizzle, version 1
-  return (uint64_t)((saddr & 0x3FFFF) >> 4) | ((uint64_t)(kLBO >> 4) << 16) | ((uint64_t)(kSBO >> 4) << 32) | (1ull << 46);
+__device__ __forceinline__ uint64_t smem_desc(uint32_t saddr) {  // K-major, 128-byte swizzle, version 1
+  return (uint64_t)((saddr & 0x3FFFF) >> 4) | (1ull << 16) | ((uint64_t)(kSBO >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
+// Byte of the 16-byte chunk c of row r in an operand whose first byte is 1024-byte aligned.
+__device__ __forceinline__ uint32_t chunk_at(int r, int c) { return r * kRowBytes + ((c ^ (r & 7)) << 4); }
 
 // Four int8 as two fp16 pairs.
 __device__ __forceinline__ void widen(uint32_t q, uint32_t &lo, uint32_t &hi) {
@@ -244,37 +254,31 @@ __device__ __forceinline__ void widen(uint32_t q, uint32_t &lo, uint32_t &hi) {
 
 // Where a role stands: the tile, and the expert, rows and channels it means.
 struct Tile {
-  int64_t tile, r0, r1;
-  int e, n0;
+  int tile, r0, r1, e, n0;
   bool have;
 };
 __device__ __forceinline__ void seek(const I8Args &p, int TN, int nct, Tile &t) {
-  const int64_t rt = t.tile / nct;
-  t.n0 = (int)(t.tile - rt * nct) * kTM;
+  const int rt = t.tile / nct;
+  t.n0 = (t.tile - rt * nct) * kTM;
   t.have = find_tile(p, rt, TN, t.e, t.r0, t.r1);
 }
 
-template <int W>
-__device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[W]) {
-  static_assert(W == 16, "width");
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
-        "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
-      : "r"(addr));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+__device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+               : "r"(addr));
 }
-__device__ __forceinline__ void tmem_st(uint32_t addr, const float (&v)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
-      "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
-      "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]));
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st(uint32_t addr, const float (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "f"(v[0]), "f"(v[1]),
+               "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
 }
 
 template <typename T, int TN>
-__global__ void __launch_bounds__(kThreads, 1) linear_i8_tc_kernel(const I8Args p) {
+__global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(const I8Args p) {
   using S = Shape<TN>;
-  extern __shared__ __align__(1024) unsigned char smem[];
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
   uint64_t *full = reinterpret_cast<uint64_t *>(smem + S::kStages * S::kStageBytes), *empty = full + S::kStages;
   uint64_t *acc_full = empty + S::kStages, *acc_empty = acc_full + 2, *done = acc_empty + 2;
   uint32_t *holder = reinterpret_cast<uint32_t *>(done + 1);
@@ -285,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_i8_tc_kernel(const I8Args 
   if (threadIdx.x == 0) {
     auto init = [](uint64_t *b, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(n)); };
     for (int s = 0; s < S::kStages; ++s) {
-      init(full + s, kLoadWarps);
+      init(full + s, S::kLoadWarps + (S::kWide ? 1 : 0));
       init(empty + s, 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -307,167 +311,213 @@ __global__ void __launch_bounds__(kThreads, 1) linear_i8_tc_kernel(const I8Args 
   const uint32_t tmem = *holder;
   bool ok = true;
 
-  if (warp >= kEpiWarps) {
-    // ---------------------------------------------------------------- loaders, and the MMAs
-    if constexpr (TN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
-    constexpr int kA = kTM / 64, kB = TN / 64 ? TN / 64 : 1, kU = kA + kB;
-    const int lw = warp - kEpiWarps, r8 = lane & 7, kp = lane >> 3, row = lw * 8 + r8;
-    const uint32_t put = smem_u32(smem) + lw * kSBO + kp * 2 * kLBO + r8 * 16;
-    Tile at{(int64_t)blockIdx.x, 0, 0, 0, 0, false};  // the tile the loads stand at
-    int kb = 0;                                       // and its slice
-    auto next_tile = [&] {  // to the next tile with work
-      do {
-        seek(p, TN, nct, at);
-        if (at.have && at.e < p.nexp) return;
-        at.tile += gridDim.x;
-      } while (at.have);
+  if (warp > S::kMmaWarp) {
+    // ---------------------------------------------------------------- wide form: the weights' copies, two idle warps
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
+    if (warp == S::kMmaWarp + 1) {
+      int st = 0, phase = 1;
+      Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
+      for (; ok; t.tile += gridDim.x) {
+        seek(p, TN, nct, t);
+        if (!t.have) break;
+        if (t.e == p.nexp) continue;
+        const unsigned char *src = p.image + ((int64_t)t.e * nct + t.n0 / kTM) * nkb * S::kStageA;
+        if (lane == 0) {
+          for (int kb = 0; kb < nkb; ++kb) {
+            ok = wait(smem_u32(empty + st), phase, stop);
+            if (!ok) break;
+            const uint32_t bar = smem_u32(full + st);
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)S::kStageA)
+                         : "memory");
+            asm volatile(
+                "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                    smem_u32(smem) + st * S::kStageBytes),
+                "l"(src + (int64_t)kb * S::kStageA), "r"((uint32_t)S::kStageA), "r"(bar)
+                : "memory");
+            if (++st == S::kStages) {
+              st = 0;
+              phase ^= 1;
+            }
+          }
+        }
+        ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+      }
+      if (!ok) *stop = 1;
+    }
+  } else if (warp == S::kMmaWarp) {
+    // ---------------------------------------------------------------- the MMAs
+    if constexpr (S::kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
+    int j = 0, unit = 0;  // stages, accumulator uses
+    Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
+    for (; ok; t.tile += gridDim.x) {
+      seek(p, TN, nct, t);
+      if (!t.have) break;
+      if (t.e == p.nexp) continue;
+      const uint32_t cols = (uint32_t)(t.r1 - t.r0 + 15) / 16 * 16;
+      const uint32_t idesc = (1u << 4) | ((uint32_t)(kTM >> 4) << 24) | ((cols >> 3) << 17);
+      if (lane == 0) {
+        for (int kb = 0; kb < nkb && ok; ++kb, ++j) {
+          const int st = j % S::kStages, buf = unit & 1, slice = kb % (kChunkK / kKB);
+          if (slice == 0 && unit >= 2) ok = wait(smem_u32(acc_empty + buf), ((unit >> 1) - 1) & 1, stop);
+          ok = ok && wait(smem_u32(full + st), (j / S::kStages) & 1, stop);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;");
+          const uint32_t base = smem_u32(smem) + st * S::kStageBytes;
+          const uint64_t a0 = smem_desc(base), b0 = smem_desc(base + S::kStageA);
+#pragma unroll
+          for (int k = 0; k < kKB / 16; ++k) {
+            const uint32_t acc = slice > 0 || k > 0 ? 1u : 0u;
+            asm volatile(
+                "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+                " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(tmem + (uint32_t)(buf * TN)),
+                "l"(a0 + (uint64_t)(k * 2)), "l"(b0 + (uint64_t)(k * 2)), "r"(idesc), "r"(acc));
+          }
+          commit(smem_u32(empty + st));
+          if (slice == kChunkK / kKB - 1 || kb == nkb - 1) {
+            commit(smem_u32(acc_full + buf));
+            ++unit;
+          }
+        }
+      }
+      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    }
+    if (lane == 0) commit(smem_u32(done));  // completes when every MMA issued above has
+    if (!ok) *stop = 1;
+  } else if (warp >= kEpiWarps) {
+    // ---------------------------------------------------------------- loaders
+    if constexpr (S::kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
+    constexpr int kLR = S::kLoadWarps * 8;  // rows the loaders cover at once
+    constexpr int kA = S::kWide ? 0 : kTM / kLR, kB = TN / kLR, kU = kA + kB;
+    const int kp = lane & 3, row = (warp - kEpiWarps) * 8 + (lane >> 2);
+    const uint32_t put = smem_u32(smem), put0 = chunk_at(row, 2 * kp), put1 = chunk_at(row, 2 * kp + 1);
+    int tile = blockIdx.x, k = 0;             // where the loads stand: the tile, this thread's column in it,
+    int now = 0;                              // its columns (rows of x, whole sixteens), 0 past the last tile,
+    uint32_t rows = 0;                        // which of this thread's rows exist,
+    const int8_t *w = nullptr, *x = nullptr;  // and its first row of either operand at column k
+    const int step = kLR * p.K;               // bytes to the thread's next row
+    auto next_tile = [&] {                    // to the next tile with work, from `tile` on
+      now = 0;
+      for (;; tile += gridDim.x) {
+        Tile t{tile, 0, 0, 0, 0, false};
+        seek(p, TN, nct, t);
+        if (!t.have) return;
+        if (t.e == p.nexp) continue;
+        k = kp * 16;
+        if constexpr (kA > 0) w = p.wq + ((int64_t)t.e * p.N + t.n0 + row) * p.K + k;
+        x = p.xq + (int64_t)(t.r0 + row) * p.K + k;
+        rows = 0;
+#pragma unroll
+        for (int i = 0; i < kU; ++i)
+          rows |= (uint32_t)(i < kA ? t.n0 + row + kLR * i < p.N : row + kLR * (i - kA) < t.r1 - t.r0) << i;
+        now = (t.r1 - t.r0 + 15) / 16 * 16;
+        return;
+      }
     };
     next_tile();
     uint4 raw[S::kAhead][kU];
-    int cols[S::kAhead];  // columns (rows of x) of the stage, 0 past the last tile; the tile's last slice: + 1 << 16
+    int cols[S::kAhead];
     auto load = [&](uint4 (&r)[kU], int &c) {
-      c = 0;
-      if (!at.have) return;
-      const int k = kb * kKB + kp * 16, nr = (int)(at.r1 - at.r0);
-      const uint4 zero = make_uint4(0, 0, 0, 0);
-      const int8_t *w = p.wq + ((int64_t)at.e * p.N + at.n0 + row) * p.K + k, *x = p.xq + (at.r0 + row) * p.K + k;
+      c = now;
+      if (!now) return;
+      const uint32_t m = k < p.K ? rows : 0u;
 #pragma unroll
-      for (int i = 0; i < kA; ++i)
-        r[i] = k < p.K && at.n0 + row + 64 * i < p.N ? __ldg(reinterpret_cast<const uint4 *>(w + (int64_t)64 * i * p.K)) : zero;
-#pragma unroll
-      for (int i = 0; i < kB; ++i)
-        r[kA + i] = k < p.K && row + 64 * i < nr ? __ldg(reinterpret_cast<const uint4 *>(x + (int64_t)64 * i * p.K)) : zero;
-      c = (nr + 15) / 16 * 16;
-      if (++kb == nkb) {
-        kb = 0;
-        c |= 1 << 16;
-        at.tile += gridDim.x;
+      for (int i = 0; i < kU; ++i) {
+        r[i] = make_uint4(0, 0, 0, 0);
+        if (m >> i & 1) r[i] = __ldg(reinterpret_cast<const uint4 *>((i < kA ? w : x) + (int64_t)step * (i < kA ? i : i - kA)));
+      }
+      k += kKB;
+      if constexpr (kA > 0) w += kKB;
+      x += kKB;
+      if (k - kp * 16 >= p.K) {
+        tile += gridDim.x;
         next_tile();
       }
     };
 #pragma unroll
     for (int a = 0; a < S::kAhead; ++a) load(raw[a], cols[a]);
-    // the MMA issuer's position: one stage behind the loader's
-    int issued = 0, unit = 0, slice = 0, pending = 0;  // stages issued; accumulator uses; slice in the chunk
-    auto issue = [&](int c) {  // stage `issued`, c as cols[]
-      const int st = issued % S::kStages, buf = unit & 1;
-      if (slice == 0 && unit >= 2) ok = ok && wait(smem_u32(acc_empty + buf), ((unit >> 1) - 1) & 1, stop);
-      ok = ok && wait(smem_u32(full + st), (issued / S::kStages) & 1, stop);
-      if (!ok) return;
-      asm volatile("tcgen05.fence::after_thread_sync;");
-      const uint32_t base = smem_u32(smem) + st * S::kStageBytes;
-      const uint64_t a0 = smem_desc(base), b0 = smem_desc(base + kTM * kKB * 2);
-      const uint32_t idesc = (1u << 4) | ((uint32_t)(kTM >> 4) << 24) | ((uint32_t)((c & 0xffff) >> 3) << 17);
-#pragma unroll
-      for (int k = 0; k < kKB / 16; ++k) {
-        const uint32_t acc = slice > 0 || k > 0 ? 1u : 0u;
-        asm volatile(
-            "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-            " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(tmem + (uint32_t)(buf * TN)),
-            "l"(a0 + (uint64_t)(k * 2 * kLBO >> 4)), "l"(b0 + (uint64_t)(k * 2 * kLBO >> 4)), "r"(idesc), "r"(acc));
-      }
-      commit(smem_u32(empty + st));
-      ++issued;
-      if (++slice == kChunkK / kKB || (c >> 16)) {
-        commit(smem_u32(acc_full + buf));
-        ++unit;
-        slice = 0;
-      }
-    };
-    int j = 0;
+    int st = 0, phase = 1;  // the stage, and the parity of its "empty" barrier (the first round passes)
     for (bool more = true; more;) {
 #pragma unroll
       for (int a = 0; a < S::kAhead; ++a) {
-        const int c = cols[a], st = j % S::kStages;
-        if (!c || !ok) {
+        if (!cols[a] || !ok) {
           more = false;
           break;
         }
-        if (j >= S::kStages) ok = __all_sync(0xffffffffu, wait(smem_u32(empty + st), (j / S::kStages - 1) & 1, stop));
+        ok = __all_sync(0xffffffffu, wait(smem_u32(empty + st), phase, stop));
         if (ok) {
           const uint32_t dst = put + st * S::kStageBytes;
 #pragma unroll
           for (int i = 0; i < kU; ++i) {
-            const int bi = i - kA;
-            if (i >= kA && row + 64 * bi >= (c & 0xffff)) continue;
+            if (i >= kA && row + kLR * (i - kA) >= cols[a]) continue;
             uint32_t h[8];
             widen(raw[a][i].x, h[0], h[1]);
             widen(raw[a][i].y, h[2], h[3]);
             widen(raw[a][i].z, h[4], h[5]);
             widen(raw[a][i].w, h[6], h[7]);
-            const uint32_t d = dst + (i < kA ? i * 8 * kSBO : kTM * kKB * 2 + bi * 8 * kSBO);
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d + kLBO), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
+            const uint32_t d = dst + (i < kA ? i * (kLR / 8) * kSBO : S::kStageA + (i - kA) * (kLR / 8) * kSBO);
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d + put0), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d + put1), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) arrive(smem_u32(full + st));
           load(raw[a], cols[a]);
-        }
-        __syncwarp();
-        if (lane == 0) {
-          if (ok) arrive(smem_u32(full + st));
-          if (lw == 0) {
-            if (j > 0 && ok) issue(pending);
-            pending = c;
+          if (++st == S::kStages) {
+            st = 0;
+            phase ^= 1;
           }
         }
-        ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
-        ++j;
       }
-    }
-    if (lw == 0 && lane == 0) {
-      if (ok && j > 0) issue(pending);
-      commit(smem_u32(done));  // completes when every MMA issued above has
     }
     if (!ok) *stop = 1;
   } else {
     // ---------------------------------------------------------------- epilogue
-    if constexpr (TN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpiRegs));
+    if constexpr (S::kWide) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpiRegs));
     constexpr int CW = TN / 2;  // columns of this warp
     const int quad = warp & 3, c0 = (warp >> 2) * CW;
     const uint32_t trow = tmem + ((uint32_t)(32 * quad) << 16) + c0;
     T *y = (T *)p.y;
     int unit = 0;
-    Tile t{(int64_t)blockIdx.x, 0, 0, 0, 0, false};
+    Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
     for (;; t.tile += gridDim.x) {
       seek(p, TN, nct, t);
       if (!t.have) break;
-      const int n = t.n0 + 32 * quad + lane, nr = (int)(t.r1 - t.r0);
+      const int n = t.n0 + 32 * quad + lane, nr = t.r1 - t.r0;
       const bool mine = n < p.N;
       if (t.e == p.nexp) {
         if (mine)
-          for (int c = c0; c < min(nr, c0 + CW); ++c) put_out(y + (t.r0 + c) * p.N + n, 0.0f);
+          for (int c = c0; c < min(nr, c0 + CW); ++c) put_out(y + (int64_t)(t.r0 + c) * p.N + n, 0.0f);
         continue;
       }
-      const float sw = mine ? __ldg(p.sw + (int64_t)t.e * p.N + n) : 0.0f;
-      const float bias = mine && p.bias ? __ldg(p.bias + (int64_t)t.e * p.N + n) : 0.0f;
       const int chunks = (nkb * kKB + kChunkK - 1) / kChunkK;
       if (chunks > 1) {
         int sum[CW];
 #pragma unroll
         for (int i = 0; i < CW; ++i) sum[i] = 0;
 #pragma unroll 1
-        for (int c = 0; c < chunks; ++c, ++unit) {
+        for (int c = chunks;; ++unit) {
           ok = __all_sync(0xffffffffu, ok && wait(smem_u32(acc_full + (unit & 1)), (unit >> 1) & 1, stop));
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;");
           const uint32_t col = trow + (unit & 1) * TN;
 #pragma unroll
-          for (int g = 0; g < CW; g += 16) {
-            float v[16];
+          for (int g = 0; g < CW; g += 8) {
+            float v[8];
             tmem_ld(col + g, v);
+            tmem_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum[g + i] += __float2int_rn(v[i]);
+            for (int i = 0; i < 8; ++i) sum[g + i] += __float2int_rn(v[i]);
           }
-          if (c == chunks - 1) {
+          if (--c == 0) {  // the sums go back to be finished below
 #pragma unroll
-            for (int g = 0; g < CW; g += 16) {
-              float v[16];
+            for (int g = 0; g < CW; g += 8) {
+              float v[8];
 #pragma unroll
-              for (int i = 0; i < 16; ++i) v[i] = __int2float_rn(sum[g + i]);
+              for (int i = 0; i < 8; ++i) v[i] = __int2float_rn(sum[g + i]);
               tmem_st(col + g, v);
             }
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-            break;  // the buffer is released below
+            break;
           }
           asm volatile("tcgen05.fence::before_thread_sync;");
           __syncwarp();
@@ -477,17 +527,23 @@ __global__ void __launch_bounds__(kThreads, 1) linear_i8_tc_kernel(const I8Args 
         ok = __all_sync(0xffffffffu, ok && wait(smem_u32(acc_full + (unit & 1)), (unit >> 1) & 1, stop));
         asm volatile("tcgen05.fence::after_thread_sync;");
       }
+      const float sw = mine ? __ldg(p.sw + (int64_t)t.e * p.N + n) : 0.0f;
+      const float bias = mine && p.bias ? __ldg(p.bias + (int64_t)t.e * p.N + n) : 0.0f;
 #pragma unroll 1
       for (int g = 0; g < CW && c0 + g < nr; g += 16) {
-        float v[16];
-        if (ok) tmem_ld(trow + (unit & 1) * TN + g, v);
+        float v[2][8];
+        if (ok) {
+          tmem_ld(trow + (unit & 1) * TN + g, v[0]);
+          tmem_ld(trow + (unit & 1) * TN + g + 8, v[1]);
+          tmem_wait_ld();
+        }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int c = c0 + g + i;
           if (c < nr && mine) {
-            float o = fmaf(v[i] * __ldg(p.sx + t.r0 + c), sw, bias);
+            float o = fmaf(v[i / 8][i % 8] * __ldg(p.sx + t.r0 + c), sw, bias);
             if (p.act == DP_ACT_TANH) o = tanhf(o);
-            put_out(y + (t.r0 + c) * p.N + n, ok ? o : __uint_as_float(0x7fc00000u));
+            put_out(y + (int64_t)(t.r0 + c) * p.N + n, ok ? o : __uint_as_float(0x7fc00000u));
           }
         }
       }
@@ -506,19 +562,51 @@ __global__ void __launch_bounds__(kThreads, 1) linear_i8_tc_kernel(const I8Args 
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmemCols));
 }
 
+// The wide form's weights: fp16 as the shared-memory image of each (128 channels, 64 of K) block, 16 KB apiece,
+// channels and columns past the end zero.  A warp widens eight channels' 64 columns.
+__global__ void __launch_bounds__(256) widen_weights_kernel(const int8_t *__restrict__ wq, int K, int N, int nexp,
+                                                            unsigned char *__restrict__ image) {
+  const int nct = (N + kTM - 1) / kTM, nkb = (K + kKB - 1) / kKB, lane = threadIdx.x & 31, r8 = lane >> 2, kp = lane & 3;
+  const int64_t groups = (int64_t)nexp * nct * (kTM / 8) * nkb;
+  for (int64_t g = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); g < groups; g += (int64_t)gridDim.x * 8) {
+    const int kb = (int)(g % nkb), rg = (int)(g / nkb % (kTM / 8));
+    const int64_t ect = g / nkb / (kTM / 8);
+    const int n = (int)(ect % nct) * kTM + rg * 8 + r8, k = kb * kKB + kp * 16;
+    uint4 q = make_uint4(0, 0, 0, 0);
+    if (n < N && k < K) q = __ldg(reinterpret_cast<const uint4 *>(wq + ((ect / nct) * N + n) * K + k));
+    uint4 lo, hi;
+    widen(q.x, lo.x, lo.y);
+    widen(q.y, lo.z, lo.w);
+    widen(q.z, hi.x, hi.y);
+    widen(q.w, hi.z, hi.w);
+    unsigned char *dst = image + (ect * nkb + kb) * (kTM * kKB * 2) + rg * kSBO;
+    *reinterpret_cast<uint4 *>(dst + chunk_at(r8, 2 * kp)) = lo;
+    *reinterpret_cast<uint4 *>(dst + chunk_at(r8, 2 * kp + 1)) = hi;
+  }
+}
+
+size_t image_bytes(int K, int N, int nexp) {
+  return (size_t)nexp * ((N + kTM - 1) / kTM) * ((K + kKB - 1) / kKB) * (kTM * kKB * 2);
+}
+
 template <typename T, int TN>
 int launch_tc(const I8Args &p, int64_t row_tiles, cudaStream_t st, const char *who) {
+  using S = Shape<TN>;
   auto k = linear_i8_tc_kernel<T, TN>;
   cudaFuncAttributes a{};
-  cudaError_t e = cudaFuncGetAttributes(&a, k);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<TN>::kSmem);
+  cudaError_t e = cudaSuccess;
+  if (S::kWide) e = cudaFuncGetAttributes(&a, k);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
   if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
-  const int regs = a.numRegs;
   // the epilogue's registers come out of what the block is launched with
-  if (TN == 256 && regs * (kEpiWarps + kLoadWarps) < kEpiWarps * kEpiRegs + kLoadWarps * kLoadRegs)
-    return set_error(DP_ERR_CUDA, "%s: kernel of %d registers", who, regs);
+  if (S::kWide && a.numRegs < kRegs) return set_error(DP_ERR_CUDA, "%s: kernel of %d registers", who, a.numRegs);
+  if (S::kWide) {
+    const int64_t warps = (int64_t)p.nexp * ((p.N + kTM - 1) / kTM) * (kTM / 8) * ((p.K + kKB - 1) / kKB);
+    const int64_t blocks = (warps + 7) / 8;
+    widen_weights_kernel<<<(unsigned)(blocks < 152 * 8 ? blocks : 152 * 8), 256, 0, st>>>(p.wq, p.K, p.N, p.nexp, p.image);
+  }
   const int64_t tiles = row_tiles * ((p.N + kTM - 1) / kTM);
-  k<<<(unsigned)(tiles < 152 ? tiles : 152), kThreads, Shape<TN>::kSmem, st>>>(p);
+  k<<<(unsigned)(tiles < 152 ? tiles : 152), S::kThreads, S::kSmem, st>>>(p);
   return DP_OK;
 }
 }  // namespace i8
@@ -550,9 +638,17 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
   return launch_status(who);
 }
 
+// Which kernel, by the rows an expert has on average.
+enum I8Form { kFew, kTiles64, kTiles128, kWideTiles };
+I8Form form_of(int64_t rows, int nexp) {
+  const int64_t each = rows / nexp;
+  return rows <= 16 ? kFew : each <= 64 ? kTiles64 : each <= 1024 ? kTiles128 : kWideTiles;
+}
+
 template <typename T>
 int linear(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t *wq, const float *sw, const float *bias,
-           int nexp, int N, const int64_t *start, int act, T *y, void *stream, const char *who) {
+           int nexp, int N, const int64_t *start, int act, T *y, void *work, size_t work_bytes, void *stream,
+           const char *who) {
   clear_error();
   if (rows < 0 || rows > 0x7fffffffLL) return set_error(DP_ERR_SHAPE, "%s: rows = %lld", who, (long long)rows);
   if (K < 16 || K % 16) return set_error(DP_ERR_SHAPE, "%s: K = %d is not a positive multiple of 16", who, K);
@@ -564,20 +660,28 @@ int linear(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t 
   if (rows == 0) return DP_OK;
   if (!xq || !sx || !wq || !sw || !y) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (((uintptr_t)xq | (uintptr_t)wq) & 15) return set_error(DP_ERR_SHAPE, "%s: xq or wq is not 16-byte aligned", who);
-  const I8Args p{xq, wq, sx, sw, bias, start, rows, K, N, nexp, act, y};
+  const I8Form form = form_of(rows, nexp);
+  if (form == kWideTiles) {
+    if (!work) return set_error(DP_ERR_NULL, "%s: work is NULL", who);
+    if (work_bytes < i8::image_bytes(K, N, nexp) || ((uintptr_t)work & 15))
+      return set_error(DP_ERR_SHAPE, "%s: work buffer of %zu bytes is too short or misaligned", who, work_bytes);
+  }
+  const I8Args p{xq, wq, sx, sw, bias, start, (int)rows, K, N, nexp, act, y, (unsigned char *)work};
   const cudaStream_t st = (cudaStream_t)stream;
   const int64_t pieces = start ? (nexp + 1 < rows ? nexp + 1 : rows) : 0;  // a tile more for each expert's remainder
   auto tiles = [&](int R) { return (rows + R - 1) / R + pieces; };
-  if (rows <= 16) {
-    const dim3 grid((unsigned)tiles(kFewRows), (N + kFewWarps - 1) / kFewWarps);
-    linear_i8_few_kernel<T><<<grid, kFewWarps * 32, 0, st>>>(p);
-  } else {
-    const int64_t each = rows / nexp;
-    int rc = each > 128 ? i8::launch_tc<T, 256>(p, tiles(256), st, who)
-             : each > 64 ? i8::launch_tc<T, 128>(p, tiles(128), st, who)
-                         : i8::launch_tc<T, 64>(p, tiles(64), st, who);
-    if (rc) return rc;
+  int rc = DP_OK;
+  switch (form) {
+    case kFew: {
+      const dim3 grid((unsigned)tiles(kFewRows), (N + kFewWarps - 1) / kFewWarps);
+      linear_i8_few_kernel<T><<<grid, kFewWarps * 32, 0, st>>>(p);
+      break;
+    }
+    case kTiles64: rc = i8::launch_tc<T, 64>(p, tiles(64), st, who); break;
+    case kTiles128: rc = i8::launch_tc<T, 128>(p, tiles(128), st, who); break;
+    case kWideTiles: rc = i8::launch_tc<T, 256>(p, tiles(256), st, who); break;
   }
+  if (rc) return rc;
   return launch_status(who);
 }
 
@@ -597,14 +701,21 @@ int take_wait_timeouts_linear_i8(unsigned int *count) {
 
 extern "C" {
 
+size_t dp_linear_i8_work_bytes(int64_t rows, int K, int N, int nexp) {
+  if (rows < 0 || K < 1 || N < 1 || nexp < 1 || dpc::form_of(rows, nexp) != dpc::kWideTiles) return 0;
+  return dpc::i8::image_bytes(K, N, nexp);
+}
+
 #define DP_I8(X, C, T)                                                                                                 \
   int dp_quant_rows_i8_##X(const C *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int K,          \
                            int8_t *xq, float *sx, void *stream) {                                                      \
     return dpc::quant_rows<T>((const T *)x, src, pos, ntok, topk, K, xq, sx, stream, "dp_quant_rows_i8_" #X);          \
   }                                                                                                                    \
   int dp_linear_i8_##X(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t *wq, const float *sw,      \
-                       const float *bias, int nexp, int N, const int64_t *start, int act, C *y, void *stream) {        \
-    return dpc::linear<T>(xq, sx, rows, K, wq, sw, bias, nexp, N, start, act, (T *)y, stream, "dp_linear_i8_" #X);     \
+                       const float *bias, int nexp, int N, const int64_t *start, int act, C *y, void *work,            \
+                       size_t work_bytes, void *stream) {                                                              \
+    return dpc::linear<T>(xq, sx, rows, K, wq, sw, bias, nexp, N, start, act, (T *)y, work, work_bytes, stream,        \
+                          "dp_linear_i8_" #X);                                                                         \
   }
 DP_I8(f64, double, double)
 DP_I8(f32, float, float)

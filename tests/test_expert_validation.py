@@ -55,14 +55,19 @@ def test_linear_i8(dpc):
         assert q(None, None, None, 4, 1, 8, FAKE, FAKE, None) == dpc.DP_ERR_NULL
         assert q(None, None, None, 0, 1, 8, None, None, None) == dpc.DP_OK
 
-        def lin(xq=FAKE, rows=4, K=32, wq=FAKE, nexp=2, N=8, start=FAKE, act=0, y=FAKE, f=getattr(lib, f"dp_linear_i8_{x}")):
-            return f(xq, FAKE, rows, K, wq, FAKE, None, nexp, N, start, act, y, None)
+        def lin(xq=FAKE, rows=4, K=32, wq=FAKE, nexp=2, N=8, start=FAKE, act=0, y=FAKE, work=FAKE, nbytes=0,
+                f=getattr(lib, f"dp_linear_i8_{x}")):
+            return f(xq, FAKE, rows, K, wq, FAKE, None, nexp, N, start, act, y, work, nbytes, None)
 
         assert lin(xq=None) == lin(wq=None) == lin(y=None) == lin(start=None) == dpc.DP_ERR_NULL
         assert lin(rows=-1) == lin(K=24) == lin(K=0) == lin(N=0) == lin(nexp=0) == lin(act=2) == dpc.DP_ERR_SHAPE
         assert lin(xq=odd) == lin(wq=odd) == dpc.DP_ERR_SHAPE
         assert lin(K=65552) == dpc.DP_ERR_UNSUPPORTED
         assert lin(rows=0, xq=None, wq=None, y=None) == dpc.DP_OK
+        need = lib.dp_linear_i8_work_bytes(10 ** 6, 32, 8, 2)
+        assert need > 0 and lib.dp_linear_i8_work_bytes(4, 32, 8, 2) == 0
+        assert lin(rows=10 ** 6, work=None, nbytes=need) == dpc.DP_ERR_NULL
+        assert lin(rows=10 ** 6, nbytes=need - 1) == lin(rows=10 ** 6, work=odd, nbytes=need) == dpc.DP_ERR_SHAPE
 
 
 def test_norm_gate(dpc):
