@@ -212,7 +212,9 @@ struct Shape {
   static constexpr int kThreads = (kMmaWarp + (kWide ? 4 : 1)) * 32;
   static constexpr int kStageA = kTM * kKB * 2, kStageBytes = kStageA + TN * kKB * 2;
   static constexpr int kStages = kWide ? 4 : 6;
-  static constexpr int kAhead = TN == 64 ? 3 : 2;  // stages held in a loader's registers
+  // Two groups of loader warps take the stages in turn: a stage costs a warp about 600 cycles of waiting (barrier,
+  // stores, proxy fence) whatever it holds, which the other group's stage hides.  A group holds its next stage in registers.
+  static constexpr int kGroups = 2;
   static constexpr uint32_t kTmemCols = 2 * TN;
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (2 * kStages + 5) * 8 + 16;  // aligned within
   static_assert(kSmem <= 227 * 1024 && TN % 64 == 0 && TN <= 256, "tile");
@@ -289,7 +291,7 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
   if (threadIdx.x == 0) {
     auto init = [](uint64_t *b, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(n)); };
     for (int s = 0; s < S::kStages; ++s) {
-      init(full + s, S::kLoadWarps + (S::kWide ? 1 : 0));
+      init(full + s, S::kLoadWarps / S::kGroups + (S::kWide ? 1 : 0));
       init(empty + s, 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -386,9 +388,9 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
   } else if (warp >= kEpiWarps) {
     // ---------------------------------------------------------------- loaders
     if constexpr (S::kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
-    constexpr int kLR = S::kLoadWarps * 8;  // rows the loaders cover at once
+    constexpr int kLR = S::kLoadWarps / S::kGroups * 8;  // rows a group covers at once
     constexpr int kA = S::kWide ? 0 : kTM / kLR, kB = TN / kLR, kU = kA + kB;
-    const int kp = lane & 3, row = (warp - kEpiWarps) * 8 + (lane >> 2);
+    const int kp = lane & 3, lw = warp - kEpiWarps, row = (lw / S::kGroups) * 8 + (lane >> 2);
     const uint32_t put = smem_u32(smem), put0 = chunk_at(row, 2 * kp), put1 = chunk_at(row, 2 * kp + 1);
     int tile = blockIdx.x, k = 0;             // where the loads stand: the tile, this thread's column in it,
     int now = 0;                              // its columns (rows of x, whole sixteens), 0 past the last tile,
@@ -414,17 +416,20 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
       }
     };
     next_tile();
-    uint4 raw[S::kAhead][kU];
-    int cols[S::kAhead];
-    auto load = [&](uint4 (&r)[kU], int &c) {
-      c = now;
-      if (!now) return;
+    uint4 raw[kU];
+    auto load = [&] {  // the stage where the loads stand, 0 columns past the last tile
+      const int c = now;
+      if (!now) return c;
       const uint32_t m = k < p.K ? rows : 0u;
 #pragma unroll
       for (int i = 0; i < kU; ++i) {
-        r[i] = make_uint4(0, 0, 0, 0);
-        if (m >> i & 1) r[i] = __ldg(reinterpret_cast<const uint4 *>((i < kA ? w : x) + (int64_t)step * (i < kA ? i : i - kA)));
+        raw[i] = make_uint4(0, 0, 0, 0);
+        if (m >> i & 1) raw[i] = __ldg(reinterpret_cast<const uint4 *>((i < kA ? w : x) + (int64_t)step * (i < kA ? i : i - kA)));
       }
+      return c;
+    };
+    auto advance = [&] {  // one slice on
+      if (!now) return;
       k += kKB;
       if constexpr (kA > 0) w += kKB;
       x += kKB;
@@ -433,40 +438,34 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
         next_tile();
       }
     };
+    int st = lw % S::kGroups, phase = 1;  // the stage, and the parity of its "empty" barrier (the first round passes)
+    for (int g = 0; g < st; ++g) advance();
+    static_assert(S::kGroups == 2 && S::kStages % S::kGroups == 0, "stages in turn");
+    for (int c = load(); c;) {
+      ok = __all_sync(0xffffffffu, wait(smem_u32(empty + st), phase, stop));
+      if (!ok) break;
+      const uint32_t dst = put + st * S::kStageBytes;
 #pragma unroll
-    for (int a = 0; a < S::kAhead; ++a) load(raw[a], cols[a]);
-    int st = 0, phase = 1;  // the stage, and the parity of its "empty" barrier (the first round passes)
-    for (bool more = true; more;) {
-#pragma unroll
-      for (int a = 0; a < S::kAhead; ++a) {
-        if (!cols[a] || !ok) {
-          more = false;
-          break;
-        }
-        ok = __all_sync(0xffffffffu, wait(smem_u32(empty + st), phase, stop));
-        if (ok) {
-          const uint32_t dst = put + st * S::kStageBytes;
-#pragma unroll
-          for (int i = 0; i < kU; ++i) {
-            if (i >= kA && row + kLR * (i - kA) >= cols[a]) continue;
-            uint32_t h[8];
-            widen(raw[a][i].x, h[0], h[1]);
-            widen(raw[a][i].y, h[2], h[3]);
-            widen(raw[a][i].z, h[4], h[5]);
-            widen(raw[a][i].w, h[6], h[7]);
-            const uint32_t d = dst + (i < kA ? i * (kLR / 8) * kSBO : S::kStageA + (i - kA) * (kLR / 8) * kSBO);
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d + put0), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d + put1), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) arrive(smem_u32(full + st));
-          load(raw[a], cols[a]);
-          if (++st == S::kStages) {
-            st = 0;
-            phase ^= 1;
-          }
-        }
+      for (int i = 0; i < kU; ++i) {
+        if (i >= kA && row + kLR * (i - kA) >= c) continue;
+        uint32_t h[8];
+        widen(raw[i].x, h[0], h[1]);
+        widen(raw[i].y, h[2], h[3]);
+        widen(raw[i].z, h[4], h[5]);
+        widen(raw[i].w, h[6], h[7]);
+        const uint32_t d = dst + (i < kA ? i * (kLR / 8) * kSBO : S::kStageA + (i - kA) * (kLR / 8) * kSBO);
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d + put0), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d + put1), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) arrive(smem_u32(full + st));
+      advance();
+      advance();
+      c = load();
+      if ((st += S::kGroups) >= S::kStages) {
+        st -= S::kStages;
+        phase ^= 1;
       }
     }
     if (!ok) *stop = 1;
@@ -529,22 +528,34 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
       }
       const float sw = mine ? __ldg(p.sw + (int64_t)t.e * p.N + n) : 0.0f;
       const float bias = mine && p.bias ? __ldg(p.bias + (int64_t)t.e * p.N + n) : 0.0f;
+      T *out = y + (int64_t)(t.r0 + c0) * p.N + n;
 #pragma unroll 1
-      for (int g = 0; g < CW && c0 + g < nr; g += 16) {
-        float v[2][8];
+      for (int g = 0; g < CW && c0 + g < nr; g += 16, out += (int64_t)16 * p.N) {
+        const int left = nr - c0 - g;
+        const float scale = lane < min(left, 16) ? __ldg(p.sx + t.r0 + c0 + g + lane) : 0.0f;
+        float v[16], v1[8];
         if (ok) {
-          tmem_ld(trow + (unit & 1) * TN + g, v[0]);
-          tmem_ld(trow + (unit & 1) * TN + g + 8, v[1]);
+          tmem_ld(trow + (unit & 1) * TN + g, reinterpret_cast<float(&)[8]>(v));
+          tmem_ld(trow + (unit & 1) * TN + g + 8, v1);
           tmem_wait_ld();
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int c = c0 + g + i;
-          if (c < nr && mine) {
-            float o = fmaf(v[i / 8][i % 8] * __ldg(p.sx + t.r0 + c), sw, bias);
-            if (p.act == DP_ACT_TANH) o = tanhf(o);
-            put_out(y + (int64_t)(t.r0 + c) * p.N + n, ok ? o : __uint_as_float(0x7fc00000u));
-          }
+        for (int i = 0; i < 8; ++i) v[8 + i] = v1[i];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = fmaf(v[i] * __shfl_sync(0xffffffffu, scale, i), sw, bias);
+        if (p.act == DP_ACT_TANH) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = tanhf(v[i]);
+        }
+        T *o = out;
+        if (ok && left >= 16) {
+          if (mine)
+#pragma unroll
+            for (int i = 0; i < 16; ++i, o += p.N) put_out(o, v[i]);
+        } else if (mine) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i, o += p.N)
+            if (i < left) put_out(o, ok ? v[i] : __uint_as_float(0x7fc00000u));
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;");
