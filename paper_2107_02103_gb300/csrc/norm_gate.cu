@@ -48,12 +48,11 @@ __device__ __forceinline__ A inv_sqrt(A x) {
 }
 
 // Mean and inverse deviation of a row held as v[EPT] per thread (0 past the row's end, in[] says which).
-template <int EPT, bool kWarpRow, typename A>
-__device__ __forceinline__ void row_stats(const A (&v)[EPT], int have, int H, bool layer, A eps, A &m, A &s, A *buf,
-                                          int &phase) {
+template <int EPT, bool kWarpRow, bool kLayer, typename A>
+__device__ __forceinline__ void row_stats(const A (&v)[EPT], int have, int H, A eps, A &m, A &s, A *buf, int &phase) {
   A sum[1];
   m = A(0);
-  if (layer) {
+  if constexpr (kLayer) {
     sum[0] = A(0);
 #pragma unroll
     for (int i = 0; i < EPT; ++i) sum[0] += v[i];
@@ -70,7 +69,7 @@ __device__ __forceinline__ void row_stats(const A (&v)[EPT], int have, int H, bo
   s = inv_sqrt(sum[0] / A(H) + eps);
 }
 
-// A thread's elements of a row: packs threadIdx + i * threads, i < EPT / V.
+// A thread's elements of a row: packs first + i * step, i < EPT / V.
 template <typename T, int V, int EPT>
 struct RowMap {
   int first, step, np;  // first pack, stride between packs, packs in the row
@@ -89,15 +88,22 @@ struct RowMap {
       }
     }
   }
-  template <typename A>
-  __device__ __forceinline__ void load_weights(const A *w, A (&v)[EPT]) const {  // f32 or f64, any alignment
+  // The shared weights, read for every row again: they stay in L1 and would cost 40 registers otherwise.  Vec: their
+  // arrays are 16-byte aligned and V elements a multiple of 16 bytes.
+  template <bool Vec, typename A>
+  __device__ __forceinline__ void weights(const A *w, A (&v)[EPT]) const {
+    constexpr int kP = Vec ? 16 / (int)sizeof(A) : 1;
 #pragma unroll
-    for (int i = 0; i < EPT / V; ++i)
+    for (int i = 0; i < EPT / V; ++i) {
+      const int c = first + i * step;
 #pragma unroll
-      for (int l = 0; l < V; ++l) {
-        const int c = first + i * step;
-        v[i * V + l] = c < np && w ? __ldg(w + c * V + l) : A(0);
+      for (int l = 0; l < V; l += kP) {
+        Pack<A, kP> x{};
+        if (c < np) x = load_pack<A, kP>(w + c * V + l);
+#pragma unroll
+        for (int k = 0; k < kP; ++k) v[i * V + l + k] = x.v[k];
       }
+    }
   }
   template <typename A>
   __device__ __forceinline__ void store(T *row, const A (&v)[EPT]) const {
@@ -122,142 +128,238 @@ struct RowMap {
 
 template <typename T>
 struct NormArgs {
-  const T *r, *f, *gate;  // r: the residual stream (backward: r2)
+  const T *in[5];  // the arrays a row is read from: forward f, r, gate; backward r2, du, dr2, f, gate
+  int nin;         // how many of them (the gate only if it has a value for each element)
+  const T *gate;   // a value for each token, or NULL
   const acc_t<T> *a, *w1, *b1, *w2, *b2;
   int64_t ntok;
-  int H, layer, gate_token;
+  int H, stages;  // stages: rows a block of the bulk form has in shared memory
   acc_t<T> eps;
   T *r2, *u;
   acc_t<T> *stats;  // [ntok][4]: m1, s1, m2, s2
-  const T *dr2, *du;
   T *dr, *df, *dgate;
-  acc_t<T> *part;  // [blocks or warps][5][H] partial column sums
+  acc_t<T> *part;  // [units][5][H] partial column sums
 };
 
-template <typename T, int V, int EPT, bool kWarpRow, int kThreads>
-__global__ void __launch_bounds__(kThreads) norm_fwd_kernel(const NormArgs<T> p) {
-  using A = acc_t<T>;
-  __shared__ A buf[2 * 32 * 3];
-  int phase = 0;
-  const int64_t t = kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
-  if (kWarpRow && t >= p.ntok) return;
-  const RowMap<T, V, EPT> map{kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x,
-                              kWarpRow ? 32 : (int)blockDim.x, p.H / V};
-  const int have = map.have();
-  A f[EPT], r[EPT], w[EPT], m1, s1, m2, s2;
-  map.load(p.f + t * p.H, f);
-  map.load(p.r + t * p.H, r);
-  row_stats<EPT, kWarpRow>(f, have, p.H, p.layer, p.eps, m1, s1, buf, phase);
-  map.load_weights(p.w1, w);
-#pragma unroll
-  for (int i = 0; i < EPT; ++i) f[i] = (f[i] - m1) * s1 * w[i];
-  if (p.b1) {
-    map.load_weights(p.b1, w);
-#pragma unroll
-    for (int i = 0; i < EPT; ++i) f[i] += w[i];
+// How rows reach a block: plain loads, or (bulk) whole rows copied ahead into shared memory, `stages` rows deep.
+// A stage may be refilled once every thread has read it, which the first block sum of a row implies.
+template <typename T, int V, int EPT, bool kBulk>
+struct RowFeed {
+  const NormArgs<T> &p;
+  const RowMap<T, V, EPT> &map;
+  int64_t t, step;  // the row at hand, and to the next one
+  unsigned char *smem;
+  uint64_t *bars;
+  int st = 0, phase = 0;
+
+  __device__ __forceinline__ uint32_t row_bytes() const { return (uint32_t)p.H * sizeof(T); }
+  __device__ __forceinline__ uint32_t bar(int s) const { return (uint32_t)__cvta_generic_to_shared(bars + s); }
+  __device__ __forceinline__ void fetch(int64_t row, int s) const {  // one thread
+    const uint32_t bytes = row_bytes(), dst = (uint32_t)__cvta_generic_to_shared(smem) + s * p.nin * bytes;
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar(s)), "r"(bytes * p.nin) : "memory");
+    for (int i = 0; i < p.nin; ++i)
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                       dst + i * bytes),
+                   "l"(p.in[i] + row * p.H), "r"(bytes), "r"(bar(s))
+                   : "memory");
   }
-  if (p.gate) {
-    if (p.gate_token) {
-      const A g = to_acc(p.gate[t]);
-#pragma unroll
-      for (int i = 0; i < EPT; ++i) f[i] *= g;
-    } else {
-      map.load(p.gate + t * p.H, w);
-#pragma unroll
-      for (int i = 0; i < EPT; ++i) f[i] *= w[i];
+  __device__ __forceinline__ void begin() {
+    if constexpr (kBulk) {
+      if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar(s)));
+        asm volatile("fence.mbarrier_init.release.cluster;");
+        for (int s = 0; s < p.stages; ++s)
+          if (t + s * step < p.ntok) fetch(t + s * step, s);
+      }
+      __syncthreads();
     }
   }
-  map.load_weights(p.a, w);
-#pragma unroll
-  for (int i = 0; i < EPT; ++i) r[i] = i < have ? fma(w[i], f[i], r[i]) : A(0);
-  map.store(p.r2 + t * p.H, r);
-  row_stats<EPT, kWarpRow>(r, have, p.H, p.layer, p.eps, m2, s2, buf, phase);
-  map.load_weights(p.w2, w);
-#pragma unroll
-  for (int i = 0; i < EPT; ++i) r[i] = (r[i] - m2) * s2 * w[i];
-  if (p.b2) {
-    map.load_weights(p.b2, w);
-#pragma unroll
-    for (int i = 0; i < EPT; ++i) r[i] += w[i];
+  __device__ __forceinline__ bool arrived() const {  // bounded: false leaves NaN rows behind
+    if constexpr (kBulk) {
+      uint32_t done = 0;
+      for (int it = 0; it < (1 << 22) && !done; ++it)
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+            : "=r"(done)
+            : "r"(bar(st)), "r"((uint32_t)phase)
+            : "memory");
+      return done != 0;
+    }
+    return true;
   }
-  map.store(p.u + t * p.H, r);
-  if (map.first == 0) {
-    A *st = p.stats + t * 4;
-    st[0] = m1;
-    st[1] = s1;
-    st[2] = m2;
-    st[3] = s2;
+  template <typename A>
+  __device__ __forceinline__ void load(int i, A (&v)[EPT]) const {
+    if constexpr (kBulk) map.load(reinterpret_cast<const T *>(smem + (st * p.nin + i) * row_bytes()), v);
+    else map.load(p.in[i] + t * p.H, v);
+  }
+  __device__ __forceinline__ void read() const {  // after a block barrier that follows the row's loads
+    if constexpr (kBulk)
+      if (threadIdx.x == 0 && t + p.stages * step < p.ntok) fetch(t + p.stages * step, st);
+  }
+  __device__ __forceinline__ void next() {
+    t += step;
+    if constexpr (kBulk)
+      if (++st == p.stages) {
+        st = 0;
+        phase ^= 1;
+      }
+  }
+};
+
+constexpr int kMaxStages = 4;
+
+template <typename T, int V, int EPT, bool kWarpRow, bool kBulk, bool kLayer, int kThreads, int kMinBlocks>
+__global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const NormArgs<T> p) {
+  using A = acc_t<T>;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ uint64_t bars[kMaxStages];
+  __shared__ A buf[2 * 32 * 3];
+  int phase = 0;
+  const RowMap<T, V, EPT> map{kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x,
+                              kWarpRow ? 32 : (int)blockDim.x, p.H / V};
+  RowFeed<T, V, EPT, kBulk> feed{
+      p, map, kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : (int64_t)blockIdx.x,
+      kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : (int64_t)gridDim.x, smem, bars};
+  const int have = map.have();
+  feed.begin();
+  T gate_next = p.gate && feed.t < p.ntok ? p.gate[feed.t] : T(0.0f);
+  for (; feed.t < p.ntok; feed.next()) {
+    const int64_t t = feed.t;
+    A f[EPT], r[EPT], g[EPT], w[EPT], m1, s1, m2, s2;
+    const T gate = gate_next;
+    if (p.gate && t + feed.step < p.ntok) gate_next = p.gate[t + feed.step];
+    const bool ok = feed.arrived();
+    feed.load(0, f);
+    feed.load(1, r);
+    if (p.nin > 2) feed.load(2, g);
+    row_stats<EPT, kWarpRow, kLayer>(f, have, p.H, p.eps, m1, s1, buf, phase);
+    feed.read();
+    if (!ok) s1 = A(__int_as_float(0x7fc00000));
+    map.template weights<kBulk>(p.w1, w);
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) f[i] = (f[i] - m1) * s1 * w[i];
+    if constexpr (kLayer) {
+      map.template weights<kBulk>(p.b1, w);
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) f[i] += w[i];
+    }
+    if (p.nin > 2) {
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) f[i] *= g[i];
+    } else if (p.gate) {
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) f[i] *= to_acc(gate);
+    }
+    map.template weights<kBulk>(p.a, w);
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) r[i] = i < have ? fma(w[i], f[i], r[i]) : A(0);
+    map.store(p.r2 + t * p.H, r);
+    row_stats<EPT, kWarpRow, kLayer>(r, have, p.H, p.eps, m2, s2, buf, phase);
+    map.template weights<kBulk>(p.w2, w);
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) r[i] = (r[i] - m2) * s2 * w[i];
+    if constexpr (kLayer) {
+      map.template weights<kBulk>(p.b2, w);
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) r[i] += w[i];
+    }
+    map.store(p.u + t * p.H, r);
+    if (map.first == 0) {
+      A *st = p.stats + t * 4;
+      st[0] = m1;
+      st[1] = s1;
+      st[2] = m2;
+      st[3] = s2;
+    }
   }
 }
 
-// Rows in turn over a fixed number of blocks (or warps): a thread keeps its columns' five sums in registers.
-template <typename T, int V, int EPT, bool kWarpRow, int kThreads>
-__global__ void __launch_bounds__(kThreads) norm_grad_kernel(const NormArgs<T> p) {
+// A thread keeps its columns' sums over the rows of its block (or warp) in registers.
+template <typename T, int V, int EPT, bool kWarpRow, bool kBulk, bool kLayer, int kThreads, int kMinBlocks>
+__global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const NormArgs<T> p) {
   using A = acc_t<T>;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ uint64_t bars[kMaxStages];
   __shared__ A buf[2 * 32 * 3];
   int phase = 0;
-  const int64_t unit = kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
-  const int64_t units = kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : gridDim.x;
+  const int64_t unit = kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
   const RowMap<T, V, EPT> map{kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x,
                               kWarpRow ? 32 : (int)blockDim.x, p.H / V};
-  A a[EPT], w1[EPT], b1[EPT], w2[EPT];
-  map.load_weights(p.a, a);
-  map.load_weights(p.w1, w1);
-  map.load_weights(p.b1, b1);
-  map.load_weights(p.w2, w2);
+  RowFeed<T, V, EPT, kBulk> feed{
+      p, map, unit, kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : (int64_t)gridDim.x, smem, bars};
   A sa[EPT], sw1[EPT], sw2[EPT], sb1[EPT], sb2[EPT];
 #pragma unroll
   for (int i = 0; i < EPT; ++i) sa[i] = sw1[i] = sw2[i] = sb1[i] = sb2[i] = A(0);
   const A inv = A(1) / A(p.H);
   const int have = map.have();
-  for (int64_t t = unit; t < p.ntok; t += units) {
-    const A *st = p.stats + t * 4;
-    const A m1 = __ldg(st), s1 = __ldg(st + 1), m2 = __ldg(st + 2), s2 = __ldg(st + 3);
-    A f[EPT], n2[EPT], du[EPT], dr[EPT], g[EPT];
-    map.load(p.r + t * p.H, n2);
-    map.load(p.du + t * p.H, du);
-    map.load(p.dr2 + t * p.H, dr);
-    map.load(p.f + t * p.H, f);
-    if (p.gate && !p.gate_token) map.load(p.gate + t * p.H, g);
-    else {
-      const A gt = p.gate ? to_acc(p.gate[t]) : A(1);
+  feed.begin();
+  const bool each = p.nin > 4;  // a gate value for each element
+  A st_next[4] = {};
+  T gate_next = T(0.0f);
+  auto peek = [&](int64_t t) {  // the next row's few numbers
+    if (t >= p.ntok) return;
+    if (p.gate) gate_next = p.gate[t];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) st_next[i] = __ldg(p.stats + t * 4 + i);
+  };
+  peek(feed.t);
+  for (; feed.t < p.ntok; feed.next()) {
+    const int64_t t = feed.t;
+    const A m1 = st_next[0], m2 = st_next[2], s2 = st_next[3], gt = p.gate ? to_acc(gate_next) : A(1);
+    A s1 = st_next[1];
+    peek(t + feed.step);
+    if (!feed.arrived()) s1 = A(__int_as_float(0x7fc00000));
+    A f[EPT], n2[EPT], du[EPT], dr[EPT], g[EPT], w[EPT];
+    feed.load(0, n2);
+    feed.load(1, du);
+    feed.load(2, dr);
+    feed.load(3, f);
+    if (each) feed.load(4, g);
+    else
 #pragma unroll
       for (int i = 0; i < EPT; ++i) g[i] = gt;
-    }
     A sums[3] = {A(0), A(0), A(0)};
+    map.template weights<kBulk>(p.w2, w);
 #pragma unroll
     for (int i = 0; i < EPT; ++i) {
       n2[i] = i < have ? (n2[i] - m2) * s2 : A(0);
       f[i] = i < have ? (f[i] - m1) * s1 : A(0);
       sw2[i] = fma(du[i], n2[i], sw2[i]);
-      sb2[i] += du[i];
-      du[i] *= w2[i];
-      sums[0] += du[i];
+      if constexpr (kLayer) sb2[i] += du[i];
+      du[i] *= w[i];
+      if constexpr (kLayer) sums[0] += du[i];
       sums[1] = fma(du[i], n2[i], sums[1]);
     }
     row_sum<3, kWarpRow>(sums, buf, phase);
-    A mean = p.layer ? sums[0] * inv : A(0), along = sums[1] * inv;
+    feed.read();
+    A mean = kLayer ? sums[0] * inv : A(0), along = sums[1] * inv;
 #pragma unroll
     for (int i = 0; i < EPT; ++i) dr[i] = i < have ? fma(s2, du[i] - fma(n2[i], along, mean), dr[i]) : A(0);
     map.store(p.dr + t * p.H, dr);
     sums[0] = sums[1] = sums[2] = A(0);
+    map.template weights<kBulk>(p.w1, w);
+    if constexpr (kLayer) map.template weights<kBulk>(p.b1, n2);
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) {  // du: p from here on
+      du[i] = kLayer ? fma(f[i], w[i], n2[i]) : f[i] * w[i];
+      sa[i] = fma(dr[i] * g[i], du[i], sa[i]);
+    }
+    map.template weights<kBulk>(p.a, n2);
 #pragma unroll
     for (int i = 0; i < EPT; ++i) {
-      const A pp = fma(f[i], w1[i], b1[i]);
-      const A dra = dr[i] * a[i], dp = dra * g[i];
-      sa[i] = fma(dr[i] * g[i], pp, sa[i]);
+      const A dra = dr[i] * n2[i], dp = dra * g[i];
       sw1[i] = fma(dp, f[i], sw1[i]);
-      sb1[i] += dp;
-      g[i] = dra * pp;  // dG
+      if constexpr (kLayer) sb1[i] += dp;
+      g[i] = dra * du[i];  // dG
       sums[2] += g[i];
-      dr[i] = dp * w1[i];
-      sums[0] += dr[i];
+      dr[i] = dp * w[i];
+      if constexpr (kLayer) sums[0] += dr[i];
       sums[1] = fma(dr[i], f[i], sums[1]);
     }
     row_sum<3, kWarpRow>(sums, buf, phase);
-    mean = p.layer ? sums[0] * inv : A(0), along = sums[1] * inv;
+    mean = kLayer ? sums[0] * inv : A(0), along = sums[1] * inv;
     if (p.dgate) {
-      if (!p.gate_token) map.store(p.dgate + t * p.H, g);
+      if (each) map.store(p.dgate + t * p.H, g);
       else if (map.first == 0) p.dgate[t] = from_acc<T>(sums[2]);
     }
 #pragma unroll
@@ -265,7 +367,6 @@ __global__ void __launch_bounds__(kThreads) norm_grad_kernel(const NormArgs<T> p
     map.store(p.df + t * p.H, dr);
   }
   A *out = p.part + unit * kNormVectors * p.H;
-  const int nvec = p.layer ? kNormVectors : 3;
 #pragma unroll
   for (int i = 0; i < EPT; ++i) {
     const int c = map.first + (i / V) * map.step;
@@ -274,7 +375,7 @@ __global__ void __launch_bounds__(kThreads) norm_grad_kernel(const NormArgs<T> p
       o[0] = sa[i];
       o[p.H] = sw1[i];
       o[2 * p.H] = sw2[i];
-      if (nvec == kNormVectors) {
+      if constexpr (kLayer) {
         o[3 * p.H] = sb1[i];
         o[4 * p.H] = sb2[i];
       }
@@ -304,32 +405,60 @@ __global__ void __launch_bounds__(256) norm_finish_kernel(const A *__restrict__ 
 constexpr int kRowWarps = 4;     // rows (warps) per block where a warp holds a row
 constexpr int kGradUnits = 304;  // blocks of the backward (two per SM); four times that in warps for short rows
 
-// Launch shape: a warp per row up to 256 elements, else a block with 8 (16 past 4096) elements a thread.
-template <typename T, bool kGrad>
-void launch(const NormArgs<T> &p, int v, cudaStream_t st) {
-  auto go = [&](auto V, auto E, auto W, auto M) {
-    constexpr int v_ = decltype(V)::value, e_ = decltype(E)::value, m_ = decltype(M)::value;
-    constexpr bool w_ = decltype(W)::value;
+// Launch shape: a warp per row up to 256 elements, else a block with 8 elements a thread (16 past 4096).  Rows whose
+// bytes and addresses are multiples of 16 come by bulk copies, as many rows ahead as fit twice (forward: four times)
+// into an SM; other rows by plain loads of the widest pack they allow.
+template <typename T, bool kGrad, bool kLayer>
+int launch(NormArgs<T> &p, int v, bool weights16, cudaStream_t st, const char *who) {
+  using std::integral_constant;
+  int rc = DP_OK;
+  auto go = [&](auto V, auto E, auto W, auto B, auto M, auto N) {
+    constexpr int v_ = decltype(V)::value, e_ = decltype(E)::value, m_ = decltype(M)::value, n_ = decltype(N)::value;
+    constexpr bool w_ = decltype(W)::value, b_ = decltype(B)::value;
     const int threads = w_ ? kRowWarps * 32 : (p.H + e_ * 32 - 1) / (e_ * 32) * 32;
-    if constexpr (kGrad) {
-      norm_grad_kernel<T, v_, e_, w_, m_><<<kGradUnits, threads, 0, st>>>(p);
-    } else {
-      const int64_t blocks = w_ ? (p.ntok + kRowWarps - 1) / kRowWarps : p.ntok;
-      norm_fwd_kernel<T, v_, e_, w_, m_><<<(unsigned)blocks, threads, 0, st>>>(p);
+    const int64_t units = w_ ? (p.ntok + kRowWarps - 1) / kRowWarps : p.ntok;
+    void (*k)(const NormArgs<T>);
+    if constexpr (kGrad) k = norm_grad_kernel<T, v_, e_, w_, b_, kLayer, m_, n_>;
+    else k = norm_fwd_kernel<T, v_, e_, w_, b_, kLayer, m_, n_>;
+    size_t smem = 0;
+    if (b_) {
+      const size_t row = (size_t)p.nin * p.H * sizeof(T), room = (size_t)200 * 1024 / n_;
+      p.stages = (int)(room / row);
+      p.stages = p.stages > kMaxStages ? kMaxStages : p.stages < 1 ? 1 : p.stages;
+      smem = row * p.stages;
+      if (smem > 32 * 1024) {  // the static part counts too
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) rc = set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+      }
     }
+    const int64_t most = kGrad ? kGradUnits : w_ ? 152 * 16 : 152 * n_;
+    const unsigned blocks = (unsigned)(kGrad || units > most ? most : units);
+    if (!rc) k<<<blocks, threads, smem, st>>>(p);
   };
+  constexpr int kFull = 16 / (int)sizeof(T);
   auto shape = [&](auto V) {
-    using std::integral_constant;
-    if (p.H <= 256) go(V, integral_constant<int, 8>{}, std::true_type{}, integral_constant<int, kRowWarps * 32>{});
-    else if (p.H <= 4096) go(V, integral_constant<int, 8>{}, std::false_type{}, integral_constant<int, 512>{});
-    else go(V, integral_constant<int, 16>{}, std::false_type{}, integral_constant<int, 1024>{});
+    using no = std::false_type;
+    using yes = std::true_type;
+    constexpr int kN = kGrad ? 2 : 4;  // blocks on an SM that registers are kept for
+    if (p.H <= 256) return go(V, integral_constant<int, 8>{}, yes{}, no{}, integral_constant<int, kRowWarps * 32>{}, integral_constant<int, kGrad ? 3 : 8>{});
+    if (p.H > 4096) return go(V, integral_constant<int, 16>{}, no{}, no{}, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+    if constexpr (decltype(V)::value == kFull)
+      if (weights16 && p.H <= 2048)
+        return go(V, integral_constant<int, 8>{}, no{}, yes{}, integral_constant<int, 256>{}, integral_constant<int, kN>{});
+    if (p.H <= 2048) return go(V, integral_constant<int, 8>{}, no{}, no{}, integral_constant<int, 256>{}, integral_constant<int, kN>{});
+    go(V, integral_constant<int, 8>{}, no{}, no{}, integral_constant<int, 512>{}, integral_constant<int, kGrad ? 1 : 2>{});
   };
   if constexpr (sizeof(T) == 2)
-    if (v == 8) return shape(std::integral_constant<int, 8>{});
+    if (v == 8) return shape(integral_constant<int, 8>{}), rc;
   if constexpr (sizeof(T) <= 4)
-    if (v == 4) return shape(std::integral_constant<int, 4>{});
-  if (v == 2) return shape(std::integral_constant<int, 2>{});
-  shape(std::integral_constant<int, 1>{});
+    if (v == 4) return shape(integral_constant<int, 4>{}), rc;
+  if (v == 2) return shape(integral_constant<int, 2>{}), rc;
+  return shape(integral_constant<int, 1>{}), rc;
+}
+
+template <typename... P>
+bool aligned16(P... ptrs) {
+  return (((uintptr_t)ptrs | ...) & 15) == 0;
 }
 
 int norm_check(int64_t ntok, int H, int kind, int gate_kind, const char *who) {
@@ -355,17 +484,19 @@ int norm_fwd(const T *r, const T *f, const T *gate, int gate_kind, const acc_t<T
   if (!r || !f || !a || !w1 || !w2 || !r2 || !u || !stats || (gate_kind != DP_GATE_NONE && !gate) ||
       (kind == DP_NORM_LAYER && (!b1 || !b2)))
     return set_error(DP_ERR_NULL, "%s: NULL array", who);
+  const bool layer = kind == DP_NORM_LAYER, full = gate_kind == DP_GATE_FULL;
   NormArgs<T> p{};
-  p.r = r, p.f = f, p.gate = gate_kind == DP_GATE_NONE ? nullptr : gate;
-  p.a = a, p.w1 = w1, p.w2 = w2;
-  p.layer = kind == DP_NORM_LAYER;
-  p.b1 = p.layer ? b1 : nullptr, p.b2 = p.layer ? b2 : nullptr;
-  p.ntok = ntok, p.H = H, p.gate_token = gate_kind == DP_GATE_TOKEN, p.eps = (acc_t<T>)eps;
+  p.in[0] = f, p.in[1] = r, p.in[2] = full ? gate : nullptr, p.nin = full ? 3 : 2;
+  p.gate = gate_kind == DP_GATE_TOKEN ? gate : nullptr;
+  p.a = a, p.w1 = w1, p.w2 = w2, p.b1 = layer ? b1 : nullptr, p.b2 = layer ? b2 : nullptr;
+  p.ntok = ntok, p.H = H, p.eps = (acc_t<T>)eps;
   p.r2 = r2, p.u = u, p.stats = stats;
-  const int v = pack_width<T>(H, r, f, gate_kind == DP_GATE_FULL ? gate : nullptr, r2, u);
+  const int v = pack_width<T>(H, r, f, p.in[2], r2, u);
   if (!v) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
-  launch<T, false>(p, v, (cudaStream_t)stream);
-  return launch_status(who);
+  const bool w16 = aligned16(a, w1, w2, p.b1, p.b2);
+  const int lrc = layer ? launch<T, false, true>(p, v, w16, (cudaStream_t)stream, who)
+                        : launch<T, false, false>(p, v, w16, (cudaStream_t)stream, who);
+  return lrc ? lrc : launch_status(who);
 }
 
 int64_t grad_units(int H) { return H <= 256 ? (int64_t)kGradUnits * kRowWarps : kGradUnits; }
@@ -385,18 +516,21 @@ int norm_grad(const T *r2, const T *f, const T *gate, int gate_kind, const acc_t
     return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (work_bytes < (size_t)grad_units(H) * kNormVectors * H * sizeof(acc_t<T>) || ((uintptr_t)work & 15))
     return set_error(DP_ERR_SHAPE, "%s: work buffer of %zu bytes is too short or misaligned", who, work_bytes);
+  const bool full = gate_kind == DP_GATE_FULL;
   NormArgs<T> p{};
-  p.r = r2, p.f = f, p.gate = gate_kind == DP_GATE_NONE ? nullptr : gate;
-  p.a = a, p.w1 = w1, p.w2 = w2, p.layer = layer, p.b1 = layer ? b1 : nullptr;
-  p.ntok = ntok, p.H = H, p.gate_token = gate_kind == DP_GATE_TOKEN;
-  p.stats = const_cast<acc_t<T> *>(stats), p.dr2 = dr2, p.du = du, p.dr = dr, p.df = df;
+  p.in[0] = r2, p.in[1] = du, p.in[2] = dr2, p.in[3] = f, p.in[4] = full ? gate : nullptr, p.nin = full ? 5 : 4;
+  p.gate = gate_kind == DP_GATE_TOKEN ? gate : nullptr;
+  p.a = a, p.w1 = w1, p.w2 = w2, p.b1 = layer ? b1 : nullptr;
+  p.ntok = ntok, p.H = H;
+  p.stats = const_cast<acc_t<T> *>(stats), p.dr = dr, p.df = df;
   p.dgate = gate_kind == DP_GATE_NONE ? nullptr : dgate;
   p.part = (acc_t<T> *)work;
-  const bool full = gate_kind == DP_GATE_FULL;
-  const int v = pack_width<T>(H, r2, f, full ? gate : nullptr, dr2, du, dr, df, full ? dgate : nullptr);
+  const int v = pack_width<T>(H, r2, f, p.in[4], dr2, du, dr, df, full ? dgate : nullptr);
   if (!v) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
   const cudaStream_t st = (cudaStream_t)stream;
-  launch<T, true>(p, v, st);
+  const bool w16 = aligned16(a, w1, w2, p.b1);
+  const int lrc = layer ? launch<T, true, true>(p, v, w16, st, who) : launch<T, true, false>(p, v, w16, st, who);
+  if (lrc) return lrc;
   norm_finish_kernel<acc_t<T>><<<dim3((H + 31) / 32, layer ? kNormVectors : 3), 256, 0, st>>>(
       p.part, (int)grad_units(H), H, da, dw1, dw2, db1, db2);
   return launch_status(who);
