@@ -18,26 +18,38 @@ namespace {
 constexpr int kNormMaxH = 16384;
 constexpr int kNormVectors = 5;  // da, dw1, dw2, db1, db2
 
-// Sums of NV values over the row's threads (a warp, or the block through `buf`), the same bits in every thread.
-template <int NV, bool kWarpRow, typename A>
-__device__ __forceinline__ void row_sum(A (&v)[NV], A *buf, int &phase) {
+// The warps' partial sums of a block, two sets used in turn (one barrier a sum); a value's partials lie side by side
+// and are read as vectors, unused warps' stay zero.
+template <typename A, int kWarps>
+struct SumBuf {
+  alignas(16) A v[2][3][kWarps];
+};
+
+// Sums of NV values over the row's threads (a warp, or the block), the same bits in every thread.
+template <int NV, bool kWarpRow, typename A, int kWarps>
+__device__ __forceinline__ void row_sum(A (&v)[NV], SumBuf<A, kWarps> &buf, int &phase) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
     for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
   if constexpr (!kWarpRow) {
-    const int warp = threadIdx.x >> 5, nwarp = blockDim.x >> 5;
-    A *b = buf + phase * (32 * 3);  // alternate halves: one barrier per sum
-    phase ^= 1;
+    constexpr int kP = 16 / (int)sizeof(A);
     if ((threadIdx.x & 31) == 0)
 #pragma unroll
-      for (int i = 0; i < NV; ++i) b[warp * 3 + i] = v[i];
+      for (int i = 0; i < NV; ++i) buf.v[phase][i][threadIdx.x >> 5] = v[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = b[i];
-    for (int w = 1; w < nwarp; ++w)
+    for (int i = 0; i < NV; ++i) {
+      A s[kP] = {};
 #pragma unroll
-      for (int i = 0; i < NV; ++i) v[i] += b[w * 3 + i];
+      for (int w = 0; w < kWarps; w += kP) {
+        const Pack<A, kP> x = load_pack<A, kP>(buf.v[phase][i] + w);
+#pragma unroll
+        for (int k = 0; k < kP; ++k) s[k] += x.v[k];
+      }
+      v[i] = kP == 4 ? (s[0] + s[1]) + (s[kP / 2] + s[kP - 1]) : s[0] + s[1];
+    }
+    phase ^= 1;
   }
 }
 
@@ -47,46 +59,38 @@ __device__ __forceinline__ A inv_sqrt(A x) {
   else return rsqrtf(x);
 }
 
-// Mean and inverse deviation of a row held as v[EPT] per thread (0 past the row's end, in[] says which).
-template <int EPT, bool kWarpRow, bool kLayer, typename A>
-__device__ __forceinline__ void row_stats(const A (&v)[EPT], int have, int H, A eps, A &m, A &s, A *buf, int &phase) {
+// Mean m and inverse deviation s of a row held as v[EPT] per thread; v becomes v - m.
+template <int EPT, bool kWarpRow, bool kLayer, typename Map, typename A, typename Buf>
+__device__ __forceinline__ void row_stats(const Map &map, A (&v)[EPT], A inv, A eps, A &m, A &s, Buf &buf, int &phase) {
   A sum[1];
   m = A(0);
   if constexpr (kLayer) {
-    sum[0] = A(0);
-#pragma unroll
-    for (int i = 0; i < EPT; ++i) sum[0] += v[i];
+    sum[0] = map.total([&](int i) { return v[i]; });
     row_sum<1, kWarpRow>(sum, buf, phase);
-    m = sum[0] / A(H);
-  }
-  sum[0] = A(0);
+    m = sum[0] * inv;
 #pragma unroll
-  for (int i = 0; i < EPT; ++i) {
-    const A d = i < have ? v[i] - m : A(0);
-    sum[0] = fma(d, d, sum[0]);
+    for (int i = 0; i < EPT; ++i) v[i] -= m;
   }
+  sum[0] = map.total([&](int i) { return v[i] * v[i]; });
   row_sum<1, kWarpRow>(sum, buf, phase);
-  s = inv_sqrt(sum[0] / A(H) + eps);
+  s = inv_sqrt(fma(sum[0], inv, eps));
 }
 
-// A thread's elements of a row: packs first + i * step, i < EPT / V.
+// A thread's elements of a row: packs first + i * step, i < EPT / V.  Packs past the row's end repeat its last one
+// (so that loads need no zeros) and are left out of sums and stores.
 template <typename T, int V, int EPT>
 struct RowMap {
+  static constexpr int kN = EPT / V;
   int first, step, np;  // first pack, stride between packs, packs in the row
+  __device__ __forceinline__ bool in(int i) const { return first + i * step < np; }
+  __device__ __forceinline__ int at(int i) const { return min(first + i * step, np - 1) * V; }
   template <typename S, typename A>
   __device__ __forceinline__ void load(const S *row, A (&v)[EPT]) const {
+    Pack<S, V> x[kN];
 #pragma unroll
-    for (int i = 0; i < EPT / V; ++i) {
-      const int c = first + i * step;
-      if (c < np) {
-        const Pack<S, V> x = load_pack<S, V>(row + (int64_t)c * V);
+    for (int i = 0; i < kN; ++i) x[i] = load_pack<S, V>(row + at(i));
 #pragma unroll
-        for (int l = 0; l < V; ++l) v[i * V + l] = to_acc(x.v[l]);
-      } else {
-#pragma unroll
-        for (int l = 0; l < V; ++l) v[i * V + l] = A(0);
-      }
-    }
+    for (int i = 0; i < EPT; ++i) v[i] = to_acc(x[i / V].v[i % V]);
   }
   // The shared weights, read for every row again: they stay in L1 and would cost 40 registers otherwise.  Vec: their
   // arrays are 16-byte aligned and V elements a multiple of 16 bytes.
@@ -94,35 +98,36 @@ struct RowMap {
   __device__ __forceinline__ void weights(const A *w, A (&v)[EPT]) const {
     constexpr int kP = Vec ? 16 / (int)sizeof(A) : 1;
 #pragma unroll
-    for (int i = 0; i < EPT / V; ++i) {
-      const int c = first + i * step;
+    for (int i = 0; i < kN; ++i)
 #pragma unroll
       for (int l = 0; l < V; l += kP) {
-        Pack<A, kP> x{};
-        if (c < np) x = load_pack<A, kP>(w + c * V + l);
+        const Pack<A, kP> x = load_pack<A, kP>(w + at(i) + l);
 #pragma unroll
         for (int k = 0; k < kP; ++k) v[i * V + l + k] = x.v[k];
       }
-    }
   }
   template <typename A>
   __device__ __forceinline__ void store(T *row, const A (&v)[EPT]) const {
 #pragma unroll
-    for (int i = 0; i < EPT / V; ++i) {
-      const int c = first + i * step;
-      if (c < np) {
-        Pack<T, V> x;
+    for (int i = 0; i < kN; ++i) {
+      Pack<T, V> x;
 #pragma unroll
-        for (int l = 0; l < V; ++l) x.v[l] = from_acc<T>(v[i * V + l]);
-        store_pack<T, V>(row + (int64_t)c * V, x);
-      }
+      for (int l = 0; l < V; ++l) x.v[l] = from_acc<T>(v[i * V + l]);
+      if (in(i)) store_pack<T, V>(row + at(i), x);
     }
   }
-  __device__ __forceinline__ int have() const {  // elements of this thread inside the row (whole packs)
-    int n = 0;
+  // The sum of f(i) over the elements that are in the row.
+  template <typename F>
+  __device__ __forceinline__ auto total(F f) const {
+    decltype(f(0)) s = 0;
 #pragma unroll
-    for (int i = 0; i < EPT / V; ++i) n += first + i * step < np ? V : 0;
-    return n;
+    for (int i = 0; i < kN; ++i) {
+      decltype(f(0)) q = f(i * V);
+#pragma unroll
+      for (int l = 1; l < V; ++l) q += f(i * V + l);
+      s += in(i) ? q : 0;
+    }
+    return s;
   }
 };
 
@@ -213,14 +218,16 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
   using A = acc_t<T>;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ uint64_t bars[kMaxStages];
-  __shared__ A buf[2 * 32 * 3];
+  __shared__ SumBuf<A, kThreads / 32> buf;
   int phase = 0;
+  for (int i = threadIdx.x; i < 6 * (kThreads / 32); i += blockDim.x) (&buf.v[0][0][0])[i] = A(0);
+  __syncthreads();
   const RowMap<T, V, EPT> map{kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x,
                               kWarpRow ? 32 : (int)blockDim.x, p.H / V};
   RowFeed<T, V, EPT, kBulk> feed{
       p, map, kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : (int64_t)blockIdx.x,
       kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : (int64_t)gridDim.x, smem, bars};
-  const int have = map.have();
+  const A inv = A(1) / A(p.H);
   feed.begin();
   T gate_next = p.gate && feed.t < p.ntok ? p.gate[feed.t] : T(0.0f);
   for (; feed.t < p.ntok; feed.next()) {
@@ -232,17 +239,14 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
     feed.load(0, f);
     feed.load(1, r);
     if (p.nin > 2) feed.load(2, g);
-    row_stats<EPT, kWarpRow, kLayer>(f, have, p.H, p.eps, m1, s1, buf, phase);
+    row_stats<EPT, kWarpRow, kLayer>(map, f, inv, p.eps, m1, s1, buf, phase);
     feed.read();
     if (!ok) s1 = A(__int_as_float(0x7fc00000));
     map.template weights<kBulk>(p.w1, w);
+    A b[EPT];
+    if constexpr (kLayer) map.template weights<kBulk>(p.b1, b);
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) f[i] = (f[i] - m1) * s1 * w[i];
-    if constexpr (kLayer) {
-      map.template weights<kBulk>(p.b1, w);
-#pragma unroll
-      for (int i = 0; i < EPT; ++i) f[i] += w[i];
-    }
+    for (int i = 0; i < EPT; ++i) f[i] = kLayer ? fma(f[i] * s1, w[i], b[i]) : f[i] * s1 * w[i];
     if (p.nin > 2) {
 #pragma unroll
       for (int i = 0; i < EPT; ++i) f[i] *= g[i];
@@ -252,17 +256,13 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
     }
     map.template weights<kBulk>(p.a, w);
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) r[i] = i < have ? fma(w[i], f[i], r[i]) : A(0);
+    for (int i = 0; i < EPT; ++i) r[i] = fma(w[i], f[i], r[i]);
     map.store(p.r2 + t * p.H, r);
-    row_stats<EPT, kWarpRow, kLayer>(r, have, p.H, p.eps, m2, s2, buf, phase);
+    row_stats<EPT, kWarpRow, kLayer>(map, r, inv, p.eps, m2, s2, buf, phase);
     map.template weights<kBulk>(p.w2, w);
+    if constexpr (kLayer) map.template weights<kBulk>(p.b2, b);
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) r[i] = (r[i] - m2) * s2 * w[i];
-    if constexpr (kLayer) {
-      map.template weights<kBulk>(p.b2, w);
-#pragma unroll
-      for (int i = 0; i < EPT; ++i) r[i] += w[i];
-    }
+    for (int i = 0; i < EPT; ++i) r[i] = kLayer ? fma(r[i] * s2, w[i], b[i]) : r[i] * s2 * w[i];
     map.store(p.u + t * p.H, r);
     if (map.first == 0) {
       A *st = p.stats + t * 4;
@@ -280,8 +280,10 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
   using A = acc_t<T>;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ uint64_t bars[kMaxStages];
-  __shared__ A buf[2 * 32 * 3];
+  __shared__ SumBuf<A, kThreads / 32> buf;
   int phase = 0;
+  for (int i = threadIdx.x; i < 6 * (kThreads / 32); i += blockDim.x) (&buf.v[0][0][0])[i] = A(0);
+  __syncthreads();
   const int64_t unit = kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
   const RowMap<T, V, EPT> map{kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x,
                               kWarpRow ? 32 : (int)blockDim.x, p.H / V};
@@ -291,7 +293,6 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
 #pragma unroll
   for (int i = 0; i < EPT; ++i) sa[i] = sw1[i] = sw2[i] = sb1[i] = sb2[i] = A(0);
   const A inv = A(1) / A(p.H);
-  const int have = map.have();
   feed.begin();
   const bool each = p.nin > 4;  // a gate value for each element
   A st_next[4] = {};
@@ -318,25 +319,25 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
     else
 #pragma unroll
       for (int i = 0; i < EPT; ++i) g[i] = gt;
-    A sums[3] = {A(0), A(0), A(0)};
     map.template weights<kBulk>(p.w2, w);
 #pragma unroll
     for (int i = 0; i < EPT; ++i) {
-      n2[i] = i < have ? (n2[i] - m2) * s2 : A(0);
-      f[i] = i < have ? (f[i] - m1) * s1 : A(0);
+      n2[i] = (n2[i] - m2) * s2;
+      f[i] = (f[i] - m1) * s1;
       sw2[i] = fma(du[i], n2[i], sw2[i]);
       if constexpr (kLayer) sb2[i] += du[i];
       du[i] *= w[i];
-      if constexpr (kLayer) sums[0] += du[i];
-      sums[1] = fma(du[i], n2[i], sums[1]);
     }
-    row_sum<3, kWarpRow>(sums, buf, phase);
+    constexpr int kOne = kLayer ? 2 : 1;
+    A one[kOne];
+    one[0] = map.total([&](int i) { return du[i] * n2[i]; });
+    if constexpr (kLayer) one[1] = map.total([&](int i) { return du[i]; });
+    row_sum<kOne, kWarpRow>(one, buf, phase);
     feed.read();
-    A mean = kLayer ? sums[0] * inv : A(0), along = sums[1] * inv;
+    A along = one[0] * inv, mean = kLayer ? one[kOne - 1] * inv : A(0);
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) dr[i] = i < have ? fma(s2, du[i] - fma(n2[i], along, mean), dr[i]) : A(0);
+    for (int i = 0; i < EPT; ++i) dr[i] = fma(s2, du[i] - (kLayer ? fma(n2[i], along, mean) : n2[i] * along), dr[i]);
     map.store(p.dr + t * p.H, dr);
-    sums[0] = sums[1] = sums[2] = A(0);
     map.template weights<kBulk>(p.w1, w);
     if constexpr (kLayer) map.template weights<kBulk>(p.b1, n2);
 #pragma unroll
@@ -351,27 +352,33 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
       sw1[i] = fma(dp, f[i], sw1[i]);
       if constexpr (kLayer) sb1[i] += dp;
       g[i] = dra * du[i];  // dG
-      sums[2] += g[i];
       dr[i] = dp * w[i];
-      if constexpr (kLayer) sums[0] += dr[i];
-      sums[1] = fma(dr[i], f[i], sums[1]);
     }
-    row_sum<3, kWarpRow>(sums, buf, phase);
-    mean = kLayer ? sums[0] * inv : A(0), along = sums[1] * inv;
+    A sums[3];
+    sums[0] = map.total([&](int i) { return dr[i] * f[i]; });
+    sums[1] = kLayer ? map.total([&](int i) { return dr[i]; }) : A(0);
+    sums[2] = p.gate ? map.total([&](int i) { return g[i]; }) : A(0);
+    if (kLayer || p.gate) {
+      row_sum<3, kWarpRow>(sums, buf, phase);
+    } else {
+      A two[1] = {sums[0]};
+      row_sum<1, kWarpRow>(two, buf, phase);
+      sums[0] = two[0];
+    }
+    along = sums[0] * inv, mean = kLayer ? sums[1] * inv : A(0);
     if (p.dgate) {
       if (each) map.store(p.dgate + t * p.H, g);
       else if (map.first == 0) p.dgate[t] = from_acc<T>(sums[2]);
     }
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) dr[i] = s1 * (dr[i] - fma(f[i], along, mean));
+    for (int i = 0; i < EPT; ++i) dr[i] = s1 * (dr[i] - (kLayer ? fma(f[i], along, mean) : f[i] * along));
     map.store(p.df + t * p.H, dr);
   }
   A *out = p.part + unit * kNormVectors * p.H;
 #pragma unroll
-  for (int i = 0; i < EPT; ++i) {
-    const int c = map.first + (i / V) * map.step;
-    if (c < map.np) {
-      A *o = out + c * V + i % V;
+  for (int i = 0; i < EPT; ++i)
+    if (map.in(i / V)) {
+      A *o = out + map.at(i / V) + i % V;
       o[0] = sa[i];
       o[p.H] = sw1[i];
       o[2 * p.H] = sw2[i];
@@ -380,7 +387,6 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
         o[4 * p.H] = sb2[i];
       }
     }
-  }
 }
 
 // Column sums of the units' partials: a block per 32 columns of one vector, eight rows of threads, fixed order.
