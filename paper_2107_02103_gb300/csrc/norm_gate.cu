@@ -143,7 +143,7 @@ struct NormArgs {
   T *r2, *u;
   acc_t<T> *stats;  // [ntok][4]: m1, s1, m2, s2
   T *dr, *df, *dgate;
-  acc_t<T> *part;  // [units][5][H] partial column sums
+  acc_t<T> *part;  // [blocks][5][H] partial column sums
 };
 
 // How rows reach a block: plain loads, or (bulk) whole rows copied ahead into shared memory, `stages` rows deep.
@@ -284,11 +284,11 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
   int phase = 0;
   for (int i = threadIdx.x; i < 6 * (kThreads / 32); i += blockDim.x) (&buf.v[0][0][0])[i] = A(0);
   __syncthreads();
-  const int64_t unit = kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
   const RowMap<T, V, EPT> map{kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x,
                               kWarpRow ? 32 : (int)blockDim.x, p.H / V};
   RowFeed<T, V, EPT, kBulk> feed{
-      p, map, unit, kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : (int64_t)gridDim.x, smem, bars};
+      p, map, kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : (int64_t)blockIdx.x,
+      kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : (int64_t)gridDim.x, smem, bars};
   A sa[EPT], sw1[EPT], sw2[EPT], sb1[EPT], sb2[EPT];
 #pragma unroll
   for (int i = 0; i < EPT; ++i) sa[i] = sw1[i] = sw2[i] = sb1[i] = sb2[i] = A(0);
@@ -374,85 +374,113 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
     for (int i = 0; i < EPT; ++i) dr[i] = s1 * (dr[i] - (kLayer ? fma(f[i], along, mean) : f[i] * along));
     map.store(p.df + t * p.H, dr);
   }
-  A *out = p.part + unit * kNormVectors * p.H;
+  constexpr int kVec = kLayer ? 5 : 3;
+  A *out = p.part + (int64_t)blockIdx.x * kNormVectors * p.H;
+  if constexpr (kWarpRow) {  // the block's warps hold the same columns: one partial for the block
+    A *all = reinterpret_cast<A *>(smem), *mine = all + (threadIdx.x >> 5) * kVec * p.H;
 #pragma unroll
-  for (int i = 0; i < EPT; ++i)
-    if (map.in(i / V)) {
-      A *o = out + map.at(i / V) + i % V;
-      o[0] = sa[i];
-      o[p.H] = sw1[i];
-      o[2 * p.H] = sw2[i];
-      if constexpr (kLayer) {
-        o[3 * p.H] = sb1[i];
-        o[4 * p.H] = sb2[i];
+    for (int i = 0; i < EPT; ++i)
+      if (map.in(i / V)) {
+        A *o = mine + map.at(i / V) + i % V;
+        o[0] = sa[i], o[p.H] = sw1[i], o[2 * p.H] = sw2[i];
+        if constexpr (kLayer) o[3 * p.H] = sb1[i], o[4 * p.H] = sb2[i];
       }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kVec * p.H; i += blockDim.x) {
+      A v = all[i];
+      for (int k = 1; k < (int)(blockDim.x >> 5); ++k) v += all[k * kVec * p.H + i];
+      out[i] = v;
     }
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPT; ++i)
+      if (map.in(i / V)) {
+        A *o = out + map.at(i / V) + i % V;
+        o[0] = sa[i], o[p.H] = sw1[i], o[2 * p.H] = sw2[i];
+        if constexpr (kLayer) o[3 * p.H] = sb1[i], o[4 * p.H] = sb2[i];
+      }
+  }
 }
 
-// Column sums of the units' partials: a block per 32 columns of one vector, eight rows of threads, fixed order.
+// Column sums of the blocks' partials: a block per 32 columns of one vector, 32 rows of threads, fixed order.
 template <typename A>
-__global__ void __launch_bounds__(256) norm_finish_kernel(const A *__restrict__ part, int units, int H, A *da, A *dw1,
-                                                          A *dw2, A *db1, A *db2) {
-  __shared__ A s[8][33];
+__global__ void __launch_bounds__(1024) norm_finish_kernel(const A *__restrict__ part, int blocks, int H, A *da, A *dw1,
+                                                           A *dw2, A *db1, A *db2) {
+  __shared__ A s[32][33];
   A *const outs[kNormVectors] = {da, dw1, dw2, db1, db2};
   A *out = outs[blockIdx.y];
   const int lane = threadIdx.x & 31, row = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   A v = A(0);
   if (c < H)
-    for (int k = row; k < units; k += 8) v += part[((int64_t)k * kNormVectors + blockIdx.y) * H + c];
+#pragma unroll 4
+    for (int k = row; k < blocks; k += 32) v += part[((int64_t)k * kNormVectors + blockIdx.y) * H + c];
   s[row][lane] = v;
   __syncthreads();
-  if (row == 0 && c < H) {
-    for (int k = 1; k < 8; ++k) v += s[k][lane];
-    out[c] = v;
-  }
+  v = s[lane][row];  // a warp a column
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (lane == 0 && blockIdx.x * 32 + row < H) out[blockIdx.x * 32 + row] = v;
 }
 
-constexpr int kRowWarps = 4;     // rows (warps) per block where a warp holds a row
-constexpr int kGradUnits = 304;  // blocks of the backward (two per SM); four times that in warps for short rows
+constexpr int kRowWarps = 4;  // rows (warps) per block where a warp holds a row
 
-// Launch shape: a warp per row up to 256 elements, else a block with 8 elements a thread (16 past 4096).  Rows whose
-// bytes and addresses are multiples of 16 come by bulk copies, as many rows ahead as fit twice (forward: four times)
-// into an SM; other rows by plain loads of the widest pack they allow.
+// Launch shape, by the row length alone: a warp per row up to 256 elements, else a block with 8 elements a thread (16
+// past 8192).  The blocks that an SM's registers hold (64 a thread forward, 128 backward) stay and take rows in turn.
+struct NormShape {
+  int ept, threads, blocks;  // elements a thread, threads a block, blocks an SM
+};
+NormShape norm_shape(int H, bool grad) {
+  if (H <= 256) return {8, kRowWarps * 32, grad ? 3 : 8};
+  const int ept = H <= 8192 ? 8 : 16, threads = (H + ept * 32 - 1) / (ept * 32) * 32;
+  const int blocks = (grad ? 512 : 1024) / threads;
+  return {ept, threads, blocks < 1 ? 1 : blocks};
+}
+
+// Rows whose bytes and addresses are multiples of 16 come by bulk copies, as many rows ahead as fit; other rows by
+// plain loads of the widest pack they allow.
 template <typename T, bool kGrad, bool kLayer>
 int launch(NormArgs<T> &p, int v, bool weights16, cudaStream_t st, const char *who) {
   using std::integral_constant;
+  using no = std::false_type;
+  using yes = std::true_type;
+  const NormShape n = norm_shape(p.H, kGrad);
   int rc = DP_OK;
   auto go = [&](auto V, auto E, auto W, auto B, auto M, auto N) {
     constexpr int v_ = decltype(V)::value, e_ = decltype(E)::value, m_ = decltype(M)::value, n_ = decltype(N)::value;
     constexpr bool w_ = decltype(W)::value, b_ = decltype(B)::value;
-    const int threads = w_ ? kRowWarps * 32 : (p.H + e_ * 32 - 1) / (e_ * 32) * 32;
-    const int64_t units = w_ ? (p.ntok + kRowWarps - 1) / kRowWarps : p.ntok;
     void (*k)(const NormArgs<T>);
     if constexpr (kGrad) k = norm_grad_kernel<T, v_, e_, w_, b_, kLayer, m_, n_>;
     else k = norm_fwd_kernel<T, v_, e_, w_, b_, kLayer, m_, n_>;
-    size_t smem = 0;
+    size_t smem = kGrad && w_ ? (size_t)kRowWarps * kNormVectors * p.H * sizeof(acc_t<T>) : 0;
     if (b_) {
-      const size_t row = (size_t)p.nin * p.H * sizeof(T), room = (size_t)200 * 1024 / n_;
+      const size_t row = (size_t)p.nin * p.H * sizeof(T), room = (size_t)200 * 1024 / n.blocks;
       p.stages = (int)(room / row);
-      p.stages = p.stages > kMaxStages ? kMaxStages : p.stages < 1 ? 1 : p.stages;
+      p.stages = p.stages > kMaxStages ? kMaxStages : p.stages;
       smem = row * p.stages;
-      if (smem > 32 * 1024) {  // the static part counts too
-        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) rc = set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+    }
+    if (smem > 32 * 1024) {  // the static part counts too
+      const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      if (e != cudaSuccess) rc = set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+    }
+    const int64_t units = w_ ? (p.ntok + kRowWarps - 1) / kRowWarps : p.ntok, most = 152 * n.blocks;
+    if (!rc) k<<<(unsigned)(kGrad || units > most ? most : units), n.threads, smem, st>>>(p);
+  };
+  auto shape = [&](auto V) {
+    constexpr integral_constant<int, 8> e8{};
+    constexpr int kFew = kGrad ? 2 : 4, kHalf = kGrad ? 1 : 2;
+    if (p.H <= 256)
+      return go(V, e8, yes{}, no{}, integral_constant<int, kRowWarps * 32>{}, integral_constant<int, kGrad ? 3 : 8>{});
+    if constexpr (decltype(V)::value * sizeof(T) == 16) {
+      if (weights16 && (size_t)p.nin * p.H * sizeof(T) * n.blocks <= 200 * 1024) {
+        if (p.H <= 2048) return go(V, e8, no{}, yes{}, integral_constant<int, 256>{}, integral_constant<int, kFew>{});
+        if (p.H <= 4096) return go(V, e8, no{}, yes{}, integral_constant<int, 512>{}, integral_constant<int, kHalf>{});
+        if (p.H <= 8192) return go(V, e8, no{}, yes{}, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
       }
     }
-    const int64_t most = kGrad ? kGradUnits : w_ ? 152 * 16 : 152 * n_;
-    const unsigned blocks = (unsigned)(kGrad || units > most ? most : units);
-    if (!rc) k<<<blocks, threads, smem, st>>>(p);
-  };
-  constexpr int kFull = 16 / (int)sizeof(T);
-  auto shape = [&](auto V) {
-    using no = std::false_type;
-    using yes = std::true_type;
-    constexpr int kN = kGrad ? 2 : 4;  // blocks on an SM that registers are kept for
-    if (p.H <= 256) return go(V, integral_constant<int, 8>{}, yes{}, no{}, integral_constant<int, kRowWarps * 32>{}, integral_constant<int, kGrad ? 3 : 8>{});
-    if (p.H > 4096) return go(V, integral_constant<int, 16>{}, no{}, no{}, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
-    if constexpr (decltype(V)::value == kFull)
-      if (weights16 && p.H <= 2048)
-        return go(V, integral_constant<int, 8>{}, no{}, yes{}, integral_constant<int, 256>{}, integral_constant<int, kN>{});
-    if (p.H <= 2048) return go(V, integral_constant<int, 8>{}, no{}, no{}, integral_constant<int, 256>{}, integral_constant<int, kN>{});
-    go(V, integral_constant<int, 8>{}, no{}, no{}, integral_constant<int, 512>{}, integral_constant<int, kGrad ? 1 : 2>{});
+    if (p.H <= 2048) return go(V, e8, no{}, no{}, integral_constant<int, 256>{}, integral_constant<int, kFew>{});
+    if (p.H <= 4096) return go(V, e8, no{}, no{}, integral_constant<int, 512>{}, integral_constant<int, kHalf>{});
+    if (p.H <= 8192) return go(V, e8, no{}, no{}, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+    go(V, integral_constant<int, 16>{}, no{}, no{}, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
   };
   if constexpr (sizeof(T) == 2)
     if (v == 8) return shape(integral_constant<int, 8>{}), rc;
@@ -505,7 +533,7 @@ int norm_fwd(const T *r, const T *f, const T *gate, int gate_kind, const acc_t<T
   return lrc ? lrc : launch_status(who);
 }
 
-int64_t grad_units(int H) { return H <= 256 ? (int64_t)kGradUnits * kRowWarps : kGradUnits; }
+int grad_blocks(int H) { return 152 * norm_shape(H, true).blocks; }
 
 template <typename T>
 int norm_grad(const T *r2, const T *f, const T *gate, int gate_kind, const acc_t<T> *a, const acc_t<T> *w1,
@@ -520,7 +548,7 @@ int norm_grad(const T *r2, const T *f, const T *gate, int gate_kind, const acc_t
       (ntok > 0 && (!r2 || !f || !stats || !dr2 || !du || !dr || !df)) ||
       (ntok > 0 && gate_kind != DP_GATE_NONE && (!gate || !dgate)))
     return set_error(DP_ERR_NULL, "%s: NULL array", who);
-  if (work_bytes < (size_t)grad_units(H) * kNormVectors * H * sizeof(acc_t<T>) || ((uintptr_t)work & 15))
+  if (work_bytes < (size_t)grad_blocks(H) * kNormVectors * H * sizeof(acc_t<T>) || ((uintptr_t)work & 15))
     return set_error(DP_ERR_SHAPE, "%s: work buffer of %zu bytes is too short or misaligned", who, work_bytes);
   const bool full = gate_kind == DP_GATE_FULL;
   NormArgs<T> p{};
@@ -537,8 +565,8 @@ int norm_grad(const T *r2, const T *f, const T *gate, int gate_kind, const acc_t
   const bool w16 = aligned16(a, w1, w2, p.b1);
   const int lrc = layer ? launch<T, true, true>(p, v, w16, st, who) : launch<T, true, false>(p, v, w16, st, who);
   if (lrc) return lrc;
-  norm_finish_kernel<acc_t<T>><<<dim3((H + 31) / 32, layer ? kNormVectors : 3), 256, 0, st>>>(
-      p.part, (int)grad_units(H), H, da, dw1, dw2, db1, db2);
+  norm_finish_kernel<acc_t<T>><<<dim3((H + 31) / 32, layer ? kNormVectors : 3), 1024, 0, st>>>(
+      p.part, grad_blocks(H), H, da, dw1, dw2, db1, db2);
   return launch_status(who);
 }
 
@@ -549,7 +577,7 @@ extern "C" {
 
 size_t dp_norm_gate_work_bytes(int H, int elem_bytes) {
   if (H < 1 || H > dpc::kNormMaxH || (elem_bytes != 2 && elem_bytes != 4 && elem_bytes != 8)) return 0;
-  return (size_t)dpc::grad_units(H) * dpc::kNormVectors * H * (elem_bytes == 8 ? 8 : 4);
+  return (size_t)dpc::grad_blocks(H) * dpc::kNormVectors * H * (elem_bytes == 8 ? 8 : 4);
 }
 
 #define DP_NORM(X, C, T, W)                                                                                            \
