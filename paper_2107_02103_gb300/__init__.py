@@ -925,36 +925,64 @@ def dp_tensor_head_grad(T, a, dA, dT=None, da=None, accumulate=False, want=("dT"
 
 
 # ---------------------------------------------------------------- several nets over the same atoms
+# A call on few atoms costs what its checks cost: one expression per tensor (_p), the functions looked up once.
 _ROW_SUFFIX = {torch.float64: "f64", torch.float32: "f32", torch.bfloat16: "bf16", torch.float16: "f16"}
+_ROW_FN = {name: {t: getattr(_lib, f"dp_{name}_{x}") for t, x in _ROW_SUFFIX.items()}
+           for name in ("route_gather", "route_combine", "route_combine_grad", "quant_rows_i8", "linear_i8",
+                        "norm_gate_fwd", "norm_gate_grad")}
+# the type of weights and sums beside rows of a type
+_WDTYPE = {torch.float64: torch.float64, torch.float32: torch.float32, torch.bfloat16: torch.float32,
+           torch.float16: torch.float32}
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _rows(t, name, dtype=None, shape=None, dim=2):
-    t = _dev(t, name, dtype, shape)
-    if t.dtype not in _ROW_SUFFIX:
-        raise TypeError(f"{name} must be f64, f32, bf16 or f16, got {t.dtype}")
-    if t.dim() != dim:
-        raise ValueError(f"{name} must have {dim} dimensions, got {tuple(t.shape)}")
-    return t
+def _p(t, name, dtype, shape, dev):
+    """The address of t, checked: a contiguous CUDA tensor of dtype and shape on device number dev."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == dev:
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _dev(t, name, dtype, shape)
+    raise ValueError(f"{name} is on device {t.get_device()}, the other tensors on {dev}")
 
 
-def _wdtype(dtype):
-    """The type of weights and sums beside rows of dtype."""
-    return torch.float64 if dtype == torch.float64 else torch.float32
+def _rows(t, name):
+    """(dtype, rows, row length, device number) of a row matrix."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    dtype = t.dtype
+    if dtype not in _ROW_SUFFIX:
+        raise TypeError(f"{name} must be f64, f32, bf16 or f16, got {dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have 2 dimensions, got {tuple(t.shape)}")
+    n, H = t.shape
+    return dtype, n, H, t.get_device()
 
 
-def _same_device(first, *others):
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError(f"tensors on different devices: {first.device} and {t.device}")
+def _pairs(pos):
+    """(ntok, topk) of a plan's pos."""
+    if not isinstance(pos, torch.Tensor) or pos.dim() != 2:
+        raise ValueError("pos must be a plan's [ntok][topk] tensor")
+    return pos.shape
 
 
-def _out(out, name, dtype, shape, like):
-    return torch.empty(shape, dtype=dtype, device=like.device) if out is None else _dev(out, name, dtype, shape)
+def _work_ptr(work, need, like, dev):
+    """(address, bytes, owner) of the scratch: the caller's, or one allocated here."""
+    if work is None:
+        if not need:
+            return None, 0, None
+        work = torch.empty((need,), dtype=torch.uint8, device=like.device)
+    else:
+        _dev(work, "work", torch.uint8)
+        if work.get_device() != dev:
+            raise ValueError(f"work is on device {work.get_device()}, the other tensors on {dev}")
+    return work.data_ptr(), work.numel(), work
 
 
 def dp_route_work_bytes(ntok, topk, nexp) -> int:
     """Bytes of device scratch dp_route_plan needs."""
-    n = int(_lib.dp_route_work_bytes(int(ntok), int(topk), int(nexp)))
+    n = _lib.dp_route_work_bytes(ntok, topk, nexp)
     if n == 0:
         raise ValueError(f"bad plan: {ntok} tokens, {topk} experts each of {nexp}")
     return n
@@ -963,85 +991,78 @@ def dp_route_work_bytes(ntok, topk, nexp) -> int:
 def dp_route_plan(expert, nexp, out=None, work=None):
     """(start [nexp+1] int64, src [ntok*topk] int32, pos [ntok][topk] int32): the pairs of expert
     [ntok][topk] (int32; ids outside [0, nexp) drop the pair) sorted by expert, stably."""
-    expert = _dev(expert, "expert", torch.int32)
+    if not isinstance(expert, torch.Tensor) or not expert.is_cuda or expert.dtype is not torch.int32:
+        raise TypeError("expert must be an int32 CUDA tensor")
     if expert.dim() != 2:
         raise ValueError(f"expert must be [ntok][topk], got {tuple(expert.shape)}")
-    ntok, topk = (int(x) for x in expert.shape)
+    nexp = int(nexp)
+    ntok, topk = expert.shape
+    dev = expert.get_device()
+    need = dp_route_work_bytes(ntok, topk, nexp)
     start, src, pos = (None, None, None) if out is None else out
-    start = _out(start, "start", torch.int64, (int(nexp) + 1,), expert)
-    src = _out(src, "src", torch.int32, (ntok * topk,), expert)
-    pos = _out(pos, "pos", torch.int32, (ntok, topk), expert)
-    if work is None:
-        work = torch.empty((dp_route_work_bytes(ntok, topk, nexp),), dtype=torch.uint8, device=expert.device)
-    else:
-        work = _dev(work, "work", torch.uint8)
-    _same_device(expert, start, src, pos, work)
-    _check(_lib.dp_route_plan(_ptr(expert), ntok, topk, int(nexp), _ptr(start), _ptr(src), _ptr(pos), _ptr(work),
-                              work.numel(), _stream(expert)))
+    if start is None:
+        start = expert.new_empty((nexp + 1,), dtype=torch.int64)
+    if src is None:
+        src = expert.new_empty((ntok * topk,))
+    if pos is None:
+        pos = torch.empty_like(expert)
+    wp, wn, work = _work_ptr(work, need, expert, dev)
+    _check(_lib.dp_route_plan(_p(expert, "expert", torch.int32, (ntok, topk), dev), ntok, topk, nexp,
+                              _p(start, "start", torch.int64, (nexp + 1,), dev),
+                              _p(src, "src", torch.int32, (ntok * topk,), dev),
+                              _p(pos, "pos", torch.int32, (ntok, topk), dev), wp, wn, _raw_stream(dev)))
     return start, src, pos
-
-
-def _plan_arrays(src, pos):
-    pos = _dev(pos, "pos", torch.int32)
-    if pos.dim() != 2:
-        raise ValueError(f"pos must be [ntok][topk], got {tuple(pos.shape)}")
-    if src is not None:
-        _dev(src, "src", torch.int32, (pos.numel(),))
-        _same_device(pos, src)
-    return int(pos.shape[0]), int(pos.shape[1])
 
 
 def dp_route_gather(x, src, pos, out=None):
     """xs [ntok*topk][H]: each token's row of x [ntok][H] at its pairs' sorted places; rows past the kept
     ones are zero."""
-    x = _rows(x, "x")
-    ntok, topk = _plan_arrays(_dev(src, "src", torch.int32), pos)
-    H = int(x.shape[1])
-    _dev(x, "x", None, (ntok, H))
-    xs = _out(out, "out", x.dtype, (ntok * topk, H), x)
-    _same_device(x, pos, xs)
-    _check(getattr(_lib, f"dp_route_gather_{_ROW_SUFFIX[x.dtype]}")(_ptr(x), _ptr(src), _ptr(pos), ntok, topk, H,
-                                                                   _ptr(xs), _stream(x)))
+    dtype, _, H, dev = _rows(x, "x")
+    ntok, topk = _pairs(pos)
+    n = ntok * topk
+    xs = x.new_empty((n, H)) if out is None else out
+    _check(_ROW_FN["route_gather"][dtype](
+        _p(x, "x", dtype, (ntok, H), dev), _p(src, "src", torch.int32, (n,), dev),
+        _p(pos, "pos", torch.int32, (ntok, topk), dev), ntok, topk, H, _p(xs, "out", dtype, (n, H), dev),
+        _raw_stream(dev)))
     return xs
 
 
 def dp_route_combine(z, pos, w=None, out=None):
     """y [ntok][H] = sum_j w[t][j] z[pos[t][j]] over the kept pairs (w None: ones; then also the backward of
     dp_route_gather)."""
-    z = _rows(z, "z")
-    ntok, topk = _plan_arrays(None, pos)
-    H = int(z.shape[1])
-    _dev(z, "z", None, (ntok * topk, H))
-    if w is not None:
-        _dev(w, "w", _wdtype(z.dtype), (ntok, topk))
-    y = _out(out, "out", z.dtype, (ntok, H), z)
-    _same_device(z, pos, w, y)
-    _check(getattr(_lib, f"dp_route_combine_{_ROW_SUFFIX[z.dtype]}")(_ptr(z), _ptr(pos), _ptr(w), ntok, topk, H,
-                                                                    _ptr(y), _stream(z)))
+    dtype, _, H, dev = _rows(z, "z")
+    ntok, topk = _pairs(pos)
+    y = z.new_empty((ntok, H)) if out is None else out
+    _check(_ROW_FN["route_combine"][dtype](
+        _p(z, "z", dtype, (ntok * topk, H), dev), _p(pos, "pos", torch.int32, (ntok, topk), dev),
+        None if w is None else _p(w, "w", _WDTYPE[dtype], (ntok, topk), dev), ntok, topk, H,
+        _p(y, "out", dtype, (ntok, H), dev), _raw_stream(dev)))
     return y
 
 
 def dp_route_combine_grad(z, src, pos, w, dy, out=None, want=("dz", "dw")):
     """(dz [ntok*topk][H], dw [ntok][topk]) of dp_route_combine from dy [ntok][H]; w None: ones.  want without
     "dw": dw is returned as None and z is not read (may be None)."""
-    dy = _rows(dy, "dy")
-    ntok, topk = _plan_arrays(_dev(src, "src", torch.int32), pos)
-    H, dtype = int(dy.shape[1]), dy.dtype
-    _dev(dy, "dy", None, (ntok, H))
+    dtype, _, H, dev = _rows(dy, "dy")
+    ntok, topk = _pairs(pos)
+    n, wd = ntok * topk, _WDTYPE[dtype]
     if "dz" not in want or set(want) - {"dz", "dw"}:
         raise ValueError("want is (dz,) or (dz, dw)")
-    if w is not None:
-        _dev(w, "w", _wdtype(dtype), (ntok, topk))
     dz, dw = (None, None) if out is None else out
-    dz = _out(dz, "dz", dtype, (ntok * topk, H), dy)
+    if dz is None:
+        dz = dy.new_empty((n, H))
     if "dw" in want:
-        _rows(z, "z", dtype, (ntok * topk, H))
-        dw = _out(dw, "dw", _wdtype(dtype), (ntok, topk), dy)
+        zp = _p(z, "z", dtype, (n, H), dev)
+        if dw is None:
+            dw = dy.new_empty((ntok, topk), dtype=wd)
+        dwp = _p(dw, "dw", wd, (ntok, topk), dev)
     else:
-        z = dw = None
-    _same_device(dy, z, src, pos, w, dz, dw)
-    _check(getattr(_lib, f"dp_route_combine_grad_{_ROW_SUFFIX[dtype]}")(
-        _ptr(z), _ptr(src), _ptr(pos), _ptr(w), _ptr(dy), ntok, topk, H, _ptr(dz), _ptr(dw), _stream(dy)))
+        zp = dwp = dw = None
+    _check(_ROW_FN["route_combine_grad"][dtype](
+        zp, _p(src, "src", torch.int32, (n,), dev), _p(pos, "pos", torch.int32, (ntok, topk), dev),
+        None if w is None else _p(w, "w", wd, (ntok, topk), dev), _p(dy, "dy", dtype, (ntok, H), dev), ntok, topk, H,
+        _p(dz, "dz", dtype, (n, H), dev), dwp, _raw_stream(dev)))
     return dz, dw
 
 
@@ -1049,20 +1070,23 @@ def dp_quant_rows_i8(x, src=None, pos=None, out=None):
     """(xq int8 [rows][ldq], sx f32 [rows]): each row of x [ntok][K] as 8-bit integers and a scale, ldq = K
     rounded up to a multiple of 16 (zeros past K).  With a plan's src and pos the rows also go to their sorted
     places (rows = ntok*topk).  Weights [nexp][N][K] are quantised by their rows, x = W.view(nexp*N, K)."""
-    x = _rows(x, "x")
-    ntok, K = (int(v) for v in x.shape)
-    topk = 1
+    dtype, ntok, K, dev = _rows(x, "x")
     if (src is None) != (pos is None):
         raise ValueError("src and pos come together")
+    topk, sp, pp = 1, None, None
     if pos is not None:
-        n, topk = _plan_arrays(src, pos)
-        _dev(x, "x", None, (n, K))
+        ntok, topk = _pairs(pos)
+        sp = _p(src, "src", torch.int32, (ntok * topk,), dev)
+        pp = _p(pos, "pos", torch.int32, (ntok, topk), dev)
+    n, ldq = ntok * topk, (K + 15) // 16 * 16
     xq, sx = (None, None) if out is None else out
-    xq = _out(xq, "xq", torch.int8, (ntok * topk, -(-K // 16) * 16), x)
-    sx = _out(sx, "sx", torch.float32, (ntok * topk,), x)
-    _same_device(x, src, pos, xq, sx)
-    _check(getattr(_lib, f"dp_quant_rows_i8_{_ROW_SUFFIX[x.dtype]}")(_ptr(x), _ptr(src), _ptr(pos), ntok, topk, K,
-                                                                    _ptr(xq), _ptr(sx), _stream(x)))
+    if xq is None:
+        xq = x.new_empty((n, ldq), dtype=torch.int8)
+    if sx is None:
+        sx = x.new_empty((n,), dtype=torch.float32)
+    _check(_ROW_FN["quant_rows_i8"][dtype](
+        _p(x, "x", dtype, (ntok, K), dev), sp, pp, ntok, topk, K, _p(xq, "xq", torch.int8, (n, ldq), dev),
+        _p(sx, "sx", torch.float32, (n,), dev), _raw_stream(dev)))
     return xq, sx
 
 
@@ -1071,7 +1095,7 @@ _ACTS = {None: 0, "tanh": 1}
 
 def dp_linear_i8_work_bytes(rows, K, N, nexp) -> int:
     """Bytes of device scratch dp_linear_i8 needs (0 for few rows)."""
-    return int(_lib.dp_linear_i8_work_bytes(int(rows), int(K), int(N), int(nexp)))
+    return _lib.dp_linear_i8_work_bytes(rows, K, N, nexp)
 
 
 def dp_linear_i8(xq, sx, wq, sw, bias=None, start=None, act=None, dtype=torch.float32, out=None, work=None):
@@ -1079,79 +1103,77 @@ def dp_linear_i8(xq, sx, wq, sw, bias=None, start=None, act=None, dtype=torch.fl
     from dp_quant_rows_i8, wq int8 [nexp][N][K] with sw, bias f32 [nexp][N]; start [nexp+1] a plan's (rows past
     start[nexp] become zeros), None with one expert for all rows; act None or "tanh"; work: a uint8 CUDA tensor of
     dp_linear_i8_work_bytes(rows, K, N, nexp) bytes, or None to allocate what is needed."""
-    xq = _dev(xq, "xq", torch.int8)
-    wq = _dev(wq, "wq", torch.int8)
+    if not isinstance(xq, torch.Tensor) or not xq.is_cuda or xq.dtype is not torch.int8:
+        raise TypeError("xq must be an int8 CUDA tensor")
+    if not isinstance(wq, torch.Tensor) or wq.dtype is not torch.int8:
+        raise TypeError("wq must be an int8 CUDA tensor")
     if xq.dim() != 2 or wq.dim() != 3 or xq.shape[1] != wq.shape[2]:
         raise ValueError(f"xq [rows][K] and wq [nexp][N][K] expected, got {tuple(xq.shape)} and {tuple(wq.shape)}")
     if act not in _ACTS:
         raise ValueError(f"act must be None or 'tanh', got {act!r}")
     if dtype not in _ROW_SUFFIX:
         raise TypeError(f"unsupported dtype {dtype}")
-    rows, K = (int(v) for v in xq.shape)
-    nexp, N = int(wq.shape[0]), int(wq.shape[1])
-    _dev(sx, "sx", torch.float32, (rows,))
-    _dev(sw, "sw", torch.float32, (nexp, N))
-    if bias is not None:
-        _dev(bias, "bias", torch.float32, (nexp, N))
-    if start is not None:
-        _dev(start, "start", torch.int64, (nexp + 1,))
-    y = _out(out, "out", dtype, (rows, N), xq)
-    if work is None:
-        need = dp_linear_i8_work_bytes(rows, K, N, nexp)
-        work = torch.empty((need,), dtype=torch.uint8, device=xq.device) if need else None
-    else:
-        work = _dev(work, "work", torch.uint8)
-    _same_device(xq, sx, wq, sw, bias, start, y, work)
-    _check(getattr(_lib, f"dp_linear_i8_{_ROW_SUFFIX[dtype]}")(
-        _ptr(xq), _ptr(sx), rows, K, _ptr(wq), _ptr(sw), _ptr(bias), nexp, N, _ptr(start), _ACTS[act], _ptr(y),
-        _ptr(work), 0 if work is None else work.numel(), _stream(xq)))
+    rows, K = xq.shape
+    nexp, N, _ = wq.shape
+    dev, f32 = xq.get_device(), torch.float32
+    y = xq.new_empty((rows, N), dtype=dtype) if out is None else out
+    need = 0 if work is not None else _lib.dp_linear_i8_work_bytes(rows, K, N, nexp)
+    wp, wn, work = _work_ptr(work, need, xq, dev)
+    _check(_ROW_FN["linear_i8"][dtype](
+        _p(xq, "xq", torch.int8, (rows, K), dev), _p(sx, "sx", f32, (rows,), dev), rows, K,
+        _p(wq, "wq", torch.int8, (nexp, N, K), dev), _p(sw, "sw", f32, (nexp, N), dev),
+        None if bias is None else _p(bias, "bias", f32, (nexp, N), dev), nexp, N,
+        None if start is None else _p(start, "start", torch.int64, (nexp + 1,), dev), _ACTS[act],
+        _p(y, "out", dtype, (rows, N), dev), wp, wn, _raw_stream(dev)))
     return y
 
 
 _NORMS = {"rms": 0, "layer": 1}
 
 
-def _norm_inputs(r, f, a, w1, w2, b1, b2, gate, kind, grad):
-    f = _rows(f, "f")
+def _norm_kind(kind, b1, b2):
     if kind not in _NORMS:
         raise ValueError(f"kind must be 'rms' or 'layer', got {kind!r}")
-    ntok, H = (int(v) for v in f.shape)
-    wd = _wdtype(f.dtype)
-    _rows(r, "r2" if grad else "r", f.dtype, (ntok, H))
-    for t, name in ((a, "a"), (w1, "w1"), (w2, "w2")):
-        _dev(t, name, wd, (H,))
-    for t, name in ((b1, "b1"), (b2, "b2")):
-        if kind == "layer":
-            _dev(t, name, wd, (H,))
-        elif t is not None:
-            raise ValueError(f"{name} goes with kind='layer'")
-    gate_kind = 0
-    if gate is not None:
-        _dev(gate, "gate", f.dtype)
-        gate_kind = 2 if gate.dim() == 2 else 1
-        _dev(gate, "gate", f.dtype, (ntok, H) if gate_kind == 2 else (ntok,))
-    _same_device(f, r, a, w1, w2, b1, b2, gate)
-    return ntok, H, wd, gate_kind
+    if kind == "rms" and not (b1 is None and b2 is None):
+        raise ValueError("b1 and b2 go with kind='layer'")
+    return _NORMS[kind]
+
+
+def _norm_gate(gate, dtype, ntok, H, dev):
+    """(address, gate kind)."""
+    if gate is None:
+        return None, 0
+    if isinstance(gate, torch.Tensor) and gate.dim() == 2:
+        return _p(gate, "gate", dtype, (ntok, H), dev), 2
+    return _p(gate, "gate", dtype, (ntok,), dev), 1
 
 
 def dp_norm_gate_fwd(r, f, a, w1, w2, b1=None, b2=None, gate=None, kind="rms", eps=1e-6, out=None):
     """(r2, u, stats): r2 = r + a G norm(f; w1, b1), u = norm(r2; w2, b2), stats [ntok][4] for the backward.
     r, f [ntok][H]; a, w1, w2 (and b1, b2 for kind="layer") [H]; gate None, [ntok] or [ntok][H]."""
-    ntok, H, wd, gk = _norm_inputs(r, f, a, w1, w2, b1, b2, gate, kind, False)
+    dtype, ntok, H, dev = _rows(f, "f")
+    k, wd, row, vec = _norm_kind(kind, b1, b2), _WDTYPE[dtype], (ntok, H), (H,)
+    rp = _p(r, "r", dtype, row, dev)
+    gp, gk = _norm_gate(gate, dtype, ntok, H, dev)
+    bp1 = _p(b1, "b1", wd, vec, dev) if k else None
+    bp2 = _p(b2, "b2", wd, vec, dev) if k else None
     r2, u, stats = (None, None, None) if out is None else out
-    r2 = _out(r2, "r2", f.dtype, (ntok, H), f)
-    u = _out(u, "u", f.dtype, (ntok, H), f)
-    stats = _out(stats, "stats", wd, (ntok, 4), f)
-    _same_device(f, r2, u, stats)
-    _check(getattr(_lib, f"dp_norm_gate_fwd_{_ROW_SUFFIX[f.dtype]}")(
-        _ptr(r), _ptr(f), _ptr(gate), gk, _ptr(a), _ptr(w1), _ptr(b1), _ptr(w2), _ptr(b2), ntok, H, _NORMS[kind],
-        float(eps), _ptr(r2), _ptr(u), _ptr(stats), _stream(f)))
+    if r2 is None:
+        r2 = torch.empty_like(r)
+    if u is None:
+        u = torch.empty_like(r)
+    if stats is None:
+        stats = f.new_empty((ntok, 4), dtype=wd)
+    _check(_ROW_FN["norm_gate_fwd"][dtype](
+        rp, _p(f, "f", dtype, row, dev), gp, gk, _p(a, "a", wd, vec, dev), _p(w1, "w1", wd, vec, dev), bp1,
+        _p(w2, "w2", wd, vec, dev), bp2, ntok, H, k, eps, _p(r2, "r2", dtype, row, dev), _p(u, "u", dtype, row, dev),
+        _p(stats, "stats", wd, (ntok, 4), dev), _raw_stream(dev)))
     return r2, u, stats
 
 
 def dp_norm_gate_work_bytes(H, dtype) -> int:
     """Bytes of device scratch dp_norm_gate_grad needs for rows of H elements of dtype."""
-    n = int(_lib.dp_norm_gate_work_bytes(int(H), torch.empty((), dtype=dtype).element_size()))
+    n = _lib.dp_norm_gate_work_bytes(H, dtype.itemsize)
     if n == 0:
         raise ValueError(f"unsupported row length {H}")
     return n
@@ -1161,23 +1183,31 @@ def dp_norm_gate_grad(r2, f, a, w1, w2, stats, dr2, du, b1=None, b2=None, gate=N
     """Backward of dp_norm_gate_fwd from dr2, du and the forward's r2 and stats: a dict of dr, df, dgate (None
     without a gate), da, dw1, dw2, and for kind="layer" db1, db2 (else None).  b2 is accepted and not read.
     out: such a dict of tensors to fill (missing ones are allocated)."""
-    ntok, H, wd, gk = _norm_inputs(r2, f, a, w1, w2, b1, b1 if b2 is None else b2, gate, kind, True)
-    _dev(stats, "stats", wd, (ntok, 4))
-    _rows(dr2, "dr2", f.dtype, (ntok, H))
-    _rows(du, "du", f.dtype, (ntok, H))
-    o = dict(out or {})
-    res = {"dr": _out(o.get("dr"), "dr", f.dtype, (ntok, H), f), "df": _out(o.get("df"), "df", f.dtype, (ntok, H), f),
-           "dgate": None if gate is None else _out(o.get("dgate"), "dgate", f.dtype, tuple(gate.shape), f)}
-    for name in ("da", "dw1", "dw2", "db1", "db2"):
-        res[name] = _out(o.get(name), name, wd, (H,), f) if kind == "layer" or name[1] != "b" else None
-    need = dp_norm_gate_work_bytes(H, f.dtype)
-    if work is None:
-        work = torch.empty((need,), dtype=torch.uint8, device=f.device)
-    else:
-        work = _dev(work, "work", torch.uint8)
-    _same_device(f, stats, dr2, du, work, *res.values())
-    _check(getattr(_lib, f"dp_norm_gate_grad_{_ROW_SUFFIX[f.dtype]}")(
-        _ptr(r2), _ptr(f), _ptr(gate), gk, _ptr(a), _ptr(w1), _ptr(b1), _ptr(w2), _ptr(stats), _ptr(dr2), _ptr(du),
-        ntok, H, _NORMS[kind], *(_ptr(res[n]) for n in ("dr", "df", "dgate", "da", "dw1", "dw2", "db1", "db2")),
-        _ptr(work), work.numel(), _stream(f)))
+    dtype, ntok, H, dev = _rows(f, "f")
+    k, wd, row, vec = _norm_kind(kind, b1, b2), _WDTYPE[dtype], (ntok, H), (H,)
+    fp = _p(f, "f", dtype, row, dev)
+    gp, gk = _norm_gate(gate, dtype, ntok, H, dev)
+    ap, bp1 = _p(a, "a", wd, vec, dev), _p(b1, "b1", wd, vec, dev) if k else None
+    res = {n: None if out is None else out.get(n) for n in ("dr", "df", "dgate", "da", "dw1", "dw2", "db1", "db2")}
+    if res["dr"] is None:
+        res["dr"] = torch.empty_like(f)
+    if res["df"] is None:
+        res["df"] = torch.empty_like(f)
+    if gate is None:
+        res["dgate"] = None
+    elif res["dgate"] is None:
+        res["dgate"] = torch.empty_like(gate)
+    for n in ("da", "dw1", "dw2", "db1", "db2") if k else ("da", "dw1", "dw2"):
+        if res[n] is None:
+            res[n] = torch.empty_like(a)
+    if not k:
+        res["db1"] = res["db2"] = None
+    ptrs = [_p(res["dr"], "dr", dtype, row, dev), _p(res["df"], "df", dtype, row, dev),
+            None if gate is None else _p(res["dgate"], "dgate", dtype, gate.shape, dev)]
+    ptrs += [None if res[n] is None else _p(res[n], n, wd, vec, dev) for n in ("da", "dw1", "dw2", "db1", "db2")]
+    wp, wn, work = _work_ptr(work, dp_norm_gate_work_bytes(H, dtype) if work is None else 0, f, dev)
+    _check(_ROW_FN["norm_gate_grad"][dtype](
+        _p(r2, "r2", dtype, row, dev), fp, gp, gk, ap, _p(w1, "w1", wd, vec, dev), bp1,
+        _p(w2, "w2", wd, vec, dev), _p(stats, "stats", wd, (ntok, 4), dev), _p(dr2, "dr2", dtype, row, dev),
+        _p(du, "du", dtype, row, dev), ntok, H, k, *ptrs, wp, wn, _raw_stream(dev)))
     return res
