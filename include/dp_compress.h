@@ -701,7 +701,8 @@ int dp_tensor_head_grad_f32(const float *T, const float *a, const float *dA, int
  *   src    [ntok topk] output: the pair at each sorted row, -1 past the kept ones
  *   pos    [ntok][topk] output: the sorted row of each pair, -1 for a dropped one
  *   work, work_bytes  device scratch, 16-byte aligned, at least
- *          dp_route_work_bytes(ntok, topk, nexp) bytes (0: bad arguments)
+ *          dp_route_work_bytes(ntok, topk, nexp) bytes (0: bad arguments; 1: few
+ *          pairs, work may be NULL)
  * Errors: DP_ERR_NULL, DP_ERR_SHAPE (ntok < 0, topk outside [1, 64], 2^31 or
  * more pairs, nexp < 1, a short or misaligned work buffer),
  * DP_ERR_UNSUPPORTED (nexp above 1024), DP_ERR_CUDA.

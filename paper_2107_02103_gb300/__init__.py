@@ -1001,12 +1001,12 @@ def dp_route_plan(expert, nexp, out=None, work=None):
     need = dp_route_work_bytes(ntok, topk, nexp)
     start, src, pos = (None, None, None) if out is None else out
     if start is None:
-        start = expert.new_empty((nexp + 1,), dtype=torch.int64)
+        start = torch.empty((nexp + 1,), dtype=torch.int64, device=expert.device)
     if src is None:
-        src = expert.new_empty((ntok * topk,))
+        src = torch.empty((ntok * topk,), dtype=torch.int32, device=expert.device)
     if pos is None:
         pos = torch.empty_like(expert)
-    wp, wn, work = _work_ptr(work, need, expert, dev)
+    wp, wn, work = _work_ptr(work, need if need > 1 else 0, expert, dev)  # 1: none needed
     _check(_lib.dp_route_plan(_p(expert, "expert", torch.int32, (ntok, topk), dev), ntok, topk, nexp,
                               _p(start, "start", torch.int64, (nexp + 1,), dev),
                               _p(src, "src", torch.int32, (ntok * topk,), dev),
@@ -1020,7 +1020,7 @@ def dp_route_gather(x, src, pos, out=None):
     dtype, _, H, dev = _rows(x, "x")
     ntok, topk = _pairs(pos)
     n = ntok * topk
-    xs = x.new_empty((n, H)) if out is None else out
+    xs = torch.empty((n, H), dtype=dtype, device=x.device) if out is None else out
     _check(_ROW_FN["route_gather"][dtype](
         _p(x, "x", dtype, (ntok, H), dev), _p(src, "src", torch.int32, (n,), dev),
         _p(pos, "pos", torch.int32, (ntok, topk), dev), ntok, topk, H, _p(xs, "out", dtype, (n, H), dev),
@@ -1033,7 +1033,7 @@ def dp_route_combine(z, pos, w=None, out=None):
     dp_route_gather)."""
     dtype, _, H, dev = _rows(z, "z")
     ntok, topk = _pairs(pos)
-    y = z.new_empty((ntok, H)) if out is None else out
+    y = torch.empty((ntok, H), dtype=dtype, device=z.device) if out is None else out
     _check(_ROW_FN["route_combine"][dtype](
         _p(z, "z", dtype, (ntok * topk, H), dev), _p(pos, "pos", torch.int32, (ntok, topk), dev),
         None if w is None else _p(w, "w", _WDTYPE[dtype], (ntok, topk), dev), ntok, topk, H,
@@ -1051,11 +1051,11 @@ def dp_route_combine_grad(z, src, pos, w, dy, out=None, want=("dz", "dw")):
         raise ValueError("want is (dz,) or (dz, dw)")
     dz, dw = (None, None) if out is None else out
     if dz is None:
-        dz = dy.new_empty((n, H))
+        dz = torch.empty((n, H), dtype=dtype, device=dy.device)
     if "dw" in want:
         zp = _p(z, "z", dtype, (n, H), dev)
         if dw is None:
-            dw = dy.new_empty((ntok, topk), dtype=wd)
+            dw = torch.empty((ntok, topk), dtype=wd, device=dy.device)
         dwp = _p(dw, "dw", wd, (ntok, topk), dev)
     else:
         zp = dwp = dw = None
@@ -1081,9 +1081,9 @@ def dp_quant_rows_i8(x, src=None, pos=None, out=None):
     n, ldq = ntok * topk, (K + 15) // 16 * 16
     xq, sx = (None, None) if out is None else out
     if xq is None:
-        xq = x.new_empty((n, ldq), dtype=torch.int8)
+        xq = torch.empty((n, ldq), dtype=torch.int8, device=x.device)
     if sx is None:
-        sx = x.new_empty((n,), dtype=torch.float32)
+        sx = torch.empty((n,), dtype=torch.float32, device=x.device)
     _check(_ROW_FN["quant_rows_i8"][dtype](
         _p(x, "x", dtype, (ntok, K), dev), sp, pp, ntok, topk, K, _p(xq, "xq", torch.int8, (n, ldq), dev),
         _p(sx, "sx", torch.float32, (n,), dev), _raw_stream(dev)))
@@ -1116,7 +1116,7 @@ def dp_linear_i8(xq, sx, wq, sw, bias=None, start=None, act=None, dtype=torch.fl
     rows, K = xq.shape
     nexp, N, _ = wq.shape
     dev, f32 = xq.get_device(), torch.float32
-    y = xq.new_empty((rows, N), dtype=dtype) if out is None else out
+    y = torch.empty((rows, N), dtype=dtype, device=xq.device) if out is None else out
     need = 0 if work is not None else _lib.dp_linear_i8_work_bytes(rows, K, N, nexp)
     wp, wn, work = _work_ptr(work, need, xq, dev)
     _check(_ROW_FN["linear_i8"][dtype](
@@ -1163,7 +1163,7 @@ def dp_norm_gate_fwd(r, f, a, w1, w2, b1=None, b2=None, gate=None, kind="rms", e
     if u is None:
         u = torch.empty_like(r)
     if stats is None:
-        stats = f.new_empty((ntok, 4), dtype=wd)
+        stats = torch.empty((ntok, 4), dtype=wd, device=f.device)
     _check(_ROW_FN["norm_gate_fwd"][dtype](
         rp, _p(f, "f", dtype, row, dev), gp, gk, _p(a, "a", wd, vec, dev), _p(w1, "w1", wd, vec, dev), bp1,
         _p(w2, "w2", wd, vec, dev), bp2, ntok, H, k, eps, _p(r2, "r2", dtype, row, dev), _p(u, "u", dtype, row, dev),

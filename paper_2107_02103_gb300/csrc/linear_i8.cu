@@ -12,74 +12,99 @@ constexpr int kMaxTopk = 64;
 constexpr int kMaxK = 65536;  // |q w| <= 2^14: int32 sums hold 2^17 of them
 
 // ------------------------------------------------------------------ rows to 8 bits
-constexpr int kQuantKeep = 4;  // packs a thread keeps in registers; longer rows are read again (from L2)
+constexpr int kQuantKeep = 4;  // packs a lane keeps in registers; longer rows are read again (from L2)
 
-// A row per block of TPR threads.  With pos, token t's row goes to the topk sorted rows pos[t][.], and the
-// rows past the kept ones (src < 0) are cleared.
-template <typename T, int V>
-__global__ void quant_rows_kernel(const T *__restrict__ x, const int32_t *__restrict__ src,
-                                  const int32_t *__restrict__ pos, int64_t ntok, int topk, int K, int ldq,
-                                  int8_t *__restrict__ xq, float *__restrict__ sx) {
-  __shared__ unsigned part[32];
-  const int64_t t = blockIdx.x, n = ntok * topk;
-  const T *row = x + t * K;
-  const int np = K / V;
-  Pack<T, V> keep[kQuantKeep];
-  unsigned most = 0;  // the largest |x| as bits: infinities and NaN come out on top
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN wins
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// rint(x r) as the low byte of a float: the product is rounded, then adding 1.5 2^23 leaves its nearest integer
+// (ties to even) in the low bits, without the slow conversions.
+__device__ __forceinline__ uint32_t to_byte(float x, float r) {
+  return __float_as_uint(__fadd_rn(__fmul_rn(x, r), 12582912.0f));
+}
+
+// G lanes a row (8 to 256; blocks of 128, or 256).  With pos, token t's row goes to the topk sorted rows pos[t][.],
+// and the rows past the kept ones (src < 0) are cleared.  Whole: rows of whole aligned packs.
+template <typename T, bool Whole, int G>
+__global__ void __launch_bounds__(G == 256 ? 256 : 128)
+    quant_rows_kernel(const T *__restrict__ x, const int32_t *__restrict__ src, const int32_t *__restrict__ pos,
+                      int64_t ntok, int topk, int K, int ldq, int8_t *__restrict__ xq, float *__restrict__ sx) {
+  constexpr int V = 16 / (int)sizeof(T), kTok = G == 256 ? 1 : 128 / G, kStep = G, kW = G <= 32 ? 1 : G / 32;
+  __shared__ float part[kTok][kW];
+  const int tid = threadIdx.x % G, slot = threadIdx.x / G;
+  const int64_t t = (int64_t)blockIdx.x * kTok + slot, n = ntok * topk;
+  const bool have = t < ntok;
+  const T *row = x + (have ? t : 0) * K;
+  const int np = ldq / V;  // packs of the row written, those past K zero
+  auto load = [&](int c, float (&v)[V]) {
+    Pack<T, V> q{};
+    if (have && c * V < K) {
+      if constexpr (Whole) q = load_pack<T, V>(row + c * V);
+      else q = load_any<T>(row + c * V, x, x + ntok * K);
+    }
 #pragma unroll
-  for (int i = 0; i < kQuantKeep; ++i) {
-    const int c = threadIdx.x + i * blockDim.x;
-    if (c < np) keep[i] = load_pack<T, V>(row + (int64_t)c * V);
-  }
+    for (int l = 0; l < V; ++l) v[l] = Whole || c * V + l < K ? (float)to_acc(q.v[l]) : 0.0f;
+  };
+  float keep[kQuantKeep][V], amax = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kQuantKeep; ++i) load(tid + i * kStep, keep[i]);
 #pragma unroll
   for (int i = 0; i < kQuantKeep; ++i)
-    if (threadIdx.x + i * blockDim.x < np)
 #pragma unroll
-      for (int l = 0; l < V; ++l) most = max(most, __float_as_uint((float)to_acc(keep[i].v[l])) & 0x7fffffffu);
-  for (int c = threadIdx.x + kQuantKeep * blockDim.x; c < np; c += blockDim.x) {
-    const Pack<T, V> v = load_pack<T, V>(row + (int64_t)c * V);
+    for (int l = 0; l < V; ++l) amax = max_nan(amax, fabsf(keep[i][l]));
+  for (int c = tid + kQuantKeep * kStep; c < np; c += kStep) {
+    float v[V];
+    load(c, v);
 #pragma unroll
-    for (int l = 0; l < V; ++l) most = max(most, __float_as_uint((float)to_acc(v.v[l])) & 0x7fffffffu);
+    for (int l = 0; l < V; ++l) amax = max_nan(amax, fabsf(v[l]));
   }
-  most = __reduce_max_sync(0xffffffffu, most);
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = most;
-  __syncthreads();
-  for (int w = 0; w < (int)(blockDim.x >> 5); ++w) most = max(most, part[w]);
-  const float amax = __uint_as_float(most);
-  const bool fine = most < 0x7f800000u && amax >= 0x1p-100f;
+#pragma unroll
+  for (int o = (G < 32 ? G : 32) / 2; o > 0; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+  if constexpr (G > 32) {
+    if (threadIdx.x % 32 == 0) part[slot][tid / 32] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kW; ++k) amax = max_nan(amax, part[slot][k]);
+  }
+  if (!have) return;
+  const bool fine = amax >= 0x1p-100f && amax < __uint_as_float(0x7f800000u);
   const float r = fine ? __fdiv_rn(127.0f, amax) : 0.0f;
-  const float s = fine ? __fdiv_rn(amax, 127.0f) : most < 0x7f800000u ? 0.0f : __uint_as_float(0x7fc00000u);
-  auto put = [&](int64_t p, int c, const Pack<int8_t, V> &q) { store_pack<int8_t, V>(xq + p * ldq + (int64_t)c * V, q); };
-  for (int c = threadIdx.x, i = 0; c < np; c += blockDim.x, ++i) {
-    Pack<T, V> v;
-    if (i < kQuantKeep) {
+  const float s = fine ? __fdiv_rn(amax, 127.0f) : amax < 1.0f ? 0.0f : __uint_as_float(0x7fc00000u);
+  auto put = [&](int64_t p, int c, const float (&v)[V]) {
+    uint32_t b[V];
 #pragma unroll
-      for (int k = 0; k < kQuantKeep; ++k)
-        if (k == i) v = keep[k];
+    for (int l = 0; l < V; ++l) b[l] = fine ? to_byte(v[l], r) : 0u;
+    int8_t *to = xq + p * ldq + c * V;
+    if constexpr (V == 2) {
+      *reinterpret_cast<uint16_t *>(to) = (uint16_t)__byte_perm(b[0], b[1], 0x40);
     } else {
-      v = load_pack<T, V>(row + (int64_t)c * V);
-    }
-    Pack<int8_t, V> q;
+      uint32_t w[V / 4];
 #pragma unroll
-    for (int l = 0; l < V; ++l) q.v[l] = fine ? (int8_t)__float2int_rn((float)to_acc(v.v[l]) * r) : (int8_t)0;
-    if (!pos) put(t, c, q);
-    else
-      for (int j = 0; j < topk; ++j) {
-        const int64_t p = __ldg(pos + t * topk + j);
-        if (p >= 0 && p < n) put(p, c, q);
-      }
-  }
-  // the padding columns, the scales, and the rows past the kept ones
-  const int64_t rows = pos ? topk : 1;
-  for (int64_t j = 0; j < rows; ++j) {
-    const int64_t q = t * rows + j, p = pos ? __ldg(pos + q) : t;
+      for (int l = 0; l < V; l += 4)
+        w[l / 4] = __byte_perm(__byte_perm(b[l], b[l + 1], 0x40), __byte_perm(b[l + 2], b[l + 3], 0x40), 0x5410);
+      if constexpr (V == 4) *reinterpret_cast<uint32_t *>(to) = w[0];
+      else *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[V / 4 - 1]);
+    }
+  };
+  for (int j = 0; j < topk; ++j) {
+    const int64_t q = t * topk + j, p = pos ? __ldg(pos + q) : t;
     if (p >= 0 && p < n) {
-      for (int c = K + threadIdx.x; c < ldq; c += blockDim.x) xq[p * ldq + c] = 0;
-      if (threadIdx.x == 0) sx[p] = s;
+#pragma unroll
+      for (int i = 0; i < kQuantKeep; ++i)
+        if (tid + i * kStep < np) put(p, tid + i * kStep, keep[i]);
+      for (int c = tid + kQuantKeep * kStep; c < np; c += kStep) {
+        float v[V];
+        load(c, v);
+        put(p, c, v);
+      }
+      if (tid == 0) sx[p] = s;
     }
     if (pos && __ldg(src + q) < 0) {
-      for (int c = threadIdx.x; c < ldq / 16; c += blockDim.x) reinterpret_cast<uint4 *>(xq + q * ldq)[c] = make_uint4(0, 0, 0, 0);
-      if (threadIdx.x == 0) sx[q] = 0.0f;
+      for (int c = tid; c < ldq / 16; c += kStep) reinterpret_cast<uint4 *>(xq + q * ldq)[c] = make_uint4(0, 0, 0, 0);
+      if (tid == 0) sx[q] = 0.0f;
     }
   }
 }
@@ -636,16 +661,19 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
   if (ntok == 0) return DP_OK;
   if (!x || !xq || !sx) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if ((uintptr_t)xq & 15) return set_error(DP_ERR_SHAPE, "%s: xq is not 16-byte aligned", who);
-  const int v = pack_width<T>(K, x);
-  if (!v) return set_error(DP_ERR_SHAPE, "%s: x is not aligned to its elements", who);
-  const int ldq = (K + 15) / 16 * 16;
-  auto go = [&](auto V) {
-    int threads = ((K / V + kQuantKeep - 1) / kQuantKeep + 31) / 32 * 32;
-    threads = threads < 32 ? 32 : threads > 512 ? 512 : threads;
-    quant_rows_kernel<T, V><<<(unsigned)ntok, threads, 0, (cudaStream_t)stream>>>(x, src, pos, ntok, topk, K, ldq, xq, sx);
+  if ((uintptr_t)x & (sizeof(T) - 1)) return set_error(DP_ERR_SHAPE, "%s: x is not aligned to its elements", who);
+  const int ldq = (K + 15) / 16 * 16, packs = ldq / (16 / (int)sizeof(T));
+  const bool whole = (((uintptr_t)x | (uintptr_t)(K * sizeof(T))) & 15) == 0;
+  auto go = [&](auto G) {
+    constexpr int g_ = decltype(G)::value, threads = g_ == 256 ? 256 : 128, tok = threads / g_;
+    auto k = whole ? quant_rows_kernel<T, true, g_> : quant_rows_kernel<T, false, g_>;
+    k<<<(unsigned)((ntok + tok - 1) / tok), threads, 0, (cudaStream_t)stream>>>(x, src, pos, ntok, topk, K, ldq, xq, sx);
   };
-  if (v == 16 / (int)sizeof(T)) go(std::integral_constant<int, 16 / (int)sizeof(T)>{});
-  else go(std::integral_constant<int, 1>{});
+  if (packs <= 8 * kQuantKeep) go(std::integral_constant<int, 8>{});  // as many lanes as hold the row
+  else if (packs <= 32 * kQuantKeep) go(std::integral_constant<int, 32>{});
+  else if (packs <= 64 * kQuantKeep) go(std::integral_constant<int, 64>{});
+  else if (packs <= 128 * kQuantKeep) go(std::integral_constant<int, 128>{});
+  else go(std::integral_constant<int, 256>{});
   return launch_status(who);
 }
 

@@ -13,66 +13,71 @@ namespace dpc {
 namespace {
 
 constexpr int kMaxExperts = 1024, kMaxTopk = 64;
-constexpr int kPlanWarps = 16;
+constexpr int kPlanWarps = 32;
 
-// One warp's part of a block's pairs: cnt[e] += the pairs of expert e among [lo, hi).  Lanes with the same
-// expert are found with a match, so that a warp adds each expert once per 32 pairs, without atomics.
-__device__ __forceinline__ void warp_count(const int32_t *expert, int64_t lo, int64_t hi, int nexp, int *cnt, int lane) {
-  for (int64_t q0 = lo; q0 < hi; q0 += 32) {
-    const int64_t q = q0 + lane;
-    int e = q < hi ? __ldg(expert + q) : -1;
-    if (e < 0 || e >= nexp) e = -1;
-    const unsigned same = __match_any_sync(0xffffffffu, e);
-    if (e >= 0 && lane == __ffs(same) - 1) cnt[e] += __popc(same);
-    __syncwarp();
+// A thread's kPer expert ids, -1 for a dropped pair or past the end; warp w of a block has 32 kPer pairs in order.
+template <int kPer>
+struct PlanIds {
+  int64_t first;  // the lane's first pair; the next are 32 apart
+  int e[kPer];
+  __device__ __forceinline__ PlanIds(const int32_t *expert, int64_t n, int nexp) {
+    first = (((int64_t)blockIdx.x * kPlanWarps + (threadIdx.x >> 5)) * kPer) * 32 + (threadIdx.x & 31);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) e[i] = first + 32 * i < n ? __ldg(expert + first + 32 * i) : -1;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (e[i] >= nexp || e[i] < 0) e[i] = -1;
   }
+};
+
+// counts[b][e]: the kept pairs of expert e in block b's pairs (integer atomics: any order gives the same).
+template <int kPer>
+__global__ void __launch_bounds__(kPlanWarps * 32)
+    plan_count_kernel(const int32_t *__restrict__ expert, int64_t n, int nexp, int *__restrict__ counts) {
+  extern __shared__ int cnt[];
+  for (int e = threadIdx.x; e < nexp; e += blockDim.x) cnt[e] = 0;
+  __syncthreads();
+  const PlanIds<kPer> ids(expert, n, nexp);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (ids.e[i] >= 0) atomicAdd(cnt + ids.e[i], 1);
+  __syncthreads();
+  for (int e = threadIdx.x; e < nexp; e += blockDim.x) counts[(int64_t)blockIdx.x * nexp + e] = cnt[e];
 }
 
-// counts[b][e]: the kept pairs of expert e in block b's chunk.
+// Every block sums the count table (its own prefix and the totals), scans the experts, then gives its pairs their
+// places: a warp's pairs of an expert follow those of the warps before it, and lanes with the same expert are found
+// with a match, so that a warp moves each counter once per 32 pairs.  With one block (counts NULL) it counts by
+// itself: a single launch.
+template <int kPer>
 __global__ void __launch_bounds__(kPlanWarps * 32)
-    plan_count_kernel(const int32_t *__restrict__ expert, int64_t n, int64_t chunk, int nexp, int *__restrict__ counts) {
-  extern __shared__ int cnt[];  // [warps][nexp]
+    plan_place_kernel(const int32_t *__restrict__ expert, int64_t n, int nexp, const int *__restrict__ counts,
+                      int64_t *__restrict__ start, int32_t *__restrict__ src, int32_t *__restrict__ pos) {
+  extern __shared__ int cnt[];  // [warps][nexp], then the scan's warp sums
+  int *sums = cnt + kPlanWarps * nexp;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = threadIdx.x; i < kPlanWarps * nexp; i += blockDim.x) cnt[i] = 0;
+  const PlanIds<kPer> ids(expert, n, nexp);
   __syncthreads();
-  const int64_t b0 = blockIdx.x * chunk, b1 = min(b0 + chunk, n), part = chunk / kPlanWarps;
-  warp_count(expert, b0 + warp * part, min(b0 + (warp + 1) * part, b1), nexp, cnt + warp * nexp, lane);
+  int *mine = cnt + warp * nexp;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (ids.e[i] >= 0) atomicAdd(mine + ids.e[i], 1);
   __syncthreads();
-  for (int e = threadIdx.x; e < nexp; e += blockDim.x) {
-    int s = 0;
-    for (int w = 0; w < kPlanWarps; ++w) s += cnt[w * nexp + e];
-    counts[(int64_t)blockIdx.x * nexp + e] = s;
-  }
-}
-
-// Every block sums the count table again (its own prefix and the totals), scans the experts, then walks its
-// pairs in order and writes src and pos.  With one block (counts NULL) it counts by itself: a single launch.
-__global__ void __launch_bounds__(kPlanWarps * 32)
-    plan_place_kernel(const int32_t *__restrict__ expert, int64_t n, int64_t chunk, int nexp,
-                      const int *__restrict__ counts, int64_t *__restrict__ start, int32_t *__restrict__ src,
-                      int32_t *__restrict__ pos) {
-  extern __shared__ int cnt[];  // [warps][nexp], then base[nexp + 1], then the scan's warp sums
-  int *base = cnt + kPlanWarps * nexp, *sums = base + nexp + 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int i = threadIdx.x; i < kPlanWarps * nexp; i += blockDim.x) cnt[i] = 0;
-  __syncthreads();
-  const int64_t b0 = blockIdx.x * chunk, b1 = min(b0 + chunk, n), part = chunk / kPlanWarps;
-  const int64_t w0 = b0 + warp * part, w1 = min(w0 + part, b1);
-  warp_count(expert, w0, w1, nexp, cnt + warp * nexp, lane);
-  __syncthreads();
-  // totals and this block's prefix per expert; an exclusive scan of the totals, kPlanWarps * 32 experts at a time
   int carry = 0;
-  for (int e0 = 0; e0 < nexp; e0 += kPlanWarps * 32) {
+  for (int e0 = 0; e0 < nexp; e0 += kPlanWarps * 32) {  // an exclusive scan of the totals
     const int e = e0 + threadIdx.x;
     int total = 0, before = 0;
     if (e < nexp) {
       if (counts) {
+#pragma unroll 8
         for (int b = 0; b < (int)gridDim.x; ++b) {
           const int c = __ldg(counts + (int64_t)b * nexp + e);
           before += b < (int)blockIdx.x ? c : 0;
           total += c;
         }
       } else {
+#pragma unroll 8
         for (int w = 0; w < kPlanWarps; ++w) total += cnt[w * nexp + e];
       }
     }
@@ -83,36 +88,36 @@ __global__ void __launch_bounds__(kPlanWarps * 32)
     }
     if (lane == 31) sums[warp] = inc;
     __syncthreads();
-    int off = carry;
-    for (int w = 0; w < kPlanWarps; ++w) {
-      off += w < warp ? sums[w] : 0;
-      carry += sums[w];
-    }
+    int before_warp = lane < warp ? sums[lane] : 0, all = sums[lane];
+    before_warp = __reduce_add_sync(0xffffffffu, before_warp);
+    all = __reduce_add_sync(0xffffffffu, all);
     if (e < nexp) {
-      const int first = off + inc - total;
+      const int first = carry + before_warp + inc - total;
       if (blockIdx.x == 0) start[e] = first;
       int run = first + before;  // from counts to each warp's next row of the expert
+#pragma unroll 8
       for (int w = 0; w < kPlanWarps; ++w) {
         const int c = cnt[w * nexp + e];
         cnt[w * nexp + e] = run;
         run += c;
       }
     }
+    carry += all;
     __syncthreads();
   }
   const int kept = carry;
   if (blockIdx.x == 0 && threadIdx.x == 0) start[nexp] = kept;
-  int *next = cnt + warp * nexp;
-  for (int64_t q0 = w0; q0 < w1; q0 += 32) {
-    const int64_t q = q0 + lane;
-    int e = q < w1 ? __ldg(expert + q) : -1;
-    if (e < 0 || e >= nexp) e = -1;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int64_t q = ids.first + 32 * i;
+    if (q - lane >= n) break;  // warp-uniform
+    const int e = ids.e[i];
     const unsigned same = __match_any_sync(0xffffffffu, e);
-    const int p = e >= 0 ? next[e] + __popc(same & ((1u << lane) - 1)) : -1;
+    const int p = e >= 0 ? mine[e] + __popc(same & ((1u << lane) - 1)) : -1;
     __syncwarp();
-    if (e >= 0 && lane == __ffs(same) - 1) next[e] += __popc(same);
+    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
     __syncwarp();
-    if (q < w1) {
+    if (q < n) {
       pos[q] = p;
       if (p >= 0) src[p] = (int32_t)q;
       if (q >= kept) src[q] = -1;
@@ -120,120 +125,173 @@ __global__ void __launch_bounds__(kPlanWarps * 32)
   }
 }
 
-constexpr int kRowWarps = 4, kSegPacks = 4;  // packs a lane has in flight; a warp moves 32 * kSegPacks of a row
+// Two ways over the rows.  Long rows: a warp takes one part of a token's row, kPart packs a lane, so that the
+// token's pairs are read once by the warp and its loads are long.  Short rows (fewer packs than lanes): a thread
+// takes one pack of any token, the packs in order over the tokens.
+constexpr int kMoveThreads = 128, kPart = 4;
 
-// xs rows of token t from one read of x[t]; also clears the rows past the kept ones that carry t's pair numbers.
-template <typename T, int V>
-__global__ void __launch_bounds__(kRowWarps * 32)
-    gather_kernel(const T *__restrict__ x, const int32_t *__restrict__ src, const int32_t *__restrict__ pos,
-                  int64_t ntok, int topk, int H, T *__restrict__ xs) {
-  const int lane = threadIdx.x & 31;
-  const int64_t t = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5), n = ntok * topk;
-  if (t >= ntok) return;
-  const int np = H / V, c0 = blockIdx.y * (32 * kSegPacks) + lane;
-  Pack<T, V> v[kSegPacks];
-#pragma unroll
-  for (int i = 0; i < kSegPacks; ++i)
-    if (c0 + 32 * i < np) v[i] = load_pack<T, V>(x + t * H + (int64_t)(c0 + 32 * i) * V);
-  for (int j = 0; j < topk; ++j) {
-    const int64_t p = __ldg(pos + t * topk + j);
-    if (p >= 0 && p < n)
-#pragma unroll
-      for (int i = 0; i < kSegPacks; ++i)
-        if (c0 + 32 * i < np) store_pack<T, V>(xs + p * H + (int64_t)(c0 + 32 * i) * V, v[i]);
-  }
-  for (int j = 0; j < topk; ++j) {
-    const int64_t p = t * topk + j;
-    if (__ldg(src + p) < 0)
-#pragma unroll
-      for (int i = 0; i < kSegPacks; ++i)
-        if (c0 + 32 * i < np) store_pack<T, V>(xs + p * H + (int64_t)(c0 + 32 * i) * V, Pack<T, V>{});
+struct Unit {
+  int64_t t;  // the token
+  int c;      // the lane's first pack; further ones 32 apart
+};
+template <bool Flat>
+__device__ __forceinline__ Unit unit_of(int np) {
+  if constexpr (Flat) {
+    const int64_t base = (int64_t)blockIdx.x * kMoveThreads, t0 = base / np;
+    const uint32_t off = (uint32_t)(base - t0 * np) + threadIdx.x, dt = off / (uint32_t)np;
+    return {t0 + dt, (int)(off - dt * np)};
+  } else {
+    return {(int64_t)blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5), (int)(blockIdx.y * 32 * kPart + (threadIdx.x & 31))};
   }
 }
 
-template <typename T, int V>
-__global__ void __launch_bounds__(kRowWarps * 32)
-    combine_kernel(const T *__restrict__ z, const int32_t *__restrict__ pos, const acc_t<T> *__restrict__ w,
-                   int64_t ntok, int topk, int H, T *__restrict__ y) {
-  using A = acc_t<T>;
-  const int lane = threadIdx.x & 31;
-  const int64_t t = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5), n = ntok * topk;
-  if (t >= ntok) return;
-  const int np = H / V, c0 = blockIdx.y * (32 * kSegPacks) + lane;
-  A sum[kSegPacks][V];
+// xs rows of token t from one read of x[t]; also clears the rows past the kept ones that carry t's pair numbers.
+// Rows that are not of whole packs: the aligned packs within each row written, read through load_any (from L1 after
+// the first), and the elements before and after them one by one.
+template <typename T, bool Whole, bool Flat>
+__global__ void __launch_bounds__(kMoveThreads)
+    gather_kernel(const T *__restrict__ x, const int32_t *__restrict__ src, const int32_t *__restrict__ pos,
+                  int64_t ntok, int topk, int H, int np, T *__restrict__ xs) {
+  constexpr int V = 16 / (int)sizeof(T), kP = Flat ? 1 : kPart;
+  const int64_t n = ntok * topk;
+  const Unit u = unit_of<Flat>(np);
+  if (u.t >= ntok) return;
+  const T *row = x + u.t * H;
+  Pack<T, V> v[kP];
+  if constexpr (Whole)
 #pragma unroll
-  for (int i = 0; i < kSegPacks; ++i)
+    for (int i = 0; i < kP; ++i)
+      if (u.c + 32 * i < np) v[i] = load_pack<T, V>(row + (u.c + 32 * i) * V);
+  auto write = [&](T *to, bool zero) {
+    int head = 0, full = np;
+    if constexpr (!Whole) {
+      head = min((int)((16 - ((uintptr_t)to & 15)) & 15) / (int)sizeof(T), H);
+      full = (H - head) / V;
+      if (u.c < H - full * V) {  // fewer elements at the ends than packs a unit may have
+        const int e = u.c < head ? u.c : u.c + full * V;
+        to[e] = zero ? T(0.0f) : row[e];
+      }
+      if (!zero)
 #pragma unroll
-    for (int l = 0; l < V; ++l) sum[i][l] = A(0);
+        for (int i = 0; i < kP; ++i)
+          if (u.c + 32 * i < full) v[i] = load_any<T>(row + head + (u.c + 32 * i) * V, x, x + ntok * H);
+    }
+#pragma unroll
+    for (int i = 0; i < kP; ++i)
+      if (u.c + 32 * i < full) store_pack<T, V>(to + head + (u.c + 32 * i) * V, zero ? Pack<T, V>{} : v[i]);
+  };
   for (int j = 0; j < topk; ++j) {
-    const int64_t p = __ldg(pos + t * topk + j);
+    const int64_t q = u.t * topk + j, p = __ldg(pos + q);
+    if (p >= 0 && p < n) write(xs + p * H, false);
+    if (__ldg(src + q) < 0) write(xs + q * H, true);
+  }
+}
+
+// The sums; V elements an access: whole rows' packs, or 1 for other rows (reading the two words under each pack of
+// every row instead measured 75 us against 64 for 30,011 x 3 rows of 1003 f16).
+template <typename T, int V, bool Flat>
+__global__ void __launch_bounds__(kMoveThreads)
+    combine_kernel(const T *__restrict__ z, const int32_t *__restrict__ pos, const acc_t<T> *__restrict__ w,
+                   int64_t ntok, int topk, int H, int np, T *__restrict__ y) {
+  using A = acc_t<T>;
+  constexpr int kP = Flat ? 1 : kPart;
+  const int64_t n = ntok * topk;
+  const Unit u = unit_of<Flat>(np);
+  if (u.t >= ntok) return;
+  A sum[kP][V] = {};
+  for (int j = 0; j < topk; ++j) {
+    const int64_t q = u.t * topk + j, p = __ldg(pos + q);
     if (p < 0 || p >= n) continue;
-    const A wj = w ? __ldg(w + t * topk + j) : A(1);
-    Pack<T, V> v[kSegPacks];
+    const A wj = w ? __ldg(w + q) : A(1);
+    const T *row = z + p * H;
+    Pack<T, V> v[kP];
 #pragma unroll
-    for (int i = 0; i < kSegPacks; ++i)
-      if (c0 + 32 * i < np) v[i] = load_pack<T, V>(z + p * H + (int64_t)(c0 + 32 * i) * V);
+    for (int i = 0; i < kP; ++i)
+      if (u.c + 32 * i < np) v[i] = load_pack<T, V>(row + (u.c + 32 * i) * V);
 #pragma unroll
-    for (int i = 0; i < kSegPacks; ++i)
+    for (int i = 0; i < kP; ++i)
 #pragma unroll
       for (int l = 0; l < V; ++l) sum[i][l] = fma(wj, to_acc(v[i].v[l]), sum[i][l]);
   }
+  T *to = y + u.t * H;
 #pragma unroll
-  for (int i = 0; i < kSegPacks; ++i)
-    if (c0 + 32 * i < np) {
+  for (int i = 0; i < kP; ++i)
+    if (u.c + 32 * i < np) {
       Pack<T, V> o;
 #pragma unroll
       for (int l = 0; l < V; ++l) o.v[l] = from_acc<T>(sum[i][l]);
-      store_pack<T, V>(y + t * H + (int64_t)(c0 + 32 * i) * V, o);
+      store_pack<T, V>(to + (u.c + 32 * i) * V, o);
     }
 }
 
-constexpr int kGradThreads = 128;
+// Accesses a lane has in flight of either row.
+template <int V>
+constexpr int kGradPacks = V > 1 ? 4 : 8;
 
-// A block per token: dz rows and the dot products for dw (each lane's partial in order, then a fixed tree).
-template <typename T, int V>
-__global__ void __launch_bounds__(kGradThreads)
+// Threads a block: more of a token's pairs in one block let rows read by elements find dy in L1 (30,011 x 3 rows of
+// 1003 f16: 136 us against 183 in blocks of 128); whole rows do better in small blocks (48 us against 58 for 12,288
+// x 2 of 1600 bf16).
+template <int V>
+constexpr int kGradThreads = V > 1 ? 128 : 256;
+
+// G lanes a pair (8 to 256): its dz row and dot product (each lane's partial in order, then a
+// fixed tree).  A token's pairs are neighbours, so that dy comes from memory once; a pair to itself leaves nothing
+// to wait for but its own rows.
+template <typename T, int V, int G>
+__global__ void __launch_bounds__(G > kGradThreads<V> ? G : kGradThreads<V>)
     combine_grad_kernel(const T *__restrict__ z, const int32_t *__restrict__ src, const int32_t *__restrict__ pos,
-                        const acc_t<T> *__restrict__ w, const T *__restrict__ dy, int64_t ntok, int topk, int H,
+                        const acc_t<T> *__restrict__ w, const T *__restrict__ dy, int64_t ntok, int topk, int H, int np,
                         T *__restrict__ dz, acc_t<T> *__restrict__ dw) {
   using A = acc_t<T>;
-  __shared__ A part[kGradThreads / 32];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, np = H / V;
-  const int64_t t = blockIdx.x, n = ntok * topk;
-  for (int j = 0; j < topk; ++j) {
-    const int64_t p = __ldg(pos + t * topk + j);
-    const bool in = p >= 0 && p < n;
-    A dot = A(0);
-    if (in) {
-      const A wj = w ? __ldg(w + t * topk + j) : A(1);
-      for (int c = threadIdx.x; c < np; c += kGradThreads) {
-        const Pack<T, V> g = load_pack<T, V>(dy + t * H + (int64_t)c * V);
-        Pack<T, V> o;
-        if (dw) {
-          const Pack<T, V> v = load_pack<T, V>(z + p * H + (int64_t)c * V);
+  constexpr int kPairs = G > kGradThreads<V> ? 1 : kGradThreads<V> / G, kW = G <= 32 ? 1 : G / 32, kP = kGradPacks<V>;
+  __shared__ A part[kPairs][kW];
+  const int tid = threadIdx.x % G, slot = threadIdx.x / G;
+  const int64_t n = ntok * topk, q = (int64_t)blockIdx.x * kPairs + slot;
+  A dot = A(0);
+  if (q < n) {
+    const int64_t p = __ldg(pos + q);
+    if (p >= 0 && p < n) {
+      const A wq = w ? __ldg(w + q) : A(1);
+      const T *g = dy + q / topk * H, *from = z + p * H;
+      T *to = dz + p * H;
+      for (int s = tid; s < np; s += kP * G) {
+        Pack<T, V> gv[kP], zv[kP];
 #pragma unroll
-          for (int l = 0; l < V; ++l) dot = fma(to_acc(g.v[l]), to_acc(v.v[l]), dot);
-        }
+        for (int i = 0; i < kP; ++i)
+          if (s + i * G < np) gv[i] = load_pack<T, V>(g + (s + i * G) * V);
+        if (dw)
 #pragma unroll
-        for (int l = 0; l < V; ++l) o.v[l] = from_acc<T>(wj * to_acc(g.v[l]));
-        store_pack<T, V>(dz + p * H + (int64_t)c * V, o);
+          for (int i = 0; i < kP; ++i)
+            if (s + i * G < np) zv[i] = load_pack<T, V>(from + (s + i * G) * V);
+#pragma unroll
+        for (int i = 0; i < kP; ++i)
+          if (s + i * G < np) {
+            Pack<T, V> o;
+#pragma unroll
+            for (int l = 0; l < V; ++l) {
+              if (dw) dot = fma(to_acc(gv[i].v[l]), to_acc(zv[i].v[l]), dot);
+              o.v[l] = from_acc<T>(wq * to_acc(gv[i].v[l]));
+            }
+            store_pack<T, V>(to + (s + i * G) * V, o);
+          }
       }
     }
-    if (dw) {  // launch-uniform
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-      if (lane == 0) part[warp] = dot;
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        A s = part[0];
-        for (int k = 1; k < kGradThreads / 32; ++k) s += part[k];
-        dw[t * topk + j] = in ? s : A(0);
-      }
-      __syncthreads();
-    }
-    const int64_t q = t * topk + j;
     if (__ldg(src + q) < 0)
-      for (int c = threadIdx.x; c < np; c += kGradThreads) store_pack<T, V>(dz + q * H + (int64_t)c * V, Pack<T, V>{});
+      for (int s = tid; s < np; s += G) store_pack<T, V>(dz + q * H + s * V, Pack<T, V>{});
+  }
+  if (dw) {  // launch-uniform; the dot of a dropped pair is 0
+#pragma unroll
+    for (int o = (G < 32 ? G : 32) / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+    if constexpr (G > 32) {
+      if (threadIdx.x % 32 == 0) part[slot][tid / 32] = dot;
+      __syncthreads();
+      if (tid == 0) {
+        dot = part[slot][0];
+#pragma unroll
+        for (int k = 1; k < kW; ++k) dot += part[slot][k];
+      }
+    }
+    if (tid == 0 && q < n) dw[q] = dot;
   }
 }
 
@@ -252,30 +310,32 @@ int row_check(int64_t ntok, int topk, int H, const char *who) {
   return DP_OK;
 }
 
-// Calls f(std::integral_constant<int, V>) for the pack width V in {16, 8, 4, 2, 1 bytes} / sizeof(T).
-template <typename T, typename F>
-void with_pack(int v, F f) {
-  if constexpr (sizeof(T) == 2)
-    if (v == 8) return f(std::integral_constant<int, 8>{});
-  if constexpr (sizeof(T) <= 4)
-    if (v == 4) return f(std::integral_constant<int, 4>{});
-  if (v == 2) return f(std::integral_constant<int, 2>{});
-  f(std::integral_constant<int, 1>{});
-}
-
-// Blocks of the plan: one while a block's pass over the pairs costs less than a second launch, else chunks of
-// at least 2048 pairs, at most 304 blocks (two per SM; each reads the whole count table).
+// Blocks of the plan and pairs a thread: one block where its walk (0.3 us for each of a thread's pairs) costs less
+// than a second launch.
 struct PlanShape {
-  int blocks;
-  int64_t chunk;
+  int blocks, per;
 };
 PlanShape plan_shape(int64_t n) {
-  int64_t blocks = n <= 8192 ? 1 : (n + 2047) / 2048;
-  blocks = blocks > 304 ? 304 : blocks < 1 ? 1 : blocks;
-  int64_t chunk = (n + blocks - 1) / blocks;
-  chunk = (chunk + kPlanWarps * 32 - 1) / (kPlanWarps * 32) * (kPlanWarps * 32);
-  if (chunk < kPlanWarps * 32) chunk = kPlanWarps * 32;
-  return {(int)((n + chunk - 1) / chunk < 1 ? 1 : (n + chunk - 1) / chunk), chunk};
+  if (n <= 4096) return {1, 4};
+  if (n <= 8192) return {1, 8};
+  if (n <= 304 * 4096) return {(int)((n + 4095) / 4096), 4};
+  return {(int)((n + 8191) / 8192), 8};
+}
+
+template <typename T>
+bool whole_rows(int H, const void *a, const void *b, const void *c = nullptr) {
+  return ((((uintptr_t)a | (uintptr_t)b | (uintptr_t)c) | (uintptr_t)(H * sizeof(T))) & 15) == 0;
+}
+template <typename T>
+bool elements_aligned(const void *a, const void *b, const void *c = nullptr) {
+  return (((uintptr_t)a | (uintptr_t)b | (uintptr_t)c) & (sizeof(T) - 1)) == 0;
+}
+// The grid of a move over rows of np packs; false where it is too large.
+bool move_grid(int64_t ntok, int np, bool flat, dim3 *grid) {
+  const int64_t x = flat ? (ntok * np + kMoveThreads - 1) / kMoveThreads : (ntok + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
+  const int64_t y = flat ? 1 : (np + 32 * kPart - 1) / (32 * kPart);
+  *grid = dim3((unsigned)x, (unsigned)y);
+  return x <= 0x7fffffffLL && y <= 65535;
 }
 
 template <typename T>
@@ -285,12 +345,16 @@ int gather(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok, int
   int rc = row_check(ntok, topk, H, who);
   if (rc || ntok == 0) return rc;
   if (!x || !src || !pos || !xs) return set_error(DP_ERR_NULL, "%s: NULL array", who);
-  const int v = pack_width<T>(H, x, xs);
-  if (!v) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
-  with_pack<T>(v, [&](auto V) {
-    const dim3 grid((unsigned)((ntok + kRowWarps - 1) / kRowWarps), (H / V + 32 * kSegPacks - 1) / (32 * kSegPacks));
-    gather_kernel<T, V><<<grid, kRowWarps * 32, 0, (cudaStream_t)stream>>>(x, src, pos, ntok, topk, H, xs);
-  });
+  if (!elements_aligned<T>(x, xs)) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool whole = whole_rows<T>(H, x, xs);
+  const bool flat = H / V < 32;
+  const int np = whole || !flat ? (H + V - 1) / V : H / V + 2 * V;  // with places for the elements at a short row's ends
+  dim3 grid;
+  if (!move_grid(ntok, np, flat, &grid)) return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, H);
+  auto k = flat ? (whole ? gather_kernel<T, true, true> : gather_kernel<T, false, true>)
+                   : (whole ? gather_kernel<T, true, false> : gather_kernel<T, false, false>);
+  k<<<grid, kMoveThreads, 0, (cudaStream_t)stream>>>(x, src, pos, ntok, topk, H, np, xs);
   return launch_status(who);
 }
 
@@ -301,12 +365,15 @@ int combine(const T *z, const int32_t *pos, const acc_t<T> *w, int64_t ntok, int
   int rc = row_check(ntok, topk, H, who);
   if (rc || ntok == 0) return rc;
   if (!z || !pos || !y) return set_error(DP_ERR_NULL, "%s: NULL array", who);
-  const int v = pack_width<T>(H, z, y);
-  if (!v) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
-  with_pack<T>(v, [&](auto V) {
-    const dim3 grid((unsigned)((ntok + kRowWarps - 1) / kRowWarps), (H / V + 32 * kSegPacks - 1) / (32 * kSegPacks));
-    combine_kernel<T, V><<<grid, kRowWarps * 32, 0, (cudaStream_t)stream>>>(z, pos, w, ntok, topk, H, y);
-  });
+  if (!elements_aligned<T>(z, y)) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool whole = whole_rows<T>(H, z, y);
+  const int np = whole ? H / V : H;
+  dim3 grid;
+  if (!move_grid(ntok, np, np < 32, &grid)) return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, H);
+  auto k = np < 32 ? (whole ? combine_kernel<T, V, true> : combine_kernel<T, 1, true>)
+                   : (whole ? combine_kernel<T, V, false> : combine_kernel<T, 1, false>);
+  k<<<grid, kMoveThreads, 0, (cudaStream_t)stream>>>(z, pos, w, ntok, topk, H, np, y);
   return launch_status(who);
 }
 
@@ -317,12 +384,25 @@ int combine_grad(const T *z, const int32_t *src, const int32_t *pos, const acc_t
   int rc = row_check(ntok, topk, H, who);
   if (rc || ntok == 0) return rc;
   if (!src || !pos || !dy || !dz || (dw && !z)) return set_error(DP_ERR_NULL, "%s: NULL array", who);
-  const int v = pack_width<T>(H, dw ? z : nullptr, dy, dz);
-  if (!v) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
-  with_pack<T>(v, [&](auto V) {
-    combine_grad_kernel<T, V><<<(unsigned)ntok, kGradThreads, 0, (cudaStream_t)stream>>>(z, src, pos, w, dy, ntok, topk,
-                                                                                         H, dz, dw);
-  });
+  const T *zr = dw ? z : nullptr;
+  if (!elements_aligned<T>(zr, dy, dz)) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool whole = whole_rows<T>(H, zr, dy, dz);
+  const int np = whole ? H / V : H, each = whole ? kGradPacks<V> : kGradPacks<1>;
+  auto go = [&](auto G) {
+    constexpr int g_ = decltype(G)::value;
+    int threads = whole ? kGradThreads<V> : kGradThreads<1>;
+    threads = threads < g_ ? g_ : threads;
+    const int pairs = threads / g_;
+    auto k = whole ? combine_grad_kernel<T, V, g_> : combine_grad_kernel<T, 1, g_>;
+    k<<<(unsigned)((ntok * topk + pairs - 1) / pairs), threads, 0, (cudaStream_t)stream>>>(z, src, pos, w, dy, ntok, topk,
+                                                                                           H, np, dz, dw);
+  };
+  if (np <= 8 * each) go(std::integral_constant<int, 8>{});  // as many lanes as hold the row
+  else if (np <= 32 * each) go(std::integral_constant<int, 32>{});
+  else if (np <= 64 * each) go(std::integral_constant<int, 64>{});
+  else if (np <= 128 * each) go(std::integral_constant<int, 128>{});
+  else go(std::integral_constant<int, 256>{});
   return launch_status(who);
 }
 
@@ -335,7 +415,7 @@ size_t dp_route_work_bytes(int64_t ntok, int topk, int nexp) {
   if (ntok < 0 || topk < 1 || topk > dpc::kMaxTopk || nexp < 1 || nexp > dpc::kMaxExperts || ntok > 0x7fffffffLL / topk)
     return 0;
   const dpc::PlanShape s = dpc::plan_shape(ntok * topk);
-  return s.blocks > 1 ? (size_t)s.blocks * nexp * sizeof(int) : 16;
+  return s.blocks > 1 ? (size_t)s.blocks * nexp * sizeof(int) : 1;
 }
 
 int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64_t *start, int32_t *src, int32_t *pos,
@@ -354,16 +434,18 @@ int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64
     if (work_bytes < dp_route_work_bytes(ntok, topk, nexp) || ((uintptr_t)work & 15))
       return set_error(DP_ERR_SHAPE, "%s: work buffer of %zu bytes is too short or misaligned", who, work_bytes);
   }
-  const size_t smem = (size_t)(kPlanWarps * nexp + nexp + 1 + kPlanWarps) * sizeof(int);
+  const size_t smem = (size_t)(kPlanWarps * nexp + kPlanWarps) * sizeof(int);
   const cudaStream_t st = (cudaStream_t)stream;
-  if (smem > 48 * 1024) {
-    const cudaError_t a = cudaFuncSetAttribute(plan_count_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    const cudaError_t b = cudaFuncSetAttribute(plan_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (a != cudaSuccess || b != cudaSuccess) return set_error(DP_ERR_CUDA, "%s: %zu bytes of shared memory", who, smem);
-  }
+  const int64_t n = ntok * topk;
   int *counts = s.blocks > 1 ? (int *)work : nullptr;
-  if (counts) plan_count_kernel<<<s.blocks, kPlanWarps * 32, smem, st>>>(expert, ntok * topk, s.chunk, nexp, counts);
-  plan_place_kernel<<<s.blocks, kPlanWarps * 32, smem, st>>>(expert, ntok * topk, s.chunk, nexp, counts, start, src, pos);
+  auto place = s.per == 8 ? plan_place_kernel<8> : plan_place_kernel<4>;
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(place, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+  }
+  auto count = s.per == 8 ? plan_count_kernel<8> : plan_count_kernel<4>;
+  if (counts) count<<<s.blocks, kPlanWarps * 32, nexp * sizeof(int), st>>>(expert, n, nexp, counts);
+  place<<<s.blocks, kPlanWarps * 32, smem, st>>>(expert, n, nexp, counts, start, src, pos);
   return launch_status(who);
 }
 

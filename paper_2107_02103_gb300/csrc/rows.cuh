@@ -5,6 +5,9 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <cstring>
+#include <type_traits>
+
 #include "dp_common.cuh"
 
 namespace dpc {
@@ -48,6 +51,47 @@ __device__ __forceinline__ Pack<T, V> load_pack(const T *p) {
 template <typename T, int V>
 __device__ __forceinline__ void store_pack(T *p, const Pack<T, V> &x) {
   *reinterpret_cast<Pack<T, V> *>(p) = x;
+}
+
+// The 16 bytes at p, whatever its alignment to them (p aligned to its elements), from the two aligned words that
+// hold them; near the ends lo, hi of its array, or past them (then zero), element by element.  A row of odd length
+// costs two loads for 16 bytes this way, the second from L1, against a load for each element.
+template <typename T>
+__device__ __forceinline__ Pack<T, 16 / (int)sizeof(T)> load_any(const T *p, const T *lo, const T *hi) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const uint32_t off = (uint32_t)((uintptr_t)p & 15);
+  const char *a = reinterpret_cast<const char *>(p) - off;
+  Pack<T, V> out;
+  if (off == 0 && p >= lo && p + V <= hi) return load_pack<T, V>(p);
+  if (a >= reinterpret_cast<const char *>(lo) && a + 32 <= reinterpret_cast<const char *>(hi)) {
+    const uint4 x = __ldg(reinterpret_cast<const uint4 *>(a)), y = __ldg(reinterpret_cast<const uint4 *>(a) + 1);
+    const uint32_t sh = (off & 3) * 8;
+    uint4 r;
+    switch (off >> 2) {  // the same for a whole row
+      case 0:
+        r = make_uint4(__funnelshift_r(x.x, x.y, sh), __funnelshift_r(x.y, x.z, sh), __funnelshift_r(x.z, x.w, sh),
+                       __funnelshift_r(x.w, y.x, sh));
+        break;
+      case 1:
+        r = make_uint4(__funnelshift_r(x.y, x.z, sh), __funnelshift_r(x.z, x.w, sh), __funnelshift_r(x.w, y.x, sh),
+                       __funnelshift_r(y.x, y.y, sh));
+        break;
+      case 2:
+        r = make_uint4(__funnelshift_r(x.z, x.w, sh), __funnelshift_r(x.w, y.x, sh), __funnelshift_r(y.x, y.y, sh),
+                       __funnelshift_r(y.y, y.z, sh));
+        break;
+      default:
+        r = make_uint4(__funnelshift_r(x.w, y.x, sh), __funnelshift_r(y.x, y.y, sh), __funnelshift_r(y.y, y.z, sh),
+                       __funnelshift_r(y.z, y.w, sh));
+    }
+    memcpy(&out, &r, 16);
+  } else {
+    T zero;
+    memset(&zero, 0, sizeof zero);
+#pragma unroll
+    for (int l = 0; l < V; ++l) out.v[l] = p + l >= lo && p + l < hi ? p[l] : zero;
+  }
+  return out;
 }
 
 // The widest pack (in elements) that rows of H elements at these addresses allow: 16 bytes down to one element.

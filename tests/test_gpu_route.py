@@ -37,7 +37,7 @@ def plan(expert, E):
 
 @pytest.mark.parametrize("T,k,E,drop", [
     (0, 1, 3, 0.0), (1, 1, 1, 0.0), (1, 2, 8, 0.0), (33, 3, 5, 0.3), (511, 2, 1024, 0.1), (4096, 2, 8, 0.0),
-    (4097, 2, 8, 0.2), (9001, 1, 2, 1.0), (20011, 3, 61, 0.2), (70001, 8, 7, 0.05), (3000, 5, 1023, 0.2),
+    (4097, 2, 8, 0.2), (9001, 1, 2, 1.0), (16384, 2, 9, 0.1), (16385, 2, 9, 0.1), (20011, 3, 61, 0.2), (70001, 8, 7, 0.05), (3000, 5, 1023, 0.2),
     (700001, 1, 3, 0.1)])
 def test_plan(T, k, E, drop):
     dpc = lib()
@@ -190,6 +190,6 @@ def test_refusals():
     with pytest.raises(ValueError):
         dpc.dp_route_combine_grad(z, src, pos, None, x, want=("dw",))
     with pytest.raises(dpc.DPError) as err:
-        dpc.dp_route_plan(torch.zeros(9000, 2, dtype=torch.int32, device="cuda"), 3,
+        dpc.dp_route_plan(torch.zeros(90000, 2, dtype=torch.int32, device="cuda"), 3,
                           work=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert err.value.code == dpc.DP_ERR_SHAPE
