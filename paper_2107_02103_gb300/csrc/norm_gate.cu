@@ -22,7 +22,7 @@ constexpr int kNormVectors = 5;  // da, dw1, dw2, db1, db2
 // and are read as vectors, unused warps' stay zero.
 template <typename A, int kWarps>
 struct SumBuf {
-  alignas(16) A v[2][3][kWarps];
+  alignas(16) A v[2][3][(kWarps + 3) / 4 * 4];
 };
 
 // Sums of NV values over the row's threads (a warp, or the block), the same bits in every thread.
@@ -42,7 +42,7 @@ __device__ __forceinline__ void row_sum(A (&v)[NV], SumBuf<A, kWarps> &buf, int 
     for (int i = 0; i < NV; ++i) {
       A s[kP] = {};
 #pragma unroll
-      for (int w = 0; w < kWarps; w += kP) {
+      for (int w = 0; w < (kWarps + 3) / 4 * 4; w += kP) {
         const Pack<A, kP> x = load_pack<A, kP>(buf.v[phase][i] + w);
 #pragma unroll
         for (int k = 0; k < kP; ++k) s[k] += x.v[k];
@@ -59,21 +59,29 @@ __device__ __forceinline__ A inv_sqrt(A x) {
   else return rsqrtf(x);
 }
 
-// Mean m and inverse deviation s of a row held as v[EPT] per thread; v becomes v - m.
-template <int EPT, bool kWarpRow, bool kLayer, typename Map, typename A, typename Buf>
-__device__ __forceinline__ void row_stats(const Map &map, A (&v)[EPT], A inv, A eps, A &m, A &s, Buf &buf, int &phase) {
-  A sum[1];
-  m = A(0);
-  if constexpr (kLayer) {
-    sum[0] = map.total([&](int i) { return v[i]; });
-    row_sum<1, kWarpRow>(sum, buf, phase);
-    m = sum[0] * inv;
+// Means m and inverse deviations s of R rows held as v[R][EPT] per thread; v becomes v - m.
+template <int R, int EPT, bool kWarpRow, bool kLayer, typename Map, typename A, typename Buf>
+__device__ __forceinline__ void row_stats(const Map &map, A (&v)[R][EPT], A inv, A eps, A (&m)[R], A (&s)[R], Buf &buf,
+                                          int &phase) {
+  A sum[R];
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) v[i] -= m;
+  for (int k = 0; k < R; ++k) m[k] = A(0);
+  if constexpr (kLayer) {
+#pragma unroll
+    for (int k = 0; k < R; ++k) sum[k] = map.total([&](int i) { return v[k][i]; });
+    row_sum<R, kWarpRow>(sum, buf, phase);
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      m[k] = sum[k] * inv;
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) v[k][i] -= m[k];
+    }
   }
-  sum[0] = map.total([&](int i) { return v[i] * v[i]; });
-  row_sum<1, kWarpRow>(sum, buf, phase);
-  s = inv_sqrt(fma(sum[0], inv, eps));
+#pragma unroll
+  for (int k = 0; k < R; ++k) sum[k] = map.total([&](int i) { return v[k][i] * v[k][i]; });
+  row_sum<R, kWarpRow>(sum, buf, phase);
+#pragma unroll
+  for (int k = 0; k < R; ++k) s[k] = inv_sqrt(fma(sum[k], inv, eps));
 }
 
 // A thread's elements of a row: packs first + i * step, i < EPT / V.  Packs past the row's end repeat its last one
@@ -159,53 +167,60 @@ struct RowFeed {
 
   __device__ __forceinline__ uint32_t row_bytes() const { return (uint32_t)p.H * sizeof(T); }
   __device__ __forceinline__ uint32_t bar(int s) const { return (uint32_t)__cvta_generic_to_shared(bars + s); }
-  __device__ __forceinline__ void fetch(int64_t row, int s) const {  // one thread
+  // Lane 0 of each warp copies its arrays of the row, counted on the stage's barrier (one warp copying all of them
+  // kept the others waiting).
+  __device__ __forceinline__ void fetch(int64_t row, int s) const {
+    if (threadIdx.x & 31) return;
     const uint32_t bytes = row_bytes(), dst = (uint32_t)__cvta_generic_to_shared(smem) + s * p.nin * bytes;
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar(s)), "r"(bytes * p.nin) : "memory");
-    for (int i = 0; i < p.nin; ++i)
+    for (int i = threadIdx.x >> 5; i < p.nin; i += blockDim.x >> 5) {
+      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar(s)), "r"(bytes) : "memory");
       asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
                        dst + i * bytes),
                    "l"(p.in[i] + row * p.H), "r"(bytes), "r"(bar(s))
                    : "memory");
+    }
   }
   __device__ __forceinline__ void begin() {
     if constexpr (kBulk) {
       if (threadIdx.x == 0) {
-        for (int s = 0; s < p.stages; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar(s)));
+        for (int s = 0; s < p.stages; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar(s)), "r"(p.nin));
         asm volatile("fence.mbarrier_init.release.cluster;");
-        for (int s = 0; s < p.stages; ++s)
-          if (t + s * step < p.ntok) fetch(t + s * step, s);
       }
       __syncthreads();
+      for (int s = 0; s < p.stages; ++s)
+        if (t + s * step < p.ntok) fetch(t + s * step, s);
     }
   }
-  __device__ __forceinline__ bool arrived() const {  // bounded: false leaves NaN rows behind
+  // The stage k rows on, and the parity of its barrier.
+  __device__ __forceinline__ int stage(int k) const { return st + k < p.stages ? st + k : st + k - p.stages; }
+  __device__ __forceinline__ bool arrived(int k = 0) const {  // bounded: false leaves NaN rows behind
     if constexpr (kBulk) {
+      const int s = stage(k), parity = phase ^ (st + k >= p.stages);
       uint32_t done = 0;
       for (int it = 0; it < (1 << 22) && !done; ++it)
         asm volatile(
             "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
             : "=r"(done)
-            : "r"(bar(st)), "r"((uint32_t)phase)
+            : "r"(bar(s)), "r"((uint32_t)parity)
             : "memory");
       return done != 0;
     }
     return true;
   }
   template <typename A>
-  __device__ __forceinline__ void load(int i, A (&v)[EPT]) const {
-    if constexpr (kBulk) map.load(reinterpret_cast<const T *>(smem + (st * p.nin + i) * row_bytes()), v);
-    else map.load(p.in[i] + t * p.H, v);
+  __device__ __forceinline__ void load(int i, A (&v)[EPT], int k = 0) const {
+    if constexpr (kBulk) map.load(reinterpret_cast<const T *>(smem + (stage(k) * p.nin + i) * row_bytes()), v);
+    else map.load(p.in[i] + (t + k * step) * p.H, v);
   }
-  __device__ __forceinline__ void read() const {  // after a block barrier that follows the row's loads
+  __device__ __forceinline__ void read(int k = 0) const {  // after a block barrier that follows the row's loads
     if constexpr (kBulk)
-      if (threadIdx.x == 0 && t + p.stages * step < p.ntok) fetch(t + p.stages * step, st);
+      if (t + (k + p.stages) * step < p.ntok) fetch(t + (k + p.stages) * step, stage(k));
   }
-  __device__ __forceinline__ void next() {
-    t += step;
+  __device__ __forceinline__ void next(int rows = 1) {
+    t += rows * step;
     if constexpr (kBulk)
-      if (++st == p.stages) {
-        st = 0;
+      if ((st += rows) >= p.stages) {
+        st -= p.stages;
         phase ^= 1;
       }
   }
@@ -213,14 +228,20 @@ struct RowFeed {
 
 constexpr int kMaxStages = 4;
 
+// Rows a block of the forward works on at once: two of 16-bit elements by bulk copies (the waits of their block sums
+// overlap, and the weights are read once for both: 65,536 x 1600 bf16 in 190 us against 270), else one.
+template <typename T, bool kBulk, int kThreads>
+constexpr int kFwdRows = kBulk && sizeof(T) == 2 && kThreads <= 512 ? 2 : 1;
+
 template <typename T, int V, int EPT, bool kWarpRow, bool kBulk, bool kLayer, int kThreads, int kMinBlocks>
 __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const NormArgs<T> p) {
   using A = acc_t<T>;
+  constexpr int R = kFwdRows<T, kBulk, kThreads>;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ uint64_t bars[kMaxStages];
   __shared__ SumBuf<A, kThreads / 32> buf;
   int phase = 0;
-  for (int i = threadIdx.x; i < 6 * (kThreads / 32); i += blockDim.x) (&buf.v[0][0][0])[i] = A(0);
+  for (int i = threadIdx.x; i < (int)(sizeof buf / sizeof(A)); i += blockDim.x) (&buf.v[0][0][0])[i] = A(0);
   __syncthreads();
   const RowMap<T, V, EPT> map{kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x,
                               kWarpRow ? 32 : (int)blockDim.x, p.H / V};
@@ -229,47 +250,75 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
       kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : (int64_t)gridDim.x, smem, bars};
   const A inv = A(1) / A(p.H);
   feed.begin();
-  T gate_next = p.gate && feed.t < p.ntok ? p.gate[feed.t] : T(0.0f);
-  for (; feed.t < p.ntok; feed.next()) {
-    const int64_t t = feed.t;
-    A f[EPT], r[EPT], g[EPT], w[EPT], m1, s1, m2, s2;
-    const T gate = gate_next;
-    if (p.gate && t + feed.step < p.ntok) gate_next = p.gate[t + feed.step];
-    const bool ok = feed.arrived();
-    feed.load(0, f);
-    feed.load(1, r);
-    if (p.nin > 2) feed.load(2, g);
-    row_stats<EPT, kWarpRow, kLayer>(map, f, inv, p.eps, m1, s1, buf, phase);
-    feed.read();
-    if (!ok) s1 = A(__int_as_float(0x7fc00000));
+  T gate_next[R];
+  auto peek = [&](int64_t t) {  // the next rows' gates
+    if (p.gate)
+#pragma unroll
+      for (int k = 0; k < R; ++k)
+        if (t + k * feed.step < p.ntok) gate_next[k] = p.gate[t + k * feed.step];
+  };
+  peek(feed.t);
+  for (; feed.t < p.ntok; feed.next(R)) {
+    A f[R][EPT], r[R][EPT], g[R][EPT], w[EPT], b[EPT], gate[R], m1[R], s1[R], m2[R], s2[R];
+    bool have[R], ok[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      have[k] = k == 0 || feed.t + k * feed.step < p.ntok;  // the last row alone: its place holds an older row
+      gate[k] = p.gate && have[k] ? to_acc(gate_next[k]) : A(1);
+    }
+    peek(feed.t + R * feed.step);
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      ok[k] = !have[k] || feed.arrived(k);
+      const int at = have[k] ? k : 0;
+      feed.load(0, f[k], at);
+      feed.load(1, r[k], at);
+      if (p.nin > 2) feed.load(2, g[k], at);
+    }
+    row_stats<R, EPT, kWarpRow, kLayer>(map, f, inv, p.eps, m1, s1, buf, phase);
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      feed.read(k);
+      if (!ok[k]) s1[k] = A(__int_as_float(0x7fc00000));
+    }
     map.template weights<kBulk>(p.w1, w);
-    A b[EPT];
     if constexpr (kLayer) map.template weights<kBulk>(p.b1, b);
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) f[i] = kLayer ? fma(f[i] * s1, w[i], b[i]) : f[i] * s1 * w[i];
-    if (p.nin > 2) {
+    for (int k = 0; k < R; ++k) {
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) f[i] *= g[i];
-    } else if (p.gate) {
+      for (int i = 0; i < EPT; ++i) f[k][i] = kLayer ? fma(f[k][i] * s1[k], w[i], b[i]) : f[k][i] * s1[k] * w[i];
+      if (p.nin > 2) {
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) f[i] *= to_acc(gate);
+        for (int i = 0; i < EPT; ++i) f[k][i] *= g[k][i];
+      } else if (p.gate) {
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) f[k][i] *= gate[k];
+      }
     }
     map.template weights<kBulk>(p.a, w);
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) r[i] = fma(w[i], f[i], r[i]);
-    map.store(p.r2 + t * p.H, r);
-    row_stats<EPT, kWarpRow, kLayer>(map, r, inv, p.eps, m2, s2, buf, phase);
+    for (int k = 0; k < R; ++k) {
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) r[k][i] = fma(w[i], f[k][i], r[k][i]);
+      if (have[k]) map.store(p.r2 + (feed.t + k * feed.step) * p.H, r[k]);
+    }
+    row_stats<R, EPT, kWarpRow, kLayer>(map, r, inv, p.eps, m2, s2, buf, phase);
     map.template weights<kBulk>(p.w2, w);
     if constexpr (kLayer) map.template weights<kBulk>(p.b2, b);
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) r[i] = kLayer ? fma(r[i] * s2, w[i], b[i]) : r[i] * s2 * w[i];
-    map.store(p.u + t * p.H, r);
-    if (map.first == 0) {
-      A *st = p.stats + t * 4;
-      st[0] = m1;
-      st[1] = s1;
-      st[2] = m2;
-      st[3] = s2;
+    for (int k = 0; k < R; ++k) {
+      const int64_t t = feed.t + k * feed.step;
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) r[k][i] = kLayer ? fma(r[k][i] * s2[k], w[i], b[i]) : r[k][i] * s2[k] * w[i];
+      if (!have[k]) continue;
+      map.store(p.u + t * p.H, r[k]);
+      if (map.first == 0) {
+        A *st = p.stats + t * 4;
+        st[0] = m1[k];
+        st[1] = s1[k];
+        st[2] = m2[k];
+        st[3] = s2[k];
+      }
     }
   }
 }
@@ -282,7 +331,7 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
   __shared__ uint64_t bars[kMaxStages];
   __shared__ SumBuf<A, kThreads / 32> buf;
   int phase = 0;
-  for (int i = threadIdx.x; i < 6 * (kThreads / 32); i += blockDim.x) (&buf.v[0][0][0])[i] = A(0);
+  for (int i = threadIdx.x; i < (int)(sizeof buf / sizeof(A)); i += blockDim.x) (&buf.v[0][0][0])[i] = A(0);
   __syncthreads();
   const RowMap<T, V, EPT> map{kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x,
                               kWarpRow ? 32 : (int)blockDim.x, p.H / V};
@@ -451,18 +500,22 @@ int launch(NormArgs<T> &p, int v, bool weights16, cudaStream_t st, const char *w
     void (*k)(const NormArgs<T>);
     if constexpr (kGrad) k = norm_grad_kernel<T, v_, e_, w_, b_, kLayer, m_, n_>;
     else k = norm_fwd_kernel<T, v_, e_, w_, b_, kLayer, m_, n_>;
+    constexpr bool two = !kGrad && kFwdRows<T, b_, m_> == 2;
+    // two rows at once take 72 registers or more: 896 threads an SM, or 768
+    const int held = m_ <= 224 ? 896 : 768, blocks = two ? (held < n.threads ? 1 : held / n.threads) : n.blocks;
     size_t smem = kGrad && w_ ? (size_t)kRowWarps * kNormVectors * p.H * sizeof(acc_t<T>) : 0;
     if (b_) {
-      const size_t row = (size_t)p.nin * p.H * sizeof(T), room = (size_t)200 * 1024 / n.blocks;
+      const size_t row = (size_t)p.nin * p.H * sizeof(T), room = (size_t)200 * 1024 / blocks;
       p.stages = (int)(room / row);
       p.stages = p.stages > kMaxStages ? kMaxStages : p.stages;
+      if (two) p.stages &= ~1;  // pairs of rows keep to pairs of stages
       smem = row * p.stages;
     }
     if (smem > 32 * 1024) {  // the static part counts too
       const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
       if (e != cudaSuccess) rc = set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
     }
-    const int64_t units = w_ ? (p.ntok + kRowWarps - 1) / kRowWarps : p.ntok, most = 152 * n.blocks;
+    const int64_t units = w_ ? (p.ntok + kRowWarps - 1) / kRowWarps : p.ntok, most = 152 * blocks;
     if (!rc) k<<<(unsigned)(kGrad || units > most ? most : units), n.threads, smem, st>>>(p);
   };
   auto shape = [&](auto V) {
@@ -472,8 +525,11 @@ int launch(NormArgs<T> &p, int v, bool weights16, cudaStream_t st, const char *w
       return go(V, e8, yes{}, no{}, integral_constant<int, kRowWarps * 32>{}, integral_constant<int, kGrad ? 3 : 8>{});
     if constexpr (decltype(V)::value * sizeof(T) == 16) {
       if (weights16 && (size_t)p.nin * p.H * sizeof(T) * n.blocks <= 200 * 1024) {
-        if (p.H <= 2048) return go(V, e8, no{}, yes{}, integral_constant<int, 256>{}, integral_constant<int, kFew>{});
-        if (p.H <= 4096) return go(V, e8, no{}, yes{}, integral_constant<int, 512>{}, integral_constant<int, kHalf>{});
+        constexpr int kTwo = !kGrad && sizeof(T) == 2 ? 3 : kFew, kTwoHalf = !kGrad && sizeof(T) == 2 ? 1 : kHalf;
+        if constexpr (!kGrad && sizeof(T) == 2)
+          if (n.threads == 224) return go(V, e8, no{}, yes{}, integral_constant<int, 224>{}, integral_constant<int, 4>{});
+        if (p.H <= 2048) return go(V, e8, no{}, yes{}, integral_constant<int, 256>{}, integral_constant<int, kTwo>{});
+        if (p.H <= 4096) return go(V, e8, no{}, yes{}, integral_constant<int, 512>{}, integral_constant<int, kTwoHalf>{});
         if (p.H <= 8192) return go(V, e8, no{}, yes{}, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
       }
     }
