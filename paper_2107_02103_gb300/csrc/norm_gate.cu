@@ -86,12 +86,22 @@ __device__ __forceinline__ void row_stats(const Map &map, A (&v)[R][EPT], A inv,
 
 // A thread's elements of a row: packs first + i * step, i < EPT / V.  Packs past the row's end repeat its last one
 // (so that loads need no zeros) and are left out of sums and stores.
-template <typename T, int V, int EPT>
+//
+// Cut rows (of a length that is no multiple of 16 bytes, in arrays that begin at one): the packs are the aligned words
+// under the row, `off` elements of the first lie before it, and the ends' packs are partly the neighbours'.  Blocks
+// take rows a multiple of eight apart, which all begin at the same place in their word, so that off, the columns a
+// thread sums and the weights beside its elements stay the same for all of a block's rows.
+template <typename T, int V, int EPT, bool kCut>
 struct RowMap {
   static constexpr int kN = EPT / V;
   int first, step, np;  // first pack, stride between packs, packs in the row
+  int off, H;           // cut rows only
   __device__ __forceinline__ bool in(int i) const { return first + i * step < np; }
   __device__ __forceinline__ int at(int i) const { return min(first + i * step, np - 1) * V; }
+  // Whether element l of pack i is the row's; its pack must be in.
+  __device__ __forceinline__ bool mine(int i, int l) const {
+    return !kCut || (unsigned)(at(i) + l - off) < (unsigned)H;
+  }
   template <typename S, typename A>
   __device__ __forceinline__ void load(const S *row, A (&v)[EPT]) const {
     Pack<S, V> x[kN];
@@ -100,8 +110,8 @@ struct RowMap {
 #pragma unroll
     for (int i = 0; i < EPT; ++i) v[i] = to_acc(x[i / V].v[i % V]);
   }
-  // The shared weights, read for every row again: they stay in L1 and would cost 40 registers otherwise.  Vec: their
-  // arrays are 16-byte aligned and V elements a multiple of 16 bytes.
+  // The shared weights, read for every row again: they stay in L1 (cut rows: in shared memory, moved by off) and would
+  // cost 40 registers otherwise.  Vec: their arrays are 16-byte aligned and V elements a multiple of 16 bytes.
   template <bool Vec, typename A>
   __device__ __forceinline__ void weights(const A *w, A (&v)[EPT]) const {
     constexpr int kP = Vec ? 16 / (int)sizeof(A) : 1;
@@ -116,28 +126,41 @@ struct RowMap {
   }
   template <typename A>
   __device__ __forceinline__ void store(T *row, const A (&v)[EPT]) const {
+    if constexpr (kCut) row -= off;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       Pack<T, V> x;
 #pragma unroll
       for (int l = 0; l < V; ++l) x.v[l] = from_acc<T>(v[i * V + l]);
-      if (in(i)) store_pack<T, V>(row + at(i), x);
+      if (!in(i)) continue;
+      if (mine(i, 0) && mine(i, V - 1)) store_pack<T, V>(row + at(i), x);
+      else
+#pragma unroll
+        for (int l = 0; l < V; ++l)
+          if (mine(i, l)) row[at(i) + l] = x.v[l];
     }
   }
   // The sum of f(i) over the elements that are in the row.
   template <typename F>
   __device__ __forceinline__ auto total(F f) const {
-    decltype(f(0)) s = 0;
+    using A = decltype(f(0));
+    A s = 0;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      decltype(f(0)) q = f(i * V);
+      A q = mine(i, 0) ? f(i * V) : A(0);
 #pragma unroll
-      for (int l = 1; l < V; ++l) q += f(i * V + l);
-      s += in(i) ? q : 0;
+      for (int l = 1; l < V; ++l) q += mine(i, l) ? f(i * V + l) : A(0);
+      s += in(i) ? q : A(0);
     }
     return s;
   }
 };
+
+// Bytes a cut row of H may lie under.
+template <typename T>
+__host__ __device__ constexpr uint32_t cut_bytes(int H) {
+  return (uint32_t)((H * sizeof(T) + 30) / 16 * 16);
+}
 
 template <typename T>
 struct NormArgs {
@@ -154,29 +177,38 @@ struct NormArgs {
   acc_t<T> *part;  // [blocks][5][H] partial column sums
 };
 
-// How rows reach a block: plain loads, or (bulk) whole rows copied ahead into shared memory, `stages` rows deep.
-// A stage may be refilled once every thread has read it, which the first block sum of a row implies.
-template <typename T, int V, int EPT, bool kBulk>
+// How rows reach a block: plain loads, or whole rows copied ahead into shared memory in bulk, `stages` rows deep
+// (kCut: the aligned words under the rows).  A stage may be refilled once every thread has read it, which the first
+// block sum of a row implies.
+enum Feed { kPlain, kBulkRows, kCutRows };
+
+template <typename T, int V, int EPT, Feed kFeed>
 struct RowFeed {
+  static constexpr bool kBulk = kFeed != kPlain, kCut = kFeed == kCutRows;
   const NormArgs<T> &p;
-  const RowMap<T, V, EPT> &map;
+  const RowMap<T, V, EPT, kCut> &map;
   int64_t t, step;  // the row at hand, and to the next one
   unsigned char *smem;
   uint64_t *bars;
   int st = 0, phase = 0;
 
-  __device__ __forceinline__ uint32_t row_bytes() const { return (uint32_t)p.H * sizeof(T); }
+  __device__ __forceinline__ uint32_t row_bytes() const {  // of a place in a stage
+    return kCut ? cut_bytes<T>(p.H) : (uint32_t)p.H * sizeof(T);
+  }
   __device__ __forceinline__ uint32_t bar(int s) const { return (uint32_t)__cvta_generic_to_shared(bars + s); }
   // Lane 0 of each warp copies its arrays of the row, counted on the stage's barrier (one warp copying all of them
   // kept the others waiting).
   __device__ __forceinline__ void fetch(int64_t row, int s) const {
     if (threadIdx.x & 31) return;
-    const uint32_t bytes = row_bytes(), dst = (uint32_t)__cvta_generic_to_shared(smem) + s * p.nin * bytes;
+    const uint32_t place = row_bytes(), dst = (uint32_t)__cvta_generic_to_shared(smem) + s * p.nin * place;
+    uint32_t bytes = place;
+    if constexpr (kCut)  // the last row's last word may reach past the array: load() takes what is left out here
+      bytes = row == p.ntok - 1 ? (uint32_t)(map.off + p.H) * sizeof(T) & ~15u : (uint32_t)map.np * 16u;
     for (int i = threadIdx.x >> 5; i < p.nin; i += blockDim.x >> 5) {
       asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar(s)), "r"(bytes) : "memory");
       asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                       dst + i * bytes),
-                   "l"(p.in[i] + row * p.H), "r"(bytes), "r"(bar(s))
+                       dst + i * place),
+                   "l"(p.in[i] + row * p.H - (kCut ? map.off : 0)), "r"(bytes), "r"(bar(s))
                    : "memory");
     }
   }
@@ -211,6 +243,15 @@ struct RowFeed {
   __device__ __forceinline__ void load(int i, A (&v)[EPT], int k = 0) const {
     if constexpr (kBulk) map.load(reinterpret_cast<const T *>(smem + (stage(k) * p.nin + i) * row_bytes()), v);
     else map.load(p.in[i] + (t + k * step) * p.H, v);
+    if constexpr (kCut)
+      if (t + k * step == p.ntok - 1) {
+#pragma unroll
+        for (int q = 0; q < map.kN; ++q)
+          if (map.in(q) && map.at(q) == (map.np - 1) * V)
+#pragma unroll
+            for (int l = 0; l < V; ++l)
+              if (map.mine(q, l)) v[q * V + l] = to_acc(p.in[i][(t + k * step) * p.H + map.at(q) + l - map.off]);
+      }
   }
   __device__ __forceinline__ void read(int k = 0) const {  // after a block barrier that follows the row's loads
     if constexpr (kBulk)
@@ -228,14 +269,23 @@ struct RowFeed {
 
 constexpr int kMaxStages = 4;
 
+// Cut rows' weights into shared memory, beside the packs of a row that begins at `off`: vector i at out + i * room.
+template <typename A>
+__device__ __forceinline__ void move_weights(const A *const (&from)[5], int n, int off, int H, int room, A *out) {
+  for (int i = 0; i < n; ++i)
+    for (int c = threadIdx.x; c < room; c += blockDim.x)
+      out[i * room + c] = (unsigned)(c - off) < (unsigned)H ? __ldg(from[i] + c - off) : A(0);
+}
+
 // Rows a block of the forward works on at once: two of 16-bit elements by bulk copies (the waits of their block sums
 // overlap, and the weights are read once for both: 65,536 x 1600 bf16 in 190 us against 270), else one.
 template <typename T, bool kBulk, int kThreads>
 constexpr int kFwdRows = kBulk && sizeof(T) == 2 && kThreads <= 512 ? 2 : 1;
 
-template <typename T, int V, int EPT, bool kWarpRow, bool kBulk, bool kLayer, int kThreads, int kMinBlocks>
+template <typename T, int V, int EPT, bool kWarpRow, Feed kFeed, bool kLayer, int kThreads, int kMinBlocks>
 __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const NormArgs<T> p) {
   using A = acc_t<T>;
+  constexpr bool kBulk = kFeed != kPlain, kCut = kFeed == kCutRows;
   constexpr int R = kFwdRows<T, kBulk, kThreads>;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ uint64_t bars[kMaxStages];
@@ -243,13 +293,22 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
   int phase = 0;
   for (int i = threadIdx.x; i < (int)(sizeof buf / sizeof(A)); i += blockDim.x) (&buf.v[0][0][0])[i] = A(0);
   __syncthreads();
-  const RowMap<T, V, EPT> map{kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x,
-                              kWarpRow ? 32 : (int)blockDim.x, p.H / V};
-  RowFeed<T, V, EPT, kBulk> feed{
+  const int off = kCut ? (int)((uint64_t)blockIdx.x * p.H % V) : 0;
+  const RowMap<T, V, EPT, kCut> map{kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x,
+                                    kWarpRow ? 32 : (int)blockDim.x, kCut ? (off + p.H + V - 1) / V : p.H / V, off, p.H};
+  RowFeed<T, V, EPT, kFeed> feed{
       p, map, kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : (int64_t)blockIdx.x,
       kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : (int64_t)gridDim.x, smem, bars};
   const A inv = A(1) / A(p.H);
   feed.begin();
+  const A *wa = p.a, *w1 = p.w1, *w2 = p.w2, *b1 = p.b1, *b2 = p.b2;
+  if constexpr (kCut) {
+    A *ws = reinterpret_cast<A *>(smem + p.stages * p.nin * feed.row_bytes());
+    const int room = cut_bytes<T>(p.H) / sizeof(T);
+    move_weights<A>({p.a, p.w1, p.w2, p.b1, p.b2}, kLayer ? 5 : 3, off, p.H, room, ws);
+    wa = ws, w1 = ws + room, w2 = ws + 2 * room, b1 = ws + 3 * room, b2 = ws + 4 * room;
+    __syncthreads();
+  }
   T gate_next[R];
   auto peek = [&](int64_t t) {  // the next rows' gates
     if (p.gate)
@@ -281,8 +340,8 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
       feed.read(k);
       if (!ok[k]) s1[k] = A(__int_as_float(0x7fc00000));
     }
-    map.template weights<kBulk>(p.w1, w);
-    if constexpr (kLayer) map.template weights<kBulk>(p.b1, b);
+    map.template weights<kBulk>(w1, w);
+    if constexpr (kLayer) map.template weights<kBulk>(b1, b);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
 #pragma unroll
@@ -295,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
         for (int i = 0; i < EPT; ++i) f[k][i] *= gate[k];
       }
     }
-    map.template weights<kBulk>(p.a, w);
+    map.template weights<kBulk>(wa, w);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
 #pragma unroll
@@ -303,8 +362,8 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
       if (have[k]) map.store(p.r2 + (feed.t + k * feed.step) * p.H, r[k]);
     }
     row_stats<R, EPT, kWarpRow, kLayer>(map, r, inv, p.eps, m2, s2, buf, phase);
-    map.template weights<kBulk>(p.w2, w);
-    if constexpr (kLayer) map.template weights<kBulk>(p.b2, b);
+    map.template weights<kBulk>(w2, w);
+    if constexpr (kLayer) map.template weights<kBulk>(b2, b);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       const int64_t t = feed.t + k * feed.step;
@@ -324,18 +383,20 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
 }
 
 // A thread keeps its columns' sums over the rows of its block (or warp) in registers.
-template <typename T, int V, int EPT, bool kWarpRow, bool kBulk, bool kLayer, int kThreads, int kMinBlocks>
+template <typename T, int V, int EPT, bool kWarpRow, Feed kFeed, bool kLayer, int kThreads, int kMinBlocks>
 __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const NormArgs<T> p) {
   using A = acc_t<T>;
+  constexpr bool kBulk = kFeed != kPlain, kCut = kFeed == kCutRows;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ uint64_t bars[kMaxStages];
   __shared__ SumBuf<A, kThreads / 32> buf;
   int phase = 0;
   for (int i = threadIdx.x; i < (int)(sizeof buf / sizeof(A)); i += blockDim.x) (&buf.v[0][0][0])[i] = A(0);
   __syncthreads();
-  const RowMap<T, V, EPT> map{kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x,
-                              kWarpRow ? 32 : (int)blockDim.x, p.H / V};
-  RowFeed<T, V, EPT, kBulk> feed{
+  const int off = kCut ? (int)((uint64_t)blockIdx.x * p.H % V) : 0;
+  const RowMap<T, V, EPT, kCut> map{kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x,
+                                    kWarpRow ? 32 : (int)blockDim.x, kCut ? (off + p.H + V - 1) / V : p.H / V, off, p.H};
+  RowFeed<T, V, EPT, kFeed> feed{
       p, map, kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : (int64_t)blockIdx.x,
       kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : (int64_t)gridDim.x, smem, bars};
   A sa[EPT], sw1[EPT], sw2[EPT], sb1[EPT], sb2[EPT];
@@ -343,6 +404,14 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
   for (int i = 0; i < EPT; ++i) sa[i] = sw1[i] = sw2[i] = sb1[i] = sb2[i] = A(0);
   const A inv = A(1) / A(p.H);
   feed.begin();
+  const A *wa = p.a, *w1 = p.w1, *w2 = p.w2, *b1 = p.b1;
+  if constexpr (kCut) {
+    A *ws = reinterpret_cast<A *>(smem + p.stages * p.nin * feed.row_bytes());
+    const int room = cut_bytes<T>(p.H) / sizeof(T);
+    move_weights<A>({p.a, p.w1, p.w2, p.b1, nullptr}, kLayer ? 4 : 3, off, p.H, room, ws);
+    wa = ws, w1 = ws + room, w2 = ws + 2 * room, b1 = ws + 3 * room;
+    __syncthreads();
+  }
   const bool each = p.nin > 4;  // a gate value for each element
   A st_next[4] = {};
   T gate_next = T(0.0f);
@@ -368,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
     else
 #pragma unroll
       for (int i = 0; i < EPT; ++i) g[i] = gt;
-    map.template weights<kBulk>(p.w2, w);
+    map.template weights<kBulk>(w2, w);
 #pragma unroll
     for (int i = 0; i < EPT; ++i) {
       n2[i] = (n2[i] - m2) * s2;
@@ -387,14 +456,14 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
 #pragma unroll
     for (int i = 0; i < EPT; ++i) dr[i] = fma(s2, du[i] - (kLayer ? fma(n2[i], along, mean) : n2[i] * along), dr[i]);
     map.store(p.dr + t * p.H, dr);
-    map.template weights<kBulk>(p.w1, w);
-    if constexpr (kLayer) map.template weights<kBulk>(p.b1, n2);
+    map.template weights<kBulk>(w1, w);
+    if constexpr (kLayer) map.template weights<kBulk>(b1, n2);
 #pragma unroll
     for (int i = 0; i < EPT; ++i) {  // du: p from here on
       du[i] = kLayer ? fma(f[i], w[i], n2[i]) : f[i] * w[i];
       sa[i] = fma(dr[i] * g[i], du[i], sa[i]);
     }
-    map.template weights<kBulk>(p.a, n2);
+    map.template weights<kBulk>(wa, n2);
 #pragma unroll
     for (int i = 0; i < EPT; ++i) {
       const A dra = dr[i] * n2[i], dp = dra * g[i];
@@ -429,8 +498,8 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
     A *all = reinterpret_cast<A *>(smem), *mine = all + (threadIdx.x >> 5) * kVec * p.H;
 #pragma unroll
     for (int i = 0; i < EPT; ++i)
-      if (map.in(i / V)) {
-        A *o = mine + map.at(i / V) + i % V;
+      if (map.in(i / V) && map.mine(i / V, i % V)) {
+        A *o = mine + map.at(i / V) + i % V - off;
         o[0] = sa[i], o[p.H] = sw1[i], o[2 * p.H] = sw2[i];
         if constexpr (kLayer) o[3 * p.H] = sb1[i], o[4 * p.H] = sb2[i];
       }
@@ -443,8 +512,8 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
   } else {
 #pragma unroll
     for (int i = 0; i < EPT; ++i)
-      if (map.in(i / V)) {
-        A *o = out + map.at(i / V) + i % V;
+      if (map.in(i / V) && map.mine(i / V, i % V)) {
+        A *o = out + map.at(i / V) + i % V - off;
         o[0] = sa[i], o[p.H] = sw1[i], o[2 * p.H] = sw2[i];
         if constexpr (kLayer) o[3 * p.H] = sb1[i], o[4 * p.H] = sb2[i];
       }
@@ -485,10 +554,11 @@ NormShape norm_shape(int H, bool grad) {
   return {ept, threads, blocks < 1 ? 1 : blocks};
 }
 
-// Rows whose bytes and addresses are multiples of 16 come by bulk copies, as many rows ahead as fit; other rows by
-// plain loads of the widest pack they allow.
+// Rows whose bytes and addresses are multiples of 16 come by bulk copies, as many rows ahead as fit; so do rows of other
+// lengths up to 2048 in arrays that begin at a multiple of 16 (cut rows); the rest by plain loads of the widest pack they
+// allow.
 template <typename T, bool kGrad, bool kLayer>
-int launch(NormArgs<T> &p, int v, bool weights16, cudaStream_t st, const char *who) {
+int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st, const char *who) {
   using std::integral_constant;
   using no = std::false_type;
   using yes = std::true_type;
@@ -496,47 +566,61 @@ int launch(NormArgs<T> &p, int v, bool weights16, cudaStream_t st, const char *w
   int rc = DP_OK;
   auto go = [&](auto V, auto E, auto W, auto B, auto M, auto N) {
     constexpr int v_ = decltype(V)::value, e_ = decltype(E)::value, m_ = decltype(M)::value, n_ = decltype(N)::value;
-    constexpr bool w_ = decltype(W)::value, b_ = decltype(B)::value;
+    constexpr bool w_ = decltype(W)::value, b_ = decltype(B)::value != kPlain;
+    constexpr Feed f_ = decltype(B)::value;
     void (*k)(const NormArgs<T>);
-    if constexpr (kGrad) k = norm_grad_kernel<T, v_, e_, w_, b_, kLayer, m_, n_>;
-    else k = norm_fwd_kernel<T, v_, e_, w_, b_, kLayer, m_, n_>;
+    if constexpr (kGrad) k = norm_grad_kernel<T, v_, e_, w_, f_, kLayer, m_, n_>;
+    else k = norm_fwd_kernel<T, v_, e_, w_, f_, kLayer, m_, n_>;
     constexpr bool two = !kGrad && kFwdRows<T, b_, m_> == 2;
     // two rows at once take 72 registers or more: 896 threads an SM, or 768
-    const int held = m_ <= 224 ? 896 : 768, blocks = two ? (held < n.threads ? 1 : held / n.threads) : n.blocks;
+    const int held = m_ <= 224 ? 896 : 768;
+    int blocks = two ? (held < n.threads ? 1 : held / n.threads) : n.blocks;
     size_t smem = kGrad && w_ ? (size_t)kRowWarps * kNormVectors * p.H * sizeof(acc_t<T>) : 0;
     if (b_) {
-      const size_t row = (size_t)p.nin * p.H * sizeof(T), room = (size_t)200 * 1024 / blocks;
-      p.stages = (int)(room / row);
-      p.stages = p.stages > kMaxStages ? kMaxStages : p.stages;
-      if (two) p.stages &= ~1;  // pairs of rows keep to pairs of stages
-      smem = row * p.stages;
+      const size_t row = (size_t)p.nin * (f_ == kCutRows ? cut_bytes<T>(p.H) : p.H * sizeof(T));
+      const size_t weights = f_ == kCutRows ? cut_bytes<T>(p.H) / sizeof(T) * kNormVectors * sizeof(acc_t<T>) : 0;
+      for (;; --blocks) {  // fewer blocks an SM where their rows would not fit
+        const int64_t room = (int64_t)200 * 1024 / blocks - (int64_t)weights;
+        p.stages = room < 0 ? 0 : room / (int64_t)row > kMaxStages ? kMaxStages : (int)(room / (int64_t)row);
+        if (two) p.stages &= ~1;  // pairs of rows keep to pairs of stages
+        if (p.stages > 0 || blocks == 1) break;
+      }
+      smem = row * p.stages + weights;
     }
     if (smem > 32 * 1024) {  // the static part counts too
       const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
       if (e != cudaSuccess) rc = set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
     }
-    const int64_t units = w_ ? (p.ntok + kRowWarps - 1) / kRowWarps : p.ntok, most = 152 * blocks;
+    const int64_t units = w_ ? (p.ntok + kRowWarps - 1) / kRowWarps : p.ntok, most = 152 * (kGrad ? n.blocks : blocks);
     if (!rc) k<<<(unsigned)(kGrad || units > most ? most : units), n.threads, smem, st>>>(p);
   };
   auto shape = [&](auto V) {
     constexpr integral_constant<int, 8> e8{};
     constexpr int kFew = kGrad ? 2 : 4, kHalf = kGrad ? 1 : 2;
+    constexpr integral_constant<Feed, kPlain> plain{};
+    constexpr integral_constant<Feed, kBulkRows> bulk{};
+    constexpr integral_constant<Feed, kCutRows> cut{};
     if (p.H <= 256)
-      return go(V, e8, yes{}, no{}, integral_constant<int, kRowWarps * 32>{}, integral_constant<int, kGrad ? 3 : 8>{});
+      return go(V, e8, yes{}, plain, integral_constant<int, kRowWarps * 32>{}, integral_constant<int, kGrad ? 3 : 8>{});
     if constexpr (decltype(V)::value * sizeof(T) == 16) {
       if (weights16 && (size_t)p.nin * p.H * sizeof(T) * n.blocks <= 200 * 1024) {
         constexpr int kTwo = !kGrad && sizeof(T) == 2 ? 3 : kFew, kTwoHalf = !kGrad && sizeof(T) == 2 ? 1 : kHalf;
         if constexpr (!kGrad && sizeof(T) == 2)
-          if (n.threads == 224) return go(V, e8, no{}, yes{}, integral_constant<int, 224>{}, integral_constant<int, 4>{});
-        if (p.H <= 2048) return go(V, e8, no{}, yes{}, integral_constant<int, 256>{}, integral_constant<int, kTwo>{});
-        if (p.H <= 4096) return go(V, e8, no{}, yes{}, integral_constant<int, 512>{}, integral_constant<int, kTwoHalf>{});
-        if (p.H <= 8192) return go(V, e8, no{}, yes{}, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+          if (n.threads == 224) return go(V, e8, no{}, bulk, integral_constant<int, 224>{}, integral_constant<int, 4>{});
+        if (p.H <= 2048) return go(V, e8, no{}, bulk, integral_constant<int, 256>{}, integral_constant<int, kTwo>{});
+        if (p.H <= 4096) return go(V, e8, no{}, bulk, integral_constant<int, 512>{}, integral_constant<int, kTwoHalf>{});
+        if (p.H <= 8192) return go(V, e8, no{}, bulk, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
       }
     }
-    if (p.H <= 2048) return go(V, e8, no{}, no{}, integral_constant<int, 256>{}, integral_constant<int, kFew>{});
-    if (p.H <= 4096) return go(V, e8, no{}, no{}, integral_constant<int, 512>{}, integral_constant<int, kHalf>{});
-    if (p.H <= 8192) return go(V, e8, no{}, no{}, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
-    go(V, integral_constant<int, 16>{}, no{}, no{}, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+    if constexpr (decltype(V)::value * sizeof(T) != 16 && sizeof(T) < 8) {
+      constexpr int kTwo = !kGrad && sizeof(T) == 2 ? 3 : kFew;
+      if (bases16 && p.H <= 2048 && cut_bytes<T>(p.H) / sizeof(T) <= (size_t)n.threads * 8)  // a place for every pack
+        return go(integral_constant<int, 16 / (int)sizeof(T)>{}, e8, no{}, cut, integral_constant<int, 256>{}, integral_constant<int, kTwo>{});
+    }
+    if (p.H <= 2048) return go(V, e8, no{}, plain, integral_constant<int, 256>{}, integral_constant<int, kFew>{});
+    if (p.H <= 4096) return go(V, e8, no{}, plain, integral_constant<int, 512>{}, integral_constant<int, kHalf>{});
+    if (p.H <= 8192) return go(V, e8, no{}, plain, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+    go(V, integral_constant<int, 16>{}, no{}, plain, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
   };
   if constexpr (sizeof(T) == 2)
     if (v == 8) return shape(integral_constant<int, 8>{}), rc;
@@ -584,8 +668,9 @@ int norm_fwd(const T *r, const T *f, const T *gate, int gate_kind, const acc_t<T
   const int v = pack_width<T>(H, r, f, p.in[2], r2, u);
   if (!v) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
   const bool w16 = aligned16(a, w1, w2, p.b1, p.b2);
-  const int lrc = layer ? launch<T, false, true>(p, v, w16, (cudaStream_t)stream, who)
-                        : launch<T, false, false>(p, v, w16, (cudaStream_t)stream, who);
+  const bool bases = aligned16(r, f, p.in[2], r2, u);
+  const int lrc = layer ? launch<T, false, true>(p, v, w16, bases, (cudaStream_t)stream, who)
+                        : launch<T, false, false>(p, v, w16, bases, (cudaStream_t)stream, who);
   return lrc ? lrc : launch_status(who);
 }
 
@@ -619,7 +704,9 @@ int norm_grad(const T *r2, const T *f, const T *gate, int gate_kind, const acc_t
   if (!v) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
   const cudaStream_t st = (cudaStream_t)stream;
   const bool w16 = aligned16(a, w1, w2, p.b1);
-  const int lrc = layer ? launch<T, true, true>(p, v, w16, st, who) : launch<T, true, false>(p, v, w16, st, who);
+  const bool bases = aligned16(r2, f, p.in[4], dr2, du, dr, df, full ? dgate : nullptr);
+  const int lrc = layer ? launch<T, true, true>(p, v, w16, bases, st, who)
+                        : launch<T, true, false>(p, v, w16, bases, st, who);
   if (lrc) return lrc;
   norm_finish_kernel<acc_t<T>><<<dim3((H + 31) / 32, layer ? kNormVectors : 3), 1024, 0, st>>>(
       p.part, grad_blocks(H), H, da, dw1, dw2, db1, db2);

@@ -48,7 +48,7 @@ def forward(d, kind):
 
 
 SHAPES = [(1, 1), (1, 240), (3, 7), (5, 256), (4, 257), (33, 1003), (40, 1600), (9, 2048), (2, 4099), (3, 8192), (2, 9000),
-          (2, 16384), (0, 64), (700, 36)]
+          (2, 16384), (0, 64), (700, 36), (2003, 259), (1500, 1003), (1301, 512), (999, 2041), (1300, 1530)]
 
 
 @pytest.mark.parametrize("dtype", ROWS, ids=IDS)
