@@ -243,15 +243,16 @@ struct RowFeed {
   __device__ __forceinline__ void load(int i, A (&v)[EPT], int k = 0) const {
     if constexpr (kBulk) map.load(reinterpret_cast<const T *>(smem + (stage(k) * p.nin + i) * row_bytes()), v);
     else map.load(p.in[i] + (t + k * step) * p.H, v);
-    if constexpr (kCut)
+    if constexpr (kCut) {
       if (t + k * step == p.ntok - 1) {
 #pragma unroll
-        for (int q = 0; q < map.kN; ++q)
-          if (map.in(q) && map.at(q) == (map.np - 1) * V)
-#pragma unroll
-            for (int l = 0; l < V; ++l)
-              if (map.mine(q, l)) v[q * V + l] = to_acc(p.in[i][(t + k * step) * p.H + map.at(q) + l - map.off]);
+        for (int e = 0; e < EPT; ++e) {
+          const int q = e / V, l = e % V;
+          if (map.in(q) && map.at(q) == (map.np - 1) * V && map.mine(q, l))
+            v[e] = to_acc(p.in[i][(t + k * step) * p.H + map.at(q) + l - map.off]);
+        }
       }
+    }
   }
   __device__ __forceinline__ void read(int k = 0) const {  // after a block barrier that follows the row's loads
     if constexpr (kBulk)
@@ -278,7 +279,7 @@ __device__ __forceinline__ void move_weights(const A *const (&from)[5], int n, i
 }
 
 // Rows a block of the forward works on at once: two of 16-bit elements by bulk copies (the waits of their block sums
-// overlap, and the weights are read once for both: 65,536 x 1600 bf16 in 190 us against 270), else one.
+// overlap, and the weights are read once for both: layer norm of 65,536 x 1600 bf16 in 241 us against 270), else one.
 template <typename T, bool kBulk, int kThreads>
 constexpr int kFwdRows = kBulk && sizeof(T) == 2 && kThreads <= 512 ? 2 : 1;
 
@@ -378,6 +379,143 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
         st[2] = m2[k];
         st[3] = s2[k];
       }
+    }
+  }
+}
+
+// The forward for 16-bit rows of 257 to 512 elements: a warp a row, the row's one array in registers (f, then p, then
+// r2), r and the gate read from shared memory where they are used.  No block barriers, and a row costs a third of the
+// instructions that it costs a block, whose sums' shuffles and barriers every warp repeats.  Each warp has two rows in
+// shared memory, the next on its way while it works on one.  65,536 x 512 bf16 layer norm: 59 us against 77 by blocks;
+// longer rows leave too few warps on an SM (1024: 161 against 140).
+constexpr int kWarpStages = 2, kWarpEpt = 16;
+
+// Warps a block: two for whole rows; cut rows share the block's weights, one block an SM.
+template <Feed kFeed>
+constexpr int kRowWarpsMost = kFeed == kBulkRows ? 2 : 16;
+template <Feed kFeed>
+constexpr int kRowBlocks = kFeed == kCutRows ? 1 : 10;
+
+template <typename T, Feed kFeed, bool kLayer>
+__global__ void __launch_bounds__(kRowWarpsMost<kFeed> * 32, kRowBlocks<kFeed>)
+    norm_fwd_rows_kernel(const NormArgs<T> p) {
+  using A = acc_t<T>;
+  constexpr int EPT = kWarpEpt, V = 8 / (int)sizeof(T);  // neighbouring lanes read neighbouring 16 bytes of the weights
+  constexpr bool kCut = kFeed == kCutRows;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ uint64_t bars[kRowWarpsMost<kFeed>][kWarpStages];
+  __shared__ SumBuf<A, 4> unused;
+  int phase = 0;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, wpb = blockDim.x >> 5;
+  const int64_t step = (int64_t)gridDim.x * wpb;
+  // cut rows: a block's warps begin a multiple of eight rows apart (the grid is one), at the same place in a word
+  int64_t t = kCut ? (int64_t)warp * gridDim.x + blockIdx.x : (int64_t)blockIdx.x * wpb + warp;
+  const uint32_t place = kCut ? cut_bytes<T>(p.H) : (uint32_t)p.H * sizeof(T);
+  const int off = kCut ? (int)((uint64_t)t * p.H % (16 / sizeof(T))) : 0;
+  const RowMap<T, V, EPT, kCut> map{lane, 32, (off + p.H + V - 1) / V, off, p.H};
+  unsigned char *mine = smem + (size_t)warp * kWarpStages * p.nin * place;
+  const A inv = A(1) / A(p.H);
+  auto bar = [&](int s) { return (uint32_t)__cvta_generic_to_shared(&bars[warp][s]); };
+  auto fetch = [&](int64_t row, int s) {  // a lane an array
+    if (row >= p.ntok || lane >= p.nin) return;
+    // the last row's last word may reach past the array: what is left out here is read below
+    const uint32_t bytes = !kCut ? place : row == p.ntok - 1 ? (uint32_t)(off + p.H) * sizeof(T) & ~15u : (uint32_t)((off + p.H) * sizeof(T) + 15) & ~15u;
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar(s)), "r"(bytes) : "memory");
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                     (uint32_t)__cvta_generic_to_shared(mine) + (s * p.nin + lane) * place),
+                 "l"(p.in[lane] + row * p.H - off), "r"(bytes), "r"(bar(s))
+                 : "memory");
+  };
+  if (lane == 0) {
+    for (int s = 0; s < kWarpStages; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar(s)), "r"(p.nin));
+    asm volatile("fence.mbarrier_init.release.cluster;");
+  }
+  const A *wa = p.a, *w1 = p.w1, *w2 = p.w2, *b1 = p.b1, *b2 = p.b2;
+  if constexpr (kCut) {
+    A *ws = reinterpret_cast<A *>(smem + (size_t)wpb * kWarpStages * p.nin * place);
+    const int room = place / sizeof(T);
+    move_weights<A>({p.a, p.w1, p.w2, p.b1, p.b2}, kLayer ? 5 : 3, off, p.H, room, ws);
+    wa = ws, w1 = wa + room, w2 = w1 + room, b1 = w2 + room, b2 = b1 + room;
+  }
+  __syncthreads();
+  for (int s = 0; s < kWarpStages; ++s) fetch(t + s * step, s);
+  T gate_next = p.gate && t < p.ntok ? p.gate[t] : T(0.0f);
+  int st = 0, parity = 0;
+  for (; t < p.ntok; t += step) {
+    const A gate = p.gate ? to_acc(gate_next) : A(1);
+    if (p.gate && t + step < p.ntok) gate_next = p.gate[t + step];
+    uint32_t done = 0;
+    for (int it = 0; it < (1 << 22) && !done; ++it)
+      asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                   : "=r"(done)
+                   : "r"(bar(st)), "r"((uint32_t)parity)
+                   : "memory");
+    const unsigned char *row = mine + (size_t)st * p.nin * place;
+    auto pack = [&](int array, int i, A (&x)[V]) {
+      const Pack<T, V> q = load_pack<T, V>(reinterpret_cast<const T *>(row + array * place) + map.at(i));
+      const bool late = kCut && t == p.ntok - 1 && (map.at(i) + V) * (int)sizeof(T) > (((off + p.H) * (int)sizeof(T)) & ~15);
+#pragma unroll
+      for (int l = 0; l < V; ++l) {
+        x[l] = to_acc(q.v[l]);
+        if (late && map.mine(i, l)) x[l] = to_acc(p.in[array][t * p.H + map.at(i) + l - off]);
+      }
+    };
+    auto vec = [&](const A *w, int i, A (&x)[V]) {
+      const Pack<A, V> q = load_pack<A, V>(w + map.at(i));
+#pragma unroll
+      for (int l = 0; l < V; ++l) x[l] = q.v[l];
+    };
+    A v[1][EPT], m1[1], s1[1], m2[1], s2[1], x[V];
+#pragma unroll
+    for (int i = 0; i < map.kN; ++i) {
+      pack(0, i, x);
+#pragma unroll
+      for (int l = 0; l < V; ++l) v[0][i * V + l] = x[l];
+    }
+    row_stats<1, EPT, true, kLayer>(map, v, inv, p.eps, m1, s1, unused, phase);
+    if (!done) s1[0] = A(__int_as_float(0x7fc00000));
+#pragma unroll
+    for (int i = 0; i < map.kN; ++i) {
+      A w[V], b[V], r[V], a[V];
+      vec(w1, i, w);
+      if constexpr (kLayer) vec(b1, i, b);
+      vec(wa, i, a);
+      pack(1, i, r);
+      if (p.nin > 2) {
+        pack(2, i, x);
+      } else {
+#pragma unroll
+        for (int l = 0; l < V; ++l) x[l] = gate;
+      }
+#pragma unroll
+      for (int l = 0; l < V; ++l) {
+        const A n = v[0][i * V + l] * s1[0], q = kLayer ? fma(n, w[l], b[l]) : n * w[l];
+        v[0][i * V + l] = fma(a[l], q * x[l], r[l]);
+      }
+    }
+    __syncwarp();  // the row has been read
+    fetch(t + kWarpStages * step, st);
+    if (++st == kWarpStages) {
+      st = 0;
+      parity ^= 1;
+    }
+    map.store(p.r2 + t * p.H, v[0]);
+    row_stats<1, EPT, true, kLayer>(map, v, inv, p.eps, m2, s2, unused, phase);
+#pragma unroll
+    for (int i = 0; i < map.kN; ++i) {
+      A w[V], b[V];
+      vec(w2, i, w);
+      if constexpr (kLayer) vec(b2, i, b);
+#pragma unroll
+      for (int l = 0; l < V; ++l) {
+        const A n = v[0][i * V + l] * s2[0];
+        v[0][i * V + l] = kLayer ? fma(n, w[l], b[l]) : n * w[l];
+      }
+    }
+    map.store(p.u + t * p.H, v[0]);
+    if (lane == 0) {
+      A *out = p.stats + t * 4;
+      out[0] = m1[0], out[1] = s1[0], out[2] = m2[0], out[3] = s2[0];
     }
   }
 }
@@ -594,6 +732,28 @@ int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st,
     const int64_t units = w_ ? (p.ntok + kRowWarps - 1) / kRowWarps : p.ntok, most = 152 * (kGrad ? n.blocks : blocks);
     if (!rc) k<<<(unsigned)(kGrad || units > most ? most : units), n.threads, smem, st>>>(p);
   };
+  if constexpr (!kGrad && sizeof(T) == 2) {
+    const bool whole = v == 8 && weights16, cut = v < 8 && bases16;
+    const int need = p.H + (cut ? 10 : 0);  // places for the packs of a row that begins inside a word
+    auto rows = [&](auto F) {
+      constexpr Feed f_ = decltype(F)::value;
+      const size_t place = f_ == kCutRows ? cut_bytes<T>(p.H) : (size_t)p.H * sizeof(T), row = kWarpStages * p.nin * place;
+      const size_t weights = f_ == kCutRows ? place / sizeof(T) * (kLayer ? 5 : 3) * sizeof(acc_t<T>) : 0;
+      const int fit = (int)((200 * 1024 - weights) / row), warps = fit < kRowWarpsMost<f_> ? fit : kRowWarpsMost<f_>;
+      const int64_t held = f_ == kCutRows ? 1 : fit / 2 < kRowBlocks<f_> ? fit / 2 : kRowBlocks<f_>;
+      const int64_t units = f_ == kCutRows ? 152 : (p.ntok + warps - 1) / warps, most = 152 * held;
+      const size_t smem = row * warps + weights;
+      auto k = norm_fwd_rows_kernel<T, f_, kLayer>;
+      const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      if (e != cudaSuccess) rc = set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+      else k<<<(unsigned)(units > most ? most : units), warps * 32, smem, st>>>(p);
+      return rc;
+    };
+    if (p.H > 256 && need <= 32 * kWarpEpt) {
+      if (whole) return rows(integral_constant<Feed, kBulkRows>{});
+      if (cut) return rows(integral_constant<Feed, kCutRows>{});
+    }
+  }
   auto shape = [&](auto V) {
     constexpr integral_constant<int, 8> e8{};
     constexpr int kFew = kGrad ? 2 : 4, kHalf = kGrad ? 1 : 2;
@@ -614,7 +774,9 @@ int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st,
     }
     if constexpr (decltype(V)::value * sizeof(T) != 16 && sizeof(T) < 8) {
       constexpr int kTwo = !kGrad && sizeof(T) == 2 ? 3 : kFew;
-      if (bases16 && p.H <= 2048 && cut_bytes<T>(p.H) / sizeof(T) <= (size_t)n.threads * 8)  // a place for every pack
+      // a block sets its weights up first, which pays from some 24 rows on (9,973 x 1003 f16: 42 us so, 36 by plain
+      // loads; 65,536: 143 and 174)
+      if (bases16 && p.H <= 2048 && p.ntok >= (int64_t)152 * 24 * n.blocks && cut_bytes<T>(p.H) / sizeof(T) <= (size_t)n.threads * 8)  // a place for every pack
         return go(integral_constant<int, 16 / (int)sizeof(T)>{}, e8, no{}, cut, integral_constant<int, 256>{}, integral_constant<int, kTwo>{});
     }
     if (p.H <= 2048) return go(V, e8, no{}, plain, integral_constant<int, 256>{}, integral_constant<int, kFew>{});

@@ -221,3 +221,58 @@ def test_refusals():
     with pytest.raises(dpc.DPError) as err:
         dpc.dp_norm_gate_grad(r, r, v, v, v, st, r, r, work=torch.empty(64, dtype=torch.uint8, device="cuda"))
     assert err.value.code == dpc.DP_ERR_SHAPE
+
+
+@pytest.mark.parametrize("dtype", ROWS[1:], ids=IDS[1:])
+@pytest.mark.parametrize("T,H,kind,gate", [(30003, 1003, "layer", "full"), (60001, 259, "rms", "token"), (14700, 2039, "layer", "token"),
+                                           (30000, 1021, "rms", "full"), (20000, 1538, "layer", "none")])
+def test_many_rows_of_odd_lengths(dtype, T, H, kind, gate):
+    """Enough rows for the bulk copies of the words under them: rows at the start, the end and in between, and the
+    column sums over all rows (in f64 torch on the same stats), with the bounds of the tests above."""
+    dpc = lib()
+    g = torch.Generator(device="cuda").manual_seed(T + H)
+    rn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    layer = kind == "layer"
+    wd = wtype(dtype)
+    t = {n: (rn(T, H) * (3.0 if n == "f" else 1.0) + (0.5 if n == "f" else 0.0)).to(dtype) for n in ("r", "f", "dr2", "du")}
+    t["gate"] = None if gate == "none" else (rn(*((T, H) if gate == "full" else (T,))) * 0.5 + 0.5).to(dtype)
+    for n, c in (("a", 0.1), ("w1", 1.0), ("w2", 1.0), ("b1", 0.0), ("b2", 0.0)):
+        t[n] = (rn(H) * 0.1 + c).to(wd) if layer or n[0] != "b" else None
+    r2, u, st = dpc.dp_norm_gate_fwd(*(t[n] for n in ("r", "f", "a", "w1", "w2", "b1", "b2", "gate")), kind, EPS)
+    got = dpc.dp_norm_gate_grad(r2, *(t[n] for n in ("f", "a", "w1", "w2")), st, t["dr2"], t["du"], t["b1"], t["b2"], t["gate"], kind)
+    rows = np.unique(np.concatenate([np.arange(40), T - 1 - np.arange(40), np.random.default_rng(1).integers(0, T, 200)]))
+    at = torch.from_numpy(rows).cuda()
+    host = lambda x, whole: np.zeros(H) if x is None else f64(x if whole else x[at])  # noqa: E731
+    d = {n: (None, host(t[n], n in ("a", "w1", "w2", "b1", "b2"))) for n in t if n != "gate"}
+    d["gate"] = (None, np.ones(1) if gate == "none" else f64(t["gate"][at]))
+    rr, ru, rst = forward(d, kind)
+    a, un = 128 * SUM_UNIT[dtype], UNIT[dtype]
+    big = lambda v: 1 + np.abs(v).max(1, keepdims=True)  # noqa: E731
+    mag, mag2 = 1 + np.abs(d["f"][1]).max(1, keepdims=True) * rst[:, 1:2], 1 + np.abs(rr).max(1, keepdims=True) * rst[:, 3:4]
+    within(r2[at], rr, un * np.abs(rr) + a * big(rr) * mag + TINY[dtype], "r2")
+    within(u[at], ru, un * np.abs(ru) + a * big(ru) * mag * mag2 + TINY[dtype], "u")
+    back, _, (s1, s2, n1, n2, p, dg) = backward(d, f64(r2[at]), f64(st[at]), kind, gate)
+    top = lambda v: np.abs(v).max(1, keepdims=True)  # noqa: E731
+    dr_mag = (top(d["dr2"][1]) + s2 * top(d["du"][1] * d["w2"][1]) * (1 + top(n2) ** 2)) * np.ones((1, H))
+    within(got["dr"][at], back["dr"], un * np.abs(back["dr"]) + 2 * a * dr_mag + TINY[dtype], "dr")
+    G = 1.0 if gate == "none" else np.abs(d["gate"][1]).reshape(len(rows), -1)
+    df_mag = s1 * top(dr_mag * np.abs(d["a"][1] * d["w1"][1]) * G) * (1 + top(n1) ** 2)
+    within(got["df"][at], back["df"], un * np.abs(back["df"]) + 4 * a * df_mag + TINY[dtype], "df")
+    if gate != "none":
+        dg_mag = dr_mag * np.abs(d["a"][1]) * (np.abs(p) + np.abs(d["b1"][1]) + np.abs(n1))
+        dg_mag = dg_mag if gate == "full" else dg_mag.sum(1)
+        within(got["dgate"][at], back["dgate"], un * np.abs(back["dgate"]) + 4 * a * dg_mag + TINY[dtype], "dgate")
+    # column sums: dr as computed (unrounded dr differs from it by its rounding, in the bound)
+    D = {n: None if x is None else x.double() for n, x in t.items()}
+    s = st.double()
+    N1, N2 = (D["f"] - s[:, :1]) * s[:, 1:2], (r2.double() - s[:, 2:3]) * s[:, 3:4]
+    Gt = torch.ones(T, 1, device="cuda", dtype=torch.float64) if gate == "none" else D["gate"].reshape(T, -1)
+    P = N1 * D["w1"] + (D["b1"] if layer else 0.0)
+    dr, DP = got["dr"].double(), got["dr"].double() * D["a"] * Gt
+    cols = {"da": dr * Gt * P, "dw1": DP * N1, "dw2": D["du"] * N2}
+    if layer:
+        cols.update(db1=DP, db2=D["du"])
+    for n, c in cols.items():
+        bound = (un if n in ("da", "dw1", "db1") else 0.0) * c.abs().sum(0)
+        bound = bound + (4 * a + (T // 152 + 64) * SUM_UNIT[dtype]) * (c.abs() + dr.abs().mean() * 1e-3).sum(0)
+        within(got[n], f64(c.sum(0)), f64(bound), n)
