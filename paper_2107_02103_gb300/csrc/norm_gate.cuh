@@ -10,6 +10,8 @@
 //   da = sum_t dr G p, dw1 = sum_t dp f^, db1 = sum_t dp, dw2 = sum_t du r2^, db2 = sum_t du
 // A row lives in the registers of one warp (H <= 256) or one block, so each array is moved once; the layer
 // norm's variance is taken around the mean in a second sweep of the registers.
+#pragma once
+
 #include "rows.cuh"
 
 namespace dpc {
@@ -685,7 +687,7 @@ constexpr int kRowWarps = 4;  // rows (warps) per block where a warp holds a row
 struct NormShape {
   int ept, threads, blocks;  // elements a thread, threads a block, blocks an SM
 };
-NormShape norm_shape(int H, bool grad) {
+inline NormShape norm_shape(int H, bool grad) {
   if (H <= 256) return {8, kRowWarps * 32, grad ? 3 : 8};
   const int ept = H <= 8192 ? 8 : 16, threads = (H + ept * 32 - 1) / (ept * 32) * 32;
   const int blocks = (grad ? 512 : 1024) / threads;
@@ -693,8 +695,8 @@ NormShape norm_shape(int H, bool grad) {
 }
 
 // Rows whose bytes and addresses are multiples of 16 come by bulk copies, as many rows ahead as fit; so do rows of other
-// lengths up to 2048 in arrays that begin at a multiple of 16 (cut rows); the rest by plain loads of the widest pack they
-// allow.
+// lengths up to 2048 in arrays that begin at a multiple of 16 (cut rows); the rest by plain loads, element by
+// element unless their packs are whole.
 template <typename T, bool kGrad, bool kLayer>
 int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st, const char *who) {
   using std::integral_constant;
@@ -784,12 +786,10 @@ int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st,
     if (p.H <= 8192) return go(V, e8, no{}, plain, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
     go(V, integral_constant<int, 16>{}, no{}, plain, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
   };
-  if constexpr (sizeof(T) == 2)
-    if (v == 8) return shape(integral_constant<int, 8>{}), rc;
-  if constexpr (sizeof(T) <= 4)
-    if (v == 4) return shape(integral_constant<int, 4>{}), rc;
-  if (v == 2) return shape(integral_constant<int, 2>{}), rc;
-  return shape(integral_constant<int, 1>{}), rc;
+  constexpr int kFull = 16 / (int)sizeof(T);
+  if (v == kFull) shape(integral_constant<int, kFull>{});
+  else shape(integral_constant<int, 1>{});
+  return rc;
 }
 
 template <typename... P>
@@ -797,7 +797,7 @@ bool aligned16(P... ptrs) {
   return (((uintptr_t)ptrs | ...) & 15) == 0;
 }
 
-int norm_check(int64_t ntok, int H, int kind, int gate_kind, const char *who) {
+inline int norm_check(int64_t ntok, int H, int kind, int gate_kind, const char *who) {
   if (ntok < 0 || ntok > 0x7fffffffLL) return set_error(DP_ERR_SHAPE, "%s: ntok = %lld", who, (long long)ntok);
   if (H < 1) return set_error(DP_ERR_SHAPE, "%s: row length %d", who, H);
   if (H > kNormMaxH) return set_error(DP_ERR_UNSUPPORTED, "%s: row length %d > %d", who, H, kNormMaxH);
@@ -807,102 +807,6 @@ int norm_check(int64_t ntok, int H, int kind, int gate_kind, const char *who) {
   return DP_OK;
 }
 
-template <typename T>
-int norm_fwd(const T *r, const T *f, const T *gate, int gate_kind, const acc_t<T> *a, const acc_t<T> *w1,
-             const acc_t<T> *b1, const acc_t<T> *w2, const acc_t<T> *b2, int64_t ntok, int H, int kind, double eps,
-             T *r2, T *u, acc_t<T> *stats, void *stream, const char *who) {
-  clear_error();
-  const int rc = norm_check(ntok, H, kind, gate_kind, who);
-  if (rc) return rc;
-  if (!(eps > 0.0) || !std::isfinite(eps) || !((acc_t<T>)eps > acc_t<T>(0)))
-    return set_error(DP_ERR_SHAPE, "%s: eps = %g must be positive", who, eps);
-  if (ntok == 0) return DP_OK;
-  if (!r || !f || !a || !w1 || !w2 || !r2 || !u || !stats || (gate_kind != DP_GATE_NONE && !gate) ||
-      (kind == DP_NORM_LAYER && (!b1 || !b2)))
-    return set_error(DP_ERR_NULL, "%s: NULL array", who);
-  const bool layer = kind == DP_NORM_LAYER, full = gate_kind == DP_GATE_FULL;
-  NormArgs<T> p{};
-  p.in[0] = f, p.in[1] = r, p.in[2] = full ? gate : nullptr, p.nin = full ? 3 : 2;
-  p.gate = gate_kind == DP_GATE_TOKEN ? gate : nullptr;
-  p.a = a, p.w1 = w1, p.w2 = w2, p.b1 = layer ? b1 : nullptr, p.b2 = layer ? b2 : nullptr;
-  p.ntok = ntok, p.H = H, p.eps = (acc_t<T>)eps;
-  p.r2 = r2, p.u = u, p.stats = stats;
-  const int v = pack_width<T>(H, r, f, p.in[2], r2, u);
-  if (!v) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
-  const bool w16 = aligned16(a, w1, w2, p.b1, p.b2);
-  const bool bases = aligned16(r, f, p.in[2], r2, u);
-  const int lrc = layer ? launch<T, false, true>(p, v, w16, bases, (cudaStream_t)stream, who)
-                        : launch<T, false, false>(p, v, w16, bases, (cudaStream_t)stream, who);
-  return lrc ? lrc : launch_status(who);
-}
-
-int grad_blocks(int H) { return 152 * norm_shape(H, true).blocks; }
-
-template <typename T>
-int norm_grad(const T *r2, const T *f, const T *gate, int gate_kind, const acc_t<T> *a, const acc_t<T> *w1,
-              const acc_t<T> *b1, const acc_t<T> *w2, const acc_t<T> *stats, const T *dr2, const T *du, int64_t ntok,
-              int H, int kind, T *dr, T *df, T *dgate, acc_t<T> *da, acc_t<T> *dw1, acc_t<T> *dw2, acc_t<T> *db1,
-              acc_t<T> *db2, void *work, size_t work_bytes, void *stream, const char *who) {
-  clear_error();
-  const int rc = norm_check(ntok, H, kind, gate_kind, who);
-  if (rc) return rc;
-  const bool layer = kind == DP_NORM_LAYER;
-  if (!da || !dw1 || !dw2 || !a || !w1 || !w2 || (layer && (!b1 || !db1 || !db2)) || !work ||
-      (ntok > 0 && (!r2 || !f || !stats || !dr2 || !du || !dr || !df)) ||
-      (ntok > 0 && gate_kind != DP_GATE_NONE && (!gate || !dgate)))
-    return set_error(DP_ERR_NULL, "%s: NULL array", who);
-  if (work_bytes < (size_t)grad_blocks(H) * kNormVectors * H * sizeof(acc_t<T>) || ((uintptr_t)work & 15))
-    return set_error(DP_ERR_SHAPE, "%s: work buffer of %zu bytes is too short or misaligned", who, work_bytes);
-  const bool full = gate_kind == DP_GATE_FULL;
-  NormArgs<T> p{};
-  p.in[0] = r2, p.in[1] = du, p.in[2] = dr2, p.in[3] = f, p.in[4] = full ? gate : nullptr, p.nin = full ? 5 : 4;
-  p.gate = gate_kind == DP_GATE_TOKEN ? gate : nullptr;
-  p.a = a, p.w1 = w1, p.w2 = w2, p.b1 = layer ? b1 : nullptr;
-  p.ntok = ntok, p.H = H;
-  p.stats = const_cast<acc_t<T> *>(stats), p.dr = dr, p.df = df;
-  p.dgate = gate_kind == DP_GATE_NONE ? nullptr : dgate;
-  p.part = (acc_t<T> *)work;
-  const int v = pack_width<T>(H, r2, f, p.in[4], dr2, du, dr, df, full ? dgate : nullptr);
-  if (!v) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
-  const cudaStream_t st = (cudaStream_t)stream;
-  const bool w16 = aligned16(a, w1, w2, p.b1);
-  const bool bases = aligned16(r2, f, p.in[4], dr2, du, dr, df, full ? dgate : nullptr);
-  const int lrc = layer ? launch<T, true, true>(p, v, w16, bases, st, who)
-                        : launch<T, true, false>(p, v, w16, bases, st, who);
-  if (lrc) return lrc;
-  norm_finish_kernel<acc_t<T>><<<dim3((H + 31) / 32, layer ? kNormVectors : 3), 1024, 0, st>>>(
-      p.part, grad_blocks(H), H, da, dw1, dw2, db1, db2);
-  return launch_status(who);
-}
 
 }  // namespace
 }  // namespace dpc
-
-extern "C" {
-
-size_t dp_norm_gate_work_bytes(int H, int elem_bytes) {
-  if (H < 1 || H > dpc::kNormMaxH || (elem_bytes != 2 && elem_bytes != 4 && elem_bytes != 8)) return 0;
-  return (size_t)dpc::grad_blocks(H) * dpc::kNormVectors * H * (elem_bytes == 8 ? 8 : 4);
-}
-
-#define DP_NORM(X, C, T, W)                                                                                            \
-  int dp_norm_gate_fwd_##X(const C *r, const C *f, const C *gate, int gate_kind, const W *a, const W *w1, const W *b1, \
-                           const W *w2, const W *b2, int64_t ntok, int H, int kind, double eps, C *r2, C *u, W *stats, \
-                           void *stream) {                                                                             \
-    return dpc::norm_fwd<T>((const T *)r, (const T *)f, (const T *)gate, gate_kind, a, w1, b1, w2, b2, ntok, H, kind,  \
-                            eps, (T *)r2, (T *)u, stats, stream, "dp_norm_gate_fwd_" #X);                              \
-  }                                                                                                                    \
-  int dp_norm_gate_grad_##X(const C *r2, const C *f, const C *gate, int gate_kind, const W *a, const W *w1,            \
-                            const W *b1, const W *w2, const W *stats, const C *dr2, const C *du, int64_t ntok, int H,  \
-                            int kind, C *dr, C *df, C *dgate, W *da, W *dw1, W *dw2, W *db1, W *db2, void *work,       \
-                            size_t work_bytes, void *stream) {                                                         \
-    return dpc::norm_grad<T>((const T *)r2, (const T *)f, (const T *)gate, gate_kind, a, w1, b1, w2, stats,            \
-                             (const T *)dr2, (const T *)du, ntok, H, kind, (T *)dr, (T *)df, (T *)dgate, da, dw1, dw2, \
-                             db1, db2, work, work_bytes, stream, "dp_norm_gate_grad_" #X);                             \
-  }
-DP_NORM(f64, double, double, double)
-DP_NORM(f32, float, float, float)
-DP_NORM(bf16, uint16_t, __nv_bfloat16, float)
-DP_NORM(f16, uint16_t, __half, float)
-
-}  // extern "C"
