@@ -677,11 +677,16 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
   return launch_status(who);
 }
 
-// Which kernel, by the rows an expert has on average.
+// Which kernel.  Measured (us, one net of 2048 -> 4096, bf16): 8 rows 13 few, 21 tiles of 64; 32 rows 27 and 21; 256
+// rows 22 by 64, 24 by 128; 512 rows 36 by 64, 25 by 128, 37 wide; 1024 rows 42 by 128, 38 wide; 4096 rows 125 by 128,
+// 93 wide.  Below 2^33 products the widening launch costs more than it saves (16,384 rows of 240 -> 240: 13 by 128, 21
+// wide).  Between 64 and 128 by their rounds over 152 SMs, one of 128 costing a fifth more.
 enum I8Form { kFew, kTiles64, kTiles128, kWideTiles };
-I8Form form_of(int64_t rows, int nexp) {
-  const int64_t each = rows / nexp;
-  return rows <= 16 ? kFew : each <= 64 ? kTiles64 : each <= 1024 ? kTiles128 : kWideTiles;
+I8Form form_of(int64_t rows, int K, int N, int nexp) {
+  if (rows <= 16) return kFew;
+  if (rows / nexp >= 512 && (double)rows * K * N >= 8589934592.0) return kWideTiles;
+  auto rounds = [&](int R) { return (((rows + R - 1) / R + nexp / 2) * ((N + i8::kTM - 1) / i8::kTM) + 151) / 152; };
+  return 6 * rounds(128) < 5 * rounds(64) ? kTiles128 : kTiles64;
 }
 
 template <typename T>
@@ -699,7 +704,7 @@ int linear(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t 
   if (rows == 0) return DP_OK;
   if (!xq || !sx || !wq || !sw || !y) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (((uintptr_t)xq | (uintptr_t)wq) & 15) return set_error(DP_ERR_SHAPE, "%s: xq or wq is not 16-byte aligned", who);
-  const I8Form form = form_of(rows, nexp);
+  const I8Form form = form_of(rows, K, N, nexp);
   if (form == kWideTiles) {
     if (!work) return set_error(DP_ERR_NULL, "%s: work is NULL", who);
     if (work_bytes < i8::image_bytes(K, N, nexp) || ((uintptr_t)work & 15))
@@ -741,7 +746,7 @@ int take_wait_timeouts_linear_i8(unsigned int *count) {
 extern "C" {
 
 size_t dp_linear_i8_work_bytes(int64_t rows, int K, int N, int nexp) {
-  if (rows < 0 || K < 1 || N < 1 || nexp < 1 || dpc::form_of(rows, nexp) != dpc::kWideTiles) return 0;
+  if (rows < 0 || K < 1 || N < 1 || nexp < 1 || dpc::form_of(rows, K, N, nexp) != dpc::kWideTiles) return 0;
   return dpc::i8::image_bytes(K, N, nexp);
 }
 

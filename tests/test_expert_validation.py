@@ -64,10 +64,10 @@ def test_linear_i8(dpc):
         assert lin(xq=odd) == lin(wq=odd) == dpc.DP_ERR_SHAPE
         assert lin(K=65552) == dpc.DP_ERR_UNSUPPORTED
         assert lin(rows=0, xq=None, wq=None, y=None) == dpc.DP_OK
-        need = lib.dp_linear_i8_work_bytes(10 ** 6, 32, 8, 2)
+        need = lib.dp_linear_i8_work_bytes(10 ** 8, 32, 8, 2)
         assert need > 0 and lib.dp_linear_i8_work_bytes(4, 32, 8, 2) == 0
-        assert lin(rows=10 ** 6, work=None, nbytes=need) == dpc.DP_ERR_NULL
-        assert lin(rows=10 ** 6, nbytes=need - 1) == lin(rows=10 ** 6, work=odd, nbytes=need) == dpc.DP_ERR_SHAPE
+        assert lin(rows=10 ** 8, work=None, nbytes=need) == dpc.DP_ERR_NULL
+        assert lin(rows=10 ** 8, nbytes=need - 1) == lin(rows=10 ** 8, work=odd, nbytes=need) == dpc.DP_ERR_SHAPE
 
 
 def test_norm_gate(dpc):

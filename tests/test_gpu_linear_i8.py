@@ -238,3 +238,42 @@ def test_refusals():
     with pytest.raises(dpc.DPError) as err:  # rows off a 16-byte boundary
         dpc.dp_linear_i8(offset_view(xq), sx, wq, sw)
     assert err.value.code == dpc.DP_ERR_SHAPE
+
+
+@pytest.mark.parametrize("dtype", ROWS, ids=IDS)
+@pytest.mark.parametrize("T,k,E,K,N,drop,act", [
+    (2100, 1, 1, 2064, 2100, 0.0, "tanh"), (6000, 1, 3, 1040, 1500, 0.1, None), (2500, 2, 4, 1600, 1111, 0.0, "tanh"),
+    (5000, 1, 2, 3088, 700, 0.5, None)])
+def test_many_rows(dtype, T, k, E, K, N, drop, act):
+    """Enough rows an expert for the wide tiles: one, two and three chunks of K, ragged tiles both ways, rows past the
+    kept ones."""
+    dpc = lib()
+    assert dpc.dp_linear_i8_work_bytes(T * k, K, N, E) > 0
+    r = np.random.default_rng(T + K)
+    start = None
+    if E > 1:
+        start = dpc.dp_route_plan(torch.from_numpy(experts(T, T, k, E, drop)).cuda(), E)[0].cpu().numpy()
+    xq, wq = (r.integers(-128, 128, s).astype(np.int8) for s in ((T * k, K), (E, N, K)))
+    sx, sw = r.random(T * k).astype(np.float32), r.random((E, N)).astype(np.float32) / (64 * K)
+    if start is not None:
+        sx[start[-1]:] = np.nan
+    check(dpc, xq, sx, wq, sw, r.normal(0, 0.1, (E, N)).astype(np.float32), start, act, dtype)
+
+
+@pytest.mark.parametrize("K", [8192, 65536])
+def test_sums_of_many_rows_are_exact_at_their_largest(K):
+    dpc = lib()
+    rows, N = 8400, 140 if K == 8192 else 32
+    xq, wq = np.full((rows, K), -128, np.int8), np.full((1, N, K), -128, np.int8)
+    xq[1::3], wq[0, 1::3] = 127, 127
+    xq[2::3, ::2], wq[0, 2::3, 1::2] = 127, 127
+    xq[5, 5] = 1
+    wq[0, 3] = 0
+    wq[0, 3, K - 1] = 1
+    assert dpc.dp_linear_i8_work_bytes(rows, K, N, 1) > 0
+    one = torch.ones(rows, device="cuda"), torch.ones(1, N, device="cuda")
+    y = dpc.dp_linear_i8(torch.from_numpy(xq).cuda(), one[0], torch.from_numpy(wq).cuda(), one[1])
+    exact = (xq.astype(np.float64) @ wq[0].astype(np.float64).T).astype(np.float32)  # sums below 2^53
+    assert np.array_equal(y.cpu().numpy(), exact)
+    again = dpc.dp_linear_i8(torch.from_numpy(xq).cuda(), one[0], torch.from_numpy(wq).cuda(), one[1])
+    assert torch.equal(y, again) and dpc.dp_tc_wait_timeouts() == 0
