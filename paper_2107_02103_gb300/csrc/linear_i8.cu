@@ -442,16 +442,10 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
     };
     next_tile();
     uint4 raw[kU];
-    auto load = [&] {  // the stage where the loads stand, 0 columns past the last tile
-      const int c = now;
-      if (!now) return c;
-      const uint32_t m = k < p.K ? rows : 0u;
-#pragma unroll
-      for (int i = 0; i < kU; ++i) {
-        raw[i] = make_uint4(0, 0, 0, 0);
-        if (m >> i & 1) raw[i] = __ldg(reinterpret_cast<const uint4 *>((i < kA ? w : x) + (int64_t)step * (i < kA ? i : i - kA)));
-      }
-      return c;
+    uint32_t wanted = 0;  // this thread's rows of the stage where the loads stand
+    auto load = [&](int i) {
+      raw[i] = make_uint4(0, 0, 0, 0);
+      if (wanted >> i & 1) raw[i] = __ldg(reinterpret_cast<const uint4 *>((i < kA ? w : x) + (int64_t)step * (i < kA ? i : i - kA)));
     };
     auto advance = [&] {  // one slice on
       if (!now) return;
@@ -466,28 +460,36 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
     int st = lw % S::kGroups, phase = 1;  // the stage, and the parity of its "empty" barrier (the first round passes)
     for (int g = 0; g < st; ++g) advance();
     static_assert(S::kGroups == 2 && S::kStages % S::kGroups == 0, "stages in turn");
-    for (int c = load(); c;) {
+    int c = now;
+    wanted = now && k < p.K ? rows : 0u;
+#pragma unroll
+    for (int i = 0; i < kU; ++i) load(i);
+    while (c) {
       ok = __all_sync(0xffffffffu, wait(smem_u32(empty + st), phase, stop));
       if (!ok) break;
       const uint32_t dst = put + st * S::kStageBytes;
+      const int cols = c;
+      advance();
+      advance();
+      c = now;
+      wanted = now && k < p.K ? rows : 0u;
 #pragma unroll
       for (int i = 0; i < kU; ++i) {
-        if (i >= kA && row + kLR * (i - kA) >= c) continue;
-        uint32_t h[8];
-        widen(raw[i].x, h[0], h[1]);
-        widen(raw[i].y, h[2], h[3]);
-        widen(raw[i].z, h[4], h[5]);
-        widen(raw[i].w, h[6], h[7]);
-        const uint32_t d = dst + (i < kA ? i * (kLR / 8) * kSBO : S::kStageA + (i - kA) * (kLR / 8) * kSBO);
-        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d + put0), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
-        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d + put1), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
+        if (i < kA || row + kLR * (i - kA) < cols) {
+          uint32_t h[8];
+          widen(raw[i].x, h[0], h[1]);
+          widen(raw[i].y, h[2], h[3]);
+          widen(raw[i].z, h[4], h[5]);
+          widen(raw[i].w, h[6], h[7]);
+          const uint32_t d = dst + (i < kA ? i * (kLR / 8) * kSBO : S::kStageA + (i - kA) * (kLR / 8) * kSBO);
+          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d + put0), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d + put1), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
+        }
+        load(i);  // the group's next stage, on its way during the fence and the next wait
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) arrive(smem_u32(full + st));
-      advance();
-      advance();
-      c = load();
       if ((st += S::kGroups) >= S::kStages) {
         st -= S::kStages;
         phase ^= 1;
