@@ -696,7 +696,7 @@ int linear(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t 
            int nexp, int N, const int64_t *start, int act, T *y, void *work, size_t work_bytes, void *stream,
            const char *who) {
   clear_error();
-  if (rows < 0 || rows > 0x7fffffffLL) return set_error(DP_ERR_SHAPE, "%s: rows = %lld", who, (long long)rows);
+  if (rows < 0 || rows > 0x7fffffffLL - 1024) return set_error(DP_ERR_SHAPE, "%s: rows = %lld", who, (long long)rows);
   if (K < 16 || K % 16) return set_error(DP_ERR_SHAPE, "%s: K = %d is not a positive multiple of 16", who, K);
   if (K > kMaxK) return set_error(DP_ERR_UNSUPPORTED, "%s: K = %d > %d", who, K, kMaxK);
   if (N < 1 || N > (1 << 18)) return set_error(DP_ERR_SHAPE, "%s: N = %d outside [1, 2^18]", who, N);
