@@ -273,11 +273,17 @@ struct RowFeed {
 constexpr int kMaxStages = 4;
 
 // Cut rows' weights into shared memory, beside the packs of a row that begins at `off`: vector i at out + i * room.
-template <typename A>
-__device__ __forceinline__ void move_weights(const A *const (&from)[5], int n, int off, int H, int room, A *out) {
-  for (int i = 0; i < n; ++i)
-    for (int c = threadIdx.x; c < room; c += blockDim.x)
-      out[i * room + c] = (unsigned)(c - off) < (unsigned)H ? __ldg(from[i] + c - off) : A(0);
+template <int N, typename A>
+__device__ __forceinline__ void move_weights(const A *const (&from)[5], int off, int H, int room, A *out) {
+#pragma unroll 2
+  for (int c = threadIdx.x; c < room; c += blockDim.x) {
+    const bool in = (unsigned)(c - off) < (unsigned)H;
+    A v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = in ? __ldg(from[i] + c - off) : A(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[i * room + c] = v[i];
+  }
 }
 
 // Rows a block of the forward works on at once: two of 16-bit elements by bulk copies (the waits of their block sums
@@ -308,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
   if constexpr (kCut) {
     A *ws = reinterpret_cast<A *>(smem + p.stages * p.nin * feed.row_bytes());
     const int room = cut_bytes<T>(p.H) / sizeof(T);
-    move_weights<A>({p.a, p.w1, p.w2, p.b1, p.b2}, kLayer ? 5 : 3, off, p.H, room, ws);
+    move_weights<kLayer ? 5 : 3, A>({p.a, p.w1, p.w2, p.b1, p.b2}, off, p.H, room, ws);
     wa = ws, w1 = ws + room, w2 = ws + 2 * room, b1 = ws + 3 * room, b2 = ws + 4 * room;
     __syncthreads();
   }
@@ -436,7 +442,7 @@ __global__ void __launch_bounds__(kRowWarpsMost<kFeed> * 32, kRowBlocks<kFeed>)
   if constexpr (kCut) {
     A *ws = reinterpret_cast<A *>(smem + (size_t)wpb * kWarpStages * p.nin * place);
     const int room = place / sizeof(T);
-    move_weights<A>({p.a, p.w1, p.w2, p.b1, p.b2}, kLayer ? 5 : 3, off, p.H, room, ws);
+    move_weights<kLayer ? 5 : 3, A>({p.a, p.w1, p.w2, p.b1, p.b2}, off, p.H, room, ws);
     wa = ws, w1 = wa + room, w2 = w1 + room, b1 = w2 + room, b2 = b1 + room;
   }
   __syncthreads();
@@ -548,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
   if constexpr (kCut) {
     A *ws = reinterpret_cast<A *>(smem + p.stages * p.nin * feed.row_bytes());
     const int room = cut_bytes<T>(p.H) / sizeof(T);
-    move_weights<A>({p.a, p.w1, p.w2, p.b1, nullptr}, kLayer ? 4 : 3, off, p.H, room, ws);
+    move_weights<kLayer ? 4 : 3, A>({p.a, p.w1, p.w2, p.b1, nullptr}, off, p.H, room, ws);
     wa = ws, w1 = ws + room, w2 = ws + 2 * room, b1 = ws + 3 * room;
     __syncthreads();
   }
@@ -776,9 +782,10 @@ int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st,
     }
     if constexpr (decltype(V)::value * sizeof(T) != 16 && sizeof(T) < 8) {
       constexpr int kTwo = !kGrad && sizeof(T) == 2 ? 3 : kFew;
-      // a block sets its weights up first, which pays from some 24 rows on (9,973 x 1003 f16: 42 us so, 36 by plain
-      // loads; 65,536: 143 and 174)
-      if (bases16 && p.H <= 2048 && p.ntok >= (int64_t)152 * 24 * n.blocks && cut_bytes<T>(p.H) / sizeof(T) <= (size_t)n.threads * 8)  // a place for every pack
+      // A block sets its weights up first, which pays from some 8 rows on, in the backward of 16-bit rows 20 (us, plain
+      // and cut, rows of 1003: backward f16 5,000 34, 44; 9,973 64, 67; 20,000 112, 102; f32 5,000 48, 43).
+      constexpr int kPays = kGrad && sizeof(T) == 2 ? 20 : 8;
+      if (bases16 && p.H <= 2048 && p.ntok >= (int64_t)152 * kPays * n.blocks && cut_bytes<T>(p.H) / sizeof(T) <= (size_t)n.threads * 8)  // a place for every pack
         return go(integral_constant<int, 16 / (int)sizeof(T)>{}, e8, no{}, cut, integral_constant<int, 256>{}, integral_constant<int, kTwo>{});
     }
     if (p.H <= 2048) return go(V, e8, no{}, plain, integral_constant<int, 256>{}, integral_constant<int, kFew>{});
