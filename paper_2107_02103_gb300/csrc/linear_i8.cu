@@ -182,14 +182,21 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_i8_few_kernel(const I8A
   }
   const int8_t *w = p.wq + ((int64_t)e * p.N + n) * p.K, *x = p.xq + (int64_t)r0 * p.K;
   int acc[kFewRows] = {};
-  for (int k = lane * 16; k < p.K; k += 512) {
-    const int4 a = __ldg(reinterpret_cast<const int4 *>(w + k));
+  constexpr int kStep = 4;  // 2 KB of the channel on its way at a time
+  for (int k0 = lane * 16; k0 < p.K; k0 += kStep * 512) {
+    int4 a[kStep];
 #pragma unroll
-    for (int i = 0; i < kFewRows; ++i)
-      if (i < nr) {
-        const int4 b = __ldg(reinterpret_cast<const int4 *>(x + (int64_t)i * p.K + k));
-        acc[i] = __dp4a(a.x, b.x, __dp4a(a.y, b.y, __dp4a(a.z, b.z, __dp4a(a.w, b.w, acc[i]))));
-      }
+    for (int u = 0; u < kStep; ++u)
+      a[u] = k0 + 512 * u < p.K ? __ldg(reinterpret_cast<const int4 *>(w + k0 + 512 * u)) : make_int4(0, 0, 0, 0);
+#pragma unroll
+    for (int u = 0; u < kStep; ++u)
+      if (k0 + 512 * u < p.K)
+#pragma unroll
+        for (int i = 0; i < kFewRows; ++i)
+          if (i < nr) {
+            const int4 b = __ldg(reinterpret_cast<const int4 *>(x + (int64_t)i * p.K + k0 + 512 * u));
+            acc[i] = __dp4a(a[u].x, b.x, __dp4a(a[u].y, b.y, __dp4a(a[u].z, b.z, __dp4a(a[u].w, b.w, acc[i]))));
+          }
   }
   int mine = 0;
 #pragma unroll

@@ -675,9 +675,16 @@ __global__ void __launch_bounds__(1024) norm_finish_kernel(const A *__restrict__
   A *out = outs[blockIdx.y];
   const int lane = threadIdx.x & 31, row = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   A v = A(0);
-  if (c < H)
-#pragma unroll 4
-    for (int k = row; k < blocks; k += 32) v += part[((int64_t)k * kNormVectors + blockIdx.y) * H + c];
+  for (int k0 = row; k0 < blocks; k0 += 32 * 10) {  // ten partials on their way at a time
+    A x[10];
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+      const int k = k0 + 32 * i;
+      x[i] = c < H && k < blocks ? __ldg(part + ((int64_t)k * kNormVectors + blockIdx.y) * H + c) : A(0);
+    }
+#pragma unroll
+    for (int i = 0; i < 10; ++i) v += x[i];
+  }
   s[row][lane] = v;
   __syncthreads();
   v = s[lane][row];  // a warp a column
