@@ -8,8 +8,11 @@
 //   t = du w2;   dr = dr2 + s2 (t - r2^ mean(t r2^) - mean t)            (mean t for the layer norm only)
 //   dp = dr a G; t1 = dp w1;  df = s1 (t1 - f^ mean(t1 f^) - mean t1);   dG = dr a p
 //   da = sum_t dr G p, dw1 = sum_t dp f^, db1 = sum_t dp, dw2 = sum_t du r2^, db2 = sum_t du
-// A row lives in the registers of one warp (H <= 256) or one block, so each array is moved once; the layer
+// A row lives in the registers of one warp (short rows) or one block, so each array is moved once; the layer
 // norm's variance is taken around the mean in a second sweep of the registers.
+// f32 is bound by memory: 24,576 x 2048 with a full gate 154 us forward (6.5 TB/s), 272 us backward (5.9 TB/s).  16-bit
+// rows, twice the elements a byte, are bound by instructions and the waits of a row's four block sums: layer norm of
+// 65,536 x 1600 bf16 241 us (4.4 TB/s) and 414 us (4.1 TB/s).
 #pragma once
 
 #include "rows.cuh"
