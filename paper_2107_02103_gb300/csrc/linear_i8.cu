@@ -49,6 +49,15 @@ __global__ void __launch_bounds__(G == 256 ? 256 : 128)
 #pragma unroll
     for (int l = 0; l < V; ++l) v[l] = Whole || c * V + l < K ? (float)to_acc(q.v[l]) : 0.0f;
   };
+  // where the first two pairs go, read beside the row
+  int place[2] = {-1, -1}, kept[2] = {0, 0};
+  if (pos && have)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (j < topk) {
+        place[j] = __ldg(pos + t * topk + j);
+        kept[j] = __ldg(src + t * topk + j);
+      }
   float keep[kQuantKeep][V], amax = 0.0f;
 #pragma unroll
   for (int i = 0; i < kQuantKeep; ++i) load(tid + i * kStep, keep[i]);
@@ -91,7 +100,7 @@ __global__ void __launch_bounds__(G == 256 ? 256 : 128)
     }
   };
   for (int j = 0; j < topk; ++j) {
-    const int64_t q = t * topk + j, p = pos ? __ldg(pos + q) : t;
+    const int64_t q = t * topk + j, p = !pos ? t : j == 0 ? place[0] : j == 1 ? place[1] : __ldg(pos + q);
     if (p >= 0 && p < n) {
 #pragma unroll
       for (int i = 0; i < kQuantKeep; ++i)
@@ -103,7 +112,7 @@ __global__ void __launch_bounds__(G == 256 ? 256 : 128)
       }
       if (tid == 0) sx[p] = s;
     }
-    if (pos && __ldg(src + q) < 0) {
+    if (pos && (j == 0 ? kept[0] : j == 1 ? kept[1] : __ldg(src + q)) < 0) {
       for (int c = tid; c < ldq / 16; c += kStep) reinterpret_cast<uint4 *>(xq + q * ldq)[c] = make_uint4(0, 0, 0, 0);
       if (tid == 0) sx[q] = 0.0f;
     }

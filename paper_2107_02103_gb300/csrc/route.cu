@@ -251,16 +251,21 @@ __global__ void __launch_bounds__(G > kGradThreads<V> ? G : kGradThreads<V>)
   const int64_t n = ntok * topk, q = (int64_t)blockIdx.x * kPairs + slot;
   A dot = A(0);
   if (q < n) {
+    const T *g = dy + q / topk * H;
+    Pack<T, V> gv[kP], zv[kP];
+    auto upstream = [&](int s) {
+#pragma unroll
+      for (int i = 0; i < kP; ++i)
+        if (s + i * G < np) gv[i] = load_pack<T, V>(g + (s + i * G) * V);
+    };
+    upstream(tid);  // on its way while the pair's place is read
     const int64_t p = __ldg(pos + q);
     if (p >= 0 && p < n) {
       const A wq = w ? __ldg(w + q) : A(1);
-      const T *g = dy + q / topk * H, *from = z + p * H;
+      const T *from = z + p * H;
       T *to = dz + p * H;
       for (int s = tid; s < np; s += kP * G) {
-        Pack<T, V> gv[kP], zv[kP];
-#pragma unroll
-        for (int i = 0; i < kP; ++i)
-          if (s + i * G < np) gv[i] = load_pack<T, V>(g + (s + i * G) * V);
+        if (s != tid) upstream(s);
         if (dw)
 #pragma unroll
           for (int i = 0; i < kP; ++i)
