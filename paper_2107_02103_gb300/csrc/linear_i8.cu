@@ -3,7 +3,7 @@
 //   amax_i = max_k |x_ik|, r_i = 127 / amax_i, q_ik = rint(x_ik r_i), sx_i = amax_i / 127        (f32 arithmetic)
 //   y_in = act(float(sum_k q_ik w_nk) sx_i sw_n + b_n)
 // The integer sum is exact.  Rows to 8 bits are bound by memory: 65,536 x 1600 f32 in 80 us (6.5 TB/s), to their sorted
-// places in 100.
+// places in 87.
 #include "rows.cuh"
 
 namespace dpc {

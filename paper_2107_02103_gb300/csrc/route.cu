@@ -8,7 +8,7 @@
 // No atomics on the data: every output row has one writer and every sum a fixed order, so results repeat
 // bit for bit.
 // All are bound by memory.  Measured (12,288 x 2 rows of 1600 bf16): plan 11 us (two launches), gather 19 us (6.3 TB/s),
-// combine 25 us (4.8 TB/s; 6.1 in f32, whose rows are longer), gradient 48 us; 16,384 x 2 x 1600 f32: 51, 51, 91 us.
+// combine 25 us (4.8 TB/s; 6.1 in f32, whose rows are longer), gradient 48 us; 16,384 x 2 x 1600 f32: 51, 51, 87 us.
 #include "rows.cuh"
 
 namespace dpc {
@@ -136,69 +136,58 @@ struct Unit {
   int64_t t;  // the token
   int c;      // the lane's first pack; further ones 32 apart
 };
-template <bool Flat>
+template <bool Flat, int kP = kPart>
 __device__ __forceinline__ Unit unit_of(int np) {
   if constexpr (Flat) {
     const int64_t base = (int64_t)blockIdx.x * kMoveThreads, t0 = base / np;
     const uint32_t off = (uint32_t)(base - t0 * np) + threadIdx.x, dt = off / (uint32_t)np;
     return {t0 + dt, (int)(off - dt * np)};
   } else {
-    return {(int64_t)blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5), (int)(blockIdx.y * 32 * kPart + (threadIdx.x & 31))};
+    return {(int64_t)blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5), (int)(blockIdx.y * 32 * kP + (threadIdx.x & 31))};
   }
 }
 
+// Accesses a lane has in flight of a row, V elements each: whole rows' packs, or single elements of other rows.  Reading
+// the two aligned words under every 16 bytes of such rows instead (us, words and elements): combine of 30,011 x 3 x 1003
+// f16 75, 48; gather of 20,000 x 2 x 701 bf16 19, 17, x 1003 f32 53, 43, but of 30,011 x 3 x 1003 f16 52, 60.
+template <int V>
+constexpr int kRowPart = V > 1 ? kPart : 8;
+
 // xs rows of token t from one read of x[t]; also clears the rows past the kept ones that carry t's pair numbers.
-// Rows that are not of whole packs: the aligned packs within each row written, read through load_any (from L1 after
-// the first), and the elements before and after them one by one.
-template <typename T, bool Whole, bool Flat>
+template <typename T, int V, bool Flat>
 __global__ void __launch_bounds__(kMoveThreads)
     gather_kernel(const T *__restrict__ x, const int32_t *__restrict__ src, const int32_t *__restrict__ pos,
                   int64_t ntok, int topk, int H, int np, T *__restrict__ xs) {
-  constexpr int V = 16 / (int)sizeof(T), kP = Flat ? 1 : kPart;
+  constexpr int kP = Flat ? 1 : kRowPart<V>;
   const int64_t n = ntok * topk;
-  const Unit u = unit_of<Flat>(np);
+  const Unit u = unit_of<Flat, kRowPart<V>>(np);
   if (u.t >= ntok) return;
   const T *row = x + u.t * H;
   Pack<T, V> v[kP];
-  if constexpr (Whole)
 #pragma unroll
-    for (int i = 0; i < kP; ++i)
-      if (u.c + 32 * i < np) v[i] = load_pack<T, V>(row + (u.c + 32 * i) * V);
-  auto write = [&](T *to, bool zero) {
-    int head = 0, full = np;
-    if constexpr (!Whole) {
-      head = min((int)((16 - ((uintptr_t)to & 15)) & 15) / (int)sizeof(T), H);
-      full = (H - head) / V;
-      if (u.c < H - full * V) {  // fewer elements at the ends than packs a unit may have
-        const int e = u.c < head ? u.c : u.c + full * V;
-        to[e] = zero ? T(0.0f) : row[e];
-      }
-      if (!zero)
-#pragma unroll
-        for (int i = 0; i < kP; ++i)
-          if (u.c + 32 * i < full) v[i] = load_any<T>(row + head + (u.c + 32 * i) * V, x, x + ntok * H);
-    }
-#pragma unroll
-    for (int i = 0; i < kP; ++i)
-      if (u.c + 32 * i < full) store_pack<T, V>(to + head + (u.c + 32 * i) * V, zero ? Pack<T, V>{} : v[i]);
-  };
+  for (int i = 0; i < kP; ++i)
+    if (u.c + 32 * i < np) v[i] = load_pack<T, V>(row + (u.c + 32 * i) * V);
   for (int j = 0; j < topk; ++j) {
     const int64_t q = u.t * topk + j, p = __ldg(pos + q);
-    if (p >= 0 && p < n) write(xs + p * H, false);
-    if (__ldg(src + q) < 0) write(xs + q * H, true);
+    if (p >= 0 && p < n)
+#pragma unroll
+      for (int i = 0; i < kP; ++i)
+        if (u.c + 32 * i < np) store_pack<T, V>(xs + p * H + (u.c + 32 * i) * V, v[i]);
+    if (__ldg(src + q) < 0)
+#pragma unroll
+      for (int i = 0; i < kP; ++i)
+        if (u.c + 32 * i < np) store_pack<T, V>(xs + q * H + (u.c + 32 * i) * V, Pack<T, V>{});
   }
 }
 
-// The sums; V elements an access: whole rows' packs, or 1 for other rows (reading the two words under each pack of
-// every row instead measured 75 us against 64 for 30,011 x 3 rows of 1003 f16).
 template <typename T, int V, bool Flat>
 __global__ void __launch_bounds__(kMoveThreads)
     combine_kernel(const T *__restrict__ z, const int32_t *__restrict__ pos, const acc_t<T> *__restrict__ w,
                    int64_t ntok, int topk, int H, int np, T *__restrict__ y) {
   using A = acc_t<T>;
-  constexpr int kP = Flat ? 1 : kPart;
+  constexpr int kP = Flat ? 1 : kRowPart<V>;
   const int64_t n = ntok * topk;
-  const Unit u = unit_of<Flat>(np);
+  const Unit u = unit_of<Flat, kRowPart<V>>(np);
   if (u.t >= ntok) return;
   A sum[kP][V] = {};
   for (int j = 0; j < topk; ++j) {
@@ -338,9 +327,9 @@ bool elements_aligned(const void *a, const void *b, const void *c = nullptr) {
   return (((uintptr_t)a | (uintptr_t)b | (uintptr_t)c) & (sizeof(T) - 1)) == 0;
 }
 // The grid of a move over rows of np packs; false where it is too large.
-bool move_grid(int64_t ntok, int np, bool flat, dim3 *grid) {
+bool move_grid(int64_t ntok, int np, bool flat, int part, dim3 *grid) {
   const int64_t x = flat ? (ntok * np + kMoveThreads - 1) / kMoveThreads : (ntok + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
-  const int64_t y = flat ? 1 : (np + 32 * kPart - 1) / (32 * kPart);
+  const int64_t y = flat ? 1 : (np + 32 * part - 1) / (32 * part);
   *grid = dim3((unsigned)x, (unsigned)y);
   return x <= 0x7fffffffLL && y <= 65535;
 }
@@ -355,12 +344,12 @@ int gather(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok, int
   if (!elements_aligned<T>(x, xs)) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
   constexpr int V = 16 / (int)sizeof(T);
   const bool whole = whole_rows<T>(H, x, xs);
-  const bool flat = H / V < 32;
-  const int np = whole || !flat ? (H + V - 1) / V : H / V + 2 * V;  // with places for the elements at a short row's ends
+  const int np = whole ? H / V : H;
   dim3 grid;
-  if (!move_grid(ntok, np, flat, &grid)) return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, H);
-  auto k = flat ? (whole ? gather_kernel<T, true, true> : gather_kernel<T, false, true>)
-                   : (whole ? gather_kernel<T, true, false> : gather_kernel<T, false, false>);
+  if (!move_grid(ntok, np, np < 32, whole ? kRowPart<V> : kRowPart<1>, &grid))
+    return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, H);
+  auto k = np < 32 ? (whole ? gather_kernel<T, V, true> : gather_kernel<T, 1, true>)
+                   : (whole ? gather_kernel<T, V, false> : gather_kernel<T, 1, false>);
   k<<<grid, kMoveThreads, 0, (cudaStream_t)stream>>>(x, src, pos, ntok, topk, H, np, xs);
   return launch_status(who);
 }
@@ -377,7 +366,8 @@ int combine(const T *z, const int32_t *pos, const acc_t<T> *w, int64_t ntok, int
   const bool whole = whole_rows<T>(H, z, y);
   const int np = whole ? H / V : H;
   dim3 grid;
-  if (!move_grid(ntok, np, np < 32, &grid)) return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, H);
+  if (!move_grid(ntok, np, np < 32, whole ? kRowPart<V> : kRowPart<1>, &grid))
+    return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, H);
   auto k = np < 32 ? (whole ? combine_kernel<T, V, true> : combine_kernel<T, 1, true>)
                    : (whole ? combine_kernel<T, V, false> : combine_kernel<T, 1, false>);
   k<<<grid, kMoveThreads, 0, (cudaStream_t)stream>>>(z, pos, w, ntok, topk, H, np, y);
