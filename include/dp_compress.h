@@ -378,7 +378,7 @@ const char *dp_profile_name(int i);
 
 /*
  * Diagnostic (not part of the paper's method): every wait of the tensor-core
- * GEMM kernels (dp_tabulate_fusion_*_tc_f64, dp_fitting_*_tc_f64) on an
+ * GEMM kernels (dp_tabulate_fusion_*_tc_f64, dp_fitting_*_tc_f64, dp_linear_i8_*) on an
  * mbarrier is bounded; a CTA whose wait gives up writes NaN outputs, reads
  * no accumulator and counts one timeout on the device.  This call waits for
  * the device to finish (cudaDeviceSynchronize), writes the count since the
