@@ -7,8 +7,10 @@
 //   backward dz[p] = w_q dy[t],  dw_q = <dy[t], z[p]>;  the gather's backward is combine without weights.
 // No atomics on the data: every output row has one writer and every sum a fixed order, so results repeat
 // bit for bit.
-// All are bound by memory.  Measured (12,288 x 2 rows of 1600 bf16): plan 11 us (two launches), gather 19 us (6.3 TB/s),
+// All are bound by memory.  Measured (12,288 x 2 rows of 1600 bf16): plan 8 us, gather 19 us (6.3 TB/s),
 // combine 25 us (4.8 TB/s; 6.1 in f32, whose rows are longer), gradient 48 us; 16,384 x 2 x 1600 f32: 51, 51, 87 us.
+#include <cooperative_groups.h>
+
 #include "rows.cuh"
 
 namespace dpc {
@@ -47,16 +49,18 @@ __global__ void __launch_bounds__(kPlanWarps * 32)
   for (int e = threadIdx.x; e < nexp; e += blockDim.x) counts[(int64_t)blockIdx.x * nexp + e] = cnt[e];
 }
 
-// Every block sums the count table (its own prefix and the totals), scans the experts, then gives its pairs their
+// Every block sums the blocks' counts (its own prefix and the totals), scans the experts, then gives its pairs their
 // places: a warp's pairs of an expert follow those of the warps before it, and lanes with the same expert are found
-// with a match, so that a warp moves each counter once per 32 pairs.  With one block (counts NULL) it counts by
-// itself: a single launch.
-template <int kPer>
+// with a match, so that a warp moves each counter once per 32 pairs.  One block counts by itself, up to eight form a
+// cluster and read one another's counts (a single launch either way), more read a table that a launch before filled.
+enum PlanCounts { kOwn, kCluster, kTable };
+template <int kPer, PlanCounts kFrom>
 __global__ void __launch_bounds__(kPlanWarps * 32)
     plan_place_kernel(const int32_t *__restrict__ expert, int64_t n, int nexp, const int *__restrict__ counts,
                       int64_t *__restrict__ start, int32_t *__restrict__ src, int32_t *__restrict__ pos) {
-  extern __shared__ int cnt[];  // [warps][nexp], then the scan's warp sums
-  int *sums = cnt + kPlanWarps * nexp;
+  extern __shared__ int cnt[];  // [warps][nexp], then the scan's warp sums, then the block's counts
+  int *sums = cnt + kPlanWarps * nexp, *block = sums + kPlanWarps;
+  namespace cg = cooperative_groups;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = threadIdx.x; i < kPlanWarps * nexp; i += blockDim.x) cnt[i] = 0;
   const PlanIds<kPer> ids(expert, n, nexp);
@@ -66,15 +70,26 @@ __global__ void __launch_bounds__(kPlanWarps * 32)
   for (int i = 0; i < kPer; ++i)
     if (ids.e[i] >= 0) atomicAdd(mine + ids.e[i], 1);
   __syncthreads();
+  if constexpr (kFrom == kCluster) {
+    for (int e = threadIdx.x; e < nexp; e += blockDim.x) {
+      int c = 0;
+#pragma unroll 8
+      for (int w = 0; w < kPlanWarps; ++w) c += cnt[w * nexp + e];
+      block[e] = c;
+    }
+    cg::this_cluster().sync();
+  }
   int carry = 0;
   for (int e0 = 0; e0 < nexp; e0 += kPlanWarps * 32) {  // an exclusive scan of the totals
     const int e = e0 + threadIdx.x;
     int total = 0, before = 0;
     if (e < nexp) {
-      if (counts) {
+      if constexpr (kFrom != kOwn) {
 #pragma unroll 8
         for (int b = 0; b < (int)gridDim.x; ++b) {
-          const int c = __ldg(counts + (int64_t)b * nexp + e);
+          int c;
+          if constexpr (kFrom == kTable) c = __ldg(counts + (int64_t)b * nexp + e);
+          else c = cg::this_cluster().map_shared_rank(block, b)[e];
           before += b < (int)blockIdx.x ? c : 0;
           total += c;
         }
@@ -109,6 +124,7 @@ __global__ void __launch_bounds__(kPlanWarps * 32)
   }
   const int kept = carry;
   if (blockIdx.x == 0 && threadIdx.x == 0) start[nexp] = kept;
+  if constexpr (kFrom == kCluster) cg::this_cluster().sync();  // nobody leaves while its counts are read
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int64_t q = ids.first + 32 * i;
@@ -306,14 +322,13 @@ int row_check(int64_t ntok, int topk, int H, const char *who) {
   return DP_OK;
 }
 
-// Blocks of the plan and pairs a thread: one block where its walk (0.3 us for each of a thread's pairs) costs less
-// than a second launch.
+// Blocks of the plan and pairs a thread (whose walk costs 0.3 us each): a cluster of up to eight blocks where that
+// holds the pairs, else two launches (24,576 pairs: 8 us in a cluster, 11 in two launches).
 struct PlanShape {
   int blocks, per;
 };
 PlanShape plan_shape(int64_t n) {
-  if (n <= 4096) return {1, 4};
-  if (n <= 8192) return {1, 8};
+  if (n <= 8 * 4096) return {(int)((n + 4095) / 4096 < 1 ? 1 : (n + 4095) / 4096), 4};
   if (n <= 304 * 4096) return {(int)((n + 4095) / 4096), 4};
   return {(int)((n + 8191) / 8192), 8};
 }
@@ -412,7 +427,7 @@ size_t dp_route_work_bytes(int64_t ntok, int topk, int nexp) {
   if (ntok < 0 || topk < 1 || topk > dpc::kMaxTopk || nexp < 1 || nexp > dpc::kMaxExperts || ntok > 0x7fffffffLL / topk)
     return 0;
   const dpc::PlanShape s = dpc::plan_shape(ntok * topk);
-  return s.blocks > 1 ? (size_t)s.blocks * nexp * sizeof(int) : 1;
+  return s.blocks > 8 ? (size_t)s.blocks * nexp * sizeof(int) : 1;
 }
 
 int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64_t *start, int32_t *src, int32_t *pos,
@@ -426,23 +441,43 @@ int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64
   if (nexp > kMaxExperts) return set_error(DP_ERR_UNSUPPORTED, "%s: nexp = %d > %d", who, nexp, kMaxExperts);
   if (!start || (ntok > 0 && (!expert || !src || !pos))) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   const PlanShape s = plan_shape(ntok * topk);
-  if (s.blocks > 1) {
+  if (s.blocks > 8) {
     if (!work) return set_error(DP_ERR_NULL, "%s: work is NULL", who);
     if (work_bytes < dp_route_work_bytes(ntok, topk, nexp) || ((uintptr_t)work & 15))
       return set_error(DP_ERR_SHAPE, "%s: work buffer of %zu bytes is too short or misaligned", who, work_bytes);
   }
-  const size_t smem = (size_t)(kPlanWarps * nexp + kPlanWarps) * sizeof(int);
+  const size_t smem = (size_t)(kPlanWarps * nexp + kPlanWarps + nexp) * sizeof(int);
   const cudaStream_t st = (cudaStream_t)stream;
   const int64_t n = ntok * topk;
-  int *counts = s.blocks > 1 ? (int *)work : nullptr;
-  auto place = s.per == 8 ? plan_place_kernel<8> : plan_place_kernel<4>;
+  int *counts = s.blocks > 8 ? (int *)work : nullptr;
+  auto place = s.blocks == 1  ? plan_place_kernel<4, kOwn>
+               : !counts      ? plan_place_kernel<4, kCluster>
+               : s.per == 4   ? plan_place_kernel<4, kTable>
+                              : plan_place_kernel<8, kTable>;
   if (smem > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(place, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
   }
-  auto count = s.per == 8 ? plan_count_kernel<8> : plan_count_kernel<4>;
-  if (counts) count<<<s.blocks, kPlanWarps * 32, nexp * sizeof(int), st>>>(expert, n, nexp, counts);
-  place<<<s.blocks, kPlanWarps * 32, smem, st>>>(expert, n, nexp, counts, start, src, pos);
+  if (counts) {
+    auto count = s.per == 8 ? plan_count_kernel<8> : plan_count_kernel<4>;
+    count<<<s.blocks, kPlanWarps * 32, nexp * sizeof(int), st>>>(expert, n, nexp, counts);
+  }
+  if (s.blocks == 1 || counts) {
+    place<<<s.blocks, kPlanWarps * 32, smem, st>>>(expert, n, nexp, counts, start, src, pos);
+  } else {
+    cudaLaunchAttribute cluster{};
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = s.blocks;
+    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(s.blocks);
+    cfg.blockDim = dim3(kPlanWarps * 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &cluster;
+    cfg.numAttrs = 1;
+    cudaLaunchKernelEx(&cfg, place, expert, n, nexp, (const int *)counts, start, src, pos);
+  }
   return launch_status(who);
 }
 

@@ -18,11 +18,11 @@ FAKE = ctypes.c_void_p(0x1000)
 
 def test_route(dpc):
     lib = dpc._lib
-    wb = dpc.dp_route_work_bytes(10000, 2, 8)
+    wb = dpc.dp_route_work_bytes(100000, 2, 8)
     assert wb >= 16 and lib.dp_route_work_bytes(4, 2, 8) == 1 and lib.dp_route_work_bytes(-1, 2, 8) == 0 and lib.dp_route_work_bytes(5, 65, 8) == 0
     assert lib.dp_route_work_bytes(2 ** 30, 2, 8) == 0 and lib.dp_route_work_bytes(5, 1, 1025) == 0
 
-    def plan(expert=FAKE, ntok=10000, topk=2, nexp=8, start=FAKE, src=FAKE, pos=FAKE, work=FAKE, nbytes=wb):
+    def plan(expert=FAKE, ntok=100000, topk=2, nexp=8, start=FAKE, src=FAKE, pos=FAKE, work=FAKE, nbytes=wb):
         return lib.dp_route_plan(expert, ntok, topk, nexp, start, src, pos, work, nbytes, None)
 
     assert plan(expert=None) == plan(start=None) == plan(src=None) == plan(pos=None) == plan(work=None) == dpc.DP_ERR_NULL

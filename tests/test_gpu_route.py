@@ -37,7 +37,7 @@ def plan(expert, E):
 
 @pytest.mark.parametrize("T,k,E,drop", [
     (0, 1, 3, 0.0), (1, 1, 1, 0.0), (1, 2, 8, 0.0), (33, 3, 5, 0.3), (511, 2, 1024, 0.1), (4096, 2, 8, 0.0),
-    (4097, 2, 8, 0.2), (9001, 1, 2, 1.0), (16384, 2, 9, 0.1), (16385, 2, 9, 0.1), (20011, 3, 61, 0.2), (70001, 8, 7, 0.05), (3000, 5, 1023, 0.2),
+    (4097, 2, 8, 0.2), (9001, 1, 2, 1.0), (16384, 2, 9, 0.1), (16385, 2, 9, 0.1), (4100, 1, 1024, 0.0), (14000, 2, 1000, 0.3), (32768, 1, 5, 0.0), (32769, 1, 5, 0.0), (20011, 3, 61, 0.2), (70001, 8, 7, 0.05), (3000, 5, 1023, 0.2),
     (700001, 1, 3, 0.1)])
 def test_plan(T, k, E, drop):
     dpc = lib()
