@@ -702,7 +702,7 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
   return launch_status(who);
 }
 
-// Which kernel.  Measured (us, one net of 2048 -> 4096, bf16): 8 rows 13 few, 21 tiles of 64; 32 rows 27 and 21; 256
+// Which kernel.  Measured (us, one net of 2048 -> 4096, bf16): 16 rows 17 few, 21 tiles of 64; 32 rows 27 and 21; 256
 // rows 22 by 64, 24 by 128; 512 rows 36 by 64, 25 by 128, 37 wide; 1024 rows 42 by 128, 38 wide; 4096 rows 125 by 128,
 // 93 wide.  Below 2^33 products the widening launch costs more than it saves (16,384 rows of 240 -> 240: 13 by 128, 21
 // wide).  Between 64 and 128 by their rounds over 152 SMs, one of 128 costing a fifth more.
