@@ -2,12 +2,13 @@
 
 Every function here has the name of a C entry point in include/dp_compress.h
 and only marshals arguments: it checks torch tensors (device, dtype,
-contiguity, shape), passes their data pointers and the current CUDA stream,
-and raises on a non-OK status.  All arithmetic runs in the CUDA kernels of
+contiguity, shape), passes their data pointers and their device's current
+CUDA stream, and raises on a non-OK status.  All arithmetic runs in the CUDA kernels of
 libdpcompress.so; there is no CPU fallback -- importing this package fails
 if the library has not been built (see build.py).
 
-Calls are asynchronous on torch.cuda.current_stream() like any CUDA op.
+Calls are asynchronous on torch.cuda.current_stream() of the tensors' device
+like any CUDA op.
 """
 from __future__ import annotations
 
@@ -187,8 +188,20 @@ def _check(rc: int):
         raise DPError(rc, dp_last_error())
 
 
-def _stream(t: torch.Tensor):
-    return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
+
+
+def _run(dev: int, fn, *args):
+    """fn(*args, stream) on device number dev and its current stream; raises on a non-OK status.  A launch goes to
+    the current device, so dev is made that for the call where it is another."""
+    if _current_device() == dev:
+        rc = fn(*args, _raw_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _raw_stream(dev))
+    if rc:
+        _check(rc)
 
 
 def _ptr(t):
@@ -250,8 +263,8 @@ def dp_embedding_net_nodes(params: torch.Tensor, widths, info: dp_table_info, ou
     if out is None:
         out = tuple(torch.empty(shape, dtype=torch.float64, device=params.device) for _ in range(3))
     y, dy, d2y = (_dev(o, "out", torch.float64, shape) for o in out)
-    _check(_lib.dp_embedding_net_nodes_f64(_ptr(params), w, len(widths) - 1, npair, ctypes.byref(info), _ptr(y),
-                                           _ptr(dy), _ptr(d2y), _stream(params)))
+    _run(params.get_device(), _lib.dp_embedding_net_nodes_f64, _ptr(params), w, len(widths) - 1, npair,
+         ctypes.byref(info), _ptr(y), _ptr(dy), _ptr(d2y))
     return y, dy, d2y
 
 
@@ -266,7 +279,7 @@ def dp_table_build(y, dy, d2y, info: dp_table_info, dtype=torch.float64, out=Non
     tdt = torch.float32 if dtype == DF64 else dtype
     table = torch.empty(shape, dtype=tdt, device=y.device) if out is None else _dev(out, "out", tdt, shape)
     fn = getattr(_lib, f"dp_table_build_{_suffix(dtype)}")
-    _check(fn(_ptr(y), _ptr(dy), _ptr(d2y), npair, M1, ctypes.byref(info), _ptr(table), _stream(y)))
+    _run(y.get_device(), fn, _ptr(y), _ptr(dy), _ptr(d2y), npair, M1, ctypes.byref(info), _ptr(table))
     return table
 
 
@@ -325,8 +338,8 @@ def _fwd(name, table, info, s, Rt, nvalid, atype, sel, out):
     shape = (nloc, 4, M1)
     T = torch.empty(shape, dtype=dtype, device=s.device) if out is None else _dev(out, "out", dtype, shape)
     fn = getattr(_lib, f"{name}_{_suffix(arith)}")
-    _check(fn(_ptr(table), ctypes.byref(info), _ptr(s), _ptr(Rt), _ptr(nvalid), _ptr(atype), nloc, nnei, ntypes,
-              selc, M1, _ptr(T), _stream(s)))
+    _run(s.get_device(), fn, _ptr(table), ctypes.byref(info), _ptr(s), _ptr(Rt), _ptr(nvalid), _ptr(atype), nloc, nnei,
+         ntypes, selc, M1, _ptr(T))
     return T
 
 
@@ -343,8 +356,8 @@ def dp_tabulate_fusion_fwd_descriptor(table, info: dp_table_info, s, Rt, nvalid,
         T = _dev(out[0], "T", dtype, (nloc, 4, M1))
         D = _dev(out[1], "D", dtype, (nloc, M1, int(M2)))
     fn = getattr(_lib, f"dp_tabulate_fusion_fwd_descriptor_{_suffix(dtype)}")
-    _check(fn(_ptr(table), ctypes.byref(info), _ptr(s), _ptr(Rt), _ptr(nvalid), _ptr(atype), nloc, nnei, ntypes,
-              selc, M1, int(M2), _ptr(T), _ptr(D), _stream(s)))
+    _run(s.get_device(), fn, _ptr(table), ctypes.byref(info), _ptr(s), _ptr(Rt), _ptr(nvalid), _ptr(atype), nloc, nnei,
+         ntypes, selc, M1, int(M2), _ptr(T), _ptr(D))
     return T, D
 
 
@@ -378,8 +391,8 @@ def _grad(name, table, info, s, Rt, nvalid, atype, sel, dT, out):
         ds = _dev(out[0], "ds", dtype, (nloc, nnei))
         dRt = _dev(out[1], "dRt", dtype, (nloc, nnei, 4))
     fn = getattr(_lib, f"{name}_{_suffix(arith)}")
-    _check(fn(_ptr(table), ctypes.byref(info), _ptr(s), _ptr(Rt), _ptr(nvalid), _ptr(atype), nloc, nnei, ntypes,
-              selc, M1, _ptr(dT), _ptr(ds), _ptr(dRt), _stream(s)))
+    _run(s.get_device(), fn, _ptr(table), ctypes.byref(info), _ptr(s), _ptr(Rt), _ptr(nvalid), _ptr(atype), nloc, nnei,
+         ntypes, selc, M1, _ptr(dT), _ptr(ds), _ptr(dRt))
     return ds, dRt
 
 
@@ -461,8 +474,8 @@ def dp_tabulate_tc_plan_f64(table, info: dp_table_info, nnei, ntypes=None, buf=N
     elif not buf.is_cuda or buf.dtype != torch.uint8 or not buf.is_contiguous() or buf.numel() < need:
         raise ValueError(f"buf must be a contiguous CUDA uint8 tensor of at least {need} bytes")
     rec = dp_tc_plan()
-    _check(_lib.dp_tabulate_tc_plan_f64(_ptr(table), ctypes.byref(info), int(nnei), ntypes, M1, _ptr(buf),
-                                        buf.numel(), ctypes.byref(rec), _stream(table)))
+    _run(table.get_device(), _lib.dp_tabulate_tc_plan_f64, _ptr(table), ctypes.byref(info), int(nnei), ntypes, M1,
+         _ptr(buf), buf.numel(), ctypes.byref(rec))
     return TcPlan(buf, rec)
 
 
@@ -499,10 +512,9 @@ def dp_tabulate_fusion_fwd_tc_f64(plan, info: dp_table_info, s, Rt, nvalid, atyp
     if nloc == 0:
         return T if M2 is None else (T, D)
     work = _tab_tc_work(work, info, nloc, nnei, ntypes, M1, s.device)
-    _check(_lib.dp_tabulate_fusion_fwd_tc_f64(ctypes.byref(plan.rec), ctypes.byref(info), _ptr(s), _ptr(Rt),
-                                              _ptr(nvalid), _ptr(atype), nloc, nnei, ntypes, selc, M1, _ptr(T),
-                                              0 if M2 is None else int(M2), None if M2 is None else _ptr(D),
-                                              _ptr(work), work.numel(), _stream(s)))
+    _run(s.get_device(), _lib.dp_tabulate_fusion_fwd_tc_f64, ctypes.byref(plan.rec), ctypes.byref(info), _ptr(s),
+         _ptr(Rt), _ptr(nvalid), _ptr(atype), nloc, nnei, ntypes, selc, M1, _ptr(T), 0 if M2 is None else int(M2),
+         None if M2 is None else _ptr(D), _ptr(work), work.numel())
     return T if M2 is None else (T, D)
 
 
@@ -524,10 +536,9 @@ def dp_tabulate_fusion_grad_tc_f64(plan, info: dp_table_info, s, Rt, nvalid, aty
     if flags and work is None:
         raise ValueError("DP_TC_REUSE_RUNS needs the forward's work buffer")
     work = _tab_tc_work(work, info, nloc, nnei, ntypes, M1, s.device)
-    _check(_lib.dp_tabulate_fusion_grad_tc_f64(ctypes.byref(plan.rec), ctypes.byref(info), _ptr(s), _ptr(Rt),
-                                               _ptr(nvalid), _ptr(atype), nloc, nnei, ntypes, selc, M1, _ptr(dT),
-                                               _ptr(ds), _ptr(dRt), _ptr(work), work.numel(), int(flags),
-                                               _stream(s)))
+    _run(s.get_device(), _lib.dp_tabulate_fusion_grad_tc_f64, ctypes.byref(plan.rec), ctypes.byref(info), _ptr(s),
+         _ptr(Rt), _ptr(nvalid), _ptr(atype), nloc, nnei, ntypes, selc, M1, _ptr(dT), _ptr(ds), _ptr(dRt), _ptr(work),
+         work.numel(), int(flags))
     return ds, dRt
 
 
@@ -564,11 +575,9 @@ def dp_tabulate_fusion_env_fwd_tc_f64(plan, info: dp_table_info, coord, nlist, s
     if nloc == 0:
         return T, D, nvalid
     work = _tab_tc_work(work, info, nloc, nnei, ntypes, M1, coord.device)
-    _check(_lib.dp_tabulate_fusion_env_fwd_tc_f64(ctypes.byref(plan.rec), ctypes.byref(info), _ptr(coord), _ptr(nlist),
-                                                  ctypes.byref(env), _ptr(atype), nloc, nnei, ntypes, selc, M1,
-                                                  _ptr(nvalid), _ptr(T), 0 if M2 is None else int(M2),
-                                                  None if M2 is None else _ptr(D), _ptr(work), work.numel(),
-                                                  _stream(coord)))
+    _run(coord.get_device(), _lib.dp_tabulate_fusion_env_fwd_tc_f64, ctypes.byref(plan.rec), ctypes.byref(info),
+         _ptr(coord), _ptr(nlist), ctypes.byref(env), _ptr(atype), nloc, nnei, ntypes, selc, M1, _ptr(nvalid), _ptr(T),
+         0 if M2 is None else int(M2), None if M2 is None else _ptr(D), _ptr(work), work.numel())
     return T, D, nvalid
 
 
@@ -588,10 +597,9 @@ def dp_tabulate_fusion_env_grad_tc_f64(plan, info: dp_table_info, coord, nlist, 
         F = _dev(out[0], "F", torch.float64, (nall, 3))
         W = _dev(out[1], "virial", torch.float64, (3, 3))
     work = _tab_tc_work(work, info, max(nloc, 1), nnei, ntypes, M1, coord.device)
-    _check(_lib.dp_tabulate_fusion_env_grad_tc_f64(ctypes.byref(plan.rec), ctypes.byref(info), _ptr(coord),
-                                                   _ptr(nlist), ctypes.byref(env), _ptr(atype), nloc, nall, nnei,
-                                                   ntypes, selc, M1, _ptr(dT), _ptr(F), _ptr(W), _ptr(work),
-                                                   work.numel(), int(flags), _stream(coord)))
+    _run(coord.get_device(), _lib.dp_tabulate_fusion_env_grad_tc_f64, ctypes.byref(plan.rec), ctypes.byref(info),
+         _ptr(coord), _ptr(nlist), ctypes.byref(env), _ptr(atype), nloc, nall, nnei, ntypes, selc, M1, _ptr(dT),
+         _ptr(F), _ptr(W), _ptr(work), work.numel(), int(flags))
     return F, W
 
 
@@ -618,8 +626,8 @@ def dp_env_mat(coord, nlist, sel, env: dp_env_info, out=None, arith=None):
         Rt = _dev(out[1], "Rt", dtype, (nloc, nnei, 4))
         nvalid = _dev(out[2], "nvalid", torch.int32, (nloc, ntypes))
     fn = getattr(_lib, f"dp_env_mat_{_suffix(arith or dtype)}")
-    _check(fn(_ptr(coord), _ptr(nlist), nloc, nnei, ntypes, selc, ctypes.byref(env), _ptr(s), _ptr(Rt), _ptr(nvalid),
-              _stream(coord)))
+    _run(coord.get_device(), fn, _ptr(coord), _ptr(nlist), nloc, nnei, ntypes, selc, ctypes.byref(env), _ptr(s),
+         _ptr(Rt), _ptr(nvalid))
     return s, Rt, nvalid
 
 
@@ -643,8 +651,8 @@ def dp_force_virial(coord, nlist, env: dp_env_info, ds, dRt, out=None, arith=Non
         F = _dev(out[0], "F", dtype, (nall, 3))
         W = _dev(out[1], "virial", dtype, (3, 3))
     fn = getattr(_lib, f"dp_force_virial_{_suffix(arith or dtype)}")
-    _check(fn(_ptr(coord), _ptr(nlist), nloc, nall, nnei, ctypes.byref(env), _ptr(ds), _ptr(dRt), _ptr(F), _ptr(W),
-              _stream(coord)))
+    _run(coord.get_device(), fn, _ptr(coord), _ptr(nlist), nloc, nall, nnei, ctypes.byref(env), _ptr(ds), _ptr(dRt),
+         _ptr(F), _ptr(W))
     return F, W
 
 
@@ -659,7 +667,7 @@ def dp_descriptor_contract(T, M2: int, out=None, arith=None) -> torch.Tensor:
     if arith == DF64 and T.dtype != torch.float64:
         raise TypeError("df64 descriptor takes f64 arrays")
     fn = getattr(_lib, f"dp_descriptor_contract_{_suffix(arith or T.dtype)}")
-    _check(fn(_ptr(T), nloc, M1, int(M2), _ptr(D), _stream(T)))
+    _run(T.get_device(), fn, _ptr(T), nloc, M1, int(M2), _ptr(D))
     return D
 
 
@@ -677,7 +685,7 @@ def dp_descriptor_contract_grad(T, dD, out=None, arith=None) -> torch.Tensor:
     if arith == DF64 and T.dtype != torch.float64:
         raise TypeError("df64 descriptor backward takes f64 arrays")
     fn = getattr(_lib, f"dp_descriptor_contract_grad_{_suffix(arith or T.dtype)}")
-    _check(fn(_ptr(T), _ptr(dD), nloc, M1, M2, _ptr(dT), _stream(T)))
+    _run(T.get_device(), fn, _ptr(T), _ptr(dD), nloc, M1, M2, _ptr(dT))
     return dT
 
 
@@ -741,7 +749,7 @@ def dp_fitting_fwd(params, widths, type_start, D, out=None, arith=None):
         E = _dev(out[0], "E", dtype, _out_shape(nloc, widths))
         act = _dev(out[1], "act", dtype, (nloc, max(H, 1)))
     fn = getattr(_lib, f"dp_fitting_fwd_{_suffix(arith or dtype)}")
-    _check(fn(_ptr(params), w, nlayer, ntypes, ts, _ptr(D), _ptr(E), _ptr(act), _stream(params)))
+    _run(params.get_device(), fn, _ptr(params), w, nlayer, ntypes, ts, _ptr(D), _ptr(E), _ptr(act))
     return E, act
 
 
@@ -762,7 +770,7 @@ def dp_fitting_grad(params, widths, type_start, act, g=None, out=None, work=None
     else:
         work = _dev(work, "work", dtype, (2, nloc, maxh))
     fn = getattr(_lib, f"dp_fitting_grad_{_suffix(arith or dtype)}")
-    _check(fn(_ptr(params), w, nlayer, ntypes, ts, _ptr(act), _ptr(g), _ptr(dD), _ptr(work), _stream(params)))
+    _run(params.get_device(), fn, _ptr(params), w, nlayer, ntypes, ts, _ptr(act), _ptr(g), _ptr(dD), _ptr(work))
     return dD
 
 
@@ -776,8 +784,8 @@ def dp_fitting_grad_noalloc_f64(params, widths, type_start, act, g=None, out=Non
         g = _dev(g, "g", torch.float64, _out_shape(nloc, widths))
     dD = torch.empty((nloc, widths[0]), dtype=torch.float64, device=params.device) if out is None else \
         _dev(out, "out", torch.float64, (nloc, widths[0]))
-    _check(_lib.dp_fitting_grad_noalloc_f64(_ptr(params), w, nlayer, ntypes, ts, _ptr(act), _ptr(g), _ptr(dD),
-                                            _stream(params)))
+    _run(params.get_device(), _lib.dp_fitting_grad_noalloc_f64, _ptr(params), w, nlayer, ntypes, ts, _ptr(act), _ptr(g),
+         _ptr(dD))
     return dD
 
 
@@ -815,8 +823,8 @@ def dp_fitting_fwd_tc_f64(params, widths, type_start, D, out=None, work=None):
         E = _dev(out[0], "E", torch.float64, _out_shape(nloc, widths))
         act = _dev(out[1], "act", torch.float64, (nloc, max(H, 1)))
     work = _tc_work(work, widths, nloc, params.device)
-    _check(_lib.dp_fitting_fwd_tc_f64(_ptr(params), w, nlayer, ntypes, ts, _ptr(D), _ptr(E), _ptr(act), _ptr(work),
-                                      work.numel(), _stream(params)))
+    _run(params.get_device(), _lib.dp_fitting_fwd_tc_f64, _ptr(params), w, nlayer, ntypes, ts, _ptr(D), _ptr(E),
+         _ptr(act), _ptr(work), work.numel())
     return E, act
 
 
@@ -830,8 +838,8 @@ def dp_fitting_grad_tc_f64(params, widths, type_start, act, g=None, out=None, wo
     dD = torch.empty((nloc, widths[0]), dtype=torch.float64, device=params.device) if out is None else \
         _dev(out, "out", torch.float64, (nloc, widths[0]))
     work = _tc_work(work, widths, nloc, params.device)
-    _check(_lib.dp_fitting_grad_tc_f64(_ptr(params), w, nlayer, ntypes, ts, _ptr(act), _ptr(g), _ptr(dD),
-                                       _ptr(work), work.numel(), _stream(params)))
+    _run(params.get_device(), _lib.dp_fitting_grad_tc_f64, _ptr(params), w, nlayer, ntypes, ts, _ptr(act), _ptr(g),
+         _ptr(dD), _ptr(work), work.numel())
     return dD
 
 
@@ -876,7 +884,7 @@ def dp_vector_head(T, a, out=None):
     """v [nloc][3] = sum_m a[m] T[1:4, m] per atom (a vector DP model's head on the compressed T)."""
     T, a, nloc, M1 = _head_inputs(T, a)
     v = torch.empty((nloc, 3), dtype=T.dtype, device=T.device) if out is None else _dev(out, "v", T.dtype, (nloc, 3))
-    _check(getattr(_lib, f"dp_vector_head_{_suffix(T.dtype)}")(_ptr(T), _ptr(a), nloc, M1, _ptr(v), _stream(T)))
+    _run(T.get_device(), getattr(_lib, f"dp_vector_head_{_suffix(T.dtype)}"), _ptr(T), _ptr(a), nloc, M1, _ptr(v))
     return v
 
 
@@ -885,7 +893,7 @@ def dp_tensor_head(T, a, out=None):
     T, a, nloc, M1 = _head_inputs(T, a)
     A = torch.empty((nloc, 3, 3), dtype=T.dtype, device=T.device) if out is None else \
         _dev(out, "A", T.dtype, (nloc, 3, 3))
-    _check(getattr(_lib, f"dp_tensor_head_{_suffix(T.dtype)}")(_ptr(T), _ptr(a), nloc, M1, _ptr(A), _stream(T)))
+    _run(T.get_device(), getattr(_lib, f"dp_tensor_head_{_suffix(T.dtype)}"), _ptr(T), _ptr(a), nloc, M1, _ptr(A))
     return A
 
 
@@ -908,7 +916,7 @@ def _head_grad(kind, T, a, dout, shape, dT, da, accumulate, want):
         da = torch.empty((nloc, M1), dtype=T.dtype, device=T.device) if da is None else \
             _dev(da, "da", T.dtype, (nloc, M1))
     fn = getattr(_lib, f"dp_{kind}_head_grad_{_suffix(T.dtype)}")
-    _check(fn(_ptr(T), _ptr(a), _ptr(dout), nloc, M1, _ptr(dT), _ptr(da), int(bool(accumulate)), _stream(T)))
+    _run(T.get_device(), fn, _ptr(T), _ptr(a), _ptr(dout), nloc, M1, _ptr(dT), _ptr(da), int(bool(accumulate)))
     return dT, da
 
 
@@ -933,7 +941,6 @@ _ROW_FN = {name: {t: getattr(_lib, f"dp_{name}_{x}") for t, x in _ROW_SUFFIX.ite
 # the type of weights and sums beside rows of a type
 _WDTYPE = {torch.float64: torch.float64, torch.float32: torch.float32, torch.bfloat16: torch.float32,
            torch.float16: torch.float32}
-_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _p(t, name, dtype, shape, dev):
@@ -1007,10 +1014,9 @@ def dp_route_plan(expert, nexp, out=None, work=None):
     if pos is None:
         pos = torch.empty_like(expert)
     wp, wn, work = _work_ptr(work, need if need > 1 else 0, expert, dev)  # 1: none needed
-    _check(_lib.dp_route_plan(_p(expert, "expert", torch.int32, (ntok, topk), dev), ntok, topk, nexp,
-                              _p(start, "start", torch.int64, (nexp + 1,), dev),
-                              _p(src, "src", torch.int32, (ntok * topk,), dev),
-                              _p(pos, "pos", torch.int32, (ntok, topk), dev), wp, wn, _raw_stream(dev)))
+    _run(dev, _lib.dp_route_plan, _p(expert, "expert", torch.int32, (ntok, topk), dev), ntok, topk, nexp,
+         _p(start, "start", torch.int64, (nexp + 1,), dev), _p(src, "src", torch.int32, (ntok * topk,), dev),
+         _p(pos, "pos", torch.int32, (ntok, topk), dev), wp, wn)
     return start, src, pos
 
 
@@ -1021,10 +1027,8 @@ def dp_route_gather(x, src, pos, out=None):
     ntok, topk = _pairs(pos)
     n = ntok * topk
     xs = torch.empty((n, H), dtype=dtype, device=x.device) if out is None else out
-    _check(_ROW_FN["route_gather"][dtype](
-        _p(x, "x", dtype, (ntok, H), dev), _p(src, "src", torch.int32, (n,), dev),
-        _p(pos, "pos", torch.int32, (ntok, topk), dev), ntok, topk, H, _p(xs, "out", dtype, (n, H), dev),
-        _raw_stream(dev)))
+    _run(dev, _ROW_FN["route_gather"][dtype], _p(x, "x", dtype, (ntok, H), dev), _p(src, "src", torch.int32, (n,), dev),
+         _p(pos, "pos", torch.int32, (ntok, topk), dev), ntok, topk, H, _p(xs, "out", dtype, (n, H), dev))
     return xs
 
 
@@ -1034,10 +1038,10 @@ def dp_route_combine(z, pos, w=None, out=None):
     dtype, _, H, dev = _rows(z, "z")
     ntok, topk = _pairs(pos)
     y = torch.empty((ntok, H), dtype=dtype, device=z.device) if out is None else out
-    _check(_ROW_FN["route_combine"][dtype](
-        _p(z, "z", dtype, (ntok * topk, H), dev), _p(pos, "pos", torch.int32, (ntok, topk), dev),
-        None if w is None else _p(w, "w", _WDTYPE[dtype], (ntok, topk), dev), ntok, topk, H,
-        _p(y, "out", dtype, (ntok, H), dev), _raw_stream(dev)))
+    _run(dev, _ROW_FN["route_combine"][dtype], _p(z, "z", dtype, (ntok * topk, H), dev),
+         _p(pos, "pos", torch.int32, (ntok, topk), dev),
+         None if w is None else _p(w, "w", _WDTYPE[dtype], (ntok, topk), dev), ntok, topk, H,
+         _p(y, "out", dtype, (ntok, H), dev))
     return y
 
 
@@ -1059,10 +1063,9 @@ def dp_route_combine_grad(z, src, pos, w, dy, out=None, want=("dz", "dw")):
         dwp = _p(dw, "dw", wd, (ntok, topk), dev)
     else:
         zp = dwp = dw = None
-    _check(_ROW_FN["route_combine_grad"][dtype](
-        zp, _p(src, "src", torch.int32, (n,), dev), _p(pos, "pos", torch.int32, (ntok, topk), dev),
-        None if w is None else _p(w, "w", wd, (ntok, topk), dev), _p(dy, "dy", dtype, (ntok, H), dev), ntok, topk, H,
-        _p(dz, "dz", dtype, (n, H), dev), dwp, _raw_stream(dev)))
+    _run(dev, _ROW_FN["route_combine_grad"][dtype], zp, _p(src, "src", torch.int32, (n,), dev),
+         _p(pos, "pos", torch.int32, (ntok, topk), dev), None if w is None else _p(w, "w", wd, (ntok, topk), dev),
+         _p(dy, "dy", dtype, (ntok, H), dev), ntok, topk, H, _p(dz, "dz", dtype, (n, H), dev), dwp)
     return dz, dw
 
 
@@ -1084,9 +1087,8 @@ def dp_quant_rows_i8(x, src=None, pos=None, out=None):
         xq = torch.empty((n, ldq), dtype=torch.int8, device=x.device)
     if sx is None:
         sx = torch.empty((n,), dtype=torch.float32, device=x.device)
-    _check(_ROW_FN["quant_rows_i8"][dtype](
-        _p(x, "x", dtype, (ntok, K), dev), sp, pp, ntok, topk, K, _p(xq, "xq", torch.int8, (n, ldq), dev),
-        _p(sx, "sx", torch.float32, (n,), dev), _raw_stream(dev)))
+    _run(dev, _ROW_FN["quant_rows_i8"][dtype], _p(x, "x", dtype, (ntok, K), dev), sp, pp, ntok, topk, K,
+         _p(xq, "xq", torch.int8, (n, ldq), dev), _p(sx, "sx", torch.float32, (n,), dev))
     return xq, sx
 
 
@@ -1119,12 +1121,11 @@ def dp_linear_i8(xq, sx, wq, sw, bias=None, start=None, act=None, dtype=torch.fl
     y = torch.empty((rows, N), dtype=dtype, device=xq.device) if out is None else out
     need = 0 if work is not None else _lib.dp_linear_i8_work_bytes(rows, K, N, nexp)
     wp, wn, work = _work_ptr(work, need, xq, dev)
-    _check(_ROW_FN["linear_i8"][dtype](
-        _p(xq, "xq", torch.int8, (rows, K), dev), _p(sx, "sx", f32, (rows,), dev), rows, K,
-        _p(wq, "wq", torch.int8, (nexp, N, K), dev), _p(sw, "sw", f32, (nexp, N), dev),
-        None if bias is None else _p(bias, "bias", f32, (nexp, N), dev), nexp, N,
-        None if start is None else _p(start, "start", torch.int64, (nexp + 1,), dev), _ACTS[act],
-        _p(y, "out", dtype, (rows, N), dev), wp, wn, _raw_stream(dev)))
+    _run(dev, _ROW_FN["linear_i8"][dtype], _p(xq, "xq", torch.int8, (rows, K), dev), _p(sx, "sx", f32, (rows,), dev),
+         rows, K, _p(wq, "wq", torch.int8, (nexp, N, K), dev), _p(sw, "sw", f32, (nexp, N), dev),
+         None if bias is None else _p(bias, "bias", f32, (nexp, N), dev), nexp, N,
+         None if start is None else _p(start, "start", torch.int64, (nexp + 1,), dev), _ACTS[act],
+         _p(y, "out", dtype, (rows, N), dev), wp, wn)
     return y
 
 
@@ -1164,10 +1165,9 @@ def dp_norm_gate_fwd(r, f, a, w1, w2, b1=None, b2=None, gate=None, kind="rms", e
         u = torch.empty_like(r)
     if stats is None:
         stats = torch.empty((ntok, 4), dtype=wd, device=f.device)
-    _check(_ROW_FN["norm_gate_fwd"][dtype](
-        rp, _p(f, "f", dtype, row, dev), gp, gk, _p(a, "a", wd, vec, dev), _p(w1, "w1", wd, vec, dev), bp1,
-        _p(w2, "w2", wd, vec, dev), bp2, ntok, H, k, eps, _p(r2, "r2", dtype, row, dev), _p(u, "u", dtype, row, dev),
-        _p(stats, "stats", wd, (ntok, 4), dev), _raw_stream(dev)))
+    _run(dev, _ROW_FN["norm_gate_fwd"][dtype], rp, _p(f, "f", dtype, row, dev), gp, gk, _p(a, "a", wd, vec, dev),
+         _p(w1, "w1", wd, vec, dev), bp1, _p(w2, "w2", wd, vec, dev), bp2, ntok, H, k, eps,
+         _p(r2, "r2", dtype, row, dev), _p(u, "u", dtype, row, dev), _p(stats, "stats", wd, (ntok, 4), dev))
     return r2, u, stats
 
 
@@ -1206,8 +1206,7 @@ def dp_norm_gate_grad(r2, f, a, w1, w2, stats, dr2, du, b1=None, b2=None, gate=N
             None if gate is None else _p(res["dgate"], "dgate", dtype, gate.shape, dev)]
     ptrs += [None if res[n] is None else _p(res[n], n, wd, vec, dev) for n in ("da", "dw1", "dw2", "db1", "db2")]
     wp, wn, work = _work_ptr(work, dp_norm_gate_work_bytes(H, dtype) if work is None else 0, f, dev)
-    _check(_ROW_FN["norm_gate_grad"][dtype](
-        _p(r2, "r2", dtype, row, dev), fp, gp, gk, ap, _p(w1, "w1", wd, vec, dev), bp1,
-        _p(w2, "w2", wd, vec, dev), _p(stats, "stats", wd, (ntok, 4), dev), _p(dr2, "dr2", dtype, row, dev),
-        _p(du, "du", dtype, row, dev), ntok, H, k, *ptrs, wp, wn, _raw_stream(dev)))
+    _run(dev, _ROW_FN["norm_gate_grad"][dtype], _p(r2, "r2", dtype, row, dev), fp, gp, gk, ap,
+         _p(w1, "w1", wd, vec, dev), bp1, _p(w2, "w2", wd, vec, dev), _p(stats, "stats", wd, (ntok, 4), dev),
+         _p(dr2, "dr2", dtype, row, dev), _p(du, "du", dtype, row, dev), ntok, H, k, *ptrs, wp, wn)
     return res
