@@ -943,6 +943,12 @@ _WDTYPE = {torch.float64: torch.float64, torch.float32: torch.float32, torch.bfl
            torch.float16: torch.float32}
 
 
+def _fits(rows, *sizes):
+    """Raises for sizes past int64 (rows) or int (the others): ctypes would pass their low bits alone."""
+    if rows >> 63 not in (0, -1) or any(v >> 31 not in (0, -1) for v in sizes):
+        raise ValueError(f"sizes out of range: {(rows, *sizes)}")
+
+
 def _p(t, name, dtype, shape, dev):
     """The address of t, checked: a contiguous CUDA tensor of dtype and shape on device number dev."""
     try:
@@ -964,6 +970,8 @@ def _rows(t, name):
     if t.dim() != 2:
         raise ValueError(f"{name} must have 2 dimensions, got {tuple(t.shape)}")
     n, H = t.shape
+    if H >> 31:
+        raise ValueError(f"{name} has rows of {H} elements")
     return dtype, n, H, t.get_device()
 
 
@@ -971,6 +979,8 @@ def _pairs(pos):
     """(ntok, topk) of a plan's pos."""
     if not isinstance(pos, torch.Tensor) or pos.dim() != 2:
         raise ValueError("pos must be a plan's [ntok][topk] tensor")
+    if pos.shape[1] >> 31:
+        raise ValueError(f"pos has {pos.shape[1]} pairs a token")
     return pos.shape
 
 
@@ -989,6 +999,7 @@ def _work_ptr(work, need, like, dev):
 
 def dp_route_work_bytes(ntok, topk, nexp) -> int:
     """Bytes of device scratch dp_route_plan needs."""
+    _fits(ntok, topk, nexp)
     n = _lib.dp_route_work_bytes(ntok, topk, nexp)
     if n == 0:
         raise ValueError(f"bad plan: {ntok} tokens, {topk} experts each of {nexp}")
@@ -1097,6 +1108,7 @@ _ACTS = {None: 0, "tanh": 1}
 
 def dp_linear_i8_work_bytes(rows, K, N, nexp) -> int:
     """Bytes of device scratch dp_linear_i8 needs (0 for few rows)."""
+    _fits(rows, K, N, nexp)
     return _lib.dp_linear_i8_work_bytes(rows, K, N, nexp)
 
 
@@ -1119,6 +1131,7 @@ def dp_linear_i8(xq, sx, wq, sw, bias=None, start=None, act=None, dtype=torch.fl
     nexp, N, _ = wq.shape
     dev, f32 = xq.get_device(), torch.float32
     y = torch.empty((rows, N), dtype=dtype, device=xq.device) if out is None else out
+    _fits(rows, K, N, nexp)
     need = 0 if work is not None else _lib.dp_linear_i8_work_bytes(rows, K, N, nexp)
     wp, wn, work = _work_ptr(work, need, xq, dev)
     _run(dev, _ROW_FN["linear_i8"][dtype], _p(xq, "xq", torch.int8, (rows, K), dev), _p(sx, "sx", f32, (rows,), dev),
@@ -1173,6 +1186,7 @@ def dp_norm_gate_fwd(r, f, a, w1, w2, b1=None, b2=None, gate=None, kind="rms", e
 
 def dp_norm_gate_work_bytes(H, dtype) -> int:
     """Bytes of device scratch dp_norm_gate_grad needs for rows of H elements of dtype."""
+    _fits(0, H)
     n = _lib.dp_norm_gate_work_bytes(H, dtype.itemsize)
     if n == 0:
         raise ValueError(f"unsupported row length {H}")

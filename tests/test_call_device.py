@@ -21,6 +21,11 @@ class OnDevice1(torch.Tensor):
     def get_device(self):
         return 1
 
+    @classmethod
+    def rows(cls, length):
+        """One row of `length` elements, all the same one in memory."""
+        return torch.zeros(1, 1).expand(1, length).as_subclass(cls)
+
 
 def on1(*shape, dtype=torch.float32):
     return torch.zeros(*shape, dtype=dtype).as_subclass(OnDevice1)

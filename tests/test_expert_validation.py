@@ -3,6 +3,9 @@ never dereferenced)."""
 import ctypes
 
 import pytest
+import torch
+
+from test_call_device import OnDevice1
 
 
 @pytest.fixture(scope="module")
@@ -91,3 +94,22 @@ def test_norm_gate(dpc):
 
         assert grad(dr=None) == grad(dgate=None) == grad(db1=None) == grad(work=None) == dpc.DP_ERR_NULL
         assert grad(nbytes=16) == grad(kind=-1) == grad(work=ctypes.c_void_p(0x1008)) == dpc.DP_ERR_SHAPE
+
+
+def test_sizes_past_a_c_int_are_refused(dpc):
+    """ctypes passes the low 32 bits of a longer size alone: a row of 2^32 + 8 elements would be one of 8."""
+    big = 2 ** 32
+    for bad in ((4, 2, big + 8), (4, big + 2, 8), (2 ** 64 + 4, 2, 8), (4, 2, -big + 8)):
+        with pytest.raises(ValueError):
+            dpc.dp_route_work_bytes(*bad)
+    for bad in ((4096, big + 2048, 4096, 1), (4096, 2048, big + 4096, 1), (4096, 2048, 4096, big + 1), (2 ** 64 + 4096, 2048, 4096, 1)):
+        with pytest.raises(ValueError):
+            dpc.dp_linear_i8_work_bytes(*bad)
+    assert dpc.dp_linear_i8_work_bytes(4096, 2048, 4096, 1) > 0
+    with pytest.raises(ValueError):
+        dpc.dp_norm_gate_work_bytes(big + 240, torch.float32)
+    long = OnDevice1.rows(big + 8)
+    with pytest.raises(ValueError, match="rows of 4294967304"):
+        dpc._rows(long, "x")
+    with pytest.raises(ValueError, match="4294967304 pairs"):
+        dpc._pairs(long)
