@@ -266,6 +266,7 @@ struct Shape {
   static constexpr uint32_t kTmemCols = 2 * TN;
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (2 * kStages + 5) * 8 + 16;  // aligned within
   static_assert(kSmem <= 227 * 1024 && TN % 64 == 0 && TN <= 256, "tile");
+  static_assert(!kWide || (kEpiWarps % 4 == 0 && kLoadWarps % 4 == 0 && kThreads % 128 == 0), "roles of whole warpgroups");
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -361,78 +362,79 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
   const uint32_t tmem = *holder;
   bool ok = true;
 
-  if (warp > S::kMmaWarp) {
-    // ---------------------------------------------------------------- wide form: the weights' copies, two idle warps
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
-    if (warp == S::kMmaWarp + 1) {
-      int st = 0, phase = 1;
+  if (warp >= S::kMmaWarp) {  // in the wide form a warpgroup: one setmaxnreg for all four of its warps
+    if constexpr (S::kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
+    if (warp == S::kMmaWarp) {
+      // -------------------------------------------------------------- the MMAs
+      int j = 0, unit = 0;  // stages, accumulator uses
       Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
       for (; ok; t.tile += gridDim.x) {
         seek(p, TN, nct, t);
         if (!t.have) break;
         if (t.e == p.nexp) continue;
-        const unsigned char *src = p.image + ((int64_t)t.e * nct + t.n0 / kTM) * nkb * S::kStageA;
+        const uint32_t cols = (uint32_t)(t.r1 - t.r0 + 15) / 16 * 16;
+        const uint32_t idesc = (1u << 4) | ((uint32_t)(kTM >> 4) << 24) | ((cols >> 3) << 17);
         if (lane == 0) {
-          for (int kb = 0; kb < nkb; ++kb) {
-            ok = wait(smem_u32(empty + st), phase, stop);
+          for (int kb = 0; kb < nkb && ok; ++kb, ++j) {
+            const int st = j % S::kStages, buf = unit & 1, slice = kb % (kChunkK / kKB);
+            if (slice == 0 && unit >= 2) ok = wait(smem_u32(acc_empty + buf), ((unit >> 1) - 1) & 1, stop);
+            ok = ok && wait(smem_u32(full + st), (j / S::kStages) & 1, stop);
             if (!ok) break;
-            const uint32_t bar = smem_u32(full + st);
-            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)S::kStageA)
-                         : "memory");
-            asm volatile(
-                "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                    smem_u32(smem) + st * S::kStageBytes),
-                "l"(src + (int64_t)kb * S::kStageA), "r"((uint32_t)S::kStageA), "r"(bar)
-                : "memory");
-            if (++st == S::kStages) {
-              st = 0;
-              phase ^= 1;
+            asm volatile("tcgen05.fence::after_thread_sync;");
+            const uint32_t base = smem_u32(smem) + st * S::kStageBytes;
+            const uint64_t a0 = smem_desc(base), b0 = smem_desc(base + S::kStageA);
+  #pragma unroll
+            for (int k = 0; k < kKB / 16; ++k) {
+              const uint32_t acc = slice > 0 || k > 0 ? 1u : 0u;
+              asm volatile(
+                  "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+                  " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(tmem + (uint32_t)(buf * TN)),
+                  "l"(a0 + (uint64_t)(k * 2)), "l"(b0 + (uint64_t)(k * 2)), "r"(idesc), "r"(acc));
+            }
+            commit(smem_u32(empty + st));
+            if (slice == kChunkK / kKB - 1 || kb == nkb - 1) {
+              commit(smem_u32(acc_full + buf));
+              ++unit;
             }
           }
         }
         ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
       }
+      if (lane == 0) commit(smem_u32(done));  // completes when every MMA issued above has
       if (!ok) *stop = 1;
-    }
-  } else if (warp == S::kMmaWarp) {
-    // ---------------------------------------------------------------- the MMAs
-    if constexpr (S::kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
-    int j = 0, unit = 0;  // stages, accumulator uses
-    Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
-    for (; ok; t.tile += gridDim.x) {
-      seek(p, TN, nct, t);
-      if (!t.have) break;
-      if (t.e == p.nexp) continue;
-      const uint32_t cols = (uint32_t)(t.r1 - t.r0 + 15) / 16 * 16;
-      const uint32_t idesc = (1u << 4) | ((uint32_t)(kTM >> 4) << 24) | ((cols >> 3) << 17);
-      if (lane == 0) {
-        for (int kb = 0; kb < nkb && ok; ++kb, ++j) {
-          const int st = j % S::kStages, buf = unit & 1, slice = kb % (kChunkK / kKB);
-          if (slice == 0 && unit >= 2) ok = wait(smem_u32(acc_empty + buf), ((unit >> 1) - 1) & 1, stop);
-          ok = ok && wait(smem_u32(full + st), (j / S::kStages) & 1, stop);
-          if (!ok) break;
-          asm volatile("tcgen05.fence::after_thread_sync;");
-          const uint32_t base = smem_u32(smem) + st * S::kStageBytes;
-          const uint64_t a0 = smem_desc(base), b0 = smem_desc(base + S::kStageA);
-#pragma unroll
-          for (int k = 0; k < kKB / 16; ++k) {
-            const uint32_t acc = slice > 0 || k > 0 ? 1u : 0u;
-            asm volatile(
-                "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-                " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(tmem + (uint32_t)(buf * TN)),
-                "l"(a0 + (uint64_t)(k * 2)), "l"(b0 + (uint64_t)(k * 2)), "r"(idesc), "r"(acc));
+    } else if constexpr (S::kWide) {
+      // -------------------------------------------------------------- the weights' copies, by one warp; two are idle
+      if (warp == S::kMmaWarp + 1) {
+        int st = 0, phase = 1;
+        Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
+        for (; ok; t.tile += gridDim.x) {
+          seek(p, TN, nct, t);
+          if (!t.have) break;
+          if (t.e == p.nexp) continue;
+          const unsigned char *src = p.image + ((int64_t)t.e * nct + t.n0 / kTM) * nkb * S::kStageA;
+          if (lane == 0) {
+            for (int kb = 0; kb < nkb; ++kb) {
+              ok = wait(smem_u32(empty + st), phase, stop);
+              if (!ok) break;
+              const uint32_t bar = smem_u32(full + st);
+              asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)S::kStageA)
+                           : "memory");
+              asm volatile(
+                  "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                      smem_u32(smem) + st * S::kStageBytes),
+                  "l"(src + (int64_t)kb * S::kStageA), "r"((uint32_t)S::kStageA), "r"(bar)
+                  : "memory");
+              if (++st == S::kStages) {
+                st = 0;
+                phase ^= 1;
+              }
+            }
           }
-          commit(smem_u32(empty + st));
-          if (slice == kChunkK / kKB - 1 || kb == nkb - 1) {
-            commit(smem_u32(acc_full + buf));
-            ++unit;
-          }
+          ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
         }
+        if (!ok) *stop = 1;
       }
-      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
     }
-    if (lane == 0) commit(smem_u32(done));  // completes when every MMA issued above has
-    if (!ok) *stop = 1;
   } else if (warp >= kEpiWarps) {
     // ---------------------------------------------------------------- loaders
     if constexpr (S::kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
