@@ -18,6 +18,9 @@ using dfl::df64;
 int set_error(int code, const char *fmt, ...);  // stores the message, returns code
 void clear_error();
 int launch_status(const char *what);  // DP_ERR_CUDA if the last launch failed
+// Lets kernel k have up to `most` bytes of dynamic shared memory on the current device.  The limit is the kernel's,
+// not the call's: `most` is the same for all of k's calls, or one would lower it under another thread's launch.
+int allow_smem(const void *k, size_t most, const char *who);
 void prof_mark(const char *name, cudaStream_t st);  // kernel timing hook (dp_profile_begin)
 int take_wait_timeouts_tabulate(unsigned int *count);  // GEMM wait timeouts per unit (dp_tc_wait_timeouts)
 int take_wait_timeouts_fitting(unsigned int *count);

@@ -28,6 +28,11 @@ int launch_status(const char *what) {
   return DP_OK;
 }
 
+int allow_smem(const void *k, size_t most, const char *who) {
+  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+  return e == cudaSuccess ? DP_OK : set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+}
+
 // Kernel timing hook (off unless dp_profile_begin was called): calls that launch several kernels
 // record the caller's events on their stream, one after each kernel, in order, with the kernel's name.
 namespace {

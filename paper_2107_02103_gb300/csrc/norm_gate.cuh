@@ -274,6 +274,7 @@ struct RowFeed {
 };
 
 constexpr int kMaxStages = 4;
+constexpr size_t kBulkRoom = 200 * 1024;  // shared memory that an SM's blocks of a bulk form divide
 
 // Cut rows' weights into shared memory, beside the packs of a row that begins at `off`: vector i at out + i * room.
 template <int N, typename A>
@@ -696,7 +697,8 @@ __global__ void __launch_bounds__(1024) norm_finish_kernel(const A *__restrict__
   if (lane == 0 && blockIdx.x * 32 + row < H) out[blockIdx.x * 32 + row] = v;
 }
 
-constexpr int kRowWarps = 4;  // rows (warps) per block where a warp holds a row
+constexpr int kRowWarps = 4;      // rows (warps) per block where a warp holds a row,
+constexpr int kWarpRowMax = 256;  // which is up to this length
 
 // Launch shape, by the row length alone: a warp per row up to 256 elements, else a block with 8 elements a thread (16
 // past 8192).  The blocks that an SM's registers hold (64 a thread forward, 128 backward) stay and take rows in turn.
@@ -704,7 +706,7 @@ struct NormShape {
   int ept, threads, blocks;  // elements a thread, threads a block, blocks an SM
 };
 inline NormShape norm_shape(int H, bool grad) {
-  if (H <= 256) return {8, kRowWarps * 32, grad ? 3 : 8};
+  if (H <= kWarpRowMax) return {8, kRowWarps * 32, grad ? 3 : 8};
   const int ept = H <= 8192 ? 8 : 16, threads = (H + ept * 32 - 1) / (ept * 32) * 32;
   const int blocks = (grad ? 512 : 1024) / threads;
   return {ept, threads, blocks < 1 ? 1 : blocks};
@@ -736,17 +738,15 @@ int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st,
       const size_t row = (size_t)p.nin * (f_ == kCutRows ? cut_bytes<T>(p.H) : p.H * sizeof(T));
       const size_t weights = f_ == kCutRows ? cut_bytes<T>(p.H) / sizeof(T) * kNormVectors * sizeof(acc_t<T>) : 0;
       for (;; --blocks) {  // fewer blocks an SM where their rows would not fit
-        const int64_t room = (int64_t)200 * 1024 / blocks - (int64_t)weights;
+        const int64_t room = (int64_t)kBulkRoom / blocks - (int64_t)weights;
         p.stages = room < 0 ? 0 : room / (int64_t)row > kMaxStages ? kMaxStages : (int)(room / (int64_t)row);
         if (two) p.stages &= ~1;  // pairs of rows keep to pairs of stages
         if (p.stages > 0 || blocks == 1) break;
       }
       smem = row * p.stages + weights;
     }
-    if (smem > 32 * 1024) {  // the static part counts too
-      const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-      if (e != cudaSuccess) rc = set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
-    }
+    constexpr size_t kMost = b_ ? kBulkRoom : (size_t)kRowWarps * kNormVectors * kWarpRowMax * sizeof(acc_t<T>);
+    if (smem > 32 * 1024) rc = allow_smem((const void *)k, kMost, who);  // the static part counts too
     const int64_t units = w_ ? (p.ntok + kRowWarps - 1) / kRowWarps : p.ntok, most = 152 * (kGrad ? n.blocks : blocks);
     if (!rc) k<<<(unsigned)(kGrad || units > most ? most : units), n.threads, smem, st>>>(p);
   };
@@ -757,17 +757,16 @@ int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st,
       constexpr Feed f_ = decltype(F)::value;
       const size_t place = f_ == kCutRows ? cut_bytes<T>(p.H) : (size_t)p.H * sizeof(T), row = kWarpStages * p.nin * place;
       const size_t weights = f_ == kCutRows ? place / sizeof(T) * (kLayer ? 5 : 3) * sizeof(acc_t<T>) : 0;
-      const int fit = (int)((200 * 1024 - weights) / row), warps = fit < kRowWarpsMost<f_> ? fit : kRowWarpsMost<f_>;
+      const int fit = (int)((kBulkRoom - weights) / row), warps = fit < kRowWarpsMost<f_> ? fit : kRowWarpsMost<f_>;
       const int64_t held = f_ == kCutRows ? 1 : fit / 2 < kRowBlocks<f_> ? fit / 2 : kRowBlocks<f_>;
       const int64_t units = f_ == kCutRows ? 152 : (p.ntok + warps - 1) / warps, most = 152 * held;
       const size_t smem = row * warps + weights;
       auto k = norm_fwd_rows_kernel<T, f_, kLayer>;
-      const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-      if (e != cudaSuccess) rc = set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
-      else k<<<(unsigned)(units > most ? most : units), warps * 32, smem, st>>>(p);
+      rc = allow_smem((const void *)k, kBulkRoom, who);
+      if (!rc) k<<<(unsigned)(units > most ? most : units), warps * 32, smem, st>>>(p);
       return rc;
     };
-    if (p.H > 256 && need <= 32 * kWarpEpt) {
+    if (p.H > kWarpRowMax && need <= 32 * kWarpEpt) {
       if (whole) return rows(integral_constant<Feed, kBulkRows>{});
       if (cut) return rows(integral_constant<Feed, kCutRows>{});
     }
@@ -778,7 +777,7 @@ int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st,
     constexpr integral_constant<Feed, kPlain> plain{};
     constexpr integral_constant<Feed, kBulkRows> bulk{};
     constexpr integral_constant<Feed, kCutRows> cut{};
-    if (p.H <= 256)
+    if (p.H <= kWarpRowMax)
       return go(V, e8, yes{}, plain, integral_constant<int, kRowWarps * 32>{}, integral_constant<int, kGrad ? 3 : 8>{});
     if constexpr (decltype(V)::value * sizeof(T) == 16) {
       if (weights16 && (size_t)p.nin * p.H * sizeof(T) * n.blocks <= 200 * 1024) {

@@ -19,6 +19,9 @@ namespace {
 constexpr int kMaxExperts = 1024, kMaxTopk = 64;
 constexpr int kPlanWarps = 32;
 
+// The placing kernel's counters: a row of them a warp, the scan's sums, the block's counts.
+constexpr size_t plan_smem(int nexp) { return (size_t)(kPlanWarps * nexp + kPlanWarps + nexp) * sizeof(int); }
+
 // A thread's kPer expert ids, -1 for a dropped pair or past the end; warp w of a block has 32 kPer pairs in order.
 template <int kPer>
 struct PlanIds {
@@ -446,7 +449,7 @@ int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64
     if (work_bytes < dp_route_work_bytes(ntok, topk, nexp) || ((uintptr_t)work & 15))
       return set_error(DP_ERR_SHAPE, "%s: work buffer of %zu bytes is too short or misaligned", who, work_bytes);
   }
-  const size_t smem = (size_t)(kPlanWarps * nexp + kPlanWarps + nexp) * sizeof(int);
+  const size_t smem = plan_smem(nexp);
   const cudaStream_t st = (cudaStream_t)stream;
   const int64_t n = ntok * topk;
   int *counts = s.blocks > 8 ? (int *)work : nullptr;
@@ -455,8 +458,8 @@ int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64
                : s.per == 4   ? plan_place_kernel<4, kTable>
                               : plan_place_kernel<8, kTable>;
   if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(place, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+    rc = allow_smem((const void *)place, plan_smem(kMaxExperts), who);
+    if (rc) return rc;
   }
   if (counts) {
     auto count = s.per == 8 ? plan_count_kernel<8> : plan_count_kernel<4>;
