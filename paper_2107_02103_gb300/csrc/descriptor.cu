@@ -13,6 +13,7 @@ namespace dpc {
 namespace {
 
 constexpr int kDescWarps = 4;
+constexpr size_t kMostSmem = 227 * 1024;  // a block's shared memory (none of it static here)
 
 template <typename real>
 __global__ void __launch_bounds__(kDescWarps * 32)
@@ -153,11 +154,10 @@ int descriptor_grad(const io_t<real> *T, const io_t<real> *dD, int64_t nloc, int
   const int64_t blocks = (nloc + kDescWarps - 1) / kDescWarps;
   if (blocks > 2147483647LL) return set_error(DP_ERR_SHAPE, "nloc too large");
   const size_t smem = (size_t)kDescWarps * desc_grad_smem_per_warp<real>(M1, M2) * sizeof(real);
-  if (smem > 227 * 1024) return set_error(DP_ERR_UNSUPPORTED, "M1 = %d, M2 = %d need too much shared memory", M1, M2);
+  if (smem > kMostSmem) return set_error(DP_ERR_UNSUPPORTED, "M1 = %d, M2 = %d need too much shared memory", M1, M2);
   if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(descriptor_grad_kernel<real>,
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "dp_descriptor_contract_grad: %s", cudaGetErrorString(e));
+    const int rc = allow_smem((const void *)descriptor_grad_kernel<real>, kMostSmem, "dp_descriptor_contract_grad");
+    if (rc) return rc;
   }
   descriptor_grad_kernel<real>
       <<<(unsigned)blocks, kDescWarps * 32, smem, (cudaStream_t)stream>>>(T, dD, nloc, M1, M2, dT);
@@ -176,11 +176,10 @@ int descriptor(const io_t<real> *T, int64_t nloc, int M1, int M2, io_t<real> *D,
   const int64_t blocks = (nloc + kDescWarps - 1) / kDescWarps;
   if (blocks > 2147483647LL) return set_error(DP_ERR_SHAPE, "nloc too large");
   const size_t smem = (size_t)kDescWarps * 4 * M1 * sizeof(real);
-  if (smem > 227 * 1024) return set_error(DP_ERR_UNSUPPORTED, "M1 = %d needs too much shared memory", M1);
+  if (smem > kMostSmem) return set_error(DP_ERR_UNSUPPORTED, "M1 = %d needs too much shared memory", M1);
   if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(descriptor_kernel<real>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               (int)smem);
-    if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "dp_descriptor_contract: %s", cudaGetErrorString(e));
+    const int rc = allow_smem((const void *)descriptor_kernel<real>, kMostSmem, "dp_descriptor_contract");
+    if (rc) return rc;
   }
   descriptor_kernel<real><<<(unsigned)blocks, kDescWarps * 32, smem, (cudaStream_t)stream>>>(T, nloc, M1, M2, D);
   return launch_status("dp_descriptor_contract");

@@ -896,8 +896,9 @@ int grad(const real *table, const dp_table_info *info, const io_t<real> *s, cons
     void (*k)(const GradParams<real>) = &grad_moments_kernel<real>;
     const size_t smem = sizeof(MomentGradStage<real>) + (size_t)4 * M1 * sizeof(real);
     if (smem > 48 * 1024) {
-      const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-      if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "dp_tabulate_fusion_grad_moments: %s", cudaGetErrorString(e));
+      constexpr size_t kMost = sizeof(MomentGradStage<real>) + (size_t)4 * DP_MAX_M1 * sizeof(real);
+      const int rc = allow_smem((const void *)k, kMost, "dp_tabulate_fusion_grad_moments");
+      if (rc) return rc;
     }
     k<<<(unsigned)nloc, kMomentWarps * 32, smem, (cudaStream_t)stream>>>(P);
     return launch_status("dp_tabulate_fusion_grad_moments");

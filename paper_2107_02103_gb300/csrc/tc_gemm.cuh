@@ -725,13 +725,15 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const TcGemm P) {
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols));
 }
 
+// The kernel's shared-memory size, set once per device (bit d of set_on: done on device d).
 int set_smem(const char *who) {
-  static std::atomic<bool> done{false};
-  if (done.load(std::memory_order_acquire)) return DP_OK;
-  const cudaError_t e = cudaFuncSetAttribute(gemm_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemTotal);
-  if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
-  done.store(true, std::memory_order_release);
-  return DP_OK;
+  static std::atomic<unsigned long long> set_on{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return set_error(DP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(cudaGetLastError()));
+  if (dev < 64 && (set_on.load(std::memory_order_acquire) >> dev & 1ull)) return DP_OK;
+  const int rc = allow_smem((const void *)gemm_kernel, kSmemTotal, who);
+  if (!rc && dev < 64) set_on.fetch_or(1ull << dev, std::memory_order_acq_rel);
+  return rc;
 }
 
 // split_rows_kernel with the row exponents found in the same kernel: one warp per group of 8 rows and

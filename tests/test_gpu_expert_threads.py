@@ -21,6 +21,12 @@ int plan_loop(int n, plan_fn *f, const int32_t *e, int64_t ntok, int topk, int n
     if ((rc = f(e, ntok, topk, nexp, start, src, pos, NULL, 0, stream))) return rc;
   return 0;
 }
+typedef int desc_fn(const void *, int64_t, int, int, void *, void *);
+int desc_loop(int n, desc_fn *f, const void *T, int64_t nloc, int M1, int M2, void *D, void *stream) {
+  for (int rc; n > 0; --n)
+    if ((rc = f(T, nloc, M1, M2, D, stream))) return rc;
+  return 0;
+}
 typedef int norm_fn(const void *, const void *, const void *, int, const void *, const void *, const void *,
                     const void *, const void *, int64_t, int, int, double, void *, void *, void *, void *);
 int norm_loop(int n, norm_fn *f, const void *x, const void *v, int64_t ntok, int H, void *r2, void *u, void *stats,
@@ -89,3 +95,17 @@ def test_norms_of_short_and_long_rows(loops):
     assert at_once(work) == [0] * len(work)
     for *_, ref, got in cases:
         assert all(torch.equal(a, b) for a, b in zip(ref, got))
+
+
+def test_descriptors_of_short_and_long_rows(loops):
+    dpc = lib()
+    cases = []
+    for M1 in (512, 1000, 600, 1600):
+        T = torch.randn(4, 4, M1, dtype=torch.float64, device="cuda")
+        ref = dpc.dp_descriptor_contract(T, 2)
+        cases.append((T, M1, ref, torch.empty_like(ref)))
+    work = [lambda s, T=T, M1=M1, D=D: loops.desc_loop(20000, dpc._lib.dp_descriptor_contract_f64, ptr(T), ctypes.c_int64(4), M1, 2,
+                                                       ptr(D), s) for T, M1, _, D in cases]
+    assert at_once(work) == [0] * len(work)
+    for _, _, ref, got in cases:
+        assert torch.equal(ref, got)
