@@ -387,6 +387,13 @@ const char *dp_profile_name(int i);
  */
 int dp_tc_wait_timeouts(unsigned int *count);
 
+/*
+ * For tests of the above: in the calls from here on, the wait for a block's
+ * stage n (dp_linear_i8_*: 64 columns of K of a tile) gives up as if it had
+ * run out; n < 0: none does, as at the start.
+ */
+int dp_give_up_at(int n);
+
 
 /*
  * Descriptor (Sec. II): with S_i = T_i^T (M1 x 4) and S_i^< its first M2

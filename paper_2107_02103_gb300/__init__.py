@@ -109,6 +109,7 @@ _SIGS = {
     "dp_profile_end": ([], ctypes.c_int),
     "dp_profile_name": ([ctypes.c_int], ctypes.c_char_p),
     "dp_tc_wait_timeouts": ([ctypes.POINTER(ctypes.c_uint)], ctypes.c_int),
+    "dp_give_up_at": ([ctypes.c_int], ctypes.c_int),
     "dp_tabulate_tc_work_bytes": ([_INFO, _I64, ctypes.c_int, ctypes.c_int, ctypes.c_int], ctypes.c_size_t),
     "dp_tabulate_tc_plan_bytes": ([_INFO, ctypes.c_int, ctypes.c_int, ctypes.c_int], ctypes.c_size_t),
     "dp_tabulate_tc_plan_f64": ([_P, _INFO, ctypes.c_int, ctypes.c_int, ctypes.c_int, _P, ctypes.c_size_t, _PLAN,
@@ -419,6 +420,11 @@ def dp_tc_wait_timeouts() -> int:
     n = ctypes.c_uint(0)
     _check(_lib.dp_tc_wait_timeouts(ctypes.byref(n)))
     return int(n.value)
+
+
+def dp_give_up_at(n: int = -1):
+    """For tests: the stage at which a bounded wait of the expert-block kernels gives up (below 0: none)."""
+    _check(_lib.dp_give_up_at(n))
 
 
 def dp_tabulate_tc_work_bytes(info: dp_table_info, nloc, nnei, ntypes, M1) -> int:

@@ -1,5 +1,7 @@
 // Host-side pieces of the C ABI: error state, table-range rules, argument
 // validation.  No device code.
+#include <atomic>
+#include <climits>
 #include <cstdarg>
 #include <cstdio>
 #include <string>
@@ -27,6 +29,11 @@ int launch_status(const char *what) {
   if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "%s: launch failed: %s", what, cudaGetErrorString(e));
   return DP_OK;
 }
+
+namespace {
+std::atomic<int> g_give_up_at{INT_MAX};
+}
+int give_up_at() { return g_give_up_at.load(std::memory_order_relaxed); }
 
 int allow_smem(const void *k, size_t most, const char *who) {
   const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
@@ -147,6 +154,11 @@ int dp_profile_end(void) {
 }
 
 const char *dp_profile_name(int i) { return i >= 0 && i < dpc::g_prof.n ? dpc::g_prof.name[i] : ""; }
+
+int dp_give_up_at(int n) {
+  dpc::g_give_up_at.store(n < 0 ? INT_MAX : n, std::memory_order_relaxed);
+  return DP_OK;
+}
 
 int dp_tc_wait_timeouts(unsigned int *count) {
   dpc::clear_error();

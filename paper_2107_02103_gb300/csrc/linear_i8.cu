@@ -127,6 +127,7 @@ struct I8Args {
   int rows, K, N, nexp, act;
   void *y;
   unsigned char *image;  // the wide form's weights (linear_i8_tc_kernel)
+  int give_up;           // the stage of a block whose wait gives up (dp_give_up_at)
 };
 
 template <typename T>
@@ -250,8 +251,6 @@ constexpr int kRegs = 96, kEpiRegs = 152, kLoadRegs = 72, kMmaRegs = 32;
 static_assert(2 * kEpiRegs + 2 * kLoadRegs + kMmaRegs <= 5 * kRegs, "register split");
 constexpr uint32_t kRowBytes = kKB * 2, kSBO = 8 * kRowBytes;  // a slice's row; the next 8 rows
 
-__device__ unsigned int g_timeouts;
-
 template <int TN>
 struct Shape {
   static constexpr bool kWide = TN == 256;  // weights come widened, by bulk copies
@@ -271,17 +270,6 @@ struct Shape {
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, const volatile int *stop) {
-  uint32_t done = 0;
-  for (int it = 0; it < (1 << 22) && !done; ++it) {
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(done)
-                 : "r"(bar), "r"(parity)
-                 : "memory");
-    if (!done && (it & 63) == 63 && stop && *stop) return false;
-  }
-  return done != 0;
-}
 __device__ __forceinline__ void arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -333,9 +321,15 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
   uint64_t *full = reinterpret_cast<uint64_t *>(smem + S::kStages * S::kStageBytes), *empty = full + S::kStages;
   uint64_t *acc_full = empty + S::kStages, *acc_empty = acc_full + 2, *done = acc_empty + 2;
   uint32_t *holder = reinterpret_cast<uint32_t *>(done + 1);
-  volatile int *stop = reinterpret_cast<int *>(holder + 1);
+  volatile int *stop = reinterpret_cast<int *>(holder + 1), *issued = stop + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int nct = (p.N + kTM - 1) / kTM, nkb = (p.K + kKB - 1) / kKB;
+  auto wait = [&](uint64_t *bar, uint32_t parity) {  // gives up with any other wait of the block
+    return bounded_wait(smem_u32(bar), parity, [&] { return *stop != 0; });
+  };
+  auto wait_on = [&](uint64_t *bar, uint32_t parity) {  // for what is in flight, come what may
+    return bounded_wait(smem_u32(bar), parity, [] { return false; });
+  };
 
   if (threadIdx.x == 0) {
     auto init = [](uint64_t *b, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(n)); };
@@ -361,6 +355,7 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
   asm volatile("tcgen05.fence::after_thread_sync;");
   const uint32_t tmem = *holder;
   bool ok = true;
+  int next = 0;  // stages copied, or a loader's next one
 
   if (warp >= S::kMmaWarp) {  // in the wide form a warpgroup: one setmaxnreg for all four of its warps
     if constexpr (S::kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
@@ -375,10 +370,11 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
         const uint32_t cols = (uint32_t)(t.r1 - t.r0 + 15) / 16 * 16;
         const uint32_t idesc = (1u << 4) | ((uint32_t)(kTM >> 4) << 24) | ((cols >> 3) << 17);
         if (lane == 0) {
-          for (int kb = 0; kb < nkb && ok; ++kb, ++j) {
+          const int end = min(nkb, p.give_up - j);  // outside the loop: inside it costs 7 % of the narrow forms' time
+          for (int kb = 0; kb < end && ok; ++kb, ++j) {
             const int st = j % S::kStages, buf = unit & 1, slice = kb % (kChunkK / kKB);
-            if (slice == 0 && unit >= 2) ok = wait(smem_u32(acc_empty + buf), ((unit >> 1) - 1) & 1, stop);
-            ok = ok && wait(smem_u32(full + st), (j / S::kStages) & 1, stop);
+            if (slice == 0 && unit >= 2) ok = wait(acc_empty + buf, ((unit >> 1) - 1) & 1);
+            ok = ok && wait(full + st, (j / S::kStages) & 1);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;");
             const uint32_t base = smem_u32(smem) + st * S::kStageBytes;
@@ -397,6 +393,7 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
               ++unit;
             }
           }
+          ok = ok && end == nkb;
         }
         ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
       }
@@ -405,7 +402,6 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
     } else if constexpr (S::kWide) {
       // -------------------------------------------------------------- the weights' copies, by one warp; two are idle
       if (warp == S::kMmaWarp + 1) {
-        int st = 0, phase = 1;
         Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
         for (; ok; t.tile += gridDim.x) {
           seek(p, TN, nct, t);
@@ -414,7 +410,8 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
           const unsigned char *src = p.image + ((int64_t)t.e * nct + t.n0 / kTM) * nkb * S::kStageA;
           if (lane == 0) {
             for (int kb = 0; kb < nkb; ++kb) {
-              ok = wait(smem_u32(empty + st), phase, stop);
+              const int st = next % S::kStages;
+              ok = wait(empty + st, (next / S::kStages & 1) ^ 1);
               if (!ok) break;
               const uint32_t bar = smem_u32(full + st);
               asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)S::kStageA)
@@ -424,15 +421,13 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
                       smem_u32(smem) + st * S::kStageBytes),
                   "l"(src + (int64_t)kb * S::kStageA), "r"((uint32_t)S::kStageA), "r"(bar)
                   : "memory");
-              if (++st == S::kStages) {
-                st = 0;
-                phase ^= 1;
-              }
+              ++next;
             }
           }
           ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
         }
         if (!ok) *stop = 1;
+        if (lane == 0) *issued = next;
       }
     }
   } else if (warp >= kEpiWarps) {
@@ -482,7 +477,7 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
         next_tile();
       }
     };
-    int st = lw % S::kGroups, phase = 1;  // the stage, and the parity of its "empty" barrier (the first round passes)
+    int st = lw % S::kGroups, round = 0;  // the stage, and its turn (the wait of the first passes)
     for (int g = 0; g < st; ++g) advance();
     static_assert(S::kGroups == 2 && S::kStages % S::kGroups == 0, "stages in turn");
     int c = now;
@@ -490,7 +485,7 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
 #pragma unroll
     for (int i = 0; i < kU; ++i) load(i);
     while (c) {
-      ok = __all_sync(0xffffffffu, wait(smem_u32(empty + st), phase, stop));
+      ok = __all_sync(0xffffffffu, wait(empty + st, (round & 1) ^ 1));
       if (!ok) break;
       const uint32_t dst = put + st * S::kStageBytes;
       const int cols = c;
@@ -517,9 +512,10 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
       if (lane == 0) arrive(smem_u32(full + st));
       if ((st += S::kGroups) >= S::kStages) {
         st -= S::kStages;
-        phase ^= 1;
+        ++round;
       }
     }
+    next = round * S::kStages + st;
     if (!ok) *stop = 1;
   } else {
     // ---------------------------------------------------------------- epilogue
@@ -547,7 +543,7 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
         for (int i = 0; i < CW; ++i) sum[i] = 0;
 #pragma unroll 1
         for (int c = chunks;; ++unit) {
-          ok = __all_sync(0xffffffffu, ok && wait(smem_u32(acc_full + (unit & 1)), (unit >> 1) & 1, stop));
+          ok = __all_sync(0xffffffffu, ok && wait(acc_full + (unit & 1), (unit >> 1) & 1));
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;");
           const uint32_t col = trow + (unit & 1) * TN;
@@ -575,7 +571,7 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
           if (lane == 0) arrive(smem_u32(acc_empty + (unit & 1)));
         }
       } else {
-        ok = __all_sync(0xffffffffu, ok && wait(smem_u32(acc_full + (unit & 1)), (unit >> 1) & 1, stop));
+        ok = __all_sync(0xffffffffu, ok && wait(acc_full + (unit & 1), (unit >> 1) & 1));
         asm volatile("tcgen05.fence::after_thread_sync;");
       }
       const float sw = mine ? __ldg(p.sw + (int64_t)t.e * p.N + n) : 0.0f;
@@ -619,8 +615,17 @@ __global__ void __launch_bounds__(Shape<TN>::kThreads, 1) linear_i8_tc_kernel(co
   }
   __syncwarp();
   __syncthreads();
-  ok = wait(smem_u32(done), 0, nullptr) && !*stop;  // no MMA is in flight when the accumulators go
-  if (__syncthreads_and(ok) == 0 && threadIdx.x == 0) atomicAdd(&g_timeouts, 1u);
+  ok = wait_on(done, 0) && !*stop;  // no MMA is in flight when the accumulators go
+  if (!__syncthreads_and(ok)) {
+    if (threadIdx.x == 0) atomicAdd(&g_wait_timeouts, 1u);
+    if constexpr (S::kWide) {  // nor any copy: the loaders' arrivals that its stage lacks, then the copy
+      if (lane == 0 && warp >= kEpiWarps && warp < S::kMmaWarp)
+        for (; next < *issued; next += S::kGroups) arrive(smem_u32(full + next % S::kStages));
+      if (lane == 0 && warp == S::kMmaWarp + 1)
+        for (int i = max(0, next - S::kStages); i < next; ++i) wait_on(full + i % S::kStages, i / S::kStages & 1);
+      __syncthreads();
+    }
+  }
   asm volatile("tcgen05.fence::after_thread_sync;");
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmemCols));
 }
@@ -737,7 +742,7 @@ int linear(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t 
     if (work_bytes < i8::image_bytes(K, N, nexp) || ((uintptr_t)work & 15))
       return set_error(DP_ERR_SHAPE, "%s: work buffer of %zu bytes is too short or misaligned", who, work_bytes);
   }
-  const I8Args p{xq, wq, sx, sw, bias, start, (int)rows, K, N, nexp, act, y, (unsigned char *)work};
+  const I8Args p{xq, wq, sx, sw, bias, start, (int)rows, K, N, nexp, act, y, (unsigned char *)work, give_up_at()};
   const cudaStream_t st = (cudaStream_t)stream;
   const int64_t pieces = start ? (nexp + 1 < rows ? nexp + 1 : rows) : 0;  // a tile more for each expert's remainder
   auto tiles = [&](int R) { return (rows + R - 1) / R + pieces; };
@@ -758,15 +763,7 @@ int linear(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t 
 
 }  // namespace
 
-int take_wait_timeouts_linear_i8(unsigned int *count) {
-  unsigned int v = 0, zero = 0;
-  cudaError_t e = cudaDeviceSynchronize();
-  if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&v, i8::g_timeouts, sizeof v);
-  if (e == cudaSuccess) e = cudaMemcpyToSymbol(i8::g_timeouts, &zero, sizeof zero);
-  if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "dp_tc_wait_timeouts: %s", cudaGetErrorString(e));
-  *count += v;
-  return DP_OK;
-}
+int take_wait_timeouts_linear_i8(unsigned int *count) { return take_unit_timeouts(count); }
 
 }  // namespace dpc
 

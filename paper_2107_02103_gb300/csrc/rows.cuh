@@ -94,6 +94,35 @@ __device__ __forceinline__ Pack<T, 16 / (int)sizeof(T)> load_any(const T *p, con
   return out;
 }
 
+// Waits on an mbarrier give up after kWaitPolls tries or when `stop`, looked at now and then, says so.  A block whose
+// wait gave up waits once more for its own copies in flight, leaves NaN and adds one to g_wait_timeouts.
+constexpr int kWaitPolls = 1 << 22;
+__device__ unsigned int g_wait_timeouts;  // of this translation unit's kernels
+
+template <typename Stop>
+__device__ __forceinline__ bool bounded_wait(uint32_t bar, uint32_t parity, Stop stop) {
+  uint32_t done = 0;
+  for (int it = 0; it < kWaitPolls && !done; ++it) {
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(done)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    if (!done && (it & 63) == 63 && stop()) return false;
+  }
+  return done != 0;
+}
+
+// The count, read after a device synchronisation, then cleared.
+[[maybe_unused]] int take_unit_timeouts(unsigned int *count) {
+  unsigned int v = 0, zero = 0;
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&v, g_wait_timeouts, sizeof v);
+  if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_wait_timeouts, &zero, sizeof zero);
+  if (e != cudaSuccess) return set_error(DP_ERR_CUDA, "dp_tc_wait_timeouts: %s", cudaGetErrorString(e));
+  *count += v;
+  return DP_OK;
+}
+
 // The widest pack (in elements) that rows of H elements at these addresses allow: 16 bytes down to one element.
 template <typename T, typename... P>
 int pack_width(int64_t H, P... ptrs) {
