@@ -378,9 +378,10 @@ const char *dp_profile_name(int i);
 
 /*
  * Diagnostic (not part of the paper's method): every wait of the tensor-core
- * GEMM kernels (dp_tabulate_fusion_*_tc_f64, dp_fitting_*_tc_f64, dp_linear_i8_*) on an
- * mbarrier is bounded; a CTA whose wait gives up writes NaN outputs, reads
- * no accumulator and counts one timeout on the device.  This call waits for
+ * GEMM kernels (dp_tabulate_fusion_*_tc_f64, dp_fitting_*_tc_f64, dp_linear_i8_*)
+ * and of the norms (dp_norm_gate_*) on an mbarrier is bounded; a CTA (or a warp
+ * with rows of its own) whose wait gives up writes NaN outputs, reads no
+ * accumulator and counts one timeout on the device.  This call waits for
  * the device to finish (cudaDeviceSynchronize), writes the count since the
  * last call to *count (host) and clears it.  0 in normal operation.
  * Errors: DP_ERR_NULL, DP_ERR_CUDA.
@@ -389,8 +390,9 @@ int dp_tc_wait_timeouts(unsigned int *count);
 
 /*
  * For tests of the above: in the calls from here on, the wait for a block's
- * stage n (dp_linear_i8_*: 64 columns of K of a tile) gives up as if it had
- * run out; n < 0: none does, as at the start.
+ * stage n (dp_linear_i8_*: 64 columns of K of a tile) or for the rows from n on
+ * (dp_norm_gate_*, where rows come by bulk copies) gives up as if it had run
+ * out; n < 0: none does, as at the start.
  */
 int dp_give_up_at(int n);
 

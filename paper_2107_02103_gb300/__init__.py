@@ -416,14 +416,14 @@ def dp_profile_end():
 
 
 def dp_tc_wait_timeouts() -> int:
-    """Tensor-core GEMM waits that gave up since the last call (synchronises the device); 0 normally."""
+    """Waits of the GEMM and norm kernels that gave up since the last call (synchronises the device); 0 normally."""
     n = ctypes.c_uint(0)
     _check(_lib.dp_tc_wait_timeouts(ctypes.byref(n)))
     return int(n.value)
 
 
 def dp_give_up_at(n: int = -1):
-    """For tests: the stage at which a bounded wait of the expert-block kernels gives up (below 0: none)."""
+    """For tests: the stage, or the first row, whose wait in the expert-block kernels gives up (below 0: none)."""
     _check(_lib.dp_give_up_at(n))
 
 

@@ -64,16 +64,22 @@ __device__ __forceinline__ A inv_sqrt(A x) {
   else return rsqrtf(x);
 }
 
-// Means m and inverse deviations s of R rows held as v[R][EPT] per thread; v becomes v - m.
+template <typename A>
+__device__ __forceinline__ A nan_of() {
+  return A(__int_as_float(0x7fc00000));
+}
+
+// Means m and inverse deviations s of R rows held as v[R][EPT] per thread; v becomes v - m.  A row that is not ok in
+// any of its threads gets s (and a layer norm's m) NaN in all of them.
 template <int R, int EPT, bool kWarpRow, bool kLayer, typename Map, typename A, typename Buf>
-__device__ __forceinline__ void row_stats(const Map &map, A (&v)[R][EPT], A inv, A eps, A (&m)[R], A (&s)[R], Buf &buf,
-                                          int &phase) {
+__device__ __forceinline__ void row_stats(const Map &map, A (&v)[R][EPT], const bool (&ok)[R], A inv, A eps, A (&m)[R],
+                                          A (&s)[R], Buf &buf, int &phase) {
   A sum[R];
 #pragma unroll
   for (int k = 0; k < R; ++k) m[k] = A(0);
   if constexpr (kLayer) {
 #pragma unroll
-    for (int k = 0; k < R; ++k) sum[k] = map.total([&](int i) { return v[k][i]; });
+    for (int k = 0; k < R; ++k) sum[k] = ok[k] ? map.total([&](int i) { return v[k][i]; }) : nan_of<A>();
     row_sum<R, kWarpRow>(sum, buf, phase);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
@@ -83,7 +89,7 @@ __device__ __forceinline__ void row_stats(const Map &map, A (&v)[R][EPT], A inv,
     }
   }
 #pragma unroll
-  for (int k = 0; k < R; ++k) sum[k] = map.total([&](int i) { return v[k][i] * v[k][i]; });
+  for (int k = 0; k < R; ++k) sum[k] = ok[k] || kLayer ? map.total([&](int i) { return v[k][i] * v[k][i]; }) : nan_of<A>();
   row_sum<R, kWarpRow>(sum, buf, phase);
 #pragma unroll
   for (int k = 0; k < R; ++k) s[k] = inv_sqrt(fma(sum[k], inv, eps));
@@ -175,6 +181,7 @@ struct NormArgs {
   const acc_t<T> *a, *w1, *b1, *w2, *b2;
   int64_t ntok;
   int H, stages;  // stages: rows a block of the bulk form has in shared memory
+  int64_t fetched;  // rows that bulk copies fetch: ntok, or fewer for a test of waits that give up (dp_give_up_at)
   acc_t<T> eps;
   T *r2, *u;
   acc_t<T> *stats;  // [ntok][4]: m1, s1, m2, s2
@@ -185,7 +192,14 @@ struct NormArgs {
 // How rows reach a block: plain loads, or whole rows copied ahead into shared memory in bulk, `stages` rows deep
 // (kCut: the aligned words under the rows).  A stage may be refilled once every thread has read it, which the first
 // block sum of a row implies.
+//
+// Waits are bounded.  A thread whose wait gives up puts NaN into the row's first sum, which all threads of the block
+// see, and raises `lost`, which tells that NaN from one of the data.  The block then leaves its loop, before it fetches
+// anything more, waits once more for what is in flight, and fills this row and its later ones with NaN.
 enum Feed { kPlain, kBulkRows, kCutRows };
+constexpr int kMaxStages = 4;
+constexpr unsigned kNoRow = 0xffffffffu;
+constexpr int kRowPolls = 1 << 16;  // of a wait for a row: 0.3 s
 
 template <typename T, int V, int EPT, Feed kFeed>
 struct RowFeed {
@@ -195,16 +209,16 @@ struct RowFeed {
   int64_t t, step;  // the row at hand, and to the next one
   unsigned char *smem;
   uint64_t *bars;
+  volatile unsigned *lost;
   int st = 0, phase = 0;
 
   __device__ __forceinline__ uint32_t row_bytes() const {  // of a place in a stage
     return kCut ? cut_bytes<T>(p.H) : (uint32_t)p.H * sizeof(T);
   }
   __device__ __forceinline__ uint32_t bar(int s) const { return (uint32_t)__cvta_generic_to_shared(bars + s); }
-  // Lane 0 of each warp copies its arrays of the row, counted on the stage's barrier (one warp copying all of them
-  // kept the others waiting).
+  // Called by lane 0 of each warp, which copies its arrays of the row, counted on the stage's barrier (one warp copying
+  // all of them kept the others waiting).
   __device__ __forceinline__ void fetch(int64_t row, int s) const {
-    if (threadIdx.x & 31) return;
     const uint32_t place = row_bytes(), dst = (uint32_t)__cvta_generic_to_shared(smem) + s * p.nin * place;
     uint32_t bytes = place;
     if constexpr (kCut)  // the last row's last word may reach past the array: load() takes what is left out here
@@ -220,29 +234,31 @@ struct RowFeed {
   __device__ __forceinline__ void begin() {
     if constexpr (kBulk) {
       if (threadIdx.x == 0) {
+        *lost = kNoRow;
         for (int s = 0; s < p.stages; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar(s)), "r"(p.nin));
         asm volatile("fence.mbarrier_init.release.cluster;");
       }
       __syncthreads();
       for (int s = 0; s < p.stages; ++s)
-        if (t + s * step < p.ntok) fetch(t + s * step, s);
+        if ((threadIdx.x & 31) == 0 && t + s * step < p.fetched) fetch(t + s * step, s);
     }
   }
   // The stage k rows on, and the parity of its barrier.
   __device__ __forceinline__ int stage(int k) const { return st + k < p.stages ? st + k : st + k - p.stages; }
-  __device__ __forceinline__ bool arrived(int k = 0) const {  // bounded: false leaves NaN rows behind
+  __device__ __forceinline__ uint32_t parity(int k) const { return phase ^ (st + k >= p.stages); }
+  __device__ __forceinline__ bool arrived(int k = 0) const {
     if constexpr (kBulk) {
-      const int s = stage(k), parity = phase ^ (st + k >= p.stages);
-      uint32_t done = 0;
-      for (int it = 0; it < (1 << 22) && !done; ++it)
-        asm volatile(
-            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-            : "=r"(done)
-            : "r"(bar(s)), "r"((uint32_t)parity)
-            : "memory");
-      return done != 0;
+      const bool ok = bounded_wait<kRowPolls>(bar(stage(k)), parity(k), [] { return false; });
+      if (!ok) *lost = (unsigned)t;
+      return ok;
     }
     return true;
+  }
+  // Whether a wait of the rows at hand gave up in any thread of the block; first: their first sum, or what follows from it.
+  template <typename A>
+  __device__ __forceinline__ bool given_up(A first) const {
+    if constexpr (kBulk) return first != first && *lost <= (unsigned)t;
+    return false;
   }
   template <typename A>
   __device__ __forceinline__ void load(int i, A (&v)[EPT], int k = 0) const {
@@ -259,9 +275,13 @@ struct RowFeed {
       }
     }
   }
-  __device__ __forceinline__ void read(int k = 0) const {  // after a block barrier that follows the row's loads
+  template <int kRows>
+  __device__ __forceinline__ void read() const {  // after a block barrier that follows the rows' loads
     if constexpr (kBulk)
-      if (t + (k + p.stages) * step < p.ntok) fetch(t + (k + p.stages) * step, stage(k));
+      if ((threadIdx.x & 31) == 0 && t + p.stages * step < p.fetched)
+#pragma unroll
+        for (int k = 0; k < kRows; ++k)
+          if (t + (k + p.stages) * step < p.fetched) fetch(t + (k + p.stages) * step, stage(k));
   }
   __device__ __forceinline__ void next(int rows = 1) {
     t += rows * step;
@@ -273,7 +293,6 @@ struct RowFeed {
   }
 };
 
-constexpr int kMaxStages = 4;
 constexpr size_t kBulkRoom = 200 * 1024;  // shared memory that an SM's blocks of a bulk form divide
 
 // Cut rows' weights into shared memory, beside the packs of a row that begins at `off`: vector i at out + i * room.
@@ -290,6 +309,33 @@ __device__ __forceinline__ void move_weights(const A *const (&from)[5], int off,
   }
 }
 
+// The block's threads fill n elements with NaN.
+template <typename T>
+__device__ __forceinline__ void fill_nan(T *to, int n) {
+#pragma unroll 1
+  for (int i = threadIdx.x; i < n; i += blockDim.x) to[i] = from_acc<T>(nan_of<acc_t<T>>());
+}
+
+// A block that gave up at its row `first` (RowFeed): waits once more for the rows in flight, fills this row and its later
+// ones of a, b [ntok][H] and c [ntok][nc] (or NULL) with NaN, and is counted.  Out of line, and with nothing from the
+// loop over the rows: what stays alive for it there costs registers (backward of 65,536 x 1600 bf16: 423 us against 396).
+template <typename T, typename C>
+__device__ __noinline__ void leave_rows(uint64_t *bars, int stages, unsigned first, int64_t fetched, int64_t ntok, int H,
+                                        T *a, T *b, C *c, int nc) {
+  const unsigned step = gridDim.x, at = (first - blockIdx.x) / step;
+  if (threadIdx.x == 0) {
+    atomicAdd(&g_wait_timeouts, 1u);
+    for (unsigned i = at; i < at + stages && blockIdx.x + (int64_t)i * step < fetched; ++i)
+      bounded_wait((uint32_t)__cvta_generic_to_shared(bars + i % stages), i / stages & 1, [] { return false; });
+  }
+  for (int64_t t = first; t < ntok; t += step) {
+    fill_nan(a + t * H, H);
+    fill_nan(b + t * H, H);
+    if (c) fill_nan(c + t * nc, nc);
+  }
+  __syncthreads();  // nobody's copies into shared memory outlive the block, nobody's stores follow these
+}
+
 // Rows a block of the forward works on at once: two of 16-bit elements by bulk copies (the waits of their block sums
 // overlap, and the weights are read once for both: layer norm of 65,536 x 1600 bf16 in 241 us against 270), else one.
 template <typename T, bool kBulk, int kThreads>
@@ -302,6 +348,7 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
   constexpr int R = kFwdRows<T, kBulk, kThreads>;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ uint64_t bars[kMaxStages];
+  __shared__ unsigned lost;
   __shared__ SumBuf<A, kThreads / 32> buf;
   int phase = 0;
   for (int i = threadIdx.x; i < (int)(sizeof buf / sizeof(A)); i += blockDim.x) (&buf.v[0][0][0])[i] = A(0);
@@ -311,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
                                     kWarpRow ? 32 : (int)blockDim.x, kCut ? (off + p.H + V - 1) / V : p.H / V, off, p.H};
   RowFeed<T, V, EPT, kFeed> feed{
       p, map, kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : (int64_t)blockIdx.x,
-      kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : (int64_t)gridDim.x, smem, bars};
+      kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : (int64_t)gridDim.x, smem, bars, &lost};
   const A inv = A(1) / A(p.H);
   feed.begin();
   const A *wa = p.a, *w1 = p.w1, *w2 = p.w2, *b1 = p.b1, *b2 = p.b2;
@@ -347,12 +394,9 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
       feed.load(1, r[k], at);
       if (p.nin > 2) feed.load(2, g[k], at);
     }
-    row_stats<R, EPT, kWarpRow, kLayer>(map, f, inv, p.eps, m1, s1, buf, phase);
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      feed.read(k);
-      if (!ok[k]) s1[k] = A(__int_as_float(0x7fc00000));
-    }
+    row_stats<R, EPT, kWarpRow, kLayer>(map, f, ok, inv, p.eps, m1, s1, buf, phase);
+    if (feed.given_up(kLayer ? m1[0] + m1[R - 1] : s1[0] + s1[R - 1])) break;
+    feed.template read<R>();
     map.template weights<kBulk>(w1, w);
     if constexpr (kLayer) map.template weights<kBulk>(b1, b);
 #pragma unroll
@@ -374,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
       for (int i = 0; i < EPT; ++i) r[k][i] = fma(w[i], f[k][i], r[k][i]);
       if (have[k]) map.store(p.r2 + (feed.t + k * feed.step) * p.H, r[k]);
     }
-    row_stats<R, EPT, kWarpRow, kLayer>(map, r, inv, p.eps, m2, s2, buf, phase);
+    row_stats<R, EPT, kWarpRow, kLayer>(map, r, ok, inv, p.eps, m2, s2, buf, phase);
     map.template weights<kBulk>(w2, w);
     if constexpr (kLayer) map.template weights<kBulk>(b2, b);
 #pragma unroll
@@ -393,6 +437,8 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
       }
     }
   }
+  if constexpr (kBulk)
+    if (lost != kNoRow) leave_rows<T>(bars, p.stages, lost, p.fetched, p.ntok, p.H, p.r2, p.u, p.stats, 4);
 }
 
 // The forward for 16-bit rows of 257 to 512 elements: a warp a row, the row's one array in registers (f, then p, then
@@ -400,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
 // instructions that it costs a block, whose sums' shuffles and barriers every warp repeats.  Each warp has two rows in
 // shared memory, the next on its way while it works on one.  65,536 x 512 bf16 layer norm: 59 us against 77 by blocks;
 // longer rows leave too few warps on an SM (1024: 161 against 140).
-constexpr int kWarpStages = 2, kWarpEpt = 16;
+constexpr int kWarpStages = 2, kWarpEpt = 16;  // the stages' order below holds for two
 
 // Warps a block: two for whole rows; cut rows share the block's weights, one block an SM.
 template <Feed kFeed>
@@ -453,15 +499,11 @@ __global__ void __launch_bounds__(kRowWarpsMost<kFeed> * 32, kRowBlocks<kFeed>)
   for (int s = 0; s < kWarpStages; ++s) fetch(t + s * step, s);
   T gate_next = p.gate && t < p.ntok ? p.gate[t] : T(0.0f);
   int st = 0, parity = 0;
+  auto never = [] { return false; };
   for (; t < p.ntok; t += step) {
     const A gate = p.gate ? to_acc(gate_next) : A(1);
     if (p.gate && t + step < p.ntok) gate_next = p.gate[t + step];
-    uint32_t done = 0;
-    for (int it = 0; it < (1 << 22) && !done; ++it)
-      asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-                   : "=r"(done)
-                   : "r"(bar(st)), "r"((uint32_t)parity)
-                   : "memory");
+    const bool ok[1] = {t < p.fetched && bounded_wait<kRowPolls>(bar(st), parity, never)};
     const unsigned char *row = mine + (size_t)st * p.nin * place;
     auto pack = [&](int array, int i, A (&x)[V]) {
       const Pack<T, V> q = load_pack<T, V>(reinterpret_cast<const T *>(row + array * place) + map.at(i));
@@ -484,8 +526,8 @@ __global__ void __launch_bounds__(kRowWarpsMost<kFeed> * 32, kRowBlocks<kFeed>)
 #pragma unroll
       for (int l = 0; l < V; ++l) v[0][i * V + l] = x[l];
     }
-    row_stats<1, EPT, true, kLayer>(map, v, inv, p.eps, m1, s1, unused, phase);
-    if (!done) s1[0] = A(__int_as_float(0x7fc00000));
+    row_stats<1, EPT, true, kLayer>(map, v, ok, inv, p.eps, m1, s1, unused, phase);
+    if (s1[0] != s1[0] && __any_sync(0xffffffffu, !ok[0])) break;  // the warp gives up
 #pragma unroll
     for (int i = 0; i < map.kN; ++i) {
       A w[V], b[V], r[V], a[V];
@@ -512,7 +554,7 @@ __global__ void __launch_bounds__(kRowWarpsMost<kFeed> * 32, kRowBlocks<kFeed>)
       parity ^= 1;
     }
     map.store(p.r2 + t * p.H, v[0]);
-    row_stats<1, EPT, true, kLayer>(map, v, inv, p.eps, m2, s2, unused, phase);
+    row_stats<1, EPT, true, kLayer>(map, v, ok, inv, p.eps, m2, s2, unused, phase);
 #pragma unroll
     for (int i = 0; i < map.kN; ++i) {
       A w[V], b[V];
@@ -530,6 +572,19 @@ __global__ void __launch_bounds__(kRowWarpsMost<kFeed> * 32, kRowBlocks<kFeed>)
       out[0] = m1[0], out[1] = s1[0], out[2] = m2[0], out[3] = s2[0];
     }
   }
+  if (t < p.ntok) {  // given up: once what is in flight has landed, NaN into this row and its later ones
+    if (lane == 0) atomicAdd(&g_wait_timeouts, 1u);
+    bounded_wait(bar(st), parity, never);
+    if (t + step < p.ntok) bounded_wait(bar(st ^ 1), parity ^ st, never);
+    A none[EPT];
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) none[i] = nan_of<A>();
+    for (; t < p.ntok; t += step) {
+      map.store(p.r2 + t * p.H, none);
+      map.store(p.u + t * p.H, none);
+      if (lane < 4) p.stats[t * 4 + lane] = none[0];
+    }
+  }
 }
 
 // A thread keeps its columns' sums over the rows of its block (or warp) in registers.
@@ -539,6 +594,7 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
   constexpr bool kBulk = kFeed != kPlain, kCut = kFeed == kCutRows;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ uint64_t bars[kMaxStages];
+  __shared__ unsigned lost;
   __shared__ SumBuf<A, kThreads / 32> buf;
   int phase = 0;
   for (int i = threadIdx.x; i < (int)(sizeof buf / sizeof(A)); i += blockDim.x) (&buf.v[0][0][0])[i] = A(0);
@@ -548,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
                                     kWarpRow ? 32 : (int)blockDim.x, kCut ? (off + p.H + V - 1) / V : p.H / V, off, p.H};
   RowFeed<T, V, EPT, kFeed> feed{
       p, map, kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : (int64_t)blockIdx.x,
-      kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : (int64_t)gridDim.x, smem, bars};
+      kWarpRow ? (int64_t)gridDim.x * (blockDim.x >> 5) : (int64_t)gridDim.x, smem, bars, &lost};
   A sa[EPT], sw1[EPT], sw2[EPT], sb1[EPT], sb2[EPT];
 #pragma unroll
   for (int i = 0; i < EPT; ++i) sa[i] = sw1[i] = sw2[i] = sb1[i] = sb2[i] = A(0);
@@ -574,10 +630,9 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
   peek(feed.t);
   for (; feed.t < p.ntok; feed.next()) {
     const int64_t t = feed.t;
-    const A m1 = st_next[0], m2 = st_next[2], s2 = st_next[3], gt = p.gate ? to_acc(gate_next) : A(1);
-    A s1 = st_next[1];
+    const A m1 = st_next[0], s1 = st_next[1], m2 = st_next[2], s2 = st_next[3], gt = p.gate ? to_acc(gate_next) : A(1);
     peek(t + feed.step);
-    if (!feed.arrived()) s1 = A(__int_as_float(0x7fc00000));
+    const bool ok = feed.arrived();
     A f[EPT], n2[EPT], du[EPT], dr[EPT], g[EPT], w[EPT];
     feed.load(0, n2);
     feed.load(1, du);
@@ -598,10 +653,11 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
     }
     constexpr int kOne = kLayer ? 2 : 1;
     A one[kOne];
-    one[0] = map.total([&](int i) { return du[i] * n2[i]; });
+    one[0] = ok ? map.total([&](int i) { return du[i] * n2[i]; }) : nan_of<A>();
     if constexpr (kLayer) one[1] = map.total([&](int i) { return du[i]; });
     row_sum<kOne, kWarpRow>(one, buf, phase);
-    feed.read();
+    if (feed.given_up(one[0])) break;
+    feed.template read<1>();
     A along = one[0] * inv, mean = kLayer ? one[kOne - 1] * inv : A(0);
 #pragma unroll
     for (int i = 0; i < EPT; ++i) dr[i] = fma(s2, du[i] - (kLayer ? fma(n2[i], along, mean) : n2[i] * along), dr[i]);
@@ -666,6 +722,11 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_grad_kernel(const N
         A *o = out + map.at(i / V) + i % V - off;
         o[0] = sa[i], o[p.H] = sw1[i], o[2 * p.H] = sw2[i];
         if constexpr (kLayer) o[3 * p.H] = sb1[i], o[4 * p.H] = sb2[i];
+      }
+    if constexpr (kBulk)
+      if (lost != kNoRow) {
+        leave_rows<T>(bars, p.stages, lost, p.fetched, p.ntok, p.H, p.dr, p.df, p.dgate, each ? p.H : 1);
+        fill_nan(out, kVec * p.H);
       }
   }
 }

@@ -22,7 +22,7 @@ int norm_fwd(const T *r, const T *f, const T *gate, int gate_kind, const acc_t<T
   p.in[0] = f, p.in[1] = r, p.in[2] = full ? gate : nullptr, p.nin = full ? 3 : 2;
   p.gate = gate_kind == DP_GATE_TOKEN ? gate : nullptr;
   p.a = a, p.w1 = w1, p.w2 = w2, p.b1 = layer ? b1 : nullptr, p.b2 = layer ? b2 : nullptr;
-  p.ntok = ntok, p.H = H, p.eps = (acc_t<T>)eps;
+  p.fetched = ntok < give_up_at() ? ntok : give_up_at(), p.ntok = ntok, p.H = H, p.eps = (acc_t<T>)eps;
   p.r2 = r2, p.u = u, p.stats = stats;
   const int v = pack_width<T>(H, r, f, p.in[2], r2, u);
   if (!v) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
@@ -34,6 +34,9 @@ int norm_fwd(const T *r, const T *f, const T *gate, int gate_kind, const acc_t<T
 }
 
 }  // namespace
+
+int take_wait_timeouts_norm_fwd(unsigned int *count) { return take_unit_timeouts(count); }
+
 }  // namespace dpc
 
 extern "C" {

@@ -26,7 +26,7 @@ int norm_grad(const T *r2, const T *f, const T *gate, int gate_kind, const acc_t
   p.in[0] = r2, p.in[1] = du, p.in[2] = dr2, p.in[3] = f, p.in[4] = full ? gate : nullptr, p.nin = full ? 5 : 4;
   p.gate = gate_kind == DP_GATE_TOKEN ? gate : nullptr;
   p.a = a, p.w1 = w1, p.w2 = w2, p.b1 = layer ? b1 : nullptr;
-  p.ntok = ntok, p.H = H;
+  p.fetched = ntok < give_up_at() ? ntok : give_up_at(), p.ntok = ntok, p.H = H;
   p.stats = const_cast<acc_t<T> *>(stats), p.dr = dr, p.df = df;
   p.dgate = gate_kind == DP_GATE_NONE ? nullptr : dgate;
   p.part = (acc_t<T> *)work;
@@ -44,6 +44,9 @@ int norm_grad(const T *r2, const T *f, const T *gate, int gate_kind, const acc_t
 }
 
 }  // namespace
+
+int take_wait_timeouts_norm_grad(unsigned int *count) { return take_unit_timeouts(count); }
+
 }  // namespace dpc
 
 extern "C" {

@@ -94,15 +94,15 @@ __device__ __forceinline__ Pack<T, 16 / (int)sizeof(T)> load_any(const T *p, con
   return out;
 }
 
-// Waits on an mbarrier give up after kWaitPolls tries or when `stop`, looked at now and then, says so.  A block whose
+// Waits on an mbarrier give up after kPolls tries or when `stop`, looked at now and then, says so.  A block whose
 // wait gave up waits once more for its own copies in flight, leaves NaN and adds one to g_wait_timeouts.
-constexpr int kWaitPolls = 1 << 22;
+constexpr int kWaitPolls = 1 << 18;  // a try takes up to 4.5 us: about a second
 __device__ unsigned int g_wait_timeouts;  // of this translation unit's kernels
 
-template <typename Stop>
+template <int kPolls = kWaitPolls, typename Stop>
 __device__ __forceinline__ bool bounded_wait(uint32_t bar, uint32_t parity, Stop stop) {
   uint32_t done = 0;
-  for (int it = 0; it < kWaitPolls && !done; ++it) {
+  for (int it = 0; it < kPolls && !done; ++it) {
     asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
                  : "=r"(done)
                  : "r"(bar), "r"(parity)
