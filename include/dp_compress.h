@@ -714,7 +714,8 @@ int dp_tensor_head_grad_f32(const float *T, const float *a, const float *dA, int
  *          pairs, work may be NULL)
  * Errors: DP_ERR_NULL, DP_ERR_SHAPE (ntok < 0, topk outside [1, 64], 2^31 or
  * more pairs, nexp < 1, a short or misaligned work buffer),
- * DP_ERR_UNSUPPORTED (nexp above 1024), DP_ERR_CUDA.
+ * DP_ERR_UNSUPPORTED (nexp above 1024), DP_ERR_CUDA.  In this call and those
+ * below DP_ERR_SHAPE also says that an array is not aligned to its elements.
  */
 size_t dp_route_work_bytes(int64_t ntok, int topk, int nexp);
 int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64_t *start, int32_t *src, int32_t *pos,
@@ -733,8 +734,7 @@ int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64
  *   x, y, dy [ntok][H]; xs, z, dz [ntok topk][H]; dw [ntok][topk]
  * Every sum has a fixed order; entries of src and pos outside their range count
  * as dropped.  ntok == 0 reads no device pointer.  Errors: DP_ERR_NULL,
- * DP_ERR_SHAPE (as the plan; H outside [1, 2^20]; an array not aligned to its
- * elements), DP_ERR_CUDA.
+ * DP_ERR_SHAPE (as the plan; H outside [1, 2^20]), DP_ERR_CUDA.
  */
 int dp_route_gather_f64(const double *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int H,
                         double *xs, void *stream);

@@ -693,7 +693,7 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
   if (ntok == 0) return DP_OK;
   if (!x || !xq || !sx) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if ((uintptr_t)xq & 15) return set_error(DP_ERR_SHAPE, "%s: xq is not 16-byte aligned", who);
-  if ((uintptr_t)x & (sizeof(T) - 1)) return set_error(DP_ERR_SHAPE, "%s: x is not aligned to its elements", who);
+  if (!at_elements(x, sx, src, pos)) return misaligned(who);
   const int ldq = (K + 15) / 16 * 16, packs = ldq / (16 / (int)sizeof(T));
   const bool whole = (((uintptr_t)x | (uintptr_t)(K * sizeof(T))) & 15) == 0;
   auto go = [&](auto G) {
@@ -736,6 +736,7 @@ int linear(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t 
   if (rows == 0) return DP_OK;
   if (!xq || !sx || !wq || !sw || !y) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (((uintptr_t)xq | (uintptr_t)wq) & 15) return set_error(DP_ERR_SHAPE, "%s: xq or wq is not 16-byte aligned", who);
+  if (!at_elements(y, sx, sw, bias, start)) return misaligned(who);
   const I8Form form = form_of(rows, K, N, nexp);
   if (form == kWideTiles) {
     if (!work) return set_error(DP_ERR_NULL, "%s: work is NULL", who);

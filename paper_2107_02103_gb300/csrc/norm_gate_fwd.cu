@@ -25,7 +25,7 @@ int norm_fwd(const T *r, const T *f, const T *gate, int gate_kind, const acc_t<T
   p.fetched = ntok < give_up_at() ? ntok : give_up_at(), p.ntok = ntok, p.H = H, p.eps = (acc_t<T>)eps;
   p.r2 = r2, p.u = u, p.stats = stats;
   const int v = pack_width<T>(H, r, f, p.in[2], r2, u);
-  if (!v) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
+  if (!v || !at_elements(p.gate, a, w1, w2, p.b1, p.b2, stats)) return misaligned(who);
   const bool w16 = aligned16(a, w1, w2, p.b1, p.b2);
   const bool bases = aligned16(r, f, p.in[2], r2, u);
   const int lrc = layer ? launch<T, false, true>(p, v, w16, bases, (cudaStream_t)stream, who)

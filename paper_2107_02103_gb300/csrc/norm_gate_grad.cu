@@ -31,7 +31,9 @@ int norm_grad(const T *r2, const T *f, const T *gate, int gate_kind, const acc_t
   p.dgate = gate_kind == DP_GATE_NONE ? nullptr : dgate;
   p.part = (acc_t<T> *)work;
   const int v = pack_width<T>(H, r2, f, p.in[4], dr2, du, dr, df, full ? dgate : nullptr);
-  if (!v) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
+  if (!v || !at_elements(p.gate, p.dgate, a, w1, w2, p.b1, stats, da, dw1, dw2) ||
+      (layer && !at_elements(db1, db2)))
+    return misaligned(who);
   const cudaStream_t st = (cudaStream_t)stream;
   const bool w16 = aligned16(a, w1, w2, p.b1);
   const bool bases = aligned16(r2, f, p.in[4], dr2, du, dr, df, full ? dgate : nullptr);

@@ -340,10 +340,6 @@ template <typename T>
 bool whole_rows(int H, const void *a, const void *b, const void *c = nullptr) {
   return ((((uintptr_t)a | (uintptr_t)b | (uintptr_t)c) | (uintptr_t)(H * sizeof(T))) & 15) == 0;
 }
-template <typename T>
-bool elements_aligned(const void *a, const void *b, const void *c = nullptr) {
-  return (((uintptr_t)a | (uintptr_t)b | (uintptr_t)c) & (sizeof(T) - 1)) == 0;
-}
 // The grid of a move over rows of np packs; false where it is too large.
 bool move_grid(int64_t ntok, int np, bool flat, int part, dim3 *grid) {
   const int64_t x = flat ? (ntok * np + kMoveThreads - 1) / kMoveThreads : (ntok + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
@@ -359,7 +355,7 @@ int gather(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok, int
   int rc = row_check(ntok, topk, H, who);
   if (rc || ntok == 0) return rc;
   if (!x || !src || !pos || !xs) return set_error(DP_ERR_NULL, "%s: NULL array", who);
-  if (!elements_aligned<T>(x, xs)) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
+  if (!at_elements(x, xs, src, pos)) return misaligned(who);
   constexpr int V = 16 / (int)sizeof(T);
   const bool whole = whole_rows<T>(H, x, xs);
   const int np = whole ? H / V : H;
@@ -379,7 +375,7 @@ int combine(const T *z, const int32_t *pos, const acc_t<T> *w, int64_t ntok, int
   int rc = row_check(ntok, topk, H, who);
   if (rc || ntok == 0) return rc;
   if (!z || !pos || !y) return set_error(DP_ERR_NULL, "%s: NULL array", who);
-  if (!elements_aligned<T>(z, y)) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
+  if (!at_elements(z, y, pos, w)) return misaligned(who);
   constexpr int V = 16 / (int)sizeof(T);
   const bool whole = whole_rows<T>(H, z, y);
   const int np = whole ? H / V : H;
@@ -400,7 +396,7 @@ int combine_grad(const T *z, const int32_t *src, const int32_t *pos, const acc_t
   if (rc || ntok == 0) return rc;
   if (!src || !pos || !dy || !dz || (dw && !z)) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   const T *zr = dw ? z : nullptr;
-  if (!elements_aligned<T>(zr, dy, dz)) return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
+  if (!at_elements(zr, dy, dz, dw) || !at_elements(src, pos, w)) return misaligned(who);
   constexpr int V = 16 / (int)sizeof(T);
   const bool whole = whole_rows<T>(H, zr, dy, dz);
   const int np = whole ? H / V : H, each = whole ? kGradPacks<V> : kGradPacks<1>;
@@ -443,6 +439,7 @@ int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64
   if (nexp < 1) return set_error(DP_ERR_SHAPE, "%s: nexp = %d", who, nexp);
   if (nexp > kMaxExperts) return set_error(DP_ERR_UNSUPPORTED, "%s: nexp = %d > %d", who, nexp, kMaxExperts);
   if (!start || (ntok > 0 && (!expert || !src || !pos))) return set_error(DP_ERR_NULL, "%s: NULL array", who);
+  if (!at_elements(expert, start, src, pos)) return misaligned(who);
   const PlanShape s = plan_shape(ntok * topk);
   if (s.blocks > 8) {
     if (!work) return set_error(DP_ERR_NULL, "%s: work is NULL", who);

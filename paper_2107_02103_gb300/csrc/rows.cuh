@@ -123,6 +123,15 @@ __device__ __forceinline__ bool bounded_wait(uint32_t bar, uint32_t parity, Stop
   return DP_OK;
 }
 
+// Whether every array begins at a multiple of its element's size (NULL does).
+template <typename... E>
+bool at_elements(const E *...p) {
+  return (... && !((uintptr_t)p & (sizeof(E) - 1)));
+}
+[[maybe_unused]] int misaligned(const char *who) {
+  return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
+}
+
 // The widest pack (in elements) that rows of H elements at these addresses allow: 16 bytes down to one element.
 template <typename T, typename... P>
 int pack_width(int64_t H, P... ptrs) {

@@ -113,3 +113,27 @@ def test_sizes_past_a_c_int_are_refused(dpc):
         dpc._rows(long, "x")
     with pytest.raises(ValueError, match="4294967304 pairs"):
         dpc._pairs(long)
+
+
+@pytest.mark.parametrize("x", ["f64", "f32", "bf16", "f16"])
+def test_arrays_off_their_elements_are_refused(dpc, x):
+    """Each array of each call in turn, one byte off: a load or store there would fault."""
+    odd, lib, shape = ctypes.c_void_p(0x1001), dpc._lib, dpc.DP_ERR_SHAPE
+
+    def each(f, args, arrays):
+        for i in arrays:
+            assert f(*[odd if j == i else a for j, a in enumerate(args)]) == shape, (f, i)
+
+    n64, wb = 4, lib.dp_norm_gate_work_bytes(32, 8)
+    each(lib.dp_route_plan, [FAKE, n64, 2, 8, FAKE, FAKE, FAKE, None, 0, None], (0, 4, 5, 6))
+    get = lambda name: getattr(lib, f"{name}_{x}")  # noqa: E731
+    each(get("dp_route_gather"), [FAKE, FAKE, FAKE, n64, 2, 8, FAKE, None], (0, 1, 2, 6))
+    each(get("dp_route_combine"), [FAKE, FAKE, FAKE, n64, 2, 8, FAKE, None], (0, 1, 2, 6))
+    each(get("dp_route_combine_grad"), [FAKE, FAKE, FAKE, FAKE, FAKE, n64, 2, 8, FAKE, FAKE, None], (0, 1, 2, 3, 4, 8, 9))
+    each(get("dp_quant_rows_i8"), [FAKE, FAKE, FAKE, n64, 2, 8, FAKE, FAKE, None], (0, 1, 2, 6, 7))
+    each(get("dp_linear_i8"), [FAKE, FAKE, n64, 32, FAKE, FAKE, FAKE, 2, 8, FAKE, 0, FAKE, None, 0, None], (0, 1, 4, 5, 6, 9, 11))
+    for gate in (1, 2):
+        each(get("dp_norm_gate_fwd"), [FAKE, FAKE, FAKE, gate, FAKE, FAKE, FAKE, FAKE, FAKE, n64, 32, 1, 1e-6, FAKE, FAKE, FAKE, None],
+             (0, 1, 2, 4, 5, 6, 7, 8, 13, 14, 15))
+        each(get("dp_norm_gate_grad"), [FAKE, FAKE, FAKE, gate] + [FAKE] * 7 + [n64, 32, 1] + [FAKE] * 9 + [wb, None],
+             (0, 1, 2, *range(4, 11), *range(14, 23)))
