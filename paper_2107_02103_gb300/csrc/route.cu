@@ -82,61 +82,57 @@ __global__ void __launch_bounds__(kPlanWarps * 32)
     }
     cg::this_cluster().sync();
   }
-  int carry = 0;
-  for (int e0 = 0; e0 < nexp; e0 += kPlanWarps * 32) {  // an exclusive scan of the totals
-    const int e = e0 + threadIdx.x;
-    int total = 0, before = 0;
-    if (e < nexp) {
-      if constexpr (kFrom != kOwn) {
+  // an exclusive scan of the totals, an expert a thread
+  static_assert(kMaxExperts <= kPlanWarps * 32, "an expert a thread");
+  const int e = threadIdx.x;
+  int total = 0, before = 0;
+  if (e < nexp) {
+    if constexpr (kFrom != kOwn) {
 #pragma unroll 8
-        for (int b = 0; b < (int)gridDim.x; ++b) {
-          int c;
-          if constexpr (kFrom == kTable) c = __ldg(counts + (int64_t)b * nexp + e);
-          else c = cg::this_cluster().map_shared_rank(block, b)[e];
-          before += b < (int)blockIdx.x ? c : 0;
-          total += c;
-        }
-      } else {
-#pragma unroll 8
-        for (int w = 0; w < kPlanWarps; ++w) total += cnt[w * nexp + e];
+      for (int b = 0; b < (int)gridDim.x; ++b) {
+        int c;
+        if constexpr (kFrom == kTable) c = __ldg(counts + (int64_t)b * nexp + e);
+        else c = cg::this_cluster().map_shared_rank(block, b)[e];
+        before += b < (int)blockIdx.x ? c : 0;
+        total += c;
       }
-    }
-    int inc = total;
-    for (int o = 1; o < 32; o <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += up;
-    }
-    if (lane == 31) sums[warp] = inc;
-    __syncthreads();
-    int before_warp = lane < warp ? sums[lane] : 0, all = sums[lane];
-    before_warp = __reduce_add_sync(0xffffffffu, before_warp);
-    all = __reduce_add_sync(0xffffffffu, all);
-    if (e < nexp) {
-      const int first = carry + before_warp + inc - total;
-      if (blockIdx.x == 0) start[e] = first;
-      int run = first + before;  // from counts to each warp's next row of the expert
+    } else {
 #pragma unroll 8
-      for (int w = 0; w < kPlanWarps; ++w) {
-        const int c = cnt[w * nexp + e];
-        cnt[w * nexp + e] = run;
-        run += c;
-      }
+      for (int w = 0; w < kPlanWarps; ++w) total += cnt[w * nexp + e];
     }
-    carry += all;
-    __syncthreads();
   }
-  const int kept = carry;
+  int inc = total;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += up;
+  }
+  if (lane == 31) sums[warp] = inc;
+  __syncthreads();
+  const int before_warp = __reduce_add_sync(0xffffffffu, lane < warp ? sums[lane] : 0);
+  const int kept = __reduce_add_sync(0xffffffffu, sums[lane]);
+  if (e < nexp) {
+    const int first = before_warp + inc - total;
+    if (blockIdx.x == 0) start[e] = first;
+    int run = first + before;  // from counts to each warp's next row of the expert
+#pragma unroll 8
+    for (int w = 0; w < kPlanWarps; ++w) {
+      const int c = cnt[w * nexp + e];
+      cnt[w * nexp + e] = run;
+      run += c;
+    }
+  }
+  __syncthreads();
   if (blockIdx.x == 0 && threadIdx.x == 0) start[nexp] = kept;
   if constexpr (kFrom == kCluster) cg::this_cluster().sync();  // nobody leaves while its counts are read
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int64_t q = ids.first + 32 * i;
     if (q - lane >= n) break;  // warp-uniform
-    const int e = ids.e[i];
-    const unsigned same = __match_any_sync(0xffffffffu, e);
-    const int p = e >= 0 ? mine[e] + __popc(same & ((1u << lane) - 1)) : -1;
+    const int own = ids.e[i];
+    const unsigned same = __match_any_sync(0xffffffffu, own);
+    const int p = own >= 0 ? mine[own] + __popc(same & ((1u << lane) - 1)) : -1;
     __syncwarp();
-    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
+    if (own >= 0 && lane == __ffs(same) - 1) mine[own] += __popc(same);
     __syncwarp();
     if (q < n) {
       pos[q] = p;
