@@ -15,6 +15,8 @@
 // 65,536 x 1600 bf16 241 us (4.4 TB/s) and 414 us (4.1 TB/s).
 #pragma once
 
+#include <algorithm>
+
 #include "rows.cuh"
 
 namespace dpc {
@@ -773,6 +775,12 @@ inline NormShape norm_shape(int H, bool grad) {
   return {ept, threads, blocks < 1 ? 1 : blocks};
 }
 
+// Two rows at once (kFwdRows) take 80 registers a thread: six warps of a scheduler's 16,384, 768 threads an SM.  Held to
+// 72 they leave room for seven, 896.  What that costs each warp pays where a fourth block comes to three, not where the
+// blocks were more already (us at 80 and 72, layer norm of 105 M bf16 elements: rows of 600 272, 292; 1000 224, 231; 1200
+// 240, 254; 1400 239, 254; 1600 264, 248; 1792 237, 228).
+constexpr int kTwoHeld = 768, kTightHeld = 896, kTightThreads = kTightHeld / 4;
+
 // Rows whose bytes and addresses are multiples of 16 come by bulk copies, as many rows ahead as fit; so do rows of other
 // lengths up to 2048 in arrays that begin at a multiple of 16 (cut rows); the rest by plain loads, element by
 // element unless their packs are whole.
@@ -791,9 +799,7 @@ int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st,
     if constexpr (kGrad) k = norm_grad_kernel<T, v_, e_, w_, f_, kLayer, m_, n_>;
     else k = norm_fwd_kernel<T, v_, e_, w_, f_, kLayer, m_, n_>;
     constexpr bool two = !kGrad && kFwdRows<T, b_, m_> == 2;
-    // two rows at once take 72 registers or more: 896 threads an SM, or 768
-    const int held = m_ <= 224 ? 896 : 768;
-    int blocks = two ? (held < n.threads ? 1 : held / n.threads) : n.blocks;
+    int blocks = two ? std::max(1, (m_ == kTightThreads ? kTightHeld : kTwoHeld) / n.threads) : n.blocks;
     size_t smem = kGrad && w_ ? (size_t)kRowWarps * kNormVectors * p.H * sizeof(acc_t<T>) : 0;
     if (b_) {
       const size_t row = (size_t)p.nin * (f_ == kCutRows ? cut_bytes<T>(p.H) : p.H * sizeof(T));
@@ -844,7 +850,8 @@ int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st,
       if (weights16 && (size_t)p.nin * p.H * sizeof(T) * n.blocks <= 200 * 1024) {
         constexpr int kTwo = !kGrad && sizeof(T) == 2 ? 3 : kFew, kTwoHalf = !kGrad && sizeof(T) == 2 ? 1 : kHalf;
         if constexpr (!kGrad && sizeof(T) == 2)
-          if (n.threads == 224) return go(V, e8, no{}, bulk, integral_constant<int, 224>{}, integral_constant<int, 4>{});
+          if (kTwoHeld / n.threads == 3 && kTightHeld / n.threads == 4)
+            return go(V, e8, no{}, bulk, integral_constant<int, kTightThreads>{}, integral_constant<int, 4>{});
         if (p.H <= 2048) return go(V, e8, no{}, bulk, integral_constant<int, 256>{}, integral_constant<int, kTwo>{});
         if (p.H <= 4096) return go(V, e8, no{}, bulk, integral_constant<int, 512>{}, integral_constant<int, kTwoHalf>{});
         if (p.H <= 8192) return go(V, e8, no{}, bulk, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
