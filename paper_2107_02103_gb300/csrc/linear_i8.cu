@@ -239,9 +239,9 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_i8_few_kernel(const I8A
 // expert, take the weights widened once (widen_weights_kernel) by bulk copies.
 // A block per SM walks the tiles; every wait is bounded, a block that gives up writes NaN and is counted.
 // Measured: 32,768 x 2048 x 4096 in 517 us, 1,063 TFLOP/s (55 % of the measured bf16 rate); 65,536 x 1600 x 240 with
-// four nets in 92 us.  Without the epilogue 471 and 74 us, without the loads of x 491 and 81: what is left is shared
-// memory: at 128 bytes a cycle a stage's operand writes and MMA reads (48 KB each) take 768 cycles where its MMAs take
-// 512.
+// four nets in 92 us, with as many rows each in 87.  Without the epilogue 471 and 74 us, without the loads of x 491 and
+// 81: what is left is shared memory: at 128 bytes a cycle a stage's operand writes and MMA reads (48 KB each) take 768
+// cycles where its MMAs take 512.  The wide form spills 116 bytes of a thread's registers.
 namespace i8 {
 constexpr int kTM = 128, kKB = 64, kChunkK = 1024;
 constexpr int kEpiWarps = 8;

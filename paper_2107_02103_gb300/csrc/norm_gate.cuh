@@ -12,7 +12,12 @@
 // norm's variance is taken around the mean in a second sweep of the registers.
 // f32 is bound by memory: 24,576 x 2048 with a full gate 154 us forward (6.5 TB/s), 272 us backward (5.9 TB/s).  16-bit
 // rows, twice the elements a byte, are bound by instructions and the waits of a row's four block sums: layer norm of
-// 65,536 x 1600 bf16 241 us (4.4 TB/s) and 414 us (4.1 TB/s).
+// 65,536 x 1600 bf16 248 us (4.2 TB/s) and 396 us (4.2 TB/s).  The registers do not hold everything in the backward of
+// rows past 4096 elements (64 a thread; 0.1 to 0.4 KB of them spilled, 0.9 to 1.9 KB past 8192) nor in f64 (forward 50 to
+// 150 bytes, backward 0.2 to 0.6 KB, up to 3.3 KB past 8192): 8,000 x 6000 f32 152 and 338 us, 4,000 x 16384 f32 400 and
+// 1,653 us with layer norm.  f64 is bound by the FP64 pipe's instructions, of which the elements' own, some 12 each
+// forward, are 0.6 of 1.60 ms for a layer norm of 20,000 x 1600; the rest is that every thread finishes a row's sums,
+// root and division for itself.  Backward 2.39 ms; root-mean-square norm without a gate 1.01 and 1.68 ms.
 #pragma once
 
 #include <algorithm>
@@ -339,7 +344,7 @@ __device__ __noinline__ void leave_rows(uint64_t *bars, int stages, unsigned fir
 }
 
 // Rows a block of the forward works on at once: two of 16-bit elements by bulk copies (the waits of their block sums
-// overlap, and the weights are read once for both: layer norm of 65,536 x 1600 bf16 in 241 us against 270), else one.
+// overlap, and the weights are read once for both: layer norm of 65,536 x 1600 bf16 in 248 us against 277), else one.
 template <typename T, bool kBulk, int kThreads>
 constexpr int kFwdRows = kBulk && sizeof(T) == 2 && kThreads <= 512 ? 2 : 1;
 
@@ -446,8 +451,8 @@ __global__ void __launch_bounds__(kThreads, kMinBlocks) norm_fwd_kernel(const No
 // The forward for 16-bit rows of 257 to 512 elements: a warp a row, the row's one array in registers (f, then p, then
 // r2), r and the gate read from shared memory where they are used.  No block barriers, and a row costs a third of the
 // instructions that it costs a block, whose sums' shuffles and barriers every warp repeats.  Each warp has two rows in
-// shared memory, the next on its way while it works on one.  65,536 x 512 bf16 layer norm: 59 us against 77 by blocks;
-// longer rows leave too few warps on an SM (1024: 161 against 140).
+// shared memory, the next on its way while it works on one.  65,536 x 512 bf16 layer norm: 60 us against 78 by blocks;
+// longer rows leave too few warps on an SM (1024 when it was tried: 161 against 140).
 constexpr int kWarpStages = 2, kWarpEpt = 16;  // the stages' order below holds for two
 
 // Warps a block: two for whole rows; cut rows share the block's weights, one block an SM.
@@ -843,11 +848,10 @@ int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st,
     constexpr int kFew = kGrad ? 2 : 4, kHalf = kGrad ? 1 : 2;
     constexpr integral_constant<Feed, kPlain> plain{};
     constexpr integral_constant<Feed, kBulkRows> bulk{};
-    constexpr integral_constant<Feed, kCutRows> cut{};
     if (p.H <= kWarpRowMax)
       return go(V, e8, yes{}, plain, integral_constant<int, kRowWarps * 32>{}, integral_constant<int, kGrad ? 3 : 8>{});
     if constexpr (decltype(V)::value * sizeof(T) == 16) {
-      if (weights16 && (size_t)p.nin * p.H * sizeof(T) * n.blocks <= 200 * 1024) {
+      if (weights16 && (size_t)p.nin * p.H * sizeof(T) * n.blocks <= kBulkRoom) {
         constexpr int kTwo = !kGrad && sizeof(T) == 2 ? 3 : kFew, kTwoHalf = !kGrad && sizeof(T) == 2 ? 1 : kHalf;
         if constexpr (!kGrad && sizeof(T) == 2)
           if (kTwoHeld / n.threads == 3 && kTightHeld / n.threads == 4)
@@ -857,13 +861,17 @@ int launch(NormArgs<T> &p, int v, bool weights16, bool bases16, cudaStream_t st,
         if (p.H <= 8192) return go(V, e8, no{}, bulk, integral_constant<int, 1024>{}, integral_constant<int, 1>{});
       }
     }
-    if constexpr (decltype(V)::value * sizeof(T) != 16 && sizeof(T) < 8) {
-      constexpr int kTwo = !kGrad && sizeof(T) == 2 ? 3 : kFew;
-      // A block sets its weights up first, which pays from some 8 rows on, in the backward of 16-bit rows 20 (us, plain
-      // and cut, rows of 1003: backward f16 5,000 34, 44; 9,973 64, 67; 20,000 112, 102; f32 5,000 48, 43).
-      constexpr int kPays = kGrad && sizeof(T) == 2 ? 20 : 8;
-      if (bases16 && p.H <= 2048 && p.ntok >= (int64_t)152 * kPays * n.blocks && cut_bytes<T>(p.H) / sizeof(T) <= (size_t)n.threads * 8)  // a place for every pack
-        return go(integral_constant<int, 16 / (int)sizeof(T)>{}, e8, no{}, cut, integral_constant<int, 256>{}, integral_constant<int, kTwo>{});
+    if constexpr (sizeof(T) < 8) {  // apart from the next, which depends on V: or f64's cut form would be compiled too
+      if constexpr (decltype(V)::value * sizeof(T) != 16) {
+        constexpr int kTwo = !kGrad && sizeof(T) == 2 ? 3 : kFew;
+        // A block sets its weights up first, which pays from some 8 rows on, in the backward of 16-bit rows 20 (us, plain
+        // and cut, rows of 1003: backward f16 5,000 35, 43; 9,973 63, 66; 20,000 111, 103; f32 5,000 42, 43).
+        constexpr int kPays = kGrad && sizeof(T) == 2 ? 20 : 8;
+        const bool places = cut_bytes<T>(p.H) / sizeof(T) <= (size_t)n.threads * 8;  // one for every pack
+        if (bases16 && p.H <= 2048 && p.ntok >= (int64_t)152 * kPays * n.blocks && places)
+          return go(integral_constant<int, 16 / (int)sizeof(T)>{}, e8, no{}, integral_constant<Feed, kCutRows>{},
+                    integral_constant<int, 256>{}, integral_constant<int, kTwo>{});
+      }
     }
     if (p.H <= 2048) return go(V, e8, no{}, plain, integral_constant<int, 256>{}, integral_constant<int, kFew>{});
     if (p.H <= 4096) return go(V, e8, no{}, plain, integral_constant<int, 512>{}, integral_constant<int, kHalf>{});
