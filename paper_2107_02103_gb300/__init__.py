@@ -985,9 +985,10 @@ def _pairs(pos):
     """(ntok, topk) of a plan's pos."""
     if not isinstance(pos, torch.Tensor) or pos.dim() != 2:
         raise ValueError("pos must be a plan's [ntok][topk] tensor")
-    if pos.shape[1] >> 31:
-        raise ValueError(f"pos has {pos.shape[1]} pairs a token")
-    return pos.shape
+    shape = pos.shape
+    if shape[1] >> 31:
+        raise ValueError(f"pos has {shape[1]} pairs a token")
+    return shape
 
 
 def _work_ptr(work, need, like, dev):
@@ -1005,7 +1006,8 @@ def _work_ptr(work, need, like, dev):
 
 def dp_route_work_bytes(ntok, topk, nexp) -> int:
     """Bytes of device scratch dp_route_plan needs."""
-    _fits(ntok, topk, nexp)
+    if (topk | nexp) >> 31 or ntok >> 63:
+        _fits(ntok, topk, nexp)
     n = _lib.dp_route_work_bytes(ntok, topk, nexp)
     if n == 0:
         raise ValueError(f"bad plan: {ntok} tokens, {topk} experts each of {nexp}")
@@ -1137,7 +1139,8 @@ def dp_linear_i8(xq, sx, wq, sw, bias=None, start=None, act=None, dtype=torch.fl
     nexp, N, _ = wq.shape
     dev, f32 = xq.get_device(), torch.float32
     y = torch.empty((rows, N), dtype=dtype, device=xq.device) if out is None else out
-    _fits(rows, K, N, nexp)
+    if (K | N | nexp) >> 31:
+        _fits(rows, K, N, nexp)
     need = 0 if work is not None else _lib.dp_linear_i8_work_bytes(rows, K, N, nexp)
     wp, wn, work = _work_ptr(work, need, xq, dev)
     _run(dev, _ROW_FN["linear_i8"][dtype], _p(xq, "xq", torch.int8, (rows, K), dev), _p(sx, "sx", f32, (rows,), dev),
@@ -1192,7 +1195,8 @@ def dp_norm_gate_fwd(r, f, a, w1, w2, b1=None, b2=None, gate=None, kind="rms", e
 
 def dp_norm_gate_work_bytes(H, dtype) -> int:
     """Bytes of device scratch dp_norm_gate_grad needs for rows of H elements of dtype."""
-    _fits(0, H)
+    if H >> 31:
+        _fits(0, H)
     n = _lib.dp_norm_gate_work_bytes(H, dtype.itemsize)
     if n == 0:
         raise ValueError(f"unsupported row length {H}")
