@@ -726,6 +726,51 @@ int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64
                   void *work, size_t work_bytes, void *stream);
 
 /*
+ * Router: the experts of each token from its logits, and their weights; expert and
+ * w are what dp_route_plan and dp_route_combine_* take.  For a row x of nexp logits
+ * and a bias b (NULL: none):
+ *   s = softmax(x) or sigmoid(x),   c = s + b
+ *   ngroup groups of nexp / ngroup neighbouring experts, each scored by the sum of
+ *   its group_top (1 or 2) largest c: the keep_groups best stay
+ *   expert[t][j] = the expert of the j-th largest c left
+ *   w[t][j] = scale s_e, or with renorm scale s_e / sum_i s_ei (the bias only chooses)
+ * Without a bias the experts are ordered by x itself (the groups by c all the same,
+ * group_top 1: by x).  Equal ones go by the lowest index.  The choice is that of
+ * exact arithmetic on the inputs: rounding does not move it (scores nearer than the
+ * f32 error bounds are compared in f64; f64 rows in f64 alone).  An expert with
+ * x = -inf or b = -inf is never chosen; a pair left without an expert gets -1 and
+ * weight 0.  A NaN stands above all numbers, and its weights are NaN.
+ *   logits [ntok][nexp];  bias [nexp];  expert, w [ntok][topk] outputs
+ * Backward, the choice held fixed, from dw = dE/dw and the forward's expert (as it
+ * came: a pair dropped later has dw 0, not another id; ids outside [0, nexp) and
+ * logits of -inf count as no pair):
+ *   dlogits [ntok][nexp] output, all of it written
+ * Every sum has a fixed order.  ntok == 0 reads no device pointer.  Errors:
+ * DP_ERR_NULL, DP_ERR_SHAPE (topk outside [1, min(64, nexp)], nexp not a multiple of
+ * ngroup, fewer experts in keep_groups groups than topk, an unknown score or
+ * group_top, a scale that is not finite, 2^31 or more pairs, alignment),
+ * DP_ERR_UNSUPPORTED (nexp above 1024), DP_ERR_CUDA.
+ */
+#define DP_SCORE_SOFTMAX 0
+#define DP_SCORE_SIGMOID 1
+int dp_route_topk_f64(const double *logits, const double *bias, int64_t ntok, int nexp, int topk, int score, int ngroup,
+                  int keep_groups, int group_top, int renorm, double scale, int32_t *expert, double *w, void *stream);
+int dp_route_topk_f32(const float *logits, const float *bias, int64_t ntok, int nexp, int topk, int score, int ngroup,
+                  int keep_groups, int group_top, int renorm, double scale, int32_t *expert, float *w, void *stream);
+int dp_route_topk_bf16(const uint16_t *logits, const float *bias, int64_t ntok, int nexp, int topk, int score, int ngroup,
+                  int keep_groups, int group_top, int renorm, double scale, int32_t *expert, float *w, void *stream);
+int dp_route_topk_f16(const uint16_t *logits, const float *bias, int64_t ntok, int nexp, int topk, int score, int ngroup,
+                  int keep_groups, int group_top, int renorm, double scale, int32_t *expert, float *w, void *stream);
+int dp_route_topk_grad_f64(const double *logits, const int32_t *expert, const double *dw, int64_t ntok, int nexp, int topk,
+                       int score, int renorm, double scale, double *dlogits, void *stream);
+int dp_route_topk_grad_f32(const float *logits, const int32_t *expert, const float *dw, int64_t ntok, int nexp, int topk,
+                       int score, int renorm, double scale, float *dlogits, void *stream);
+int dp_route_topk_grad_bf16(const uint16_t *logits, const int32_t *expert, const float *dw, int64_t ntok, int nexp, int topk,
+                       int score, int renorm, double scale, uint16_t *dlogits, void *stream);
+int dp_route_topk_grad_f16(const uint16_t *logits, const int32_t *expert, const float *dw, int64_t ntok, int nexp, int topk,
+                       int score, int renorm, double scale, uint16_t *dlogits, void *stream);
+
+/*
  * Rows to their sorted places and back, H elements a row, with a plan's src and pos.
  *   gather   xs[p] = x[src[p] / topk]; rows past the kept ones are zero
  *            (its backward is combine of the rows' gradients with w NULL)
@@ -824,6 +869,92 @@ int dp_linear_i8_bf16(const int8_t *xq, const float *sx, int64_t rows, int K, co
 int dp_linear_i8_f16(const int8_t *xq, const float *sx, int64_t rows, int K, const int8_t *wq, const float *sw,
                      const float *bias, int nexp, int N, const int64_t *start, int act, uint16_t *y, void *work,
                      size_t work_bytes, void *stream);
+
+/*
+ * Rows to microscaled 4-bit floating point: 32 neighbours along K share a power of
+ * two.  x is rounded to f32; then, for each block of 32 (the last one padded with zeros),
+ *   amax = max_k |x_k|,  e = max(floor(log2 amax) - 2, -127)
+ *   q_k = the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives to x_k 2^-e, ties
+ *         to the even code, +-6 for what lies above (amax 2^-e is below 8)
+ * so x_k ~ q_k 2^e.  Code: sign, two bits of exponent, one of mantissa (0 .. 7 the values
+ * above in order, +8 the sign; -0 keeps it).  A block that holds an infinity or NaN gets
+ * the scale 255, NaN (its rows' outputs become NaN).  Weights are rows too:
+ * W [nexp][N][K] by its nexp N rows.
+ *   xq  [rows][ldq / 2] output, two codes a byte, the lower four bits first; ldq = K
+ *       rounded up to a multiple of 64, codes past K zero; 16-byte aligned
+ *   sx  [rows][lds] output: e + 127 of each block; lds = 8 ceil(K / 256), scales past
+ *       the last block 0; 8-byte aligned
+ * src and pos as dp_quant_rows_i8_* (rows past the kept ones: all zero).
+ * Errors: DP_ERR_NULL, DP_ERR_SHAPE, DP_ERR_UNSUPPORTED (K above 65536), DP_ERR_CUDA.
+ */
+int dp_quant_rows_mx4_f64(const double *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int K,
+                      uint8_t *xq, uint8_t *sx, void *stream);
+int dp_quant_rows_mx4_f32(const float *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int K,
+                      uint8_t *xq, uint8_t *sx, void *stream);
+int dp_quant_rows_mx4_bf16(const uint16_t *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int K,
+                      uint8_t *xq, uint8_t *sx, void *stream);
+int dp_quant_rows_mx4_f16(const uint16_t *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int K,
+                      uint8_t *xq, uint8_t *sx, void *stream);
+
+/*
+ * Product of such rows with such weights:
+ *   y_in = act(sum_k x_ik w_enk + bias_en),  e the expert of row i
+ * with the values that codes and scales stand for; products are exact, sums f32, y
+ * rounded to the rows' type.  It has no gradient, as dp_linear_i8_* has none.
+ *   xq [rows][K / 2], sx [rows][8 ceil(K / 256)], K a multiple of 64 (the quantiser's ldq)
+ *   wq [nexp][N][K / 2], sw [nexp][N][8 ceil(K / 256)];  bias [nexp][N] (NULL: none)
+ *   start, act, y as dp_linear_i8_*
+ * xq and wq are 16-byte, sx and sw 8-byte aligned.  No scratch.  rows == 0 reads no
+ * device pointer.  Errors: DP_ERR_NULL, DP_ERR_SHAPE, DP_ERR_UNSUPPORTED (K above
+ * 65536), DP_ERR_CUDA.
+ */
+int dp_linear_mx4_f64(const uint8_t *xq, const uint8_t *sx, int64_t rows, int K, const uint8_t *wq, const uint8_t *sw,
+                  const float *bias, int nexp, int N, const int64_t *start, int act, double *y, void *stream);
+int dp_linear_mx4_f32(const uint8_t *xq, const uint8_t *sx, int64_t rows, int K, const uint8_t *wq, const uint8_t *sw,
+                  const float *bias, int nexp, int N, const int64_t *start, int act, float *y, void *stream);
+int dp_linear_mx4_bf16(const uint8_t *xq, const uint8_t *sx, int64_t rows, int K, const uint8_t *wq, const uint8_t *sw,
+                  const float *bias, int nexp, int N, const int64_t *start, int act, uint16_t *y, void *stream);
+int dp_linear_mx4_f16(const uint8_t *xq, const uint8_t *sx, int64_t rows, int K, const uint8_t *wq, const uint8_t *sw,
+                  const float *bias, int nexp, int N, const int64_t *start, int act, uint16_t *y, void *stream);
+
+/*
+ * Embedding of ids (atom types, so that nets shared by all types can tell them apart):
+ *   y[t] = add[t] + scale W[ids[t]]
+ * add NULL: zeros; an id outside [0, nvocab) adds nothing.  y may be add.
+ *   W [nvocab][H];  ids [ntok] int32;  add, y [ntok][H]
+ * Gradient, by the ids sorted (add's gradient is dy):
+ *   plan  start [nvocab + 1], src [ntok] outputs: the tokens of id v, in order, are
+ *         src[start[v] .. start[v + 1] - 1]; past start[nvocab] src is -1 (what
+ *         dp_route_plan gives for ids as experts, which takes up to 1024 of them)
+ *   grad  dW[v] = scale sum_t dy[t] over the tokens of v, f32 (f64 rows: f64); every row
+ *         is written, or with accumulate the sums are added to what dW holds
+ *   work, work_bytes  device scratch, 16-byte aligned, at least the bytes of the two
+ *         functions (0: bad arguments; 1: work may be NULL)
+ * Every sum has a fixed order.  ntok == 0: start and dW are zero.  Errors: DP_ERR_NULL,
+ * DP_ERR_SHAPE (ntok < 0 or 2^31 - 4096 and more, nvocab < 1, H outside [1, 2^20], a scale
+ * that is not finite, alignment, a short work buffer), DP_ERR_UNSUPPORTED (nvocab 2^24
+ * and more), DP_ERR_CUDA.
+ */
+size_t dp_embed_plan_work_bytes(int64_t ntok, int nvocab);
+int dp_embed_plan(const int32_t *ids, int64_t ntok, int nvocab, int64_t *start, int32_t *src, void *work,
+                  size_t work_bytes, void *stream);
+size_t dp_embed_grad_work_bytes(int64_t ntok, int H, int elem_bytes);
+int dp_embed_fwd_f64(const double *W, const int32_t *ids, int64_t ntok, int nvocab, int H, double scale, const double *add,
+                 double *y, void *stream);
+int dp_embed_fwd_f32(const float *W, const int32_t *ids, int64_t ntok, int nvocab, int H, double scale, const float *add,
+                 float *y, void *stream);
+int dp_embed_fwd_bf16(const uint16_t *W, const int32_t *ids, int64_t ntok, int nvocab, int H, double scale, const uint16_t *add,
+                 uint16_t *y, void *stream);
+int dp_embed_fwd_f16(const uint16_t *W, const int32_t *ids, int64_t ntok, int nvocab, int H, double scale, const uint16_t *add,
+                 uint16_t *y, void *stream);
+int dp_embed_grad_f64(const double *dy, const int32_t *ids, const int64_t *start, const int32_t *src, int64_t ntok,
+                  int nvocab, int H, double scale, int accumulate, double *dW, void *work, size_t work_bytes, void *stream);
+int dp_embed_grad_f32(const float *dy, const int32_t *ids, const int64_t *start, const int32_t *src, int64_t ntok,
+                  int nvocab, int H, double scale, int accumulate, float *dW, void *work, size_t work_bytes, void *stream);
+int dp_embed_grad_bf16(const uint16_t *dy, const int32_t *ids, const int64_t *start, const int32_t *src, int64_t ntok,
+                  int nvocab, int H, double scale, int accumulate, float *dW, void *work, size_t work_bytes, void *stream);
+int dp_embed_grad_f16(const uint16_t *dy, const int32_t *ids, const int64_t *start, const int32_t *src, int64_t ntok,
+                  int nvocab, int H, double scale, int accumulate, float *dW, void *work, size_t work_bytes, void *stream);
 
 /*
  * The norms around a block with its gate and residual scale.  For each token,

@@ -160,10 +160,22 @@ _SIGS = {
     "dp_route_plan": ([_P, _I64, ctypes.c_int, ctypes.c_int, _P, _P, _P, _P, ctypes.c_size_t, _P], ctypes.c_int),
     "dp_linear_i8_work_bytes": ([_I64, ctypes.c_int, ctypes.c_int, ctypes.c_int], ctypes.c_size_t),
     "dp_norm_gate_work_bytes": ([ctypes.c_int, ctypes.c_int], ctypes.c_size_t),
+    "dp_embed_plan_work_bytes": ([_I64, ctypes.c_int], ctypes.c_size_t),
+    "dp_embed_plan": ([_P, _I64, ctypes.c_int, _P, _P, _P, ctypes.c_size_t, _P], ctypes.c_int),
+    "dp_embed_grad_work_bytes": ([_I64, ctypes.c_int, ctypes.c_int], ctypes.c_size_t),
     **{f"{name}_{x}": (args, ctypes.c_int) for x in ("f64", "f32", "bf16", "f16") for name, args in (
         ("dp_route_gather", [_P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _P]),
         ("dp_route_combine", [_P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _P]),
         ("dp_route_combine_grad", [_P, _P, _P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _P, _P]),
+        ("dp_route_topk", [_P, _P, _I64, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                           ctypes.c_int, ctypes.c_int, _D, _P, _P, _P]),
+        ("dp_route_topk_grad", [_P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, _D, _P, _P]),
+        ("dp_embed_fwd", [_P, _P, _I64, ctypes.c_int, ctypes.c_int, _D, _P, _P, _P]),
+        ("dp_embed_grad", [_P, _P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _D, ctypes.c_int, _P, _P, ctypes.c_size_t,
+                           _P]),
+        ("dp_quant_rows_mx4", [_P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _P, _P]),
+        ("dp_linear_mx4", [_P, _P, _I64, ctypes.c_int, _P, _P, _P, ctypes.c_int, ctypes.c_int, _P, ctypes.c_int, _P,
+                           _P]),
         ("dp_quant_rows_i8", [_P, _P, _P, _I64, ctypes.c_int, ctypes.c_int, _P, _P, _P]),
         ("dp_linear_i8", [_P, _P, _I64, ctypes.c_int, _P, _P, _P, ctypes.c_int, ctypes.c_int, _P, ctypes.c_int, _P,
                           _P, ctypes.c_size_t, _P]),
@@ -942,7 +954,8 @@ def dp_tensor_head_grad(T, a, dA, dT=None, da=None, accumulate=False, want=("dT"
 # A call on few atoms costs what its checks cost: one expression per tensor (_p), the functions looked up once.
 _ROW_SUFFIX = {torch.float64: "f64", torch.float32: "f32", torch.bfloat16: "bf16", torch.float16: "f16"}
 _ROW_FN = {name: {t: getattr(_lib, f"dp_{name}_{x}") for t, x in _ROW_SUFFIX.items()}
-           for name in ("route_gather", "route_combine", "route_combine_grad", "quant_rows_i8", "linear_i8",
+           for name in ("route_topk", "route_topk_grad", "route_gather", "route_combine", "route_combine_grad",
+                        "quant_rows_i8", "linear_i8", "quant_rows_mx4", "linear_mx4", "embed_fwd", "embed_grad",
                         "norm_gate_fwd", "norm_gate_grad")}
 # the type of weights and sums beside rows of a type
 _WDTYPE = {torch.float64: torch.float64, torch.float32: torch.float32, torch.bfloat16: torch.float32,
@@ -1002,6 +1015,49 @@ def _work_ptr(work, need, like, dev):
         if work.get_device() != dev:
             raise ValueError(f"work is on device {work.get_device()}, the other tensors on {dev}")
     return work.data_ptr(), work.numel(), work
+
+
+_SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _score(score):
+    if score not in _SCORES:
+        raise ValueError(f"score must be 'softmax' or 'sigmoid', got {score!r}")
+    return _SCORES[score]
+
+
+def dp_route_topk(logits, topk, bias=None, score="softmax", ngroup=1, keep_groups=None, group_top=2, renorm=True,
+                  scale=1.0, out=None):
+    """(expert int32 [ntok][topk], w [ntok][topk]): each token's topk experts by s + bias, s the softmax or sigmoid of
+    logits [ntok][nexp], best first, within the keep_groups (None: all) of ngroup groups with the largest sums of their
+    group_top best; w = scale s, renormalised over the token's experts with renorm.  Experts with a logit or bias of
+    -inf are never chosen (-1 and weight 0 where none is left).  expert goes to dp_route_plan, w to dp_route_combine."""
+    dtype, ntok, nexp, dev = _rows(logits, "logits")
+    k, wd, topk, ngroup = _score(score), _WDTYPE[dtype], int(topk), int(ngroup)
+    keep = ngroup if keep_groups is None else int(keep_groups)
+    if (topk | ngroup | keep | int(group_top)) >> 31:
+        _fits(ntok, topk, ngroup, keep, int(group_top))
+    expert, w = (None, None) if out is None else out
+    if expert is None:
+        expert = torch.empty((ntok, max(topk, 0)), dtype=torch.int32, device=logits.device)
+    if w is None:
+        w = torch.empty((ntok, max(topk, 0)), dtype=wd, device=logits.device)
+    _run(dev, _ROW_FN["route_topk"][dtype], _p(logits, "logits", dtype, (ntok, nexp), dev),
+         None if bias is None else _p(bias, "bias", wd, (nexp,), dev), ntok, nexp, topk, k, ngroup, keep, int(group_top),
+         bool(renorm), scale, _p(expert, "expert", torch.int32, (ntok, topk), dev), _p(w, "w", wd, (ntok, topk), dev))
+    return expert, w
+
+
+def dp_route_topk_grad(logits, expert, dw, score="softmax", renorm=True, scale=1.0, out=None):
+    """dlogits [ntok][nexp] of dp_route_topk's weights from dw [ntok][topk] and the expert it returned, the choice held
+    fixed; score, renorm and scale as there."""
+    dtype, ntok, nexp, dev = _rows(logits, "logits")
+    shape = _pairs(expert)
+    dx = torch.empty_like(logits) if out is None else out
+    _run(dev, _ROW_FN["route_topk_grad"][dtype], _p(logits, "logits", dtype, (ntok, nexp), dev),
+         _p(expert, "expert", torch.int32, (ntok, shape[1]), dev), _p(dw, "dw", _WDTYPE[dtype], (ntok, shape[1]), dev),
+         ntok, nexp, shape[1], _score(score), bool(renorm), scale, _p(dx, "out", dtype, (ntok, nexp), dev))
+    return dx
 
 
 def dp_route_work_bytes(ntok, topk, nexp) -> int:
@@ -1149,6 +1205,136 @@ def dp_linear_i8(xq, sx, wq, sw, bias=None, start=None, act=None, dtype=torch.fl
          None if start is None else _p(start, "start", torch.int64, (nexp + 1,), dev), _ACTS[act],
          _p(y, "out", dtype, (rows, N), dev), wp, wn)
     return y
+
+
+def dp_quant_rows_mx4(x, src=None, pos=None, out=None):
+    """(xq uint8 [rows][ldq/2], sx uint8 [rows][lds]): each row of x [ntok][K] as 4-bit floating-point codes, two a byte
+    (the lower four bits first), with a power of two (code - 127) for 32 neighbours; ldq = K rounded up to a multiple of
+    64, lds = 8 ceil(K/256).  src, pos and weights as in dp_quant_rows_i8."""
+    dtype, ntok, K, dev = _rows(x, "x")
+    if (src is None) != (pos is None):
+        raise ValueError("src and pos come together")
+    topk, sp, pp = 1, None, None
+    if pos is not None:
+        ntok, topk = _pairs(pos)
+        sp = _p(src, "src", torch.int32, (ntok * topk,), dev)
+        pp = _p(pos, "pos", torch.int32, (ntok, topk), dev)
+    n, half, lds = ntok * topk, (K + 63) // 64 * 32, (K + 255) // 256 * 8
+    xq, sx = (None, None) if out is None else out
+    if xq is None:
+        xq = torch.empty((n, half), dtype=torch.uint8, device=x.device)
+    if sx is None:
+        sx = torch.empty((n, lds), dtype=torch.uint8, device=x.device)
+    _run(dev, _ROW_FN["quant_rows_mx4"][dtype], _p(x, "x", dtype, (ntok, K), dev), sp, pp, ntok, topk, K,
+         _p(xq, "xq", torch.uint8, (n, half), dev), _p(sx, "sx", torch.uint8, (n, lds), dev))
+    return xq, sx
+
+
+def dp_linear_mx4(xq, sx, wq, sw, bias=None, start=None, act=None, dtype=torch.float32, out=None):
+    """y [rows][N] of dtype: act(x w^T + bias) on the values that 4-bit codes and scales stand for; xq [rows][ldq/2] and
+    sx [rows][lds] from dp_quant_rows_mx4, wq [nexp][N][ldq/2] and sw [nexp][N][lds] likewise, bias f32 [nexp][N];
+    start and act as in dp_linear_i8."""
+    u8 = torch.uint8
+    if not isinstance(xq, torch.Tensor) or not xq.is_cuda or xq.dtype is not u8:
+        raise TypeError("xq must be a uint8 CUDA tensor")
+    if not isinstance(wq, torch.Tensor) or wq.dtype is not u8:
+        raise TypeError("wq must be a uint8 CUDA tensor")
+    if xq.dim() != 2 or wq.dim() != 3 or xq.shape[1] != wq.shape[2]:
+        raise ValueError(f"xq [rows][ldq/2] and wq [nexp][N][ldq/2] expected, got {tuple(xq.shape)} and {tuple(wq.shape)}")
+    if act not in _ACTS:
+        raise ValueError(f"act must be None or 'tanh', got {act!r}")
+    if dtype not in _ROW_SUFFIX:
+        raise TypeError(f"unsupported dtype {dtype}")
+    rows, half = xq.shape
+    nexp, N, _ = wq.shape
+    dev, f32, K, lds = xq.get_device(), torch.float32, 2 * half, (half + 127) // 128 * 8
+    if (K | N | nexp) >> 31:
+        _fits(rows, K, N, nexp)
+    y = torch.empty((rows, N), dtype=dtype, device=xq.device) if out is None else out
+    _run(dev, _ROW_FN["linear_mx4"][dtype], _p(xq, "xq", u8, (rows, half), dev), _p(sx, "sx", u8, (rows, lds), dev), rows, K,
+         _p(wq, "wq", u8, (nexp, N, half), dev), _p(sw, "sw", u8, (nexp, N, lds), dev),
+         None if bias is None else _p(bias, "bias", f32, (nexp, N), dev), nexp, N,
+         None if start is None else _p(start, "start", torch.int64, (nexp + 1,), dev), _ACTS[act],
+         _p(y, "out", dtype, (rows, N), dev))
+    return y
+
+
+def _ids(ids):
+    """(ids, device number) of a vector of ids."""
+    if not isinstance(ids, torch.Tensor) or not ids.is_cuda or ids.dtype is not torch.int32:
+        raise TypeError("ids must be an int32 CUDA tensor")
+    if ids.dim() != 1:
+        raise ValueError(f"ids must be [ntok], got {tuple(ids.shape)}")
+    return ids.shape[0], ids.get_device()
+
+
+def dp_embed_fwd(W, ids, scale=1.0, add=None, out=None):
+    """y [ntok][H] = add + scale W[ids] (add None: zeros); ids int32 [ntok], those outside [0, nvocab) add nothing.  out
+    may be add."""
+    dtype, nvocab, H, dev = _rows(W, "W")
+    ntok, _ = _ids(ids)
+    if nvocab >> 31:
+        _fits(ntok, nvocab)
+    y = torch.empty((ntok, H), dtype=dtype, device=W.device) if out is None else out
+    _run(dev, _ROW_FN["embed_fwd"][dtype], _p(W, "W", dtype, (nvocab, H), dev), _p(ids, "ids", torch.int32, (ntok,), dev),
+         ntok, nvocab, H, scale, None if add is None else _p(add, "add", dtype, (ntok, H), dev),
+         _p(y, "out", dtype, (ntok, H), dev))
+    return y
+
+
+def dp_embed_plan_work_bytes(ntok, nvocab) -> int:
+    """Bytes of device scratch dp_embed_plan needs."""
+    _fits(ntok, nvocab)
+    n = _lib.dp_embed_plan_work_bytes(ntok, nvocab)
+    if n == 0:
+        raise ValueError(f"bad plan: {ntok} tokens, {nvocab} ids")
+    return n
+
+
+def dp_embed_plan(ids, nvocab, out=None, work=None):
+    """(start [nvocab+1] int64, src [ntok] int32): the tokens sorted by their id, stably; those whose id lies outside
+    [0, nvocab) come last, as -1."""
+    ntok, dev = _ids(ids)
+    nvocab = int(nvocab)
+    need = dp_embed_plan_work_bytes(ntok, nvocab)
+    start, src = (None, None) if out is None else out
+    if start is None:
+        start = torch.empty((nvocab + 1,), dtype=torch.int64, device=ids.device)
+    if src is None:
+        src = torch.empty((ntok,), dtype=torch.int32, device=ids.device)
+    wp, wn, work = _work_ptr(work, need if need > 1 else 0, ids, dev)  # 1: none needed
+    _run(dev, _lib.dp_embed_plan, _p(ids, "ids", torch.int32, (ntok,), dev), ntok, nvocab,
+         _p(start, "start", torch.int64, (nvocab + 1,), dev), _p(src, "src", torch.int32, (ntok,), dev), wp, wn)
+    return start, src
+
+
+def dp_embed_grad_work_bytes(ntok, H, dtype) -> int:
+    """Bytes of device scratch dp_embed_grad needs for rows of H elements of dtype."""
+    _fits(ntok, H)
+    n = _lib.dp_embed_grad_work_bytes(ntok, H, dtype.itemsize)
+    if n == 0:
+        raise ValueError(f"bad rows: {ntok} of {H} elements")
+    return n
+
+
+def dp_embed_grad(dy, ids, start, src, scale=1.0, out=None, accumulate=False, work=None):
+    """dW [nvocab][H] (f32, f64 for f64 rows) of dp_embed_fwd from dy [ntok][H] and the plan of ids; accumulate adds to
+    what out holds."""
+    dtype, ntok, H, dev = _rows(dy, "dy")
+    wd = _WDTYPE[dtype]
+    if not isinstance(start, torch.Tensor) or start.dim() != 1 or start.shape[0] < 2:
+        raise ValueError("start must be a plan's [nvocab+1] tensor")
+    nvocab = start.shape[0] - 1
+    if nvocab >> 31:
+        _fits(ntok, nvocab)
+    if accumulate and out is None:
+        raise ValueError("accumulate needs the out to add to")
+    dW = torch.empty((nvocab, H), dtype=wd, device=dy.device) if out is None else out
+    wp, wn, work = _work_ptr(work, dp_embed_grad_work_bytes(ntok, H, dtype) if work is None else 0, dy, dev)
+    _run(dev, _ROW_FN["embed_grad"][dtype], _p(dy, "dy", dtype, (ntok, H), dev), _p(ids, "ids", torch.int32, (ntok,), dev),
+         _p(start, "start", torch.int64, (nvocab + 1,), dev), _p(src, "src", torch.int32, (ntok,), dev), ntok, nvocab, H,
+         scale, bool(accumulate), _p(dW, "out", wd, (nvocab, H), dev), wp, wn)
+    return dW
 
 
 _NORMS = {"rms": 0, "layer": 1}

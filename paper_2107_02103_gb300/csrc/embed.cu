@@ -1,0 +1,502 @@
+// Embedding of ids (atom types) and its gradient.
+//   y[t]  = add[t] + scale W[id_t]                 an id outside [0, nvocab) adds nothing
+//   dW[v] = (dW[v] +) scale sum_{t: id_t = v} dy[t]
+// The gradient's sums run over the tokens sorted by id, in their order, cut at multiples of a number of rows that
+// the sizes alone give, and the pieces of a cut run are added in order: no atomics, results repeat bit for bit.
+// All are bound by memory.
+#include "rows.cuh"
+
+namespace dpc {
+namespace {
+
+constexpr int kMaxVocab = (1 << 24) - 1, kMaxH = 1 << 20;
+
+// ------------------------------------------------------------------ the plan: a stable radix sort of the ids
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortPer = 4, kSortBlock = kSortThreads * kSortPer;
+constexpr int kDigits = 256;
+
+// Ids as sort keys: nvocab for those that stand for no row.
+__device__ __forceinline__ uint32_t sort_key(int32_t id, int nvocab) {
+  return (uint32_t)id < (uint32_t)nvocab ? (uint32_t)id : (uint32_t)nvocab;
+}
+
+// A thread's kSortPer items of a block in order by warp, 32 apart: the warp counts them by digit.
+struct SortItems {
+  uint32_t key[kSortPer];
+  int64_t first;
+};
+
+// The place of every item of a block in a digit, after the warps before it and those before it in its warp.  cnt: a row
+// of kDigits counters a warp, from counts to the warp's next place.
+__device__ __forceinline__ void count_digits(const SortItems &it, int64_t n, int shift, int mask, int *mine) {
+#pragma unroll
+  for (int i = 0; i < kSortPer; ++i)
+    if (it.first + 32 * i < n) atomicAdd(mine + (it.key[i] >> shift & mask), 1);  // integers: any order gives the same
+}
+
+__device__ __forceinline__ int take_place(uint32_t d, bool have, int lane, int *mine) {
+  const unsigned same = __match_any_sync(0xffffffffu, have ? d : 0xffffffffu);
+  const int p = have ? mine[d] + __popc(same & ((1u << lane) - 1)) : 0;
+  __syncwarp();
+  if (have && lane == __ffs(same) - 1) mine[d] += __popc(same);
+  __syncwarp();
+  return p;
+}
+
+// An exclusive scan of 256 values by the first 256 threads of a block (all threads call).
+__device__ __forceinline__ int scan_digits(int v, int *sums) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int inc = v;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += up;
+  }
+  if (lane == 31 && warp < kDigits / 32) sums[warp] = inc;
+  __syncthreads();
+  int before = 0;
+  for (int w = 0; w < kDigits / 32; ++w) before += w < warp ? sums[w] : 0;
+  __syncthreads();
+  return before + inc - v;
+}
+
+// start[v] = the first of n sorted keys that is at least v.
+__device__ __forceinline__ int lower_bound(const uint32_t *keys, int n, uint32_t v) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (keys[mid] < v) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Up to kSortBlock ids in one block, all digits in shared memory.
+constexpr size_t kSmallSmem = (size_t)(kSortWarps * kDigits + 4 * kSortBlock + kSortWarps) * sizeof(int);
+__global__ void __launch_bounds__(kSortThreads)
+    embed_plan_small_kernel(const int32_t *__restrict__ ids, int n, int nvocab, int passes, int bits,
+                            int64_t *__restrict__ start, int32_t *__restrict__ src) {
+  extern __shared__ int smem[];
+  int *cnt = smem, *sums = cnt + kSortWarps * kDigits;
+  uint32_t *keys = (uint32_t *)(sums + kSortWarps);
+  int *idx = (int *)(keys + 2 * kSortBlock);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, mask = (1 << bits) - 1;
+  SortItems it;
+  int id[kSortPer];
+  it.first = warp * kSortPer * 32 + lane;
+#pragma unroll
+  for (int i = 0; i < kSortPer; ++i) {
+    id[i] = (int)it.first + 32 * i;
+    it.key[i] = id[i] < n ? sort_key(__ldg(ids + id[i]), nvocab) : 0u;
+  }
+  for (int pass = 0; pass < passes; ++pass) {
+    for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) cnt[i] = 0;
+    __syncthreads();
+    int *mine = cnt + warp * kDigits;
+    const int shift = pass * bits;
+    count_digits(it, n, shift, mask, mine);
+    __syncthreads();
+    int total = 0;
+    if (threadIdx.x < kDigits)
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) total += cnt[w * kDigits + threadIdx.x];
+    int run = scan_digits(total, sums);
+    if (threadIdx.x < kDigits)
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) {
+        const int c = cnt[w * kDigits + threadIdx.x];
+        cnt[w * kDigits + threadIdx.x] = run;
+        run += c;
+      }
+    __syncthreads();
+    uint32_t *to_k = keys + (pass & 1) * kSortBlock;
+    int *to_i = idx + (pass & 1) * kSortBlock;
+#pragma unroll
+    for (int i = 0; i < kSortPer; ++i) {
+      const bool have = it.first + 32 * i < n;
+      const int p = take_place(it.key[i] >> shift & mask, have, lane, mine);
+      if (have) {
+        to_k[p] = it.key[i];
+        to_i[p] = id[i];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSortPer; ++i)
+      if (it.first + 32 * i < n) {
+        it.key[i] = to_k[it.first + 32 * i];
+        id[i] = to_i[it.first + 32 * i];
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < kSortPer; ++i)
+    if (it.first + 32 * i < n) src[it.first + 32 * i] = it.key[i] < (uint32_t)nvocab ? id[i] : -1;
+  const uint32_t *sorted = keys + ((passes - 1) & 1) * kSortBlock;
+  for (int v = threadIdx.x; v <= nvocab; v += kSortThreads) start[v] = lower_bound(sorted, n, v);
+}
+
+// More ids, a pass of a digit: counts[d][block], each digit's scan over the blocks with its total behind, and the move.
+__global__ void __launch_bounds__(kSortThreads)
+    sort_count_kernel(const int32_t *__restrict__ ids, const uint32_t *__restrict__ keys, int64_t n, int nvocab, int shift,
+                      int mask, int *__restrict__ counts) {
+  __shared__ int cnt[kDigits];
+  if (threadIdx.x < kDigits) cnt[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t first = (int64_t)blockIdx.x * kSortBlock + threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < kSortPer; ++i) {
+    const int64_t q = first + (int64_t)i * kSortThreads;
+    if (q < n) atomicAdd(cnt + ((keys ? __ldg(keys + q) : sort_key(__ldg(ids + q), nvocab)) >> shift & mask), 1);
+  }
+  __syncthreads();
+  if (threadIdx.x < kDigits) counts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = cnt[threadIdx.x];
+}
+
+__global__ void __launch_bounds__(kDigits) sort_scan_kernel(int *__restrict__ counts, int nb, int *__restrict__ totals) {
+  __shared__ int sums[kDigits / 32], chunk;
+  int *row = counts + (int64_t)blockIdx.x * nb;
+  int base = 0;
+  for (int b0 = 0; b0 < nb; b0 += kDigits) {
+    const int b = b0 + threadIdx.x, c = b < nb ? row[b] : 0;
+    const int before = scan_digits(c, sums);
+    if (b < nb) row[b] = base + before;
+    if (threadIdx.x == kDigits - 1) chunk = before + c;
+    __syncthreads();
+    base += chunk;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) totals[blockIdx.x] = base;
+}
+
+__global__ void __launch_bounds__(kSortThreads)
+    sort_place_kernel(const int32_t *__restrict__ ids, const uint32_t *__restrict__ keys, const int *__restrict__ idx,
+                      int64_t n, int nvocab, int shift, int mask, const int *__restrict__ counts,
+                      const int *__restrict__ totals, uint32_t *__restrict__ to_key, int *__restrict__ to_idx, bool last) {
+  __shared__ int cnt[kSortWarps * kDigits], sums[kSortWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) cnt[i] = 0;
+  SortItems it;
+  int id[kSortPer];
+  it.first = (int64_t)blockIdx.x * kSortBlock + warp * kSortPer * 32 + lane;
+#pragma unroll
+  for (int i = 0; i < kSortPer; ++i) {
+    const int64_t q = it.first + 32 * i;
+    it.key[i] = q >= n ? 0u : keys ? __ldg(keys + q) : sort_key(__ldg(ids + q), nvocab);
+    id[i] = q >= n ? 0 : idx ? __ldg(idx + q) : (int)q;
+  }
+  __syncthreads();
+  int *mine = cnt + warp * kDigits;
+  count_digits(it, n, shift, mask, mine);
+  __syncthreads();
+  const int d = threadIdx.x;
+  int run = scan_digits(d < kDigits ? __ldg(totals + d) : 0, sums);
+  if (d < kDigits) {
+    run += __ldg(counts + (int64_t)d * gridDim.x + blockIdx.x);
+#pragma unroll 8
+    for (int w = 0; w < kSortWarps; ++w) {
+      const int c = cnt[w * kDigits + d];
+      cnt[w * kDigits + d] = run;
+      run += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSortPer; ++i) {
+    const bool have = it.first + 32 * i < n;
+    const int p = take_place(it.key[i] >> shift & mask, have, lane, mine);
+    if (have) {
+      to_key[p] = it.key[i];
+      to_idx[p] = last && it.key[i] >= (uint32_t)nvocab ? -1 : id[i];
+    }
+  }
+}
+
+__global__ void __launch_bounds__(256)
+    embed_start_kernel(const uint32_t *__restrict__ keys, int n, int nvocab, int64_t *__restrict__ start) {
+  const int v = blockIdx.x * 256 + threadIdx.x;
+  if (v <= nvocab) start[v] = lower_bound(keys, n, v);
+}
+
+struct SortShape {
+  int blocks, passes, bits;
+};
+SortShape sort_shape(int64_t n, int nvocab) {
+  int bits = 1;
+  while (nvocab >> bits) ++bits;  // keys up to nvocab
+  SortShape s;
+  s.passes = (bits + 7) / 8;
+  s.bits = (bits + s.passes - 1) / s.passes;
+  s.blocks = (int)((n + kSortBlock - 1) / kSortBlock);
+  return s;
+}
+
+// ------------------------------------------------------------------ the rows
+// V elements an access; a row's packs go to np threads in order, rows after rows.
+template <typename T, int V>
+__global__ void __launch_bounds__(128)
+    embed_fwd_kernel(const T *__restrict__ W, const int32_t *__restrict__ ids, int64_t ntok, int nvocab, int H, int np,
+                     acc_t<T> scale, const T *add, T *y) {  // y may be add
+  using A = acc_t<T>;
+  const int64_t base = (int64_t)blockIdx.x * 128, t0 = base / np;
+  const uint32_t off = (uint32_t)(base - t0 * np) + threadIdx.x, dt = off / (uint32_t)np;
+  const int64_t t = t0 + dt;
+  const int c = (int)(off - dt * np) * V;
+  if (t >= ntok) return;
+  const int32_t id = __ldg(ids + t);
+  const bool have = (uint32_t)id < (uint32_t)nvocab;
+  Pack<T, V> a{}, w{};
+  if (add) a = load_pack<T, V>(add + t * H + c);
+  if (have) w = load_pack<T, V>(W + (int64_t)id * H + c);
+  Pack<T, V> o;
+#pragma unroll
+  for (int l = 0; l < V; ++l) {
+    const A from = add ? to_acc(a.v[l]) : A(0);
+    o.v[l] = from_acc<T>(have ? fma(scale, to_acc(w.v[l]), from) : from);
+  }
+  store_pack<T, V>(y + t * H + c, o);
+}
+
+// Blocks below `chunks x strips` sum a chunk of R sorted rows over a strip of columns: runs of an id that lie in the
+// chunk go to dW, what continues from the chunk before or into the next to `part` ([chunk][2][H]: the piece that begins
+// at the chunk's first row, and the one after it).  Further blocks clear the rows of ids that no token has.
+constexpr int kSumThreads = 256, kSumAhead = 8;
+template <typename T, int V>
+__global__ void __launch_bounds__(kSumThreads)
+    embed_grad_kernel(const T *__restrict__ dy, const int32_t *__restrict__ ids, const int64_t *__restrict__ start,
+                      const int32_t *__restrict__ src, int64_t ntok, int nvocab, int H, int np, int R, int chunks, int strips,
+                      acc_t<T> scale, bool accumulate, acc_t<T> *__restrict__ dW, acc_t<T> *__restrict__ part) {
+  using A = acc_t<T>;
+  if ((int)blockIdx.x >= chunks * strips) {
+    const int v = (int)blockIdx.x - chunks * strips;
+    if (__ldg(start + v) == __ldg(start + v + 1))
+      for (int c = threadIdx.x; c < H; c += kSumThreads) dW[(int64_t)v * H + c] = A(0);
+    return;
+  }
+  const int chunk = blockIdx.x / strips, strip = blockIdx.x - chunk * strips;
+  const int c = (strip * kSumThreads + threadIdx.x) * V;
+  const int64_t kept = min(max(__ldg(start + nvocab), (int64_t)0), ntok), r0 = (int64_t)chunk * R;
+  if (r0 >= kept || c >= H) return;
+  const int rows = (int)min((int64_t)R, kept - r0);
+  auto id_at = [&](int64_t p) -> int {  // of sorted row p; -1 where the plan is not one of these ids
+    const int q = __ldg(src + p);
+    return q >= 0 && q < ntok ? __ldg(ids + q) : -1;
+  };
+  const int before = chunk ? id_at(r0 - 1) : -1, after = r0 + rows < kept ? id_at(r0 + rows) : -1;
+  A sum[V] = {};
+  int run = id_at(r0), first = 0;  // the run at hand and its first row
+  auto put = [&](int end) {        // its rows end before `end`
+    if ((uint32_t)run < (uint32_t)nvocab) {
+      const bool cut = (first == 0 && before == run) || (end == rows && after == run);
+      A *to = cut ? part + ((int64_t)chunk * 2 + (first ? 1 : 0)) * H + c : dW + (int64_t)run * H + c;
+#pragma unroll
+      for (int l = 0; l < V; ++l) to[l] = cut ? sum[l] : accumulate ? fma(scale, sum[l], to[l]) : scale * sum[l];
+    }
+#pragma unroll
+    for (int l = 0; l < V; ++l) sum[l] = A(0);
+  };
+  for (int r = 0; r < rows; r += kSumAhead) {
+    Pack<T, V> v[kSumAhead];
+    int id[kSumAhead];
+#pragma unroll
+    for (int i = 0; i < kSumAhead; ++i) {
+      const int q = r + i < rows ? __ldg(src + r0 + r + i) : -1;
+      const bool have = q >= 0 && q < ntok;
+      id[i] = have ? __ldg(ids + q) : -1;
+      v[i] = have ? load_pack<T, V>(dy + (int64_t)q * H + c) : Pack<T, V>{};
+    }
+#pragma unroll
+    for (int i = 0; i < kSumAhead; ++i)
+      if (r + i < rows) {
+        if (id[i] != run) {
+          put(r + i);
+          run = id[i];
+          first = r + i;
+        }
+#pragma unroll
+        for (int l = 0; l < V; ++l) sum[l] += to_acc(v[i].v[l]);
+      }
+  }
+  put(rows);
+}
+
+// The runs that chunks cut: the block of the first chunk that such a run continues into adds its pieces in order.
+template <typename A>
+__global__ void __launch_bounds__(kSumThreads)
+    embed_join_kernel(const int32_t *__restrict__ ids, const int64_t *__restrict__ start, const int32_t *__restrict__ src,
+                      int64_t ntok, int nvocab, int H, int R, int chunks, A scale, bool accumulate, A *__restrict__ dW,
+                      const A *__restrict__ part) {
+  const int chunk = blockIdx.x + 1, c = blockIdx.y * kSumThreads + threadIdx.x;
+  const int64_t kept = min(max(__ldg(start + nvocab), (int64_t)0), ntok), r0 = (int64_t)chunk * R;
+  if (r0 >= kept || c >= H) return;
+  const int q = __ldg(src + r0);
+  if (q < 0 || q >= ntok) return;
+  const int v = __ldg(ids + q);
+  if ((uint32_t)v >= (uint32_t)nvocab) return;
+  const int64_t s0 = __ldg(start + v), s1 = min(__ldg(start + v + 1), kept);
+  if (s0 < 0 || s0 >= r0 || s0 / R != chunk - 1) return;  // not cut here, or not here first
+  const int last = (int)((s1 - 1) / R);
+  A sum = part[((int64_t)(chunk - 1) * 2 + (s0 % R ? 1 : 0)) * H + c];
+#pragma unroll 8
+  for (int k = chunk; k <= last; ++k) sum += part[(int64_t)k * 2 * H + c];
+  A *to = dW + (int64_t)v * H + c;
+  *to = accumulate ? fma(scale, sum, *to) : scale * sum;
+}
+
+struct SumShape {
+  int R, chunks, strips;
+};
+// About two blocks' worth of rows an SM, in chunks of whole batches of loads.
+SumShape sum_shape(int64_t ntok, int np) {
+  SumShape s;
+  s.strips = (np + kSumThreads - 1) / kSumThreads;
+  const int64_t want = 152 * 4 / s.strips > 0 ? 152 * 4 / s.strips : 1;
+  int64_t R = (ntok + want - 1) / want;
+  R = (R + kSumAhead - 1) / kSumAhead * kSumAhead;
+  s.R = (int)(R < 16 ? 16 : R);
+  s.chunks = (int)((ntok + s.R - 1) / s.R);
+  return s;
+}
+// The chunks of rows of H elements, whether they move in packs or not.
+size_t part_bytes(int64_t ntok, int H, int elem) {
+  const int V = 16 / elem;
+  const SumShape a = sum_shape(ntok, (H + V - 1) / V), b = sum_shape(ntok, H);
+  const size_t n = (size_t)(a.chunks > b.chunks ? a.chunks : b.chunks);
+  return n * 2 * H * (elem == 8 ? 8 : 4);
+}
+
+int embed_check(int64_t ntok, int nvocab, const char *who) {
+  if (ntok < 0 || ntok > 0x7fffffffLL - kSortBlock) return set_error(DP_ERR_SHAPE, "%s: ntok = %lld", who, (long long)ntok);
+  if (nvocab < 1) return set_error(DP_ERR_SHAPE, "%s: nvocab = %d", who, nvocab);
+  if (nvocab > kMaxVocab) return set_error(DP_ERR_UNSUPPORTED, "%s: nvocab = %d > %d", who, nvocab, kMaxVocab);
+  return DP_OK;
+}
+int embed_check(int64_t ntok, int nvocab, int H, double scale, const char *who) {
+  const int rc = embed_check(ntok, nvocab, who);
+  if (rc) return rc;
+  if (H < 1 || H > kMaxH) return set_error(DP_ERR_SHAPE, "%s: row length %d outside [1, 2^20]", who, H);
+  if (!std::isfinite(scale)) return set_error(DP_ERR_SHAPE, "%s: scale = %g", who, scale);
+  return DP_OK;
+}
+
+template <typename T>
+int embed_fwd(const T *W, const int32_t *ids, int64_t ntok, int nvocab, int H, double scale, const T *add, T *y,
+              void *stream, const char *who) {
+  clear_error();
+  const int rc = embed_check(ntok, nvocab, H, scale, who);
+  if (rc || ntok == 0) return rc;
+  if (!W || !ids || !y) return set_error(DP_ERR_NULL, "%s: NULL array", who);
+  if (!at_elements(W, add, y) || !at_elements(ids)) return misaligned(who);
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool whole = pack_width<T>(H, W, add, y) >= V;
+  const int np = whole ? H / V : H;
+  const int64_t blocks = (ntok * np + 127) / 128;
+  if (blocks > 0x7fffffffLL) return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, H);
+  auto k = whole ? embed_fwd_kernel<T, V> : embed_fwd_kernel<T, 1>;
+  k<<<(unsigned)blocks, 128, 0, (cudaStream_t)stream>>>(W, ids, ntok, nvocab, H, np, (acc_t<T>)scale, add, y);
+  return launch_status(who);
+}
+
+template <typename T>
+int embed_grad(const T *dy, const int32_t *ids, const int64_t *start, const int32_t *src, int64_t ntok, int nvocab, int H,
+               double scale, int accumulate, acc_t<T> *dW, void *work, size_t work_bytes, void *stream, const char *who) {
+  using A = acc_t<T>;
+  clear_error();
+  const int rc = embed_check(ntok, nvocab, H, scale, who);
+  if (rc) return rc;
+  if (!start || !dW || (ntok > 0 && (!dy || !ids || !src))) return set_error(DP_ERR_NULL, "%s: NULL array", who);
+  if (!at_elements(dy) || !at_elements(ids, src) || !at_elements(start) || !at_elements(dW)) return misaligned(who);
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool whole = pack_width<T>(H, dy) >= V;
+  const int np = whole ? H / V : H;
+  const SumShape s = sum_shape(ntok, np);
+  if (s.chunks > 1) {
+    if (!work) return set_error(DP_ERR_NULL, "%s: work is NULL", who);
+    if (work_bytes < part_bytes(ntok, H, sizeof(T)) || ((uintptr_t)work & 15))
+      return set_error(DP_ERR_SHAPE, "%s: work buffer of %zu bytes is too short or misaligned", who, work_bytes);
+  }
+  const int64_t blocks = (int64_t)s.chunks * s.strips + (accumulate ? 0 : nvocab);
+  if (blocks == 0) return DP_OK;
+  if (blocks > 0x7fffffffLL) return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, H);
+  const cudaStream_t st = (cudaStream_t)stream;
+  auto k = whole ? embed_grad_kernel<T, V> : embed_grad_kernel<T, 1>;
+  k<<<(unsigned)blocks, kSumThreads, 0, st>>>(dy, ids, start, src, ntok, nvocab, H, np, s.R, s.chunks, s.strips, (A)scale,
+                                              accumulate != 0, dW, (A *)work);
+  if (s.chunks > 1)
+    embed_join_kernel<A><<<dim3(s.chunks - 1, (H + kSumThreads - 1) / kSumThreads), kSumThreads, 0, st>>>(
+        ids, start, src, ntok, nvocab, H, s.R, s.chunks, (A)scale, accumulate != 0, dW, (const A *)work);
+  return launch_status(who);
+}
+
+}  // namespace
+}  // namespace dpc
+
+extern "C" {
+
+size_t dp_embed_plan_work_bytes(int64_t ntok, int nvocab) {
+  if (ntok < 0 || ntok > 0x7fffffffLL - dpc::kSortBlock || nvocab < 1 || nvocab > dpc::kMaxVocab) return 0;
+  const dpc::SortShape s = dpc::sort_shape(ntok, nvocab);
+  if (s.blocks <= 1) return 1;
+  return ((size_t)ntok * 4 + (size_t)(s.blocks + 1) * dpc::kDigits) * sizeof(int);
+}
+
+int dp_embed_plan(const int32_t *ids, int64_t ntok, int nvocab, int64_t *start, int32_t *src, void *work,
+                  size_t work_bytes, void *stream) {
+  using namespace dpc;
+  const char *who = "dp_embed_plan";
+  clear_error();
+  int rc = embed_check(ntok, nvocab, who);
+  if (rc) return rc;
+  if (!start || (ntok > 0 && (!ids || !src))) return set_error(DP_ERR_NULL, "%s: NULL array", who);
+  if (!at_elements(ids, src) || !at_elements(start)) return misaligned(who);
+  const SortShape s = sort_shape(ntok, nvocab);
+  const cudaStream_t st = (cudaStream_t)stream;
+  if (s.blocks <= 1) {
+    rc = allow_smem((const void *)embed_plan_small_kernel, kSmallSmem, who);
+    if (rc) return rc;
+    embed_plan_small_kernel<<<1, kSortThreads, kSmallSmem, st>>>(ids, (int)ntok, nvocab, s.passes, s.bits, start, src);
+    return launch_status(who);
+  }
+  if (!work) return set_error(DP_ERR_NULL, "%s: work is NULL", who);
+  if (work_bytes < dp_embed_plan_work_bytes(ntok, nvocab) || ((uintptr_t)work & 15))
+    return set_error(DP_ERR_SHAPE, "%s: work buffer of %zu bytes is too short or misaligned", who, work_bytes);
+  uint32_t *keys[2] = {(uint32_t *)work, (uint32_t *)work + ntok};
+  int *idx[2] = {(int *)work + 2 * ntok, (int *)work + 3 * ntok}, *counts = (int *)work + 4 * ntok;
+  int *totals = counts + (int64_t)s.blocks * kDigits;
+  const int mask = (1 << s.bits) - 1;
+  for (int pass = 0; pass < s.passes; ++pass) {
+    const uint32_t *from = pass ? keys[(pass - 1) & 1] : nullptr;
+    const int *from_idx = pass ? idx[(pass - 1) & 1] : nullptr;
+    const bool last = pass == s.passes - 1;
+    sort_count_kernel<<<s.blocks, kSortThreads, 0, st>>>(ids, from, ntok, nvocab, pass * s.bits, mask, counts);
+    sort_scan_kernel<<<kDigits, kDigits, 0, st>>>(counts, s.blocks, totals);
+    sort_place_kernel<<<s.blocks, kSortThreads, 0, st>>>(ids, from, from_idx, ntok, nvocab, pass * s.bits, mask, counts, totals,
+                                                         keys[pass & 1], last ? src : idx[pass & 1], last);
+  }
+  embed_start_kernel<<<(nvocab + 256) / 256, 256, 0, st>>>(keys[(s.passes - 1) & 1], (int)ntok, nvocab, start);
+  return launch_status(who);
+}
+
+size_t dp_embed_grad_work_bytes(int64_t ntok, int H, int elem_bytes) {
+  if (ntok < 0 || ntok > 0x7fffffffLL - dpc::kSortBlock || H < 1 || H > dpc::kMaxH) return 0;
+  if (elem_bytes != 2 && elem_bytes != 4 && elem_bytes != 8) return 0;
+  const size_t n = dpc::part_bytes(ntok, H, elem_bytes);
+  return n ? n : 1;
+}
+
+#define DP_EMBED(X, C, T, W_)                                                                                        \
+  int dp_embed_fwd_##X(const C *W, const int32_t *ids, int64_t ntok, int nvocab, int H, double scale, const C *add,  \
+                       C *y, void *stream) {                                                                         \
+    return dpc::embed_fwd<T>((const T *)W, ids, ntok, nvocab, H, scale, (const T *)add, (T *)y, stream,              \
+                             "dp_embed_fwd_" #X);                                                                    \
+  }                                                                                                                  \
+  int dp_embed_grad_##X(const C *dy, const int32_t *ids, const int64_t *start, const int32_t *src, int64_t ntok,     \
+                        int nvocab, int H, double scale, int accumulate, W_ *dW, void *work, size_t work_bytes,      \
+                        void *stream) {                                                                              \
+    return dpc::embed_grad<T>((const T *)dy, ids, start, src, ntok, nvocab, H, scale, accumulate, dW, work,          \
+                              work_bytes, stream, "dp_embed_grad_" #X);                                              \
+  }
+DP_EMBED(f64, double, double, double)
+DP_EMBED(f32, float, float, float)
+DP_EMBED(bf16, uint16_t, __nv_bfloat16, float)
+DP_EMBED(f16, uint16_t, __half, float)
+
+}  // extern "C"

@@ -15,12 +15,6 @@ constexpr int kMaxK = 65536;  // |q w| <= 2^14: int32 sums hold 2^17 of them
 // ------------------------------------------------------------------ rows to 8 bits
 constexpr int kQuantKeep = 4;  // packs a lane keeps in registers; longer rows are read again (from L2)
 
-__device__ __forceinline__ float max_nan(float a, float b) {  // NaN wins
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-
 // rint(x r) as the low byte of a float: the product is rounded, then adding 1.5 2^23 leaves its nearest integer
 // (ties to even) in the low bits, without the slow conversions.
 __device__ __forceinline__ uint32_t to_byte(float x, float r) {
@@ -130,52 +124,6 @@ struct I8Args {
   int give_up;           // the stage of a block whose wait gives up (dp_give_up_at)
 };
 
-template <typename T>
-__device__ __forceinline__ void put_out(T *y, float v) {
-  if constexpr (sizeof(T) == 8) *y = (double)v;
-  else *y = from_acc<T>(v);
-}
-
-// Row tile `tile` of the sorted rows cut into tiles of at most R rows that lie in one expert: the expert (nexp for
-// the rows past start[nexp]) and its rows [r0, r1).  A warp looks at 32 experts at a time.
-__device__ __forceinline__ bool find_tile(const I8Args &p, int tile, int R, int &e, int &r0, int &r1) {
-  const int rows = p.rows;
-  if (!p.start) {
-    if (tile >= (rows + R - 1) / R) return false;
-    e = 0;
-    r0 = tile * R;
-    r1 = min(R, rows - r0) + r0;
-    return true;
-  }
-  const int lane = threadIdx.x & 31;
-  int before = 0;
-  for (int e0 = 0; e0 <= p.nexp; e0 += 32) {
-    const int k = e0 + lane;
-    int lo = 0, hi = 0;
-    if (k <= p.nexp) {
-      lo = k ? (int)min(max(__ldg(p.start + k), (int64_t)0), (int64_t)rows) : 0;
-      hi = k < p.nexp ? (int)min(max(__ldg(p.start + k + 1), (int64_t)lo), (int64_t)rows) : rows;
-    }
-    const int mine = (hi - lo + R - 1) / R;
-    int inc = mine;
-    for (int o = 1; o < 32; o <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += up;
-    }
-    const unsigned hit = __ballot_sync(0xffffffffu, before + inc > tile);
-    if (hit) {
-      const int who = __ffs(hit) - 1;
-      const int first = lo + (tile - (before + inc - mine)) * R;
-      e = e0 + who;
-      r0 = __shfl_sync(0xffffffffu, first, who);
-      r1 = min(R, __shfl_sync(0xffffffffu, hi, who) - r0) + r0;
-      return true;
-    }
-    before += __shfl_sync(0xffffffffu, inc, 31);
-  }
-  return false;
-}
-
 constexpr int kFewWarps = 8, kFewRows = 8;
 
 // A warp per output channel and tile of up to eight rows: weights read once per tile, 16 bytes a lane, four products an
@@ -183,7 +131,7 @@ constexpr int kFewWarps = 8, kFewRows = 8;
 template <typename T>
 __global__ void __launch_bounds__(kFewWarps * 32) linear_i8_few_kernel(const I8Args p) {
   int e, r0, r1;
-  if (!find_tile(p, blockIdx.x, kFewRows, e, r0, r1)) return;
+  if (!find_tile(p.start, p.rows, p.nexp, blockIdx.x, kFewRows, e, r0, r1)) return;
   const int lane = threadIdx.x & 31, n = blockIdx.y * kFewWarps + (threadIdx.x >> 5), nr = r1 - r0;
   if (n >= p.N) return;
   T *y = (T *)p.y;
@@ -299,7 +247,7 @@ struct Tile {
 __device__ __forceinline__ void seek(const I8Args &p, int TN, int nct, Tile &t) {
   const int rt = t.tile / nct;
   t.n0 = (t.tile - rt * nct) * kTM;
-  t.have = find_tile(p, rt, TN, t.e, t.r0, t.r1);
+  t.have = find_tile(p.start, p.rows, p.nexp, rt, TN, t.e, t.r0, t.r1);
 }
 
 __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[8]) {

@@ -94,6 +94,58 @@ __device__ __forceinline__ Pack<T, 16 / (int)sizeof(T)> load_any(const T *p, con
   return out;
 }
 
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN wins
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void put_out(T *y, float v) {
+  if constexpr (sizeof(T) == 8) *y = (double)v;
+  else *y = from_acc<T>(v);
+}
+
+// Row tile `tile` of the sorted rows cut into tiles of at most R rows that lie in one expert: the expert (nexp for
+// the rows past start[nexp]) and its rows [r0, r1).  A warp looks at 32 experts at a time.
+__device__ __forceinline__ bool find_tile(const int64_t *start, int rows, int nexp, int tile, int R, int &e, int &r0,
+                                          int &r1) {
+  if (!start) {
+    if (tile >= (rows + R - 1) / R) return false;
+    e = 0;
+    r0 = tile * R;
+    r1 = min(R, rows - r0) + r0;
+    return true;
+  }
+  const int lane = threadIdx.x & 31;
+  int before = 0;
+  for (int e0 = 0; e0 <= nexp; e0 += 32) {
+    const int k = e0 + lane;
+    int lo = 0, hi = 0;
+    if (k <= nexp) {
+      lo = k ? (int)min(max(__ldg(start + k), (int64_t)0), (int64_t)rows) : 0;
+      hi = k < nexp ? (int)min(max(__ldg(start + k + 1), (int64_t)lo), (int64_t)rows) : rows;
+    }
+    const int mine = (hi - lo + R - 1) / R;
+    int inc = mine;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += up;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, before + inc > tile);
+    if (hit) {
+      const int who = __ffs(hit) - 1;
+      const int first = lo + (tile - (before + inc - mine)) * R;
+      e = e0 + who;
+      r0 = __shfl_sync(0xffffffffu, first, who);
+      r1 = min(R, __shfl_sync(0xffffffffu, hi, who) - r0) + r0;
+      return true;
+    }
+    before += __shfl_sync(0xffffffffu, inc, 31);
+  }
+  return false;
+}
+
 // Waits on an mbarrier give up after kPolls tries or when `stop`, looked at now and then, says so.  A block whose
 // wait gave up waits once more for its own copies in flight, leaves NaN and adds one to g_wait_timeouts.
 constexpr int kWaitPolls = 1 << 18;  // a try takes up to 4.5 us: about a second
