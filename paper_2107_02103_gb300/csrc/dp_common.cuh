@@ -25,6 +25,7 @@ void prof_mark(const char *name, cudaStream_t st);  // kernel timing hook (dp_pr
 int take_wait_timeouts_tabulate(unsigned int *count);  // GEMM wait timeouts per unit (dp_tc_wait_timeouts)
 int take_wait_timeouts_fitting(unsigned int *count);
 int take_wait_timeouts_linear_i8(unsigned int *count);
+int take_wait_timeouts_linear_mx4(unsigned int *count);
 int take_wait_timeouts_norm_fwd(unsigned int *count);
 int take_wait_timeouts_norm_grad(unsigned int *count);
 int give_up_at();  // the stage or row whose wait gives up in a test (dp_give_up_at), else INT_MAX

@@ -167,6 +167,7 @@ int dp_tc_wait_timeouts(unsigned int *count) {
   int rc = dpc::take_wait_timeouts_tabulate(count);
   if (!rc) rc = dpc::take_wait_timeouts_fitting(count);
   if (!rc) rc = dpc::take_wait_timeouts_linear_i8(count);
+  if (!rc) rc = dpc::take_wait_timeouts_linear_mx4(count);
   if (!rc) rc = dpc::take_wait_timeouts_norm_fwd(count);
   if (!rc) rc = dpc::take_wait_timeouts_norm_grad(count);
   return rc;

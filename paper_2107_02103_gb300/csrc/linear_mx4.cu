@@ -4,6 +4,8 @@
 //   negatives) to x_k 2^-e, ties to the even code, 6 for what lies above (amax 2^-e is below 8);  x_k ~ q_k 2^e
 //   y_in = act(sum_b 2^(e_ib + e_nb) sum_(k in b) q_ik w_nk + b_n)
 // Codes are sign, two exponent bits, one mantissa bit, two a byte with the lower four bits first; a scale is e + 127 in a byte.
+#include <cuda.h>
+
 #include "rows.cuh"
 
 namespace dpc {
@@ -83,6 +85,7 @@ struct Mx4Args {
   const int64_t *start;  // [nexp + 1], or NULL: one expert for all rows
   int rows, K, N, nexp, act;  // K: of the codes, a multiple of 64
   void *y;
+  int give_up;  // the stage of a block whose wait gives up (dp_give_up_at)
 };
 
 // Four codes (the lower 16 bits) as four int8, twice their values: a byte permutation looks up the magnitudes, and gives
@@ -160,6 +163,373 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
   }
 }
 
+// ------------------------------------------------------------------ the product on the tensor cores
+// A tile is 128 output channels (the MMA's rows) by up to TN sorted rows of one expert (its columns), so that an epilogue
+// warp holds 32 neighbouring channels of a row and stores them side by side.  The block-scaled MMA takes codes and scales
+// as they are: K 64 an instruction, a scale for 32.
+//   One lane copies a stage's codes, 256 of K, by tensor-map copies into K-major rows of 128 bytes in the 128-byte swizzle
+//   (a map reads zeros past the arrays; rows of another expert or past N land in columns and rows that nobody reads).
+//   Four warps bring the scales, a row of either operand a thread, eight scales a stage, read four stages ahead: in shared
+//   memory 128 rows' four scales of 128 of K are 512 bytes, row r at 16 (r % 32) + 4 (r / 32), which is how they go to
+//   the tensor memory's columns (repeated in its four lane quadrants).
+//   One lane issues a stage's copies to tensor memory and its MMAs; scales have two places there, taken in turn, and a place
+//   is written again when the MMAs that read it have completed.
+//   Eight epilogue warps (two per lane quadrant, half the columns each) finish a tile while the next one runs.
+// A block per SM walks the tiles; every wait is bounded, a block that gives up writes NaN and is counted.
+namespace mx4 {
+constexpr int kTM = 128, kKB = 256, kRowBytes = kKB / 2;
+constexpr int kEpiWarps = 8, kScaleWarps = 4, kCopyWarp = kEpiWarps + kScaleWarps, kMmaWarp = kCopyWarp + 1;
+constexpr int kThreads = (kMmaWarp + 1) * 32;
+constexpr int kAhead = 4;  // stages a thread's scales are read ahead
+
+template <int TN>
+struct Shape {
+  static constexpr int kA = kTM * kRowBytes, kB = TN * kRowBytes, kSA = 1024, kBlocksB = (TN + 127) / 128, kSB = 1024 * kBlocksB;
+  static constexpr int kStageBytes = kA + kB + kSA + kSB;
+  static constexpr int kStages = TN > 128 ? 4 : TN > 64 ? 6 : 8;
+  // an accumulator and a place of scales in each half of the columns
+  static constexpr uint32_t kHalf = TN > 128 ? 256 : TN > 64 ? 256 : 128, kTmemCols = 2 * kHalf, kScaleAt = TN;
+  static constexpr uint32_t kColsA = 4, kColsB = 4 * kBlocksB;  // of 128 of K
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (3 * kStages + 5) * 8 + 16;  // aligned within
+  static_assert(kStageBytes % 1024 == 0 && kSmem <= 227 * 1024 && TN % 32 == 0 && TN + 2 * (kColsA + kColsB) <= kHalf, "tile");
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// Shared-memory descriptors, version 1: codes K-major in the 128-byte swizzle (8 rows are 1024 bytes), scales as 32 rows
+// of 16 bytes without swizzle (8 rows are 128 bytes).
+__device__ __forceinline__ uint64_t code_desc(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFF) >> 4) | (1ull << 16) | ((uint64_t)(8 * kRowBytes >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFF) >> 4) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
+}
+__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t saddr) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(scale_desc(saddr)) : "memory");
+}
+__device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+        "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(addr));
+}
+__device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+               "l"((uint64_t)map), "r"(x), "r"(y), "r"(bar)
+               : "memory");
+}
+
+// Where a role stands: the tile, and the expert, rows and channels it means.
+struct Tile {
+  int tile, r0, r1, e, n0;
+  bool have;
+};
+__device__ __forceinline__ void seek(const Mx4Args &p, int TN, int nct, Tile &t) {
+  const int rt = t.tile / nct;
+  t.n0 = (t.tile - rt * nct) * kTM;
+  t.have = find_tile(p.start, p.rows, p.nexp, rt, TN, t.e, t.r0, t.r1);
+}
+// The next tile with products, from t on.
+__device__ __forceinline__ void seek_work(const Mx4Args &p, int TN, int nct, Tile &t) {
+  for (;; t.tile += gridDim.x) {
+    seek(p, TN, nct, t);
+    if (!t.have || t.e < p.nexp) return;
+  }
+}
+
+template <typename T, int TN>
+__global__ void __launch_bounds__(kThreads, 1)
+    linear_mx4_tc_kernel(const Mx4Args p, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap) {
+  using S = Shape<TN>;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
+  uint64_t *codes = reinterpret_cast<uint64_t *>(smem + S::kStages * S::kStageBytes), *scales = codes + S::kStages;
+  uint64_t *empty = scales + S::kStages, *acc_full = empty + S::kStages, *acc_empty = acc_full + 2, *done = acc_empty + 2;
+  uint32_t *holder = reinterpret_cast<uint32_t *>(done + 1);
+  volatile int *stop = reinterpret_cast<int *>(holder + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int nct = (p.N + kTM - 1) / kTM, nkb = (p.K + kKB - 1) / kKB;
+  auto wait = [&](uint64_t *bar, uint32_t parity) {  // gives up with any other wait of the block
+    return bounded_wait(smem_u32(bar), parity, [&] { return *stop != 0; });
+  };
+  auto wait_on = [&](uint64_t *bar, uint32_t parity) {  // for what is in flight, come what may
+    return bounded_wait(smem_u32(bar), parity, [] { return false; });
+  };
+
+  if (threadIdx.x == 0) {
+    auto init = [](uint64_t *b, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(n)); };
+    for (int s = 0; s < S::kStages; ++s) {
+      init(codes + s, 1);
+      init(scales + s, kScaleWarps);
+      init(empty + s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      init(acc_full + b, 1);
+      init(acc_empty + b, kEpiWarps);
+    }
+    init(done, 1);
+    *stop = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(holder)),
+                 "r"(S::kTmemCols));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;");
+  const uint32_t tmem = *holder;
+  bool ok = true;
+  int copied = 0;  // stages copied
+
+  if (warp == kMmaWarp) {
+    // ---------------------------------------------------------------- the MMAs
+    int j = 0, unit = 0;  // stages, tiles
+    Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
+    for (; ok; t.tile += gridDim.x, ++unit) {
+      seek_work(p, TN, nct, t);
+      if (!t.have) break;
+      const uint32_t cols = (uint32_t)(t.r1 - t.r0 + 15) / 16 * 16;
+      // fp4 operands, K-major; scales are powers of two
+      const uint32_t idesc = (1u << 7) | (1u << 10) | ((cols >> 3) << 17) | (1u << 23) | ((uint32_t)(kTM >> 7) << 27);
+      if (lane == 0) {
+        const int buf = unit & 1;
+        if (unit >= 2) ok = wait(acc_empty + buf, ((unit >> 1) - 1) & 1);
+        const int end = min(nkb, p.give_up - j);
+        const uint32_t acc = tmem + buf * S::kHalf;
+        for (int kb = 0; kb < end && ok; ++kb, ++j) {
+          const int st = j % S::kStages, par = (j / S::kStages) & 1, at = j & 1;
+          ok = wait(codes + st, par) && wait(scales + st, par);
+          if (ok && j >= 2) ok = wait(empty + (j - 2) % S::kStages, ((j - 2) / S::kStages) & 1);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;");
+          const uint32_t base = smem_u32(smem) + st * S::kStageBytes, sa = base + S::kA + S::kB, sb = sa + S::kSA;
+          const uint32_t ta = tmem + at * S::kHalf + S::kScaleAt, tb = ta + 2 * S::kColsA;
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            scales_to_tmem(ta + g * S::kColsA, sa + g * 512);
+#pragma unroll
+            for (int b = 0; b < S::kBlocksB; ++b) scales_to_tmem(tb + g * S::kColsB + 4 * b, sb + (g * S::kBlocksB + b) * 512);
+          }
+          const uint64_t a0 = code_desc(base), b0 = code_desc(base + S::kA);
+#pragma unroll
+          for (int k = 0; k < kKB / 64; ++k) {
+            if (kb * kKB + k * 64 >= p.K) break;
+            const uint32_t which = (uint32_t)(k & 1) * 2, id = idesc | (which << 4) | (which << 29);  // a word's lower or upper two scales
+            asm volatile(
+                "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+                " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(acc),
+                "l"(a0 + (uint64_t)(k * 2)), "l"(b0 + (uint64_t)(k * 2)), "r"(id), "r"(ta + (k >> 1) * S::kColsA),
+                "r"(tb + (k >> 1) * S::kColsB), "r"(kb > 0 || k > 0 ? 1u : 0u)
+                : "memory");
+          }
+          commit(smem_u32(empty + st));
+          if (kb == nkb - 1) commit(smem_u32(acc_full + buf));
+        }
+        ok = ok && end == nkb;
+      }
+      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    }
+    if (lane == 0) commit(smem_u32(done));  // completes when every MMA issued above has
+    if (!ok) *stop = 1;
+  } else if (warp == kCopyWarp) {
+    // ---------------------------------------------------------------- the codes
+    Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
+    for (; ok; t.tile += gridDim.x) {
+      seek_work(p, TN, nct, t);
+      if (!t.have) break;
+      if (lane == 0) {
+        for (int kb = 0; kb < nkb; ++kb) {
+          const int st = copied % S::kStages;
+          ok = wait(empty + st, (copied / S::kStages & 1) ^ 1);
+          if (!ok) break;
+          const uint32_t bar = smem_u32(codes + st), dst = smem_u32(smem) + st * S::kStageBytes;
+          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)(S::kA + S::kB))
+                       : "memory");
+          copy_tile(dst, &wmap, kb * kRowBytes, t.e * p.N + t.n0, bar);
+          copy_tile(dst + S::kA, &xmap, kb * kRowBytes, t.r0, bar);
+          ++copied;
+        }
+      }
+      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    }
+    if (!ok) *stop = 1;
+  } else if (warp >= kEpiWarps) {
+    // ---------------------------------------------------------------- the scales
+    const int r = threadIdx.x - kEpiWarps * 32, lds = scale_cols(p.K);
+    Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
+    const uint8_t *a = nullptr, *b0 = nullptr, *b1 = nullptr;  // this thread's rows at the stage to be read next
+    int kb = 0;
+    auto enter = [&] {
+      kb = 0;
+      if (!t.have) return;
+      a = t.n0 + r < p.N ? p.sw + ((int64_t)t.e * p.N + t.n0 + r) * lds : nullptr;
+      b0 = r < t.r1 - t.r0 ? p.sx + (int64_t)(t.r0 + r) * lds : nullptr;
+      b1 = S::kBlocksB > 1 && r + 128 < t.r1 - t.r0 ? p.sx + (int64_t)(t.r0 + r + 128) * lds : nullptr;
+    };
+    seek_work(p, TN, nct, t);
+    enter();
+    uint2 va[kAhead], v0[kAhead], v1[kAhead];
+    bool live[kAhead];
+    auto read = [&](int d) {
+      const uint2 zero = make_uint2(0, 0);
+      live[d] = t.have;
+      va[d] = t.have && a ? __ldg(reinterpret_cast<const uint2 *>(a) + kb) : zero;
+      v0[d] = t.have && b0 ? __ldg(reinterpret_cast<const uint2 *>(b0) + kb) : zero;
+      if constexpr (S::kBlocksB > 1) v1[d] = t.have && b1 ? __ldg(reinterpret_cast<const uint2 *>(b1) + kb) : zero;
+      if (t.have && ++kb == nkb) {
+        t.tile += gridDim.x;
+        seek_work(p, TN, nct, t);
+        enter();
+      }
+    };
+#pragma unroll
+    for (int d = 0; d < kAhead; ++d) read(d);
+    const uint32_t at = smem_u32(smem) + S::kA + S::kB + (r % 32) * 16 + (r / 32) * 4;
+    auto put = [&](uint32_t to, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(v) : "memory"); };
+    bool more = true;
+    for (int j = 0; more;) {
+#pragma unroll
+      for (int d = 0; d < kAhead; ++d) {
+        more = more && live[d];
+        if (!more) break;
+        const int st = j % S::kStages;
+        ok = __all_sync(0xffffffffu, wait(empty + st, (j / S::kStages & 1) ^ 1));
+        more = ok;
+        if (!more) break;
+        const uint32_t to = at + st * S::kStageBytes;
+        put(to, va[d].x);
+        put(to + 512, va[d].y);
+        put(to + S::kSA, v0[d].x);
+        put(to + S::kSA + 512 * S::kBlocksB, v0[d].y);
+        if constexpr (S::kBlocksB > 1) {
+          put(to + S::kSA + 512, v1[d].x);
+          put(to + S::kSA + 512 * 3, v1[d].y);
+        }
+        read(d);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) arrive(smem_u32(scales + st));
+        ++j;
+      }
+    }
+    if (!ok) *stop = 1;
+  } else {
+    // ---------------------------------------------------------------- epilogue
+    constexpr int CW = TN / 2;  // columns of this warp
+    const int quad = warp & 3, c0 = (warp >> 2) * CW;
+    const uint32_t trow = tmem + ((uint32_t)(32 * quad) << 16) + c0;
+    T *y = (T *)p.y;
+    int unit = 0;
+    Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
+    for (;; t.tile += gridDim.x) {
+      seek(p, TN, nct, t);
+      if (!t.have) break;
+      const int n = t.n0 + 32 * quad + lane, nr = t.r1 - t.r0;
+      const bool mine = n < p.N;
+      if (t.e == p.nexp) {
+        if (mine)
+          for (int c = c0; c < min(nr, c0 + CW); ++c) put_out(y + (int64_t)(t.r0 + c) * p.N + n, 0.0f);
+        continue;
+      }
+      const float bias = mine && p.bias ? __ldg(p.bias + (int64_t)t.e * p.N + n) : 0.0f;
+      ok = __all_sync(0xffffffffu, ok && wait(acc_full + (unit & 1), (unit >> 1) & 1));
+      asm volatile("tcgen05.fence::after_thread_sync;");
+      T *out = y + (int64_t)(t.r0 + c0) * p.N + n;
+#pragma unroll 1
+      for (int g = 0; g < CW && c0 + g < nr; g += 16, out += (int64_t)16 * p.N) {
+        const int left = nr - c0 - g;
+        float v[16];
+        if (ok) {
+          tmem_ld(trow + (unit & 1) * S::kHalf + g, v);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = ok ? v[i] + bias : __uint_as_float(0x7fc00000u);
+        if (p.act == DP_ACT_TANH) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = tanhf(v[i]);
+        }
+        T *o = out;
+        if (mine) {
+          if (left >= 16) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i, o += p.N) put_out(o, v[i]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i, o += p.N)
+              if (i < left) put_out(o, v[i]);
+          }
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;");
+      __syncwarp();
+      if (lane == 0) arrive(smem_u32(acc_empty + (unit & 1)));
+      ++unit;
+    }
+    if (!ok) *stop = 1;
+  }
+  __syncwarp();
+  __syncthreads();
+  ok = wait_on(done, 0) && !*stop;  // no MMA is in flight when the accumulators go
+  if (!__syncthreads_and(ok)) {
+    if (threadIdx.x == 0) atomicAdd(&g_wait_timeouts, 1u);
+    if (warp == kCopyWarp && lane == 0)  // nor any copy
+      for (int i = max(0, copied - S::kStages); i < copied; ++i) wait_on(codes + i % S::kStages, i / S::kStages & 1);
+    __syncthreads();
+  }
+  asm volatile("tcgen05.fence::after_thread_sync;");
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmemCols));
+}
+
+// The driver's encoder of tensor maps, looked up once.
+using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                              const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encoder() {
+  static const EncodeFn fn = [] {
+    void *f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return (EncodeFn)f;
+  }();
+  return fn;
+}
+
+// Rows of `bytes` bytes, in boxes of `box` rows by 128 bytes.
+bool make_map(CUtensorMap *m, const void *base, int64_t rows, int bytes, int box) {
+  const EncodeFn fn = encoder();
+  const cuuint64_t dims[2] = {(cuuint64_t)bytes, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)bytes};
+  const cuuint32_t boxes[2] = {(cuuint32_t)kRowBytes, (cuuint32_t)box}, steps[2] = {1, 1};
+  return fn && fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, boxes, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int TN>
+int launch_tc(const Mx4Args &p, int64_t row_tiles, cudaStream_t st, const char *who) {
+  using S = Shape<TN>;
+  auto k = linear_mx4_tc_kernel<T, TN>;
+  const int rc = allow_smem((const void *)k, S::kSmem, who);
+  if (rc) return rc;
+  CUtensorMap xmap, wmap;
+  if (!make_map(&xmap, p.xq, p.rows, p.K / 2, TN) || !make_map(&wmap, p.wq, (int64_t)p.nexp * p.N, p.K / 2, kTM))
+    return set_error(DP_ERR_CUDA, "%s: no tensor map", who);
+  const int64_t tiles = row_tiles * ((p.N + kTM - 1) / kTM);
+  k<<<(unsigned)(tiles < 152 ? tiles : 152), kThreads, S::kSmem, st>>>(p, xmap, wmap);
+  return DP_OK;
+}
+}  // namespace mx4
+
 template <typename T>
 int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok, int topk, int K, uint8_t *xq, uint8_t *sx,
                void *stream, const char *who) {
@@ -184,6 +554,18 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
   return launch_status(who);
 }
 
+// Which kernel: tiles of more rows need fewer rounds over 152 SMs, but a round of them takes longer.
+enum Mx4Form { kFew, kTiles64, kTiles128, kTiles224 };
+Mx4Form form_of(int64_t rows, int N, int nexp) {
+  if (rows <= 16) return kFew;
+  auto cost = [&](int R) {
+    const int64_t rounds = (((rows + R - 1) / R + nexp / 2) * ((N + mx4::kTM - 1) / mx4::kTM) + 151) / 152;
+    return rounds * (R + 64);
+  };
+  const int64_t c64 = cost(64), c128 = cost(128), c224 = cost(224);
+  return c224 < c128 && c224 < c64 ? kTiles224 : c128 < c64 ? kTiles128 : kTiles64;
+}
+
 template <typename T>
 int linear(const uint8_t *xq, const uint8_t *sx, int64_t rows, int K, const uint8_t *wq, const uint8_t *sw, const float *bias,
            int nexp, int N, const int64_t *start, int act, T *y, void *stream, const char *who) {
@@ -200,16 +582,29 @@ int linear(const uint8_t *xq, const uint8_t *sx, int64_t rows, int K, const uint
   if ((((uintptr_t)xq | (uintptr_t)wq) & 15) || (((uintptr_t)sx | (uintptr_t)sw) & 7))
     return set_error(DP_ERR_SHAPE, "%s: xq, wq, sx or sw is not aligned", who);
   if (!at_elements(y) || !at_elements(bias) || !at_elements(start)) return misaligned(who);
-  const Mx4Args p{xq, sx, wq, sw, bias, start, (int)rows, K, N, nexp, act, y};
+  const Mx4Args p{xq, sx, wq, sw, bias, start, (int)rows, K, N, nexp, act, y, give_up_at()};
   const cudaStream_t st = (cudaStream_t)stream;
   const int64_t pieces = start ? (nexp + 1 < rows ? nexp + 1 : rows) : 0;  // a tile more for each expert's remainder
   auto tiles = [&](int R) { return (rows + R - 1) / R + pieces; };
-  const dim3 grid((unsigned)tiles(kFewRows), (N + kFewWarps - 1) / kFewWarps);
-  linear_mx4_few_kernel<T><<<grid, kFewWarps * 32, 0, st>>>(p);
+  int rc = DP_OK;
+  switch (form_of(rows, N, nexp)) {
+    case kFew: {
+      const dim3 grid((unsigned)tiles(kFewRows), (N + kFewWarps - 1) / kFewWarps);
+      linear_mx4_few_kernel<T><<<grid, kFewWarps * 32, 0, st>>>(p);
+      break;
+    }
+    case kTiles64: rc = mx4::launch_tc<T, 64>(p, tiles(64), st, who); break;
+    case kTiles128: rc = mx4::launch_tc<T, 128>(p, tiles(128), st, who); break;
+    case kTiles224: rc = mx4::launch_tc<T, 224>(p, tiles(224), st, who); break;
+  }
+  if (rc) return rc;
   return launch_status(who);
 }
 
 }  // namespace
+
+int take_wait_timeouts_linear_mx4(unsigned int *count) { return take_unit_timeouts(count); }
+
 }  // namespace dpc
 
 extern "C" {

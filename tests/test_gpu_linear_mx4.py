@@ -95,11 +95,16 @@ def check(y, x, w, bias, act, dtype, what=""):
         ref = np.tanh(ref)
         b = np.minimum(b, 2.0) + 4 * 2.0 ** -24
     unit = max(UNIT[dtype], 2.0 ** -24)
+    # what lies beyond the row type's largest value rounds to an infinity: both count as that value
+    top = float(torch.finfo(dtype).max)
+    y, ref = np.clip(y if isinstance(y, np.ndarray) else f64(y), -top, top), np.clip(ref, -top, top)
     within(y, ref, b + (np.abs(ref) + b) * unit + TINY[dtype], what)
 
 
 PRODUCTS = [(1, 64, 1, 1), (1, 1600, 100, 1), (3, 240, 33, 1), (16, 1003, 70, 1), (17, 64, 5, 1), (17, 1237, 517, 1), (64, 256, 128, 1), (65, 512, 129, 1), (130, 320, 260, 1),
-            (300, 96, 17, 1), (500, 1600, 240, 1), (1000, 2048, 300, 1), (40, 4096, 64, 1), (2000, 64, 64, 1)]
+            (300, 96, 17, 1), (500, 1600, 240, 1), (1000, 2048, 300, 1), (40, 4096, 64, 1), (2000, 64, 64, 1),
+            # tiles of 128 and of 224 rows
+            (12000, 320, 260, 1), (30000, 64, 300, 1), (6000, 1088, 2100, 1)]
 
 
 @pytest.mark.parametrize("dtype", ROWS, ids=IDS)
@@ -153,7 +158,7 @@ def test_a_scale_of_nan_spoils_its_row_or_channel_only(n):
     check(y[np.ix_(~bad_r, ~bad_c)], M.values(M.pack(code), scale)[~bad_r], wv[0][~bad_c], np.zeros((~bad_c).sum()), None, torch.float32)
 
 
-EXPERTS = [(1, 2, 8, 240, 100), (6, 2, 3, 64, 9), (40, 2, 5, 96, 130), (400, 2, 13, 1237, 150), (300, 3, 61, 70, 31), (900, 1, 4, 320, 240), (700, 2, 2, 512, 64), (50, 1, 1024, 64, 7)]
+EXPERTS = [(1, 2, 8, 240, 100), (6, 2, 3, 64, 9), (40, 2, 5, 96, 130), (400, 2, 13, 1237, 150), (300, 3, 61, 70, 31), (900, 1, 4, 320, 240), (700, 2, 2, 512, 64), (50, 1, 1024, 64, 7), (9000, 2, 5, 96, 800)]
 
 
 @pytest.mark.parametrize("dtype", ROWS, ids=IDS)
@@ -213,3 +218,30 @@ def test_graph_and_repeats():
     xin.copy_(x)
     graph.replay()
     assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("stage", [0, 1, 2, 5, 23])
+@pytest.mark.parametrize("n,K,N", [(60, 64, 200), (700, 2304, 1000), (12000, 320, 260), (9000, 2048, 1300)])
+def test_waits_that_give_up(n, K, N, stage):
+    """Bounded waits that give up, as a test hook makes them: the outputs they leave are NaN, all others right, the count
+    says so, and the next call is sound."""
+    dpc = lib()
+    assert dpc.dp_tc_wait_timeouts() == 0
+    g = torch.Generator("cuda").manual_seed(n)
+    u8 = lambda lo, hi, *s: torch.randint(lo, hi, s, generator=g, dtype=torch.uint8, device="cuda")  # noqa: E731
+    lds = (K + 255) // 256 * 8
+    args = u8(0, 256, n, K // 2), u8(120, 130, n, lds), u8(0, 256, 1, N, K // 2), u8(120, 130, 1, N, lds)
+    good = dpc.dp_linear_mx4(*args)
+    assert not torch.isnan(good).any()
+    try:
+        dpc.dp_give_up_at(stage)
+        got = dpc.dp_linear_mx4(*args)
+    finally:
+        dpc.dp_give_up_at(-1)
+    count = dpc.dp_tc_wait_timeouts()
+    lost = torch.isnan(got)
+    assert torch.equal(got[~lost], good[~lost])
+    assert bool(lost.any()) == (count > 0) == (stage < -(-K // 256) or count > 0)
+    if stage == 0:
+        assert lost.all()
+    assert torch.equal(dpc.dp_linear_mx4(*args), good) and dpc.dp_tc_wait_timeouts() == 0
