@@ -18,7 +18,24 @@ __host__ __device__ constexpr int code_cols(int K) { return (K + 63) / 64 * 64; 
 __host__ __device__ constexpr int scale_cols(int K) { return (K + 255) / 256 * 8; }      // scales of a row
 
 // ------------------------------------------------------------------ rows to 4 bits
-// The codes of eight values, the first in the lowest bits.
+// The codes of two, four or eight values, the first in the lowest bits.
+__device__ __forceinline__ uint8_t to_codes(const float (&v)[2]) {
+  uint32_t r;
+  asm("{\n .reg .b8 a;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n mov.b32 %0, {a, a, a, a};\n}"
+      : "=r"(r)
+      : "f"(v[0]), "f"(v[1]));
+  return (uint8_t)r;
+}
+__device__ __forceinline__ uint16_t to_codes(const float (&v)[4]) {
+  uint32_t r;
+  asm("{\n .reg .b8 a, b;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+      " mov.b32 %0, {a, b, a, b};\n}"
+      : "=r"(r)
+      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]));
+  return (uint16_t)r;
+}
 __device__ __forceinline__ uint32_t to_codes(const float (&v)[8]) {
   uint32_t r;
   asm("{\n .reg .b8 a, b, c, d;\n"
@@ -32,48 +49,85 @@ __device__ __forceinline__ uint32_t to_codes(const float (&v)[8]) {
   return r;
 }
 
-// A warp takes 256 elements of a token's row, eight a lane, four lanes a scale.  With pos the row goes to the topk sorted
-// rows pos[t][.], and the rows past the kept ones (src < 0) are cleared.  Whole: rows of whole aligned packs.
+constexpr int kQuantPacks = 4;  // packs a lane has on their way
+constexpr int kQuantWarps = 4;
+
+// A warp takes `part` packs of 16 bytes of a token's row (at most kQuantPacks a lane), 32 elements in neighbouring lanes;
+// `slices` warps side by side a token, kQuantWarps and more of them in a block.  With pos the row goes to the topk sorted rows pos[t][.], and the rows past the kept ones (src < 0) are cleared.
+// Whole: rows of whole aligned packs.
 template <typename T, bool Whole>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(256)
     quant_rows_mx4_kernel(const T *__restrict__ x, const int32_t *__restrict__ src, const int32_t *__restrict__ pos,
-                          int64_t ntok, int topk, int K, int parts, uint8_t *__restrict__ xq, uint8_t *__restrict__ sx) {
-  constexpr int V = 16 / (int)sizeof(T), kP = 8 / V;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5), t = unit / parts, n = ntok * topk;
-  const int part = (int)(unit - t * parts), lane = threadIdx.x & 31, c = part * 256 + lane * 8;
+                          int64_t ntok, int topk, int K, int part, int tokens, uint8_t *__restrict__ xq,
+                          uint8_t *__restrict__ sx) {
+  constexpr int V = 16 / (int)sizeof(T), kLanes = kBlock / V;  // lanes of a scale
+  using Code = decltype(to_codes(std::declval<const float (&)[V]>()));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ldq = code_cols(K), lds = scale_cols(K);
+  const int slot = tokens > 1 ? warp % tokens : 0, slice = tokens > 1 ? warp / tokens : (int)(blockIdx.y * (blockDim.x >> 5)) + warp;
+  const int64_t t = (int64_t)blockIdx.x * tokens + slot, n = ntok * topk;
   if (t >= ntok) return;
-  const int ldq = code_cols(K), lds = scale_cols(K);
+  const int first = slice * part, end = min(first + part, ldq / V);
+  // where the first two pairs go, read beside the row
+  int place[2] = {-1, -1}, kept[2] = {0, 0};
+  if (pos)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (j < topk) {
+        place[j] = __ldg(pos + t * topk + j);
+        kept[j] = __ldg(src + t * topk + j);
+      }
   const T *row = x + t * K;
-  float v[8], amax = 0.0f;
+  Pack<T, V> in[kQuantPacks];
 #pragma unroll
-  for (int i = 0; i < kP; ++i) {
-    Pack<T, V> q{};
-    if (c + i * V < K) {
-      if constexpr (Whole) q = load_pack<T, V>(row + c + i * V);
-      else q = load_any<T>(row + c + i * V, x, x + ntok * K);
+  for (int i = 0; i < kQuantPacks; ++i) {
+    const int c = (first + i * 32 + lane) * V;
+    in[i] = Pack<T, V>{};
+    if (first + i * 32 + lane < end && c < K) {
+      if constexpr (Whole) in[i] = load_pack<T, V>(row + c);
+      else in[i] = load_any<T>(row + c, x, x + ntok * K);
     }
-#pragma unroll
-    for (int l = 0; l < V; ++l) v[i * V + l] = Whole || c + i * V + l < K ? (float)to_acc(q.v[l]) : 0.0f;
   }
+  Code codes[kQuantPacks];
+  uint8_t scales[kQuantPacks];
 #pragma unroll
-  for (int l = 0; l < 8; ++l) amax = max_nan(amax, fabsf(v[l]));
-  amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-  amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-  const uint32_t exponent = __float_as_uint(amax) >> 23;  // 255: an infinity or NaN in the block
-  const uint32_t scale = exponent == 255 ? 255u : exponent < 2 ? 0u : exponent - 2;
-  const float r = __uint_as_float((254u - scale) << 23);  // 2^-e
+  for (int i = 0; i < kQuantPacks; ++i) {
+    const int c = (first + i * 32 + lane) * V;
+    float v[V];
 #pragma unroll
-  for (int l = 0; l < 8; ++l) v[l] *= r;  // exact, but where it is far below the least code
-  const uint32_t codes = scale == 255 ? 0u : to_codes(v);
+    for (int l = 0; l < V; ++l) v[l] = Whole || c + l < K ? (float)to_acc(in[i].v[l]) : 0.0f;
+    float amax = fabsf(v[0]);
+#pragma unroll
+    for (int l = 1; l < V; ++l) amax = max_nan(amax, fabsf(v[l]));
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    const uint32_t exponent = __float_as_uint(amax) >> 23;  // 255: an infinity or NaN in the block
+    const uint32_t scale = exponent == 255 ? 255u : exponent < 2 ? 0u : exponent - 2;
+    const float r = scale == 255 ? 0.0f : __uint_as_float((254u - scale) << 23);  // 2^-e
+#pragma unroll
+    for (int l = 0; l < V; ++l) v[l] *= r;  // exact, but where it is far below the least code
+    codes[i] = scale == 255 ? Code(0) : to_codes(v);
+    scales[i] = (uint8_t)scale;
+  }
+  const int pad = slice == 0 && lane < lds - ldq / kBlock ? ldq / kBlock + lane : -1;  // scales past the last block
   for (int j = 0; j < topk; ++j) {
-    const int64_t q = t * topk + j, p = pos ? __ldg(pos + q) : t;
+    const int64_t q = t * topk + j, p = !pos ? t : j == 0 ? place[0] : j == 1 ? place[1] : __ldg(pos + q);
     if (p >= 0 && p < n) {
-      if (c < ldq) reinterpret_cast<uint32_t *>(xq + p * (ldq / 2))[c / 8] = codes;
-      if (lane % 4 == 0) sx[p * lds + c / kBlock] = (uint8_t)scale;
+      Code *to = reinterpret_cast<Code *>(xq + p * (ldq / 2)) + first + lane;
+      uint8_t *ts = sx + p * lds;
+#pragma unroll
+      for (int i = 0; i < kQuantPacks; ++i)
+        if (first + i * 32 + lane < end) {
+          to[i * 32] = codes[i];
+          if (lane % kLanes == 0) ts[(first + i * 32 + lane) / kLanes] = scales[i];
+        }
+      if (pad >= 0) ts[pad] = 0;
     }
-    if (pos && __ldg(src + q) < 0) {
-      if (c < ldq) reinterpret_cast<uint32_t *>(xq + q * (ldq / 2))[c / 8] = 0u;
-      if (lane % 4 == 0) sx[q * lds + c / kBlock] = 0;
+    if (pos && (j == 0 ? kept[0] : j == 1 ? kept[1] : __ldg(src + q)) < 0) {
+      for (int c = first + lane; c < end; c += 32) {
+        reinterpret_cast<Code *>(xq + q * (ldq / 2))[c] = 0;
+        if (lane % kLanes == 0) sx[q * lds + c / kLanes] = 0;
+      }
+      if (pad >= 0) sx[q * lds + pad] = 0;
     }
   }
 }
@@ -169,9 +223,10 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
 // as they are: K 64 an instruction, a scale for 32.
 //   One lane copies a stage's codes, 256 of K, by tensor-map copies into K-major rows of 128 bytes in the 128-byte swizzle
 //   (a map reads zeros past the arrays; rows of another expert or past N land in columns and rows that nobody reads).
-//   Four warps bring the scales, a row of either operand a thread, eight scales a stage, read four stages ahead: in shared
-//   memory 128 rows' four scales of 128 of K are 512 bytes, row r at 16 (r % 32) + 4 (r / 32), which is how they go to
-//   the tensor memory's columns (repeated in its four lane quadrants).
+//   Four warps bring the scales of four stages at a time into one of two places, four lanes a row: in shared memory 128
+//   rows' four scales of 128 of K are 512 bytes, row r at 16 (r % 32) + 4 (r / 32), which is how they go to the tensor
+//   memory's columns (repeated in its four lane quadrants).  A proxy fence waits for the thread's loads in flight, some
+//   1000 cycles: once for each stage that bounded the product at 2.0 PFLOP/s.
 //   One lane issues a stage's copies to tensor memory and its MMAs; scales have two places there, taken in turn, and a place
 //   is written again when the MMAs that read it have completed.
 //   Eight epilogue warps (two per lane quadrant, half the columns each) finish a tile while the next one runs.
@@ -180,17 +235,17 @@ namespace mx4 {
 constexpr int kTM = 128, kKB = 256, kRowBytes = kKB / 2;
 constexpr int kEpiWarps = 8, kScaleWarps = 4, kCopyWarp = kEpiWarps + kScaleWarps, kMmaWarp = kCopyWarp + 1;
 constexpr int kThreads = (kMmaWarp + 1) * 32;
-constexpr int kAhead = 4;  // stages a thread's scales are read ahead
+constexpr int kGroup = 4;  // stages whose scales come together
 
 template <int TN>
 struct Shape {
-  static constexpr int kA = kTM * kRowBytes, kB = TN * kRowBytes, kSA = 1024, kBlocksB = (TN + 127) / 128, kSB = 1024 * kBlocksB;
-  static constexpr int kStageBytes = kA + kB + kSA + kSB;
+  static constexpr int kA = kTM * kRowBytes, kB = TN * kRowBytes, kStageBytes = kA + kB;
+  static constexpr int kSA = 1024, kBlocksB = (TN + 127) / 128, kScaleBytes = kSA + 1024 * kBlocksB;  // of a stage
   static constexpr int kStages = TN > 128 ? 4 : TN > 64 ? 6 : 8;
   // an accumulator and a place of scales in each half of the columns
   static constexpr uint32_t kHalf = TN > 128 ? 256 : TN > 64 ? 256 : 128, kTmemCols = 2 * kHalf, kScaleAt = TN;
   static constexpr uint32_t kColsA = 4, kColsB = 4 * kBlocksB;  // of 128 of K
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (3 * kStages + 5) * 8 + 16;  // aligned within
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 2 * kGroup * kScaleBytes + (2 * kStages + 9) * 8 + 16;  // aligned within
   static_assert(kStageBytes % 1024 == 0 && kSmem <= 227 * 1024 && TN % 32 == 0 && TN + 2 * (kColsA + kColsB) <= kHalf, "tile");
 };
 
@@ -249,8 +304,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   using S = Shape<TN>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
-  uint64_t *codes = reinterpret_cast<uint64_t *>(smem + S::kStages * S::kStageBytes), *scales = codes + S::kStages;
-  uint64_t *empty = scales + S::kStages, *acc_full = empty + S::kStages, *acc_empty = acc_full + 2, *done = acc_empty + 2;
+  unsigned char *scale_room = smem + S::kStages * S::kStageBytes;
+  uint64_t *codes = reinterpret_cast<uint64_t *>(scale_room + 2 * kGroup * S::kScaleBytes), *empty = codes + S::kStages;
+  uint64_t *scales = empty + S::kStages, *scales_empty = scales + 2, *acc_full = scales_empty + 2, *acc_empty = acc_full + 2;
+  uint64_t *done = acc_empty + 2;
   uint32_t *holder = reinterpret_cast<uint32_t *>(done + 1);
   volatile int *stop = reinterpret_cast<int *>(holder + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -266,10 +323,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto init = [](uint64_t *b, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(n)); };
     for (int s = 0; s < S::kStages; ++s) {
       init(codes + s, 1);
-      init(scales + s, kScaleWarps);
       init(empty + s, 1);
     }
     for (int b = 0; b < 2; ++b) {
+      init(scales + b, kScaleWarps);
+      init(scales_empty + b, 1);
       init(acc_full + b, 1);
       init(acc_empty + b, kEpiWarps);
     }
@@ -291,7 +349,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- the MMAs
-    int j = 0, unit = 0;  // stages, tiles
+    int j = 0, unit = 0, group = 0;  // stages, tiles, groups of scales
     Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
     for (; ok; t.tile += gridDim.x, ++unit) {
       seek_work(p, TN, nct, t);
@@ -305,12 +363,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int end = min(nkb, p.give_up - j);
         const uint32_t acc = tmem + buf * S::kHalf;
         for (int kb = 0; kb < end && ok; ++kb, ++j) {
-          const int st = j % S::kStages, par = (j / S::kStages) & 1, at = j & 1;
-          ok = wait(codes + st, par) && wait(scales + st, par);
+          const int st = j % S::kStages, at = j & 1, place = group & 1;
+          if (kb % kGroup == 0) ok = wait(scales + place, (group >> 1) & 1);
+          ok = ok && wait(codes + st, (j / S::kStages) & 1);
           if (ok && j >= 2) ok = wait(empty + (j - 2) % S::kStages, ((j - 2) / S::kStages) & 1);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;");
-          const uint32_t base = smem_u32(smem) + st * S::kStageBytes, sa = base + S::kA + S::kB, sb = sa + S::kSA;
+          const uint32_t base = smem_u32(smem) + st * S::kStageBytes;
+          const uint32_t sa = smem_u32(scale_room) + (place * kGroup + kb % kGroup) * S::kScaleBytes, sb = sa + S::kSA;
           const uint32_t ta = tmem + at * S::kHalf + S::kScaleAt, tb = ta + 2 * S::kColsA;
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
@@ -331,6 +391,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 : "memory");
           }
           commit(smem_u32(empty + st));
+          if (kb % kGroup == kGroup - 1 || kb == nkb - 1) {
+            commit(smem_u32(scales_empty + place));
+            ++group;
+          }
           if (kb == nkb - 1) commit(smem_u32(acc_full + buf));
         }
         ok = ok && end == nkb;
@@ -363,62 +427,46 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!ok) *stop = 1;
   } else if (warp >= kEpiWarps) {
     // ---------------------------------------------------------------- the scales
-    const int r = threadIdx.x - kEpiWarps * 32, lds = scale_cols(p.K);
+    constexpr int kRA = kTM / 32, kRB = TN / 32;  // rows of a thread
+    const int at = threadIdx.x - kEpiWarps * 32, row = at / 4, s = at % 4, lds = scale_cols(p.K);
     Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
-    const uint8_t *a = nullptr, *b0 = nullptr, *b1 = nullptr;  // this thread's rows at the stage to be read next
-    int kb = 0;
-    auto enter = [&] {
-      kb = 0;
-      if (!t.have) return;
-      a = t.n0 + r < p.N ? p.sw + ((int64_t)t.e * p.N + t.n0 + r) * lds : nullptr;
-      b0 = r < t.r1 - t.r0 ? p.sx + (int64_t)(t.r0 + r) * lds : nullptr;
-      b1 = S::kBlocksB > 1 && r + 128 < t.r1 - t.r0 ? p.sx + (int64_t)(t.r0 + r + 128) * lds : nullptr;
+    int kb = 0, group = 0;
+    uint2 v[kRA + kRB];
+    auto read = [&] {  // of stage kb + s
+      const uint8_t *a = p.sw + ((int64_t)t.e * p.N + t.n0 + row) * lds, *b = p.sx + (int64_t)(t.r0 + row) * lds;
+      const int na = kb + s < nkb ? p.N - t.n0 - row : 0, nb = kb + s < nkb ? t.r1 - t.r0 - row : 0, k = (kb + s) * 8;
+#pragma unroll
+      for (int i = 0; i < kRA + kRB; ++i) {
+        const int r = 32 * (i < kRA ? i : i - kRA);
+        v[i] = make_uint2(0, 0);
+        if (r < (i < kRA ? na : nb)) v[i] = __ldg(reinterpret_cast<const uint2 *>((i < kRA ? a : b) + (int64_t)r * lds + k));
+      }
     };
     seek_work(p, TN, nct, t);
-    enter();
-    uint2 va[kAhead], v0[kAhead], v1[kAhead];
-    bool live[kAhead];
-    auto read = [&](int d) {
-      const uint2 zero = make_uint2(0, 0);
-      live[d] = t.have;
-      va[d] = t.have && a ? __ldg(reinterpret_cast<const uint2 *>(a) + kb) : zero;
-      v0[d] = t.have && b0 ? __ldg(reinterpret_cast<const uint2 *>(b0) + kb) : zero;
-      if constexpr (S::kBlocksB > 1) v1[d] = t.have && b1 ? __ldg(reinterpret_cast<const uint2 *>(b1) + kb) : zero;
-      if (t.have && ++kb == nkb) {
+    if (t.have) read();
+    const uint32_t to0 = smem_u32(scale_room) + s * S::kScaleBytes + row * 16;
+    while (t.have) {
+      ok = __all_sync(0xffffffffu, wait(scales_empty + (group & 1), (group >> 1 & 1) ^ 1));
+      if (!ok) break;
+      const uint32_t to = to0 + (group & 1) * kGroup * S::kScaleBytes;
+#pragma unroll
+      for (int i = 0; i < kRA + kRB; ++i) {  // row r of an operand: block r / 128 of each 128 of K, word r / 32 % 4
+        const int q = i < kRA ? i : i - kRA, nblk = i < kRA ? 1 : S::kBlocksB;
+        const uint32_t d = to + (i < kRA ? 0 : S::kSA) + q / 4 * 512 + q % 4 * 4;
+        asm volatile("st.shared.b32 [%0], %1;" ::"r"(d), "r"(v[i].x) : "memory");
+        asm volatile("st.shared.b32 [%0], %1;" ::"r"(d + 512 * nblk), "r"(v[i].y) : "memory");
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) arrive(smem_u32(scales + (group & 1)));
+      ++group;
+      kb += kGroup;
+      if (kb >= nkb) {
+        kb = 0;
         t.tile += gridDim.x;
         seek_work(p, TN, nct, t);
-        enter();
       }
-    };
-#pragma unroll
-    for (int d = 0; d < kAhead; ++d) read(d);
-    const uint32_t at = smem_u32(smem) + S::kA + S::kB + (r % 32) * 16 + (r / 32) * 4;
-    auto put = [&](uint32_t to, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(v) : "memory"); };
-    bool more = true;
-    for (int j = 0; more;) {
-#pragma unroll
-      for (int d = 0; d < kAhead; ++d) {
-        more = more && live[d];
-        if (!more) break;
-        const int st = j % S::kStages;
-        ok = __all_sync(0xffffffffu, wait(empty + st, (j / S::kStages & 1) ^ 1));
-        more = ok;
-        if (!more) break;
-        const uint32_t to = at + st * S::kStageBytes;
-        put(to, va[d].x);
-        put(to + 512, va[d].y);
-        put(to + S::kSA, v0[d].x);
-        put(to + S::kSA + 512 * S::kBlocksB, v0[d].y);
-        if constexpr (S::kBlocksB > 1) {
-          put(to + S::kSA + 512, v1[d].x);
-          put(to + S::kSA + 512 * 3, v1[d].y);
-        }
-        read(d);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) arrive(smem_u32(scales + st));
-        ++j;
-      }
+      if (t.have) read();  // on its way while the MMAs work on what is there
     }
     if (!ok) *stop = 1;
   } else {
@@ -545,12 +593,14 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
   if (!x || !xq || !sx) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (((uintptr_t)xq & 15) || ((uintptr_t)sx & 7)) return set_error(DP_ERR_SHAPE, "%s: xq or sx is not aligned", who);
   if (!at_elements(x) || !at_elements(src, pos)) return misaligned(who);
-  const int parts = (K + 255) / 256;
-  const int64_t blocks = (ntok * parts + 3) / 4;
-  if (blocks > 0x7fffffffLL) return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, K);
+  constexpr int V = 16 / (int)sizeof(T), kLanes = kBlock / V;
+  const int packs = code_cols(K) / V, slices = (packs + 32 * kQuantPacks - 1) / (32 * kQuantPacks);
+  const int part = ((packs + slices - 1) / slices + kLanes - 1) / kLanes * kLanes;  // whole blocks of 32 elements
   const bool whole = (((uintptr_t)x | (uintptr_t)(K * sizeof(T))) & 15) == 0;
   auto k = whole ? quant_rows_mx4_kernel<T, true> : quant_rows_mx4_kernel<T, false>;
-  k<<<(unsigned)blocks, 128, 0, (cudaStream_t)stream>>>(x, src, pos, ntok, topk, K, parts, xq, sx);
+  const int tokens = slices < kQuantWarps ? kQuantWarps / slices : 1, warps = slices * tokens < 8 ? slices * tokens : 8;
+  const dim3 grid((unsigned)((ntok + tokens - 1) / tokens), (unsigned)((slices + 7) / 8));
+  k<<<grid, warps * 32, 0, (cudaStream_t)stream>>>(x, src, pos, ntok, topk, K, part, tokens, xq, sx);
   return launch_status(who);
 }
 
