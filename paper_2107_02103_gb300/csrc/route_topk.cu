@@ -4,9 +4,10 @@
 //   expert[j] = the j-th largest c left,  w_j = scale s_ej, or scale s_ej / sum_i s_ei
 // Without a bias the experts are ordered by x itself, which has the order of s and no rounding.  Ties go to the lowest
 // index, a NaN stands above all numbers, an expert with x = -inf or b = -inf is never chosen (-1, weight 0).
-// The choice is that of exact arithmetic: c is computed in f32, and a token in which two neighbours of the order (the
-// first one left out included) or the last group kept and the first one dropped are nearer than their error bounds is
-// done again in f64.
+// The choice is that of exact arithmetic, in up to three steps: first on f32 scores cut to leave room for the expert's index
+// in the same word (one integer is compared and moved, and no two are equal); a token in which two neighbours of that
+// order (the first one left out included) or the last group kept and the first one dropped are nearer than their error
+// bounds is done again on whole f32 scores, and where those are too near, in f64.
 // Backward, the choice held fixed, n_j = s_ej / sum_i s_ei:
 //   renormalised  g_j = scale n_j (dw_j - sum_i n_i dw_i)   softmax dx_ej += g_j,  sigmoid dx_ej += g_j (1 - s_ej)
 //   plain         softmax dx_e = sum_(j: e_j = e) g_j - s_e sum_j g_j with g_j = scale dw_j s_ej
@@ -28,6 +29,8 @@ struct TopkArgs {
   double scale;
   int32_t *expert;
   void *w;
+  uint32_t mask;  // the bits of an expert's index
+  uint32_t inv_per;  // floor(e inv_per / 2^32) is the group of expert e
 };
 
 template <typename A>
@@ -67,16 +70,6 @@ __device__ __forceinline__ V over(unsigned mask, V v, F f) {
   return v;
 }
 template <int L, typename V>
-__device__ __forceinline__ V max_over(unsigned mask, V v) {
-  if constexpr (L == 32 && std::is_same<V, uint32_t>::value) return __reduce_max_sync(mask, v);
-  return over<L>(mask, v, [](V a, V b) { return a > b ? a : b; });
-}
-template <int L>
-__device__ __forceinline__ int min_over(unsigned mask, int v) {
-  if constexpr (L == 32) return __reduce_min_sync(mask, v);
-  return over<L>(mask, v, [](int a, int b) { return a < b ? a : b; });
-}
-template <int L, typename V>
 __device__ __forceinline__ V sum_over(unsigned mask, V v) {
   return over<L>(mask, v, [](V a, V b) { return a + b; });
 }
@@ -84,6 +77,11 @@ __device__ __forceinline__ V sum_over(unsigned mask, V v) {
 template <int L, typename A>
 __device__ __forceinline__ A most_over(unsigned mask, A v) {
   return over<L>(mask, v, [](A a, A b) { return a != a || a > b ? a : b; });
+}
+constexpr unsigned kAll = 0xffffffffu;
+__device__ __forceinline__ uint32_t warp_max(uint32_t v) { return __reduce_max_sync(kAll, v); }
+__device__ __forceinline__ unsigned long long warp_max(unsigned long long v) {
+  return over<32>(kAll, v, [](unsigned long long a, unsigned long long b) { return a > b ? a : b; });
 }
 
 __device__ __forceinline__ float exp_(float x) { return expf(x); }
@@ -105,62 +103,100 @@ __device__ __forceinline__ A relative_score(A x, A most, bool sigm) {
   return exp_(x - (most < A(0) ? most : A(0))) / (A(1) + exp_(x));
 }
 
-// One token on L lanes, N logits a lane: lane's i-th is expert i L + lane.  True: two scores are too near to tell apart
-// in A, and nothing is written.  `room`: shared memory of the token, E + 2 G words of 8 bytes, for the groups.
-template <typename T, typename A, int L, int N>
-__device__ bool choose(const TopkArgs &p, int64_t t, int lane, unsigned mask, unsigned char *room) {
+// f32 scores for the order: the relative error of s in ulp of 2^-23 (an exponential 2, a quotient, sum or difference 0.5;
+// `range` the size of the softmax's argument x - m):
+//   sigmoid  2 of the exponential, its product with the reciprocal, that and 1 + e: below 4
+//   softmax  2, the argument's rounding 0.5 range, the quotient; the total: its terms' 2 and their arguments' roundings
+//            (in the mean below 4), and (32 + 5) / 2 of its additions: below 28 + 0.5 range
+__device__ __forceinline__ float score_error(float range, bool sigm) { return sigm ? 0x1p-21f : 0x1p-18f + 0x1p-24f * fminf(range, 128.0f); }
+// Two scores that f32 cannot order: x the logits, b the biases (c = s + b), range the larger |argument|.  Equal inputs
+// give equal scores; else s <= |c| + |b|, and the sum's own rounding is half an ulp.
+__device__ __forceinline__ bool too_near(float c0, float c1, float x0, float x1, float b0, float b1, float range, bool sigm) {
+  if (x0 == x1 && b0 == b1) return false;
+  return !(c0 - c1 > (score_error(range, sigm) + 0x1p-23f) * (fabsf(c0) + fabsf(c1) + fabsf(b0) + fabsf(b1)));
+}
+// The same of two groups' scores, sums of up to two c each.  The four s come to at most 4 (sigmoid) or 1 (softmax, where
+// range s is at most 0.4): within 2^-18.9 or 2^-17.7 together, and the sums' roundings.
+__device__ __forceinline__ bool groups_too_near(float a, float b, bool sigm) {
+  return !(a - b > (sigm ? 0x1p-18f : 0x1p-17f) * (1.0f + fabsf(b)));
+}
+
+// The first step's scores: the short exponential's documented error is 2 + 1.173 |argument| ulp, the short quotient's 2.
+__device__ __forceinline__ float rough_sigmoid(float x) {
+  const float e = __expf(x < 0.0f ? x : -x);
+  return __fdividef(x < 0.0f ? e : 1.0f, 1.0f + e);
+}
+__device__ __forceinline__ float rough_error(float range, bool sigm) {
+  return (sigm ? 0x1p-20f : 0x1p-18f) + 0x1p-21f * fminf(range, 128.0f);
+}
+// A key with the index of its expert in the low bits (mask: all of them), the lower index the larger; 0 stays 0.
+__device__ __forceinline__ uint32_t pack_key(uint32_t key, uint32_t mask, int e) { return key ? (key & ~mask) | (mask - e) : 0u; }
+__device__ __forceinline__ int packed_expert(uint32_t key, uint32_t mask) { return key ? (int)(mask - (key & mask)) : -1; }
+// Neighbours of the packed order that it may have wrong: their cut scores as intervals.
+__device__ __forceinline__ bool packed_near(uint32_t k0, uint32_t k1, uint32_t mask, float x0, float x1, float b0, float b1,
+                                            float range, bool sigm) {
+  if (x0 == x1 && b0 == b1) return false;
+  const float c0 = from_key(k0 & ~mask), c1 = from_key(k1 | mask);
+  return !(c0 - c1 > (rough_error(range, sigm) + 0x1p-23f) * (fabsf(c0) + fabsf(c1) + fabsf(b0) + fabsf(b1)));
+}
+
+// One token on a warp, N logits a lane: the i-th is expert 32 i + lane.  S chosen pairs a lane (and the first one left
+// out).  True: two scores are too near to tell apart in A, and nothing is written.  `room`: shared memory of the token,
+// E + 3 G words of 8 bytes, for the groups.
+template <typename T, typename A, int N, int S>
+__device__ bool choose(const TopkArgs &p, int64_t t, unsigned char *room) {
   using U = key_t_<A>;
   constexpr bool kExact = sizeof(A) == 8;
-  constexpr int kSlots = (kMaxTopk < L * N ? kMaxTopk : L * N) / L;
+  const int lane = threadIdx.x & 31;
   const T *x = (const T *)p.x + t * p.E;
   const acc_t<T> *bias = (const acc_t<T> *)p.bias;
   const bool grouped = p.keep < p.G, by_score = p.bias || (grouped && p.gtop == 2);
   A v[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = i * L + lane < p.E ? (A)to_acc(x[i * L + lane]) : none<A>();
+  for (int i = 0; i < N; ++i) v[i] = i * 32 + lane < p.E ? (A)to_acc(x[i * 32 + lane]) : none<A>();
   A most = none<A>(), total = A(0);
   if (!p.sigmoid && (by_score || !p.renorm)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) most = v[i] != v[i] || v[i] > most ? v[i] : most;
-    most = most_over<L>(mask, most);
+    most = most_over<32>(kAll, most);
 #pragma unroll
     for (int i = 0; i < N; ++i) total += v[i] == none<A>() ? A(0) : exp_(v[i] - most);
-    total = sum_over<L>(mask, total);
+    total = sum_over<32>(kAll, total);
   }
-  auto score = [&](A xe) { return p.sigmoid ? sigmoid(xe) : exp_(xe - most) / total; };
 
   U key[N];
-  A *room_c = (A *)room;
+  const int per = p.E / p.G;
+  U *ckey = (U *)room;  // of group g from g (per + 1) on: lanes of neighbouring groups fall on different banks
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int e = i * L + lane;
+    const int e = i * 32 + lane;
     A c = v[i], by = v[i];
     if (by_score && e < p.E) {
       const A b = bias ? (A)__ldg(bias + e) : A(0);
-      const bool out = v[i] == none<A>() || b == none<A>();
-      c = out ? none<A>() : score(v[i]) + b;
+      const A s = p.sigmoid ? sigmoid(v[i]) : exp_(v[i] - most) / total;
+      c = v[i] == none<A>() || b == none<A>() ? none<A>() : s + b;
       by = bias ? c : v[i];
     }
     key[i] = to_key(by);
-    if (grouped && e < p.E) room_c[e] = c;
+    if (grouped && e < p.E) ckey[e + e / per] = to_key(c);
   }
   bool near = false;
   if (grouped) {
-    U *gkey = (U *)(room + (size_t)p.E * 8), *kept = (U *)(room + (size_t)(p.E + p.G) * 8);
-    const int per = p.E / p.G;
-    __syncwarp(mask);
-    for (int g = lane; g < p.G; g += L) {
+    U *gkey = (U *)(room + (size_t)(p.E + p.G) * 8), *kept = gkey + p.G;
+    __syncwarp();
+    for (int g = lane; g < p.G; g += 32) {
       U a = 0, b = 0;
       for (int i = 0; i < per; ++i) {
-        const U c = to_key(room_c[g * per + i]);
-        b = c > a ? a : c > b ? c : b;
+        const U c = ckey[g * (per + 1) + i];
+        const U less = c < a ? c : a;
+        b = less > b ? less : b;
         a = c > a ? c : a;
       }
       gkey[g] = p.gtop == 2 && b ? to_key(from_key(a) + from_key(b)) : a;
     }
-    __syncwarp(mask);
+    __syncwarp();
     U last = ~(U)0, first = 0;  // the least group kept, the best one dropped
-    for (int g = lane; g < p.G; g += L) {
+    for (int g = lane; g < p.G; g += 32) {
       const U mine = gkey[g];
       int rank = 0;
       for (int o = 0; o < p.G; ++o) rank += gkey[o] > mine || (gkey[o] == mine && o < g);
@@ -168,125 +204,109 @@ __device__ bool choose(const TopkArgs &p, int64_t t, int lane, unsigned mask, un
       if (rank < p.keep) last = mine < last ? mine : last;
       else first = mine > first ? mine : first;
     }
-    __syncwarp(mask);
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int e = i * L + lane;
+      const int e = i * 32 + lane;
       if (e < p.E && !kept[e / per]) key[i] = 0;
     }
-    if (!kExact && by_score) {
-      last = ~max_over<L>(mask, (U)~last);
-      first = max_over<L>(mask, first);
-      const A a = from_key(last), b = from_key(first);
-      // an s is within 2^-20 of its value (s <= 1: 2 ulp of the exponential, its argument's rounding, sum and quotient)
-      near = first != 0 && !(a - b > A(0x1p-18) * (A(1) + fabs((double)b)));
+    if constexpr (!kExact) {
+      last = ~warp_max((U)~last);
+      first = warp_max(first);
+      near = by_score && first != 0 && groups_too_near(from_key(last), from_key(first), p.sigmoid);
     }
   }
 
-  // the best of each lane, then of the token, k times and once more for the first one left out
+  // the best of each lane, then of the warp, k times and once more for the first one left out
   U best;
   int at;
-  A bx;
   auto rescan = [&] {
     best = 0;
     at = 0;
-    bx = A(0);
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (key[i] > best) {
         best = key[i];
         at = i;
-        bx = v[i];
       }
   };
   rescan();
-  int se[kSlots];
-  A sx[kSlots], sc[kSlots];
+  int se[S];
+  U sk[S];
 #pragma unroll
-  for (int s = 0; s < kSlots; ++s) {
+  for (int s = 0; s < S; ++s) {
     se[s] = -1;
-    sx[s] = none<A>();
-    sc[s] = none<A>();
+    sk[s] = 0;
   }
   const bool check = !kExact && p.bias;
-  int left_e = -1;
-  A left_x = A(0), left_c = none<A>();
   for (int j = 0; j < p.k + (check ? 1 : 0); ++j) {
-    const U m = max_over<L>(mask, best);
+    const U m = warp_max(best);
     if (m == 0) break;
-    const int e = min_over<L>(mask, best == m ? at * L + lane : INT_MAX);
-    const A xe = __shfl_sync(mask, bx, e % L, L);
-    if (e % L == lane) {
+    const int e = __reduce_min_sync(kAll, best == m ? at * 32 + lane : INT_MAX);
+    if (e % 32 == lane) {
 #pragma unroll
       for (int i = 0; i < N; ++i)
         if (i == at) key[i] = 0;
       rescan();
     }
-    if (j == p.k) {
-      left_e = e;
-      left_x = xe;
-      left_c = from_key(m);
-    } else {
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s)
-        if (j == s * L + lane) {
-          se[s] = e;
-          sx[s] = xe;
-          sc[s] = from_key(m);
+    for (int s = 0; s < S; ++s)
+      if (j == s * 32 + lane) {
+        se[s] = e;
+        sk[s] = m;
+      }
+  }
+  A sx[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) sx[s] = se[s] >= 0 ? (A)to_acc(x[se[s]]) : none<A>();
+  if constexpr (!kExact) {
+    if (check) {
+      float c[S], b[S];
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        c[s] = from_key(sk[s]);
+        b[s] = se[s] >= 0 ? __ldg(bias + se[s]) : 0.0f;
+      }
+#pragma unroll
+      for (int s = 0; s < S; ++s) {  // a pair and the next one: the next lane's, of the last lane the first lane's next
+        const int from = (lane + 1) % 32, s1 = s + 1 < S ? s + 1 : s;
+        const float c0 = __shfl_sync(kAll, c[s], from), c1 = __shfl_sync(kAll, c[s1], from);
+        const float x0 = __shfl_sync(kAll, sx[s], from), x1 = __shfl_sync(kAll, sx[s1], from);
+        const float b0 = __shfl_sync(kAll, b[s], from), b1 = __shfl_sync(kAll, b[s1], from);
+        const int e0 = __shfl_sync(kAll, se[s], from), e1 = __shfl_sync(kAll, se[s1], from);
+        const bool wrap = lane == 31;
+        const float nx = wrap ? x1 : x0;
+        if (s * 32 + lane < p.k && se[s] >= 0 && (wrap ? (S > 1 ? e1 : -1) : e0) >= 0) {
+          const float range = most - fminf(sx[s], nx);
+          near |= too_near(c[s], wrap ? c1 : c0, sx[s], nx, b[s], wrap ? b1 : b0, range, p.sigmoid);
         }
-    }
-  }
-  if (check) {
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s) {
-      const int up = lane + 1 < L ? s : s + 1;  // whose next one is where
-      int ne = __shfl_sync(mask, se[s], (lane + 1) % L, L);
-      A nx = __shfl_sync(mask, sx[s], (lane + 1) % L, L), nc = __shfl_sync(mask, sc[s], (lane + 1) % L, L);
-      const int s1 = s + 1 < kSlots ? s + 1 : s;
-      const int ne1 = __shfl_sync(mask, se[s1], 0, L);
-      const A nx1 = __shfl_sync(mask, sx[s1], 0, L), nc1 = __shfl_sync(mask, sc[s1], 0, L);
-      if (up != s) {
-        ne = ne1;
-        nx = nx1;
-        nc = nc1;
-      }
-      if (s * L + lane == p.k - 1) {
-        ne = left_e;
-        nx = left_x;
-        nc = left_c;
-      }
-      if (s * L + lane < p.k && se[s] >= 0 && ne >= 0) {
-        const A b0 = (A)__ldg(bias + se[s]), b1 = (A)__ldg(bias + ne);
-        // s is off by less than 2^-21 of itself (2 ulp of the exponential, quotient, sum) and, in a softmax, by its
-        // argument's rounding; s <= |c| + |b|
-        A eps = A(0x1p-20);
-        if (!p.sigmoid) eps += A(0x1p-23) * (most - (sx[s] < nx ? sx[s] : nx));
-        const A tol = eps * (fabsf(sc[s]) + fabsf(nc) + fabsf(b0) + fabsf(b1));
-        near |= !(sx[s] == nx && b0 == b1) && !(sc[s] - nc > tol);
       }
     }
+    if (by_score && __any_sync(kAll, near)) return true;
   }
-  if (!kExact && by_score && __any_sync(mask, near)) return true;
 
   A wsum = A(1), top = A(0);
-  A ws[kSlots];
+  A ws[S];
   if (p.renorm) {
     top = none<A>();
 #pragma unroll
-    for (int s = 0; s < kSlots; ++s) top = sx[s] != sx[s] || sx[s] > top ? sx[s] : top;
-    top = most_over<L>(mask, top);
+    for (int s = 0; s < S; ++s) {
+      if (s * 32 + lane >= p.k) se[s] = -1;  // the first one left out
+      if (se[s] >= 0) top = sx[s] != sx[s] || sx[s] > top ? sx[s] : top;
+    }
+    top = most_over<32>(kAll, top);
     wsum = A(0);
   }
 #pragma unroll
-  for (int s = 0; s < kSlots; ++s) {
-    ws[s] = se[s] < 0 ? A(0) : p.renorm ? relative_score(sx[s], top, p.sigmoid) : score(sx[s]);
+  for (int s = 0; s < S; ++s) {
+    ws[s] = se[s] < 0 ? A(0) : p.renorm ? relative_score(sx[s], top, p.sigmoid) : p.sigmoid ? sigmoid(sx[s]) : exp_(sx[s] - most) / total;
     if (p.renorm) wsum += ws[s];
   }
   // total * 0: a NaN or +inf anywhere makes every score of a softmax NaN, also where the chosen logits are numbers
-  if (p.renorm) wsum = sum_over<L>(mask, wsum) + (by_score ? total * A(0) : A(0));
+  if (p.renorm) wsum = sum_over<32>(kAll, wsum) + (by_score ? total * A(0) : A(0));
 #pragma unroll
-  for (int s = 0; s < kSlots; ++s) {
-    const int j = s * L + lane;
+  for (int s = 0; s < S; ++s) {
+    const int j = s * 32 + lane;
     if (j < p.k) {
       p.expert[t * p.k + j] = se[s];
       ((acc_t<T> *)p.w)[t * p.k + j] = se[s] < 0 ? acc_t<T>(0) : (acc_t<T>)((A)p.scale * (ws[s] / wsum));
@@ -295,24 +315,520 @@ __device__ bool choose(const TopkArgs &p, int64_t t, int lane, unsigned mask, un
   return false;
 }
 
-template <typename T, int L, int N>
-__device__ __noinline__ void choose_exact(const TopkArgs &p, int64_t t, int lane, unsigned mask, unsigned char *room) {
-  choose<T, double, L, N>(p, t, lane, mask, room);
+// The later steps, rarely taken.
+template <typename T, int N, int S>
+__device__ __noinline__ void choose_again(const TopkArgs &p, int64_t t, unsigned char *room) {
+  __syncwarp();
+  if (!choose<T, float, N, S>(p, t, room)) return;
+  __syncwarp();
+  choose<T, double, N, S>(p, t, room);
 }
 
-template <typename T, int L, int N>
+// The first step for a token on a warp; true: not sure.
+template <typename T, int N, int S>
+__device__ __forceinline__ bool choose_packed(const TopkArgs &p, int64_t t, unsigned char *room) {
+  const int lane = threadIdx.x & 31;
+  const T *x = (const T *)p.x + t * p.E;
+  const float *bias = (const float *)p.bias;
+  const bool grouped = p.keep < p.G, by_score = p.bias || (grouped && p.gtop == 2);
+  const uint32_t mask = p.mask;
+  float v[N], most = none<float>(), total = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = i * 32 + lane < p.E ? to_acc(x[i * 32 + lane]) : none<float>();
+  if (!p.sigmoid && (by_score || !p.renorm)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = v[i] != v[i] || v[i] > most ? v[i] : most;
+    most = most_over<32>(kAll, most);
+#pragma unroll
+    for (int i = 0; i < N; ++i) total += v[i] == none<float>() ? 0.0f : expf(v[i] - most);
+    total = sum_over<32>(kAll, total);
+  }
+  uint32_t key[N], best = 0;
+  const int per = p.E / p.G;
+  uint32_t *ckey = (uint32_t *)room, *gkey = ckey + p.E + p.G, *kept = gkey + p.G;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int e = i * 32 + lane;
+    uint32_t by = to_key(v[i]), c = by;
+    if (by_score && e < p.E) {
+      const float b = bias ? __ldg(bias + e) : 0.0f, s = p.sigmoid ? rough_sigmoid(v[i]) : __fdividef(__expf(v[i] - most), total);
+      c = v[i] == none<float>() || b == none<float>() ? 0u : to_key(s + b);
+      by = bias ? c : by;
+    }
+    if (grouped && e < p.E) ckey[e + e / per] = c;
+    key[i] = pack_key(by, mask, e);
+  }
+  bool near = false;
+  if (grouped) {
+    __syncwarp();
+    for (int g = lane; g < p.G; g += 32) {
+      uint32_t a = 0, b = 0;
+      const uint32_t *from = ckey + g * (per + 1);
+#pragma unroll 4
+      for (int i = 0; i < per; ++i) {
+        const uint32_t c = from[i];
+        b = max(b, min(a, c));
+        a = max(a, c);
+      }
+      gkey[g] = p.gtop == 2 && b ? to_key(from_key(a) + from_key(b)) : a;
+    }
+    __syncwarp();
+    uint32_t last = kAll, first = 0;
+    for (int g = lane; g < p.G; g += 32) {
+      const uint32_t mine = gkey[g];
+      int rank = 0;
+#pragma unroll 4
+      for (int o = 0; o < p.G; ++o) rank += gkey[o] > mine || (gkey[o] == mine && o < g);
+      kept[g] = rank < p.keep;
+      if (rank < p.keep) last = min(last, mine);
+      else first = max(first, mine);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = i * 32 + lane;
+      if (e < p.E && !kept[e / per]) key[i] = 0;
+    }
+    if (by_score) {
+      const float a = from_key(~warp_max(~last)), b = from_key(first = warp_max(first));
+      near = first != 0 && !(a - b > 0x1p-16f * (1.0f + fabsf(b)));  // the four s' errors, as groups_too_near
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) best = max(best, key[i]);
+  uint32_t sk[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) sk[s] = 0;
+  const bool check = p.bias || (sizeof(T) == 4);  // 16-bit logits are whole beside the index
+  const int picks = p.k + (check ? 1 : 0);
+  for (int j = 0; j < picks; ++j) {
+    const uint32_t m = warp_max(best);
+    if (m == 0) break;
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      if (j == s * 32 + lane) sk[s] = m;
+    if (m == best) {
+      best = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        key[i] = key[i] == m ? 0u : key[i];
+        best = max(best, key[i]);
+      }
+    }
+  }
+  int se[S];
+  float sx[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    se[s] = packed_expert(sk[s], mask);
+    sx[s] = se[s] >= 0 ? to_acc(x[se[s]]) : none<float>();
+  }
+  if (check) {
+    float b[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) b[s] = bias && se[s] >= 0 ? __ldg(bias + se[s]) : 0.0f;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {  // a pair and the next one: the next lane's, of the last lane the first lane's next
+      const int from = (lane + 1) % 32;
+      uint32_t nk = __shfl_sync(kAll, sk[s], from);
+      float nx = __shfl_sync(kAll, sx[s], from), nb = __shfl_sync(kAll, b[s], from);
+      if constexpr (S > 1) {
+        const int s1 = s + 1 < S ? s + 1 : s;
+        const uint32_t k1 = __shfl_sync(kAll, sk[s1], from);
+        const float x1 = __shfl_sync(kAll, sx[s1], from), b1 = __shfl_sync(kAll, b[s1], from);
+        if (lane == 31) {
+          nk = k1;
+          nx = x1;
+          nb = b1;
+        }
+      } else {
+        if (lane == 31) nk = 0;
+      }
+      if (s * 32 + lane < p.k && sk[s] != 0 && nk != 0) {
+        if (bias) near |= packed_near(sk[s], nk, mask, sx[s], nx, b[s], nb, p.sigmoid ? fmaxf(fabsf(sx[s]), fabsf(nx)) : most - fminf(sx[s], nx), p.sigmoid);
+        else near |= ((sk[s] ^ nk) & ~mask) == 0 && sx[s] != nx;
+      }
+    }
+  }
+  if (__any_sync(kAll, near)) return true;
+
+  float wsum = 1.0f, top = none<float>(), ws[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    if (s * 32 + lane >= p.k) se[s] = -1;  // the first one left out
+    if (se[s] >= 0) top = sx[s] != sx[s] || sx[s] > top ? sx[s] : top;
+  }
+  if (p.renorm) {
+    top = most_over<32>(kAll, top);
+    wsum = 0.0f;
+  }
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    ws[s] = se[s] < 0 ? 0.0f : p.renorm ? relative_score(sx[s], top, p.sigmoid) : p.sigmoid ? sigmoid(sx[s]) : expf(sx[s] - most) / total;
+    if (p.renorm) wsum += ws[s];
+  }
+  if (p.renorm) wsum = sum_over<32>(kAll, wsum) + (by_score ? total * 0.0f : 0.0f);  // as in choose()
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    const int j = s * 32 + lane;
+    if (j < p.k) {
+      p.expert[t * p.k + j] = se[s];
+      ((float *)p.w)[t * p.k + j] = se[s] < 0 ? 0.0f : (float)p.scale * (ws[s] / wsum);
+    }
+  }
+  return false;
+}
+
+// Words of 8 bytes of a token's groups.
+__host__ __device__ constexpr int room_words(int E, int G) { return E + 3 * G; }
+
+template <typename T, int N, int S>
 __global__ void __launch_bounds__(kThreads) topk_kernel(const __grid_constant__ TopkArgs p) {
   extern __shared__ __align__(16) unsigned char rooms[];
-  const int slot = threadIdx.x / L, lane = threadIdx.x % L;
-  const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + slot;
+  const int64_t t = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
   if (t >= p.ntok) return;
-  const unsigned mask = L == 32 ? 0xffffffffu : ((1u << (L % 32)) - 1) << (threadIdx.x % 32 / L * L);
-  unsigned char *room = rooms + (size_t)slot * (p.E + 2 * p.G) * 8;
-  if (choose<T, acc_t<T>, L, N>(p, t, lane, mask, room))
-    if constexpr (sizeof(T) < 8) {
-      __syncwarp(mask);
-      choose_exact<T, L, N>(p, t, lane, mask, room);
+  unsigned char *room = rooms + (size_t)(threadIdx.x / 32) * room_words(p.E, p.G) * 8;
+  if constexpr (sizeof(T) == 8) {
+    choose<T, double, N, S>(p, t, room);
+  } else {
+    if (choose_packed<T, N, S>(p, t, room)) choose_again<T, N, S>(p, t, room);
+  }
+}
+
+// Up to eight experts a token, the usual case: eight lanes a token.  Each lane sorts eight packed keys at a time in
+// registers (19 exchanges) and merges them into its list of the best eight; three exchanges of lists between lanes leave
+// the token's in all of them, and lane j works out pair j.  Some 200 instructions a token of 128 logits, where the warp a
+// token above takes 550 (its reductions, one an expert, leave most lanes idle).
+constexpr int kList = 8;
+__device__ __forceinline__ void exchange(uint32_t &a, uint32_t &b) {
+  const uint32_t most = max(a, b);
+  b = min(a, b);
+  a = most;
+}
+__device__ __forceinline__ void sort8(uint32_t (&k)[8]) {  // descending
+  constexpr int net[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6},
+                              {0, 4}, {3, 7}, {1, 5}, {2, 6}, {1, 4}, {3, 6}, {2, 4}, {3, 5}, {3, 4}};
+#pragma unroll
+  for (int i = 0; i < 19; ++i) exchange(k[net[i][0]], k[net[i][1]]);
+}
+// The best eight of two descending lists, and the two best of the others.
+__device__ __forceinline__ void leave(uint32_t k, uint32_t (&left)[2]) {
+  left[1] = max(left[1], min(left[0], k));
+  left[0] = max(left[0], k);
+}
+__device__ __forceinline__ void merge8(uint32_t (&a)[8], const uint32_t (&b)[8], uint32_t (&left)[2]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    leave(min(a[i], b[7 - i]), left);
+    a[i] = max(a[i], b[7 - i]);
+  }
+#pragma unroll
+  for (int h = 4; h > 0; h >>= 1)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (!(i & h)) exchange(a[i], a[i + h]);
+}
+constexpr uint32_t kNoKey = 0x007fffffu;  // to_bits(-inf): no candidate, nor is what lies below
+__device__ __forceinline__ uint32_t to_bits(float c) {  // as to_key in three instructions; the sum makes -0 and NaN positive
+  const uint32_t u = __float_as_uint(c + 0.0f);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+
+// What the packed keys leave open is settled in f64, on the few scores in question, by a token's eight lanes (m8).
+__device__ __noinline__ double exact_score(double x, bool sigm, double most, double total) {
+  if (!sigm) return exp(x - most) / total;
+  const double e = exp(x < 0.0 ? x : -x);
+  return (x < 0.0 ? e : 1.0) / (1.0 + e);
+}
+template <typename T>
+__device__ __noinline__ double exact_total(const T *x, int E, float most, unsigned m8) {
+  double total = 0.0;
+  for (int e0 = threadIdx.x % 8; e0 < E; e0 += 32) {  // four exponentials on their way
+    double part[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const double v = e0 + 8 * i < E ? (double)to_acc(x[e0 + 8 * i]) : -INFINITY;
+      part[i] = v == -INFINITY ? 0.0 : exp(v - most);
     }
+    total += (part[0] + part[1]) + (part[2] + part[3]);
+  }
+  return sum_over<8>(m8, total);
+}
+// c as an ordered integer (to_key), 0 for an expert that is never chosen.
+template <typename T>
+__device__ __forceinline__ unsigned long long exact_key(const TopkArgs &p, const T *x, int e, float most, double total) {
+  const double v = to_acc(x[e]), b = p.bias ? (double)__ldg((const float *)p.bias + e) : 0.0;
+  return v == -INFINITY || b == -INFINITY ? 0ull : to_key(exact_score(v, p.sigmoid, most, total) + b);
+}
+// The groups to keep of a token: those surely above the border stay, the ones near it (up to eight) by their exact
+// scores.  gkey: the groups' f32 scores, a, b: those of the last one kept and the first one dropped.  False: too many.
+template <typename T>
+__device__ __noinline__ bool settle_groups(const TopkArgs &p, const T *x, const uint32_t *gkey, uint32_t *kept, float a, float b,
+                                           float most, unsigned m8) {
+  const int sub = threadIdx.x % 8, per = p.E / p.G;
+  const double total = p.sigmoid ? 1.0 : exact_total(x, p.E, most, m8);
+  const float tol = 0x1p-16f * (1.0f + fabsf(b));
+  int sure = 0, n = 0, g_of = -1;
+  unsigned long long of = 0;
+  for (int g = 0; g < p.G; ++g) {
+    const float s = from_key(gkey[g]);
+    const bool stays = kept[g], open = gkey[g] > kNoKey && !(stays ? s - b > tol : a - s > tol);
+    if (!open) {
+      sure += stays;
+      continue;
+    }
+    unsigned long long k0 = 0, k1 = 0;  // the group's two best
+    for (int i = sub; i < per; i += 8) {
+      const unsigned long long k = exact_key(p, x, g * per + i, most, total);
+      k1 = k > k0 ? k0 : k > k1 ? k : k1;
+      k0 = k > k0 ? k : k0;
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+      const unsigned long long q0 = __shfl_xor_sync(m8, k0, o), q1 = __shfl_xor_sync(m8, k1, o);
+      const unsigned long long low = k0 < q0 ? k0 : q0, high = k1 > q1 ? k1 : q1;
+      k1 = low > high ? low : high;
+      k0 = k0 > q0 ? k0 : q0;
+    }
+    if (n == sub) {
+      g_of = g;
+      of = p.gtop == 2 && k1 ? to_key(from_key(k0) + from_key(k1)) : k0;
+    }
+    ++n;
+  }
+  if (n > 8) return false;
+  int rank = 0;
+  for (int o = 0; o < n; ++o) {
+    const unsigned long long k = __shfl_sync(m8, of, o, 8);
+    rank += k > of || (k == of && o < sub);
+  }
+  if (g_of >= 0) kept[g_of] = rank < p.keep - sure;
+  return true;
+}
+// The list's experts and the best beyond it in their exact order: lane j's e (-1: none) becomes the j-th.  left: the two
+// best packed keys beyond the list.  False: the second of them may belong to the first k.
+template <typename T>
+__device__ __noinline__ bool settle_list(const TopkArgs &p, const T *x, int &e, uint32_t left0, uint32_t left1, float most, unsigned m8) {
+  const int sub = threadIdx.x % 8;
+  const double total = p.sigmoid || !p.bias ? 1.0 : exact_total(x, p.E, most, m8);
+  auto exact = [&](int of) { return of < 0 ? 0ull : p.bias ? exact_key(p, x, of, most, total) : to_key((double)to_acc(x[of])); };
+  const int e9 = left0 > kNoKey ? (int)(p.mask - (left0 & p.mask)) : -1;
+  const unsigned long long key = exact(e), key9 = exact(e9);
+  const bool after9 = key9 > key || (key9 == key && key9 && e9 < e);
+  int rank = after9;
+#pragma unroll
+  for (int o = 0; o < 8; ++o) {
+    const unsigned long long k = __shfl_sync(m8, key, o, 8);
+    const int eo = __shfl_sync(m8, e, o, 8);
+    rank += k > key || (k == key && (k ? eo < e : o < sub));  // those without an expert stay in order at the end
+  }
+  const int rank9 = 8 - __popc(__ballot_sync(m8, after9));
+  unsigned long long last = rank9 == p.k - 1 ? key9 : 0ull;  // the k-th
+  int sorted = rank9 == sub ? e9 : -1;
+#pragma unroll
+  for (int o = 0; o < 8; ++o) {
+    const int r = __shfl_sync(m8, rank, o, 8), eo = __shfl_sync(m8, e, o, 8);
+    const unsigned long long k = __shfl_sync(m8, key, o, 8);
+    if (r == sub) sorted = eo;
+    if (r == p.k - 1) last = k;
+  }
+  e = sorted;
+  if (left1 <= kNoKey) return true;
+  const float c = from_key(left1 | p.mask);
+  float tol = 0.0f;
+  if (p.bias) {
+    const int el = (int)(p.mask - (left1 & p.mask));
+    const float xl = to_acc(x[el]), b = __ldg((const float *)p.bias + el);
+    tol = (rough_error(p.sigmoid ? fabsf(xl) : most - xl, p.sigmoid) + 0x1p-23f) * (fabsf(c) + fabsf(b));
+  }
+  return last != 0 && from_key(last) - c > tol;
+}
+
+__host__ __device__ constexpr int list_words(int E, int G) { return (E + E / 8 + 1 + 2 * G) | 1; }
+
+template <typename T, bool Whole>
+__global__ void __launch_bounds__(kThreads, 5) topk_lists_kernel(const __grid_constant__ TopkArgs p) {
+  extern __shared__ __align__(16) unsigned char rooms[];
+  constexpr int V = 16 / (int)sizeof(T);
+  const int sub = threadIdx.x % 8, slot = threadIdx.x / 8;
+  const int64_t t_ = (int64_t)blockIdx.x * (kThreads / 8) + slot, t = t_ < p.ntok ? t_ : p.ntok - 1;
+  const bool mine = t_ < p.ntok;
+  const T *x = (const T *)p.x + t * p.E;
+  const float *bias = (const float *)p.bias;
+  const bool grouped = p.keep < p.G, by_score = p.bias || (grouped && p.gtop == 2);
+  const uint32_t mask = p.mask;
+  auto load = [&](int e0, float (&v)[8]) {  // -inf past the last expert
+    if constexpr (Whole) {
+#pragma unroll
+      for (int i = 0; i < 8; i += V) {
+        Pack<T, V> q;
+        if (e0 + i < p.E) q = load_pack<T, V>(x + e0 + i);
+#pragma unroll
+        for (int l = 0; l < V; ++l) v[i + l] = e0 + i < p.E ? to_acc(q.v[l]) : none<float>();
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = e0 + i < p.E ? to_acc(x[e0 + i]) : none<float>();
+    }
+  };
+  const int first = sub * 8;
+  float most = none<float>(), total = 0.0f;
+  if (!p.sigmoid && (by_score || !p.renorm)) {
+    for (int e0 = first; e0 < p.E; e0 += 64) {
+      float v[8];
+      load(e0, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = v[i] != v[i] || v[i] > most ? v[i] : most;
+    }
+    most = most_over<8>(kAll, most);
+    for (int e0 = first; e0 < p.E; e0 += 64) {  // at most 16 parts of eight terms
+      float v[8], part = 0.0f;
+      load(e0, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) part += v[i] == none<float>() ? 0.0f : expf(v[i] - most);
+      total += part;
+    }
+    total = sum_over<8>(kAll, total);
+  }
+  auto biases = [&](int e0, float (&b)[8]) {
+    if (bias && e0 + 8 <= p.E && !((uintptr_t)bias & 15)) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 4) {
+        const float4 q = __ldg(reinterpret_cast<const float4 *>(bias + e0 + i));
+        b[i] = q.x;
+        b[i + 1] = q.y;
+        b[i + 2] = q.z;
+        b[i + 3] = q.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) b[i] = bias && e0 + i < p.E ? __ldg(bias + e0 + i) : 0.0f;
+    }
+  };
+  auto bits = [&](float v, float b) {  // the order of c
+    const float s = p.sigmoid ? rough_sigmoid(v) : __fdividef(__expf(v - most), total);
+    return v == none<float>() || b == none<float>() ? kNoKey : to_bits(s + b);
+  };
+  bool lost = false;  // not to be settled here
+  const unsigned m8 = 0xffu << (threadIdx.x & 24);
+  // the token's keys (a word more for eight: lanes and groups begin on different banks), the groups' scores
+  uint32_t *ckey = (uint32_t *)rooms + slot * list_words(p.E, p.G), *gkey = ckey + p.E + p.E / 8 + 1, *kept = gkey + p.G;
+  const int per = p.E / p.G;
+  if (grouped) {
+    for (int e0 = first; e0 < p.E; e0 += 64) {
+      float v[8], b[8];
+      load(e0, v);
+      if (by_score) biases(e0, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (e0 + i < p.E) ckey[e0 + e0 / 8 + i] = by_score ? bits(v[i], b[i]) : to_bits(v[i]);
+    }
+    __syncwarp();
+    for (int g = sub; g < p.G; g += 8) {
+      uint32_t a = kNoKey, b = kNoKey;
+#pragma unroll 4
+      for (int i = g * per; i < (g + 1) * per; ++i) {
+        const uint32_t k = ckey[i + i / 8];
+        b = max(b, min(a, k));
+        a = max(a, k);
+      }
+      gkey[g] = p.gtop == 2 && b > kNoKey ? to_bits(from_key(a) + from_key(b)) : a;
+    }
+    __syncwarp();
+    uint32_t last = kAll, next = 0;  // the least group kept, the best one dropped
+    for (int g = sub; g < p.G; g += 8) {
+      const uint32_t k = gkey[g];
+      int rank = 0;
+#pragma unroll 4
+      for (int o = 0; o < p.G; ++o) rank += gkey[o] > k || (gkey[o] == k && o < g);
+      kept[g] = rank < p.keep;
+      if (rank < p.keep) last = min(last, k);
+      else next = max(next, k);
+    }
+    last = over<8>(kAll, last, [](uint32_t a, uint32_t b) { return min(a, b); });
+    next = over<8>(kAll, next, [](uint32_t a, uint32_t b) { return max(a, b); });
+    const float a = from_key(last), b = from_key(next);
+    if (by_score && next > kNoKey && !(a - b > 0x1p-16f * (1.0f + fabsf(b))))  // the four s' errors, as groups_too_near
+      lost = !settle_groups(p, x, gkey, kept, a, b, most, m8);
+    __syncwarp();
+  }
+  uint32_t list[8], left[2] = {0, 0};  // the two best beyond the list
+#pragma unroll
+  for (int i = 0; i < 8; ++i) list[i] = 0;
+#pragma unroll 1
+  for (int e0 = first; e0 < p.E; e0 += 64) {
+    uint32_t k[8];
+    float v[8], b[8];
+    if (!(grouped && bias)) load(e0, v);
+    if (!grouped && bias) biases(e0, b);
+    const bool same = per % 8 == 0;  // eight neighbours of one group
+    const bool in = grouped && same && e0 < p.E && kept[__umulhi(e0, p.inv_per)];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = e0 + i;
+      if (!grouped) k[i] = bias ? bits(v[i], b[i]) : to_bits(v[i]);
+      else k[i] = !(same ? in : e < p.E && kept[__umulhi(e, p.inv_per)]) ? 0u : bias ? ckey[e0 + e0 / 8 + i] : to_bits(v[i]);
+      k[i] = (k[i] & ~mask) | ((mask - e) & mask);  // past the last expert: no candidate
+    }
+    sort8(k);
+    if (e0 == first) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) list[i] = k[i];
+    } else {
+      merge8(list, k, left);
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) {
+    uint32_t b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i] = __shfl_xor_sync(kAll, list[i], o);
+    const uint32_t l0 = __shfl_xor_sync(kAll, left[0], o), l1 = __shfl_xor_sync(kAll, left[1], o);
+    leave(l0, left);
+    leave(l1, left);
+    merge8(list, b, left);
+  }
+  uint32_t key = 0, next = left[0];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (i == sub) key = list[i];
+    if (i == sub + 1) next = list[i];
+  }
+  int e = key > kNoKey ? (int)(mask - (key & mask)) : -1;
+  float xe = e >= 0 ? to_acc(x[e]) : none<float>();
+  if (bias || sizeof(T) == 4) {  // 16-bit logits are whole beside the index
+    bool near = false;
+    if (sub < p.k && e >= 0 && next > kNoKey) {
+      const int en = (int)(mask - (next & mask));
+      const float xn = to_acc(x[en]);
+      if (bias) near = packed_near(key, next, mask, xe, xn, __ldg(bias + e), __ldg(bias + en), p.sigmoid ? fmaxf(fabsf(xe), fabsf(xn)) : most - fminf(xe, xn), p.sigmoid);
+      else near = ((key ^ next) & ~mask) == 0 && xe != xn;
+    }
+    if (__ballot_sync(kAll, near) & m8) {
+      lost |= !settle_list(p, x, e, left[0], left[1], most, m8);
+      xe = e >= 0 ? to_acc(x[e]) : none<float>();
+    }
+    __syncwarp();
+  }
+  const bool have = sub < p.k && e >= 0;
+  if (!have) xe = none<float>();
+  const float top = p.renorm ? most_over<8>(kAll, xe) : 0.0f;
+  const float w = !have ? 0.0f : p.renorm ? relative_score(xe, top, p.sigmoid) : p.sigmoid ? sigmoid(xe) : expf(xe - most) / total;
+  const float sum = p.renorm ? sum_over<8>(kAll, w) + (by_score ? total * 0.0f : 0.0f) : 1.0f;  // as in choose()
+  const unsigned unsure = __ballot_sync(kAll, lost && mine);
+  if (mine && sub < p.k && !lost) {
+    p.expert[t * p.k + sub] = have ? e : -1;
+    ((float *)p.w)[t * p.k + sub] = have ? (float)p.scale * (w / sum) : 0.0f;
+  }
+  if (unsure) {  // the warp's rooms are read no more
+    unsigned char *room = (unsigned char *)((uint32_t *)rooms + (threadIdx.x / 32) * 4 * list_words(p.E, p.G));
+    for (int i = 0; i < 4; ++i)
+      if (unsure >> (8 * i) & 255) {
+        const int64_t again = (int64_t)blockIdx.x * (kThreads / 8) + (threadIdx.x / 32) * 4 + i;
+        if (p.E <= 256) choose_again<T, 8, 1>(p, again, room);
+        else choose_again<T, 32, 1>(p, again, room);
+      }
+  }
 }
 
 struct TopkGradArgs {
@@ -324,6 +840,69 @@ struct TopkGradArgs {
   double scale;
   void *dx;
 };
+
+// The gradient where it reaches the chosen logits alone: a warp takes `tokens` (up to 32) neighbouring ones, a thread
+// works out a token's few values and adds them into a tile of zeros in shared memory, which the warp then stores.
+// Bound by the zeros' way to memory.
+template <typename T, int V>
+__global__ void __launch_bounds__(64) topk_grad_sparse_kernel(const __grid_constant__ TopkGradArgs p, int tokens) {
+  using A = acc_t<T>;
+  extern __shared__ __align__(16) unsigned char tiles[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const int64_t t0 = ((int64_t)blockIdx.x * 2 + warp) * tokens, t = t0 + lane;
+  if (t0 >= p.ntok) return;
+  const int have = (int)min((int64_t)tokens, p.ntok - t0), n = have * p.E;
+  A *tile = (A *)tiles + (size_t)warp * ((tokens * p.E + 15) / 16 * 16);
+  for (int c = lane; c < n; c += 32) tile[c] = A(0);
+  __syncwarp();
+  if (lane < have) {
+    const T *x = (const T *)p.x + t * p.E;
+    const int32_t *e = p.expert + t * p.k;
+    const A *dw = (const A *)p.dw + t * p.k;
+    A *to = tile + lane * p.E;
+    auto logit = [&](int j) {  // -inf: no pair
+      const int ej = __ldg(e + j);
+      return (unsigned)ej < (unsigned)p.E ? to_acc(x[ej]) : none<A>();
+    };
+    const A scale = (A)p.scale;
+    A sum = A(1), mean = A(0), top = none<A>();
+    if (p.renorm) {
+      for (int j = 0; j < p.k; ++j) {
+        const A v = logit(j);
+        top = v != v || v > top ? v : top;
+      }
+      sum = A(0);
+      for (int j = 0; j < p.k; ++j) {
+        const A v = logit(j);
+        if (v == none<A>()) continue;
+        const A r = relative_score(v, top, p.sigmoid);
+        sum += r;
+        mean += r * (scale * __ldg(dw + j));
+      }
+      mean /= sum;
+    }
+    for (int j = 0; j < p.k; ++j) {
+      const A v = logit(j);
+      if (v == none<A>()) continue;
+      const A r = p.renorm ? relative_score(v, top, p.sigmoid) / sum : sigmoid(v);
+      A g = r * (scale * __ldg(dw + j) - mean);
+      if (p.sigmoid) g *= sigmoid(-v);
+      to[__ldg(e + j)] += g;
+    }
+  }
+  __syncwarp();
+  T *dx = (T *)p.dx + t0 * p.E;
+  for (int c = lane * V; c < n; c += 32 * V) {
+    if (c + V <= n) {
+      Pack<T, V> o;
+#pragma unroll
+      for (int l = 0; l < V; ++l) o.v[l] = from_acc<T>(tile[c + l]);
+      store_pack<T, V>(dx + c, o);
+    } else {
+      for (int l = c; l < n; ++l) dx[l] = from_acc<T>(tile[l]);
+    }
+  }
+}
 
 template <typename T, int L, int N>
 __global__ void __launch_bounds__(kThreads) topk_grad_kernel(const __grid_constant__ TopkGradArgs p) {
@@ -347,57 +926,28 @@ __global__ void __launch_bounds__(kThreads) topk_grad_kernel(const __grid_consta
     g[s] = e[s] >= 0 ? scale * __ldg((const A *)p.dw + t * p.k + j) : A(0);
   }
   A out[N];
+  A most = none<A>(), total = A(0), sum = A(0);
 #pragma unroll
-  for (int i = 0; i < N; ++i) out[i] = A(0);
-  if (p.renorm) {
-    A top = none<A>();
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s) top = xe[s] != xe[s] || xe[s] > top ? xe[s] : top;
-    top = most_over<L>(mask, top);
-    A n[kSlots], sum = A(0), mean = A(0);
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s) {
-      n[s] = e[s] >= 0 ? relative_score(xe[s], top, p.sigmoid) : A(0);
-      sum += n[s];
-    }
-    sum = sum_over<L>(mask, sum);
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s) {
-      n[s] = e[s] >= 0 ? n[s] / sum : A(0);
-      mean += n[s] * g[s];
-    }
-    mean = sum_over<L>(mask, mean);
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s)
-      if (e[s] >= 0) g[s] = n[s] * (g[s] - mean) * (p.sigmoid ? sigmoid(-xe[s]) : A(1));
-  } else if (p.sigmoid) {
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s)
-      if (e[s] >= 0) g[s] *= sigmoid(xe[s]) * sigmoid(-xe[s]);
-  } else {
-    A most = none<A>(), total = A(0), sum = A(0);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      out[i] = i * L + lane < p.E ? to_acc(x[i * L + lane]) : none<A>();
-      most = out[i] != out[i] || out[i] > most ? out[i] : most;
-    }
-    most = most_over<L>(mask, most);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      out[i] = out[i] == none<A>() ? A(0) : exp_(out[i] - most);
-      total += out[i];
-    }
-    total = sum_over<L>(mask, total);
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s) {
-      if (e[s] >= 0) g[s] *= exp_(xe[s] - most) / total;
-      sum += g[s];
-    }
-    sum = sum_over<L>(mask, sum);
-    const A f = total > A(0) || total != total ? sum / total : A(0);
-#pragma unroll
-    for (int i = 0; i < N; ++i) out[i] = -out[i] * f;
+  for (int i = 0; i < N; ++i) {
+    out[i] = i * L + lane < p.E ? to_acc(x[i * L + lane]) : none<A>();
+    most = out[i] != out[i] || out[i] > most ? out[i] : most;
   }
+  most = most_over<L>(mask, most);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    out[i] = out[i] == none<A>() ? A(0) : exp_(out[i] - most);
+    total += out[i];
+  }
+  total = sum_over<L>(mask, total);
+#pragma unroll
+  for (int s = 0; s < kSlots; ++s) {
+    if (e[s] >= 0) g[s] *= exp_(xe[s] - most) / total;
+    sum += g[s];
+  }
+  sum = sum_over<L>(mask, sum);
+  const A f = total > A(0) || total != total ? sum / total : A(0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) out[i] = -out[i] * f;
 #pragma unroll
   for (int s = 0; s < kSlots; ++s)
     for (int l = 0; l < L && s * L + l < p.k; ++l) {
@@ -446,14 +996,38 @@ int topk(const T *x, const acc_t<T> *bias, int64_t ntok, int E, int k, int score
   if (ntok == 0) return DP_OK;
   if (!x || !expert || !w) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (!at_elements(x, bias, w) || !at_elements(expert)) return misaligned(who);
-  const TopkArgs p{x, bias, ntok, E, k, score == DP_SCORE_SIGMOID, G, keep, E / G == 1 ? 1 : gtop, renorm != 0, scale, expert, w};
-  with_shape(E, [&](auto L_, auto N_) {
-    constexpr int L = decltype(L_)::value, N = decltype(N_)::value, tok = kThreads / L;
-    const size_t smem = keep < G ? (size_t)tok * (E + 2 * G) * 8 : 0;
-    auto kernel = topk_kernel<T, L, N>;
-    if (smem > 48 * 1024 && (rc = allow_smem((const void *)kernel, (size_t)kThreads * N * 3 * 8, who))) return;
-    kernel<<<(unsigned)((ntok + tok - 1) / tok), kThreads, smem, (cudaStream_t)stream>>>(p);
-  });
+  if (G == E) G = keep = 1;  // groups of one: their best are the best experts
+  TopkArgs p{x, bias, ntok, E, k, score == DP_SCORE_SIGMOID, G, keep, gtop, renorm != 0, scale, expert, w, 0, 0};
+  p.inv_per = (uint32_t)(((1ull << 32) + E / G - 1) / (E / G));
+  while ((int)p.mask < E - 1) p.mask = 2 * p.mask + 1;
+  const cudaStream_t st = (cudaStream_t)stream;
+  if constexpr (sizeof(T) < 8)
+    if (k <= kList) {
+      constexpr int tok = kThreads / 8;
+      const bool whole = (((uintptr_t)x | (uintptr_t)(E * sizeof(T))) & 15) == 0;
+      auto kernel = whole ? topk_lists_kernel<T, true> : topk_lists_kernel<T, false>;
+      const size_t smem = keep < G ? (size_t)tok * list_words(E, G) * 4 : 0;
+      if (smem > 48 * 1024 && (rc = allow_smem((const void *)kernel, (size_t)tok * list_words(kMaxExperts, kMaxExperts / 2) * 4, who))) return rc;
+      kernel<<<(unsigned)((ntok + tok - 1) / tok), kThreads, smem, st>>>(p);
+      return launch_status(who);
+    }
+  auto go = [&](auto N_, auto S_) {
+    constexpr int N = decltype(N_)::value, S = decltype(S_)::value, tok = kThreads / 32;
+    const size_t smem = keep < G ? (size_t)tok * room_words(E, G) * 8 : 0;
+    auto kernel = topk_kernel<T, N, S>;
+    if (smem > 48 * 1024 && (rc = allow_smem((const void *)kernel, (size_t)tok * room_words(32 * N, 16 * N) * 8, who))) return;
+    kernel<<<(unsigned)((ntok + tok - 1) / tok), kThreads, smem, st>>>(p);
+  };
+  using std::integral_constant;
+  if (k < 32) {
+    if (E <= 32) go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+    else if (E <= 128) go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+    else if (E <= 256) go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    else go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+  } else {
+    if (E <= 256) go(integral_constant<int, 8>{}, integral_constant<int, 3>{});
+    else go(integral_constant<int, 32>{}, integral_constant<int, 3>{});
+  }
   return rc ? rc : launch_status(who);
 }
 
@@ -468,6 +1042,17 @@ int topk_grad(const T *x, const int32_t *expert, const acc_t<T> *dw, int64_t nto
   if (!x || !expert || !dw || !dx) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (!at_elements(x, dx) || !at_elements(expert) || !at_elements(dw)) return misaligned(who);
   const TopkGradArgs p{x, expert, dw, ntok, E, k, score == DP_SCORE_SIGMOID, renorm != 0, scale, dx};
+  if (renorm || score == DP_SCORE_SIGMOID) {
+    const int most = 8192 / (int)sizeof(acc_t<T>) / E, tokens = most >= 32 ? 32 : most >= 8 ? most / 8 * 8 : most < 1 ? 1 : most;
+    const size_t smem = (size_t)(tokens * E + 15) / 16 * 16 * sizeof(acc_t<T>) * 2;
+    constexpr int V = 16 / (int)sizeof(T);
+    // a warp's tile begins at whole packs
+    const bool whole = (((uintptr_t)dx | (uintptr_t)(tokens * E * sizeof(T))) & 15) == 0;
+    auto k_ = whole ? topk_grad_sparse_kernel<T, V> : topk_grad_sparse_kernel<T, 1>;
+    const int64_t blocks = (ntok + 2 * tokens - 1) / (2 * tokens);
+    k_<<<(unsigned)blocks, 64, smem, (cudaStream_t)stream>>>(p, tokens);
+    return launch_status(who);
+  }
   with_shape(E, [&](auto L_, auto N_) {
     constexpr int L = decltype(L_)::value, N = decltype(N_)::value, tok = kThreads / L;
     topk_grad_kernel<T, L, N><<<(unsigned)((ntok + tok - 1) / tok), kThreads, 0, (cudaStream_t)stream>>>(p);
