@@ -4,6 +4,8 @@
 // The gradient's sums run over the tokens sorted by id, in their order, cut at multiples of a number of rows that
 // the sizes alone give, and the pieces of a cut run are added in order: no atomics, results repeat bit for bit.
 // All are bound by memory.
+#include <cooperative_groups.h>
+
 #include "rows.cuh"
 
 namespace dpc {
@@ -12,6 +14,8 @@ namespace {
 constexpr int kMaxVocab = (1 << 24) - 1, kMaxH = 1 << 20;
 
 // ------------------------------------------------------------------ the plan: a stable radix sort of the ids
+// Up to 4096 ids in one block, up to 65,536 in a cluster of up to eight blocks that read one another's counts (one launch
+// either way), more in three launches a digit.
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortPer = 4, kSortBlock = kSortThreads * kSortPer;
 constexpr int kDigits = 256;
 
@@ -20,17 +24,19 @@ __device__ __forceinline__ uint32_t sort_key(int32_t id, int nvocab) {
   return (uint32_t)id < (uint32_t)nvocab ? (uint32_t)id : (uint32_t)nvocab;
 }
 
-// A thread's kSortPer items of a block in order by warp, 32 apart: the warp counts them by digit.
+// A thread's kPer items of a block in order by warp, 32 apart: the warp counts them by digit.
+template <int kPer>
 struct SortItems {
-  uint32_t key[kSortPer];
+  uint32_t key[kPer];
   int64_t first;
 };
 
 // The place of every item of a block in a digit, after the warps before it and those before it in its warp.  cnt: a row
 // of kDigits counters a warp, from counts to the warp's next place.
-__device__ __forceinline__ void count_digits(const SortItems &it, int64_t n, int shift, int mask, int *mine) {
+template <int kPer>
+__device__ __forceinline__ void count_digits(const SortItems<kPer> &it, int64_t n, int shift, int mask, int *mine) {
 #pragma unroll
-  for (int i = 0; i < kSortPer; ++i)
+  for (int i = 0; i < kPer; ++i)
     if (it.first + 32 * i < n) atomicAdd(mine + (it.key[i] >> shift & mask), 1);  // integers: any order gives the same
 }
 
@@ -80,7 +86,7 @@ __global__ void __launch_bounds__(kSortThreads)
   uint32_t *keys = (uint32_t *)(sums + kSortWarps);
   int *idx = (int *)(keys + 2 * kSortBlock);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, mask = (1 << bits) - 1;
-  SortItems it;
+  SortItems<kSortPer> it;
   int id[kSortPer];
   it.first = warp * kSortPer * 32 + lane;
 #pragma unroll
@@ -134,6 +140,88 @@ __global__ void __launch_bounds__(kSortThreads)
   for (int v = threadIdx.x; v <= nvocab; v += kSortThreads) start[v] = lower_bound(sorted, n, v);
 }
 
+// The digits' places in global memory (keys and idx: two of each), blocks of a cluster.  A block's counts of a digit's
+// pass lie in its shared memory until all have read them.  start: with one digit its scan, else each block searches the
+// ids between its sorted keys.
+constexpr int kClusterBlocks = 8, kClusterStart = 1 << 16;
+template <int kPer>
+__global__ void __launch_bounds__(kSortThreads)
+    embed_plan_cluster_kernel(const int32_t *__restrict__ ids, int n, int nvocab, int passes, int bits, uint32_t *keys, int *idx,
+                              int64_t *__restrict__ start, int32_t *src) {
+  namespace cg = cooperative_groups;
+  constexpr int kItems = kSortThreads * kPer;
+  __shared__ int cnt[kSortWarps * kDigits], block[kDigits], sums[kDigits / 32];
+  static_assert(kItems <= kSortWarps * kDigits, "a block's keys in the counters' place");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, mask = (1 << bits) - 1, d = threadIdx.x;
+  SortItems<kPer> it;
+  int id[kPer];
+  it.first = (int64_t)blockIdx.x * kItems + warp * kPer * 32 + lane;
+  for (int pass = 0; pass < passes; ++pass) {
+    const uint32_t *from_k = keys + (int64_t)((pass - 1) & 1) * n;
+    const int *from_i = idx + (int64_t)((pass - 1) & 1) * n;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {  // written by other blocks in the pass before: not through L1
+      const int64_t q = it.first + 32 * i;
+      it.key[i] = q >= n ? 0u : pass ? __ldcg(from_k + q) : sort_key(__ldg(ids + q), nvocab);
+      id[i] = q >= n ? 0 : pass ? __ldcg(from_i + q) : (int)q;
+    }
+    for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) cnt[i] = 0;
+    __syncthreads();
+    int *mine = cnt + warp * kDigits;
+    const int shift = pass * bits;
+    count_digits(it, n, shift, mask, mine);
+    __syncthreads();
+    if (d < kDigits) {
+      int c = 0;
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) c += cnt[w * kDigits + d];
+      block[d] = c;
+    }
+    cg::this_cluster().sync();
+    int total = 0, before = 0;
+    if (d < kDigits)
+      for (int b = 0; b < (int)gridDim.x; ++b) {
+        const int c = cg::this_cluster().map_shared_rank(block, b)[d];
+        before += b < (int)blockIdx.x ? c : 0;
+        total += c;
+      }
+    int run = scan_digits(total, sums);
+    if (passes == 1 && blockIdx.x == 0 && d <= nvocab) start[d] = run;
+    if (d < kDigits) {
+      run += before;
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) {
+        const int c = cnt[w * kDigits + d];
+        cnt[w * kDigits + d] = run;
+        run += c;
+      }
+    }
+    __syncthreads();
+    const bool last = pass == passes - 1;
+    uint32_t *to_k = keys + (int64_t)(pass & 1) * n;
+    int *to_i = last ? src : idx + (int64_t)(pass & 1) * n;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const bool have = it.first + 32 * i < n;
+      const int p = take_place(it.key[i] >> shift & mask, have, lane, mine);
+      if (have) {
+        if (!last || passes > 1) to_k[p] = it.key[i];
+        to_i[p] = last && it.key[i] >= (uint32_t)nvocab ? -1 : id[i];
+      }
+    }
+    cg::this_cluster().sync();  // the counts are read, the places written
+  }
+  if (passes == 1 || nvocab > kClusterStart) return;
+  uint32_t *sorted = (uint32_t *)cnt;
+  const uint32_t *from = keys + (int64_t)((passes - 1) & 1) * n;
+  const int first = blockIdx.x * kItems, own = min(kItems, n - first);
+  for (int i = threadIdx.x; i < own; i += kSortThreads) sorted[i] = __ldcg(from + first + i);
+  const int low = first ? (int)__ldcg(from + first - 1) + 1 : 0;
+  __syncthreads();
+  const int high = first + own == n ? nvocab : (int)sorted[own - 1];
+  for (int v = low + threadIdx.x; v <= high; v += kSortThreads) start[v] = first + lower_bound(sorted, own, v);
+}
+
 // More ids, a pass of a digit: counts[d][block], each digit's scan over the blocks with its total behind, and the move.
 __global__ void __launch_bounds__(kSortThreads)
     sort_count_kernel(const int32_t *__restrict__ ids, const uint32_t *__restrict__ keys, int64_t n, int nvocab, int shift,
@@ -174,7 +262,7 @@ __global__ void __launch_bounds__(kSortThreads)
   __shared__ int cnt[kSortWarps * kDigits], sums[kSortWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) cnt[i] = 0;
-  SortItems it;
+  SortItems<kSortPer> it;
   int id[kSortPer];
   it.first = (int64_t)blockIdx.x * kSortBlock + warp * kSortPer * 32 + lane;
 #pragma unroll
@@ -230,137 +318,205 @@ SortShape sort_shape(int64_t n, int nvocab) {
 }
 
 // ------------------------------------------------------------------ the rows
-// V elements an access; a row's packs go to np threads in order, rows after rows.
-template <typename T, int V>
-__global__ void __launch_bounds__(128)
+// V elements an access.  Long rows: a warp takes kFwdPart packs a lane of a token's row.  Short ones (Flat, fewer packs than
+// lanes): a thread takes one pack, the packs in order over the tokens.
+constexpr int kFwdThreads = 128, kFwdPart = 2;
+template <typename T, int V, bool Flat>
+__global__ void __launch_bounds__(kFwdThreads)
     embed_fwd_kernel(const T *__restrict__ W, const int32_t *__restrict__ ids, int64_t ntok, int nvocab, int H, int np,
                      acc_t<T> scale, const T *add, T *y) {  // y may be add
   using A = acc_t<T>;
-  const int64_t base = (int64_t)blockIdx.x * 128, t0 = base / np;
-  const uint32_t off = (uint32_t)(base - t0 * np) + threadIdx.x, dt = off / (uint32_t)np;
-  const int64_t t = t0 + dt;
-  const int c = (int)(off - dt * np) * V;
+  constexpr int kP = Flat ? 1 : kFwdPart;
+  int64_t t;
+  int c;
+  if constexpr (Flat) {
+    const int64_t base = (int64_t)blockIdx.x * kFwdThreads, t0 = base / np;
+    const uint32_t off = (uint32_t)(base - t0 * np) + threadIdx.x, dt = off / (uint32_t)np;
+    t = t0 + dt;
+    c = (int)(off - dt * np);
+  } else {
+    t = (int64_t)blockIdx.x * (kFwdThreads / 32) + (threadIdx.x >> 5);
+    c = (int)(blockIdx.y * 32 * kP + (threadIdx.x & 31));
+  }
   if (t >= ntok) return;
+  Pack<T, V> a[kP], w[kP];
+#pragma unroll
+  for (int i = 0; i < kP; ++i)
+    if (add && c + 32 * i < np) a[i] = load_pack<T, V>(add + t * H + (c + 32 * i) * V);
   const int32_t id = __ldg(ids + t);
   const bool have = (uint32_t)id < (uint32_t)nvocab;
-  Pack<T, V> a{}, w{};
-  if (add) a = load_pack<T, V>(add + t * H + c);
-  if (have) w = load_pack<T, V>(W + (int64_t)id * H + c);
-  Pack<T, V> o;
+  const T *row = W + (int64_t)id * H;
 #pragma unroll
-  for (int l = 0; l < V; ++l) {
-    const A from = add ? to_acc(a.v[l]) : A(0);
-    o.v[l] = from_acc<T>(have ? fma(scale, to_acc(w.v[l]), from) : from);
-  }
-  store_pack<T, V>(y + t * H + c, o);
+  for (int i = 0; i < kP; ++i)
+    if (have && c + 32 * i < np) w[i] = load_pack<T, V>(row + (c + 32 * i) * V);
+#pragma unroll
+  for (int i = 0; i < kP; ++i)
+    if (c + 32 * i < np) {
+      Pack<T, V> o;
+#pragma unroll
+      for (int l = 0; l < V; ++l) {
+        const A from = add ? to_acc(a[i].v[l]) : A(0);
+        o.v[l] = from_acc<T>(have ? fma(scale, to_acc(w[i].v[l]), from) : from);
+      }
+      store_pack<T, V>(y + t * H + (c + 32 * i) * V, o);
+    }
 }
 
-// Blocks below `chunks x strips` sum a chunk of R sorted rows over a strip of columns: runs of an id that lie in the
-// chunk go to dW, what continues from the chunk before or into the next to `part` ([chunk][2][H]: the piece that begins
-// at the chunk's first row, and the one after it).  Further blocks clear the rows of ids that no token has.
-constexpr int kSumThreads = 256, kSumAhead = 8;
+// A group of `width` threads sums a chunk of R sorted rows over a strip of columns: runs of an id that lie in the chunk go
+// to dW, what continues from the chunk before or into the next to `part` ([chunk][2][H]: the piece that begins at the
+// chunk's first row, and the one after it); cut[chunk] is the id of the run that begins in the chunk and goes on, else -1.
+// Further blocks clear the rows of ids that no token has.  The chunk's tokens and ids are read first, so that the rows'
+// addresses wait for shared memory alone.
+constexpr int kSumThreads = 256, kMaxRows = 256, kMaxGroups = 8, kClearRows = 32;
+// Rows of a thread on their way.
+template <int V>
+constexpr int kSumAhead = V > 1 ? 8 : 16;
+struct SumShape {
+  int R, chunks, strips, width, groups;
+  int64_t blocks;  // that sum
+};
 template <typename T, int V>
 __global__ void __launch_bounds__(kSumThreads)
     embed_grad_kernel(const T *__restrict__ dy, const int32_t *__restrict__ ids, const int64_t *__restrict__ start,
-                      const int32_t *__restrict__ src, int64_t ntok, int nvocab, int H, int np, int R, int chunks, int strips,
-                      acc_t<T> scale, bool accumulate, acc_t<T> *__restrict__ dW, acc_t<T> *__restrict__ part) {
+                      const int32_t *__restrict__ src, int64_t ntok, int nvocab, int H, const __grid_constant__ SumShape s,
+                      acc_t<T> scale, bool accumulate, acc_t<T> *__restrict__ dW, acc_t<T> *__restrict__ part,
+                      int *__restrict__ cut) {
   using A = acc_t<T>;
-  if ((int)blockIdx.x >= chunks * strips) {
-    const int v = (int)blockIdx.x - chunks * strips;
-    if (__ldg(start + v) == __ldg(start + v + 1))
-      for (int c = threadIdx.x; c < H; c += kSumThreads) dW[(int64_t)v * H + c] = A(0);
+  constexpr int kAhead = kSumAhead<V>;
+  if ((int64_t)blockIdx.x >= s.blocks) {
+    const int64_t v0 = ((int64_t)blockIdx.x - s.blocks) * kClearRows;
+    const int lane = threadIdx.x & 31;
+    const int64_t at = v0 + lane < nvocab ? __ldg(start + v0 + lane) : 0, end = v0 + lane < nvocab ? __ldg(start + v0 + lane + 1) : 1;
+    unsigned empty = __ballot_sync(0xffffffffu, at == end);
+    for (int n = 0; empty; empty &= empty - 1, ++n)
+      if (n % (int)(blockDim.x / 32) == (int)threadIdx.x / 32) {
+        A *row = dW + (v0 + __ffs(empty) - 1) * H;
+        if ((((uintptr_t)dW | (uintptr_t)(H * sizeof(A))) & 15) == 0) {
+          for (int c = lane; c < H / (16 / (int)sizeof(A)); c += 32) reinterpret_cast<uint4 *>(row)[c] = make_uint4(0, 0, 0, 0);
+        } else {
+          for (int c = lane; c < H; c += 32) row[c] = A(0);
+        }
+      }
     return;
   }
-  const int chunk = blockIdx.x / strips, strip = blockIdx.x - chunk * strips;
-  const int c = (strip * kSumThreads + threadIdx.x) * V;
-  const int64_t kept = min(max(__ldg(start + nvocab), (int64_t)0), ntok), r0 = (int64_t)chunk * R;
-  if (r0 >= kept || c >= H) return;
-  const int rows = (int)min((int64_t)R, kept - r0);
-  auto id_at = [&](int64_t p) -> int {  // of sorted row p; -1 where the plan is not one of these ids
-    const int q = __ldg(src + p);
-    return q >= 0 && q < ntok ? __ldg(ids + q) : -1;
-  };
-  const int before = chunk ? id_at(r0 - 1) : -1, after = r0 + rows < kept ? id_at(r0 + rows) : -1;
+  __shared__ int froms[kMaxGroups * (kMaxRows + kSumAhead<1>)], idsm[kMaxGroups * (kMaxRows + 2)];
+  const int group = threadIdx.x / s.width, tid = threadIdx.x - group * s.width;
+  const int64_t unit = (int64_t)blockIdx.x * s.groups + group, chunk = unit / s.strips;
+  const int strip = (int)(unit - chunk * s.strips);
+  // a row's token (-1: none), and its id, of one row before, and one behind
+  int *from = froms + group * (s.R + kSumAhead<1>), *id = idsm + group * (s.R + 2);
+  const int64_t kept = min(max(__ldg(start + nvocab), (int64_t)0), ntok), r0 = chunk * s.R;
+  const int rows = chunk < s.chunks ? (int)min((int64_t)s.R, max(kept - r0, (int64_t)0)) : 0;
+  for (int r = tid - 1; r < rows + kAhead; r += s.width) {
+    const int64_t p = r0 + r;
+    const int q = p >= 0 && p < kept && r <= rows ? __ldg(src + p) : -1;
+    const bool have = q >= 0 && q < ntok;  // the plan may not be one of these ids
+    if (r <= rows) id[r + 1] = have ? __ldg(ids + q) : -1;
+    if (r >= 0) from[r] = have && r < rows ? q : -1;
+  }
+  __syncthreads();
+  if (chunk >= s.chunks) return;
+  if (rows == 0) {
+    if (strip == 0 && tid == 0) cut[chunk] = -1;
+    return;
+  }
+  const int c = (strip * s.width + tid) * V;
+  if (c >= H) return;
+  const int before = id[0], after = id[rows + 1];
   A sum[V] = {};
-  int run = id_at(r0), first = 0;  // the run at hand and its first row
-  auto put = [&](int end) {        // its rows end before `end`
+  int run = id[1], first = 0;  // the run at hand and its first row
+  auto put = [&](int end) {    // its rows end before `end`
     if ((uint32_t)run < (uint32_t)nvocab) {
-      const bool cut = (first == 0 && before == run) || (end == rows && after == run);
-      A *to = cut ? part + ((int64_t)chunk * 2 + (first ? 1 : 0)) * H + c : dW + (int64_t)run * H + c;
+      const bool is_cut = (first == 0 && before == run) || (end == rows && after == run);
+      A *to = is_cut ? part + (chunk * 2 + (first ? 1 : 0)) * H + c : dW + (int64_t)run * H + c;
 #pragma unroll
-      for (int l = 0; l < V; ++l) to[l] = cut ? sum[l] : accumulate ? fma(scale, sum[l], to[l]) : scale * sum[l];
+      for (int l = 0; l < V; ++l) to[l] = is_cut ? sum[l] : accumulate ? fma(scale, sum[l], to[l]) : scale * sum[l];
     }
 #pragma unroll
     for (int l = 0; l < V; ++l) sum[l] = A(0);
   };
-  for (int r = 0; r < rows; r += kSumAhead) {
-    Pack<T, V> v[kSumAhead];
-    int id[kSumAhead];
+  for (int r = 0; r < rows; r += kAhead) {
+    Pack<T, V> v[kAhead];
 #pragma unroll
-    for (int i = 0; i < kSumAhead; ++i) {
-      const int q = r + i < rows ? __ldg(src + r0 + r + i) : -1;
-      const bool have = q >= 0 && q < ntok;
-      id[i] = have ? __ldg(ids + q) : -1;
-      v[i] = have ? load_pack<T, V>(dy + (int64_t)q * H + c) : Pack<T, V>{};
+    for (int i = 0; i < kAhead; ++i) {
+      const int q = from[r + i];
+      v[i] = q >= 0 ? load_pack<T, V>(dy + (int64_t)q * H + c) : Pack<T, V>{};
     }
 #pragma unroll
-    for (int i = 0; i < kSumAhead; ++i)
+    for (int i = 0; i < kAhead; ++i)
       if (r + i < rows) {
-        if (id[i] != run) {
+        const int now = id[r + i + 1];
+        if (now != run) {
           put(r + i);
-          run = id[i];
+          run = now;
           first = r + i;
         }
 #pragma unroll
         for (int l = 0; l < V; ++l) sum[l] += to_acc(v[i].v[l]);
       }
   }
+  if (c == 0) cut[chunk] = (uint32_t)run < (uint32_t)nvocab && after == run && !(first == 0 && before == run) ? run : -1;
   put(rows);
 }
 
-// The runs that chunks cut: the block of the first chunk that such a run continues into adds its pieces in order.
-template <typename A>
-__global__ void __launch_bounds__(kSumThreads)
-    embed_join_kernel(const int32_t *__restrict__ ids, const int64_t *__restrict__ start, const int32_t *__restrict__ src,
-                      int64_t ntok, int nvocab, int H, int R, int chunks, A scale, bool accumulate, A *__restrict__ dW,
-                      const A *__restrict__ part) {
-  const int chunk = blockIdx.x + 1, c = blockIdx.y * kSumThreads + threadIdx.x;
-  const int64_t kept = min(max(__ldg(start + nvocab), (int64_t)0), ntok), r0 = (int64_t)chunk * R;
-  if (r0 >= kept || c >= H) return;
-  const int q = __ldg(src + r0);
-  if (q < 0 || q >= ntok) return;
-  const int v = __ldg(ids + q);
-  if ((uint32_t)v >= (uint32_t)nvocab) return;
-  const int64_t s0 = __ldg(start + v), s1 = min(__ldg(start + v + 1), kept);
-  if (s0 < 0 || s0 >= r0 || s0 / R != chunk - 1) return;  // not cut here, or not here first
-  const int last = (int)((s1 - 1) / R);
-  A sum = part[((int64_t)(chunk - 1) * 2 + (s0 % R ? 1 : 0)) * H + c];
+// The runs that chunks cut, eight chunks a block: a run's pieces are added in four parts of neighbouring ones, each in order,
+// and the parts in order.
+constexpr int kJoinSlots = 8, kJoinParts = 4;
+template <typename A, int V>
+__global__ void __launch_bounds__(kJoinSlots *kJoinParts * 32)
+    embed_join_kernel(const int64_t *__restrict__ start, int64_t ntok, int nvocab, int H, int R, int chunks, A scale,
+                      bool accumulate, A *__restrict__ dW, const A *__restrict__ part, const int *__restrict__ cut) {
+  __shared__ Pack<A, V> sums[kJoinSlots][kJoinParts][32];
+  const int lane = threadIdx.x % 32, which = threadIdx.x / 32 % kJoinParts, slot = threadIdx.x / (32 * kJoinParts);
+  const int chunk = blockIdx.x * kJoinSlots + slot, c = (blockIdx.y * 32 + lane) * V;
+  const int v = chunk < chunks ? __ldg(cut + chunk) : -1;
+  if (!__syncthreads_or(v >= 0)) return;
+  Pack<A, V> sum{};
+  if (v >= 0 && v < nvocab && c < H) {
+    const int64_t s0 = __ldg(start + v), s1 = min(__ldg(start + v + 1), ntok);
+    const int n = (int)min((s1 - 1) / R, (int64_t)chunks - 1) - chunk + 1, each = (n + kJoinParts - 1) / kJoinParts;  // pieces
+    const int end = min(n, (which + 1) * each);
 #pragma unroll 8
-  for (int k = chunk; k <= last; ++k) sum += part[(int64_t)k * 2 * H + c];
+    for (int k = which * each; k < end; ++k) {
+      const Pack<A, V> p = load_pack<A, V>(part + ((int64_t)(chunk + k) * 2 + (k == 0 && s0 % R ? 1 : 0)) * H + c);
+#pragma unroll
+      for (int l = 0; l < V; ++l) sum.v[l] += p.v[l];
+    }
+  }
+  sums[slot][which][lane] = sum;
+  __syncthreads();
+  if (which || v < 0 || v >= nvocab || c >= H) return;
+#pragma unroll
+  for (int k = 1; k < kJoinParts; ++k)
+#pragma unroll
+    for (int l = 0; l < V; ++l) sum.v[l] += sums[slot][k][lane].v[l];
   A *to = dW + (int64_t)v * H + c;
-  *to = accumulate ? fma(scale, sum, *to) : scale * sum;
+#pragma unroll
+  for (int l = 0; l < V; ++l) to[l] = accumulate ? fma(scale, sum.v[l], to[l]) : scale * sum.v[l];
 }
 
-struct SumShape {
-  int R, chunks, strips;
-};
-// About two blocks' worth of rows an SM, in chunks of whole batches of loads.
+// Strips of at most kSumThreads packs, whole warps a group, as many groups a block as fit, chunks of 16 to 256 rows.
 SumShape sum_shape(int64_t ntok, int np) {
   SumShape s;
   s.strips = (np + kSumThreads - 1) / kSumThreads;
-  const int64_t want = 152 * 4 / s.strips > 0 ? 152 * 4 / s.strips : 1;
-  int64_t R = (ntok + want - 1) / want;
-  R = (R + kSumAhead - 1) / kSumAhead * kSumAhead;
-  s.R = (int)(R < 16 ? 16 : R);
+  s.width = ((np + s.strips - 1) / s.strips + 31) / 32 * 32;
+  s.groups = kSumThreads / s.width;
+  int64_t want = (int64_t)152 * 4 * s.groups / s.strips;  // chunks of four blocks an SM, all resident
+  if (want < 1) want = 1;
+  int64_t R = ((ntok + want - 1) / want + 15) / 16 * 16;
+  s.R = (int)(R < 16 ? 16 : R > kMaxRows ? kMaxRows : R);
   s.chunks = (int)((ntok + s.R - 1) / s.R);
+  s.blocks = ((int64_t)s.chunks * s.strips + s.groups - 1) / s.groups;
   return s;
 }
-// The chunks of rows of H elements, whether they move in packs or not.
-size_t part_bytes(int64_t ntok, int H, int elem) {
+// The pieces of the chunks of rows of H elements, whether they move in packs or not, then the chunks' cut.
+size_t part_chunks(int64_t ntok, int H, int elem) {
   const int V = 16 / elem;
   const SumShape a = sum_shape(ntok, (H + V - 1) / V), b = sum_shape(ntok, H);
-  const size_t n = (size_t)(a.chunks > b.chunks ? a.chunks : b.chunks);
-  return n * 2 * H * (elem == 8 ? 8 : 4);
+  return (size_t)(a.chunks > b.chunks ? a.chunks : b.chunks);
+}
+size_t part_bytes(int64_t ntok, int H, int elem) {
+  return part_chunks(ntok, H, elem) * ((size_t)2 * H * (elem == 8 ? 8 : 4) + sizeof(int));
 }
 
 int embed_check(int64_t ntok, int nvocab, const char *who) {
@@ -388,10 +544,13 @@ int embed_fwd(const T *W, const int32_t *ids, int64_t ntok, int nvocab, int H, d
   constexpr int V = 16 / (int)sizeof(T);
   const bool whole = pack_width<T>(H, W, add, y) >= V;
   const int np = whole ? H / V : H;
-  const int64_t blocks = (ntok * np + 127) / 128;
-  if (blocks > 0x7fffffffLL) return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, H);
-  auto k = whole ? embed_fwd_kernel<T, V> : embed_fwd_kernel<T, 1>;
-  k<<<(unsigned)blocks, 128, 0, (cudaStream_t)stream>>>(W, ids, ntok, nvocab, H, np, (acc_t<T>)scale, add, y);
+  const bool flat = np < 32;
+  const int64_t bx = flat ? (ntok * np + kFwdThreads - 1) / kFwdThreads : (ntok + kFwdThreads / 32 - 1) / (kFwdThreads / 32);
+  const int by = flat ? 1 : (np + 32 * kFwdPart - 1) / (32 * kFwdPart);
+  if (bx > 0x7fffffffLL || by > 65535) return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, H);
+  auto k = flat ? (whole ? embed_fwd_kernel<T, V, true> : embed_fwd_kernel<T, 1, true>)
+                : (whole ? embed_fwd_kernel<T, V, false> : embed_fwd_kernel<T, 1, false>);
+  k<<<dim3((unsigned)bx, (unsigned)by), kFwdThreads, 0, (cudaStream_t)stream>>>(W, ids, ntok, nvocab, H, np, (acc_t<T>)scale, add, y);
   return launch_status(who);
 }
 
@@ -408,21 +567,26 @@ int embed_grad(const T *dy, const int32_t *ids, const int64_t *start, const int3
   const bool whole = pack_width<T>(H, dy) >= V;
   const int np = whole ? H / V : H;
   const SumShape s = sum_shape(ntok, np);
-  if (s.chunks > 1) {
+  if (s.chunks > 0) {
     if (!work) return set_error(DP_ERR_NULL, "%s: work is NULL", who);
     if (work_bytes < part_bytes(ntok, H, sizeof(T)) || ((uintptr_t)work & 15))
       return set_error(DP_ERR_SHAPE, "%s: work buffer of %zu bytes is too short or misaligned", who, work_bytes);
   }
-  const int64_t blocks = (int64_t)s.chunks * s.strips + (accumulate ? 0 : nvocab);
+  const int64_t blocks = s.blocks + (accumulate ? 0 : (nvocab + kClearRows - 1) / kClearRows);
   if (blocks == 0) return DP_OK;
   if (blocks > 0x7fffffffLL) return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, H);
   const cudaStream_t st = (cudaStream_t)stream;
+  A *part = (A *)work;
+  int *cut = s.chunks ? (int *)(part + part_chunks(ntok, H, sizeof(T)) * 2 * H) : nullptr;
   auto k = whole ? embed_grad_kernel<T, V> : embed_grad_kernel<T, 1>;
-  k<<<(unsigned)blocks, kSumThreads, 0, st>>>(dy, ids, start, src, ntok, nvocab, H, np, s.R, s.chunks, s.strips, (A)scale,
-                                              accumulate != 0, dW, (A *)work);
-  if (s.chunks > 1)
-    embed_join_kernel<A><<<dim3(s.chunks - 1, (H + kSumThreads - 1) / kSumThreads), kSumThreads, 0, st>>>(
-        ids, start, src, ntok, nvocab, H, s.R, s.chunks, (A)scale, accumulate != 0, dW, (const A *)work);
+  k<<<(unsigned)blocks, s.groups * s.width, 0, st>>>(dy, ids, start, src, ntok, nvocab, H, s, (A)scale, accumulate != 0, dW, part, cut);
+  if (s.chunks > 1) {
+    constexpr int VA = 16 / (int)sizeof(A);
+    const bool packs = pack_width<A>(H, dW) >= VA;
+    const dim3 grid((s.chunks + kJoinSlots - 1) / kJoinSlots, (H + 32 * (packs ? VA : 1) - 1) / (32 * (packs ? VA : 1)));
+    auto join = packs ? embed_join_kernel<A, VA> : embed_join_kernel<A, 1>;
+    join<<<grid, kJoinSlots * kJoinParts * 32, 0, st>>>(start, ntok, nvocab, H, s.R, s.chunks, (A)scale, accumulate != 0, dW, part, cut);
+  }
   return launch_status(who);
 }
 
@@ -458,6 +622,25 @@ int dp_embed_plan(const int32_t *ids, int64_t ntok, int nvocab, int64_t *start, 
   if (!work) return set_error(DP_ERR_NULL, "%s: work is NULL", who);
   if (work_bytes < dp_embed_plan_work_bytes(ntok, nvocab) || ((uintptr_t)work & 15))
     return set_error(DP_ERR_SHAPE, "%s: work buffer of %zu bytes is too short or misaligned", who, work_bytes);
+  if (ntok <= (int64_t)kClusterBlocks * 8 * kSortThreads) {
+    const int per = ntok <= (int64_t)kClusterBlocks * 4 * kSortThreads ? 4 : 8;
+    cudaLaunchAttribute cluster{};
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = (unsigned)((ntok + per * kSortThreads - 1) / (per * kSortThreads));
+    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(cluster.val.clusterDim.x);
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.stream = st;
+    cfg.attrs = &cluster;
+    cfg.numAttrs = 1;
+    auto k = per == 4 ? embed_plan_cluster_kernel<4> : embed_plan_cluster_kernel<8>;
+    uint32_t *keys = (uint32_t *)work;
+    cudaLaunchKernelEx(&cfg, k, ids, (int)ntok, nvocab, s.passes, s.bits, keys, (int *)work + 2 * ntok, start, src);
+    if (s.passes > 1 && nvocab > kClusterStart)
+      embed_start_kernel<<<(nvocab + 256) / 256, 256, 0, st>>>(keys + (int64_t)((s.passes - 1) & 1) * ntok, (int)ntok, nvocab, start);
+    return launch_status(who);
+  }
   uint32_t *keys[2] = {(uint32_t *)work, (uint32_t *)work + ntok};
   int *idx[2] = {(int *)work + 2 * ntok, (int *)work + 3 * ntok}, *counts = (int *)work + 4 * ntok;
   int *totals = counts + (int64_t)s.blocks * kDigits;

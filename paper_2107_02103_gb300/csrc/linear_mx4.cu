@@ -49,13 +49,39 @@ __device__ __forceinline__ uint32_t to_codes(const float (&v)[8]) {
   return r;
 }
 
+// The bits of the largest |x| of a block of 32 as an f32, in all of the lanes that hold it; NaN above all.  Without the sign
+// the bits of floating-point numbers are ordered as they are.
+template <typename T, int V>
+__device__ __forceinline__ uint32_t block_amax(const Pack<T, V> &q) {
+  constexpr int kLanes = kBlock / V;
+  if constexpr (sizeof(T) == 2) {
+    uint32_t w[4], m;
+    memcpy(w, &q, 16);
+    m = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+    m = max(m >> 16, m & 0xffffu);
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) return m << 16;
+    else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));
+  } else {
+    uint32_t m = 0;
+#pragma unroll
+    for (int l = 0; l < V; ++l) m = max(m, __float_as_uint((float)q.v[l]) & 0x7fffffffu);
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    return m;
+  }
+}
+
 constexpr int kQuantPacks = 4;  // packs a lane has on their way
 constexpr int kQuantWarps = 4;
 
 // A warp takes `part` packs of 16 bytes of a token's row (at most kQuantPacks a lane), 32 elements in neighbouring lanes;
-// `slices` warps side by side a token, kQuantWarps and more of them in a block.  With pos the row goes to the topk sorted rows pos[t][.], and the rows past the kept ones (src < 0) are cleared.
-// Whole: rows of whole aligned packs.
-template <typename T, bool Whole>
+// `slices` warps side by side a token, kQuantWarps and more of them in a block.  With pos the row goes to the topk sorted
+// rows pos[t][.], and the rows past the kept ones (src < 0) are cleared.  Rows: kExact, whole aligned packs and whole
+// blocks of 64 elements; kWhole, whole aligned packs; kAny.
+enum QuantRows { kExact, kWhole, kAny };
+template <typename T, QuantRows kRows>
 __global__ void __launch_bounds__(256)
     quant_rows_mx4_kernel(const T *__restrict__ x, const int32_t *__restrict__ src, const int32_t *__restrict__ pos,
                           int64_t ntok, int topk, int K, int part, int tokens, uint8_t *__restrict__ xq,
@@ -66,7 +92,7 @@ __global__ void __launch_bounds__(256)
   const int slot = tokens > 1 ? warp % tokens : 0, slice = tokens > 1 ? warp / tokens : (int)(blockIdx.y * (blockDim.x >> 5)) + warp;
   const int64_t t = (int64_t)blockIdx.x * tokens + slot, n = ntok * topk;
   if (t >= ntok) return;
-  const int first = slice * part, end = min(first + part, ldq / V);
+  const int first = slice * part, count = min(part, ldq / V - first) - lane;  // of this lane on, 32 apart
   // where the first two pairs go, read beside the row
   int place[2] = {-1, -1}, kept[2] = {0, 0};
   if (pos)
@@ -76,56 +102,63 @@ __global__ void __launch_bounds__(256)
         place[j] = __ldg(pos + t * topk + j);
         kept[j] = __ldg(src + t * topk + j);
       }
-  const T *row = x + t * K;
+  const int c0 = (first + lane) * V;
+  const T *row = x + t * K + c0;
   Pack<T, V> in[kQuantPacks];
 #pragma unroll
   for (int i = 0; i < kQuantPacks; ++i) {
-    const int c = (first + i * 32 + lane) * V;
-    in[i] = Pack<T, V>{};
-    if (first + i * 32 + lane < end && c < K) {
-      if constexpr (Whole) in[i] = load_pack<T, V>(row + c);
-      else in[i] = load_any<T>(row + c, x, x + ntok * K);
+    if constexpr (kRows == kExact) {
+      if (i * 32 < count) in[i] = load_pack<T, V>(row + i * 32 * V);
+    } else {
+      in[i] = Pack<T, V>{};
+      if (i * 32 < count && c0 + i * 32 * V < K) {
+        if constexpr (kRows == kWhole) in[i] = load_pack<T, V>(row + i * 32 * V);
+        else in[i] = load_any<T>(row + i * 32 * V, x, x + ntok * K);
+      }
+      if constexpr (kRows == kAny) {
+        const T zero = from_acc<T>(acc_t<T>(0));
+#pragma unroll
+        for (int l = 0; l < V; ++l)
+          if (c0 + i * 32 * V + l >= K) in[i].v[l] = zero;
+      }
     }
   }
   Code codes[kQuantPacks];
-  uint8_t scales[kQuantPacks];
+  uint32_t scales[kQuantPacks];
 #pragma unroll
   for (int i = 0; i < kQuantPacks; ++i) {
-    const int c = (first + i * 32 + lane) * V;
+    // 2^-e from the exponent's bits, which are at least two (e >= -127)
+    const uint32_t amax = block_amax<T, V>(in[i]), top = max(amax & 0x7f800000u, 2u << 23);
+    const float r = __uint_as_float(0x80000000u - top);
     float v[V];
 #pragma unroll
-    for (int l = 0; l < V; ++l) v[l] = Whole || c + l < K ? (float)to_acc(in[i].v[l]) : 0.0f;
-    float amax = fabsf(v[0]);
-#pragma unroll
-    for (int l = 1; l < V; ++l) amax = max_nan(amax, fabsf(v[l]));
-#pragma unroll
-    for (int o = 1; o < kLanes; o <<= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    const uint32_t exponent = __float_as_uint(amax) >> 23;  // 255: an infinity or NaN in the block
-    const uint32_t scale = exponent == 255 ? 255u : exponent < 2 ? 0u : exponent - 2;
-    const float r = scale == 255 ? 0.0f : __uint_as_float((254u - scale) << 23);  // 2^-e
-#pragma unroll
-    for (int l = 0; l < V; ++l) v[l] *= r;  // exact, but where it is far below the least code
-    codes[i] = scale == 255 ? Code(0) : to_codes(v);
-    scales[i] = (uint8_t)scale;
+    for (int l = 0; l < V; ++l) v[l] = (float)to_acc(in[i].v[l]) * r;  // exact, but where it is far below the least code
+    codes[i] = to_codes(v);
+    scales[i] = (top >> 23) - 2;
+    if (amax >= 0x7f800000u) {  // an infinity or NaN in the block
+      codes[i] = 0;
+      scales[i] = 255;
+    }
   }
+  const bool leads = lane % kLanes == 0;
   const int pad = slice == 0 && lane < lds - ldq / kBlock ? ldq / kBlock + lane : -1;  // scales past the last block
   for (int j = 0; j < topk; ++j) {
     const int64_t q = t * topk + j, p = !pos ? t : j == 0 ? place[0] : j == 1 ? place[1] : __ldg(pos + q);
     if (p >= 0 && p < n) {
       Code *to = reinterpret_cast<Code *>(xq + p * (ldq / 2)) + first + lane;
-      uint8_t *ts = sx + p * lds;
+      uint8_t *ts = sx + p * lds + (first + lane) / kLanes;
 #pragma unroll
       for (int i = 0; i < kQuantPacks; ++i)
-        if (first + i * 32 + lane < end) {
+        if (i * 32 < count) {
           to[i * 32] = codes[i];
-          if (lane % kLanes == 0) ts[(first + i * 32 + lane) / kLanes] = scales[i];
+          if (leads) ts[i * (32 / kLanes)] = (uint8_t)scales[i];
         }
-      if (pad >= 0) ts[pad] = 0;
+      if (pad >= 0) sx[p * lds + pad] = 0;
     }
     if (pos && (j == 0 ? kept[0] : j == 1 ? kept[1] : __ldg(src + q)) < 0) {
-      for (int c = first + lane; c < end; c += 32) {
-        reinterpret_cast<Code *>(xq + q * (ldq / 2))[c] = 0;
-        if (lane % kLanes == 0) sx[q * lds + c / kLanes] = 0;
+      for (int i = 0; i < count; i += 32) {
+        (reinterpret_cast<Code *>(xq + q * (ldq / 2)) + first + lane)[i] = 0;
+        if (leads) (sx + q * lds + (first + lane) / kLanes)[i / kLanes] = 0;
       }
       if (pad >= 0) sx[q * lds + pad] = 0;
     }
@@ -597,7 +630,7 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
   const int packs = code_cols(K) / V, slices = (packs + 32 * kQuantPacks - 1) / (32 * kQuantPacks);
   const int part = ((packs + slices - 1) / slices + kLanes - 1) / kLanes * kLanes;  // whole blocks of 32 elements
   const bool whole = (((uintptr_t)x | (uintptr_t)(K * sizeof(T))) & 15) == 0;
-  auto k = whole ? quant_rows_mx4_kernel<T, true> : quant_rows_mx4_kernel<T, false>;
+  auto k = !whole ? quant_rows_mx4_kernel<T, kAny> : K % 64 ? quant_rows_mx4_kernel<T, kWhole> : quant_rows_mx4_kernel<T, kExact>;
   const int tokens = slices < kQuantWarps ? kQuantWarps / slices : 1, warps = slices * tokens < 8 ? slices * tokens : 8;
   const dim3 grid((unsigned)((ntok + tokens - 1) / tokens), (unsigned)((slices + 7) / 8));
   k<<<grid, warps * 32, 0, (cudaStream_t)stream>>>(x, src, pos, ntok, topk, K, part, tokens, xq, sx);

@@ -853,41 +853,55 @@ __global__ void __launch_bounds__(64) topk_grad_sparse_kernel(const __grid_const
   if (t0 >= p.ntok) return;
   const int have = (int)min((int64_t)tokens, p.ntok - t0), n = have * p.E;
   A *tile = (A *)tiles + (size_t)warp * ((tokens * p.E + 15) / 16 * 16);
-  for (int c = lane; c < n; c += 32) tile[c] = A(0);
+  constexpr int kVA = 16 / (int)sizeof(A);
+  for (int c = lane * kVA; c < n; c += 32 * kVA) store_pack<A, kVA>(tile + c, Pack<A, kVA>{});  // in whole packs
   __syncwarp();
   if (lane < have) {
+    constexpr int kAtOnce = 8;  // pairs whose logits are on their way
     const T *x = (const T *)p.x + t * p.E;
-    const int32_t *e = p.expert + t * p.k;
-    const A *dw = (const A *)p.dw + t * p.k;
-    A *to = tile + lane * p.E;
-    auto logit = [&](int j) {  // -inf: no pair
-      const int ej = __ldg(e + j);
-      return (unsigned)ej < (unsigned)p.E ? to_acc(x[ej]) : none<A>();
-    };
     const A scale = (A)p.scale;
+    A *to = tile + lane * p.E;
+    int e[kAtOnce];
+    A v[kAtOnce], d[kAtOnce];
+    auto read = [&](int j0) {  // -inf: no pair
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        e[i] = j0 + i < p.k ? __ldg(p.expert + t * p.k + j0 + i) : -1;
+        d[i] = j0 + i < p.k ? scale * __ldg((const A *)p.dw + t * p.k + j0 + i) : A(0);
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) v[i] = (unsigned)e[i] < (unsigned)p.E ? to_acc(x[e[i]]) : none<A>();
+    };
+    read(0);
     A sum = A(1), mean = A(0), top = none<A>();
     if (p.renorm) {
-      for (int j = 0; j < p.k; ++j) {
-        const A v = logit(j);
-        top = v != v || v > top ? v : top;
+      for (int j0 = 0; j0 < p.k; j0 += kAtOnce) {
+        if (j0) read(j0);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) top = v[i] != v[i] || v[i] > top ? v[i] : top;
       }
       sum = A(0);
-      for (int j = 0; j < p.k; ++j) {
-        const A v = logit(j);
-        if (v == none<A>()) continue;
-        const A r = relative_score(v, top, p.sigmoid);
-        sum += r;
-        mean += r * (scale * __ldg(dw + j));
+      for (int j0 = 0; j0 < p.k; j0 += kAtOnce) {
+        if (p.k > kAtOnce) read(j0);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          if (v[i] != none<A>()) {
+            const A r = relative_score(v[i], top, p.sigmoid);
+            sum += r;
+            mean += r * d[i];
+          }
       }
       mean /= sum;
     }
-    for (int j = 0; j < p.k; ++j) {
-      const A v = logit(j);
-      if (v == none<A>()) continue;
-      const A r = p.renorm ? relative_score(v, top, p.sigmoid) / sum : sigmoid(v);
-      A g = r * (scale * __ldg(dw + j) - mean);
-      if (p.sigmoid) g *= sigmoid(-v);
-      to[__ldg(e + j)] += g;
+    for (int j0 = 0; j0 < p.k; j0 += kAtOnce) {
+      if (p.k > kAtOnce) read(j0);
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        if (v[i] != none<A>()) {
+          A g = (p.renorm ? relative_score(v[i], top, p.sigmoid) / sum : sigmoid(v[i])) * (d[i] - mean);
+          if (p.sigmoid) g *= sigmoid(-v[i]);
+          to[e[i]] += g;
+        }
     }
   }
   __syncwarp();
