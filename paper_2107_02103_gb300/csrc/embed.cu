@@ -180,8 +180,9 @@ __global__ void __launch_bounds__(kSortThreads)
     cg::this_cluster().sync();
     int total = 0, before = 0;
     if (d < kDigits)
-      for (int b = 0; b < (int)gridDim.x; ++b) {
-        const int c = cg::this_cluster().map_shared_rank(block, b)[d];
+#pragma unroll
+      for (int b = 0; b < kClusterBlocks; ++b) {
+        const int c = b < (int)gridDim.x ? cg::this_cluster().map_shared_rank(block, b)[d] : 0;
         before += b < (int)blockIdx.x ? c : 0;
         total += c;
       }
@@ -368,9 +369,12 @@ __global__ void __launch_bounds__(kFwdThreads)
 // Further blocks clear the rows of ids that no token has.  The chunk's tokens and ids are read first, so that the rows'
 // addresses wait for shared memory alone.
 constexpr int kSumThreads = 256, kMaxRows = 256, kMaxGroups = 8, kClearRows = 32;
-// Rows of a thread on their way.
+// Rows of a thread on their way, and its accesses of a row: a row's bookkeeping costs more than one element's sum.
 template <int V>
-constexpr int kSumAhead = V > 1 ? 8 : 16;
+constexpr int kSumAhead = V > 1 ? 8 : 4;
+template <int V>
+constexpr int kSumCols = V > 1 ? 1 : 4;
+constexpr int kMostAhead = 8;
 struct SumShape {
   int R, chunks, strips, width, groups;
   int64_t blocks;  // that sum
@@ -382,8 +386,8 @@ __global__ void __launch_bounds__(kSumThreads)
                       acc_t<T> scale, bool accumulate, acc_t<T> *__restrict__ dW, acc_t<T> *__restrict__ part,
                       int *__restrict__ cut) {
   using A = acc_t<T>;
-  constexpr int kAhead = kSumAhead<V>;
-  if ((int64_t)blockIdx.x >= s.blocks) {
+  constexpr int kAhead = kSumAhead<V>, kCols = kSumCols<V>;
+  if ((int64_t)blockIdx.x >= s.blocks) {  // (in turn with the others instead: 48 -> 56 us for 24,571 x 1003 f16 to 30,011 rows)
     const int64_t v0 = ((int64_t)blockIdx.x - s.blocks) * kClearRows;
     const int lane = threadIdx.x & 31;
     const int64_t at = v0 + lane < nvocab ? __ldg(start + v0 + lane) : 0, end = v0 + lane < nvocab ? __ldg(start + v0 + lane + 1) : 1;
@@ -399,12 +403,12 @@ __global__ void __launch_bounds__(kSumThreads)
       }
     return;
   }
-  __shared__ int froms[kMaxGroups * (kMaxRows + kSumAhead<1>)], idsm[kMaxGroups * (kMaxRows + 2)];
+  __shared__ int froms[kMaxGroups * (kMaxRows + kMostAhead)], idsm[kMaxGroups * (kMaxRows + 2)];
   const int group = threadIdx.x / s.width, tid = threadIdx.x - group * s.width;
   const int64_t unit = (int64_t)blockIdx.x * s.groups + group, chunk = unit / s.strips;
   const int strip = (int)(unit - chunk * s.strips);
   // a row's token (-1: none), and its id, of one row before, and one behind
-  int *from = froms + group * (s.R + kSumAhead<1>), *id = idsm + group * (s.R + 2);
+  int *from = froms + group * (s.R + kMostAhead), *id = idsm + group * (s.R + 2);
   const int64_t kept = min(max(__ldg(start + nvocab), (int64_t)0), ntok), r0 = chunk * s.R;
   const int rows = chunk < s.chunks ? (int)min((int64_t)s.R, max(kept - r0, (int64_t)0)) : 0;
   for (int r = tid - 1; r < rows + kAhead; r += s.width) {
@@ -420,27 +424,37 @@ __global__ void __launch_bounds__(kSumThreads)
     if (strip == 0 && tid == 0) cut[chunk] = -1;
     return;
   }
-  const int c = (strip * s.width + tid) * V;
+  const int c = (strip * s.width * kCols + tid) * V, step = s.width * V;  // its accesses are `step` apart
   if (c >= H) return;
   const int before = id[0], after = id[rows + 1];
-  A sum[V] = {};
+  A sum[kCols][V] = {};
   int run = id[1], first = 0;  // the run at hand and its first row
   auto put = [&](int end) {    // its rows end before `end`
     if ((uint32_t)run < (uint32_t)nvocab) {
       const bool is_cut = (first == 0 && before == run) || (end == rows && after == run);
       A *to = is_cut ? part + (chunk * 2 + (first ? 1 : 0)) * H + c : dW + (int64_t)run * H + c;
 #pragma unroll
-      for (int l = 0; l < V; ++l) to[l] = is_cut ? sum[l] : accumulate ? fma(scale, sum[l], to[l]) : scale * sum[l];
+      for (int u = 0; u < kCols; ++u, to += step)
+        if (kCols == 1 || c + u * step < H)
+#pragma unroll
+          for (int l = 0; l < V; ++l) to[l] = is_cut ? sum[u][l] : accumulate ? fma(scale, sum[u][l], to[l]) : scale * sum[u][l];
     }
 #pragma unroll
-    for (int l = 0; l < V; ++l) sum[l] = A(0);
+    for (int u = 0; u < kCols; ++u)
+#pragma unroll
+      for (int l = 0; l < V; ++l) sum[u][l] = A(0);
   };
   for (int r = 0; r < rows; r += kAhead) {
-    Pack<T, V> v[kAhead];
+    Pack<T, V> v[kAhead][kCols];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const int q = from[r + i];
-      v[i] = q >= 0 ? load_pack<T, V>(dy + (int64_t)q * H + c) : Pack<T, V>{};
+      const T *row = dy + (int64_t)q * H + c;
+#pragma unroll
+      for (int u = 0; u < kCols; ++u) {
+        v[i][u] = Pack<T, V>{};
+        if (q >= 0 && (kCols == 1 || c + u * step < H)) v[i][u] = load_pack<T, V>(row + u * step);
+      }
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
@@ -452,7 +466,9 @@ __global__ void __launch_bounds__(kSumThreads)
           first = r + i;
         }
 #pragma unroll
-        for (int l = 0; l < V; ++l) sum[l] += to_acc(v[i].v[l]);
+        for (int u = 0; u < kCols; ++u)
+#pragma unroll
+          for (int l = 0; l < V; ++l) sum[u][l] += to_acc(v[i][u].v[l]);
       }
   }
   if (c == 0) cut[chunk] = (uint32_t)run < (uint32_t)nvocab && after == run && !(first == 0 && before == run) ? run : -1;
@@ -475,12 +491,18 @@ __global__ void __launch_bounds__(kJoinSlots *kJoinParts * 32)
   if (v >= 0 && v < nvocab && c < H) {
     const int64_t s0 = __ldg(start + v), s1 = min(__ldg(start + v + 1), ntok);
     const int n = (int)min((s1 - 1) / R, (int64_t)chunks - 1) - chunk + 1, each = (n + kJoinParts - 1) / kJoinParts;  // pieces
-    const int end = min(n, (which + 1) * each);
-#pragma unroll 8
-    for (int k = which * each; k < end; ++k) {
-      const Pack<A, V> p = load_pack<A, V>(part + ((int64_t)(chunk + k) * 2 + (k == 0 && s0 % R ? 1 : 0)) * H + c);
+    const int first = which * each, end = min(n, first + each);
+    const A *from = part + (int64_t)(chunk + first) * 2 * H + c;
+    for (int k = first; k < end; k += 8, from += (int64_t)16 * H) {  // eight pieces on their way
+      Pack<A, V> p[8];
 #pragma unroll
-      for (int l = 0; l < V; ++l) sum.v[l] += p.v[l];
+      for (int i = 0; i < 8; ++i)
+        if (k + i < end) p[i] = load_pack<A, V>(from + (int64_t)2 * i * H + (k + i == 0 && s0 != (int64_t)chunk * R ? H : 0));
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (k + i < end)
+#pragma unroll
+          for (int l = 0; l < V; ++l) sum.v[l] += p[i].v[l];
     }
   }
   sums[slot][which][lane] = sum;
@@ -496,10 +518,11 @@ __global__ void __launch_bounds__(kJoinSlots *kJoinParts * 32)
 }
 
 // Strips of at most kSumThreads packs, whole warps a group, as many groups a block as fit, chunks of 16 to 256 rows.
-SumShape sum_shape(int64_t ntok, int np) {
+SumShape sum_shape(int64_t ntok, int np, bool packs) {
   SumShape s;
-  s.strips = (np + kSumThreads - 1) / kSumThreads;
-  s.width = ((np + s.strips - 1) / s.strips + 31) / 32 * 32;
+  const int cols = packs ? 1 : kSumCols<1>, threads = (np + cols - 1) / cols;  // of a row
+  s.strips = (threads + kSumThreads - 1) / kSumThreads;
+  s.width = ((threads + s.strips - 1) / s.strips + 31) / 32 * 32;
   s.groups = kSumThreads / s.width;
   int64_t want = (int64_t)152 * 4 * s.groups / s.strips;  // chunks of four blocks an SM, all resident
   if (want < 1) want = 1;
@@ -512,7 +535,7 @@ SumShape sum_shape(int64_t ntok, int np) {
 // The pieces of the chunks of rows of H elements, whether they move in packs or not, then the chunks' cut.
 size_t part_chunks(int64_t ntok, int H, int elem) {
   const int V = 16 / elem;
-  const SumShape a = sum_shape(ntok, (H + V - 1) / V), b = sum_shape(ntok, H);
+  const SumShape a = sum_shape(ntok, (H + V - 1) / V, true), b = sum_shape(ntok, H, false);
   return (size_t)(a.chunks > b.chunks ? a.chunks : b.chunks);
 }
 size_t part_bytes(int64_t ntok, int H, int elem) {
@@ -566,7 +589,7 @@ int embed_grad(const T *dy, const int32_t *ids, const int64_t *start, const int3
   constexpr int V = 16 / (int)sizeof(T);
   const bool whole = pack_width<T>(H, dy) >= V;
   const int np = whole ? H / V : H;
-  const SumShape s = sum_shape(ntok, np);
+  const SumShape s = sum_shape(ntok, np, whole);
   if (s.chunks > 0) {
     if (!work) return set_error(DP_ERR_NULL, "%s: work is NULL", who);
     if (work_bytes < part_bytes(ntok, H, sizeof(T)) || ((uintptr_t)work & 15))

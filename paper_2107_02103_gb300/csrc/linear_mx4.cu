@@ -18,24 +18,7 @@ __host__ __device__ constexpr int code_cols(int K) { return (K + 63) / 64 * 64; 
 __host__ __device__ constexpr int scale_cols(int K) { return (K + 255) / 256 * 8; }      // scales of a row
 
 // ------------------------------------------------------------------ rows to 4 bits
-// The codes of two, four or eight values, the first in the lowest bits.
-__device__ __forceinline__ uint8_t to_codes(const float (&v)[2]) {
-  uint32_t r;
-  asm("{\n .reg .b8 a;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n mov.b32 %0, {a, a, a, a};\n}"
-      : "=r"(r)
-      : "f"(v[0]), "f"(v[1]));
-  return (uint8_t)r;
-}
-__device__ __forceinline__ uint16_t to_codes(const float (&v)[4]) {
-  uint32_t r;
-  asm("{\n .reg .b8 a, b;\n"
-      " cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n"
-      " cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
-      " mov.b32 %0, {a, b, a, b};\n}"
-      : "=r"(r)
-      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]));
-  return (uint16_t)r;
-}
+// The codes of eight values, the first in the lowest bits.
 __device__ __forceinline__ uint32_t to_codes(const float (&v)[8]) {
   uint32_t r;
   asm("{\n .reg .b8 a, b, c, d;\n"
@@ -49,50 +32,51 @@ __device__ __forceinline__ uint32_t to_codes(const float (&v)[8]) {
   return r;
 }
 
-// The bits of the largest |x| of a block of 32 as an f32, in all of the lanes that hold it; NaN above all.  Without the sign
-// the bits of floating-point numbers are ordered as they are.
-template <typename T, int V>
-__device__ __forceinline__ uint32_t block_amax(const Pack<T, V> &q) {
-  constexpr int kLanes = kBlock / V;
-  if constexpr (sizeof(T) == 2) {
-    uint32_t w[4], m;
-    memcpy(w, &q, 16);
-    m = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+// Eight neighbouring elements of a row, as many as a lane takes at a time; four lanes have a scale.
+template <typename T>
+struct Eight {
+  static constexpr int V = 16 / (int)sizeof(T), kN = 8 / V;
+  Pack<T, V> p[kN];
+  __device__ __forceinline__ float at(int l) const { return (float)to_acc(p[l / V].v[l % V]); }
+  // The bits of their largest |x| as an f32, NaN above all: without the sign the bits are ordered as the numbers are.
+  __device__ __forceinline__ uint32_t amax() const {
+    if constexpr (sizeof(T) == 2) {
+      uint32_t w[4], m;
+      memcpy(w, p, 16);
+      m = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+      m = max(m >> 16, m & 0xffffu);
+      if constexpr (std::is_same<T, __nv_bfloat16>::value) return m << 16;
+      else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));
+    } else {
+      uint32_t m = 0;
 #pragma unroll
-    for (int o = 1; o < kLanes; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
-    m = max(m >> 16, m & 0xffffu);
-    if constexpr (std::is_same<T, __nv_bfloat16>::value) return m << 16;
-    else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));
-  } else {
-    uint32_t m = 0;
-#pragma unroll
-    for (int l = 0; l < V; ++l) m = max(m, __float_as_uint((float)q.v[l]) & 0x7fffffffu);
-#pragma unroll
-    for (int o = 1; o < kLanes; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-    return m;
+      for (int l = 0; l < 8; ++l) m = max(m, __float_as_uint(at(l)) & 0x7fffffffu);
+      return m;
+    }
   }
-}
+};
 
-constexpr int kQuantPacks = 4;  // packs a lane has on their way
 constexpr int kQuantWarps = 4;
+template <typename T>
+constexpr int kQuantEights = 8 / (int)sizeof(T);  // a lane has 64 bytes on their way
 
-// A warp takes `part` packs of 16 bytes of a token's row (at most kQuantPacks a lane), 32 elements in neighbouring lanes;
-// `slices` warps side by side a token, kQuantWarps and more of them in a block.  With pos the row goes to the topk sorted
-// rows pos[t][.], and the rows past the kept ones (src < 0) are cleared.  Rows: kExact, whole aligned packs and whole
-// blocks of 64 elements; kWhole, whole aligned packs; kAny.
+// A warp takes `part` eights of a token's row; `slices` warps side by side a token, kQuantWarps and more of them in a
+// block.  With pos the row goes to the topk sorted rows pos[t][.], and the rows past the kept ones (src < 0) are cleared.
+// Rows: kExact, whole aligned packs and whole blocks of 64 elements; kWhole, whole aligned packs; kAny.
+// Bound by memory; what it takes in instructions comes second: four elements a lane at a time, with three exchanges of the
+// largest instead of two and codes in two bytes, took 98 us for 65,536 x 1600 f32.
 enum QuantRows { kExact, kWhole, kAny };
 template <typename T, QuantRows kRows>
 __global__ void __launch_bounds__(256)
     quant_rows_mx4_kernel(const T *__restrict__ x, const int32_t *__restrict__ src, const int32_t *__restrict__ pos,
                           int64_t ntok, int topk, int K, int part, int tokens, uint8_t *__restrict__ xq,
                           uint8_t *__restrict__ sx) {
-  constexpr int V = 16 / (int)sizeof(T), kLanes = kBlock / V;  // lanes of a scale
-  using Code = decltype(to_codes(std::declval<const float (&)[V]>()));
+  constexpr int V = 16 / (int)sizeof(T), kE = kQuantEights<T>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ldq = code_cols(K), lds = scale_cols(K);
   const int slot = tokens > 1 ? warp % tokens : 0, slice = tokens > 1 ? warp / tokens : (int)(blockIdx.y * (blockDim.x >> 5)) + warp;
   const int64_t t = (int64_t)blockIdx.x * tokens + slot, n = ntok * topk;
   if (t >= ntok) return;
-  const int first = slice * part, count = min(part, ldq / V - first) - lane;  // of this lane on, 32 apart
+  const int first = slice * part, total = min(part, ldq / 8 - first), count = total - lane;  // of this lane on, 32 apart
   // where the first two pairs go, read beside the row
   int place[2] = {-1, -1}, kept[2] = {0, 0};
   if (pos)
@@ -102,37 +86,44 @@ __global__ void __launch_bounds__(256)
         place[j] = __ldg(pos + t * topk + j);
         kept[j] = __ldg(src + t * topk + j);
       }
-  const int c0 = (first + lane) * V;
+  const int c0 = (first + lane) * 8;
   const T *row = x + t * K + c0;
-  Pack<T, V> in[kQuantPacks];
+  Eight<T> in[kE];
 #pragma unroll
-  for (int i = 0; i < kQuantPacks; ++i) {
-    if constexpr (kRows == kExact) {
-      if (i * 32 < count) in[i] = load_pack<T, V>(row + i * 32 * V);
-    } else {
-      in[i] = Pack<T, V>{};
-      if (i * 32 < count && c0 + i * 32 * V < K) {
-        if constexpr (kRows == kWhole) in[i] = load_pack<T, V>(row + i * 32 * V);
-        else in[i] = load_any<T>(row + i * 32 * V, x, x + ntok * K);
-      }
-      if constexpr (kRows == kAny) {
-        const T zero = from_acc<T>(acc_t<T>(0));
+  for (int i = 0; i < kE; ++i)
 #pragma unroll
-        for (int l = 0; l < V; ++l)
-          if (c0 + i * 32 * V + l >= K) in[i].v[l] = zero;
+    for (int h = 0; h < Eight<T>::kN; ++h) {
+      const int d = i * 256 + h * V;
+      Pack<T, V> &q = in[i].p[h];
+      if constexpr (kRows == kExact) {
+        if (i * 32 < count) q = load_pack<T, V>(row + d);
+      } else {
+        q = Pack<T, V>{};
+        if (i * 32 < count && c0 + d < K) {
+          if constexpr (kRows == kWhole) q = load_pack<T, V>(row + d);
+          else q = load_any<T>(row + d, x, x + ntok * K);
+        }
+        if constexpr (kRows == kAny) {
+          const T zero = from_acc<T>(acc_t<T>(0));
+#pragma unroll
+          for (int l = 0; l < V; ++l)
+            if (c0 + d + l >= K) q.v[l] = zero;
+        }
       }
     }
-  }
-  Code codes[kQuantPacks];
-  uint32_t scales[kQuantPacks];
+  uint32_t codes[kE], scales[kE];
 #pragma unroll
-  for (int i = 0; i < kQuantPacks; ++i) {
+  for (int i = 0; i < kE; ++i) {
+    if (i * 32 >= total) break;  // for the warp
+    uint32_t amax = in[i].amax();
+    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
     // 2^-e from the exponent's bits, which are at least two (e >= -127)
-    const uint32_t amax = block_amax<T, V>(in[i]), top = max(amax & 0x7f800000u, 2u << 23);
+    const uint32_t top = max(amax & 0x7f800000u, 2u << 23);
     const float r = __uint_as_float(0x80000000u - top);
-    float v[V];
+    float v[8];
 #pragma unroll
-    for (int l = 0; l < V; ++l) v[l] = (float)to_acc(in[i].v[l]) * r;  // exact, but where it is far below the least code
+    for (int l = 0; l < 8; ++l) v[l] = in[i].at(l) * r;  // exact, but where it is far below the least code
     codes[i] = to_codes(v);
     scales[i] = (top >> 23) - 2;
     if (amax >= 0x7f800000u) {  // an infinity or NaN in the block
@@ -140,25 +131,25 @@ __global__ void __launch_bounds__(256)
       scales[i] = 255;
     }
   }
-  const bool leads = lane % kLanes == 0;
+  const bool leads = lane % 4 == 0;
   const int pad = slice == 0 && lane < lds - ldq / kBlock ? ldq / kBlock + lane : -1;  // scales past the last block
   for (int j = 0; j < topk; ++j) {
     const int64_t q = t * topk + j, p = !pos ? t : j == 0 ? place[0] : j == 1 ? place[1] : __ldg(pos + q);
     if (p >= 0 && p < n) {
-      Code *to = reinterpret_cast<Code *>(xq + p * (ldq / 2)) + first + lane;
-      uint8_t *ts = sx + p * lds + (first + lane) / kLanes;
+      uint32_t *to = reinterpret_cast<uint32_t *>(xq + p * (ldq / 2)) + first + lane;
+      uint8_t *ts = sx + p * lds + (first + lane) / 4;
 #pragma unroll
-      for (int i = 0; i < kQuantPacks; ++i)
+      for (int i = 0; i < kE; ++i)
         if (i * 32 < count) {
           to[i * 32] = codes[i];
-          if (leads) ts[i * (32 / kLanes)] = (uint8_t)scales[i];
+          if (leads) ts[i * 8] = (uint8_t)scales[i];
         }
       if (pad >= 0) sx[p * lds + pad] = 0;
     }
     if (pos && (j == 0 ? kept[0] : j == 1 ? kept[1] : __ldg(src + q)) < 0) {
       for (int i = 0; i < count; i += 32) {
-        (reinterpret_cast<Code *>(xq + q * (ldq / 2)) + first + lane)[i] = 0;
-        if (leads) (sx + q * lds + (first + lane) / kLanes)[i / kLanes] = 0;
+        (reinterpret_cast<uint32_t *>(xq + q * (ldq / 2)) + first + lane)[i] = 0;
+        if (leads) (sx + q * lds + (first + lane) / 4)[i / 4] = 0;
       }
       if (pad >= 0) sx[q * lds + pad] = 0;
     }
@@ -626,9 +617,8 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
   if (!x || !xq || !sx) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (((uintptr_t)xq & 15) || ((uintptr_t)sx & 7)) return set_error(DP_ERR_SHAPE, "%s: xq or sx is not aligned", who);
   if (!at_elements(x) || !at_elements(src, pos)) return misaligned(who);
-  constexpr int V = 16 / (int)sizeof(T), kLanes = kBlock / V;
-  const int packs = code_cols(K) / V, slices = (packs + 32 * kQuantPacks - 1) / (32 * kQuantPacks);
-  const int part = ((packs + slices - 1) / slices + kLanes - 1) / kLanes * kLanes;  // whole blocks of 32 elements
+  const int eights = code_cols(K) / 8, most = 32 * kQuantEights<T>, slices = (eights + most - 1) / most;
+  const int part = ((eights + slices - 1) / slices + 31) / 32 * 32;  // all lanes of a warp, and whole blocks of 32 elements
   const bool whole = (((uintptr_t)x | (uintptr_t)(K * sizeof(T))) & 15) == 0;
   auto k = !whole ? quant_rows_mx4_kernel<T, kAny> : K % 64 ? quant_rows_mx4_kernel<T, kWhole> : quant_rows_mx4_kernel<T, kExact>;
   const int tokens = slices < kQuantWarps ? kQuantWarps / slices : 1, warps = slices * tokens < 8 ? slices * tokens : 8;
