@@ -24,30 +24,41 @@ __device__ __forceinline__ uint32_t sort_key(int32_t id, int nvocab) {
   return (uint32_t)id < (uint32_t)nvocab ? (uint32_t)id : (uint32_t)nvocab;
 }
 
-// A thread's kPer items of a block in order by warp, 32 apart: the warp counts them by digit.
+// A thread's kPer items of a block in order by warp, 32 apart: the warp counts them by digit, then gives each its place
+// in its digit, after the warps before it and those before it in its warp.  The lanes with the same digit are found by a
+// vote on each of its bits (a warp-wide match takes twice as long), and one of them moves the warp's counter: no atomics.
+// mine: the warp's counters of the digits, from counts to the next places.
 template <int kPer>
 struct SortItems {
   uint32_t key[kPer];
+  unsigned same[kPer];
   int64_t first;
-};
-
-// The place of every item of a block in a digit, after the warps before it and those before it in its warp.  cnt: a row
-// of kDigits counters a warp, from counts to the warp's next place.
-template <int kPer>
-__device__ __forceinline__ void count_digits(const SortItems<kPer> &it, int64_t n, int shift, int mask, int *mine) {
+  __device__ __forceinline__ void count(int64_t n, int shift, int bits, int *mine) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i)
-    if (it.first + 32 * i < n) atomicAdd(mine + (it.key[i] >> shift & mask), 1);  // integers: any order gives the same
-}
-
-__device__ __forceinline__ int take_place(uint32_t d, bool have, int lane, int *mine) {
-  const unsigned same = __match_any_sync(0xffffffffu, have ? d : 0xffffffffu);
-  const int p = have ? mine[d] + __popc(same & ((1u << lane) - 1)) : 0;
-  __syncwarp();
-  if (have && lane == __ffs(same) - 1) mine[d] += __popc(same);
-  __syncwarp();
-  return p;
-}
+    for (int i = 0; i < kPer; ++i) {
+      const uint32_t d = key[i] >> shift;
+      const bool have = first + 32 * i < n;
+      same[i] = __ballot_sync(0xffffffffu, have);
+      for (int b = 0; b < bits; ++b) {
+        const unsigned set = __ballot_sync(0xffffffffu, d >> b & 1);
+        same[i] &= d >> b & 1 ? set : ~set;
+      }
+      if (have && lane == __ffs(same[i]) - 1) mine[d & ((1u << bits) - 1)] += __popc(same[i]);
+      __syncwarp();
+    }
+  }
+  // Item i's place (of a lane that has one).
+  __device__ __forceinline__ int place(int i, bool have, int shift, int mask, int *mine) const {
+    const int lane = threadIdx.x & 31;
+    const uint32_t d = key[i] >> shift & mask;
+    const int p = have ? mine[d] + __popc(same[i] & ((1u << lane) - 1)) : 0;
+    __syncwarp();
+    if (have && lane == __ffs(same[i]) - 1) mine[d] += __popc(same[i]);
+    __syncwarp();
+    return p;
+  }
+};
 
 // An exclusive scan of 256 values by the first 256 threads of a block (all threads call).
 __device__ __forceinline__ int scan_digits(int v, int *sums) {
@@ -99,7 +110,7 @@ __global__ void __launch_bounds__(kSortThreads)
     __syncthreads();
     int *mine = cnt + warp * kDigits;
     const int shift = pass * bits;
-    count_digits(it, n, shift, mask, mine);
+    it.count(n, shift, bits, mine);
     __syncthreads();
     int total = 0;
     if (threadIdx.x < kDigits)
@@ -119,7 +130,7 @@ __global__ void __launch_bounds__(kSortThreads)
 #pragma unroll
     for (int i = 0; i < kSortPer; ++i) {
       const bool have = it.first + 32 * i < n;
-      const int p = take_place(it.key[i] >> shift & mask, have, lane, mine);
+      const int p = it.place(i, have, shift, mask, mine);
       if (have) {
         to_k[p] = it.key[i];
         to_i[p] = id[i];
@@ -169,7 +180,7 @@ __global__ void __launch_bounds__(kSortThreads)
     __syncthreads();
     int *mine = cnt + warp * kDigits;
     const int shift = pass * bits;
-    count_digits(it, n, shift, mask, mine);
+    it.count(n, shift, bits, mine);
     __syncthreads();
     if (d < kDigits) {
       int c = 0;
@@ -204,7 +215,7 @@ __global__ void __launch_bounds__(kSortThreads)
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const bool have = it.first + 32 * i < n;
-      const int p = take_place(it.key[i] >> shift & mask, have, lane, mine);
+      const int p = it.place(i, have, shift, mask, mine);
       if (have) {
         if (!last || passes > 1) to_k[p] = it.key[i];
         to_i[p] = last && it.key[i] >= (uint32_t)nvocab ? -1 : id[i];
@@ -258,10 +269,10 @@ __global__ void __launch_bounds__(kDigits) sort_scan_kernel(int *__restrict__ co
 
 __global__ void __launch_bounds__(kSortThreads)
     sort_place_kernel(const int32_t *__restrict__ ids, const uint32_t *__restrict__ keys, const int *__restrict__ idx,
-                      int64_t n, int nvocab, int shift, int mask, const int *__restrict__ counts,
+                      int64_t n, int nvocab, int shift, int bits, const int *__restrict__ counts,
                       const int *__restrict__ totals, uint32_t *__restrict__ to_key, int *__restrict__ to_idx, bool last) {
   __shared__ int cnt[kSortWarps * kDigits], sums[kSortWarps];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, mask = (1 << bits) - 1;
   for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) cnt[i] = 0;
   SortItems<kSortPer> it;
   int id[kSortPer];
@@ -274,7 +285,7 @@ __global__ void __launch_bounds__(kSortThreads)
   }
   __syncthreads();
   int *mine = cnt + warp * kDigits;
-  count_digits(it, n, shift, mask, mine);
+  it.count(n, shift, bits, mine);
   __syncthreads();
   const int d = threadIdx.x;
   int run = scan_digits(d < kDigits ? __ldg(totals + d) : 0, sums);
@@ -291,7 +302,7 @@ __global__ void __launch_bounds__(kSortThreads)
 #pragma unroll
   for (int i = 0; i < kSortPer; ++i) {
     const bool have = it.first + 32 * i < n;
-    const int p = take_place(it.key[i] >> shift & mask, have, lane, mine);
+    const int p = it.place(i, have, shift, mask, mine);
     if (have) {
       to_key[p] = it.key[i];
       to_idx[p] = last && it.key[i] >= (uint32_t)nvocab ? -1 : id[i];
@@ -478,43 +489,57 @@ __global__ void __launch_bounds__(kSumThreads)
 // The runs that chunks cut, eight chunks a block: a run's pieces are added in four parts of neighbouring ones, each in order,
 // and the parts in order.
 constexpr int kJoinSlots = 8, kJoinParts = 4;
+template <int V>
+constexpr int kJoinCols = V > 1 ? 1 : 4;
 template <typename A, int V>
 __global__ void __launch_bounds__(kJoinSlots *kJoinParts * 32)
     embed_join_kernel(const int64_t *__restrict__ start, int64_t ntok, int nvocab, int H, int R, int chunks, A scale,
                       bool accumulate, A *__restrict__ dW, const A *__restrict__ part, const int *__restrict__ cut) {
-  __shared__ Pack<A, V> sums[kJoinSlots][kJoinParts][32];
+  __shared__ Pack<A, V> sums[kJoinSlots][kJoinParts][kJoinCols<V>][32];
+  constexpr int kCols = kJoinCols<V>;  // accesses of a thread, 32 apart
   const int lane = threadIdx.x % 32, which = threadIdx.x / 32 % kJoinParts, slot = threadIdx.x / (32 * kJoinParts);
-  const int chunk = blockIdx.x * kJoinSlots + slot, c = (blockIdx.y * 32 + lane) * V;
+  const int chunk = blockIdx.x * kJoinSlots + slot, c = (blockIdx.y * 32 * kCols + lane) * V;
   const int v = chunk < chunks ? __ldg(cut + chunk) : -1;
   if (!__syncthreads_or(v >= 0)) return;
-  Pack<A, V> sum{};
-  if (v >= 0 && v < nvocab && c < H) {
+  Pack<A, V> sum[kCols] = {};
+  if (v >= 0 && v < nvocab) {
     const int64_t s0 = __ldg(start + v), s1 = min(__ldg(start + v + 1), ntok);
     const int n = (int)min((s1 - 1) / R, (int64_t)chunks - 1) - chunk + 1, each = (n + kJoinParts - 1) / kJoinParts;  // pieces
     const int first = which * each, end = min(n, first + each);
+    constexpr int kAhead = 8 / kCols;  // pieces on their way
     const A *from = part + (int64_t)(chunk + first) * 2 * H + c;
-    for (int k = first; k < end; k += 8, from += (int64_t)16 * H) {  // eight pieces on their way
-      Pack<A, V> p[8];
+    for (int k = first; k < end; k += kAhead, from += (int64_t)2 * kAhead * H) {
+      Pack<A, V> p[kAhead][kCols];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k + i < end) p[i] = load_pack<A, V>(from + (int64_t)2 * i * H + (k + i == 0 && s0 != (int64_t)chunk * R ? H : 0));
+      for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k + i < end)
+        for (int u = 0; u < kCols; ++u)
+          if (k + i < end && c + 32 * V * u < H)
+            p[i][u] = load_pack<A, V>(from + 32 * V * u + (int64_t)2 * i * H + (k + i == 0 && s0 != (int64_t)chunk * R ? H : 0));
 #pragma unroll
-          for (int l = 0; l < V; ++l) sum.v[l] += p[i].v[l];
+      for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+        for (int u = 0; u < kCols; ++u)
+          if (k + i < end && c + 32 * V * u < H)
+#pragma unroll
+            for (int l = 0; l < V; ++l) sum[u].v[l] += p[i][u].v[l];
     }
   }
-  sums[slot][which][lane] = sum;
+#pragma unroll
+  for (int u = 0; u < kCols; ++u) sums[slot][which][u][lane] = sum[u];
   __syncthreads();
-  if (which || v < 0 || v >= nvocab || c >= H) return;
+  if (which || v < 0 || v >= nvocab) return;
 #pragma unroll
-  for (int k = 1; k < kJoinParts; ++k)
+  for (int u = 0; u < kCols; ++u) {
+    if (c + 32 * V * u >= H) break;
 #pragma unroll
-    for (int l = 0; l < V; ++l) sum.v[l] += sums[slot][k][lane].v[l];
-  A *to = dW + (int64_t)v * H + c;
+    for (int k = 1; k < kJoinParts; ++k)
 #pragma unroll
-  for (int l = 0; l < V; ++l) to[l] = accumulate ? fma(scale, sum.v[l], to[l]) : scale * sum.v[l];
+      for (int l = 0; l < V; ++l) sum[u].v[l] += sums[slot][k][u][lane].v[l];
+    A *to = dW + (int64_t)v * H + c + 32 * V * u;
+#pragma unroll
+    for (int l = 0; l < V; ++l) to[l] = accumulate ? fma(scale, sum[u].v[l], to[l]) : scale * sum[u].v[l];
+  }
 }
 
 // Strips of at most kSumThreads packs, whole warps a group, as many groups a block as fit, chunks of 16 to 256 rows.
@@ -606,7 +631,8 @@ int embed_grad(const T *dy, const int32_t *ids, const int64_t *start, const int3
   if (s.chunks > 1) {
     constexpr int VA = 16 / (int)sizeof(A);
     const bool packs = pack_width<A>(H, dW) >= VA;
-    const dim3 grid((s.chunks + kJoinSlots - 1) / kJoinSlots, (H + 32 * (packs ? VA : 1) - 1) / (32 * (packs ? VA : 1)));
+    const int cols = 32 * (packs ? VA : kJoinCols<1>);  // of a block
+    const dim3 grid((s.chunks + kJoinSlots - 1) / kJoinSlots, (H + cols - 1) / cols);
     auto join = packs ? embed_join_kernel<A, VA> : embed_join_kernel<A, 1>;
     join<<<grid, kJoinSlots * kJoinParts * 32, 0, st>>>(start, ntok, nvocab, H, s.R, s.chunks, (A)scale, accumulate != 0, dW, part, cut);
   }
@@ -674,7 +700,7 @@ int dp_embed_plan(const int32_t *ids, int64_t ntok, int nvocab, int64_t *start, 
     const bool last = pass == s.passes - 1;
     sort_count_kernel<<<s.blocks, kSortThreads, 0, st>>>(ids, from, ntok, nvocab, pass * s.bits, mask, counts);
     sort_scan_kernel<<<kDigits, kDigits, 0, st>>>(counts, s.blocks, totals);
-    sort_place_kernel<<<s.blocks, kSortThreads, 0, st>>>(ids, from, from_idx, ntok, nvocab, pass * s.bits, mask, counts, totals,
+    sort_place_kernel<<<s.blocks, kSortThreads, 0, st>>>(ids, from, from_idx, ntok, nvocab, pass * s.bits, s.bits, counts, totals,
                                                          keys[pass & 1], last ? src : idx[pass & 1], last);
   }
   embed_start_kernel<<<(nvocab + 256) / 256, 256, 0, st>>>(keys[(s.passes - 1) & 1], (int)ntok, nvocab, start);

@@ -247,12 +247,13 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
 // as they are: K 64 an instruction, a scale for 32.
 //   One lane copies a stage's codes, 256 of K, by tensor-map copies into K-major rows of 128 bytes in the 128-byte swizzle
 //   (a map reads zeros past the arrays; rows of another expert or past N land in columns and rows that nobody reads).
-//   Four warps bring the scales of four stages at a time into one of two places, four lanes a row: in shared memory 128
-//   rows' four scales of 128 of K are 512 bytes, row r at 16 (r % 32) + 4 (r / 32), which is how they go to the tensor
-//   memory's columns (repeated in its four lane quadrants).  A proxy fence waits for the thread's loads in flight, some
-//   1000 cycles: once for each stage that bounded the product at 2.0 PFLOP/s.
-//   One lane issues a stage's copies to tensor memory and its MMAs; scales have two places there, taken in turn, and a place
-//   is written again when the MMAs that read it have completed.
+//   Four warps bring the scales, of four stages at a time, four lanes a row, through shared memory: there 128 rows' four
+//   scales of 128 of K are 512 bytes, row r at 16 (r % 32) + 4 (r / 32), so that lane r of each of the warps finds the
+//   words that its quadrant of tensor memory holds in lane r, and writes them there with tcgen05.st.  The scales have five
+//   places, taken in turn; a place is written again when the MMAs that read it have completed.  (Copies from shared to
+//   tensor memory by the MMAs' own thread, tcgen05.cp, take turns with the MMAs: a stage took 2000 cycles whatever its
+//   tile, 32,768 x 2048 x 4096 264 us.)
+//   One lane issues the MMAs.
 //   Eight epilogue warps (two per lane quadrant, half the columns each) finish a tile while the next one runs.
 // A block per SM walks the tiles; every wait is bounded, a block that gives up writes NaN and is counted.
 namespace mx4 {
@@ -265,12 +266,14 @@ template <int TN>
 struct Shape {
   static constexpr int kA = kTM * kRowBytes, kB = TN * kRowBytes, kStageBytes = kA + kB;
   static constexpr int kSA = 1024, kBlocksB = (TN + 127) / 128, kScaleBytes = kSA + 1024 * kBlocksB;  // of a stage
-  static constexpr int kStages = TN > 128 ? 4 : TN > 64 ? 6 : 8;
-  // an accumulator and a place of scales in each half of the columns
-  static constexpr uint32_t kHalf = TN > 128 ? 256 : TN > 64 ? 256 : 128, kTmemCols = 2 * kHalf, kScaleAt = TN;
+  static constexpr int kStages = TN > 128 ? 5 : TN > 64 ? 6 : 8;
   static constexpr uint32_t kColsA = 4, kColsB = 4 * kBlocksB;  // of 128 of K
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 2 * kGroup * kScaleBytes + (2 * kStages + 9) * 8 + 16;  // aligned within
-  static_assert(kStageBytes % 1024 == 0 && kSmem <= 227 * 1024 && TN % 32 == 0 && TN + 2 * (kColsA + kColsB) <= kHalf, "tile");
+  // two accumulators, then the scales' places
+  static constexpr int kPlaces = 5;
+  static constexpr uint32_t kPlaceCols = 2 * (kColsA + kColsB), kScaleAt = 2 * TN, kTmemCols = TN > 64 ? 512 : 256;
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 2 * kGroup * kScaleBytes + (2 * kStages + kPlaces + 9) * 8 + 16;  // aligned within
+  static_assert(kStageBytes % 1024 == 0 && kSmem <= 227 * 1024 && TN % 32 == 0 && kScaleAt + kPlaces * kPlaceCols <= kTmemCols, "tile");
+  static_assert(kPlaces <= kStages, "a place's MMAs are known by their stage's barrier, which has not turned again");
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -280,16 +283,12 @@ __device__ __forceinline__ void arrive(uint32_t bar) {
 __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-// Shared-memory descriptors, version 1: codes K-major in the 128-byte swizzle (8 rows are 1024 bytes), scales as 32 rows
-// of 16 bytes without swizzle (8 rows are 128 bytes).
+// Shared-memory descriptor, version 1: codes K-major in the 128-byte swizzle (8 rows are 1024 bytes).
 __device__ __forceinline__ uint64_t code_desc(uint32_t saddr) {
   return (uint64_t)((saddr & 0x3FFFF) >> 4) | (1ull << 16) | ((uint64_t)(8 * kRowBytes >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
-__device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
-  return (uint64_t)((saddr & 0x3FFFF) >> 4) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
-}
-__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t saddr) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(scale_desc(saddr)) : "memory");
+__device__ __forceinline__ void tmem_st(uint32_t addr, const uint4 &v) {  // four columns
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w));
 }
 __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[16]) {
   asm volatile(
@@ -330,7 +329,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   unsigned char *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
   unsigned char *scale_room = smem + S::kStages * S::kStageBytes;
   uint64_t *codes = reinterpret_cast<uint64_t *>(scale_room + 2 * kGroup * S::kScaleBytes), *empty = codes + S::kStages;
-  uint64_t *scales = empty + S::kStages, *scales_empty = scales + 2, *acc_full = scales_empty + 2, *acc_empty = acc_full + 2;
+  uint64_t *scales = empty + S::kStages, *staged = scales + S::kPlaces, *unstaged = staged + 2, *acc_full = unstaged + 2;
+  uint64_t *acc_empty = acc_full + 2;
   uint64_t *done = acc_empty + 2;
   uint32_t *holder = reinterpret_cast<uint32_t *>(done + 1);
   volatile int *stop = reinterpret_cast<int *>(holder + 1);
@@ -349,9 +349,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       init(codes + s, 1);
       init(empty + s, 1);
     }
+    for (int b = 0; b < S::kPlaces; ++b) init(scales + b, kScaleWarps);
     for (int b = 0; b < 2; ++b) {
-      init(scales + b, kScaleWarps);
-      init(scales_empty + b, 1);
+      init(staged + b, kScaleWarps);
+      init(unstaged + b, kScaleWarps);
       init(acc_full + b, 1);
       init(acc_empty + b, kEpiWarps);
     }
@@ -373,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- the MMAs
-    int j = 0, unit = 0, group = 0;  // stages, tiles, groups of scales
+    int j = 0, unit = 0;  // stages, tiles
     Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
     for (; ok; t.tile += gridDim.x, ++unit) {
       seek_work(p, TN, nct, t);
@@ -385,23 +386,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int buf = unit & 1;
         if (unit >= 2) ok = wait(acc_empty + buf, ((unit >> 1) - 1) & 1);
         const int end = min(nkb, p.give_up - j);
-        const uint32_t acc = tmem + buf * S::kHalf;
+        const uint32_t acc = tmem + buf * TN;
         for (int kb = 0; kb < end && ok; ++kb, ++j) {
-          const int st = j % S::kStages, at = j & 1, place = group & 1;
-          if (kb % kGroup == 0) ok = wait(scales + place, (group >> 1) & 1);
-          ok = ok && wait(codes + st, (j / S::kStages) & 1);
-          if (ok && j >= 2) ok = wait(empty + (j - 2) % S::kStages, ((j - 2) / S::kStages) & 1);
+          const int st = j % S::kStages;
+          const uint32_t ta = tmem + S::kScaleAt + (j % S::kPlaces) * S::kPlaceCols, tb = ta + 2 * S::kColsA;
+          ok = wait(scales + j % S::kPlaces, (j / S::kPlaces) & 1) && wait(codes + st, (j / S::kStages) & 1);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;");
           const uint32_t base = smem_u32(smem) + st * S::kStageBytes;
-          const uint32_t sa = smem_u32(scale_room) + (place * kGroup + kb % kGroup) * S::kScaleBytes, sb = sa + S::kSA;
-          const uint32_t ta = tmem + at * S::kHalf + S::kScaleAt, tb = ta + 2 * S::kColsA;
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            scales_to_tmem(ta + g * S::kColsA, sa + g * 512);
-#pragma unroll
-            for (int b = 0; b < S::kBlocksB; ++b) scales_to_tmem(tb + g * S::kColsB + 4 * b, sb + (g * S::kBlocksB + b) * 512);
-          }
           const uint64_t a0 = code_desc(base), b0 = code_desc(base + S::kA);
 #pragma unroll
           for (int k = 0; k < kKB / 64; ++k) {
@@ -415,10 +407,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                 : "memory");
           }
           commit(smem_u32(empty + st));
-          if (kb % kGroup == kGroup - 1 || kb == nkb - 1) {
-            commit(smem_u32(scales_empty + place));
-            ++group;
-          }
           if (kb == nkb - 1) commit(smem_u32(acc_full + buf));
         }
         ok = ok && end == nkb;
@@ -468,11 +456,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     seek_work(p, TN, nct, t);
     if (t.have) read();
-    const uint32_t to0 = smem_u32(scale_room) + s * S::kScaleBytes + row * 16;
-    while (t.have) {
-      ok = __all_sync(0xffffffffu, wait(scales_empty + (group & 1), (group >> 1 & 1) ^ 1));
+    const uint32_t room = smem_u32(scale_room), to0 = room + s * S::kScaleBytes + row * 16;
+    const uint32_t quadrant = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + S::kScaleAt;
+    auto all_wait = [&](uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+    for (int j = 0; ok && t.have; ++group) {
+      const int buf = group & 1;
+      ok = all_wait(unstaged + buf, (group >> 1 & 1) ^ 1);  // the four warps have read what lay there
       if (!ok) break;
-      const uint32_t to = to0 + (group & 1) * kGroup * S::kScaleBytes;
+      const uint32_t to = to0 + buf * kGroup * S::kScaleBytes;
 #pragma unroll
       for (int i = 0; i < kRA + kRB; ++i) {  // row r of an operand: block r / 128 of each 128 of K, word r / 32 % 4
         const int q = i < kRA ? i : i - kRA, nblk = i < kRA ? 1 : S::kBlocksB;
@@ -480,10 +471,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("st.shared.b32 [%0], %1;" ::"r"(d), "r"(v[i].x) : "memory");
         asm volatile("st.shared.b32 [%0], %1;" ::"r"(d + 512 * nblk), "r"(v[i].y) : "memory");
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) arrive(smem_u32(scales + (group & 1)));
-      ++group;
+      if (lane == 0) arrive(smem_u32(staged + buf));
+      const int stages = min(kGroup, nkb - kb);
       kb += kGroup;
       if (kb >= nkb) {
         kb = 0;
@@ -491,6 +481,26 @@ __global__ void __launch_bounds__(kThreads, 1)
         seek_work(p, TN, nct, t);
       }
       if (t.have) read();  // on its way while the MMAs work on what is there
+      ok = all_wait(staged + buf, group >> 1 & 1);
+      for (int i = 0; ok && i < stages; ++i, ++j) {
+        const uint32_t from = room + (buf * kGroup + i) * S::kScaleBytes + lane * 16;
+        constexpr int kBlocks = S::kScaleBytes / 512;  // an operand's 128 rows by 128 of K, in the order of the columns
+        uint4 w[kBlocks];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+          asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[b].x), "=r"(w[b].y), "=r"(w[b].z), "=r"(w[b].w) : "r"(from + b * 512));
+        if (j >= S::kPlaces) ok = all_wait(empty + (j - S::kPlaces) % S::kStages, ((j - S::kPlaces) / S::kStages) & 1);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;");
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) tmem_st(quadrant + (j % S::kPlaces) * S::kPlaceCols + 4 * b, w[b]);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;");
+        __syncwarp();
+        if (lane == 0) arrive(smem_u32(scales + j % S::kPlaces));
+      }
+      __syncwarp();
+      if (lane == 0) arrive(smem_u32(unstaged + buf));
     }
     if (!ok) *stop = 1;
   } else {
@@ -520,7 +530,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int left = nr - c0 - g;
         float v[16];
         if (ok) {
-          tmem_ld(trow + (unit & 1) * S::kHalf + g, v);
+          tmem_ld(trow + (unit & 1) * TN + g, v);
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
         }
 #pragma unroll
@@ -628,15 +638,15 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
 }
 
 // Which kernel: tiles of more rows need fewer rounds over 152 SMs, but a round of them takes longer.
-enum Mx4Form { kFew, kTiles64, kTiles128, kTiles224 };
+enum Mx4Form { kFew, kTiles64, kTiles128, kTiles192 };
 Mx4Form form_of(int64_t rows, int N, int nexp) {
   if (rows <= 16) return kFew;
   auto cost = [&](int R) {
     const int64_t rounds = (((rows + R - 1) / R + nexp / 2) * ((N + mx4::kTM - 1) / mx4::kTM) + 151) / 152;
     return rounds * (R + 64);
   };
-  const int64_t c64 = cost(64), c128 = cost(128), c224 = cost(224);
-  return c224 < c128 && c224 < c64 ? kTiles224 : c128 < c64 ? kTiles128 : kTiles64;
+  const int64_t c64 = cost(64), c128 = cost(128), c192 = cost(192);
+  return c192 < c128 && c192 < c64 ? kTiles192 : c128 < c64 ? kTiles128 : kTiles64;
 }
 
 template <typename T>
@@ -668,7 +678,7 @@ int linear(const uint8_t *xq, const uint8_t *sx, int64_t rows, int K, const uint
     }
     case kTiles64: rc = mx4::launch_tc<T, 64>(p, tiles(64), st, who); break;
     case kTiles128: rc = mx4::launch_tc<T, 128>(p, tiles(128), st, who); break;
-    case kTiles224: rc = mx4::launch_tc<T, 224>(p, tiles(224), st, who); break;
+    case kTiles192: rc = mx4::launch_tc<T, 192>(p, tiles(192), st, who); break;
   }
   if (rc) return rc;
   return launch_status(who);
