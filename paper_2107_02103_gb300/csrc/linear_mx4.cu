@@ -249,10 +249,10 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
 //   (a map reads zeros past the arrays; rows of another expert or past N land in columns and rows that nobody reads).
 //   Four warps bring the scales, of four stages at a time, four lanes a row, through shared memory: there 128 rows' four
 //   scales of 128 of K are 512 bytes, row r at 16 (r % 32) + 4 (r / 32), so that lane r of each of the warps finds the
-//   words that its quadrant of tensor memory holds in lane r, and writes them there with tcgen05.st.  The scales have five
-//   places, taken in turn; a place is written again when the MMAs that read it have completed.  (Copies from shared to
-//   tensor memory by the MMAs' own thread, tcgen05.cp, take turns with the MMAs: a stage took 2000 cycles whatever its
-//   tile, 32,768 x 2048 x 4096 264 us.)
+//   words that its quadrant of tensor memory holds in lane r, and writes them there with tcgen05.st, two stages at a time.
+//   Two stages' scales have two places, taken in turn; a place is written again when the MMAs that read it have completed.
+//   (Copies from shared to tensor memory by the MMAs' own thread, tcgen05.cp, take turns with the MMAs: a stage took 2000
+//   cycles whatever its tile, 32,768 x 2048 x 4096 264 us; stages one by one 220 us.)
 //   One lane issues the MMAs.
 //   Eight epilogue warps (two per lane quadrant, half the columns each) finish a tile while the next one runs.
 // A block per SM walks the tiles; every wait is bounded, a block that gives up writes NaN and is counted.
@@ -269,11 +269,10 @@ struct Shape {
   static constexpr int kStages = TN > 128 ? 5 : TN > 64 ? 6 : 8;
   static constexpr uint32_t kColsA = 4, kColsB = 4 * kBlocksB;  // of 128 of K
   // two accumulators, then the scales' places
-  static constexpr int kPlaces = 5;
-  static constexpr uint32_t kPlaceCols = 2 * (kColsA + kColsB), kScaleAt = 2 * TN, kTmemCols = TN > 64 ? 512 : 256;
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 2 * kGroup * kScaleBytes + (2 * kStages + kPlaces + 9) * 8 + 16;  // aligned within
-  static_assert(kStageBytes % 1024 == 0 && kSmem <= 227 * 1024 && TN % 32 == 0 && kScaleAt + kPlaces * kPlaceCols <= kTmemCols, "tile");
-  static_assert(kPlaces <= kStages, "a place's MMAs are known by their stage's barrier, which has not turned again");
+  static constexpr uint32_t kStageCols = 2 * (kColsA + kColsB), kPlaceCols = 2 * kStageCols, kScaleAt = 2 * TN;
+  static constexpr uint32_t kTmemCols = TN > 64 ? 512 : 256;
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 2 * kGroup * kScaleBytes + (2 * kStages + 13) * 8 + 16;  // aligned within
+  static_assert(kStageBytes % 1024 == 0 && kSmem <= 227 * 1024 && TN % 32 == 0 && kScaleAt + 2 * kPlaceCols <= kTmemCols, "tile");
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -329,7 +328,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   unsigned char *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
   unsigned char *scale_room = smem + S::kStages * S::kStageBytes;
   uint64_t *codes = reinterpret_cast<uint64_t *>(scale_room + 2 * kGroup * S::kScaleBytes), *empty = codes + S::kStages;
-  uint64_t *scales = empty + S::kStages, *staged = scales + S::kPlaces, *unstaged = staged + 2, *acc_full = unstaged + 2;
+  uint64_t *scales = empty + S::kStages, *scales_read = scales + 2, *staged = scales_read + 2, *unstaged = staged + 2;
+  uint64_t *acc_full = unstaged + 2;
   uint64_t *acc_empty = acc_full + 2;
   uint64_t *done = acc_empty + 2;
   uint32_t *holder = reinterpret_cast<uint32_t *>(done + 1);
@@ -349,8 +349,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       init(codes + s, 1);
       init(empty + s, 1);
     }
-    for (int b = 0; b < S::kPlaces; ++b) init(scales + b, kScaleWarps);
     for (int b = 0; b < 2; ++b) {
+      init(scales + b, kScaleWarps);
+      init(scales_read + b, 1);
       init(staged + b, kScaleWarps);
       init(unstaged + b, kScaleWarps);
       init(acc_full + b, 1);
@@ -374,40 +375,58 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- the MMAs
-    int j = 0, unit = 0;  // stages, tiles
+    int j = 0, unit = 0, pair = 0;  // stages, tiles, pairs of stages
+    int st = 0;                     // j's place
+    uint32_t turn = 0;              // and the parity of its turn
+    const uint64_t a_at = code_desc(smem_u32(smem)), b_at = a_at + (S::kA >> 4);
     Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
     for (; ok; t.tile += gridDim.x, ++unit) {
       seek_work(p, TN, nct, t);
       if (!t.have) break;
       const uint32_t cols = (uint32_t)(t.r1 - t.r0 + 15) / 16 * 16;
-      // fp4 operands, K-major; scales are powers of two
-      const uint32_t idesc = (1u << 7) | (1u << 10) | ((cols >> 3) << 17) | (1u << 23) | ((uint32_t)(kTM >> 7) << 27);
+      // fp4 operands, K-major; scales are powers of two, a word's lower two or upper two
+      const uint32_t low = (1u << 7) | (1u << 10) | ((cols >> 3) << 17) | (1u << 23) | ((uint32_t)(kTM >> 7) << 27);
+      const uint32_t high = low | (2u << 4) | (2u << 29);
       if (lane == 0) {
         const int buf = unit & 1;
         if (unit >= 2) ok = wait(acc_empty + buf, ((unit >> 1) - 1) & 1);
         const int end = min(nkb, p.give_up - j);
         const uint32_t acc = tmem + buf * TN;
+        auto mma = [&](int k, uint64_t a, uint64_t b, uint32_t ta, bool add) {
+          asm volatile(
+              "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+              " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(acc),
+              "l"(a + (uint64_t)(k * 2)), "l"(b + (uint64_t)(k * 2)), "r"(k & 1 ? high : low), "r"(ta + (k >> 1) * S::kColsA),
+              "r"(ta + 2 * S::kColsA + (k >> 1) * S::kColsB), "r"(add ? 1u : 0u)
+              : "memory");
+        };
         for (int kb = 0; kb < end && ok; ++kb, ++j) {
-          const int st = j % S::kStages;
-          const uint32_t ta = tmem + S::kScaleAt + (j % S::kPlaces) * S::kPlaceCols, tb = ta + 2 * S::kColsA;
-          ok = wait(scales + j % S::kPlaces, (j / S::kPlaces) & 1) && wait(codes + st, (j / S::kStages) & 1);
+          const uint32_t ta = tmem + S::kScaleAt + (pair & 1) * S::kPlaceCols + (kb & 1) * S::kStageCols;
+          if (!(kb & 1)) ok = wait(scales + (pair & 1), (pair >> 1) & 1);
+          ok = ok && wait(codes + st, turn);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;");
-          const uint32_t base = smem_u32(smem) + st * S::kStageBytes;
-          const uint64_t a0 = code_desc(base), b0 = code_desc(base + S::kA);
+          const uint64_t a = a_at + (uint64_t)(st * (S::kStageBytes >> 4)), b = b_at + (uint64_t)(st * (S::kStageBytes >> 4));
+          if ((kb + 1) * kKB <= p.K) {
+            mma(0, a, b, ta, kb > 0);
+            mma(1, a, b, ta, true);
+            mma(2, a, b, ta, true);
+            mma(3, a, b, ta, true);
+          } else {
 #pragma unroll
-          for (int k = 0; k < kKB / 64; ++k) {
-            if (kb * kKB + k * 64 >= p.K) break;
-            const uint32_t which = (uint32_t)(k & 1) * 2, id = idesc | (which << 4) | (which << 29);  // a word's lower or upper two scales
-            asm volatile(
-                "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
-                " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(acc),
-                "l"(a0 + (uint64_t)(k * 2)), "l"(b0 + (uint64_t)(k * 2)), "r"(id), "r"(ta + (k >> 1) * S::kColsA),
-                "r"(tb + (k >> 1) * S::kColsB), "r"(kb > 0 || k > 0 ? 1u : 0u)
-                : "memory");
+            for (int k = 0; k < kKB / 64 - 1; ++k)
+              if (kb * kKB + k * 64 < p.K) mma(k, a, b, ta, kb > 0 || k > 0);
           }
           commit(smem_u32(empty + st));
+          if ((kb & 1) || kb == nkb - 1) {
+            commit(smem_u32(scales_read + (pair & 1)));
+            ++pair;
+          }
           if (kb == nkb - 1) commit(smem_u32(acc_full + buf));
+          if (++st == S::kStages) {
+            st = 0;
+            turn ^= 1;
+          }
         }
         ok = ok && end == nkb;
       }
@@ -459,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t room = smem_u32(scale_room), to0 = room + s * S::kScaleBytes + row * 16;
     const uint32_t quadrant = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + S::kScaleAt;
     auto all_wait = [&](uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
-    for (int j = 0; ok && t.have; ++group) {
+    for (int pair = 0; ok && t.have; ++group) {
       const int buf = group & 1;
       ok = all_wait(unstaged + buf, (group >> 1 & 1) ^ 1);  // the four warps have read what lay there
       if (!ok) break;
@@ -482,22 +501,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (t.have) read();  // on its way while the MMAs work on what is there
       ok = all_wait(staged + buf, group >> 1 & 1);
-      for (int i = 0; ok && i < stages; ++i, ++j) {
+      for (int i = 0; ok && i < stages; i += 2, ++pair) {
         const uint32_t from = room + (buf * kGroup + i) * S::kScaleBytes + lane * 16;
         constexpr int kBlocks = S::kScaleBytes / 512;  // an operand's 128 rows by 128 of K, in the order of the columns
-        uint4 w[kBlocks];
+        uint4 w[2 * kBlocks];
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
+        for (int b = 0; b < 2 * kBlocks; ++b)  // of a last stage alone: what lay there before, for columns that are not read
           asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[b].x), "=r"(w[b].y), "=r"(w[b].z), "=r"(w[b].w) : "r"(from + b * 512));
-        if (j >= S::kPlaces) ok = all_wait(empty + (j - S::kPlaces) % S::kStages, ((j - S::kPlaces) / S::kStages) & 1);
+        ok = all_wait(scales_read + (pair & 1), (pair >> 1 & 1) ^ 1);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;");
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) tmem_st(quadrant + (j % S::kPlaces) * S::kPlaceCols + 4 * b, w[b]);
+        for (int b = 0; b < 2 * kBlocks; ++b) tmem_st(quadrant + (pair & 1) * S::kPlaceCols + 4 * b, w[b]);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;");
         __syncwarp();
-        if (lane == 0) arrive(smem_u32(scales + j % S::kPlaces));
+        if (lane == 0) arrive(smem_u32(scales + (pair & 1)));
       }
       __syncwarp();
       if (lane == 0) arrive(smem_u32(unstaged + buf));
