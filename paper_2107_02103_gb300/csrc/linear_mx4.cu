@@ -253,7 +253,8 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
 //   Two stages' scales have two places, taken in turn; a place is written again when the MMAs that read it have completed.
 //   (Copies from shared to tensor memory by the MMAs' own thread, tcgen05.cp, take turns with the MMAs: a stage took 2000
 //   cycles whatever its tile, 32,768 x 2048 x 4096 264 us; stages one by one 220 us.)
-//   One lane issues the MMAs.
+//   One lane issues the MMAs; its warp walks the stages together, so that addresses and descriptors stay in uniform
+//   registers (in a branch for one lane a stage's issue took 600 cycles).
 //   Eight epilogue warps (two per lane quadrant, half the columns each) finish a tile while the next one runs.
 // A block per SM walks the tiles; every wait is bounded, a block that gives up writes NaN and is counted.
 namespace mx4 {
@@ -278,6 +279,11 @@ struct Shape {
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool elect_one() {  // one lane of a converged warp
+  uint32_t is;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(is));
+  return is != 0;
 }
 __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -378,6 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     int j = 0, unit = 0, pair = 0;  // stages, tiles, pairs of stages
     int st = 0;                     // j's place
     uint32_t turn = 0;              // and the parity of its turn
+    const bool leader = elect_one();
     const uint64_t a_at = code_desc(smem_u32(smem)), b_at = a_at + (S::kA >> 4);
     Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
     for (; ok; t.tile += gridDim.x, ++unit) {
@@ -387,26 +394,28 @@ __global__ void __launch_bounds__(kThreads, 1)
       // fp4 operands, K-major; scales are powers of two, a word's lower two or upper two
       const uint32_t low = (1u << 7) | (1u << 10) | ((cols >> 3) << 17) | (1u << 23) | ((uint32_t)(kTM >> 7) << 27);
       const uint32_t high = low | (2u << 4) | (2u << 29);
-      if (lane == 0) {
-        const int buf = unit & 1;
-        if (unit >= 2) ok = wait(acc_empty + buf, ((unit >> 1) - 1) & 1);
-        const int end = min(nkb, p.give_up - j);
-        const uint32_t acc = tmem + buf * TN;
-        auto mma = [&](int k, uint64_t a, uint64_t b, uint32_t ta, bool add) {
-          asm volatile(
-              "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
-              " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(acc),
-              "l"(a + (uint64_t)(k * 2)), "l"(b + (uint64_t)(k * 2)), "r"(k & 1 ? high : low), "r"(ta + (k >> 1) * S::kColsA),
-              "r"(ta + 2 * S::kColsA + (k >> 1) * S::kColsB), "r"(add ? 1u : 0u)
-              : "memory");
-        };
-        for (int kb = 0; kb < end && ok; ++kb, ++j) {
-          const uint32_t ta = tmem + S::kScaleAt + (pair & 1) * S::kPlaceCols + (kb & 1) * S::kStageCols;
-          if (!(kb & 1)) ok = wait(scales + (pair & 1), (pair >> 1) & 1);
-          ok = ok && wait(codes + st, turn);
-          if (!ok) break;
-          asm volatile("tcgen05.fence::after_thread_sync;");
-          const uint64_t a = a_at + (uint64_t)(st * (S::kStageBytes >> 4)), b = b_at + (uint64_t)(st * (S::kStageBytes >> 4));
+      const int buf = unit & 1;
+      auto all = [&](uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+      if (unit >= 2) ok = all(acc_empty + buf, ((unit >> 1) - 1) & 1);
+      const int end = min(nkb, p.give_up - j);
+      const uint32_t acc = tmem + buf * TN;
+      auto mma = [&](int k, uint64_t a, uint64_t b, uint32_t ta, bool add) {
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(acc),
+            "l"(a + (uint64_t)(k * 2)), "l"(b + (uint64_t)(k * 2)), "r"(k & 1 ? high : low), "r"(ta + (k >> 1) * S::kColsA),
+            "r"(ta + 2 * S::kColsA + (k >> 1) * S::kColsB), "r"(add ? 1u : 0u)
+            : "memory");
+      };
+      for (int kb = 0; kb < end && ok; ++kb, ++j) {
+        const uint32_t ta = tmem + S::kScaleAt + (pair & 1) * S::kPlaceCols + (kb & 1) * S::kStageCols;
+        if (!(kb & 1)) ok = all(scales + (pair & 1), (pair >> 1) & 1);
+        ok = ok && all(codes + st, turn);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;");
+        const uint64_t a = a_at + (uint64_t)(st * (S::kStageBytes >> 4)), b = b_at + (uint64_t)(st * (S::kStageBytes >> 4));
+        const bool last = kb == nkb - 1, ends = (kb & 1) || last;  // a pair
+        if (leader) {
           if ((kb + 1) * kKB <= p.K) {
             mma(0, a, b, ta, kb > 0);
             mma(1, a, b, ta, true);
@@ -418,21 +427,19 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (kb * kKB + k * 64 < p.K) mma(k, a, b, ta, kb > 0 || k > 0);
           }
           commit(smem_u32(empty + st));
-          if ((kb & 1) || kb == nkb - 1) {
-            commit(smem_u32(scales_read + (pair & 1)));
-            ++pair;
-          }
-          if (kb == nkb - 1) commit(smem_u32(acc_full + buf));
-          if (++st == S::kStages) {
-            st = 0;
-            turn ^= 1;
-          }
+          if (ends) commit(smem_u32(scales_read + (pair & 1)));
+          if (last) commit(smem_u32(acc_full + buf));
         }
-        ok = ok && end == nkb;
+        __syncwarp();
+        if (ends) ++pair;
+        if (++st == S::kStages) {
+          st = 0;
+          turn ^= 1;
+        }
       }
-      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+      ok = ok && end == nkb;
     }
-    if (lane == 0) commit(smem_u32(done));  // completes when every MMA issued above has
+    if (leader) commit(smem_u32(done));  // completes when every MMA issued above has
     if (!ok) *stop = 1;
   } else if (warp == kCopyWarp) {
     // ---------------------------------------------------------------- the codes
