@@ -198,9 +198,9 @@ __device__ __forceinline__ float pow2_of(uint32_t code) {
   return __uint_as_float(code == 0 ? 0x00400000u : code == 255 ? 0x7fc00000u : code << 23);
 }
 
-constexpr int kFewWarps = 8, kFewRows = 8;
+constexpr int kFewWarps = 8, kFewRows = 2;
 
-// A warp per output channel and tile of up to eight rows, a scale's block a lane: the block's sum is exact in integers.
+// A warp per output channel and tile of up to two rows, a scale's block a lane: the block's sum is exact in integers.
 template <typename T>
 __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx4Args p) {
   int e, r0, r1;
@@ -250,11 +250,12 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
 //   Four warps bring the scales, of four stages at a time, four lanes a row, through shared memory: there 128 rows' four
 //   scales of 128 of K are 512 bytes, row r at 16 (r % 32) + 4 (r / 32), so that lane r of each of the warps finds the
 //   words that its quadrant of tensor memory holds in lane r, and writes them there with tcgen05.st, two stages at a time.
-//   Two stages' scales have two places, taken in turn; a place is written again when the MMAs that read it have completed.
+//   Two stages' scales have three places, taken in turn; a place is written again when the MMAs that read it have completed.
 //   (Copies from shared to tensor memory by the MMAs' own thread, tcgen05.cp, take turns with the MMAs: a stage took 2000
 //   cycles whatever its tile, 32,768 x 2048 x 4096 264 us; stages one by one 220 us.)
 //   One lane issues the MMAs; its warp walks the stages together, so that addresses and descriptors stay in uniform
-//   registers (in a branch for one lane a stage's issue took 600 cycles).
+//   registers (in a branch for one lane a stage's issue took 600 cycles), and waits once for two stages: the scales'
+//   warps have waited for their codes.
 //   Eight epilogue warps (two per lane quadrant, half the columns each) finish a tile while the next one runs.
 // A block per SM walks the tiles; every wait is bounded, a block that gives up writes NaN and is counted.
 namespace mx4 {
@@ -268,12 +269,13 @@ struct Shape {
   static constexpr int kA = kTM * kRowBytes, kB = TN * kRowBytes, kStageBytes = kA + kB;
   static constexpr int kSA = 1024, kBlocksB = (TN + 127) / 128, kScaleBytes = kSA + 1024 * kBlocksB;  // of a stage
   static constexpr int kStages = TN > 128 ? 5 : TN > 64 ? 6 : 8;
-  static constexpr uint32_t kColsA = 4, kColsB = 4 * kBlocksB;  // of 128 of K
+  static constexpr uint32_t kColsA = 4, kColsB = TN / 32;  // of 128 of K
   // two accumulators, then the scales' places
+  static constexpr int kPlaces = 3;
   static constexpr uint32_t kStageCols = 2 * (kColsA + kColsB), kPlaceCols = 2 * kStageCols, kScaleAt = 2 * TN;
   static constexpr uint32_t kTmemCols = TN > 64 ? 512 : 256;
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 2 * kGroup * kScaleBytes + (2 * kStages + 13) * 8 + 16;  // aligned within
-  static_assert(kStageBytes % 1024 == 0 && kSmem <= 227 * 1024 && TN % 32 == 0 && kScaleAt + 2 * kPlaceCols <= kTmemCols, "tile");
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 2 * kGroup * kScaleBytes + (2 * kStages + kPlaces + 9) * 8 + 16;  // aligned within
+  static_assert(kStageBytes % 1024 == 0 && kSmem <= 227 * 1024 && TN % 32 == 0 && kScaleAt + kPlaces * kPlaceCols <= kTmemCols, "tile");
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -292,7 +294,10 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 __device__ __forceinline__ uint64_t code_desc(uint32_t saddr) {
   return (uint64_t)((saddr & 0x3FFFF) >> 4) | (1ull << 16) | ((uint64_t)(8 * kRowBytes >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
-__device__ __forceinline__ void tmem_st(uint32_t addr, const uint4 &v) {  // four columns
+__device__ __forceinline__ void tmem_st2(uint32_t addr, const uint4 &v) {  // two columns
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1,%2};" ::"r"(addr), "r"(v.x), "r"(v.y));
+}
+__device__ __forceinline__ void tmem_st(uint32_t addr, const uint4 &v) {  // four
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w));
 }
 __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[16]) {
@@ -334,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   unsigned char *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
   unsigned char *scale_room = smem + S::kStages * S::kStageBytes;
   uint64_t *codes = reinterpret_cast<uint64_t *>(scale_room + 2 * kGroup * S::kScaleBytes), *empty = codes + S::kStages;
-  uint64_t *scales = empty + S::kStages, *scales_read = scales + 2, *staged = scales_read + 2, *unstaged = staged + 2;
+  uint64_t *scales = empty + S::kStages, *staged = scales + S::kPlaces, *unstaged = staged + 2;
   uint64_t *acc_full = unstaged + 2;
   uint64_t *acc_empty = acc_full + 2;
   uint64_t *done = acc_empty + 2;
@@ -355,9 +360,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       init(codes + s, 1);
       init(empty + s, 1);
     }
+    for (int b = 0; b < S::kPlaces; ++b) init(scales + b, kScaleWarps);
     for (int b = 0; b < 2; ++b) {
-      init(scales + b, kScaleWarps);
-      init(scales_read + b, 1);
       init(staged + b, kScaleWarps);
       init(unstaged + b, kScaleWarps);
       init(acc_full + b, 1);
@@ -381,9 +385,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- the MMAs
-    int j = 0, unit = 0, pair = 0;  // stages, tiles, pairs of stages
-    int st = 0;                     // j's place
-    uint32_t turn = 0;              // and the parity of its turn
+    int j = 0, unit = 0;     // stages, tiles
+    int st = 0, place = 0;   // j's place, its scales' place
+    uint32_t turn = 0;       // the parity of the latter's turn
     const bool leader = elect_one();
     const uint64_t a_at = code_desc(smem_u32(smem)), b_at = a_at + (S::kA >> 4);
     Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
@@ -407,37 +411,37 @@ __global__ void __launch_bounds__(kThreads, 1)
             "r"(ta + 2 * S::kColsA + (k >> 1) * S::kColsB), "r"(add ? 1u : 0u)
             : "memory");
       };
-      for (int kb = 0; kb < end && ok; ++kb, ++j) {
-        const uint32_t ta = tmem + S::kScaleAt + (pair & 1) * S::kPlaceCols + (kb & 1) * S::kStageCols;
-        if (!(kb & 1)) ok = all(scales + (pair & 1), (pair >> 1) & 1);
-        ok = ok && all(codes + st, turn);
+      for (int kb = 0; kb < nkb; kb += 2) {
+        const int n = min(2, nkb - kb);
+        ok = ok && kb + n <= end && all(scales + place, turn);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;");
-        const uint64_t a = a_at + (uint64_t)(st * (S::kStageBytes >> 4)), b = b_at + (uint64_t)(st * (S::kStageBytes >> 4));
-        const bool last = kb == nkb - 1, ends = (kb & 1) || last;  // a pair
-        if (leader) {
-          if ((kb + 1) * kKB <= p.K) {
-            mma(0, a, b, ta, kb > 0);
-            mma(1, a, b, ta, true);
-            mma(2, a, b, ta, true);
-            mma(3, a, b, ta, true);
-          } else {
-#pragma unroll
-            for (int k = 0; k < kKB / 64 - 1; ++k)
-              if (kb * kKB + k * 64 < p.K) mma(k, a, b, ta, kb > 0 || k > 0);
-          }
-          commit(smem_u32(empty + st));
-          if (ends) commit(smem_u32(scales_read + (pair & 1)));
-          if (last) commit(smem_u32(acc_full + buf));
-        }
-        __syncwarp();
-        if (ends) ++pair;
-        if (++st == S::kStages) {
-          st = 0;
+        const uint32_t ta = tmem + S::kScaleAt + place * S::kPlaceCols;
+        if (++place == S::kPlaces) {
+          place = 0;
           turn ^= 1;
         }
+        for (int i = 0; i < n; ++i, ++j) {
+          const uint64_t a = a_at + (uint64_t)(st * (S::kStageBytes >> 4)), b = b_at + (uint64_t)(st * (S::kStageBytes >> 4));
+          const uint32_t tai = ta + i * S::kStageCols;
+          if (leader) {
+            if ((kb + i + 1) * kKB <= p.K) {
+              mma(0, a, b, tai, kb + i > 0);
+              mma(1, a, b, tai, true);
+              mma(2, a, b, tai, true);
+              mma(3, a, b, tai, true);
+            } else {
+#pragma unroll
+              for (int k = 0; k < kKB / 64 - 1; ++k)
+                if ((kb + i) * kKB + k * 64 < p.K) mma(k, a, b, tai, kb + i > 0 || k > 0);
+            }
+            commit(smem_u32(empty + st));
+            if (kb + i == nkb - 1) commit(smem_u32(acc_full + buf));
+          }
+          if (++st == S::kStages) st = 0;
+        }
+        __syncwarp();
       }
-      ok = ok && end == nkb;
     }
     if (leader) commit(smem_u32(done));  // completes when every MMA issued above has
     if (!ok) *stop = 1;
@@ -485,7 +489,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t room = smem_u32(scale_room), to0 = room + s * S::kScaleBytes + row * 16;
     const uint32_t quadrant = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + S::kScaleAt;
     auto all_wait = [&](uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
-    for (int pair = 0; ok && t.have; ++group) {
+    int j = 0, place = 0, last0 = -1, last1 = -1, last2 = -1;  // the stage, the pair's place; the last stages of the pairs before, the latest first
+    static_assert(S::kPlaces == 3, "as many pairs before");
+    for (; ok && t.have; ++group) {
       const int buf = group & 1;
       ok = all_wait(unstaged + buf, (group >> 1 & 1) ^ 1);  // the four warps have read what lay there
       if (!ok) break;
@@ -508,22 +514,39 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (t.have) read();  // on its way while the MMAs work on what is there
       ok = all_wait(staged + buf, group >> 1 & 1);
-      for (int i = 0; ok && i < stages; i += 2, ++pair) {
+      for (int i = 0; ok && i < stages; i += 2) {
         const uint32_t from = room + (buf * kGroup + i) * S::kScaleBytes + lane * 16;
         constexpr int kBlocks = S::kScaleBytes / 512;  // an operand's 128 rows by 128 of K, in the order of the columns
         uint4 w[2 * kBlocks];
 #pragma unroll
         for (int b = 0; b < 2 * kBlocks; ++b)  // of a last stage alone: what lay there before, for columns that are not read
           asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[b].x), "=r"(w[b].y), "=r"(w[b].z), "=r"(w[b].w) : "r"(from + b * 512));
-        ok = all_wait(scales_read + (pair & 1), (pair >> 1 & 1) ^ 1);
+        const int n = min(2, stages - i);
+        if (last2 >= 0) ok = all_wait(empty + last2 % S::kStages, last2 / S::kStages & 1);  // the place's MMAs are through
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;");
+        uint32_t at = quadrant + place * S::kPlaceCols;
 #pragma unroll
-        for (int b = 0; b < 2 * kBlocks; ++b) tmem_st(quadrant + (pair & 1) * S::kPlaceCols + 4 * b, w[b]);
+        for (int b = 0; b < 2 * kBlocks; ++b) {
+          const int in = b % kBlocks;  // A of both 128 of K, then B's blocks of both
+          const uint32_t cols = in < 2 ? S::kColsA : (in - 2) % S::kBlocksB < S::kBlocksB - 1 ? 4 : S::kColsB - 4 * (S::kBlocksB - 1);
+          if (cols == 4) tmem_st(at, w[b]);
+          else tmem_st2(at, w[b]);
+          at += cols;
+        }
+        static_assert(S::kColsB % 2 == 0 && (S::kColsB % 4 == 0 || S::kColsB % 4 == 2), "two or four columns");
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;");
+        if (warp == kEpiWarps)  // one of the warps waits for the codes too
+          for (int k = j; ok && k < j + n; ++k) ok = all_wait(codes + k % S::kStages, k / S::kStages & 1);
+        if (!ok) break;
         __syncwarp();
-        if (lane == 0) arrive(smem_u32(scales + (pair & 1)));
+        if (lane == 0) arrive(smem_u32(scales + place));
+        if (++place == S::kPlaces) place = 0;
+        j += n;
+        last2 = last1;
+        last1 = last0;
+        last0 = j - 1;
       }
       __syncwarp();
       if (lane == 0) arrive(smem_u32(unstaged + buf));
@@ -663,13 +686,16 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
   return launch_status(who);
 }
 
-// Which kernel: tiles of more rows need fewer rounds over 152 SMs, but a round of them takes longer.
+// Which kernel.  One or two rows: the tiles' start costs 2 us more than a short dot product (back to back, us, few and
+// tiles of 64: 1 row of 1600 -> 2048 6.2 and 8.2, 2 rows of it in two experts 8.3 and 8.3, 2 rows of 4096 -> 4096 12.9 and
+// 11.1, 1 row of 8192 -> 8192 20.6 and 16.4, 4 rows of 1600 -> 2048 8.2 and 8.2).  Tiles of more rows need fewer rounds over
+// 152 SMs, and a round of them takes little longer: 3.4, 3.8 and 4.3 us at K 2048 for 64, 128 and 192 rows.
 enum Mx4Form { kFew, kTiles64, kTiles128, kTiles192 };
-Mx4Form form_of(int64_t rows, int N, int nexp) {
-  if (rows <= 16) return kFew;
+Mx4Form form_of(int64_t rows, int K, int N, int nexp) {
+  if (rows <= kFewRows && rows * K * N <= 1 << 23) return kFew;
   auto cost = [&](int R) {
     const int64_t rounds = (((rows + R - 1) / R + nexp / 2) * ((N + mx4::kTM - 1) / mx4::kTM) + 151) / 152;
-    return rounds * (R + 64);
+    return rounds * (R + 360);
   };
   const int64_t c64 = cost(64), c128 = cost(128), c192 = cost(192);
   return c192 < c128 && c192 < c64 ? kTiles192 : c128 < c64 ? kTiles128 : kTiles64;
@@ -696,7 +722,7 @@ int linear(const uint8_t *xq, const uint8_t *sx, int64_t rows, int K, const uint
   const int64_t pieces = start ? (nexp + 1 < rows ? nexp + 1 : rows) : 0;  // a tile more for each expert's remainder
   auto tiles = [&](int R) { return (rows + R - 1) / R + pieces; };
   int rc = DP_OK;
-  switch (form_of(rows, N, nexp)) {
+  switch (form_of(rows, K, N, nexp)) {
     case kFew: {
       const dim3 grid((unsigned)tiles(kFewRows), (N + kFewWarps - 1) / kFewWarps);
       linear_mx4_few_kernel<T><<<grid, kFewWarps * 32, 0, st>>>(p);

@@ -103,8 +103,8 @@ def check(y, x, w, bias, act, dtype, what=""):
 
 PRODUCTS = [(1, 64, 1, 1), (1, 1600, 100, 1), (3, 240, 33, 1), (16, 1003, 70, 1), (17, 64, 5, 1), (17, 1237, 517, 1), (64, 256, 128, 1), (65, 512, 129, 1), (130, 320, 260, 1),
             (300, 96, 17, 1), (500, 1600, 240, 1), (1000, 2048, 300, 1), (40, 4096, 64, 1), (2000, 64, 64, 1),
-            # tiles of 128 and of 224 rows
-            (12000, 320, 260, 1), (30000, 64, 300, 1), (6000, 1088, 2100, 1)]
+            # tiles of 128 and of 192 rows
+            (12000, 320, 260, 1), (30000, 64, 300, 1), (6000, 1088, 2100, 1), (2, 512, 33, 1), (2, 4096, 2100, 1), (4, 1600, 300, 1)]
 
 
 @pytest.mark.parametrize("dtype", ROWS, ids=IDS)
