@@ -24,41 +24,31 @@ __device__ __forceinline__ uint32_t sort_key(int32_t id, int nvocab) {
   return (uint32_t)id < (uint32_t)nvocab ? (uint32_t)id : (uint32_t)nvocab;
 }
 
-// A thread's kPer items of a block in order by warp, 32 apart: the warp counts them by digit, then gives each its place
-// in its digit, after the warps before it and those before it in its warp.  The lanes with the same digit are found by a
-// vote on each of its bits (a warp-wide match takes twice as long), and one of them moves the warp's counter: no atomics.
-// mine: the warp's counters of the digits, from counts to the next places.
+// A thread's kPer items of a block in order by warp, 32 apart: the warp counts them by digit.
 template <int kPer>
 struct SortItems {
   uint32_t key[kPer];
-  unsigned same[kPer];
   int64_t first;
-  __device__ __forceinline__ void count(int64_t n, int shift, int bits, int *mine) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const uint32_t d = key[i] >> shift;
-      const bool have = first + 32 * i < n;
-      same[i] = __ballot_sync(0xffffffffu, have);
-      for (int b = 0; b < bits; ++b) {
-        const unsigned set = __ballot_sync(0xffffffffu, d >> b & 1);
-        same[i] &= d >> b & 1 ? set : ~set;
-      }
-      if (have && lane == __ffs(same[i]) - 1) mine[d & ((1u << bits) - 1)] += __popc(same[i]);
-      __syncwarp();
-    }
-  }
-  // Item i's place (of a lane that has one).
-  __device__ __forceinline__ int place(int i, bool have, int shift, int mask, int *mine) const {
-    const int lane = threadIdx.x & 31;
-    const uint32_t d = key[i] >> shift & mask;
-    const int p = have ? mine[d] + __popc(same[i] & ((1u << lane) - 1)) : 0;
-    __syncwarp();
-    if (have && lane == __ffs(same[i]) - 1) mine[d] += __popc(same[i]);
-    __syncwarp();
-    return p;
-  }
 };
+
+// The place of every item of a block in a digit, after the warps before it and those before it in its warp.  cnt: a row
+// of kDigits counters a warp, from counts to the warp's next place.
+template <int kPer>
+__device__ __forceinline__ void count_digits(const SortItems<kPer> &it, int64_t n, int shift, int mask, int *mine) {
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (it.first + 32 * i < n) atomicAdd(mine + (it.key[i] >> shift & mask), 1);  // integers: any order gives the same
+}
+
+// (Voting on each bit of the digit instead of the match, once for the count and the place: 12 -> 15 us for 65,536 ids.)
+__device__ __forceinline__ int take_place(uint32_t d, bool have, int lane, int *mine) {
+  const unsigned same = __match_any_sync(0xffffffffu, have ? d : 0xffffffffu);
+  const int p = have ? mine[d] + __popc(same & ((1u << lane) - 1)) : 0;
+  __syncwarp();
+  if (have && lane == __ffs(same) - 1) mine[d] += __popc(same);
+  __syncwarp();
+  return p;
+}
 
 // An exclusive scan of 256 values by the first 256 threads of a block (all threads call).
 __device__ __forceinline__ int scan_digits(int v, int *sums) {
@@ -110,7 +100,7 @@ __global__ void __launch_bounds__(kSortThreads)
     __syncthreads();
     int *mine = cnt + warp * kDigits;
     const int shift = pass * bits;
-    it.count(n, shift, bits, mine);
+    count_digits(it, n, shift, mask, mine);
     __syncthreads();
     int total = 0;
     if (threadIdx.x < kDigits)
@@ -130,7 +120,7 @@ __global__ void __launch_bounds__(kSortThreads)
 #pragma unroll
     for (int i = 0; i < kSortPer; ++i) {
       const bool have = it.first + 32 * i < n;
-      const int p = it.place(i, have, shift, mask, mine);
+      const int p = take_place(it.key[i] >> shift & mask, have, lane, mine);
       if (have) {
         to_k[p] = it.key[i];
         to_i[p] = id[i];
@@ -180,7 +170,7 @@ __global__ void __launch_bounds__(kSortThreads)
     __syncthreads();
     int *mine = cnt + warp * kDigits;
     const int shift = pass * bits;
-    it.count(n, shift, bits, mine);
+    count_digits(it, n, shift, mask, mine);
     __syncthreads();
     if (d < kDigits) {
       int c = 0;
@@ -215,7 +205,7 @@ __global__ void __launch_bounds__(kSortThreads)
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const bool have = it.first + 32 * i < n;
-      const int p = it.place(i, have, shift, mask, mine);
+      const int p = take_place(it.key[i] >> shift & mask, have, lane, mine);
       if (have) {
         if (!last || passes > 1) to_k[p] = it.key[i];
         to_i[p] = last && it.key[i] >= (uint32_t)nvocab ? -1 : id[i];
@@ -285,7 +275,7 @@ __global__ void __launch_bounds__(kSortThreads)
   }
   __syncthreads();
   int *mine = cnt + warp * kDigits;
-  it.count(n, shift, bits, mine);
+  count_digits(it, n, shift, mask, mine);
   __syncthreads();
   const int d = threadIdx.x;
   int run = scan_digits(d < kDigits ? __ldg(totals + d) : 0, sums);
@@ -302,7 +292,7 @@ __global__ void __launch_bounds__(kSortThreads)
 #pragma unroll
   for (int i = 0; i < kSortPer; ++i) {
     const bool have = it.first + 32 * i < n;
-    const int p = it.place(i, have, shift, mask, mine);
+    const int p = take_place(it.key[i] >> shift & mask, have, lane, mine);
     if (have) {
       to_key[p] = it.key[i];
       to_idx[p] = last && it.key[i] >= (uint32_t)nvocab ? -1 : id[i];
@@ -486,9 +476,9 @@ __global__ void __launch_bounds__(kSumThreads)
   put(rows);
 }
 
-// The runs that chunks cut, eight chunks a block: a run's pieces are added in four parts of neighbouring ones, each in order,
-// and the parts in order.
-constexpr int kJoinSlots = 8, kJoinParts = 4;
+// The runs that chunks cut, four chunks a block: a run's pieces are added in four parts of neighbouring ones, each in
+// order, and the parts in order.  (One part: a run of a tenth of 24,571 tokens, 50 pieces, took 21 us.)
+constexpr int kJoinSlots = 4, kJoinParts = 4;
 template <int V>
 constexpr int kJoinCols = V > 1 ? 1 : 4;
 template <typename A, int V>
@@ -503,10 +493,10 @@ __global__ void __launch_bounds__(kJoinSlots *kJoinParts * 32)
   if (!__syncthreads_or(v >= 0)) return;
   Pack<A, V> sum[kCols] = {};
   if (v >= 0 && v < nvocab) {
-    const int64_t s0 = __ldg(start + v), s1 = min(__ldg(start + v + 1), ntok);
-    const int n = (int)min((s1 - 1) / R, (int64_t)chunks - 1) - chunk + 1, each = (n + kJoinParts - 1) / kJoinParts;  // pieces
+    const int s0 = (int)__ldg(start + v), s1 = (int)min(__ldg(start + v + 1), ntok);  // below 2^31
+    const int n = min((s1 - 1) / R, chunks - 1) - chunk + 1, each = (n + kJoinParts - 1) / kJoinParts;  // pieces
     const int first = which * each, end = min(n, first + each);
-    constexpr int kAhead = 8 / kCols;  // pieces on their way
+    constexpr int kAhead = kCols > 1 ? 4 : 8;  // pieces on their way
     const A *from = part + (int64_t)(chunk + first) * 2 * H + c;
     for (int k = first; k < end; k += kAhead, from += (int64_t)2 * kAhead * H) {
       Pack<A, V> p[kAhead][kCols];
@@ -515,7 +505,7 @@ __global__ void __launch_bounds__(kJoinSlots *kJoinParts * 32)
 #pragma unroll
         for (int u = 0; u < kCols; ++u)
           if (k + i < end && c + 32 * V * u < H)
-            p[i][u] = load_pack<A, V>(from + 32 * V * u + (int64_t)2 * i * H + (k + i == 0 && s0 != (int64_t)chunk * R ? H : 0));
+            p[i][u] = load_pack<A, V>(from + 32 * V * u + (int64_t)2 * i * H + (k + i == 0 && s0 != chunk * R ? H : 0));
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
 #pragma unroll

@@ -56,11 +56,10 @@ struct Eight {
   }
 };
 
-constexpr int kQuantWarps = 4;
 template <typename T>
-constexpr int kQuantEights = 8 / (int)sizeof(T);  // a lane has 64 bytes on their way
+constexpr int kQuantEights = sizeof(T) == 8 ? 2 : 4;  // a lane has 64 (16 bits) or 128 bytes on their way
 
-// A warp takes `part` eights of a token's row; `slices` warps side by side a token, kQuantWarps and more of them in a
+// A warp takes `part` eights of a token's row; `slices` warps side by side a token, about four of them or more in a
 // block.  With pos the row goes to the topk sorted rows pos[t][.], and the rows past the kept ones (src < 0) are cleared.
 // Rows: kExact, whole aligned packs and whole blocks of 64 elements; kWhole, whole aligned packs; kAny.
 // Bound by memory; what it takes in instructions comes second: four elements a lane at a time, with three exchanges of the
@@ -69,12 +68,12 @@ enum QuantRows { kExact, kWhole, kAny };
 template <typename T, QuantRows kRows>
 __global__ void __launch_bounds__(256)
     quant_rows_mx4_kernel(const T *__restrict__ x, const int32_t *__restrict__ src, const int32_t *__restrict__ pos,
-                          int64_t ntok, int topk, int K, int part, int tokens, uint8_t *__restrict__ xq,
+                          int64_t ntok, int topk, int K, int part, int token_bits, uint8_t *__restrict__ xq,
                           uint8_t *__restrict__ sx) {
   constexpr int V = 16 / (int)sizeof(T), kE = kQuantEights<T>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ldq = code_cols(K), lds = scale_cols(K);
-  const int slot = tokens > 1 ? warp % tokens : 0, slice = tokens > 1 ? warp / tokens : (int)(blockIdx.y * (blockDim.x >> 5)) + warp;
-  const int64_t t = (int64_t)blockIdx.x * tokens + slot, n = ntok * topk;
+  const int slice = (int)(blockIdx.y * (blockDim.x >> 5 >> token_bits)) + (warp >> token_bits);
+  const int64_t t = ((int64_t)blockIdx.x << token_bits) + (warp & ((1 << token_bits) - 1)), n = ntok * topk;
   if (t >= ntok) return;
   const int first = slice * part, total = min(part, ldq / 8 - first), count = total - lane;  // of this lane on, 32 apart
   // where the first two pairs go, read beside the row
@@ -680,9 +679,10 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
   const int part = ((eights + slices - 1) / slices + 31) / 32 * 32;  // all lanes of a warp, and whole blocks of 32 elements
   const bool whole = (((uintptr_t)x | (uintptr_t)(K * sizeof(T))) & 15) == 0;
   auto k = !whole ? quant_rows_mx4_kernel<T, kAny> : K % 64 ? quant_rows_mx4_kernel<T, kWhole> : quant_rows_mx4_kernel<T, kExact>;
-  const int tokens = slices < kQuantWarps ? kQuantWarps / slices : 1, warps = slices * tokens < 8 ? slices * tokens : 8;
+  const int token_bits = slices == 1 ? 2 : slices == 2 ? 1 : 0, tokens = 1 << token_bits;  // of a block
+  const int warps = slices * tokens < 8 ? slices * tokens : 8;
   const dim3 grid((unsigned)((ntok + tokens - 1) / tokens), (unsigned)((slices + 7) / 8));
-  k<<<grid, warps * 32, 0, (cudaStream_t)stream>>>(x, src, pos, ntok, topk, K, part, tokens, xq, sx);
+  k<<<grid, warps * 32, 0, (cudaStream_t)stream>>>(x, src, pos, ntok, topk, K, part, token_bits, xq, sx);
   return launch_status(who);
 }
 

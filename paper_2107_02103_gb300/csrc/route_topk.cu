@@ -121,10 +121,21 @@ __device__ __forceinline__ bool groups_too_near(float a, float b, bool sigm) {
   return !(a - b > (sigm ? 0x1p-18f : 0x1p-17f) * (1.0f + fabsf(b)));
 }
 
-// The first step's scores: the short exponential's documented error is 2 + 1.173 |argument| ulp, the short quotient's 2.
+// The first step's scores, by the hardware's base-two exponential (documented error 2^-22, its argument's roundings |x| ulp)
+// and reciprocal (1 ulp).
+__device__ __forceinline__ float rough_exp(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.442695041f));
+  return y;
+}
+__device__ __forceinline__ float rough_rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ float rough_sigmoid(float x) {
-  const float e = __expf(x < 0.0f ? x : -x);
-  return __fdividef(x < 0.0f ? e : 1.0f, 1.0f + e);
+  const float e = rough_exp(-fabsf(x)), r = rough_rcp(1.0f + e);
+  return x < 0.0f ? e * r : r;
 }
 __device__ __forceinline__ float rough_error(float range, bool sigm) {
   return (sigm ? 0x1p-20f : 0x1p-18f) + 0x1p-21f * fminf(range, 128.0f);
@@ -351,7 +362,7 @@ __device__ __forceinline__ bool choose_packed(const TopkArgs &p, int64_t t, unsi
     const int e = i * 32 + lane;
     uint32_t by = to_key(v[i]), c = by;
     if (by_score && e < p.E) {
-      const float b = bias ? __ldg(bias + e) : 0.0f, s = p.sigmoid ? rough_sigmoid(v[i]) : __fdividef(__expf(v[i] - most), total);
+      const float b = bias ? __ldg(bias + e) : 0.0f, s = p.sigmoid ? rough_sigmoid(v[i]) : rough_exp(v[i] - most) * rough_rcp(total);
       c = v[i] == none<float>() || b == none<float>() ? 0u : to_key(s + b);
       by = bias ? c : by;
     }
@@ -706,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, 5) topk_lists_kernel(const __grid_co
     }
   };
   auto bits = [&](float v, float b) {  // the order of c
-    const float s = p.sigmoid ? rough_sigmoid(v) : __fdividef(__expf(v - most), total);
+    const float s = p.sigmoid ? rough_sigmoid(v) : rough_exp(v - most) * rough_rcp(total);
     return v == none<float>() || b == none<float>() ? kNoKey : to_bits(s + b);
   };
   bool lost = false;  // not to be settled here
