@@ -9,7 +9,13 @@ weighted sum, normed, gated and scaled into the residual stream:
     E    = sum_i <u2_i, v>
 
 Two ways through the nets: in f64 or f32 with dp_fitting_* (values, and the gradient dE/du that the forces need), and
-in 8-bit integers (values only: ranking many candidate structures).
+in 8-bit integers or microscaled 4-bit floating point (values only: ranking many candidate structures).
+
+TypedBlock puts in front what nets shared by all types need: the type's embedding in the rows, and a router that chooses
+the experts, both with their gradients:
+
+    u    = D + scale W[type]                                   embed
+    expert, w = the topk of softmax or sigmoid(u R) + bias     router
 
     python examples/expert_fitting.py          # needs a GPU and the built library
 """
@@ -36,6 +42,7 @@ class ExpertBlock:
     v: torch.Tensor  # energy weights [H]
     kind: str = "rms"
     i8: tuple | None = None
+    mx4: tuple | None = None
 
     @classmethod
     def random(cls, seed, nexp, H, hidden, dtype=torch.float64, device="cuda"):
@@ -97,6 +104,63 @@ class ExpertBlock:
         return u2 @ self.v
 
 
+    def quantise4(self):
+        """The nets' weights as 4-bit rows with a power of two for 32 values, once."""
+        H, hidden, _ = self.widths
+        n = self.params.shape[0]
+        W1, b1, W2, b2 = torch.split(self.params, [H * hidden, hidden, hidden * H, H], dim=1)
+        layers = []
+        for W, b, k, m in ((W1, b1, H, hidden), (W2, b2, hidden, H)):
+            q, s = dpc.dp_quant_rows_mx4(W.reshape(n, k, m).transpose(1, 2).reshape(n * m, k).contiguous())
+            layers.append((q.view(n, m, -1), s.view(n, m, -1), b.float().contiguous()))
+        self.mx4 = tuple(layers)
+        return self
+
+    def screen4(self, u, expert, weight, gate=None):
+        """screen() with the nets in microscaled 4-bit floating point."""
+        (q1, s1, b1), (q2, s2, b2) = self.mx4
+        start, src, pos = dpc.dp_route_plan(expert, self.params.shape[0])
+        xq, sx = dpc.dp_quant_rows_mx4(u, src, pos)
+        h = dpc.dp_linear_mx4(xq, sx, q1, s1, b1, start, act="tanh", dtype=u.dtype)
+        hq, sh = dpc.dp_quant_rows_mx4(h)
+        z = dpc.dp_linear_mx4(hq, sh, q2, s2, b2, start, dtype=u.dtype)
+        y = dpc.dp_route_combine(z, pos, weight)
+        _, u2, _ = dpc.dp_norm_gate_fwd(u, y, self.a, self.w1, self.w2, gate=gate, kind=self.kind)
+        return u2 @ self.v
+
+
+@dataclass
+class TypedBlock:
+    """An ExpertBlock behind the embedding of the atoms' types and a router."""
+    block: ExpertBlock
+    W: torch.Tensor  # [ntypes][H]
+    R: torch.Tensor  # router [H][nexp]
+    bias: torch.Tensor | None = None  # balances the experts' loads: chooses, and has no gradient
+    topk: int = 2
+    score: str = "sigmoid"
+    scale: float = 0.5
+
+    def choose(self, D, types):
+        u = dpc.dp_embed_fwd(self.W, types, scale=self.scale, add=D)
+        logits = u @ self.R
+        expert, weight = dpc.dp_route_topk(logits, self.topk, bias=self.bias, score=self.score)
+        return u, logits, expert, weight
+
+    def forward(self, D, types):
+        u, logits, expert, weight = self.choose(D, types)
+        E, saved = self.block.forward(u, expert, weight)
+        return E, (u, types, logits, expert, saved)
+
+    def backward(self, saved):
+        """dE/dD, dE/dW and dE/dR."""
+        u, types, logits, expert, inner = saved
+        du, dweight, _ = self.block.backward(inner)
+        dlogits = dpc.dp_route_topk_grad(logits, expert, dweight, score=self.score)
+        dD = du + dlogits @ self.R.t()  # of u, and so of the rows that the embedding was added to
+        start, src = dpc.dp_embed_plan(types, self.W.shape[0])
+        return dD, dpc.dp_embed_grad(dD, types, start, src, scale=self.scale), u.t() @ dlogits
+
+
 def route(logits, topk):
     """Experts and weights of each atom from the router's logits [nloc][nexp]."""
     top = torch.topk(logits, topk, dim=1)
@@ -128,6 +192,16 @@ def main():
                         (block.params, block.widths, block.a, block.w1, block.w2, block.v))).quantise()
     e8 = low.screen(u.float(), expert, weight.float())
     print(f"in 8-bit integers: E = {float(e8.double().sum()):.6f}")
+    e4 = low.quantise4().screen4(u.float(), expert, weight.float())
+    print(f"in 4-bit floating point: E = {float(e4.double().sum()):.6f}")
+    g = torch.Generator("cuda").manual_seed(3)
+    rn = lambda *s: torch.randn(*s, dtype=torch.float64, device="cuda", generator=g)  # noqa: E731
+    typed = TypedBlock(block, 0.3 * rn(4, u.shape[1]), rn(u.shape[1], 8) / u.shape[1] ** 0.5, bias=0.05 * rn(8))
+    types = (torch.arange(u.shape[0], device="cuda") % 4).to(torch.int32)
+    E, saved = typed.forward(u, types)
+    dD, dW, dR = typed.backward(saved)
+    print(f"with types and a router: E = {float(E):.9f}, |dE/dD| = {float(dD.norm()):.6f}, |dE/dW| = {float(dW.norm()):.6f}, "
+          f"|dE/dR| = {float(dR.norm()):.6f}")
 
 
 if __name__ == "__main__":

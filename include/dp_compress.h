@@ -378,8 +378,8 @@ const char *dp_profile_name(int i);
 
 /*
  * Diagnostic (not part of the paper's method): every wait of the tensor-core
- * GEMM kernels (dp_tabulate_fusion_*_tc_f64, dp_fitting_*_tc_f64, dp_linear_i8_*)
- * and of the norms (dp_norm_gate_*) on an mbarrier is bounded; a CTA (or a warp
+ * GEMM kernels (dp_tabulate_fusion_*_tc_f64, dp_fitting_*_tc_f64, dp_linear_i8_*,
+ * dp_linear_mx4_*) and of the norms (dp_norm_gate_*) on an mbarrier is bounded; a CTA (or a warp
  * with rows of its own) whose wait gives up writes NaN outputs, reads no
  * accumulator and counts one timeout on the device.  This call waits for
  * the device to finish (cudaDeviceSynchronize), writes the count since the
@@ -688,13 +688,14 @@ int dp_tensor_head_grad_f32(const float *T, const float *a, const float *dA, int
 
 /* ------------------------------------------------------------------------
  * Several nets ("experts") over the same atoms: rows of features are sorted
- * by the net they go to and brought back with weights, the nets' layers may
- * run in 8-bit integers where only values are wanted (screening), and the
+ * by the net they go to (which a router chooses) and brought back with weights, the
+ * nets' layers may run in 8-bit integers or 4-bit floating point where only values
+ * are wanted (screening), rows get their atoms' types as embeddings, and the
  * norms around a block are one pass with its gate and residual scale.  The
  * paper's fitting nets are the case of one expert per atom, its type.  The
  * dp_fitting_* calls take the sorted rows of up to DP_MAX_TYPES (8) nets, whose
  * type_start is start copied to the host; more nets, or none of the host's
- * waiting, need the 8-bit product, which has no gradient.
+ * waiting, need the 8-bit or 4-bit product, which have no gradient.
  *
  * Suffixes: rows of f64, f32, bf16 or f16 (the last two as uint16_t bit
  * patterns); weights, scales and sums are f32 (f64 for f64 rows).  Unlike the
@@ -929,7 +930,8 @@ int dp_linear_mx4_f16(const uint8_t *xq, const uint8_t *sx, int64_t rows, int K,
  *   grad  dW[v] = scale sum_t dy[t] over the tokens of v, f32 (f64 rows: f64); every row
  *         is written, or with accumulate the sums are added to what dW holds
  *   work, work_bytes  device scratch, 16-byte aligned, at least the bytes of the two
- *         functions (0: bad arguments; 1: work may be NULL)
+ *         functions (0: bad arguments; 1: work may be NULL); calls that share one, two
+ *         captured ones too, must not overlap on the GPU
  * Every sum has a fixed order.  ntok == 0: start and dW are zero.  Errors: DP_ERR_NULL,
  * DP_ERR_SHAPE (ntok < 0 or 2^31 - 4096 and more, nvocab < 1, H outside [1, 2^20], a scale
  * that is not finite, alignment, a short work buffer), DP_ERR_UNSUPPORTED (nvocab 2^24

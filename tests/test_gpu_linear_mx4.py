@@ -245,3 +245,22 @@ def test_waits_that_give_up(n, K, N, stage):
     if stage == 0:
         assert lost.all()
     assert torch.equal(dpc.dp_linear_mx4(*args), good) and dpc.dp_tc_wait_timeouts() == 0
+
+
+def test_products_on_two_streams_at_once():
+    dpc = lib()
+    cases = []
+    for n, K, N in ((3000, 1088, 700), (500, 2304, 1500)):
+        r = np.random.default_rng(n)
+        code, scale = M.quantise(r.normal(size=(n, K)))
+        args = torch.from_numpy(M.pack(code)).cuda(), torch.from_numpy(scale).cuda(), *weights(n, 1, N, K)[:2]
+        cases.append((args, dpc.dp_linear_mx4(*args), []))
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for st, (args, _, got) in zip(streams, cases):
+            with torch.cuda.stream(st):
+                got.append(dpc.dp_linear_mx4(*args))
+    torch.cuda.synchronize()
+    for _, want, got in cases:
+        assert all(torch.equal(y, want) for y in got)

@@ -98,12 +98,13 @@ def test_choice_and_weights(dtype, T, E, k, G, keep, top, kind, variant):
 
 @pytest.mark.parametrize("dtype", ROWS[1:], ids=IDS[1:])
 @pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
-@pytest.mark.parametrize("G,keep,top", [(1, 1, 1), (4, 2, 2), (4, 2, 1)])
-def test_scores_nearer_than_f32_tells_apart(dtype, kind, G, keep, top):
+@pytest.mark.parametrize("G,keep,top", [(1, 1, 1), (4, 2, 2), (4, 2, 1), (12, 5, 2), (24, 7, 2)])
+@pytest.mark.parametrize("k", [2, 6, 8, 9, 12])
+def test_scores_nearer_than_f32_tells_apart(dtype, kind, G, keep, top, k):
     """A bias of C - s, rounded to f32, makes all scores of a row differ by roundings alone: the choice is still that of
     exact arithmetic.  The reference's own neighbours differ by more than its error (64 bits of mantissa)."""
     dpc = lib()
-    T, E, k = 40, 48, 6
+    T, E = 40, 48
     x, xr = rnd(5, 1, E, dtype=dtype)
     x, xr = x.expand(T, E).contiguous(), np.broadcast_to(xr, (T, E))
     s = scores(xr, kind)[0]
@@ -294,3 +295,48 @@ def test_many_tokens_streams_and_graph():
     xs.copy_(x)
     graph.replay()
     assert torch.equal(out[0], e) and torch.equal(out[1], w) and torch.equal(gout, dx)
+
+
+@pytest.mark.parametrize("E,k", [(60, 3), (200, 8), (1000, 8), (1000, 20), (1024, 64)])
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_f32_logits_that_share_their_upper_bits(E, k, kind, sign):
+    """Neighbouring floats in any order: what a key shortened by the expert's index cannot tell apart, without a bias and
+    with one that is the same for all (scores equal in f32, logits not)."""
+    dpc = lib()
+    r = np.random.default_rng(E + k)
+    v = np.stack([r.permutation(E) for _ in range(50)]).astype(np.float64)
+    x = torch.from_numpy(sign * (1.0 + v * 2.0 ** -23)).float().cuda()
+    want = np.argsort(-sign * v, axis=1)[:, :k]
+    e, _ = dpc.dp_route_topk(x, k, score=kind)
+    assert np.array_equal(e.cpu().numpy(), want)
+    b = torch.full((E,), 0.25, device="cuda")
+    e, _ = dpc.dp_route_topk(x, k, bias=b, score=kind)
+    assert np.array_equal(e.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("T", [1, 3, 4, 5, 15, 16, 17, 33])
+def test_few_close_pairs_among_clear_ones(T):
+    """Two of a token's best scores closer than f32 holds, the others apart: at each place of the order, at its end, and in
+    tokens beside others that need nothing."""
+    dpc = lib()
+    E, k = 40, 5
+    r = np.random.default_rng(T)
+    for place in range(k + 1):
+        c = np.sort(r.uniform(0.2, 0.9, (T, E)), axis=1)[:, ::-1].copy()
+        c[:, :10] += np.linspace(1.0, 0.1, 10)  # clear gaps among the best
+        # a logit's f32 neighbours differ by more than f32 scores near 1 do
+        lo = torch.full((T, E), -3.0)
+        x = lo + 0.1 * torch.from_numpy(r.normal(size=(T, E))).float()
+        b = torch.zeros(E)
+        order_ = r.permutation(E)
+        b[order_] = torch.from_numpy(c[0]).float()
+        x = x[:1].expand(T, E).contiguous()
+        s0 = scores(x.double().numpy(), "sigmoid")[0]
+        # the pair: equal c but for the bias's rounding
+        i, j = order_[place], order_[place + 1]
+        b[j] = float(np.float32(float(s0[i]) + float(b[i]) - float(s0[j])))
+        e, w = dpc.dp_route_topk(x.cuda(), k, bias=b.cuda(), score="sigmoid")
+        re, rw = reference(x.double().numpy(), b.double().numpy(), k, "sigmoid", 1, 1, 1, True, 1.0)
+        assert np.array_equal(e.cpu().numpy(), re), place
+        within(w, rw, np.abs(rw) * weight_bound(x.double().numpy(), E, k, True, torch.float32), "w")

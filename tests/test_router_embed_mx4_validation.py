@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_call_device import OnDevice1, on1
+from test_call_device import OnDevice1, devices, on1  # noqa: F401
 
 
 @pytest.fixture(scope="module")
@@ -169,3 +169,41 @@ def test_reference_quantiser():
     assert list(scale[0]) == [127, 0, 126, 0, 0, 0, 0, 0]
     v = M.values(M.pack(code), scale)
     assert list(v[0, :6]) == [6.0, 0.0, 1.0, 2.0, -4.0, 6.0] and v[0, 64] == 3.0
+
+
+def calls(dpc):
+    i32, i64, u8 = torch.int32, torch.int64, torch.uint8
+    x, w, e, ids = on1(4, 32), on1(4, 2), on1(4, 2, dtype=i32), on1(4, dtype=i32)
+    q, s = on1(4, 32, dtype=u8), on1(4, 8, dtype=u8)
+    plan, work = (on1(9, dtype=i64), ids), on1(1 << 16, dtype=u8)
+    return {
+        "dp_route_topk_f32": lambda: dpc.dp_route_topk(x, 2, out=(e, w)),
+        "dp_route_topk_grad_f32": lambda: dpc.dp_route_topk_grad(x, e, w, out=x),
+        "dp_quant_rows_mx4_f32": lambda: dpc.dp_quant_rows_mx4(x, out=(q, s)),
+        "dp_linear_mx4_f32": lambda: dpc.dp_linear_mx4(q, s, q[None], s[None], out=on1(4, 4)),
+        "dp_embed_plan": lambda: dpc.dp_embed_plan(ids, 8, out=plan),
+        "dp_embed_fwd_f32": lambda: dpc.dp_embed_fwd(on1(8, 32), ids, add=x, out=x),
+        "dp_embed_grad_f32": lambda: dpc.dp_embed_grad(x, ids, *plan, out=on1(8, 32), work=work),
+    }
+
+
+@pytest.mark.parametrize("name", ["dp_route_topk_f32", "dp_route_topk_grad_f32", "dp_quant_rows_mx4_f32", "dp_linear_mx4_f32", "dp_embed_plan",
+                                  "dp_embed_fwd_f32", "dp_embed_grad_f32"])
+@pytest.mark.parametrize("current", [0, 1])
+def test_launches_on_the_tensors_device(dpc, devices, monkeypatch, name, current):  # noqa: F811
+    devices[0] = current
+    seen = []
+    real = getattr(dpc._lib, name)
+
+    def launch(*args):
+        assert len(args) == len(real.argtypes)
+        seen.append((devices[0], getattr(args[-1], "value", args[-1])))
+        return 0
+
+    monkeypatch.setattr(dpc._lib, name, launch)
+    for table in dpc._ROW_FN.values():
+        for t, fn in table.items():
+            if fn is real:
+                monkeypatch.setitem(table, t, launch)
+    calls(dpc)[name]()
+    assert seen == [(1, 101)] and devices[0] == current
