@@ -322,13 +322,15 @@ SortShape sort_shape(int64_t n, int nvocab) {
 // ------------------------------------------------------------------ the rows
 // V elements an access.  Long rows: a warp takes kFwdPart packs a lane of a token's row.  Short ones (Flat, fewer packs than
 // lanes): a thread takes one pack, the packs in order over the tokens.
-constexpr int kFwdThreads = 128, kFwdPart = 2;
+constexpr int kFwdThreads = 128;
+template <int V>
+constexpr int kFwdPart = V > 1 ? 2 : 8;  // accesses of a lane
 template <typename T, int V, bool Flat>
 __global__ void __launch_bounds__(kFwdThreads)
     embed_fwd_kernel(const T *__restrict__ W, const int32_t *__restrict__ ids, int64_t ntok, int nvocab, int H, int np,
                      acc_t<T> scale, const T *add, T *y) {  // y may be add
   using A = acc_t<T>;
-  constexpr int kP = Flat ? 1 : kFwdPart;
+  constexpr int kP = Flat ? 1 : kFwdPart<V>;
   int64_t t;
   int c;
   if constexpr (Flat) {
@@ -391,13 +393,15 @@ __global__ void __launch_bounds__(kSumThreads)
   if ((int64_t)blockIdx.x >= s.blocks) {  // (in turn with the others instead: 48 -> 56 us for 24,571 x 1003 f16 to 30,011 rows)
     const int64_t v0 = ((int64_t)blockIdx.x - s.blocks) * kClearRows;
     const int lane = threadIdx.x & 31;
-    const int64_t at = v0 + lane < nvocab ? __ldg(start + v0 + lane) : 0, end = v0 + lane < nvocab ? __ldg(start + v0 + lane + 1) : 1;
+    const bool in = v0 + lane < nvocab;
+    const int64_t at = in ? __ldg(start + v0 + lane) : 0, end = in ? __ldg(start + v0 + lane + 1) : 1;
     unsigned empty = __ballot_sync(0xffffffffu, at == end);
     for (int n = 0; empty; empty &= empty - 1, ++n)
       if (n % (int)(blockDim.x / 32) == (int)threadIdx.x / 32) {
         A *row = dW + (v0 + __ffs(empty) - 1) * H;
         if ((((uintptr_t)dW | (uintptr_t)(H * sizeof(A))) & 15) == 0) {
-          for (int c = lane; c < H / (16 / (int)sizeof(A)); c += 32) reinterpret_cast<uint4 *>(row)[c] = make_uint4(0, 0, 0, 0);
+          for (int c = lane; c < H / (16 / (int)sizeof(A)); c += 32)
+            reinterpret_cast<uint4 *>(row)[c] = make_uint4(0, 0, 0, 0);
         } else {
           for (int c = lane; c < H; c += 32) row[c] = A(0);
         }
@@ -438,7 +442,8 @@ __global__ void __launch_bounds__(kSumThreads)
       for (int u = 0; u < kCols; ++u, to += step)
         if (kCols == 1 || c + u * step < H)
 #pragma unroll
-          for (int l = 0; l < V; ++l) to[l] = is_cut ? sum[u][l] : accumulate ? fma(scale, sum[u][l], to[l]) : scale * sum[u][l];
+          for (int l = 0; l < V; ++l)
+            to[l] = is_cut ? sum[u][l] : accumulate ? fma(scale, sum[u][l], to[l]) : scale * sum[u][l];
     }
 #pragma unroll
     for (int u = 0; u < kCols; ++u)
@@ -584,11 +589,12 @@ int embed_fwd(const T *W, const int32_t *ids, int64_t ntok, int nvocab, int H, d
   const int np = whole ? H / V : H;
   const bool flat = np < 32;
   const int64_t bx = flat ? (ntok * np + kFwdThreads - 1) / kFwdThreads : (ntok + kFwdThreads / 32 - 1) / (kFwdThreads / 32);
-  const int by = flat ? 1 : (np + 32 * kFwdPart - 1) / (32 * kFwdPart);
+  const int part = 32 * (whole ? kFwdPart<V> : kFwdPart<1>), by = flat ? 1 : (np + part - 1) / part;
   if (bx > 0x7fffffffLL || by > 65535) return set_error(DP_ERR_SHAPE, "%s: %lld rows of %d", who, (long long)ntok, H);
   auto k = flat ? (whole ? embed_fwd_kernel<T, V, true> : embed_fwd_kernel<T, 1, true>)
                 : (whole ? embed_fwd_kernel<T, V, false> : embed_fwd_kernel<T, 1, false>);
-  k<<<dim3((unsigned)bx, (unsigned)by), kFwdThreads, 0, (cudaStream_t)stream>>>(W, ids, ntok, nvocab, H, np, (acc_t<T>)scale, add, y);
+  k<<<dim3((unsigned)bx, (unsigned)by), kFwdThreads, 0, (cudaStream_t)stream>>>(W, ids, ntok, nvocab, H, np,
+                                                                                     (acc_t<T>)scale, add, y);
   return launch_status(who);
 }
 
@@ -617,14 +623,16 @@ int embed_grad(const T *dy, const int32_t *ids, const int64_t *start, const int3
   A *part = (A *)work;
   int *cut = s.chunks ? (int *)(part + part_chunks(ntok, H, sizeof(T)) * 2 * H) : nullptr;
   auto k = whole ? embed_grad_kernel<T, V> : embed_grad_kernel<T, 1>;
-  k<<<(unsigned)blocks, s.groups * s.width, 0, st>>>(dy, ids, start, src, ntok, nvocab, H, s, (A)scale, accumulate != 0, dW, part, cut);
+  k<<<(unsigned)blocks, s.groups * s.width, 0, st>>>(dy, ids, start, src, ntok, nvocab, H, s, (A)scale,
+                                                      accumulate != 0, dW, part, cut);
   if (s.chunks > 1) {
     constexpr int VA = 16 / (int)sizeof(A);
     const bool packs = pack_width<A>(H, dW) >= VA;
     const int cols = 32 * (packs ? VA : kJoinCols<1>);  // of a block
     const dim3 grid((s.chunks + kJoinSlots - 1) / kJoinSlots, (H + cols - 1) / cols);
     auto join = packs ? embed_join_kernel<A, VA> : embed_join_kernel<A, 1>;
-    join<<<grid, kJoinSlots * kJoinParts * 32, 0, st>>>(start, ntok, nvocab, H, s.R, s.chunks, (A)scale, accumulate != 0, dW, part, cut);
+    join<<<grid, kJoinSlots * kJoinParts * 32, 0, st>>>(start, ntok, nvocab, H, s.R, s.chunks, (A)scale,
+                                                          accumulate != 0, dW, part, cut);
   }
   return launch_status(who);
 }
@@ -677,7 +685,8 @@ int dp_embed_plan(const int32_t *ids, int64_t ntok, int nvocab, int64_t *start, 
     uint32_t *keys = (uint32_t *)work;
     cudaLaunchKernelEx(&cfg, k, ids, (int)ntok, nvocab, s.passes, s.bits, keys, (int *)work + 2 * ntok, start, src);
     if (s.passes > 1 && nvocab > kClusterStart)
-      embed_start_kernel<<<(nvocab + 256) / 256, 256, 0, st>>>(keys + (int64_t)((s.passes - 1) & 1) * ntok, (int)ntok, nvocab, start);
+      embed_start_kernel<<<(nvocab + 256) / 256, 256, 0, st>>>(keys + (int64_t)((s.passes - 1) & 1) * ntok, (int)ntok,
+                                                                 nvocab, start);
     return launch_status(who);
   }
   uint32_t *keys[2] = {(uint32_t *)work, (uint32_t *)work + ntok};

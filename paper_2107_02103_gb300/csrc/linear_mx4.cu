@@ -3,7 +3,8 @@
 //   amax = max_k |x_k|,  e = max(floor(log2 amax) - 2, -127),  q_k = the nearest of 0, .5, 1, 1.5, 2, 3, 4, 6 (and their
 //   negatives) to x_k 2^-e, ties to the even code, 6 for what lies above (amax 2^-e is below 8);  x_k ~ q_k 2^e
 //   y_in = act(sum_b 2^(e_ib + e_nb) sum_(k in b) q_ik w_nk + b_n)
-// Codes are sign, two exponent bits, one mantissa bit, two a byte with the lower four bits first; a scale is e + 127 in a byte.
+// Codes are sign, two exponent bits, one mantissa bit, two a byte with the lower four bits first; a
+// scale is e + 127 in a byte.
 #include <cuda.h>
 
 #include "rows.cuh"
@@ -213,7 +214,8 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
   }
   const int nb = p.K / kBlock, lds = scale_cols(p.K);
   const int64_t c = (int64_t)e * p.N + n;
-  const uint4 *w = reinterpret_cast<const uint4 *>(p.wq + c * (p.K / 2)), *x = reinterpret_cast<const uint4 *>(p.xq + (int64_t)r0 * (p.K / 2));
+  const uint4 *w = reinterpret_cast<const uint4 *>(p.wq + c * (p.K / 2));
+  const uint4 *x = reinterpret_cast<const uint4 *>(p.xq + (int64_t)r0 * (p.K / 2));
   float acc[kFewRows] = {};
   for (int b = lane; b < nb; b += 32) {
     const Block32 wb(__ldg(w + b));
@@ -273,8 +275,10 @@ struct Shape {
   static constexpr int kPlaces = 3;
   static constexpr uint32_t kStageCols = 2 * (kColsA + kColsB), kPlaceCols = 2 * kStageCols, kScaleAt = 2 * TN;
   static constexpr uint32_t kTmemCols = TN > 64 ? 512 : 256;
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 2 * kGroup * kScaleBytes + (2 * kStages + kPlaces + 9) * 8 + 16;  // aligned within
-  static_assert(kStageBytes % 1024 == 0 && kSmem <= 227 * 1024 && TN % 32 == 0 && kScaleAt + kPlaces * kPlaceCols <= kTmemCols, "tile");
+  static constexpr int kBarriers = 2 * kStages + kPlaces + 9;
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 2 * kGroup * kScaleBytes + kBarriers * 8 + 16;
+  static_assert(kStageBytes % 1024 == 0 && kSmem <= 227 * 1024 && TN % 32 == 0, "tile");
+  static_assert(kScaleAt + kPlaces * kPlaceCols <= kTmemCols, "accumulators and scales");
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -421,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           turn ^= 1;
         }
         for (int i = 0; i < n; ++i, ++j) {
-          const uint64_t a = a_at + (uint64_t)(st * (S::kStageBytes >> 4)), b = b_at + (uint64_t)(st * (S::kStageBytes >> 4));
+          const uint64_t place_of = (uint64_t)(st * (S::kStageBytes >> 4)), a = a_at + place_of, b = b_at + place_of;
           const uint32_t tai = ta + i * S::kStageCols;
           if (leader) {
             if ((kb + i + 1) * kKB <= p.K) {
@@ -488,7 +492,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t room = smem_u32(scale_room), to0 = room + s * S::kScaleBytes + row * 16;
     const uint32_t quadrant = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + S::kScaleAt;
     auto all_wait = [&](uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
-    int j = 0, place = 0, last0 = -1, last1 = -1, last2 = -1;  // the stage, the pair's place; the last stages of the pairs before, the latest first
+    int j = 0, place = 0;                      // the stage, the pair's place
+    int last0 = -1, last1 = -1, last2 = -1;    // the last stages of the pairs before, the latest first
     static_assert(S::kPlaces == 3, "as many pairs before");
     for (; ok && t.have; ++group) {
       const int buf = group & 1;
@@ -519,7 +524,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint4 w[2 * kBlocks];
 #pragma unroll
         for (int b = 0; b < 2 * kBlocks; ++b)  // of a last stage alone: what lay there before, for columns that are not read
-          asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[b].x), "=r"(w[b].y), "=r"(w[b].z), "=r"(w[b].w) : "r"(from + b * 512));
+          asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                       : "=r"(w[b].x), "=r"(w[b].y), "=r"(w[b].z), "=r"(w[b].w)
+                       : "r"(from + b * 512));
         const int n = min(2, stages - i);
         if (last2 >= 0) ok = all_wait(empty + last2 % S::kStages, last2 / S::kStages & 1);  // the place's MMAs are through
         if (!ok) break;
@@ -527,8 +534,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t at = quadrant + place * S::kPlaceCols;
 #pragma unroll
         for (int b = 0; b < 2 * kBlocks; ++b) {
-          const int in = b % kBlocks;  // A of both 128 of K, then B's blocks of both
-          const uint32_t cols = in < 2 ? S::kColsA : (in - 2) % S::kBlocksB < S::kBlocksB - 1 ? 4 : S::kColsB - 4 * (S::kBlocksB - 1);
+          const int in = b % kBlocks;  // A of both 128 of K, then B's blocks of both, the last of them as far as TN goes
+          const bool whole = in < 2 || (in - 2) % S::kBlocksB < S::kBlocksB - 1;
+          const uint32_t cols = whole ? 4 : S::kColsB - 4 * (S::kBlocksB - 1);
           if (cols == 4) tmem_st(at, w[b]);
           else tmem_st2(at, w[b]);
           at += cols;
@@ -678,7 +686,9 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
   const int eights = code_cols(K) / 8, most = 32 * kQuantEights<T>, slices = (eights + most - 1) / most;
   const int part = ((eights + slices - 1) / slices + 31) / 32 * 32;  // all lanes of a warp, and whole blocks of 32 elements
   const bool whole = (((uintptr_t)x | (uintptr_t)(K * sizeof(T))) & 15) == 0;
-  auto k = !whole ? quant_rows_mx4_kernel<T, kAny> : K % 64 ? quant_rows_mx4_kernel<T, kWhole> : quant_rows_mx4_kernel<T, kExact>;
+  auto k = !whole   ? quant_rows_mx4_kernel<T, kAny>
+           : K % 64 ? quant_rows_mx4_kernel<T, kWhole>
+                    : quant_rows_mx4_kernel<T, kExact>;
   const int token_bits = slices == 1 ? 2 : slices == 2 ? 1 : 0, tokens = 1 << token_bits;  // of a block
   const int warps = slices * tokens < 8 ? slices * tokens : 8;
   const dim3 grid((unsigned)((ntok + tokens - 1) / tokens), (unsigned)((slices + 7) / 8));

@@ -94,6 +94,9 @@ __device__ __forceinline__ A sigmoid(A x) {
 template <typename A>
 __device__ __forceinline__ A none() { return -A(INFINITY); }
 
+// s of a logit, from the row's largest and the sum of exp(x - most) for a softmax.
+template <typename A>
+__device__ __forceinline__ A score_of(A x, bool sigm, A most, A total) { return sigm ? sigmoid(x) : exp_(x - most) / total; }
 // Scores of chosen logits up to a factor common to the row that keeps their sum from underflowing: for a softmax
 // exp(x - m), for a sigmoid s exp(-m) with m = min(0, largest x).
 template <typename A>
@@ -108,10 +111,13 @@ __device__ __forceinline__ A relative_score(A x, A most, bool sigm) {
 //   sigmoid  2 of the exponential, its product with the reciprocal, that and 1 + e: below 4
 //   softmax  2, the argument's rounding 0.5 range, the quotient; the total: its terms' 2 and their arguments' roundings
 //            (in the mean below 4), and (32 + 5) / 2 of its additions: below 28 + 0.5 range
-__device__ __forceinline__ float score_error(float range, bool sigm) { return sigm ? 0x1p-21f : 0x1p-18f + 0x1p-24f * fminf(range, 128.0f); }
+__device__ __forceinline__ float score_error(float range, bool sigm) {
+  return sigm ? 0x1p-21f : 0x1p-18f + 0x1p-24f * fminf(range, 128.0f);
+}
 // Two scores that f32 cannot order: x the logits, b the biases (c = s + b), range the larger |argument|.  Equal inputs
 // give equal scores; else s <= |c| + |b|, and the sum's own rounding is half an ulp.
-__device__ __forceinline__ bool too_near(float c0, float c1, float x0, float x1, float b0, float b1, float range, bool sigm) {
+__device__ __forceinline__ bool too_near(float c0, float c1, float x0, float x1, float b0, float b1, float range,
+                                         bool sigm) {
   if (x0 == x1 && b0 == b1) return false;
   return !(c0 - c1 > (score_error(range, sigm) + 0x1p-23f) * (fabsf(c0) + fabsf(c1) + fabsf(b0) + fabsf(b1)));
 }
@@ -141,8 +147,14 @@ __device__ __forceinline__ float rough_error(float range, bool sigm) {
   return (sigm ? 0x1p-20f : 0x1p-18f) + 0x1p-21f * fminf(range, 128.0f);
 }
 // A key with the index of its expert in the low bits (mask: all of them), the lower index the larger; 0 stays 0.
-__device__ __forceinline__ uint32_t pack_key(uint32_t key, uint32_t mask, int e) { return key ? (key & ~mask) | (mask - e) : 0u; }
+__device__ __forceinline__ uint32_t pack_key(uint32_t key, uint32_t mask, int e) {
+  return key ? (key & ~mask) | (mask - e) : 0u;
+}
 __device__ __forceinline__ int packed_expert(uint32_t key, uint32_t mask) { return key ? (int)(mask - (key & mask)) : -1; }
+// The size of the exponential's argument in a score.
+__device__ __forceinline__ float range_of(float x0, float x1, float most, bool sigm) {
+  return sigm ? fmaxf(fabsf(x0), fabsf(x1)) : most - fminf(x0, x1);
+}
 // Neighbours of the packed order that it may have wrong: their cut scores as intervals.
 __device__ __forceinline__ bool packed_near(uint32_t k0, uint32_t k1, uint32_t mask, float x0, float x1, float b0, float b1,
                                             float range, bool sigm) {
@@ -310,7 +322,7 @@ __device__ bool choose(const TopkArgs &p, int64_t t, unsigned char *room) {
   }
 #pragma unroll
   for (int s = 0; s < S; ++s) {
-    ws[s] = se[s] < 0 ? A(0) : p.renorm ? relative_score(sx[s], top, p.sigmoid) : p.sigmoid ? sigmoid(sx[s]) : exp_(sx[s] - most) / total;
+    ws[s] = se[s] < 0 ? A(0) : p.renorm ? relative_score(sx[s], top, p.sigmoid) : score_of(sx[s], p.sigmoid, most, total);
     if (p.renorm) wsum += ws[s];
   }
   // total * 0: a NaN or +inf anywhere makes every score of a softmax NaN, also where the chosen logits are numbers
@@ -362,7 +374,8 @@ __device__ __forceinline__ bool choose_packed(const TopkArgs &p, int64_t t, unsi
     const int e = i * 32 + lane;
     uint32_t by = to_key(v[i]), c = by;
     if (by_score && e < p.E) {
-      const float b = bias ? __ldg(bias + e) : 0.0f, s = p.sigmoid ? rough_sigmoid(v[i]) : rough_exp(v[i] - most) * rough_rcp(total);
+      const float b = bias ? __ldg(bias + e) : 0.0f;
+      const float s = p.sigmoid ? rough_sigmoid(v[i]) : rough_exp(v[i] - most) * rough_rcp(total);
       c = v[i] == none<float>() || b == none<float>() ? 0u : to_key(s + b);
       by = bias ? c : by;
     }
@@ -456,7 +469,8 @@ __device__ __forceinline__ bool choose_packed(const TopkArgs &p, int64_t t, unsi
         if (lane == 31) nk = 0;
       }
       if (s * 32 + lane < p.k && sk[s] != 0 && nk != 0) {
-        if (bias) near |= packed_near(sk[s], nk, mask, sx[s], nx, b[s], nb, p.sigmoid ? fmaxf(fabsf(sx[s]), fabsf(nx)) : most - fminf(sx[s], nx), p.sigmoid);
+        const float range = range_of(sx[s], nx, most, p.sigmoid);
+        if (bias) near |= packed_near(sk[s], nk, mask, sx[s], nx, b[s], nb, range, p.sigmoid);
         else near |= ((sk[s] ^ nk) & ~mask) == 0 && sx[s] != nx;
       }
     }
@@ -475,7 +489,7 @@ __device__ __forceinline__ bool choose_packed(const TopkArgs &p, int64_t t, unsi
   }
 #pragma unroll
   for (int s = 0; s < S; ++s) {
-    ws[s] = se[s] < 0 ? 0.0f : p.renorm ? relative_score(sx[s], top, p.sigmoid) : p.sigmoid ? sigmoid(sx[s]) : expf(sx[s] - most) / total;
+    ws[s] = se[s] < 0 ? 0.0f : p.renorm ? relative_score(sx[s], top, p.sigmoid) : score_of(sx[s], p.sigmoid, most, total);
     if (p.renorm) wsum += ws[s];
   }
   if (p.renorm) wsum = sum_over<32>(kAll, wsum) + (by_score ? total * 0.0f : 0.0f);  // as in choose()
@@ -574,8 +588,8 @@ __device__ __forceinline__ unsigned long long exact_key(const TopkArgs &p, const
 // The groups to keep of a token: those surely above the border stay, the ones near it (up to eight) by their exact
 // scores.  gkey: the groups' f32 scores, a, b: those of the last one kept and the first one dropped.  False: too many.
 template <typename T>
-__device__ __noinline__ bool settle_groups(const TopkArgs &p, const T *x, const uint32_t *gkey, uint32_t *kept, float a, float b,
-                                           float most, unsigned m8) {
+__device__ __noinline__ bool settle_groups(const TopkArgs &p, const T *x, const uint32_t *gkey, uint32_t *kept, float a,
+                                           float b, float most, unsigned m8) {
   const int sub = threadIdx.x % 8, per = p.E / p.G;
   const double total = p.sigmoid ? 1.0 : exact_total(x, p.E, most, m8);
   const float tol = 0x1p-16f * (1.0f + fabsf(b));
@@ -619,10 +633,13 @@ __device__ __noinline__ bool settle_groups(const TopkArgs &p, const T *x, const 
 // The list's experts and the best beyond it in their exact order: lane j's e (-1: none) becomes the j-th.  left: the two
 // best packed keys beyond the list.  False: the second of them may belong to the first k.
 template <typename T>
-__device__ __noinline__ bool settle_list(const TopkArgs &p, const T *x, int &e, uint32_t left0, uint32_t left1, float most, unsigned m8) {
+__device__ __noinline__ bool settle_list(const TopkArgs &p, const T *x, int &e, uint32_t left0, uint32_t left1, float most,
+                                         unsigned m8) {
   const int sub = threadIdx.x % 8;
   const double total = p.sigmoid || !p.bias ? 1.0 : exact_total(x, p.E, most, m8);
-  auto exact = [&](int of) { return of < 0 ? 0ull : p.bias ? exact_key(p, x, of, most, total) : to_key((double)to_acc(x[of])); };
+  auto exact = [&](int of) {
+    return of < 0 ? 0ull : p.bias ? exact_key(p, x, of, most, total) : to_key((double)to_acc(x[of]));
+  };
   const int e9 = left0 > kNoKey ? (int)(p.mask - (left0 & p.mask)) : -1;
   const unsigned long long key = exact(e), key9 = exact(e9);
   const bool after9 = key9 > key || (key9 == key && key9 && e9 < e);
@@ -658,7 +675,7 @@ __device__ __noinline__ bool settle_list(const TopkArgs &p, const T *x, int &e, 
 __host__ __device__ constexpr int list_words(int E, int G) { return (E + E / 8 + 1 + 2 * G) | 1; }
 
 template <typename T, bool Whole>
-__global__ void __launch_bounds__(kThreads, 5) topk_lists_kernel(const __grid_constant__ TopkArgs p) {
+__global__ void __launch_bounds__(kThreads, 8) topk_lists_kernel(const __grid_constant__ TopkArgs p) {
   extern __shared__ __align__(16) unsigned char rooms[];
   constexpr int V = 16 / (int)sizeof(T);
   const int sub = threadIdx.x % 8, slot = threadIdx.x / 8;
@@ -812,7 +829,8 @@ __global__ void __launch_bounds__(kThreads, 5) topk_lists_kernel(const __grid_co
     if (sub < p.k && e >= 0 && next > kNoKey) {
       const int en = (int)(mask - (next & mask));
       const float xn = to_acc(x[en]);
-      if (bias) near = packed_near(key, next, mask, xe, xn, __ldg(bias + e), __ldg(bias + en), p.sigmoid ? fmaxf(fabsf(xe), fabsf(xn)) : most - fminf(xe, xn), p.sigmoid);
+      const float range = range_of(xe, xn, most, p.sigmoid);
+      if (bias) near = packed_near(key, next, mask, xe, xn, __ldg(bias + e), __ldg(bias + en), range, p.sigmoid);
       else near = ((key ^ next) & ~mask) == 0 && xe != xn;
     }
     if (__ballot_sync(kAll, near) & m8) {
@@ -824,7 +842,7 @@ __global__ void __launch_bounds__(kThreads, 5) topk_lists_kernel(const __grid_co
   const bool have = sub < p.k && e >= 0;
   if (!have) xe = none<float>();
   const float top = p.renorm ? most_over<8>(kAll, xe) : 0.0f;
-  const float w = !have ? 0.0f : p.renorm ? relative_score(xe, top, p.sigmoid) : p.sigmoid ? sigmoid(xe) : expf(xe - most) / total;
+  const float w = !have ? 0.0f : p.renorm ? relative_score(xe, top, p.sigmoid) : score_of(xe, p.sigmoid, most, total);
   const float sum = p.renorm ? sum_over<8>(kAll, w) + (by_score ? total * 0.0f : 0.0f) : 1.0f;  // as in choose()
   const unsigned unsure = __ballot_sync(kAll, lost && mine);
   if (mine && sub < p.k && !lost) {
@@ -1032,7 +1050,8 @@ int topk(const T *x, const acc_t<T> *bias, int64_t ntok, int E, int k, int score
       const bool whole = (((uintptr_t)x | (uintptr_t)(E * sizeof(T))) & 15) == 0;
       auto kernel = whole ? topk_lists_kernel<T, true> : topk_lists_kernel<T, false>;
       const size_t smem = keep < G ? (size_t)tok * list_words(E, G) * 4 : 0;
-      if (smem > 48 * 1024 && (rc = allow_smem((const void *)kernel, (size_t)tok * list_words(kMaxExperts, kMaxExperts / 2) * 4, who))) return rc;
+      constexpr size_t most = (size_t)tok * list_words(kMaxExperts, kMaxExperts / 2) * 4;
+      if (smem > 48 * 1024 && (rc = allow_smem((const void *)kernel, most, who))) return rc;
       kernel<<<(unsigned)((ntok + tok - 1) / tok), kThreads, smem, st>>>(p);
       return launch_status(who);
     }
@@ -1040,7 +1059,8 @@ int topk(const T *x, const acc_t<T> *bias, int64_t ntok, int E, int k, int score
     constexpr int N = decltype(N_)::value, S = decltype(S_)::value, tok = kThreads / 32;
     const size_t smem = keep < G ? (size_t)tok * room_words(E, G) * 8 : 0;
     auto kernel = topk_kernel<T, N, S>;
-    if (smem > 48 * 1024 && (rc = allow_smem((const void *)kernel, (size_t)tok * room_words(32 * N, 16 * N) * 8, who))) return;
+    constexpr size_t most = (size_t)tok * room_words(32 * N, 16 * N) * 8;
+    if (smem > 48 * 1024 && (rc = allow_smem((const void *)kernel, most, who))) return;
     kernel<<<(unsigned)((ntok + tok - 1) / tok), kThreads, smem, st>>>(p);
   };
   using std::integral_constant;
@@ -1068,7 +1088,8 @@ int topk_grad(const T *x, const int32_t *expert, const acc_t<T> *dw, int64_t nto
   if (!at_elements(x, dx) || !at_elements(expert) || !at_elements(dw)) return misaligned(who);
   const TopkGradArgs p{x, expert, dw, ntok, E, k, score == DP_SCORE_SIGMOID, renorm != 0, scale, dx};
   if (renorm || score == DP_SCORE_SIGMOID) {
-    const int most = 8192 / (int)sizeof(acc_t<T>) / E, tokens = most >= 32 ? 32 : most >= 8 ? most / 8 * 8 : most < 1 ? 1 : most;
+    const int most = 8192 / (int)sizeof(acc_t<T>) / E;  // tokens of a tile of 8 KB
+    const int tokens = most >= 32 ? 32 : most >= 8 ? most / 8 * 8 : most < 1 ? 1 : most;
     const size_t smem = (size_t)(tokens * E + 15) / 16 * 16 * sizeof(acc_t<T>) * 2;
     constexpr int V = 16 / (int)sizeof(T);
     // a warp's tile begins at whole packs
