@@ -16,7 +16,7 @@ namespace {
 constexpr int kMaxVocab = (1 << 24) - 1, kMaxH = 1 << 20;
 
 // ------------------------------------------------------------------ the plan: a stable radix sort of the ids
-// Up to 4096 ids in one block, up to 65,536 in a cluster of up to eight blocks that read one another's counts (one launch
+// Up to 4096 tokens in one block, up to 65,536 in a cluster of up to eight blocks that read one another's counts (one launch
 // either way), more in three launches a digit.
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortPer = 4, kSortBlock = kSortThreads * kSortPer;
 constexpr int kDigits = 256;
@@ -320,6 +320,9 @@ SortShape sort_shape(int64_t n, int nvocab) {
   s.blocks = (int)((n + kSortBlock - 1) / kSortBlock);
   return s;
 }
+
+// Whether one block does it all, start included: not where there are many more ids than its threads can search for.
+bool plan_is_small(int64_t ntok, int nvocab) { return ntok == 0 || (ntok <= kSortBlock && nvocab <= kClusterStart); }
 
 // ------------------------------------------------------------------ the rows
 // V elements an access.  Long rows: a warp takes kFwdPart packs a lane of a token's row.  Short ones (Flat, fewer packs than
@@ -647,7 +650,7 @@ extern "C" {
 size_t dp_embed_plan_work_bytes(int64_t ntok, int nvocab) {
   if (ntok < 0 || ntok > 0x7fffffffLL - dpc::kSortBlock || nvocab < 1 || nvocab > dpc::kMaxVocab) return 0;
   const dpc::SortShape s = dpc::sort_shape(ntok, nvocab);
-  if (s.blocks <= 1) return 1;
+  if (dpc::plan_is_small(ntok, nvocab)) return 1;
   return ((size_t)ntok * 4 + (size_t)(s.blocks + 1) * dpc::kDigits) * sizeof(int);
 }
 
@@ -662,7 +665,7 @@ int dp_embed_plan(const int32_t *ids, int64_t ntok, int nvocab, int64_t *start, 
   if (!at_elements(ids, src) || !at_elements(start)) return misaligned(who);
   const SortShape s = sort_shape(ntok, nvocab);
   const cudaStream_t st = (cudaStream_t)stream;
-  if (s.blocks <= 1) {
+  if (plan_is_small(ntok, nvocab)) {
     rc = allow_smem((const void *)embed_plan_small_kernel, kSmallSmem, who);
     if (rc) return rc;
     embed_plan_small_kernel<<<1, kSortThreads, kSmallSmem, st>>>(ids, (int)ntok, nvocab, s.passes, s.bits, start, src);
