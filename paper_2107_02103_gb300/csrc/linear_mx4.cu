@@ -266,7 +266,8 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
 // what bounds it are the barriers between the roles.  Without the copies of codes 269 us, without the output 269.
 namespace mx4 {
 constexpr int kTM = 128, kKB = 256, kRowBytes = kKB / 2;
-constexpr int kEpiWarps = 8, kScaleWarps = 4, kCopyWarp = kEpiWarps + kScaleWarps, kMmaWarp = kCopyWarp + 1;
+constexpr int kEpiWarps = 8, kScaleWarps = 4, kScaleSets = 2;
+constexpr int kCopyWarp = kEpiWarps + kScaleWarps * kScaleSets, kMmaWarp = kCopyWarp + 1;
 constexpr int kThreads = (kMmaWarp + 1) * 32;
 constexpr int kGroup = 4;  // stages whose scales come together
 
@@ -478,9 +479,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp >= kEpiWarps) {
     // ---------------------------------------------------------------- the scales
     constexpr int kRA = kTM / 32, kRB = TN / 32;  // rows of a thread
-    const int at = threadIdx.x - kEpiWarps * 32, row = at / 4, s = at % 4, lds = scale_cols(p.K);
+    const int set = (warp - kEpiWarps) / kScaleWarps, at = threadIdx.x - (kEpiWarps + set * kScaleWarps) * 32;
+    const int row = at / 4, s = at % 4, lds = scale_cols(p.K);
     Tile t{(int)blockIdx.x, 0, 0, 0, 0, false};
-    int kb = 0, group = 0;
+    int kb = 0;
     uint2 v[kRA + kRB];
     auto read = [&] {  // of stage kb + s
       const uint8_t *a = p.sw + ((int64_t)t.e * p.N + t.n0 + row) * lds, *b = p.sx + (int64_t)(t.r0 + row) * lds;
@@ -492,19 +494,40 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (r < (i < kRA ? na : nb)) v[i] = __ldg(reinterpret_cast<const uint2 *>((i < kRA ? a : b) + (int64_t)r * lds + k));
       }
     };
+    // the groups of four stages go to the two sets of warps in turn, each with a place of its own in shared memory
+    int j = 0, place = 0;                    // the stage, its pair's place in tensor memory
+    int last0 = -1, last1 = -1, last2 = -1;  // the last stages of the pairs before, the latest first
+    static_assert(S::kPlaces == 3 && kScaleSets == 2, "as many pairs before; a place a set");
+    auto next_pair = [&](int n) {
+      if (++place == S::kPlaces) place = 0;
+      j += n;
+      last2 = last1;
+      last1 = last0;
+      last0 = j - 1;
+    };
+    auto next_group = [&] {
+      kb += kGroup;
+      if (kb >= nkb) {
+        kb = 0;
+        t.tile += gridDim.x;
+        seek_work(p, TN, nct, t);
+      }
+    };
+    auto skip_group = [&] {  // the other set's
+      if (!t.have) return;
+      const int stages = min(kGroup, nkb - kb);
+      for (int i = 0; i < stages; i += 2) next_pair(min(2, stages - i));
+      next_group();
+    };
     seek_work(p, TN, nct, t);
+    if (set) skip_group();
     if (t.have) read();
-    const uint32_t room = smem_u32(scale_room), to0 = room + s * S::kScaleBytes + row * 16;
+    const uint32_t room = smem_u32(scale_room) + set * kGroup * S::kScaleBytes, to = room + s * S::kScaleBytes + row * 16;
     const uint32_t quadrant = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + S::kScaleAt;
     auto all_wait = [&](uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
-    int j = 0, place = 0;                      // the stage, the pair's place
-    int last0 = -1, last1 = -1, last2 = -1;    // the last stages of the pairs before, the latest first
-    static_assert(S::kPlaces == 3, "as many pairs before");
-    for (; ok && t.have; ++group) {
-      const int buf = group & 1;
-      ok = all_wait(unstaged + buf, (group >> 1 & 1) ^ 1);  // the four warps have read what lay there
+    for (uint32_t turn = 0; ok && t.have; turn ^= 1) {
+      ok = all_wait(unstaged + set, turn ^ 1);  // the set's warps have read what lay there
       if (!ok) break;
-      const uint32_t to = to0 + buf * kGroup * S::kScaleBytes;
 #pragma unroll
       for (int i = 0; i < kRA + kRB; ++i) {  // row r of an operand: block r / 128 of each 128 of K, word r / 32 % 4
         const int q = i < kRA ? i : i - kRA, nblk = i < kRA ? 1 : S::kBlocksB;
@@ -513,18 +536,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("st.shared.b32 [%0], %1;" ::"r"(d + 512 * nblk), "r"(v[i].y) : "memory");
       }
       __syncwarp();
-      if (lane == 0) arrive(smem_u32(staged + buf));
+      if (lane == 0) arrive(smem_u32(staged + set));
       const int stages = min(kGroup, nkb - kb);
-      kb += kGroup;
-      if (kb >= nkb) {
-        kb = 0;
-        t.tile += gridDim.x;
-        seek_work(p, TN, nct, t);
-      }
-      if (t.have) read();  // on its way while the MMAs work on what is there
-      ok = all_wait(staged + buf, group >> 1 & 1);
+      ok = all_wait(staged + set, turn);
       for (int i = 0; ok && i < stages; i += 2) {
-        const uint32_t from = room + (buf * kGroup + i) * S::kScaleBytes + lane * 16;
+        const uint32_t from = room + i * S::kScaleBytes + lane * 16;
         constexpr int kBlocks = S::kScaleBytes / 512;  // an operand's 128 rows by 128 of K, in the order of the columns
         uint4 w[2 * kBlocks];
 #pragma unroll
@@ -549,19 +565,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         static_assert(S::kColsB % 2 == 0 && (S::kColsB % 4 == 0 || S::kColsB % 4 == 2), "two or four columns");
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;");
-        if (warp == kEpiWarps)  // one of the warps waits for the codes too
+        if ((warp - kEpiWarps) % kScaleWarps == 0)  // one of the warps waits for the codes too
           for (int k = j; ok && k < j + n; ++k) ok = all_wait(codes + k % S::kStages, k / S::kStages & 1);
         if (!ok) break;
         __syncwarp();
         if (lane == 0) arrive(smem_u32(scales + place));
-        if (++place == S::kPlaces) place = 0;
-        j += n;
-        last2 = last1;
-        last1 = last0;
-        last0 = j - 1;
+        next_pair(n);
       }
       __syncwarp();
-      if (lane == 0) arrive(smem_u32(unstaged + buf));
+      if (lane == 0) arrive(smem_u32(unstaged + set));
+      next_group();
+      skip_group();
+      if (t.have) read();  // on its way while the other set works
     }
     if (!ok) *stop = 1;
   } else {
