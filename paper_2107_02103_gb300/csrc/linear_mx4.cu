@@ -250,9 +250,10 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
 // as they are: K 64 an instruction, a scale for 32.
 //   One lane copies a stage's codes, 256 of K, by tensor-map copies into K-major rows of 128 bytes in the 128-byte swizzle
 //   (a map reads zeros past the arrays; rows of another expert or past N land in columns and rows that nobody reads).
-//   Four warps bring the scales, of four stages at a time, four lanes a row, through shared memory: there 128 rows' four
-//   scales of 128 of K are 512 bytes, row r at 16 (r % 32) + 4 (r / 32), so that lane r of each of the warps finds the
-//   words that its quadrant of tensor memory holds in lane r, and writes them there with tcgen05.st, two stages at a time.
+//   Two sets of four warps bring the scales, of four stages at a time in turn, four lanes a row, through shared memory
+//   (one set: 156 us for 32,768 x 2048 x 4096).  There 128 rows' four scales of 128 of K are 512 bytes, row r at
+//   16 (r % 32) + 4 (r / 32), so that lane r of each of a set's warps finds the words that its quadrant of tensor memory
+//   holds in lane r, and writes them there with tcgen05.st, two stages at a time.
 //   Two stages' scales have three places, taken in turn; a place is written again when the MMAs that read it have completed.
 //   (Copies from shared to tensor memory by the MMAs' own thread, tcgen05.cp, take turns with the MMAs: a stage took 2000
 //   cycles whatever its tile, 32,768 x 2048 x 4096 264 us; stages one by one 220 us.)
@@ -261,9 +262,10 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
 //   warps have waited for their codes.
 //   Eight epilogue warps (two per lane quadrant, half the columns each) finish a tile while the next one runs.
 // A block per SM walks the tiles; every wait is bounded, a block that gives up writes NaN and is counted.
-// Measured: 32,768 x 2048 x 4096 bf16 in 156 us (3.5 PFLOP/s, 1.8 times the measured bf16 rate), 8192 cubed 277 us (4.0),
-// 65,536 x 1600 x 240 f32 with four nets 37 us.  A stage takes 480 ns whatever its tile, its MMAs 41 each (128 x 192 by 64):
-// what bounds it are the barriers between the roles.  Without the copies of codes 269 us, without the output 269.
+// Measured: 32,768 x 2048 x 4096 bf16 in 136 us (4.0 PFLOP/s, 2.1 times the measured bf16 rate), 8192 cubed 224 us (4.9),
+// 65,536 x 1600 x 240 f32 with four nets 37 us.  A stage of 8192 cubed takes 390 ns for 192 rows, 310 for 128, 280 for 64,
+// and with one of its four MMAs 355: what bounds it are the barriers between the roles.  Without the output 212 us, the wide
+// product 119.
 namespace mx4 {
 constexpr int kTM = 128, kKB = 256, kRowBytes = kKB / 2;
 constexpr int kEpiWarps = 8, kScaleWarps = 4, kScaleSets = 2;
@@ -317,7 +319,8 @@ __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[16]) {
       : "r"(addr));
 }
 __device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+               " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
                "l"((uint64_t)map), "r"(x), "r"(y), "r"(bar)
                : "memory");
 }
@@ -498,6 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     int j = 0, place = 0;                    // the stage, its pair's place in tensor memory
     int last0 = -1, last1 = -1, last2 = -1;  // the last stages of the pairs before, the latest first
     static_assert(S::kPlaces == 3 && kScaleSets == 2, "as many pairs before; a place a set");
+    static_assert(S::kStages > 2 * (S::kPlaces - 1), "a last stage's barrier does not turn again before this pair's MMAs");
     auto next_pair = [&](int n) {
       if (++place == S::kPlaces) place = 0;
       j += n;
@@ -719,13 +723,13 @@ int quant_rows(const T *x, const int32_t *src, const int32_t *pos, int64_t ntok,
 // Which kernel.  One or two rows: the tiles' start costs 2 us more than a short dot product (back to back, us, few and
 // tiles of 64: 1 row of 1600 -> 2048 6.2 and 8.2, 2 rows of it in two experts 8.3 and 8.3, 2 rows of 4096 -> 4096 12.9 and
 // 11.1, 1 row of 8192 -> 8192 20.6 and 16.4, 4 rows of 1600 -> 2048 8.2 and 8.2).  Tiles of more rows need fewer rounds over
-// 152 SMs, and a round of them takes little longer: 3.4, 3.8 and 4.3 us at K 2048 for 64, 128 and 192 rows.
+// 152 SMs, and a round of them takes little longer: 2.8, 3.2 and 3.8 us at K 2048 for 64, 128 and 192 rows.
 enum Mx4Form { kFew, kTiles64, kTiles128, kTiles192 };
 Mx4Form form_of(int64_t rows, int K, int N, int nexp) {
   if (rows <= kFewRows && rows * K * N <= 1 << 23) return kFew;
   auto cost = [&](int R) {
     const int64_t rounds = (((rows + R - 1) / R + nexp / 2) * ((N + mx4::kTM - 1) / mx4::kTM) + 151) / 152;
-    return rounds * (R + 360);
+    return rounds * (R + 280);
   };
   const int64_t c64 = cost(64), c128 = cost(128), c192 = cost(192);
   return c192 < c128 && c192 < c64 ? kTiles192 : c128 < c64 ? kTiles128 : kTiles64;
