@@ -158,7 +158,7 @@ def test_a_scale_of_nan_spoils_its_row_or_channel_only(n):
     check(y[np.ix_(~bad_r, ~bad_c)], M.values(M.pack(code), scale)[~bad_r], wv[0][~bad_c], np.zeros((~bad_c).sum()), None, torch.float32)
 
 
-EXPERTS = [(1, 2, 8, 240, 100), (6, 2, 3, 64, 9), (40, 2, 5, 96, 130), (400, 2, 13, 1237, 150), (300, 3, 61, 70, 31), (900, 1, 4, 320, 240), (700, 2, 2, 512, 64), (50, 1, 1024, 64, 7), (9000, 2, 5, 96, 800)]
+EXPERTS = [(1, 2, 8, 240, 100), (6, 2, 3, 64, 9), (40, 2, 5, 96, 130), (400, 2, 13, 1237, 150), (300, 3, 61, 70, 31), (900, 1, 4, 320, 240), (700, 2, 2, 512, 64), (50, 1, 1024, 64, 7), (9000, 2, 5, 96, 800), (300, 2, 1, 96, 130), (500, 1, 1, 1100, 200)]
 
 
 @pytest.mark.parametrize("dtype", ROWS, ids=IDS)
@@ -182,6 +182,20 @@ def test_experts(dtype, T, k, E, K, N, drop):
     for n in range(E):
         check(y[rs[n]: rs[n + 1]], xv[rs[n]: rs[n + 1]], wv[n], f64(bias)[n], "tanh", dtype, f"expert {n}")
     assert not y[rs[E]:].any()
+
+
+@pytest.mark.parametrize("T,E,N", [(1, 1, 5), (5, 3, 200), (700, 4, 130), (3000, 64, 7)])
+def test_every_pair_dropped(T, E, N):
+    """No expert has a row: every row of the result is zero."""
+    dpc = lib()
+    start, src, pos = dpc.dp_route_plan(torch.full((T, 2), -1, dtype=torch.int32, device="cuda"), E)
+    x, _ = rows(T, T, 320, torch.float32)
+    xq, sx = dpc.dp_quant_rows_mx4(x, src, pos)
+    assert not xq.any()
+    wq, sw, _ = weights(N, E, N, 320)
+    out = torch.full((T * 2, N), float("nan"), device="cuda")
+    dpc.dp_linear_mx4(xq, sx, wq, sw, bias=torch.ones(E, N, device="cuda"), start=start, act="tanh", out=out)
+    assert (out == 0).all()
 
 
 def test_rows_behind_the_output_stay(dtype=torch.float32):
