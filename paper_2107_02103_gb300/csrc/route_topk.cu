@@ -629,6 +629,7 @@ __device__ __noinline__ bool settle_groups(const TopkArgs &p, const T *x, const 
     const unsigned long long k = __shfl_sync(m8, of, o, 8);
     rank += k > of || (k == of && o < sub);
   }
+  __syncwarp(m8);  // all lanes have read the flags
   if (g_of >= 0) kept[g_of] = rank < p.keep - sure;
   return true;
 }
@@ -775,6 +776,7 @@ __global__ void __launch_bounds__(kThreads, 8) topk_lists_kernel(const __grid_co
       if (rank < p.keep) last = min(last, k);
       else next = max(next, k);
     }
+    __syncwarp();  // settle_groups reads the flags of all lanes' groups
     last = over<8>(kAll, last, [](uint32_t a, uint32_t b) { return min(a, b); });
     next = over<8>(kAll, next, [](uint32_t a, uint32_t b) { return max(a, b); });
     const float a = from_key(last), b = from_key(next);
