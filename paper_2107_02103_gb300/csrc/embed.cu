@@ -9,6 +9,7 @@
 #include <cooperative_groups.h>
 
 #include "rows.cuh"
+#include "search.cuh"
 
 namespace dpc {
 namespace {
@@ -70,13 +71,7 @@ __device__ __forceinline__ int scan_digits(int v, int *sums) {
 
 // start[v] = the first of n sorted keys that is at least v.
 __device__ __forceinline__ int lower_bound(const uint32_t *keys, int n, uint32_t v) {
-  int lo = 0, hi = n;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (keys[mid] < v) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo;
+  return dpc::lower_bound([keys](int i) { return keys[i]; }, n, v);
 }
 
 // Up to kSortBlock ids in one block, all digits in shared memory.
