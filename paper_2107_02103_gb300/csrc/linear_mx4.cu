@@ -570,7 +570,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;");
         if ((warp - kEpiWarps) % kScaleWarps == 0)  // one of the warps waits for the codes too
-          for (int k = j; ok && k < j + n; ++k) ok = all_wait(codes + k % S::kStages, k / S::kStages & 1);
+          for (int k = j; ok && k < j + n; ++k) {
+            // A parity tells a turn from the next, not from the one after that: the place's turn before must be over, which
+            // the other set may have waited for.  Its MMAs are through if they lie before the last2 waited for above; with
+            // fewer stages than three pairs have, that is waited for here (the codes are copied after it anyway).
+            if (S::kStages < 2 * S::kPlaces && k >= S::kStages)
+              ok = all_wait(empty + k % S::kStages, (k / S::kStages - 1) & 1);
+            ok = ok && all_wait(codes + k % S::kStages, k / S::kStages & 1);
+          }
         if (!ok) break;
         __syncwarp();
         if (lane == 0) arrive(smem_u32(scales + place));

@@ -26,3 +26,34 @@ def test_group_flags_are_ordered_between_lanes():
     settle = body(source("route_topk.cu"), "bool settle_groups(")
     read, write = settle.index("kept[g]"), settle.index("kept[g_of] = ")
     assert read < write and re.search(r"__syncwarp\(m8\);", settle[read: write])
+
+
+def test_the_four_bit_products_turns_are_told_apart():
+    """A wait on a parity returns at once while the turn before the awaited one is still open.  A set of scale warps waits
+    for the codes of its own pairs of stages alone, so for each stage k the codes of stage k - kStages, which the other set
+    may have waited for, must be known to have arrived: their MMAs lie at or before the last stage three pairs back
+    (waited for before the pair is written), or stage k - kStages is waited for by itself."""
+    src = source("linear_mx4.cu")
+    wide, mid, small = map(int, re.search(r"kStages = TN > 128 \? (\d+) : TN > 64 \? (\d+) : (\d+);", src).groups())
+    places, group = int(re.search(r"kPlaces = (\d+);", src).group(1)), int(re.search(r"kGroup = (\d+);", src).group(1))
+    assert "if (last2 >= 0) ok = all_wait(empty + last2 % S::kStages, last2 / S::kStages & 1);" in src and places == 3
+    waits = re.search(r"if \(S::kStages < 2 \* S::kPlaces && k >= S::kStages\)\s*"
+                      r"ok = all_wait\(empty \+ k % S::kStages, \(k / S::kStages - 1\) & 1\);\s*"
+                      r"ok = ok && all_wait\(codes \+ k % S::kStages, k / S::kStages & 1\);", src)
+    for stages in (wide, mid, small):
+        own_wait = waits is not None and stages < 2 * places
+        for nkb in range(1, 14):
+            last, j = [], 0  # of the pairs so far
+            for _ in range(12):  # tiles
+                for kb in range(0, nkb, group):
+                    n_group = min(group, nkb - kb)
+                    for i in range(0, n_group, 2):
+                        n = min(2, n_group - i)
+                        through = last[-places] if len(last) >= places else -1  # MMAs known to be through
+                        for k in range(j, j + n):
+                            if k >= stages:
+                                assert k - stages <= through or own_wait, (stages, nkb, k)
+                                # the turn before that, of the barrier that tells it
+                                assert k - 2 * stages <= through, (stages, nkb, k)
+                        j += n
+                        last.append(j - 1)
