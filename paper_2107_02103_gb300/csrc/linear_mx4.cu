@@ -567,17 +567,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           at += cols;
         }
         static_assert(S::kColsB % 2 == 0 && (S::kColsB % 4 == 0 || S::kColsB % 4 == 2), "two or four columns");
+        // One of the warps waits for the codes too.  A parity tells a turn from the next, not from the one after that: the
+        // place's turn before, which the other set may have waited for, must be over.  It is if its MMAs are through: those
+        // up to last2 are, and with fewer stages than three pairs have, the others are waited for (the codes are copied after
+        // them anyway) while the scales are on their way.
+        const bool brings_codes = (warp - kEpiWarps) % kScaleWarps == 0;
+        if (S::kStages < 2 * S::kPlaces && brings_codes)
+          for (int k = max(j, last2 + 1 + S::kStages); ok && k < j + n; ++k)
+            ok = all_wait(empty + k % S::kStages, (k / S::kStages - 1) & 1);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;");
-        if ((warp - kEpiWarps) % kScaleWarps == 0)  // one of the warps waits for the codes too
-          for (int k = j; ok && k < j + n; ++k) {
-            // A parity tells a turn from the next, not from the one after that: the place's turn before must be over, which
-            // the other set may have waited for.  Its MMAs are through if they lie before the last2 waited for above; with
-            // fewer stages than three pairs have, that is waited for here (the codes are copied after it anyway).
-            if (S::kStages < 2 * S::kPlaces && k >= S::kStages)
-              ok = all_wait(empty + k % S::kStages, (k / S::kStages - 1) & 1);
-            ok = ok && all_wait(codes + k % S::kStages, k / S::kStages & 1);
-          }
+        if (brings_codes)
+          for (int k = j; ok && k < j + n; ++k) ok = all_wait(codes + k % S::kStages, k / S::kStages & 1);
         if (!ok) break;
         __syncwarp();
         if (lane == 0) arrive(smem_u32(scales + place));

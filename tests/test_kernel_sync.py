@@ -37,9 +37,11 @@ def test_the_four_bit_products_turns_are_told_apart():
     wide, mid, small = map(int, re.search(r"kStages = TN > 128 \? (\d+) : TN > 64 \? (\d+) : (\d+);", src).groups())
     places, group = int(re.search(r"kPlaces = (\d+);", src).group(1)), int(re.search(r"kGroup = (\d+);", src).group(1))
     assert "if (last2 >= 0) ok = all_wait(empty + last2 % S::kStages, last2 / S::kStages & 1);" in src and places == 3
-    waits = re.search(r"if \(S::kStages < 2 \* S::kPlaces && k >= S::kStages\)\s*"
-                      r"ok = all_wait\(empty \+ k % S::kStages, \(k / S::kStages - 1\) & 1\);\s*"
-                      r"ok = ok && all_wait\(codes \+ k % S::kStages, k / S::kStages & 1\);", src)
+    waits = re.search(r"if \(S::kStages < 2 \* S::kPlaces && brings_codes\)\s*"
+                      r"for \(int k = max\(j, last2 \+ 1 \+ S::kStages\); ok && k < j \+ n; \+\+k\)\s*"
+                      r"ok = all_wait\(empty \+ k % S::kStages, \(k / S::kStages - 1\) & 1\);.*?"
+                      r"if \(brings_codes\)\s*for \(int k = j; ok && k < j \+ n; \+\+k\) "
+                      r"ok = all_wait\(codes \+ k % S::kStages, k / S::kStages & 1\);", src, re.S)
     for stages in (wide, mid, small):
         own_wait = waits is not None and stages < 2 * places
         for nkb in range(1, 14):
