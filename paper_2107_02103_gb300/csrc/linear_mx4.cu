@@ -221,12 +221,16 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
   float acc[kFewRows] = {};
   for (int b = lane; b < nb; b += 32) {
     const Block32 wb(__ldg(w + b));
-    const float s = pow2_of(__ldg(p.sw + c * lds + b));
+    const uint32_t cw = __ldg(p.sw + c * lds + b);
 #pragma unroll
     for (int i = 0; i < kFewRows; ++i)
       if (i < nr) {
         const Block32 xb(__ldg(x + (int64_t)i * nb + b));
-        acc[i] = fmaf((float)dot(wb, xb), s * pow2_of(__ldg(p.sx + (int64_t)(r0 + i) * lds + b)), acc[i]);
+        // the scales' product as two powers of two of equal size: neither the sum's product with the first (exact) nor
+        // the powers leave f32's range unless the block's sum does
+        const uint32_t cx = __ldg(p.sx + (int64_t)(r0 + i) * lds + b);
+        const uint32_t half = cw == 255 || cx == 255 ? 255 : (cw + cx) / 2;
+        acc[i] = fmaf(0.25f * (float)dot(wb, xb) * pow2_of(half), pow2_of(cw + cx - half), acc[i]);
       }
   }
   float mine = 0.0f;
@@ -238,7 +242,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
     if (lane == i) mine = s;
   }
   if (lane < nr) {
-    float v = fmaf(mine, 0.25f, p.bias ? __ldg(p.bias + c) : 0.0f);
+    float v = mine + (p.bias ? __ldg(p.bias + c) : 0.0f);
     if (p.act == DP_ACT_TANH) v = tanhf(v);
     put_out(y + (int64_t)(r0 + lane) * p.N + n, v);
   }
