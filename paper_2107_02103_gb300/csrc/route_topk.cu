@@ -5,9 +5,10 @@
 // Without a bias the experts are ordered by x itself, which has the order of s and no rounding.  Ties go to the lowest
 // index, a NaN stands above all numbers, an expert with x = -inf or b = -inf is never chosen (-1, weight 0).
 // The choice is that of exact arithmetic, in up to three steps: first on f32 scores cut to leave room for the expert's index
-// in the same word (one integer is compared and moved, and no two are equal); a token in which two neighbours of that
-// order (the first one left out included) or the last group kept and the first one dropped are nearer than their error
-// bounds is done again on whole f32 scores, and where those are too near, in f64.
+// in the same word (one integer is compared and moved, and no two are equal); a token in which two neighbours of the chosen
+// ones, the last of them and any that is left out (whose error may be far larger than a neighbour's: an s near 1 that a
+// bias cancels), or the last group kept and the first one dropped are nearer than their error bounds is done again on whole
+// f32 scores, and where those are too near, in f64.
 // Backward, the choice held fixed, n_j = s_ej / sum_i s_ei:
 //   renormalised  g_j = scale n_j (dw_j - sum_i n_i dw_i)   softmax dx_ej += g_j,  sigmoid dx_ej += g_j (1 - s_ej)
 //   plain         softmax dx_e = sum_(j: e_j = e) g_j - s_e sum_j g_j with g_j = scale dw_j s_ej
@@ -163,8 +164,29 @@ __device__ __forceinline__ bool packed_near(uint32_t k0, uint32_t k1, uint32_t m
   return !(c0 - c1 > (rough_error(range, sigm) + 0x1p-23f) * (fabsf(c0) + fabsf(c1) + fabsf(b0) + fabsf(b1)));
 }
 
-// One token on a warp, N logits a lane: the i-th is expert 32 i + lane.  S chosen pairs a lane (and the first one left
-// out).  True: two scores are too near to tell apart in A, and nothing is written.  `room`: shared memory of the token,
+// The largest c that an expert whose f32 score is at most c1 may have: s = c - b is at most |c1| + bmost (the largest finite
+// |b|) and 1, the size of its exponential's argument at most ln(1 / s), and s ln(1 / s) grows up to s = 1/e.
+__device__ __forceinline__ float reach_of(float c1, float bmost, bool sigm) {
+  const float s = fminf(1.0f, fabsf(c1) + bmost);
+  const float range = fmaxf(1.0f, 0.6932f * (float)(127 - (int)(__float_as_uint(s) >> 23)));
+  return c1 + rough_error(range, sigm) * s + 0x1p-22f * fabsf(c1);
+}
+// The least c that a chosen one may have.
+__device__ __forceinline__ float least_of(float c, float x, float b, float most, bool sigm) {
+  return c - (rough_error(range_of(x, x, most, sigm), sigm) + 0x1p-23f) * (fabsf(c) + fabsf(b));
+}
+
+// The value of pair k - 1 of a warp's pairs.
+template <int S, typename V>
+__device__ __forceinline__ V of_last(int k, const V (&v)[S]) {
+  V at = v[0];
+#pragma unroll
+  for (int s = 1; s < S; ++s)
+    if ((k - 1) / 32 == s) at = v[s];
+  return __shfl_sync(kAll, at, (k - 1) % 32);
+}
+
+// One token on a warp, N logits a lane: the i-th is expert 32 i + lane.  S chosen pairs a lane.  True: two scores are too near to tell apart in A, and nothing is written.  `room`: shared memory of the token,
 // E + 3 G words of 8 bytes, for the groups.
 template <typename T, typename A, int N, int S>
 __device__ bool choose(const TopkArgs &p, int64_t t, unsigned char *room) {
@@ -240,7 +262,7 @@ __device__ bool choose(const TopkArgs &p, int64_t t, unsigned char *room) {
     }
   }
 
-  // the best of each lane, then of the warp, k times and once more for the first one left out
+  // the best of each lane, then of the warp, k times; the keys of those that are left out stay
   U best;
   int at;
   auto rescan = [&] {
@@ -262,7 +284,7 @@ __device__ bool choose(const TopkArgs &p, int64_t t, unsigned char *room) {
     sk[s] = 0;
   }
   const bool check = !kExact && p.bias;
-  for (int j = 0; j < p.k + (check ? 1 : 0); ++j) {
+  for (int j = 0; j < p.k; ++j) {
     const U m = warp_max(best);
     if (m == 0) break;
     const int e = __reduce_min_sync(kAll, best == m ? at * 32 + lane : INT_MAX);
@@ -304,6 +326,18 @@ __device__ bool choose(const TopkArgs &p, int64_t t, unsigned char *room) {
           near |= too_near(c[s], wrap ? c1 : c0, sx[s], nx, b[s], wrap ? b1 : b0, range, p.sigmoid);
         }
       }
+      const int el = of_last(p.k, se);
+      if (el >= 0) {
+        const float cl = from_key(of_last(p.k, sk)), xl = to_acc(x[el]), bl = __ldg(bias + el);
+        if (best && !(least_of(cl, xl, bl, most, p.sigmoid) > reach_of(from_key(best), 1.0f, p.sigmoid)))
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            if (key[i]) {
+              const int e = i * 32 + lane;
+              const float xe = to_acc(x[e]);
+              near |= too_near(cl, from_key(key[i]), xl, xe, bl, __ldg(bias + e), most - fminf(xl, xe), p.sigmoid);
+            }
+      }
     }
     if (by_score && __any_sync(kAll, near)) return true;
   }
@@ -314,7 +348,6 @@ __device__ bool choose(const TopkArgs &p, int64_t t, unsigned char *room) {
     top = none<A>();
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      if (s * 32 + lane >= p.k) se[s] = -1;  // the first one left out
       if (se[s] >= 0) top = sx[s] != sx[s] || sx[s] > top ? sx[s] : top;
     }
     top = most_over<32>(kAll, top);
@@ -424,8 +457,7 @@ __device__ __forceinline__ bool choose_packed(const TopkArgs &p, int64_t t, unsi
 #pragma unroll
   for (int s = 0; s < S; ++s) sk[s] = 0;
   const bool check = p.bias || (sizeof(T) == 4);  // 16-bit logits are whole beside the index
-  const int picks = p.k + (check ? 1 : 0);
-  for (int j = 0; j < picks; ++j) {
+  for (int j = 0; j < p.k; ++j) {
     const uint32_t m = warp_max(best);
     if (m == 0) break;
 #pragma unroll
@@ -474,13 +506,28 @@ __device__ __forceinline__ bool choose_packed(const TopkArgs &p, int64_t t, unsi
         else near |= ((sk[s] ^ nk) & ~mask) == 0 && sx[s] != nx;
       }
     }
+    const uint32_t kl = of_last(p.k, sk);
+    if (kl) {
+      const int el = packed_expert(kl, mask);
+      const float xl = to_acc(x[el]), bl = bias ? __ldg(bias + el) : 0.0f;
+      // the lane's best by the widest bounds, its others by their own only where those do not do
+      if (best && (bias ? !(least_of(from_key(kl & ~mask), xl, bl, most, p.sigmoid) > reach_of(from_key(best | mask), 1.0f, p.sigmoid))
+                        : ((kl ^ best) & ~mask) == 0))
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (key[i]) {
+            const int e = i * 32 + lane;
+            const float xe = to_acc(x[e]);
+            if (bias) near |= packed_near(kl, key[i], mask, xl, xe, bl, __ldg(bias + e), range_of(xl, xe, most, p.sigmoid), p.sigmoid);
+            else near |= ((kl ^ key[i]) & ~mask) == 0 && xl != xe;
+          }
+    }
   }
   if (__any_sync(kAll, near)) return true;
 
   float wsum = 1.0f, top = none<float>(), ws[S];
 #pragma unroll
   for (int s = 0; s < S; ++s) {
-    if (s * 32 + lane >= p.k) se[s] = -1;  // the first one left out
     if (se[s] >= 0) top = sx[s] != sx[s] || sx[s] > top ? sx[s] : top;
   }
   if (p.renorm) {
@@ -507,8 +554,9 @@ __device__ __forceinline__ bool choose_packed(const TopkArgs &p, int64_t t, unsi
 // Words of 8 bytes of a token's groups.
 __host__ __device__ constexpr int room_words(int E, int G) { return E + 3 * G; }
 
+// With 32 logits a lane four blocks an SM: at the 134 registers it else takes, 8192 x 1024 with 40 chosen took 506 us, not 461.
 template <typename T, int N, int S>
-__global__ void __launch_bounds__(kThreads) topk_kernel(const __grid_constant__ TopkArgs p) {
+__global__ void __launch_bounds__(kThreads, N == 32 ? 4 : 1) topk_kernel(const __grid_constant__ TopkArgs p) {
   extern __shared__ __align__(16) unsigned char rooms[];
   const int64_t t = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
   if (t >= p.ntok) return;
@@ -538,15 +586,11 @@ __device__ __forceinline__ void sort8(uint32_t (&k)[8]) {  // descending
 #pragma unroll
   for (int i = 0; i < 19; ++i) exchange(k[net[i][0]], k[net[i][1]]);
 }
-// The best eight of two descending lists, and the two best of the others.
-__device__ __forceinline__ void leave(uint32_t k, uint32_t (&left)[2]) {
-  left[1] = max(left[1], min(left[0], k));
-  left[0] = max(left[0], k);
-}
-__device__ __forceinline__ void merge8(uint32_t (&a)[8], const uint32_t (&b)[8], uint32_t (&left)[2]) {
+// The best eight of two descending lists, and the best of the others.
+__device__ __forceinline__ void merge8(uint32_t (&a)[8], const uint32_t (&b)[8], uint32_t &left) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    leave(min(a[i], b[7 - i]), left);
+    left = max(left, min(a[i], b[7 - i]));
     a[i] = max(a[i], b[7 - i]);
   }
 #pragma unroll
@@ -633,19 +677,45 @@ __device__ __noinline__ bool settle_groups(const TopkArgs &p, const T *x, const 
   if (g_of >= 0) kept[g_of] = rank < p.keep - sure;
   return true;
 }
-// The list's experts and the best beyond it in their exact order: lane j's e (-1: none) becomes the j-th.  left: the two
-// best packed keys beyond the list.  False: the second of them may belong to the first k.
+// Whether an expert beside the lanes' e and e9 may have a larger c than `low`, the least of the k-th one, el.  kept: the
+// groups' flags, or NULL.
 template <typename T>
-__device__ __noinline__ bool settle_list(const TopkArgs &p, const T *x, int &e, uint32_t left0, uint32_t left1, float most,
+__device__ __noinline__ bool one_ahead(const TopkArgs &p, const T *x, int e, int e9, int el, double low, const uint32_t *kept,
+                                       float most, float total, unsigned m8) {
+  const float *bias = (const float *)p.bias;
+  const float xl = to_acc(x[el]), bl = bias ? __ldg(bias + el) : 0.0f;
+  const int per = p.E / p.G;
+  int listed[8];
+#pragma unroll
+  for (int o = 0; o < 8; ++o) listed[o] = __shfl_sync(m8, e, o, 8);
+  bool ahead = false;
+#pragma unroll 2
+  for (int i = threadIdx.x % 8; i < p.E; i += 8) {
+    const float v = to_acc(x[i]), b = bias ? __ldg(bias + i) : 0.0f;
+    bool out = i == e9 || v == none<float>() || b == none<float>() || (v == xl && b == bl && i > el);
+#pragma unroll
+    for (int o = 0; o < 8; ++o) out |= i == listed[o];
+    if (out || (kept && !kept[i / per])) continue;
+    const float c = bias ? score_of(v, p.sigmoid, most, total) + b : v;
+    const float tol = bias ? (score_error(most - v, p.sigmoid) + 0x1p-23f) * (fabsf(c) + fabsf(b)) : 0.0f;
+    ahead |= !(low - c > tol);
+  }
+  return __any_sync(m8, ahead);
+}
+// The list's experts and the best beyond it in their exact order: lane j's e (-1: none) becomes the j-th.  left: the best
+// packed key beyond the list; kept as above.  False: one beyond them may belong to the first k.
+template <typename T>
+__device__ __noinline__ bool settle_list(const TopkArgs &p, const T *x, int &e, uint32_t left, const uint32_t *kept, float most,
                                          unsigned m8) {
   const int sub = threadIdx.x % 8;
   const double total = p.sigmoid || !p.bias ? 1.0 : exact_total(x, p.E, most, m8);
   auto exact = [&](int of) {
     return of < 0 ? 0ull : p.bias ? exact_key(p, x, of, most, total) : to_key((double)to_acc(x[of]));
   };
-  const int e9 = left0 > kNoKey ? (int)(p.mask - (left0 & p.mask)) : -1;
+  const int e9 = left > kNoKey ? (int)(p.mask - (left & p.mask)) : -1;
   const unsigned long long key = exact(e), key9 = exact(e9);
   const bool after9 = key9 > key || (key9 == key && key9 && e9 < e);
+  const int listed = e;
   int rank = after9;
 #pragma unroll
   for (int o = 0; o < 8; ++o) {
@@ -664,15 +734,11 @@ __device__ __noinline__ bool settle_list(const TopkArgs &p, const T *x, int &e, 
     if (r == p.k - 1) last = k;
   }
   e = sorted;
-  if (left1 <= kNoKey) return true;
-  const float c = from_key(left1 | p.mask);
-  float tol = 0.0f;
-  if (p.bias) {
-    const int el = (int)(p.mask - (left1 & p.mask));
-    const float xl = to_acc(x[el]), b = __ldg((const float *)p.bias + el);
-    tol = (rough_error(p.sigmoid ? fabsf(xl) : most - xl, p.sigmoid) + 0x1p-23f) * (fabsf(c) + fabsf(b));
-  }
-  return last != 0 && from_key(last) - c > tol;
+  const int el = __shfl_sync(m8, e, p.k - 1, 8);
+  if (el < 0) return true;  // all that may be chosen are
+  const float beyond = from_key(left | p.mask);  // those are behind it in the packed order
+  if (left <= kNoKey || from_key(last) > (p.bias ? reach_of(beyond, 1.0f, p.sigmoid) : beyond)) return true;
+  return !one_ahead(p, x, listed, e9, el, from_key(last), kept, most, (float)total, m8);
 }
 
 __host__ __device__ constexpr int list_words(int E, int G) { return (E + E / 8 + 1 + 2 * G) | 1; }
@@ -784,7 +850,7 @@ __global__ void __launch_bounds__(kThreads, 8) topk_lists_kernel(const __grid_co
       lost = !settle_groups(p, x, gkey, kept, a, b, most, m8);
     __syncwarp();
   }
-  uint32_t list[8], left[2] = {0, 0};  // the two best beyond the list
+  uint32_t list[8], left = 0;  // the best beyond the list
 #pragma unroll
   for (int i = 0; i < 8; ++i) list[i] = 0;
 #pragma unroll 1
@@ -815,12 +881,10 @@ __global__ void __launch_bounds__(kThreads, 8) topk_lists_kernel(const __grid_co
     uint32_t b[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) b[i] = __shfl_xor_sync(kAll, list[i], o);
-    const uint32_t l0 = __shfl_xor_sync(kAll, left[0], o), l1 = __shfl_xor_sync(kAll, left[1], o);
-    leave(l0, left);
-    leave(l1, left);
+    left = max(left, __shfl_xor_sync(kAll, left, o));
     merge8(list, b, left);
   }
-  uint32_t key = 0, next = left[0];
+  uint32_t key = 0, next = left;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     if (i == sub) key = list[i];
@@ -829,16 +893,44 @@ __global__ void __launch_bounds__(kThreads, 8) topk_lists_kernel(const __grid_co
   int e = key > kNoKey ? (int)(mask - (key & mask)) : -1;
   float xe = e >= 0 ? to_acc(x[e]) : none<float>();
   if (bias || sizeof(T) == 4) {  // 16-bit logits are whole beside the index
+    // Neighbours in the order: the chosen ones each with the next, the last of them with all that follow.  Those may begin
+    // with its equals, which are rightly behind it: the first pair that differs, its lane `border`, decides.
+    const bool pair = e >= 0 && next > kNoKey;
+    const int en = pair ? (int)(mask - (next & mask)) : 0;
+    const float xn = pair ? to_acc(x[en]) : 0.0f;
+    const float b0 = bias && pair ? __ldg(bias + e) : 0.0f, b1 = bias && pair ? __ldg(bias + en) : 0.0f;
+    const bool same = pair && xe == xn && b0 == b1;
+    const unsigned at = threadIdx.x & 24;
+    const int border = __ffs((~__ballot_sync(kAll, same) >> at & 255) >> (p.k - 1)) + p.k - 2;  // k - 2: none
     bool near = false;
-    if (sub < p.k && e >= 0 && next > kNoKey) {
-      const int en = (int)(mask - (next & mask));
-      const float xn = to_acc(x[en]);
-      const float range = range_of(xe, xn, most, p.sigmoid);
-      if (bias) near = packed_near(key, next, mask, xe, xn, __ldg(bias + e), __ldg(bias + en), range, p.sigmoid);
-      else near = ((key ^ next) & ~mask) == 0 && xe != xn;
+    float low = 0.0f;  // the least that c may be
+    if (pair && !same) {
+      if (!bias) {
+        near = (sub < p.k - 1 || sub == border) && ((key ^ next) & ~mask) == 0;
+      } else if (sub < p.k - 1) {
+        near = packed_near(key, next, mask, xe, xn, b0, b1, range_of(xe, xn, most, p.sigmoid), p.sigmoid);
+      } else if (sub == border) {
+        low = least_of(from_key(key & ~mask), xe, b0, most, p.sigmoid);
+        near = !(low > reach_of(from_key(next | mask), 1.0f, p.sigmoid));
+      }
     }
-    if (__ballot_sync(kAll, near) & m8) {
-      lost |= !settle_list(p, x, e, left[0], left[1], most, m8);
+    if (bias && __any_sync(kAll, near)) {  // looked at again with the largest |b|, where scores are far below 1
+      float bmost = 0.0f;
+      for (int i = sub; i < p.E; i += 8) {
+        const float b = fabsf(__ldg(bias + i));
+        bmost = b < INFINITY ? fmaxf(bmost, b) : bmost;  // -inf is out, +inf comes first
+      }
+      bmost = over<8>(kAll, bmost, [](float a, float b) { return fmaxf(a, b); });
+      if (near && sub == border) near = !(low > reach_of(from_key(next | mask), bmost, p.sigmoid));
+    }
+    bool unsure = __ballot_sync(kAll, near) & m8;
+    if (!unsure && border < p.k - 1) {  // its equals fill the list
+      if (bias) low = least_of(from_key(key & ~mask), xe, b0, most, p.sigmoid);
+      unsure = one_ahead(p, x, e, -1, __shfl_sync(m8, e, p.k - 1, 8), __shfl_sync(m8, bias ? low : xe, p.k - 1, 8),
+                         grouped ? kept : nullptr, most, total, m8);
+    }
+    if (unsure) {
+      lost |= !settle_list(p, x, e, left, grouped ? kept : nullptr, most, m8);
       xe = e >= 0 ? to_acc(x[e]) : none<float>();
     }
     __syncwarp();
