@@ -122,6 +122,9 @@ __device__ __forceinline__ bool too_near(float c0, float c1, float x0, float x1,
   if (x0 == x1 && b0 == b1) return false;
   return !(c0 - c1 > (score_error(range, sigm) + 0x1p-23f) * (fabsf(c0) + fabsf(c1) + fabsf(b0) + fabsf(b1)));
 }
+// A group's score from its two best (0 in the place of none), at half its size: no sum leaves the type's range.
+template <typename A>
+__device__ __forceinline__ A half_sum(A a, A b) { return A(0.5) * a + A(0.5) * b; }
 // The same of two groups' scores, sums of up to two c each.  The four s come to at most 4 (sigmoid) or 1 (softmax, where
 // range s is at most 0.4): within 2^-18.9 or 2^-17.7 together, and the sums' roundings.
 __device__ __forceinline__ bool groups_too_near(float a, float b, bool sigm) {
@@ -237,7 +240,7 @@ __device__ bool choose(const TopkArgs &p, int64_t t, unsigned char *room) {
         b = less > b ? less : b;
         a = c > a ? c : a;
       }
-      gkey[g] = p.gtop == 2 && b ? to_key(from_key(a) + from_key(b)) : a;
+      gkey[g] = p.gtop == 2 && a ? to_key(half_sum(from_key(a), b ? from_key(b) : decltype(from_key(a))(0))) : a;
     }
     __syncwarp();
     U last = ~(U)0, first = 0;  // the least group kept, the best one dropped
@@ -427,7 +430,7 @@ __device__ __forceinline__ bool choose_packed(const TopkArgs &p, int64_t t, unsi
         b = max(b, min(a, c));
         a = max(a, c);
       }
-      gkey[g] = p.gtop == 2 && b ? to_key(from_key(a) + from_key(b)) : a;
+      gkey[g] = p.gtop == 2 && a ? to_key(half_sum(from_key(a), b ? from_key(b) : decltype(from_key(a))(0))) : a;
     }
     __syncwarp();
     uint32_t last = kAll, first = 0;
@@ -663,7 +666,7 @@ __device__ __noinline__ bool settle_groups(const TopkArgs &p, const T *x, const 
     }
     if (n == sub) {
       g_of = g;
-      of = p.gtop == 2 && k1 ? to_key(from_key(k0) + from_key(k1)) : k0;
+      of = p.gtop == 2 && k0 ? to_key(half_sum(from_key(k0), k1 ? from_key(k1) : 0.0)) : k0;
     }
     ++n;
   }
@@ -829,7 +832,7 @@ __global__ void __launch_bounds__(kThreads, 8) topk_lists_kernel(const __grid_co
         b = max(b, min(a, k));
         a = max(a, k);
       }
-      gkey[g] = p.gtop == 2 && b > kNoKey ? to_bits(from_key(a) + from_key(b)) : a;
+      gkey[g] = p.gtop == 2 && a > kNoKey ? to_bits(half_sum(from_key(a), b > kNoKey ? from_key(b) : 0.0f)) : a;
     }
     __syncwarp();
     uint32_t last = kAll, next = 0;  // the least group kept, the best one dropped
