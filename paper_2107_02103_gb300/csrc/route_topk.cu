@@ -125,10 +125,17 @@ __device__ __forceinline__ bool too_near(float c0, float c1, float x0, float x1,
 // A group's score from its two best (0 in the place of none), at half its size: no sum leaves the type's range.
 template <typename A>
 __device__ __forceinline__ A half_sum(A a, A b) { return A(0.5) * a + A(0.5) * b; }
-// The same of two groups' scores, sums of up to two c each.  The four s come to at most 4 (sigmoid) or 1 (softmax, where
-// range s is at most 0.4): within 2^-18.9 or 2^-17.7 together, and the sums' roundings.
-__device__ __forceinline__ bool groups_too_near(float a, float b, bool sigm) {
-  return !(a - b > (sigm ? 0x1p-18f : 0x1p-17f) * (1.0f + fabsf(b)));
+// The least and the largest that a group's score may be, `spread` the sum of the |c| that it is made of (which may cancel in
+// it): half of two s' errors or one s' error come to less than 2^-18 (a softmax's s to at most 1 together, and
+// s ln(1 / s) to 0.37 each), the roundings of s + b and of the score to 2^-24 of the spread.
+__device__ __forceinline__ float group_error(float spread) { return 0x1p-18f + 0x1p-23f * spread; }
+__device__ __forceinline__ float group_least(float score, float spread) {
+  const float v = score - group_error(spread);
+  return score != score ? INFINITY : v == v ? v : -INFINITY;
+}
+__device__ __forceinline__ float group_most(float score, float spread) {
+  const float v = score + group_error(spread);
+  return v == v ? v : INFINITY;
 }
 
 // The first step's scores, by the hardware's base-two exponential (documented error 2^-22, its argument's roundings |x| ulp)
@@ -177,6 +184,13 @@ __device__ __forceinline__ float reach_of(float c1, float bmost, bool sigm) {
 // The least c that a chosen one may have.
 __device__ __forceinline__ float least_of(float c, float x, float b, float most, bool sigm) {
   return c - (rough_error(range_of(x, x, most, sigm), sigm) + 0x1p-23f) * (fabsf(c) + fabsf(b));
+}
+
+// Whether the warp's least group kept and largest one dropped leave the choice of groups open.
+__device__ __forceinline__ bool groups_near(float least, float next) {
+  least = over<32>(kAll, least, [](float a, float b) { return fminf(a, b); });
+  next = over<32>(kAll, next, [](float a, float b) { return fmaxf(a, b); });
+  return next > -INFINITY && !(least > next);
 }
 
 // The value of pair k - 1 of a warp's pairs.
@@ -240,17 +254,23 @@ __device__ bool choose(const TopkArgs &p, int64_t t, unsigned char *room) {
         b = less > b ? less : b;
         a = c > a ? c : a;
       }
-      gkey[g] = p.gtop == 2 && a ? to_key(half_sum(from_key(a), b ? from_key(b) : decltype(from_key(a))(0))) : a;
+      const A ca = a ? from_key(a) : A(0), cb = p.gtop == 2 && b ? from_key(b) : A(0);
+      gkey[g] = p.gtop == 2 && a ? to_key(half_sum(ca, cb)) : a;
+      if constexpr (!kExact) kept[g] = __float_as_uint(fabsf(ca) + fabsf(cb));  // until it is ranked, by this lane
     }
     __syncwarp();
-    U last = ~(U)0, first = 0;  // the least group kept, the best one dropped
+    [[maybe_unused]] float least = INFINITY, next = -INFINITY;  // of the groups kept, and the largest of those dropped
     for (int g = lane; g < p.G; g += 32) {
       const U mine = gkey[g];
       int rank = 0;
       for (int o = 0; o < p.G; ++o) rank += gkey[o] > mine || (gkey[o] == mine && o < g);
+      if constexpr (!kExact)
+        if (mine) {
+          const float spread = __uint_as_float(kept[g]);
+          if (rank < p.keep) least = fminf(least, group_least(from_key(mine), spread));
+          else next = fmaxf(next, group_most(from_key(mine), spread));
+        }
       kept[g] = rank < p.keep;
-      if (rank < p.keep) last = mine < last ? mine : last;
-      else first = mine > first ? mine : first;
     }
     __syncwarp();
 #pragma unroll
@@ -258,11 +278,7 @@ __device__ bool choose(const TopkArgs &p, int64_t t, unsigned char *room) {
       const int e = i * 32 + lane;
       if (e < p.E && !kept[e / per]) key[i] = 0;
     }
-    if constexpr (!kExact) {
-      last = ~warp_max((U)~last);
-      first = warp_max(first);
-      near = by_score && first != 0 && groups_too_near(from_key(last), from_key(first), p.sigmoid);
-    }
+    if constexpr (!kExact) near = by_score && groups_near(least, next);
   }
 
   // the best of each lane, then of the warp, k times; the keys of those that are left out stay
@@ -430,18 +446,23 @@ __device__ __forceinline__ bool choose_packed(const TopkArgs &p, int64_t t, unsi
         b = max(b, min(a, c));
         a = max(a, c);
       }
-      gkey[g] = p.gtop == 2 && a ? to_key(half_sum(from_key(a), b ? from_key(b) : decltype(from_key(a))(0))) : a;
+      const float ca = a ? from_key(a) : 0.0f, cb = p.gtop == 2 && b ? from_key(b) : 0.0f;
+      gkey[g] = p.gtop == 2 && a ? to_key(half_sum(ca, cb)) : a;
+      kept[g] = __float_as_uint(fabsf(ca) + fabsf(cb));  // until it is ranked, by this lane
     }
     __syncwarp();
-    uint32_t last = kAll, first = 0;
+    float least = INFINITY, next = -INFINITY;  // as in choose()
     for (int g = lane; g < p.G; g += 32) {
       const uint32_t mine = gkey[g];
       int rank = 0;
 #pragma unroll 4
       for (int o = 0; o < p.G; ++o) rank += gkey[o] > mine || (gkey[o] == mine && o < g);
+      if (mine) {
+        const float spread = __uint_as_float(kept[g]);
+        if (rank < p.keep) least = fminf(least, group_least(from_key(mine), spread));
+        else next = fmaxf(next, group_most(from_key(mine), spread));
+      }
       kept[g] = rank < p.keep;
-      if (rank < p.keep) last = min(last, mine);
-      else first = max(first, mine);
     }
     __syncwarp();
 #pragma unroll
@@ -449,10 +470,7 @@ __device__ __forceinline__ bool choose_packed(const TopkArgs &p, int64_t t, unsi
       const int e = i * 32 + lane;
       if (e < p.E && !kept[e / per]) key[i] = 0;
     }
-    if (by_score) {
-      const float a = from_key(~warp_max(~last)), b = from_key(first = warp_max(first));
-      near = first != 0 && !(a - b > 0x1p-16f * (1.0f + fabsf(b)));  // the four s' errors, as groups_too_near
-    }
+    near = by_score && groups_near(least, next);
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) best = max(best, key[i]);
@@ -635,18 +653,18 @@ __device__ __forceinline__ unsigned long long exact_key(const TopkArgs &p, const
   return v == -INFINITY || b == -INFINITY ? 0ull : to_key(exact_score(v, p.sigmoid, most, total) + b);
 }
 // The groups to keep of a token: those surely above the border stay, the ones near it (up to eight) by their exact
-// scores.  gkey: the groups' f32 scores, a, b: those of the last one kept and the first one dropped.  False: too many.
+// scores.  gkey, spread: the groups' f32 scores and what they are made of, least, next: as in choose().  False: too many.
 template <typename T>
-__device__ __noinline__ bool settle_groups(const TopkArgs &p, const T *x, const uint32_t *gkey, uint32_t *kept, float a,
-                                           float b, float most, unsigned m8) {
+__device__ __noinline__ bool settle_groups(const TopkArgs &p, const T *x, const uint32_t *gkey, const float *spread,
+                                           uint32_t *kept, float least, float next, float most, unsigned m8) {
   const int sub = threadIdx.x % 8, per = p.E / p.G;
   const double total = p.sigmoid ? 1.0 : exact_total(x, p.E, most, m8);
-  const float tol = 0x1p-16f * (1.0f + fabsf(b));
   int sure = 0, n = 0, g_of = -1;
   unsigned long long of = 0;
   for (int g = 0; g < p.G; ++g) {
     const float s = from_key(gkey[g]);
-    const bool stays = kept[g], open = gkey[g] > kNoKey && !(stays ? s - b > tol : a - s > tol);
+    const bool stays = kept[g];
+    const bool open = gkey[g] > kNoKey && !(stays ? group_least(s, spread[g]) > next : group_most(s, spread[g]) < least);
     if (!open) {
       sure += stays;
       continue;
@@ -744,7 +762,7 @@ __device__ __noinline__ bool settle_list(const TopkArgs &p, const T *x, int &e, 
   return !one_ahead(p, x, listed, e9, el, from_key(last), kept, most, (float)total, m8);
 }
 
-__host__ __device__ constexpr int list_words(int E, int G) { return (E + E / 8 + 1 + 2 * G) | 1; }
+__host__ __device__ constexpr int list_words(int E, int G) { return (E + E / 8 + 1 + 3 * G) | 1; }
 
 template <typename T, bool Whole>
 __global__ void __launch_bounds__(kThreads, 8) topk_lists_kernel(const __grid_constant__ TopkArgs p) {
@@ -813,6 +831,7 @@ __global__ void __launch_bounds__(kThreads, 8) topk_lists_kernel(const __grid_co
   const unsigned m8 = 0xffu << (threadIdx.x & 24);
   // the token's keys (a word more for eight: lanes and groups begin on different banks), the groups' scores
   uint32_t *ckey = (uint32_t *)rooms + slot * list_words(p.E, p.G), *gkey = ckey + p.E + p.E / 8 + 1, *kept = gkey + p.G;
+  float *spread = (float *)(kept + p.G);
   const int per = p.E / p.G;
   if (grouped) {
     for (int e0 = first; e0 < p.E; e0 += 64) {
@@ -832,25 +851,28 @@ __global__ void __launch_bounds__(kThreads, 8) topk_lists_kernel(const __grid_co
         b = max(b, min(a, k));
         a = max(a, k);
       }
-      gkey[g] = p.gtop == 2 && a > kNoKey ? to_bits(half_sum(from_key(a), b > kNoKey ? from_key(b) : 0.0f)) : a;
+      const float ca = a > kNoKey ? from_key(a) : 0.0f, cb = p.gtop == 2 && b > kNoKey ? from_key(b) : 0.0f;
+      gkey[g] = p.gtop == 2 && a > kNoKey ? to_bits(half_sum(ca, cb)) : a;
+      spread[g] = fabsf(ca) + fabsf(cb);
     }
     __syncwarp();
-    uint32_t last = kAll, next = 0;  // the least group kept, the best one dropped
+    float least = INFINITY, next = -INFINITY;  // as in choose()
     for (int g = sub; g < p.G; g += 8) {
       const uint32_t k = gkey[g];
       int rank = 0;
 #pragma unroll 4
       for (int o = 0; o < p.G; ++o) rank += gkey[o] > k || (gkey[o] == k && o < g);
       kept[g] = rank < p.keep;
-      if (rank < p.keep) last = min(last, k);
-      else next = max(next, k);
+      if (k > kNoKey) {
+        if (rank < p.keep) least = fminf(least, group_least(from_key(k), spread[g]));
+        else next = fmaxf(next, group_most(from_key(k), spread[g]));
+      }
     }
     __syncwarp();  // settle_groups reads the flags of all lanes' groups
-    last = over<8>(kAll, last, [](uint32_t a, uint32_t b) { return min(a, b); });
-    next = over<8>(kAll, next, [](uint32_t a, uint32_t b) { return max(a, b); });
-    const float a = from_key(last), b = from_key(next);
-    if (by_score && next > kNoKey && !(a - b > 0x1p-16f * (1.0f + fabsf(b))))  // the four s' errors, as groups_too_near
-      lost = !settle_groups(p, x, gkey, kept, a, b, most, m8);
+    least = over<8>(kAll, least, [](float a, float b) { return fminf(a, b); });
+    next = over<8>(kAll, next, [](float a, float b) { return fmaxf(a, b); });
+    if (by_score && next > -INFINITY && !(least > next))
+      lost = !settle_groups(p, x, gkey, spread, kept, least, next, most, m8);
     __syncwarp();
   }
   uint32_t list[8], left = 0;  // the best beyond the list
