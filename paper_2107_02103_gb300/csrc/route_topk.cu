@@ -115,12 +115,14 @@ __device__ __forceinline__ A relative_score(A x, A most, bool sigm) {
 __device__ __forceinline__ float score_error(float range, bool sigm) {
   return sigm ? 0x1p-21f : 0x1p-18f + 0x1p-24f * fminf(range, 128.0f);
 }
+// And absolutely, for exponentials and scores below the normal range, which the hardware's instructions flush.
+constexpr float kFlushed = 0x1p-125f;
 // Two scores that f32 cannot order: x the logits, b the biases (c = s + b), range the larger |argument|.  Equal inputs
 // give equal scores; else s <= |c| + |b|, and the sum's own rounding is half an ulp.
 __device__ __forceinline__ bool too_near(float c0, float c1, float x0, float x1, float b0, float b1, float range,
                                          bool sigm) {
   if (x0 == x1 && b0 == b1) return false;
-  return !(c0 - c1 > (score_error(range, sigm) + 0x1p-23f) * (fabsf(c0) + fabsf(c1) + fabsf(b0) + fabsf(b1)));
+  return !(c0 - c1 > (score_error(range, sigm) + 0x1p-23f) * (fabsf(c0) + fabsf(c1) + fabsf(b0) + fabsf(b1)) + kFlushed);
 }
 // A group's score from its two best (0 in the place of none), at half its size: no sum leaves the type's range.
 template <typename A>
@@ -171,7 +173,7 @@ __device__ __forceinline__ bool packed_near(uint32_t k0, uint32_t k1, uint32_t m
                                             float range, bool sigm) {
   if (x0 == x1 && b0 == b1) return false;
   const float c0 = from_key(k0 & ~mask), c1 = from_key(k1 | mask);
-  return !(c0 - c1 > (rough_error(range, sigm) + 0x1p-23f) * (fabsf(c0) + fabsf(c1) + fabsf(b0) + fabsf(b1)));
+  return !(c0 - c1 > (rough_error(range, sigm) + 0x1p-23f) * (fabsf(c0) + fabsf(c1) + fabsf(b0) + fabsf(b1)) + kFlushed);
 }
 
 // The largest c that an expert whose f32 score is at most c1 may have: s = c - b is at most |c1| + bmost (the largest finite
@@ -179,7 +181,7 @@ __device__ __forceinline__ bool packed_near(uint32_t k0, uint32_t k1, uint32_t m
 __device__ __forceinline__ float reach_of(float c1, float bmost, bool sigm) {
   const float s = fminf(1.0f, fabsf(c1) + bmost);
   const float range = fmaxf(1.0f, 0.6932f * (float)(127 - (int)(__float_as_uint(s) >> 23)));
-  return c1 + rough_error(range, sigm) * s + 0x1p-22f * fabsf(c1);
+  return c1 + (rough_error(range, sigm) * s + 0x1p-22f * fabsf(c1) + kFlushed);
 }
 // The least c that a chosen one may have.
 __device__ __forceinline__ float least_of(float c, float x, float b, float most, bool sigm) {
@@ -718,7 +720,7 @@ __device__ __noinline__ bool one_ahead(const TopkArgs &p, const T *x, int e, int
     for (int o = 0; o < 8; ++o) out |= i == listed[o];
     if (out || (kept && !kept[i / per])) continue;
     const float c = bias ? score_of(v, p.sigmoid, most, total) + b : v;
-    const float tol = bias ? (score_error(most - v, p.sigmoid) + 0x1p-23f) * (fabsf(c) + fabsf(b)) : 0.0f;
+    const float tol = bias ? (score_error(most - v, p.sigmoid) + 0x1p-23f) * (fabsf(c) + fabsf(b)) + kFlushed : 0.0f;
     ahead |= !(low - c > tol);
   }
   return __any_sync(m8, ahead);

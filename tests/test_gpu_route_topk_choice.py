@@ -93,3 +93,22 @@ def test_equal_ones_at_the_border_before_a_larger_one(E, k, same, bias):
     # one bias for all: the order of the logits
     re, _ = reference(x.astype(np.float64), None, k, "sigmoid", 1, 1, 1, True, 1.0)
     assert np.array_equal(e.cpu().numpy(), re)
+
+
+@pytest.mark.parametrize("E,k", [(2, 1), (40, 1), (40, 3), (40, 12), (300, 40)])
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+def test_scores_below_the_normal_range(E, k, kind):
+    """Scores of 2^-126.5 and biases of 2^-127: no relative bound holds for what the hardware's exponential flushes."""
+    dpc = lib()
+    x = np.full((2, E), -104.0, np.float32)
+    b = np.zeros(E, np.float32)
+    x[:, 0], x[:, 1], b[0] = -97.0, -87.68, 2.0 ** -127
+    x[1, :2], b[1] = x[1, 1::-1], 0.0
+    if E > 2:  # what the others lie under
+        x[:, 2] = 0.0
+        b[2] = -np.inf
+    elif kind == "softmax":
+        pytest.skip("a softmax of these alone is near 1")
+    e, _ = dpc.dp_route_topk(torch.from_numpy(x).cuda(), k, bias=torch.from_numpy(b).cuda(), score=kind)
+    re, _ = reference(x.astype(np.float64), b.astype(np.float64), k, kind, 1, 1, 1, True, 1.0)
+    assert np.array_equal(e.cpu().numpy(), re)
