@@ -737,8 +737,10 @@ int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64
  *   w[t][j] = scale s_e, or with renorm scale s_e / sum_i s_ei (the bias only chooses)
  * Without a bias the experts are ordered by x itself (the groups by c all the same,
  * group_top 1: by x).  Equal ones go by the lowest index.  The choice is that of
- * exact arithmetic on the inputs: rounding does not move it (scores nearer than the
- * f32 error bounds are compared in f64; f64 rows in f64 alone).  An expert with
+ * exact arithmetic on the inputs as far as f64 tells scores apart: those nearer than
+ * the f32 error bounds are compared in f64 (f64 rows in f64 alone), and finite ones
+ * that are equal there go by the larger logit, so that a bias that is the same for all
+ * experts moves no order (groups equal there go by the lowest index).  An expert with
  * x = -inf or b = -inf is never chosen; a pair left without an expert gets -1 and
  * weight 0.  A NaN stands above all numbers, and its weights are NaN.
  *   logits [ntok][nexp];  bias [nexp];  expert, w [ntok][topk] outputs

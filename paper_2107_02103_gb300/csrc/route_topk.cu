@@ -63,6 +63,10 @@ __device__ __forceinline__ double from_key(unsigned long long k) {
   return __longlong_as_double((long long)((k >> 63) ? k & 0x7fffffffffffffffull : ~k));
 }
 
+// Whether equal scores c go by their logits: a sigmoid of 40 is 1 in f64, and c grows with x where the biases are equal.
+// NaN and +inf are equal ones.
+__device__ __forceinline__ bool goes_by_logit(unsigned long long key) { return key != 0 && key < 0xfff0000000000000ull; }
+
 // Reductions over the L lanes of a token (mask: those lanes).
 template <int L, typename V, typename F>
 __device__ __forceinline__ V over(unsigned mask, V v, F f) {
@@ -284,44 +288,95 @@ __device__ bool choose(const TopkArgs &p, int64_t t, unsigned char *room) {
   }
 
   // the best of each lane, then of the warp, k times; the keys of those that are left out stay
-  U best;
-  int at;
-  auto rescan = [&] {
-    best = 0;
-    at = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (key[i] > best) {
-        best = key[i];
-        at = i;
-      }
-  };
-  rescan();
   int se[S];
   U sk[S];
+  U best;
+  auto pick = [&](auto by_logit) {
+    constexpr bool kByLogit = decltype(by_logit)::value;
+    int at;
+    auto rescan = [&] {
+      best = 0;
+      at = 0;
 #pragma unroll
-  for (int s = 0; s < S; ++s) {
-    se[s] = -1;
-    sk[s] = 0;
-  }
-  const bool check = !kExact && p.bias;
-  for (int j = 0; j < p.k; ++j) {
-    const U m = warp_max(best);
-    if (m == 0) break;
-    const int e = __reduce_min_sync(kAll, best == m ? at * 32 + lane : INT_MAX);
-    if (e % 32 == lane) {
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (i == at) key[i] = 0;
-      rescan();
-    }
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-      if (j == s * 32 + lane) {
-        se[s] = e;
-        sk[s] = m;
+      for (int i = 0; i < N; ++i) {
+        bool first = key[i] > best;
+        if constexpr (kByLogit)
+          if (key[i] == best && bias && goes_by_logit(best)) first = to_acc(x[i * 32 + lane]) > to_acc(x[at * 32 + lane]);
+        if (first) {
+          best = key[i];
+          at = i;
+        }
       }
-  }
+    };
+    rescan();
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      se[s] = -1;
+      sk[s] = 0;
+    }
+    for (int j = 0; j < p.k; ++j) {
+      const U m = warp_max(best);
+      if (m == 0) break;
+      bool mine = best == m;
+      if constexpr (kByLogit)
+        if (bias && goes_by_logit(m) && __popc(__ballot_sync(kAll, mine)) > 1) {
+          const A xm = mine ? (A)to_acc(x[at * 32 + lane]) : none<A>(), largest = most_over<32>(kAll, xm);  // by all lanes
+          mine = mine && xm == largest;
+        }
+      const int e = __reduce_min_sync(kAll, mine ? at * 32 + lane : INT_MAX);
+      if (e % 32 == lane) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (i == at) key[i] = 0;
+        rescan();
+      }
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+        if (j == s * 32 + lane) {
+          se[s] = e;
+          sk[s] = m;
+        }
+    }
+  };
+  // Ties in f64 go by the logit in the same pass, but where 32 keys a lane leave no registers for it (8192 x 1024 f32 with 40
+  // chosen, a few tokens of which come here: 513 us with, 472 without): there in a second one.
+  pick(std::bool_constant<kExact && N <= 8>{});
+  if constexpr (kExact && N > 8)
+    if (bias) {  // equal scores of unequal logits, among the chosen ones or across their end
+      const U kl = of_last(p.k, sk);
+      const A xl = kl ? (A)to_acc(x[of_last(p.k, se)]) : A(0);
+      bool tie = false;
+#pragma unroll
+      for (int i = 0; i < N; ++i) tie |= goes_by_logit(kl) && key[i] == kl && (A)to_acc(x[i * 32 + lane]) != xl;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const int from = (lane + 1) % 32, s1 = s + 1 < S ? s + 1 : s;
+        const U k0 = __shfl_sync(kAll, sk[s], from), k1 = __shfl_sync(kAll, sk[s1], from);
+        const int e0 = __shfl_sync(kAll, se[s], from), e1 = __shfl_sync(kAll, se[s1], from);
+        const bool wrap = lane == 31;
+        const U nk = wrap ? (S > 1 ? k1 : 0) : k0;
+        if (goes_by_logit(sk[s]) && sk[s] == nk) tie |= to_acc(x[se[s]]) != to_acc(x[wrap ? e1 : e0]);
+      }
+      if (__any_sync(kAll, tie)) {
+        for (int j = 0; j < p.k; ++j) {
+          int e = se[0];
+          U m = sk[0];
+#pragma unroll
+          for (int s = 1; s < S; ++s)
+            if (j / 32 == s) {
+              e = se[s];
+              m = sk[s];
+            }
+          e = __shfl_sync(kAll, e, j % 32);
+          m = __shfl_sync(kAll, m, j % 32);
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            if (e == i * 32 + lane) key[i] = m;
+        }
+        pick(std::true_type{});
+      }
+    }
+  const bool check = !kExact && p.bias;
   A sx[S];
 #pragma unroll
   for (int s = 0; s < S; ++s) sx[s] = se[s] >= 0 ? (A)to_acc(x[se[s]]) : none<A>();
@@ -399,6 +454,13 @@ __device__ __noinline__ void choose_again(const TopkArgs &p, int64_t t, unsigned
   if (!choose<T, float, N, S>(p, t, room)) return;
   __syncwarp();
   choose<T, double, N, S>(p, t, room);
+}
+
+// What the eight lanes of a token could not settle, whose bounds are those of f32 scores: in f64 at once.
+template <typename T, int N>
+__device__ __noinline__ void choose_exact(const TopkArgs &p, int64_t t, unsigned char *room) {
+  __syncwarp();
+  choose<T, double, N, 1>(p, t, room);
 }
 
 // The first step for a token on a warp; true: not sure.
@@ -577,9 +639,10 @@ __device__ __forceinline__ bool choose_packed(const TopkArgs &p, int64_t t, unsi
 // Words of 8 bytes of a token's groups.
 __host__ __device__ constexpr int room_words(int E, int G) { return E + 3 * G; }
 
-// With 32 logits a lane four blocks an SM: at the 134 registers it else takes, 8192 x 1024 with 40 chosen took 506 us, not 461.
+// Four or eight blocks an SM: at the 134 registers that 32 logits a lane else take, 8192 x 1024 with 40 chosen took 506 us,
+// not 461; with fewer logits it is the later steps that would take more than 64.
 template <typename T, int N, int S>
-__global__ void __launch_bounds__(kThreads, N == 32 ? 4 : 1) topk_kernel(const __grid_constant__ TopkArgs p) {
+__global__ void __launch_bounds__(kThreads, N == 32 ? 4 : 8) topk_kernel(const __grid_constant__ TopkArgs p) {
   extern __shared__ __align__(16) unsigned char rooms[];
   const int64_t t = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
   if (t >= p.ntok) return;
@@ -737,14 +800,19 @@ __device__ __noinline__ bool settle_list(const TopkArgs &p, const T *x, int &e, 
   };
   const int e9 = left > kNoKey ? (int)(p.mask - (left & p.mask)) : -1;
   const unsigned long long key = exact(e), key9 = exact(e9);
-  const bool after9 = key9 > key || (key9 == key && key9 && e9 < e);
+  const float xe = e >= 0 ? to_acc(x[e]) : 0.0f, x9 = e9 >= 0 ? to_acc(x[e9]) : 0.0f;
+  auto before = [](unsigned long long k0, float x0, int e0, unsigned long long k1, float x1, int e1) {  // k1 not 0
+    return k0 > k1 || (k0 == k1 && (goes_by_logit(k1) && x0 != x1 ? x0 > x1 : e0 < e1));
+  };
+  const bool after9 = key9 && before(key9, x9, e9, key, xe, e);
   const int listed = e;
   int rank = after9;
 #pragma unroll
   for (int o = 0; o < 8; ++o) {
     const unsigned long long k = __shfl_sync(m8, key, o, 8);
     const int eo = __shfl_sync(m8, e, o, 8);
-    rank += k > key || (k == key && (k ? eo < e : o < sub));  // those without an expert stay in order at the end
+    const float xo = __shfl_sync(m8, xe, o, 8);
+    rank += k | key ? before(k, xo, eo, key, xe, e) : o < sub;  // those without an expert stay in order at the end
   }
   const int rank9 = 8 - __popc(__ballot_sync(m8, after9));
   unsigned long long last = rank9 == p.k - 1 ? key9 : 0ull;  // the k-th
@@ -977,8 +1045,8 @@ __global__ void __launch_bounds__(kThreads, 8) topk_lists_kernel(const __grid_co
     for (int i = 0; i < 4; ++i)
       if (unsure >> (8 * i) & 255) {
         const int64_t again = (int64_t)blockIdx.x * (kThreads / 8) + (threadIdx.x / 32) * 4 + i;
-        if (p.E <= 256) choose_again<T, 8, 1>(p, again, room);
-        else choose_again<T, 32, 1>(p, again, room);
+        if (p.E <= 256) choose_exact<T, 8>(p, again, room);
+        else choose_exact<T, 32>(p, again, room);
       }
   }
 }

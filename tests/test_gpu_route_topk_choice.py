@@ -112,3 +112,28 @@ def test_scores_below_the_normal_range(E, k, kind):
     e, _ = dpc.dp_route_topk(torch.from_numpy(x).cuda(), k, bias=torch.from_numpy(b).cuda(), score=kind)
     re, _ = reference(x.astype(np.float64), b.astype(np.float64), k, kind, 1, 1, 1, True, 1.0)
     assert np.array_equal(e.cpu().numpy(), re)
+
+
+@pytest.mark.parametrize("dtype", [torch.float64, torch.float32, torch.bfloat16, torch.float16], ids=["f64", "f32", "bf16", "f16"])
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,k,G,keep", [(2, 1, 1, 1), (30, 4, 1, 1), (30, 8, 1, 1), (30, 8, 5, 2), (128, 6, 8, 4), (128, 12, 1, 1), (128, 12, 8, 4), (1000, 50, 1, 1), (1000, 8, 10, 2)])
+@pytest.mark.parametrize("value", [0.0, 0.5, -3.0])
+def test_one_bias_for_all_keeps_the_order_of_the_logits(dtype, kind, E, k, G, keep, value):
+    """Sigmoids of 40 and 45 are both 1 in f64, a softmax's 1e-20 vanishes beside 0.5: a bias that is the same for all
+    changes no choice, nor do groups scored by their best one."""
+    dpc = lib()
+    r = np.random.default_rng(E + k)
+    x = torch.from_numpy(np.concatenate([r.uniform(-60, 60, (20, E)), r.uniform(35, 60, (20, E)), np.round(r.uniform(38, 44, (20, E)))])).to(dtype)
+    x[0, :2] = torch.tensor([40.0, 45.0]).to(dtype)
+    b = torch.full((E,), value, dtype=torch.float64 if dtype == torch.float64 else torch.float32, device="cuda")
+    kw = dict(score=kind, ngroup=G, keep_groups=keep, group_top=1)
+    e, w = dpc.dp_route_topk(x.cuda(), k, bias=b, **kw)
+    if G > 1:  # groups whose best scores are equal in f64 go by the lowest index: those that differ there
+        x64 = x.double()
+        s = torch.sigmoid(x64) if kind == "sigmoid" else torch.softmax(x64, 1)
+        best = (s.view(-1, G, E // G).amax(2) + b.double().cpu()[0]).sort(1).values
+        clear = (best.diff(dim=1) > 1e-10 * best[:, 1:].abs()).all(1).numpy()
+    else:
+        clear = np.ones(x.shape[0], bool)
+    re, _ = reference(x.double().numpy(), None, k, kind, G, keep, 1, True, 1.0)
+    assert np.array_equal(e.cpu().numpy()[clear], re[clear])
