@@ -751,8 +751,8 @@ int dp_route_plan(const int32_t *expert, int64_t ntok, int topk, int nexp, int64
  * Every sum has a fixed order.  ntok == 0 reads no device pointer.  Errors:
  * DP_ERR_NULL, DP_ERR_SHAPE (topk outside [1, min(64, nexp)], nexp not a multiple of
  * ngroup, fewer experts in keep_groups groups than topk, an unknown score or
- * group_top, a scale that is not finite, 2^31 or more pairs, alignment),
- * DP_ERR_UNSUPPORTED (nexp above 1024), DP_ERR_CUDA.
+ * group_top, a scale that is not finite as f32 (f64 rows: f64), 2^31 or more pairs,
+ * alignment), DP_ERR_UNSUPPORTED (nexp above 1024), DP_ERR_CUDA.
  */
 #define DP_SCORE_SOFTMAX 0
 #define DP_SCORE_SIGMOID 1
@@ -936,8 +936,8 @@ int dp_linear_mx4_f16(const uint8_t *xq, const uint8_t *sx, int64_t rows, int K,
  *         captured ones too, must not overlap on the GPU
  * Every sum has a fixed order.  ntok == 0: start and dW are zero.  Errors: DP_ERR_NULL,
  * DP_ERR_SHAPE (ntok < 0 or 2^31 - 4096 and more, nvocab < 1, H outside [1, 2^20], a scale
- * that is not finite, alignment, a short work buffer), DP_ERR_UNSUPPORTED (nvocab 2^24
- * and more), DP_ERR_CUDA.
+ * that is not finite as f32 (f64 rows: f64), alignment, a short work buffer),
+ * DP_ERR_UNSUPPORTED (nvocab 2^24 and more), DP_ERR_CUDA.
  */
 size_t dp_embed_plan_work_bytes(int64_t ntok, int nvocab);
 int dp_embed_plan(const int32_t *ids, int64_t ntok, int nvocab, int64_t *start, int32_t *src, void *work,

@@ -568,11 +568,12 @@ int embed_check(int64_t ntok, int nvocab, const char *who) {
   if (nvocab > kMaxVocab) return set_error(DP_ERR_UNSUPPORTED, "%s: nvocab = %d > %d", who, nvocab, kMaxVocab);
   return DP_OK;
 }
+template <typename A>
 int embed_check(int64_t ntok, int nvocab, int H, double scale, const char *who) {
   const int rc = embed_check(ntok, nvocab, who);
   if (rc) return rc;
   if (H < 1 || H > kMaxH) return set_error(DP_ERR_SHAPE, "%s: row length %d outside [1, 2^20]", who, H);
-  if (!std::isfinite(scale)) return set_error(DP_ERR_SHAPE, "%s: scale = %g", who, scale);
+  if (!scale_fits<A>(scale)) return set_error(DP_ERR_SHAPE, "%s: scale = %g", who, scale);
   return DP_OK;
 }
 
@@ -580,7 +581,7 @@ template <typename T>
 int embed_fwd(const T *W, const int32_t *ids, int64_t ntok, int nvocab, int H, double scale, const T *add, T *y,
               void *stream, const char *who) {
   clear_error();
-  const int rc = embed_check(ntok, nvocab, H, scale, who);
+  const int rc = embed_check<acc_t<T>>(ntok, nvocab, H, scale, who);
   if (rc || ntok == 0) return rc;
   if (!W || !ids || !y) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (!at_elements(W, add, y) || !at_elements(ids)) return misaligned(who);
@@ -603,7 +604,7 @@ int embed_grad(const T *dy, const int32_t *ids, const int64_t *start, const int3
                double scale, int accumulate, acc_t<T> *dW, void *work, size_t work_bytes, void *stream, const char *who) {
   using A = acc_t<T>;
   clear_error();
-  const int rc = embed_check(ntok, nvocab, H, scale, who);
+  const int rc = embed_check<A>(ntok, nvocab, H, scale, who);
   if (rc) return rc;
   if (!start || !dW || (ntok > 0 && (!dy || !ids || !src))) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (!at_elements(dy) || !at_elements(ids, src) || !at_elements(start) || !at_elements(dW)) return misaligned(who);

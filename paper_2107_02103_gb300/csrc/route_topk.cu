@@ -1239,7 +1239,7 @@ int topk(const T *x, const acc_t<T> *bias, int64_t ntok, int E, int k, int score
   if (keep < 1 || keep > G || keep * (E / G) < k)
     return set_error(DP_ERR_SHAPE, "%s: %d experts of %d groups of %d", who, k, keep, E / G);
   if (gtop != 1 && gtop != 2) return set_error(DP_ERR_SHAPE, "%s: group_top = %d", who, gtop);
-  if (!std::isfinite(scale)) return set_error(DP_ERR_SHAPE, "%s: scale = %g", who, scale);
+  if (!scale_fits<acc_t<T>>(scale)) return set_error(DP_ERR_SHAPE, "%s: scale = %g", who, scale);
   if (ntok == 0) return DP_OK;
   if (!x || !expert || !w) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (!at_elements(x, bias, w) || !at_elements(expert)) return misaligned(who);
@@ -1286,7 +1286,7 @@ int topk_grad(const T *x, const int32_t *expert, const acc_t<T> *dw, int64_t nto
   clear_error();
   const int rc = topk_check(ntok, E, k, score, who);
   if (rc) return rc;
-  if (!std::isfinite(scale)) return set_error(DP_ERR_SHAPE, "%s: scale = %g", who, scale);
+  if (!scale_fits<acc_t<T>>(scale)) return set_error(DP_ERR_SHAPE, "%s: scale = %g", who, scale);
   if (ntok == 0) return DP_OK;
   if (!x || !expert || !dw || !dx) return set_error(DP_ERR_NULL, "%s: NULL array", who);
   if (!at_elements(x, dx) || !at_elements(expert) || !at_elements(dw)) return misaligned(who);

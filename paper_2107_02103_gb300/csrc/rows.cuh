@@ -5,7 +5,9 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <cmath>
 #include <cstring>
+#include <limits>
 #include <type_traits>
 
 #include "dp_common.cuh"
@@ -182,6 +184,12 @@ bool at_elements(const E *...p) {
 }
 [[maybe_unused]] int misaligned(const char *who) {
   return set_error(DP_ERR_SHAPE, "%s: an array is not aligned to its elements", who);
+}
+
+// Whether a scale is a finite number in the type that the sums have.
+template <typename A>
+bool scale_fits(double scale) {
+  return std::fabs(scale) <= (double)std::numeric_limits<A>::max();
 }
 
 // The widest pack (in elements) that rows of H elements at these addresses allow: 16 bytes down to one element.
