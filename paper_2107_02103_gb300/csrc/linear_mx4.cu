@@ -266,10 +266,10 @@ __global__ void __launch_bounds__(kFewWarps * 32) linear_mx4_few_kernel(const Mx
 //   warps have waited for their codes.
 //   Eight epilogue warps (two per lane quadrant, half the columns each) finish a tile while the next one runs.
 // A block per SM walks the tiles; every wait is bounded, a block that gives up writes NaN and is counted.
-// Measured: 32,768 x 2048 x 4096 bf16 in 136 us (4.0 PFLOP/s, 2.1 times the measured bf16 rate), 8192 cubed 224 us (4.9),
+// Measured: 32,768 x 2048 x 4096 bf16 in 139 us (4.0 PFLOP/s, 2.1 times the measured bf16 rate), 8192 cubed 228 us (4.8),
 // 65,536 x 1600 x 240 f32 with four nets 37 us.  A stage of 8192 cubed takes 390 ns for 192 rows, 310 for 128, 280 for 64,
 // and with one of its four MMAs 355: what bounds it are the barriers between the roles.  Without the output 212 us, the wide
-// product 119.
+// product 119 (stages and these without the wait for a stage's turn before, which costs some 2 %).
 namespace mx4 {
 constexpr int kTM = 128, kKB = 256, kRowBytes = kKB / 2;
 constexpr int kEpiWarps = 8, kScaleWarps = 4, kScaleSets = 2;

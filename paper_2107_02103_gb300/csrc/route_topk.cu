@@ -658,8 +658,8 @@ __global__ void __launch_bounds__(kThreads, N == 32 ? 4 : 8) topk_kernel(const _
 // registers (19 exchanges) and merges them into its list of the best eight; three exchanges of lists between lanes leave
 // the token's in all of them, and lane j works out pair j.  Bound by instructions: 220 a token for the best eight of 128
 // logits, 65,536 tokens bf16 in 23 us (a warp a token as above, whose reductions, one an expert, leave most lanes idle: 550
-// and 42; a thread a token with its column in shared memory: 400, 72), 470 with scores, a bias and four of eight groups, 46
-// us (103, 115).  Eight blocks an SM at 64 registers: with five at 96 it took 54.
+// and 42; a thread a token with its column in shared memory: 400, 72), 480 with scores, a bias and four of eight groups, 46
+// us (103, 115).  Eight blocks an SM at 64 registers, some 30 of a thread's spilled: with five at 96 it took 54.
 constexpr int kList = 8;
 __device__ __forceinline__ void exchange(uint32_t &a, uint32_t &b) {
   const uint32_t most = max(a, b);
