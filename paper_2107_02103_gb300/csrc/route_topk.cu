@@ -5,11 +5,12 @@
 // Without a bias the experts are ordered by x itself, which has the order of s and no rounding.  Scores that are equal in
 // f64 go by the larger logit, equal logits by the lowest index, a NaN stands above all numbers, an expert with x = -inf or
 // b = -inf is never chosen (-1, weight 0).
-// The choice is that of exact arithmetic as far as f64 has it, in up to three steps: first on f32 scores cut to leave room for the expert's index
-// in the same word (one integer is compared and moved, and no two are equal); a token in which two neighbours of the chosen
-// ones, the last of them and any that is left out (whose error may be far larger than a neighbour's: an s near 1 that a
-// bias cancels), or the last group kept and the first one dropped are nearer than their error bounds is settled in f64 on
-// those in question (eight lanes a token), or done again on whole f32 scores and then in f64 (a warp a token).
+// The choice is that of exact arithmetic as far as f64 has it, in up to three steps: first on f32 scores cut to leave
+// room for the expert's index in the same word (one integer is compared and moved, and no two are equal); a token in
+// which two neighbours of the chosen ones, the last of them and any that is left out (whose error may be far larger
+// than a neighbour's: an s near 1 that a bias cancels), or the last group kept and the first one dropped are nearer
+// than their error bounds is settled in f64 on those in question (eight lanes a token), or done again on whole f32
+// scores and then in f64 (a warp a token).
 // Backward, the choice held fixed, n_j = s_ej / sum_i s_ei:
 //   renormalised  g_j = scale n_j (dw_j - sum_i n_i dw_i)   softmax dx_ej += g_j,  sigmoid dx_ej += g_j (1 - s_ej)
 //   plain         softmax dx_e = sum_(j: e_j = e) g_j - s_e sum_j g_j with g_j = scale dw_j s_ej
